@@ -59,7 +59,7 @@ typedef enum {
 } hift_status;
 
 typedef enum { HIFT_BOTTOM2UP = 0, HIFT_TOP2DOWN = 1, HIFT_RANDOM = 2 } hift_strategy;
-typedef enum { HIFT_ADAMW = 0, HIFT_ADAGRAD = 1, HIFT_SGD = 2, HIFT_ADAFACTOR = 3 } hift_opt_kind;
+typedef enum { HIFT_ADAMW = 0, HIFT_ADAGRAD = 1, HIFT_SGD = 2, HIFT_ADAFACTOR = 3, HIFT_MUON = 4 } hift_opt_kind;
 enum { HIFT_ARCH_PRELN_DECODER = 0, HIFT_ARCH_POSTLN_ENCODER = 1, HIFT_ARCH_RMS_ROPE_DECODER = 2 };
 enum { HIFT_F32 = 0, HIFT_BF16 = 1 };
 enum { HIFT_KIND_MATRIX = 0, HIFT_KIND_GAIN = 1, HIFT_KIND_BIAS = 2 };
@@ -507,6 +507,61 @@ hift_status hift_kernel_norm_fwd(int32_t dtype, int32_t rms, int64_t rows, int32
 hift_status hift_kernel_cross_entropy(int32_t dtype, int64_t rows, int32_t V, void* logits,
                                       const int32_t* labels, float* row_loss_scratch,
                                       float* loss_out, void* stream);
+
+/* Log probabilities of given tokens, entropy of each row and its most probable alternatives: what a loss on scored tokens (policy
+ * gradients, preference losses, distillation of sampled answers) is formed from, and what a fine-tuned model would answer.
+ * logits: device [rows, V], rows ld >= V apart (any alignment of whole elements); scale > 0: the reciprocal of the temperature.  With
+ * z = scale * logits, m a row's largest z and S its sum of exp(z - m):
+ *   logp[r] = (z[y] - m) - ln S for the row's target y = targets[r]; 0 for a row without one (a target outside [0, V))
+ *   entropy[r] = - sum p ln p in nats
+ *   stats[r] = (m, ln S): what the gradient needs
+ *   top_ids[r], top_logp[r]: the `top` (0 .. 32, at most V) largest logits' ids and log probabilities, in falling order; of equal logits the
+ *   lowest id comes first, -0 equals 0, NaN precedes everything.
+ * Entries of -inf (masked tokens) have probability 0.  A row of nothing else: logp and top_logp -inf, entropy 0, stats (0, -inf).  A NaN or
+ * +inf makes its row's numbers NaN.  targets / logp, entropy, stats: device, fp32 (targets int32), NULL where not wanted; top_logp,
+ * top_ids: device [rows, top].  Sums in fp32 whatever dtype is. */
+hift_status hift_kernel_token_logprob(int32_t dtype, int64_t rows, int32_t V, int64_t ld, const void* logits, const int32_t* targets,
+                                      float scale, int32_t top, float* logp, float* entropy, float* stats, float* top_logp,
+                                      int32_t* top_ids, void* stream);
+/* The gradient with respect to the logits of sum_r d_logp[r] logp[r] + d_entropy[r] entropy[r]: row r, column j receives
+ *   scale (d_logp (1(j = y) - p_j) - d_entropy p_j (ln p_j + entropy))
+ * (d_logp counts for rows with a target only; the alternatives have no gradient).  stats, entropy: as the forward call left them (entropy may
+ * be NULL where d_entropy is); d_logp, d_entropy: device fp32 [rows], NULL for zeros.  dlogits: device [rows, V] of the logits' type, rows
+ * ldd apart; may be the logits themselves (ldd = ld).  Masked entries and rows of nothing else receive 0; columns from V on are not written. */
+hift_status hift_kernel_token_logprob_bwd(int32_t dtype, int64_t rows, int32_t V, int64_t ld, const void* logits, const int32_t* targets,
+                                          float scale, const float* stats, const float* entropy, const float* d_logp,
+                                          const float* d_entropy, int64_t ldd, void* dlogits, void* stream);
+
+/* Orthogonalisation of matrices by Newton-Schulz steps: X = src / max(|src|_F, eps); `steps` (1 .. 16) times
+ * X <- a X + b (X X^T) X + c (X X^T)^2 X; dst = X.  src, dst: device, rows ld_src / ld_dst >= cols apart, of type src_dtype / dst_dtype (HIFT_F32
+ * or HIFT_BF16); dst may be src where the types are the same.  Products carry 22 bits of every factor and fp32 sums.  A src of zeros gives
+ * zeros; one that holds NaN or infinities gives NaN.  Matrices of one call share launches, so hand in together what is there together.
+ * Either side at most 65536 long; a matrix with a side of 0 is skipped.  HIFT_EINVAL also for a < 1 (small singular values would not grow)
+ * and for coefficients under which the singular values, all in [0, 1] at first, could leave fp16's range.
+ * workspace: device, 16-byte aligned, hift_kernel_orthogonalize_bytes (which reads rows and cols only), free again once the call's work on
+ * the stream is done.  No atomics: the same call gives the same bits. */
+typedef struct {
+  int64_t rows, cols;
+  const void* src; int64_t ld_src;
+  void* dst; int64_t ld_dst;
+} hift_matrix;
+hift_status hift_kernel_orthogonalize_bytes(int32_t count, const hift_matrix* matrices, size_t* bytes);
+hift_status hift_kernel_orthogonalize(int32_t src_dtype, int32_t dst_dtype, int32_t count, const hift_matrix* matrices, int32_t steps,
+                                      double a, double b, double c, float eps, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The update of HIFT_MUON for matrices (fp32, contiguous [rows, cols]; compute_copy bf16 or NULL): with mu = opt->momentum
+ *   momentum <- mu momentum + grad;   O = orthogonalised (grad + mu momentum): five steps of (3.4445, -4.7750, 2.0315), eps 1e-7
+ *   master <- (1 - lr weight_decay) master - lr 0.2 sqrt(max(rows, cols)) O;   compute_copy <- master rounded
+ * (the factor gives the step the size that AdamW's has at the same rate).  Uses kind, lr, momentum and weight_decay of opt.  Work space as
+ * for hift_kernel_orthogonalize. */
+typedef struct {
+  int64_t rows, cols;
+  float* master; const float* grad; float* momentum;
+  void* compute_copy;
+} hift_muon_matrix;
+hift_status hift_kernel_muon_bytes(int32_t count, const hift_muon_matrix* matrices, size_t* bytes);
+hift_status hift_kernel_muon(const hift_opt* opt, int32_t count, const hift_muon_matrix* matrices, void* workspace, size_t workspace_bytes,
+                             void* stream);
 
 #ifdef __cplusplus
 }

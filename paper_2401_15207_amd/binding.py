@@ -17,7 +17,7 @@ if not os.path.exists(LIB_PATH):
 lib = C.CDLL(LIB_PATH)
 
 STRATEGY = {"bottom2up": 0, "top2down": 1, "random": 2}
-OPT_KIND = {"adamw": 0, "adagrad": 1, "sgd": 2, "adafactor": 3}
+OPT_KIND = {"adamw": 0, "adagrad": 1, "sgd": 2, "adafactor": 3, "muon": 4}
 
 
 class HiftError(RuntimeError):
@@ -55,6 +55,15 @@ class Batch(C.Structure):
 class TensorInfo(C.Structure):
     _fields_ = [("name", C.c_char * 32), ("unit", C.c_int32), ("kind", C.c_int32), ("offset", C.c_int64),
                 ("rows", C.c_int64), ("cols", C.c_int64)]
+
+
+class Matrix(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int64), ("src", C.c_void_p), ("ld_src", C.c_int64), ("dst", C.c_void_p), ("ld_dst", C.c_int64)]
+
+
+class MuonMatrix(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int64), ("master", C.c_void_p), ("grad", C.c_void_p), ("momentum", C.c_void_p),
+                ("compute_copy", C.c_void_p)]
 
 
 lib.hift_last_error.restype = C.c_char_p
@@ -116,6 +125,12 @@ _SIGS = {
     "hift_kernel_attention_fwd": [_i32, _i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp],
     "hift_kernel_attention_bwd": [_i32, _i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp],
     "hift_kernel_cross_entropy": [_i32, _i64, _i32, _vp, _vp, _vp, _vp, _vp],
+    "hift_kernel_token_logprob": [_i32, _i64, _i32, _i64, _vp, _vp, C.c_float, _i32, _vp, _vp, _vp, _vp, _vp, _vp],
+    "hift_kernel_token_logprob_bwd": [_i32, _i64, _i32, _i64, _vp, _vp, C.c_float, _vp, _vp, _vp, _vp, _i64, _vp, _vp],
+    "hift_kernel_orthogonalize_bytes": [_i32, _P(Matrix), _P(_sz)],
+    "hift_kernel_orthogonalize": [_i32, _i32, _i32, _P(Matrix), _i32, C.c_double, C.c_double, C.c_double, C.c_float, _vp, _sz, _vp],
+    "hift_kernel_muon_bytes": [_i32, _P(MuonMatrix), _P(_sz)],
+    "hift_kernel_muon": [_P(Opt), _i32, _P(MuonMatrix), _vp, _sz, _vp],
 }
 for _n, _a in _SIGS.items():
     getattr(lib, _n).argtypes = _a
@@ -312,6 +327,114 @@ def kernel_cross_entropy(dtype, rows, V, logits, labels, row_loss, loss_out, str
     import torch
     st = (stream or torch.cuda.current_stream()).cuda_stream
     _check(lib.hift_kernel_cross_entropy(dtype, rows, V, _ptr(logits), _ptr(labels), _ptr(row_loss), _ptr(loss_out), st))
+
+
+def _dtype_code(t) -> int:
+    codes = {torch.float32: 0, torch.bfloat16: 1}
+    if t.dtype not in codes:
+        raise ValueError(f"float32 or bfloat16 expected, not {t.dtype}")
+    return codes[t.dtype]
+
+
+def _rows_of(name, t, dtype=None, shape=None, contiguous=False):
+    """t as a device matrix whose rows are contiguous; returns the distance between them."""
+    if not t.is_cuda or t.dim() != 2 or (dtype is not None and t.dtype != dtype) or (shape is not None and tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"{name}: a device matrix{'' if shape is None else ' ' + str(tuple(shape))}{'' if dtype is None else f' of {dtype}'} "
+                         f"expected, not {tuple(t.shape)} of {t.dtype} on {t.device}")
+    ld = t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
+    if (t.shape[1] > 1 and t.stride(1) != 1) or ld < t.shape[1] or (contiguous and not t.is_contiguous()):
+        raise ValueError(f"{name}: rows have to be contiguous{' and to follow each other' if contiguous else ''}")
+    return ld
+
+
+def _row_values(name, t, rows, dtype=None, cols=1):
+    if t is None:
+        return None
+    if not t.is_cuda or not t.is_contiguous() or t.numel() != rows * cols or t.dtype != (dtype or torch.float32):
+        raise ValueError(f"{name}: {rows * cols} contiguous values of {dtype or torch.float32} on the device expected")
+    return t.data_ptr()
+
+
+def kernel_token_logprob(logits, vocab, targets, scale, logp, entropy, stats, top_logp=None, top_ids=None, stream=None):
+    """logits: [rows, >= vocab] (rows contiguous, any distance apart); the outputs (fp32; top_ids int32) may be None where they are not wanted,
+    targets (int32) where logp is; the number of alternatives is top_ids' second size."""
+    st = (stream or torch.cuda.current_stream()).cuda_stream
+    ld, rows = _rows_of("logits", logits), logits.shape[0]
+    if vocab > logits.shape[1]:
+        raise ValueError(f"vocab {vocab}, but rows hold {logits.shape[1]}")
+    top = 0 if top_ids is None else top_ids.shape[1]
+    _check(lib.hift_kernel_token_logprob(_dtype_code(logits), rows, vocab, ld, _ptr(logits), _row_values("targets", targets, rows, torch.int32), scale, top,
+                                         _row_values("logp", logp, rows), _row_values("entropy", entropy, rows), _row_values("stats", stats, rows, cols=2),
+                                         _row_values("top_logp", top_logp, rows, cols=top) if top else None,
+                                         _row_values("top_ids", top_ids, rows, torch.int32, top) if top else None, st))
+
+
+def kernel_token_logprob_bwd(logits, vocab, targets, scale, stats, entropy, d_logp, d_entropy, dlogits, stream=None):
+    """dlogits: like logits, or logits itself; entropy, d_logp, d_entropy may be None (see hift.h)."""
+    st = (stream or torch.cuda.current_stream()).cuda_stream
+    ld, ldd, rows = _rows_of("logits", logits), _rows_of("dlogits", dlogits, logits.dtype), logits.shape[0]
+    if vocab > logits.shape[1] or vocab > dlogits.shape[1] or dlogits.shape[0] != rows:
+        raise ValueError(f"vocab {vocab}, but logits are {tuple(logits.shape)} and dlogits {tuple(dlogits.shape)}")
+    _check(lib.hift_kernel_token_logprob_bwd(_dtype_code(logits), rows, vocab, ld, _ptr(logits), _row_values("targets", targets, rows, torch.int32), scale,
+                                             _row_values("stats", stats, rows, cols=2), _row_values("entropy", entropy, rows),
+                                             _row_values("d_logp", d_logp, rows), _row_values("d_entropy", d_entropy, rows), ldd, _ptr(dlogits), st))
+
+
+def _workspace(query, n, arr, workspace, stream):
+    """The caller's work space, or one from torch's allocator that it keeps until the stream is done with it."""
+    if workspace is None:
+        b = _sz()
+        _check(query(n, arr, C.byref(b)))
+        workspace = torch.empty(max(b.value, 16), dtype=torch.uint8, device="cuda")
+        if stream is not None:
+            stream.wait_stream(torch.cuda.current_stream())   # the memory may still be in use there
+            workspace.record_stream(stream)
+    return workspace, workspace.numel() * workspace.element_size()
+
+
+def kernel_orthogonalize_bytes(shapes) -> int:
+    """Work space of kernel_orthogonalize and kernel_muon for matrices of these shapes."""
+    arr = (Matrix * max(len(shapes), 1))(*[Matrix(r, c) for r, c in shapes])
+    b = _sz()
+    _check(lib.hift_kernel_orthogonalize_bytes(len(shapes), arr, C.byref(b)))
+    return b.value
+
+
+MUON_COEFFICIENTS = (3.4445, -4.7750, 2.0315)
+
+
+def kernel_orthogonalize(src, dst, steps=5, coefficients=MUON_COEFFICIENTS, eps=1e-7, workspace=None, stream=None):
+    """src, dst: lists of device matrices of the same shapes, all of one type each (float32 or bfloat16); dst may be src."""
+    st = (stream or torch.cuda.current_stream()).cuda_stream
+    if len(src) != len(dst):
+        raise ValueError(f"{len(src)} matrices, {len(dst)} results")
+    if not src:
+        return
+    arr = (Matrix * len(src))()
+    for i, (s, d) in enumerate(zip(src, dst)):
+        lds, ldd = _rows_of(f"src[{i}]", s, src[0].dtype), _rows_of(f"dst[{i}]", d, dst[0].dtype, s.shape)
+        arr[i] = Matrix(s.shape[0], s.shape[1], s.data_ptr(), lds, d.data_ptr(), ldd)
+    ws, n = _workspace(lib.hift_kernel_orthogonalize_bytes, len(src), arr, workspace, stream)
+    _check(lib.hift_kernel_orthogonalize(_dtype_code(src[0]), _dtype_code(dst[0]), len(src), arr, steps, *coefficients, eps, _ptr(ws), n, st))
+
+
+def kernel_muon(opt: dict, master, grad, momentum, compute_copy=None, workspace=None, stream=None):
+    """The update of matrices by HIFT_MUON: lists of contiguous float32 matrices, and of their bfloat16 copies (or None)."""
+    st = (stream or torch.cuda.current_stream()).cuda_stream
+    n = len(master)
+    if len(grad) != n or len(momentum) != n or (compute_copy is not None and len(compute_copy) != n):
+        raise ValueError("as many gradients, momentum buffers and copies as matrices expected")
+    arr = (MuonMatrix * max(n, 1))()
+    for i in range(n):
+        w, cc = master[i], None if compute_copy is None else compute_copy[i]
+        for name, t, dt in (("master", w, torch.float32), ("grad", grad[i], torch.float32), ("momentum", momentum[i], torch.float32),
+                            ("compute_copy", cc, torch.bfloat16)):
+            if t is not None:
+                _rows_of(f"{name}[{i}]", t, dt, w.shape, contiguous=True)
+        arr[i] = MuonMatrix(w.shape[0], w.shape[1], _ptr(w), _ptr(grad[i]), _ptr(momentum[i]), _ptr(cc))
+    o = make_opt(opt)
+    ws, nb = _workspace(lib.hift_kernel_muon_bytes, n, arr, workspace, stream)
+    _check(lib.hift_kernel_muon(C.byref(o), n, arr, _ptr(ws), nb, st))
 
 
 def _hip_runtime():

@@ -166,6 +166,16 @@ hipError_t cross_entropy_count(int64_t rows, const int32_t* labels, float* row_l
 hipError_t cross_entropy_rows(int dt, int64_t rows, int V, int64_t ld, void* logits, const int32_t* labels, float* row_loss,
                               hipStream_t st);
 hipError_t cross_entropy_mean(int64_t rows, const float* row_loss, float* loss_out, hipStream_t st);
+constexpr int LOGPROB_TOP_MAX = 32;
+constexpr int64_t LOGPROB_ROWS_MAX = int64_t(1) << 22;
+// Log probabilities of given tokens, the rows' entropies, the `top` most probable entries and what the gradient needs (logprob.hip).
+// targets (outside [0, V): none, logp 0), logp, entropy, stats [rows, 2], top_logp / top_ids [rows, top]: each may be null where it is not wanted.
+hipError_t token_logprob(int dt, int64_t rows, int V, int64_t ld, const void* logits, const int32_t* targets, float scale, int top, float* logp,
+                         float* entropy, float* stats, float* top_logp, int32_t* top_ids, hipStream_t st);
+// dlogits = sum over the rows' gradients d_logp and d_entropy (either may be null: 0); may be the logits themselves (with ldd = ld).  Entries
+// [V, zero_to) of a row are set to 0.
+hipError_t token_logprob_bwd(int dt, int64_t rows, int V, int64_t ld, const void* logits, const int32_t* targets, float scale, const float* stats,
+                             const float* entropy, const float* d_logp, const float* d_entropy, int64_t ldd, void* dlogits, int zero_to, hipStream_t st);
 // g_tok[v, :] = (add ? g_tok[v, :] : as zeroed by the caller) + sum over positions t holding token v of dx[t, :],
 // in position order (no atomics: the first position holding a token does its row);  g_pos[s, :] = sum_b dx[b*S+s, :].
 // stamps (optional, one per token): those of tokens that occur are set to `stamp`.
@@ -219,5 +229,25 @@ size_t adafactor_work_floats(int64_t rows, int64_t cols);
 hipError_t adafactor_update(double lr, double wd, bool decay, int64_t t, int64_t rows, int64_t cols, float* master,
                             const float* grad, float* fac, float* work, void* compute_copy /* bf16 or null */,
                             hipStream_t st);
+
+// Newton-Schulz orthogonalisation of matrices, and the update of weights by it (muon.hip).  An item with a master: src is the gradient
+// (fp32, contiguous), momentum, master and copy (bf16, or null) are [rows, cols], contiguous; else dst receives the result.
+struct NsItem {
+  int64_t rows, cols;
+  const void* src; int64_t ld_src;
+  void* dst; int64_t ld_dst;
+  float *momentum, *master;
+  void* copy;
+};
+struct NsRun {
+  int steps;
+  double co[3];  // a, b, c of a step
+  float eps;
+  double lr;     // the update's
+  float mu, decay;
+};
+bool ns_coefficients_hold(const double (&co)[3], int steps);  // the singular values stay in range
+size_t ns_workspace(const NsItem* items, int count);          // bytes; newton_schulz wants them 16-byte aligned
+hipError_t newton_schulz(const NsItem* items, int count, int dt_src, int dt_dst, const NsRun& run, void* workspace, hipStream_t st);
 
 }  // namespace hift

@@ -10,12 +10,14 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <new>
 #include <string>
 #include <vector>
 
 #include "../../include/hift.h"
 #include "copy_parts.h"
 #include "kernels.h"
+#include "ns_plan.h"
 #include "state_slots.h"
 
 using namespace hift;
@@ -200,6 +202,11 @@ hift_status check_opt(const hift_opt* o) {
   if (o->kind < 0 || o->kind > 3) return fail(HIFT_EINVAL, "optimizer kind %d unknown", o->kind);
   if (o->momentum < 0.0) return fail(HIFT_EINVAL, "momentum must be >= 0");
   return HIFT_OK;
+}
+
+// The steps of HIFT_MUON: Newton-Schulz of degree five with the coefficients of Jordan et al. 2024.
+NsRun muon_run(const hift_opt& o) {
+  return NsRun{5, {3.4445, -4.7750, 2.0315}, 1e-7f, o.lr, (float)o.momentum, (float)(1.0 - o.lr * o.weight_decay)};
 }
 
 inline size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -1481,6 +1488,42 @@ hift_status unit_span(const hift_model* M, int ulo, int uhi, int64_t* off, int64
 
 }  // namespace
 
+// ---- arguments of the operators on lists of matrices ------------------------------------------
+namespace {
+constexpr int32_t NS_COUNT_MAX = 1 << 16;
+// items from the caller's array, checked: item(i, it) fills one
+template <class F>
+hift_status ns_items(int32_t count, const void* matrices, std::vector<NsItem>* items, F item) {
+  if (count < 0 || count > NS_COUNT_MAX) return fail(HIFT_EINVAL, "%d matrices", count);
+  if (count > 0 && !matrices) return fail(HIFT_EINVAL, "matrices are null");
+  try {
+    items->assign(count, NsItem{});
+  } catch (const std::bad_alloc&) {
+    return fail(HIFT_ENOMEM, "no host memory for %d matrices", count);
+  }
+  for (int32_t i = 0; i < count; ++i) {
+    NsItem& it = (*items)[i];
+    item(i, it);
+    if (it.rows < 0 || it.cols < 0 || it.rows > NS_SIDE_MAX || it.cols > NS_SIDE_MAX)
+      return fail(HIFT_EINVAL, "matrix %d is %lld x %lld: either side is at most %lld", i, (long long)it.rows, (long long)it.cols, (long long)NS_SIDE_MAX);
+  }
+  return HIFT_OK;
+}
+void ortho_item(const hift_matrix& m, NsItem& it) {
+  it.rows = m.rows; it.cols = m.cols; it.src = m.src; it.ld_src = m.ld_src; it.dst = m.dst; it.ld_dst = m.ld_dst;
+}
+void muon_item(const hift_muon_matrix& m, NsItem& it) {
+  it.rows = m.rows; it.cols = m.cols; it.src = m.grad; it.ld_src = m.cols; it.momentum = m.momentum; it.master = m.master; it.copy = m.compute_copy;
+}
+hift_status check_ns_workspace(const std::vector<NsItem>& items, const void* workspace, size_t bytes) {
+  const size_t need = ns_workspace(items.data(), (int)items.size());
+  if (need == 0) return HIFT_OK;
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15)) return fail(HIFT_EINVAL, "work space must be non-null and 16-byte aligned");
+  if (bytes < need) return fail(HIFT_ENOMEM, "work space holds %zu bytes, %zu are needed", bytes, need);
+  return HIFT_OK;
+}
+}  // namespace
+
 // ==========================================================================================
 // C ABI
 // ==========================================================================================
@@ -2543,6 +2586,104 @@ hift_status hift_kernel_cross_entropy(int32_t dtype, int64_t rows, int32_t V, vo
   if (rows < 0 || V < 1) return fail(HIFT_EINVAL, "bad shape");
   HIP_TRY(cross_entropy(dtype == HIFT_BF16 ? DT_BF16 : DT_F32, rows, V, logits, labels, row_loss_scratch, loss_out,
                         (hipStream_t)stream));
+  return HIFT_OK;
+}
+
+namespace {
+hift_status check_logits(int32_t dtype, int64_t rows, int32_t V, int64_t ld, const void* logits, float scale) {
+  if (dtype != HIFT_F32 && dtype != HIFT_BF16) return fail(HIFT_EINVAL, "dtype unknown");
+  if (rows < 0 || V < 1 || ld < V) return fail(HIFT_EINVAL, "bad shape: %lld rows of %d entries, %lld apart", (long long)rows, V, (long long)ld);
+  if (rows > LOGPROB_ROWS_MAX) return fail(HIFT_EINVAL, "more than %lld rows in one call", (long long)LOGPROB_ROWS_MAX);
+  if (!(scale > 0.f) || std::isinf(scale)) return fail(HIFT_EINVAL, "scale must be positive and finite");
+  if (rows > 0 && !logits) return fail(HIFT_EINVAL, "logits are null");
+  if (reinterpret_cast<uintptr_t>(logits) % (dtype == HIFT_BF16 ? 2 : 4)) return fail(HIFT_EINVAL, "logits do not lie on whole elements");
+  return HIFT_OK;
+}
+}  // namespace
+
+hift_status hift_kernel_token_logprob(int32_t dtype, int64_t rows, int32_t V, int64_t ld, const void* logits, const int32_t* targets,
+                                      float scale, int32_t top, float* logp, float* entropy, float* stats, float* top_logp,
+                                      int32_t* top_ids, void* stream) {
+  ST_TRY(check_logits(dtype, rows, V, ld, logits, scale));
+  if (logp && !targets) return fail(HIFT_EINVAL, "log probabilities need targets");
+  if (top < 0 || top > LOGPROB_TOP_MAX || top > V) return fail(HIFT_EINVAL, "top must be in [0, min(%d, V)]", LOGPROB_TOP_MAX);
+  if (top > 0 && rows > 0 && (!top_logp || !top_ids)) return fail(HIFT_EINVAL, "top needs top_logp and top_ids");
+  HIP_TRY(token_logprob(dtype == HIFT_BF16 ? DT_BF16 : DT_F32, rows, V, ld, logits, targets, scale, top, logp, entropy, stats, top_logp, top_ids,
+                        (hipStream_t)stream));
+  return HIFT_OK;
+}
+
+hift_status hift_kernel_token_logprob_bwd(int32_t dtype, int64_t rows, int32_t V, int64_t ld, const void* logits, const int32_t* targets,
+                                          float scale, const float* stats, const float* entropy, const float* d_logp,
+                                          const float* d_entropy, int64_t ldd, void* dlogits, void* stream) {
+  ST_TRY(check_logits(dtype, rows, V, ld, logits, scale));
+  if (ldd < V) return fail(HIFT_EINVAL, "rows of the gradient are %lld apart and %d long", (long long)ldd, V);
+  if (rows > 0 && (!stats || !dlogits)) return fail(HIFT_EINVAL, "stats or dlogits null");
+  if (d_logp && !targets) return fail(HIFT_EINVAL, "d_logp needs targets");
+  if (d_entropy && !entropy) return fail(HIFT_EINVAL, "d_entropy needs the entropies");
+  if (reinterpret_cast<uintptr_t>(dlogits) % (dtype == HIFT_BF16 ? 2 : 4)) return fail(HIFT_EINVAL, "dlogits do not lie on whole elements");
+  if (dlogits == logits && ldd != ld) return fail(HIFT_EINVAL, "in place the rows lie where they were (ldd = ld)");
+  HIP_TRY(token_logprob_bwd(dtype == HIFT_BF16 ? DT_BF16 : DT_F32, rows, V, ld, logits, targets, scale, stats, entropy, d_logp, d_entropy, ldd, dlogits,
+                            V, (hipStream_t)stream));
+  return HIFT_OK;
+}
+
+hift_status hift_kernel_orthogonalize_bytes(int32_t count, const hift_matrix* matrices, size_t* bytes) {
+  if (!bytes) return fail(HIFT_EINVAL, "bytes is null");
+  std::vector<NsItem> items;
+  ST_TRY(ns_items(count, matrices, &items, [&](int i, NsItem& it) { ortho_item(matrices[i], it); }));
+  *bytes = ns_workspace(items.data(), count);
+  return HIFT_OK;
+}
+
+hift_status hift_kernel_orthogonalize(int32_t src_dtype, int32_t dst_dtype, int32_t count, const hift_matrix* matrices, int32_t steps,
+                                      double a, double b, double c, float eps, void* workspace, size_t workspace_bytes, void* stream) {
+  if ((src_dtype != HIFT_F32 && src_dtype != HIFT_BF16) || (dst_dtype != HIFT_F32 && dst_dtype != HIFT_BF16)) return fail(HIFT_EINVAL, "dtype unknown");
+  if (steps < 1 || steps > NS_STEPS_MAX) return fail(HIFT_EINVAL, "steps must be in [1, %d]", NS_STEPS_MAX);
+  if (!(eps >= 1e-30f) || std::isinf(eps)) return fail(HIFT_EINVAL, "eps must be at least 1e-30");
+  NsRun run{steps, {a, b, c}, eps, 0.0, 0.f, 0.f};
+  if (!ns_coefficients_hold(run.co, steps)) return fail(HIFT_EINVAL, "the singular values grow without bound under (%g, %g, %g)", a, b, c);
+  std::vector<NsItem> items;
+  ST_TRY(ns_items(count, matrices, &items, [&](int i, NsItem& it) { ortho_item(matrices[i], it); }));
+  for (int32_t i = 0; i < count; ++i) {
+    const NsItem& it = items[i];
+    if (it.rows == 0 || it.cols == 0) continue;
+    if (!it.src || !it.dst) return fail(HIFT_EINVAL, "matrix %d: src or dst null", i);
+    if (it.ld_src < it.cols || it.ld_dst < it.cols) return fail(HIFT_EINVAL, "matrix %d: rows overlap (leading dimension shorter than a row)", i);
+    if (reinterpret_cast<uintptr_t>(it.src) % (src_dtype == HIFT_BF16 ? 2 : 4) || reinterpret_cast<uintptr_t>(it.dst) % (dst_dtype == HIFT_BF16 ? 2 : 4))
+      return fail(HIFT_EINVAL, "matrix %d does not lie on whole elements", i);
+    if (it.src == it.dst && (src_dtype != dst_dtype || it.ld_src != it.ld_dst)) return fail(HIFT_EINVAL, "matrix %d: in place, type and rows stay", i);
+  }
+  ST_TRY(check_ns_workspace(items, workspace, workspace_bytes));
+  HIP_TRY(newton_schulz(items.data(), count, src_dtype == HIFT_BF16 ? DT_BF16 : DT_F32, dst_dtype == HIFT_BF16 ? DT_BF16 : DT_F32, run, workspace,
+                        (hipStream_t)stream));
+  return HIFT_OK;
+}
+
+hift_status hift_kernel_muon_bytes(int32_t count, const hift_muon_matrix* matrices, size_t* bytes) {
+  if (!bytes) return fail(HIFT_EINVAL, "bytes is null");
+  std::vector<NsItem> items;
+  ST_TRY(ns_items(count, matrices, &items, [&](int i, NsItem& it) { muon_item(matrices[i], it); }));
+  *bytes = ns_workspace(items.data(), count);
+  return HIFT_OK;
+}
+
+hift_status hift_kernel_muon(const hift_opt* opt, int32_t count, const hift_muon_matrix* matrices, void* workspace, size_t workspace_bytes,
+                             void* stream) {
+  if (!opt || opt->kind != HIFT_MUON) return fail(HIFT_EINVAL, "the optimizer is not HIFT_MUON");
+  if (!(opt->momentum >= 0.0 && opt->momentum < 1.0)) return fail(HIFT_EINVAL, "momentum must be in [0, 1)");
+  std::vector<NsItem> items;
+  ST_TRY(ns_items(count, matrices, &items, [&](int i, NsItem& it) { muon_item(matrices[i], it); }));
+  for (int32_t i = 0; i < count; ++i) {
+    const NsItem& it = items[i];
+    if (it.rows == 0 || it.cols == 0) continue;
+    if (!it.src || !it.momentum || !it.master) return fail(HIFT_EINVAL, "matrix %d: master, grad or momentum null", i);
+    if ((reinterpret_cast<uintptr_t>(it.src) | reinterpret_cast<uintptr_t>(it.momentum) | reinterpret_cast<uintptr_t>(it.master)) % 4 ||
+        reinterpret_cast<uintptr_t>(it.copy) % 2)
+      return fail(HIFT_EINVAL, "matrix %d does not lie on whole elements", i);
+  }
+  ST_TRY(check_ns_workspace(items, workspace, workspace_bytes));
+  HIP_TRY(newton_schulz(items.data(), count, DT_F32, DT_F32, muon_run(*opt), workspace, (hipStream_t)stream));
   return HIFT_OK;
 }
 

@@ -1,0 +1,84 @@
+"""Scales and work space of the Newton-Schulz orthogonalisation (csrc/ns_plan.h), compiled with the host compiler."""
+import ctypes
+import os
+import subprocess
+
+import numpy as np
+import pytest
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2401_15207_amd", "csrc")
+CODE = r"""
+#include "ns_plan.h"
+using namespace hift;
+extern "C" int scales(const double* co, double r, float* x, float* a, float* b, double* next) {
+  const double c[3] = {co[0], co[1], co[2]};
+  NsScales s;
+  if (!ns_scales(c, r, &s)) return 0;
+  *x = s.x; *a = s.a; *b = s.b; *next = s.r_next;
+  return 1;
+}
+extern "C" int together(int first, int count, const long long* s) {
+  return ns_together(first, count, [&](int i, int64_t* r, int64_t* c) { *r = s[2 * i]; *c = s[2 * i + 1]; });
+}
+extern "C" size_t bytes(int count, const long long* s) {
+  return ns_workspace_bytes(count, [&](int i, int64_t* r, int64_t* c) { *r = s[2 * i]; *c = s[2 * i + 1]; });
+}
+extern "C" size_t one(long long r, long long c) { return ns_bytes(r, c); }
+"""
+
+
+@pytest.fixture(scope="module")
+def plan(tmp_path_factory):
+    d = tmp_path_factory.mktemp("ns")
+    src, so = d / "ns.cpp", d / "ns.so"
+    src.write_text(CODE)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-shared", "-fPIC", "-I", CSRC, str(src), "-o", str(so)], check=True)
+    lib = ctypes.CDLL(str(so))
+    lib.bytes.restype = lib.one.restype = ctypes.c_size_t
+    lib.one.argtypes = [ctypes.c_longlong] * 2
+    return lib
+
+
+def scales(lib, co, r):
+    c = (ctypes.c_double * 3)(*co)
+    x, a, b, n = ctypes.c_float(), ctypes.c_float(), ctypes.c_float(), ctypes.c_double()
+    ok = lib.scales(c, ctypes.c_double(r), ctypes.byref(x), ctypes.byref(a), ctypes.byref(b), ctypes.byref(n))
+    return (x.value, a.value, b.value, n.value) if ok else None
+
+
+@pytest.mark.parametrize("co", [(3.4445, -4.7750, 2.0315), (1.5, -0.5, 0.0), (1.875, -1.25, 0.375), (2.0, -1.5, 0.5), (0.0, 0.0, 1.0), (0.0, 1.0, 0.0),
+                                (-2.0, 3.0, -1.5), (4.0, 0.0, -2.0)])
+def test_scales_keep_every_factor_in_range(plan, co):
+    r = 1.001
+    for _ in range(8):
+        got = scales(plan, co, r)
+        if got is None:
+            break
+        x, a, b, nxt = got
+        t = np.linspace(0.0, r, 20001)
+        q = np.abs(co[0] + co[1] * t ** 2 + co[2] * t ** 4)
+        for scale, most in ((x, r), (a, r * r), (b, q.max())):
+            assert scale == 2.0 ** round(np.log2(scale)) and scale * most <= 32768.0 * (1 + 1e-6) and scale * most > 16383.0 * (1 - 1e-6)
+        assert nxt >= (t * q).max()
+        assert nxt <= max(1e-3, (t * q).max()) * 1.01
+        r = nxt
+
+
+def test_coefficients_that_let_values_grow_are_refused(plan):
+    for co, r in (((1e4, 0.0, 0.0), 1.0), ((float("nan"), 0.0, 0.0), 1.0), ((0.0, 0.0, 0.0), 1.0), ((1.0, 1.0, 1.0), 2000.0), ((float("inf"), 0.0, 0.0), 1.0)):
+        assert scales(plan, co, r) is None
+
+
+def test_work_space_and_launches(plan):
+    def call(f, shapes, *first):
+        return f(*first, len(shapes), (ctypes.c_longlong * (2 * max(len(shapes), 1)))(*[v for s in shapes for v in s]))
+
+    assert call(plan.bytes, []) == 0 and call(plan.bytes, [(0, 5), (5, 0)]) == 0
+    assert plan.one(65, 300) == plan.one(300, 65) and plan.one(1, 1) % 16 == 0
+    small = [(8, 8)] * 40
+    assert call(plan.together, small, 0) == 16 and call(plan.together, small, 32) == 8
+    assert call(plan.bytes, small) == 16 * plan.one(8, 8)
+    large = [(8192, 8192), (8192, 8192), (64, 64)]      # each fills launches by itself
+    assert call(plan.together, large, 0) == 1 and call(plan.together, large, 1) == 1
+    assert call(plan.bytes, large) == plan.one(8192, 8192)
+    assert call(plan.bytes, [(4096, 4096)] * 4) == 4 * plan.one(4096, 4096)
