@@ -205,8 +205,8 @@ hift_status check_opt(const hift_opt* o) {
 }
 
 // The steps of HIFT_MUON: Newton-Schulz of degree five with the coefficients of Jordan et al. 2024.
-NsRun muon_run(const hift_opt& o) {
-  return NsRun{5, {3.4445, -4.7750, 2.0315}, 1e-7f, o.lr, (float)o.momentum, (float)(1.0 - o.lr * o.weight_decay)};
+NsRun muon_run(const hift_opt& o, bool bf16_model) {
+  return NsRun{5, {3.4445, -4.7750, 2.0315}, 1e-7f, o.lr, (float)o.momentum, (float)(1.0 - o.lr * o.weight_decay), bf16_model};
 }
 
 inline size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -2641,7 +2641,7 @@ hift_status hift_kernel_orthogonalize(int32_t src_dtype, int32_t dst_dtype, int3
   if ((src_dtype != HIFT_F32 && src_dtype != HIFT_BF16) || (dst_dtype != HIFT_F32 && dst_dtype != HIFT_BF16)) return fail(HIFT_EINVAL, "dtype unknown");
   if (steps < 1 || steps > NS_STEPS_MAX) return fail(HIFT_EINVAL, "steps must be in [1, %d]", NS_STEPS_MAX);
   if (!(eps >= 1e-30f) || std::isinf(eps)) return fail(HIFT_EINVAL, "eps must be at least 1e-30");
-  NsRun run{steps, {a, b, c}, eps, 0.0, 0.f, 0.f};
+  NsRun run{steps, {a, b, c}, eps, 0.0, 0.f, 0.f, dst_dtype == HIFT_BF16};
   if (!ns_coefficients_hold(run.co, steps)) return fail(HIFT_EINVAL, "the singular values grow without bound under (%g, %g, %g)", a, b, c);
   std::vector<NsItem> items;
   ST_TRY(ns_items(count, matrices, &items, [&](int i, NsItem& it) { ortho_item(matrices[i], it); }));
@@ -2683,7 +2683,9 @@ hift_status hift_kernel_muon(const hift_opt* opt, int32_t count, const hift_muon
       return fail(HIFT_EINVAL, "matrix %d does not lie on whole elements", i);
   }
   ST_TRY(check_ns_workspace(items, workspace, workspace_bytes));
-  HIP_TRY(newton_schulz(items.data(), count, DT_F32, DT_F32, muon_run(*opt), workspace, (hipStream_t)stream));
+  // (weights without bf16 copies are an fp32 model's)
+  const bool few = count > 0 && std::all_of(items.begin(), items.end(), [](const NsItem& it) { return it.copy != nullptr; });
+  HIP_TRY(newton_schulz(items.data(), count, DT_F32, DT_F32, muon_run(*opt, few), workspace, (hipStream_t)stream));
   return HIFT_OK;
 }
 

@@ -7,6 +7,12 @@
 // bf16 nor one fp16 number holds enough.  Every factor is kept as the sum of two fp16 numbers, high and low (22 bits; see ns_plan.h for
 // the scales), and a product is three matrix instructions, high high + high low + low high, summed in fp32: results as exact as fp32
 // products give them, at a third of the fp16 rate instead of an eleventh of it.
+// A result that goes into bf16 numbers (rounded to 2^-9 of themselves) need not be that exact.  Roundings of A and B act on X as a factor from
+// the left does, so they stay what they are: those of X alone are multiplied.  So with NsRun::few the matrices of 512 and more on the
+// short side take high high alone for A and for A A, high high + high low for B X and high high again for the last B X.  What
+// the roundings of the two diagonals leave, which no sum averages out, is put back by the epilogues (a_rest, b_rest).  Simulated in 64 bits on random,
+// low-rank (noise 1e-3 of it) and decaying (1e-6) matrices of 512 x 512 .. 2048: 3e-4 to 1.3e-3 off in the 2-norm, half as far as the
+// rounding to bf16 itself; with single numbers throughout 3e-3, and 3e-2 where the rank is low.
 // Factors lie in the matrix instruction's register order: blocks of 32 rows x 16 k, 1 KB of high and 1 KB of low numbers, lane l of a
 // wavefront holding row l % 32 and k 8 (l / 32) .. +7 of it, so that a fragment is one contiguous load; blocks along k follow each other.
 #include <math.h>
@@ -40,6 +46,7 @@ struct NsMatrix {
   int n, m;             // short and long side, filled up
   int tall;             // rows > cols: X is U^T
   _Float16 *x, *xt, *xt2, *a, *b;  // X [n, m], X^T [m, n] now and after the step, A and B [n, n]
+  float *a_rest, *b_rest;  // [n] of A's and B's diagonal what the high numbers leave (fewer products)
   double* norm_parts;
   int* small;           // how many powers of two X is below 1 at the start (norms below eps; ns_start_k)
   int block0;           // first workgroup of the launch that works on it
@@ -167,8 +174,13 @@ struct NsStep {
 // Where accumulator i of lane l lies in its 32 x 32 block: column l % 32 and row 8 (i / 4) + 4 (l / 32) + i % 4.
 __device__ __forceinline__ int acc_row(int i, int lane) { return 8 * (i >> 2) + 4 * (lane >> 5) + (i & 3); }
 
-// v: entries [i0 ..][j0 ..] of a 32 x 32 block, as a factor of rows j and k i (four consecutive k of a lane at a time) ...
-__device__ __forceinline__ void put_rows_j(const Factor& f, int i0, int j0, const f32x16& v, int lane) {
+constexpr int TURN_PITCH = 36;  // words: the turned block's rows are read in 16-byte pieces
+
+// v: entries [i0 ..][j0 ..] of a 32 x 32 block, into a factor of rows j and k i (four consecutive k of a lane at a time) and, if
+// `other`, turned around in LDS into one of rows i and k j.  LOW_J, LOW_I: the low numbers too.
+template <bool LOW_J, bool LOW_I>
+__device__ __forceinline__ void put_block(const Factor& rows_j, const Factor& rows_i, bool other, int i0, int j0, const f32x16& v, uint32_t* turned,
+                                          int lane) {
 #pragma unroll
   for (int g = 0; g < 4; ++g) {
     half4 hi, lo;
@@ -177,117 +189,232 @@ __device__ __forceinline__ void put_rows_j(const Factor& f, int i0, int j0, cons
       _Float16 h, l;
       split(v[4 * g + e], h, l);
       hi[e] = h; lo[e] = l;
+      if (other) {
+        typedef _Float16 half2 __attribute__((ext_vector_type(2)));
+        const half2 both = {h, l};
+        turned[acc_row(4 * g + e, lane) * TURN_PITCH + (lane & 31)] = __builtin_bit_cast(uint32_t, both);
+      }
     }
-    _Float16* p = f.block(j0 / 32, i0 / 16 + (g >> 1)) + ((lane & 31) + 32 * (g & 1)) * 8 + 4 * (lane >> 5);
+    _Float16* p = rows_j.block(j0 / 32, i0 / 16 + (g >> 1)) + ((lane & 31) + 32 * (g & 1)) * 8 + 4 * (lane >> 5);
     *reinterpret_cast<half4*>(p) = hi;
-    *reinterpret_cast<half4*>(p + 512) = lo;
+    if (LOW_J) *reinterpret_cast<half4*>(p + 512) = lo;
   }
-}
-// ... and as one of rows i and k j
-__device__ __forceinline__ void put_rows_i(const Factor& f, int i0, int j0, const f32x16& v, int lane) {
-  const int j = lane & 31;
+  if (!other) return;
+  __builtin_amdgcn_wave_barrier();  // (a wavefront's own LDS accesses stay in order)
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    _Float16 h, l;
-    split(v[i], h, l);
-    _Float16* p = f.block(i0 / 32, j0 / 16 + (j >> 4)) + (acc_row(i, lane) + 32 * ((j >> 3) & 1)) * 8 + (j & 7);
-    p[0] = h;
-    p[512] = l;
+  for (int b = 0; b < 2; ++b) {
+    const uint32_t* row = turned + (lane & 31) * TURN_PITCH + b * 16 + 8 * (lane >> 5);
+    uint32_t w[8], hi[4], lo[4];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e] = row[e];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      hi[e] = (w[2 * e] & 0xFFFFu) | w[2 * e + 1] << 16;
+      lo[e] = w[2 * e] >> 16 | (w[2 * e + 1] & 0xFFFF0000u);
+    }
+    _Float16* p = rows_i.block(i0 / 32, j0 / 16 + b) + lane * 8;
+    *reinterpret_cast<hift_u32x4*>(p) = hift_u32x4{hi[0], hi[1], hi[2], hi[3]};
+    if (LOW_I) *reinterpret_cast<hift_u32x4*>(p + 512) = hift_u32x4{lo[0], lo[1], lo[2], lo[3]};
   }
+  __builtin_amdgcn_wave_barrier();
 }
 
-template <int MODE, typename OUT>
-__global__ void __launch_bounds__(256) ns_product_k(NsTable t, NsStep st) {
+// Four consecutive k of a lane's row of a factor of rows j and k i, where put_block leaves accumulators 4 g .. 4 g + 3
+__device__ __forceinline__ const _Float16* at_block(const Factor& rows_j, int i0, int j0, int g, int lane) {
+  return rows_j.block(j0 / 32, i0 / 16 + (g >> 1)) + ((lane & 31) + 32 * (g & 1)) * 8 + 4 * (lane >> 5);
+}
+
+// Tiles of 256 x 256 by 2 x 4 wavefronts, of 128 x 128 by 2 x 2.  Both operands travel into LDS with direct-to-LDS loads, as they lie, into a
+// ring of stages of 16 or 32 k; a stage's fragments are read into registers under the products of the stage before.
+// PP, QP: numbers of P and Q that take part: 2 and 2 (three products), 1 and 2 (two), 1 and 1 (one).
+template <int SIDE, int PP, int QP>
+struct NsTile {
+  static constexpr int WI = 2, WJ = SIDE == 256 ? 4 : 2, NW = WI * WJ;
+  static constexpr int BI = SIDE / 32 / WI, BJ = SIDE / 32 / WJ;   // blocks of 32 x 32 a wavefront
+  static constexpr int KS = PP + QP == 2 ? 2 : 1;                  // blocks along k of a stage
+  static constexpr int PN = SIDE / 32 * KS * PP, PIECES = PN + SIDE / 32 * KS * QP;  // KB of P in a stage, and of both
+  static constexpr int LOADS = PIECES / NW;                        // load instructions a wavefront and stage, 1 KB each
+  static constexpr int STAGE = PIECES * 1024, RING = SIDE == 256 ? 4 : 3, LDS = RING * STAGE;
+  static_assert(PIECES % NW == 0 && LDS <= 160 * 1024 && NW * 32 * TURN_PITCH * 4 <= LDS, "blocks turn in the ring");
+};
+
+template <int SIDE, int MODE, int PP, int QP, typename OUT>
+__global__ void __launch_bounds__((64 * NsTile<SIDE, PP, QP>::NW), 2) ns_product_k(NsTable t, NsStep st) {
+  typedef NsTile<SIDE, PP, QP> T;
+  constexpr int BI = T::BI, BJ = T::BJ, RING = T::RING, KS = T::KS;
+  constexpr bool FEW = PP + QP < 4;
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const NsMatrix& q = matrix_of(t, blockIdx.x);
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // Workgroups are dealt round-robin to the 8 XCDs (every matrix starts at a multiple of 8): each XCD gets a contiguous run of tiles, so
+  // that those it works on at a time share operands in its L2.
+  constexpr bool SYM = MODE == NS_GRAM || MODE == NS_POLY;
+  const bool turn = MODE == NS_LAST && q.tall;  // dst's columns along the lanes
+  const int side_i = (turn ? q.m : q.n) / SIDE, side_j = (SYM || turn ? q.n : q.m) / SIDE;
+  const int tiles = SYM ? side_i * (side_i + 1) / 2 : side_i * side_j;
   int id = blockIdx.x - q.block0;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  id = (id & 7) * ((tiles + 7) >> 3) + (id >> 3);
+  if (id >= tiles) return;
   Factor P, Q;
   int ti, tj;
-  if (MODE == NS_GRAM || MODE == NS_POLY) {
+  if (SYM) {
     P.p = Q.p = MODE == NS_GRAM ? q.x : q.a;
     P.kb = Q.kb = (MODE == NS_GRAM ? q.m : q.n) / 16;
     ti = 0;
-    const int tiles = q.n / 128;
-    while (id >= tiles - ti) { id -= tiles - ti; ++ti; }
+    while (id >= side_i - ti) { id -= side_i - ti; ++ti; }
     tj = ti + id;
   } else {
     const Factor b{q.b, q.n / 16}, x{q.xt, q.n / 16};
-    const bool turn = MODE == NS_LAST && q.tall;  // dst's columns along the lanes
     P = turn ? x : b;
     Q = turn ? b : x;
-    const int across = (turn ? q.n : q.m) / 128;
-    ti = id / across;
-    tj = id % across;
+    // down bands of 4 tile rows
+    const int band = id / (4 * side_j), in_band = id - band * 4 * side_j, rows = min(4, side_i - band * 4);
+    ti = band * 4 + in_band % rows;
+    tj = in_band / rows;
   }
   const int small = *q.small, up = max(0, small - st.grown);  // X is stored times 2^up
-  const int i0 = ti * 128 + (wave >> 1) * 64, j0 = tj * 128 + (wave & 1) * 64;
+  const int stages = P.kb / KS;
 
-  f32x16 acc[2][2] = {};
-  for (int k = 0; k < P.kb; ++k) {
-    half8 ph[2], pl[2], qh[2], ql[2];
+  const uint64_t pa = reinterpret_cast<uint64_t>(P.block(ti * (SIDE / 32), 0)), qa = reinterpret_cast<uint64_t>(Q.block(tj * (SIDE / 32), 0));
+  const uint32_t lds0 = (uint32_t)reinterpret_cast<uintptr_t>(smem), voff = lane * 16;
+  auto slot = [](int s) __attribute__((always_inline)) { return RING & (RING - 1) ? s % RING : s & (RING - 1); };
+  auto request = [&](int s) __attribute__((always_inline)) {
+    const uint32_t at = lds0 + (uint32_t)slot(s) * T::STAGE;
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const _Float16* p = P.block(i0 / 32 + b, k) + lane * 8;
-      ph[b] = *reinterpret_cast<const half8*>(p);
-      pl[b] = *reinterpret_cast<const half8*>(p + 512);
-      p = Q.block(j0 / 32 + b, k) + lane * 8;
-      qh[b] = *reinterpret_cast<const half8*>(p);
-      ql[b] = *reinterpret_cast<const half8*>(p + 512);
+    for (int i = 0; i < T::LOADS; ++i) {
+      const int load = wave * T::LOADS + i;
+      const bool is_q = load >= T::PN;
+      const int in = is_q ? load - T::PN : load, planes = is_q ? QP : PP, rb = in / (KS * planes), rest = in % (KS * planes);
+      const uint64_t base = is_q ? qa : pa;
+      const hift_u32x4 rsrc = {(uint32_t)base, (uint32_t)(base >> 32) & 0xFFFFu, 0xFFFFFFF0u, 0x00020000u};
+      const uint32_t soff = ((uint32_t)rb * P.kb + s * KS + rest / planes) * 2048u + (rest % planes) * 1024u;
+      load_to_lds_b128(rsrc, at + (uint32_t)load * 1024, voff, soff);
     }
+  };
+  const int wi = wave / T::WJ, wj = wave % T::WJ;
+  half8 p[2][KS][BI][PP], r[2][KS][BJ][QP];  // fragments of two stages: high and low numbers
+  auto read = [&](int to, int s) __attribute__((always_inline)) {
+    const unsigned char* at = smem + slot(s) * T::STAGE + lane * 16;
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
+    for (int k = 0; k < KS; ++k) {
 #pragma unroll
-      for (int y = 0; y < 2; ++y) {
-        acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(pl[x], qh[y], acc[x][y], 0, 0, 0);
-        acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[x], ql[y], acc[x][y], 0, 0, 0);
-        acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ph[x], qh[y], acc[x][y], 0, 0, 0);
-      }
+      for (int b = 0; b < BI; ++b)
+#pragma unroll
+        for (int h = 0; h < PP; ++h) p[to][k][b][h] = *reinterpret_cast<const half8*>(at + (((wi * BI + b) * KS + k) * PP + h) * 1024);
+#pragma unroll
+      for (int b = 0; b < BJ; ++b)
+#pragma unroll
+        for (int h = 0; h < QP; ++h) r[to][k][b][h] = *reinterpret_cast<const half8*>(at + (T::PN + ((wj * BJ + b) * KS + k) * QP + h) * 1024);
+    }
+  };
+  f32x16 acc[BI][BJ] = {};
+  auto multiply = [&](int c) __attribute__((always_inline)) {
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int h = PP + QP - 2; h >= 0; --h)  // low high, high low, high high
+#pragma unroll
+        for (int x = 0; x < BI; ++x)
+#pragma unroll
+          for (int y = 0; y < BJ; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(p[c][k][x][h == 2], r[c][k][y][h == 1], acc[x][y], 0, 0, 0);
+  };
+#pragma unroll
+  for (int s = 0; s < RING; ++s)
+    if (s < stages) request(s);
+  if (RING <= stages) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((RING - 1) * T::LOADS) : "memory");
+  else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  read(0, 0);
+  // Past the wait the stage after s has landed (all but the younger stages' requests), and past the barrier s's buffer, whose fragments every
+  // wavefront has, is free for the stage a whole ring further on.  Near the end fewer requests are in flight: there the wait is for all.
+  auto stage = [&](int s, int c, bool tail) __attribute__((always_inline)) {
+    if (!tail) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((RING - 2) * T::LOADS) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    read(c ^ 1, s + 1);  // (past the end: what the ring holds, and never multiplied)
+    if (!tail || s + RING < stages) request(s + RING);
+    multiply(c);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  int s = 0;
+  for (; s + 1 + RING < stages; s += 2) {
+    stage(s, 0, false);
+    stage(s + 1, 1, false);
+  }
+  // (the number of stages is even)
+  for (; s < stages; s += 2) {
+    stage(s, 0, true);
+    stage(s + 1, 1, true);
   }
 
+  __syncthreads();  // the ring is free: nothing is on its way there either
+  uint32_t* turned = reinterpret_cast<uint32_t*>(smem) + wave * 32 * TURN_PITCH;
 #pragma unroll
-  for (int x = 0; x < 2; ++x)
+  for (int x = 0; x < BI; ++x)
 #pragma unroll
-    for (int y = 0; y < 2; ++y) {
+    for (int y = 0; y < BJ; ++y) {
       f32x16 v = acc[x][y];
-      const int i = i0 + 32 * x, j = j0 + 32 * y;
+      const int i = ti * SIDE + (wi * BI + x) * 32, j = tj * SIDE + (wj * BJ + y) * 32;
       if (MODE == NS_POLY) {
         // A at the same place: rows j, k i of a symmetric factor
         const Factor a{q.a, q.n / 16};
+        const float rest_j = FEW ? q.a_rest[j + (lane & 31)] : 0.f;
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-          const _Float16* p = a.block(j / 32, i / 16 + (g >> 1)) + ((lane & 31) + 32 * (g & 1)) * 8 + 4 * (lane >> 5);
-          const half4 hi = *reinterpret_cast<const half4*>(p), lo = *reinterpret_cast<const half4*>(p + 512);
+          const _Float16* f = at_block(a, i, j, g, lane);
+          const half4 hi = *reinterpret_cast<const half4*>(f), lo = *reinterpret_cast<const half4*>(f + 512);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const bool diagonal = i + acc_row(4 * g + e, lane) == j + (lane & 31);
-            v[4 * g + e] = (fmaf(st.cc, v[4 * g + e], st.cb * ((float)hi[e] + (float)lo[e])) + (diagonal ? st.ca : 0.f)) * st.out_scale;
+            const int row = i + acc_row(4 * g + e, lane);
+            float aa = v[4 * g + e];
+            if (FEW) aa = fmaf((float)hi[e], q.a_rest[row] + rest_j, aa);  // what the diagonal's low numbers add to A A
+            v[4 * g + e] = (fmaf(st.cc, aa, st.cb * ((float)hi[e] + (float)lo[e])) + (row == j + (lane & 31) ? st.ca : 0.f)) * st.out_scale;
           }
         }
-      } else if (MODE != NS_LAST) {
+      } else {
+        if (!SYM && FEW) {
+          // What the diagonal of B's low numbers adds to B X: X at the same place, in the factor whose rows are j
+          const Factor f = turn ? Factor{q.x, q.m / 16} : Factor{q.xt, q.n / 16};
+          const float rest_j = turn ? q.b_rest[j + (lane & 31)] : 0.f;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) v[e] = ldexpf(v[e] * st.unscale * st.out_scale, MODE == NS_GRAM ? -2 * up : max(0, small - st.grown - st.growth) - up);
+          for (int g = 0; g < 4; ++g) {
+            const half4 hi = *reinterpret_cast<const half4*>(at_block(f, i, j, g, lane));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[4 * g + e] = fmaf((float)hi[e], turn ? rest_j : q.b_rest[i + acc_row(4 * g + e, lane)], v[4 * g + e]);
+          }
+        }
+        if (MODE != NS_LAST) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) v[e] = ldexpf(v[e] * st.unscale * st.out_scale, MODE == NS_GRAM ? -2 * up : max(0, small - st.grown - st.growth) - up);
+        }
       }
-      if (MODE == NS_GRAM || MODE == NS_POLY) {
+      if (SYM) {
         const Factor out{MODE == NS_GRAM ? q.a : q.b, q.n / 16};
-        put_rows_j(out, i, j, v, lane);
-        if (ti != tj) put_rows_i(out, i, j, v, lane);
+        constexpr bool LOW = !FEW || MODE == NS_GRAM;
+        put_block<LOW, LOW>(out, out, ti != tj, i, j, v, turned, lane);
+        if (FEW && i == j) {
+          float* rest = MODE == NS_GRAM ? q.a_rest : q.b_rest;
+#pragma unroll
+          for (int e = 0; e < 16; ++e)
+            if (acc_row(e, lane) == (lane & 31)) rest[i + (lane & 31)] = v[e] - (float)(_Float16)v[e];
+        }
       } else if (MODE == NS_APPLY) {
-        put_rows_j(Factor{q.xt2, q.n / 16}, i, j, v, lane);
-        put_rows_i(Factor{q.x, q.m / 16}, i, j, v, lane);
+        put_block<true, !FEW>(Factor{q.xt2, q.n / 16}, Factor{q.x, q.m / 16}, true, i, j, v, turned, lane);
       } else {
         const int64_t c = j + (lane & 31);
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          const int64_t r = i + acc_row(e, lane);
-          if (r >= q.rows || c >= q.cols) continue;
+          const int64_t row = i + acc_row(e, lane);
+          if (row >= q.rows || c >= q.cols) continue;
           const float o = ldexpf(v[e] * st.unscale, -up);
           if (q.master) {
-            float* w = q.master + r * q.cols + c;
+            float* w = q.master + row * q.cols + c;
             const float nw = fmaf(-q.factor, o, st.decay * *w);
             *w = nw;
-            if (q.copy) q.copy[r * q.cols + c] = from_f32<bf16>(nw);
+            if (q.copy) q.copy[row * q.cols + c] = from_f32<bf16>(nw);
           } else {
-            reinterpret_cast<OUT*>(q.dst)[r * q.ld_dst + c] = from_f32<OUT>(o);
+            reinterpret_cast<OUT*>(q.dst)[row * q.ld_dst + c] = from_f32<OUT>(o);
           }
         }
       }
@@ -305,7 +432,37 @@ uint32_t spread(NsTable& t, F blocks) {
   return (uint32_t)at;
 }
 
-hipError_t steps_of(NsTable& t, int dt_src, int dt_dst, const NsRun& run, hipStream_t st) {
+template <int SIDE, int MODE, int PP, int QP, typename OUT = float>
+hipError_t product(NsTable& t, const NsStep& p, hipStream_t st) {
+  typedef NsTile<SIDE, PP, QP> T;
+  const uint32_t blocks = spread(t, [](const NsMatrix& q) {
+    const int64_t n = q.n / SIDE, tiles = MODE == NS_GRAM || MODE == NS_POLY ? n * (n + 1) / 2 : n * (q.m / SIDE);
+    return (tiles + 7) / 8 * 8;
+  });
+  static bool attr_done = false;  // one flag per instantiation
+  const auto kern = ns_product_k<SIDE, MODE, PP, QP, OUT>;
+  if (!attr_done) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS);
+    if (e != hipSuccess) return e;
+    attr_done = true;
+  }
+  kern<<<blocks, 64 * T::NW, T::LDS, st>>>(t, p);
+  return hipGetLastError();
+}
+
+// The products of one step.  FEW: one product each for A, A A and the last B X, two for the others.
+template <int SIDE, bool FEW>
+hipError_t step_of(NsTable& t, const NsStep& gram, const NsStep& poly, const NsStep& apply, bool last, int dt_dst, hipStream_t st) {
+  constexpr int ONE = FEW ? 1 : 2;
+  hipError_t e = product<SIDE, NS_GRAM, ONE, ONE>(t, gram, st);
+  if (e == hipSuccess) e = product<SIDE, NS_POLY, ONE, ONE>(t, poly, st);
+  if (e != hipSuccess) return e;
+  if (!last) return product<SIDE, NS_APPLY, ONE, 2>(t, apply, st);
+  if (dt_dst == DT_BF16) return product<SIDE, NS_LAST, ONE, ONE, bf16>(t, apply, st);
+  return product<SIDE, NS_LAST, ONE, ONE>(t, apply, st);
+}
+
+hipError_t steps_of(NsTable& t, int side, int dt_src, int dt_dst, const NsRun& run, bool few, hipStream_t st) {
   const uint32_t parts = spread(t, [](const NsMatrix&) { return NS_NORM_PARTS; });
   if (dt_src == DT_BF16) ns_norm_k<bf16><<<parts, 256, 0, st>>>(t, run.mu);
   else ns_norm_k<float><<<parts, 256, 0, st>>>(t, run.mu);
@@ -317,33 +474,26 @@ hipError_t steps_of(NsTable& t, int dt_src, int dt_dst, const NsRun& run, hipStr
   if (dt_src == DT_BF16) ns_start_k<bf16><<<squares, 256, 0, st>>>(t, run.mu, run.eps, s.x);
   else ns_start_k<float><<<squares, 256, 0, st>>>(t, run.mu, run.eps, s.x);
   for (int k = 0; k < run.steps; ++k) {
-    if (!ns_scales(run.co, r, &s)) return hipErrorInvalidValue;
-    NsStep p{};
-    p.grown = k * growth;
-    p.growth = growth;
-    p.unscale = 1.f / (s.x * s.x);
-    p.out_scale = s.a;
-    const uint32_t half = spread(t, [](const NsMatrix& q) { return (int64_t)(q.n / 128) * (q.n / 128 + 1) / 2; });
-    ns_product_k<NS_GRAM, float><<<half, 256, 0, st>>>(t, p);
-    p.ca = (float)run.co[0];
-    p.cb = (float)run.co[1] / s.a;
-    p.cc = (float)run.co[2] / (s.a * s.a);
-    p.out_scale = s.b;
-    ns_product_k<NS_POLY, float><<<half, 256, 0, st>>>(t, p);
-    p.unscale = 1.f / (s.b * s.x);
-    const uint32_t whole = spread(t, [](const NsMatrix& q) { return (int64_t)(q.n / 128) * (q.m / 128); });
+    NsStep gram{}, poly{}, apply{};
+    gram.grown = apply.grown = k * growth;
+    gram.growth = apply.growth = growth;
+    gram.unscale = 1.f / (s.x * s.x);
+    gram.out_scale = s.a;
+    poly.ca = (float)run.co[0];
+    poly.cb = (float)run.co[1] / s.a;
+    poly.cc = (float)run.co[2] / (s.a * s.a);
+    poly.out_scale = s.b;
+    apply.unscale = 1.f / (s.b * s.x);
+    apply.decay = run.decay;
     r = std::max(s.r_next, 1.0);  // (and what norms below eps are stored as)
-    if (k + 1 < run.steps) {
-      NsScales next;
-      if (!ns_scales(run.co, r, &next)) return hipErrorInvalidValue;
-      p.out_scale = next.x;
-      ns_product_k<NS_APPLY, float><<<whole, 256, 0, st>>>(t, p);
+    if (!ns_scales(run.co, r, &s)) return hipErrorInvalidValue;
+    apply.out_scale = s.x;
+    const bool last = k + 1 == run.steps;
+    const auto step = side == 256 ? (few ? step_of<256, true> : step_of<256, false>) : (few ? step_of<128, true> : step_of<128, false>);
+    const hipError_t e = step(t, gram, poly, apply, last, dt_dst, st);
+    if (e != hipSuccess) return e;
+    if (!last)
       for (int i = 0; i < t.count; ++i) std::swap(t.m[i].xt, t.m[i].xt2);
-    } else {
-      p.decay = run.decay;
-      if (dt_dst == DT_BF16) ns_product_k<NS_LAST, bf16><<<whole, 256, 0, st>>>(t, p);
-      else ns_product_k<NS_LAST, float><<<whole, 256, 0, st>>>(t, p);
-    }
   }
   return hipGetLastError();
 }
@@ -366,21 +516,19 @@ size_t ns_workspace(const NsItem* items, int count) {
 }
 
 hipError_t newton_schulz(const NsItem* items, int count, int dt_src, int dt_dst, const NsRun& run, void* workspace, hipStream_t st) {
-  const auto shape = [&](int i, int64_t* r, int64_t* c) { *r = items[i].rows; *c = items[i].cols; };
-  for (int at = 0; at < count;) {
-    const int n = ns_together(at, count, shape);
+  hipError_t err = hipSuccess;
+  ns_launches(count, run.few, [&](int i, int64_t* r, int64_t* c) { *r = items[i].rows; *c = items[i].cols; }, [&](const int* which, int n, int side, bool large) {
     NsTable t{};
     unsigned char* ws = reinterpret_cast<unsigned char*>(workspace);
-    for (int i = at; i < at + n; ++i) {
-      const NsItem& it = items[i];
-      if (it.rows == 0 || it.cols == 0) continue;
+    for (int i = 0; i < n; ++i) {
+      const NsItem& it = items[which[i]];
       NsMatrix& q = t.m[t.count++];
       q.rows = it.rows; q.cols = it.cols; q.ld_src = it.ld_src; q.ld_dst = it.ld_dst;
       q.src = it.src; q.momentum = it.momentum; q.dst = it.dst; q.master = it.master; q.copy = (bf16*)it.copy;
       q.factor = (float)(run.lr * 0.2 * sqrt((double)std::max(it.rows, it.cols)));
       q.tall = it.rows > it.cols;
-      q.n = (int)ns_up(std::min(it.rows, it.cols));
-      q.m = (int)ns_up(std::max(it.rows, it.cols));
+      q.n = (int)ns_up(std::min(it.rows, it.cols), side);
+      q.m = (int)ns_up(std::max(it.rows, it.cols), side);
       auto take = [&](int64_t entries) {
         _Float16* p = reinterpret_cast<_Float16*>(ws);
         ws += entries * 4;
@@ -391,18 +539,17 @@ hipError_t newton_schulz(const NsItem* items, int count, int dt_src, int dt_dst,
       q.xt2 = take((int64_t)q.n * q.m);
       q.a = take((int64_t)q.n * q.n);
       q.b = take((int64_t)q.n * q.n);
+      q.a_rest = reinterpret_cast<float*>(ws);
+      q.b_rest = q.a_rest + q.n;
+      ws += q.n * 8;
       q.norm_parts = reinterpret_cast<double*>(ws);
       ws += NS_NORM_PARTS * 8;
       q.small = reinterpret_cast<int*>(ws);
       ws += 16;
     }
-    if (t.count > 0) {
-      const hipError_t e = steps_of(t, dt_src, dt_dst, run, st);
-      if (e != hipSuccess) return e;
-    }
-    at += n;
-  }
-  return hipSuccess;
+    if (err == hipSuccess) err = steps_of(t, side, dt_src, dt_dst, run, large, st);
+  });
+  return err;
 }
 
 }  // namespace hift

@@ -50,48 +50,70 @@ inline int ns_growth(const double (&co)[3]) { return (int)ceil(log2(fabs(co[0]) 
 
 constexpr int NS_STEPS_MAX = 16;   // steps of a call
 constexpr int NS_TABLE = 16;       // matrices of a launch
-constexpr int NS_PAD = 128;        // both sides of a matrix are filled up with zeros to a multiple of this
 constexpr int64_t NS_SIDE_MAX = 65536;
-// Matrices share launches until together they have this many entries: from there on a launch has several tiles for each of the 256
-// compute units by itself, and more matrices would only need more work space.
-constexpr int64_t NS_TOGETHER = int64_t(1) << 26;
+// Matrices share launches until together they have this many entries: a few large ones fill the last round of a launch's tiles over the
+// 256 compute units, more would only need more work space.
+constexpr int64_t NS_TOGETHER = int64_t(1) << 28;
+// Tiles of a matrix's products; both of its sides are filled up with zeros to a multiple.  256 x 256 where at least 64 of them cover it.
+inline int ns_side(int64_t rows, int64_t cols) { return std::min(rows, cols) >= 1280 && rows * cols >= int64_t(64) * 256 * 256 ? 256 : 128; }
 
-inline int64_t ns_up(int64_t x) { return (x + NS_PAD - 1) / NS_PAD * NS_PAD; }
-// Work space of one matrix: X, X^T before and after a step, A and B, two fp16 numbers to an entry, the sums of its norm, and
-// how far that is below eps.
+// Whose products are fewer for a bf16 result: smaller ones are bound by latency, and further off with them.
+inline bool ns_large(int64_t rows, int64_t cols) { return std::min(rows, cols) >= 512; }
+
+inline int64_t ns_up(int64_t x, int side) { return (x + side - 1) / side * side; }
+// Work space of one matrix: X, X^T before and after a step, A and B, two fp16 numbers to an entry, two diagonals, the sums
+// of its norm, and how far that is below eps.
 constexpr int NS_NORM_PARTS = 256;
 inline size_t ns_bytes(int64_t rows, int64_t cols) {
-  const int64_t n = ns_up(std::min(rows, cols)), m = ns_up(std::max(rows, cols));
-  return (size_t)(3 * n * m + 2 * n * n) * 4 + NS_NORM_PARTS * 8 + 16;
+  const int side = ns_side(rows, cols);
+  const int64_t n = ns_up(std::min(rows, cols), side), m = ns_up(std::max(rows, cols), side);
+  return (size_t)(3 * n * m + 2 * n * n) * 4 + (size_t)n * 8 + NS_NORM_PARTS * 8 + 16;
 }
-// How many matrices from `first` on share launches.  shape(i, &rows, &cols)
-template <class F>
-inline int ns_together(int first, int count, F shape) {
-  int64_t entries = 0;
-  int n = 0;
-  while (first + n < count && n < NS_TABLE) {
-    int64_t r, c;
-    shape(first + n, &r, &c);
-    if (n > 0 && entries + r * c > NS_TOGETHER) break;
-    entries += r * c;
-    ++n;
-  }
-  return n;
-}
-template <class F>
-inline size_t ns_workspace_bytes(int count, F shape) {
-  size_t most = 0;
-  for (int at = 0; at < count;) {
-    const int n = ns_together(at, count, shape);
-    size_t sum = 0;
-    for (int i = at; i < at + n; ++i) {
+// The launches of a list: launch(indexes, how many, tile side, large) for matrices that share them, those with the most work first (their tiles
+// then do not come last).  shape(i, &rows, &cols); matrices without entries are left out.
+// few: large ones apart, as they take fewer products.
+template <class S, class F>
+inline void ns_launches(int count, bool few, S shape, F launch) {
+  for (int kind = 0; kind < (few ? 3 : 2); ++kind) {
+    const int side = kind == 0 ? 256 : 128;
+    const bool large = few && kind < 2;
+    int which[NS_TABLE], n = 0;
+    int64_t entries = 0, longest[NS_TABLE];
+    const auto flush = [&]() {
+      if (n > 0) launch((const int*)which, n, side, large);
+      n = 0;
+      entries = 0;
+    };
+    for (int i = 0; i < count; ++i) {
       int64_t r, c;
       shape(i, &r, &c);
-      sum += r > 0 && c > 0 ? ns_bytes(r, c) : 0;
+      if (r == 0 || c == 0 || ns_side(r, c) != side || (few && ns_large(r, c) != large)) continue;
+      if (n == NS_TABLE || (n > 0 && entries + r * c > NS_TOGETHER)) flush();
+      int at = n++;
+      for (; at > 0 && longest[at - 1] < std::max(r, c); --at) {
+        which[at] = which[at - 1];
+        longest[at] = longest[at - 1];
+      }
+      which[at] = i;
+      longest[at] = std::max(r, c);
+      entries += r * c;
     }
-    most = std::max(most, sum);
-    at += n;
+    flush();
   }
+}
+template <class S>
+inline size_t ns_workspace_bytes(int count, S shape) {
+  size_t most = 0;
+  for (bool few : {false, true})
+    ns_launches(count, few, shape, [&](const int* which, int n, int, bool) {
+      size_t sum = 0;
+      for (int i = 0; i < n; ++i) {
+        int64_t r, c;
+        shape(which[i], &r, &c);
+        sum += ns_bytes(r, c);
+      }
+      most = std::max(most, sum);
+    });
   return most;
 }
 

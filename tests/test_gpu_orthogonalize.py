@@ -89,6 +89,50 @@ def test_larger(r, c):
     assert (out.double() - reference(u)).norm().item() <= 5 * 2.0 ** -21 * COEF[0] ** 5 * math.sqrt(min(r, c))
 
 
+@pytest.mark.parametrize("shapes", [[(512, 700), (700, 512), (1100, 600)], [(1500, 3000), (2900, 1400), (2048, 2048), (600, 520)]])
+def test_results_in_bf16(shapes):
+    """Large matrices take fewer products for a result in bf16, each within 2^-9 of the 2-norm (as its rounding is) whatever the spectrum."""
+    import torch
+    import paper_2401_15207_amd as H
+    g = torch.Generator(device="cuda")
+    g.manual_seed(len(shapes))
+    for noise in (1.0, 1e-3, 1e-5):
+        u = [torch.randn(r, 9, generator=g, device="cuda") @ torch.randn(9, c, generator=g, device="cuda") + noise * torch.randn(r, c, generator=g, device="cuda")
+             for r, c in shapes]
+        out, exact = [torch.empty(s, device="cuda", dtype=torch.bfloat16) for s in shapes], [torch.empty(s, device="cuda") for s in shapes]
+        H.kernel_orthogonalize(u, out)
+        H.kernel_orthogonalize(u, exact)
+        again = [torch.empty_like(x) for x in out]
+        H.kernel_orthogonalize(u, again)
+        for a, b, c, x in zip(u, out, exact, again):
+            want = reference(a)
+            assert rel(b, want) <= 2.0 ** -9 + 2.0 ** -9, (noise, tuple(a.shape))
+            # (fp32 results keep all of them; roundings of 22 bits, amplified by low rank)
+            assert (c.double() - want).norm().item() <= 5 * 2.0 ** -21 * COEF[0] ** 5 * math.sqrt(min(a.shape))
+            assert torch.equal(b, x)
+
+
+def test_update_of_large_matrices():
+    import torch
+    import paper_2401_15207_amd as H
+    shapes = [(1400, 2900), (2900, 1400), (520, 600)]
+    g = torch.Generator(device="cuda")
+    g.manual_seed(11)
+    w, gr, m = ([torch.randn(s, generator=g, device="cuda") * size for s in shapes] for size in (0.02, 1e-4, 1e-3))
+    opt = dict(kind="muon", lr=1e-2, momentum=0.95, weight_decay=0.0)
+    for copies in (True, False):
+        w1, m1 = [x.clone() for x in w], [x.clone() for x in m]
+        cc = [torch.empty(s, device="cuda", dtype=torch.bfloat16) for s in shapes] if copies else None
+        H.kernel_muon(opt, w1, gr, m1, cc)
+        for i, s in enumerate(shapes):
+            m64 = 0.95 * m[i].double() + gr[i].double()
+            o = reference(gr[i].double() + 0.95 * m64) * 1e-2 * 0.2 * math.sqrt(max(s))
+            # an fp32 model's update keeps all products, a bf16 model's is within 2^-9 of the step
+            assert (w1[i].double() - (w[i].double() - o)).norm().item() <= (2.0 ** -9 if copies else 15 * 2.0 ** -22 * COEF[0] ** 5) * o.norm().item() + 2.0 ** -23 * w[i].norm().item()
+            assert rel(m1[i], m64) <= 2.0 ** -23
+            assert not copies or torch.equal(cc[i], w1[i].to(torch.bfloat16))
+
+
 def test_other_steps_and_coefficients():
     import torch
     import paper_2401_15207_amd as H

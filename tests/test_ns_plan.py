@@ -17,8 +17,14 @@ extern "C" int scales(const double* co, double r, float* x, float* a, float* b, 
   *x = s.x; *a = s.a; *b = s.b; *next = s.r_next;
   return 1;
 }
-extern "C" int together(int first, int count, const long long* s) {
-  return ns_together(first, count, [&](int i, int64_t* r, int64_t* c) { *r = s[2 * i]; *c = s[2 * i + 1]; });
+extern "C" int launches(int count, int few, const long long* s, int* out) {  // side, how many, which ...
+  int n = 0;
+  ns_launches(count, few != 0, [&](int i, int64_t* r, int64_t* c) { *r = s[2 * i]; *c = s[2 * i + 1]; }, [&](const int* which, int k, int side, bool) {
+    out[n++] = side;
+    out[n++] = k;
+    for (int i = 0; i < k; ++i) out[n++] = which[i];
+  });
+  return n;
 }
 extern "C" size_t bytes(int count, const long long* s) {
   return ns_workspace_bytes(count, [&](int i, int64_t* r, int64_t* c) { *r = s[2 * i]; *c = s[2 * i + 1]; });
@@ -75,10 +81,21 @@ def test_work_space_and_launches(plan):
 
     assert call(plan.bytes, []) == 0 and call(plan.bytes, [(0, 5), (5, 0)]) == 0
     assert plan.one(65, 300) == plan.one(300, 65) and plan.one(1, 1) % 16 == 0
+    def launches(shapes, few=0):
+        out = (ctypes.c_int * (4 * len(shapes) + 8))()
+        n, at, got = plan.launches(len(shapes), few, (ctypes.c_longlong * (2 * len(shapes)))(*[v for s in shapes for v in s]), out), 0, []
+        while at < n:
+            got.append((out[at], list(out[at + 2:at + 2 + out[at + 1]])))
+            at += 2 + out[at + 1]
+        return got
+
     small = [(8, 8)] * 40
-    assert call(plan.together, small, 0) == 16 and call(plan.together, small, 32) == 8
+    assert launches(small) == [(128, list(range(0, 16))), (128, list(range(16, 32))), (128, list(range(32, 40)))]
     assert call(plan.bytes, small) == 16 * plan.one(8, 8)
-    large = [(8192, 8192), (8192, 8192), (64, 64)]      # each fills launches by itself
-    assert call(plan.together, large, 0) == 1 and call(plan.together, large, 1) == 1
-    assert call(plan.bytes, large) == plan.one(8192, 8192)
-    assert call(plan.bytes, [(4096, 4096)] * 4) == 4 * plan.one(4096, 4096)
+    # tiles of either size apart, the longest first, nothing for a side of 0, and no more than fits together
+    mixed = [(64, 64), (4096, 4096), (0, 7), (4096, 11008), (100, 300)]
+    assert launches(mixed) == [(256, [3, 1]), (128, [4, 0])] and launches([(64, 64), (600, 900)]) == [(128, [1, 0])]
+    assert launches([(64, 64), (600, 900), (2048, 2048)], 1) == [(256, [2]), (128, [1]), (128, [0])]   # (products to a step differ)
+    assert call(plan.bytes, mixed) == plan.one(4096, 4096) + plan.one(4096, 11008)
+    large = [(16384, 16384), (16384, 16384), (64, 64)]
+    assert launches(large) == [(256, [0]), (256, [1]), (128, [2])] and call(plan.bytes, large) == plan.one(16384, 16384)
