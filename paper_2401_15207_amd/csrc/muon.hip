@@ -13,8 +13,10 @@
 // the roundings of the two diagonals leave, which no sum averages out, is put back by the epilogues (a_rest, b_rest).  Simulated in 64 bits on random,
 // low-rank (noise 1e-3 of it) and decaying (1e-6) matrices of 512 x 512 .. 2048: 3e-4 to 1.3e-3 off in the 2-norm, half as far as the
 // rounding to bf16 itself; with single numbers throughout 3e-3, and 3e-2 where the rank is low.
-// Factors lie in the matrix instruction's register order: blocks of 32 rows x 16 k, 1 KB of high and 1 KB of low numbers, lane l of a
-// wavefront holding row l % 32 and k 8 (l / 32) .. +7 of it, so that a fragment is one contiguous load; blocks along k follow each other.
+// Factors lie in the matrix instruction's register order: blocks of 32 rows x 16 k, 1 KB of high or of low numbers, lane l of a wavefront
+// holding row l % 32 and k 8 (l / 32) .. +7 of it, so that a fragment is one contiguous load; blocks along k follow each other, high and
+// low ones apart (side by side, A of high numbers alone took 39 us instead of 36 in a layer 1024 wide).
+#include <limits.h>
 #include <math.h>
 
 #include "common.h"
@@ -28,11 +30,12 @@ typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef _Float16 half4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-// A factor of rows x k entries (multiples of 32 and 16): block (row / 32, k / 16) starts 1024 ((row / 32) (k total / 16) + k / 16) numbers in.
+// A factor of rows x k entries (multiples of 32 and 16): for every 32 rows the blocks of their high numbers along k, then those of the low ones.
 struct Factor {
   _Float16* p;
   int kb;  // blocks along k
-  __device__ __forceinline__ _Float16* block(int rb, int b) const { return p + ((int64_t)rb * kb + b) * 1024; }
+  __device__ __forceinline__ _Float16* block(int rb, int b) const { return p + ((int64_t)rb * 2 * kb + b) * 512; }
+  __device__ __forceinline__ int low() const { return kb * 512; }  // from a high number to its low one
 };
 
 struct NsMatrix {
@@ -49,18 +52,22 @@ struct NsMatrix {
   float *a_rest, *b_rest;  // [n] of A's and B's diagonal what the high numbers leave (fewer products)
   double* norm_parts;
   int* small;           // how many powers of two X is below 1 at the start (norms below eps; ns_start_k)
-  int block0;           // first workgroup of the launch that works on it
+  int parts;            // workgroups that share the k range of one of its tiles
 };
+// first[i]: the first workgroup of a launch that works on matrix i; from `count` on, beyond all of them.
 struct NsTable {
+  int first[NS_TABLE];
   int count;
   NsMatrix m[NS_TABLE];
 };
 static_assert(sizeof(NsTable) < 3500, "kernel arguments");
 
-__device__ __forceinline__ const NsMatrix& matrix_of(const NsTable& t, int block) {
+// (all of `first` in one load and a comparison each: a search would wait for memory at every step)
+__device__ __forceinline__ int matrix_of(const NsTable& t, int block) {
   int i = 0;
-  while (i + 1 < t.count && block >= t.m[i + 1].block0) ++i;
-  return t.m[i];
+#pragma unroll
+  for (int j = 1; j < NS_TABLE; ++j) i += block >= t.first[j];
+  return __builtin_amdgcn_readfirstlane(i);
 }
 
 __device__ __forceinline__ void split(float v, _Float16& hi, _Float16& lo) {
@@ -72,10 +79,12 @@ __device__ __forceinline__ void split(float v, _Float16& hi, _Float16& lo) {
 // Sums of squares in 64 bits (an entry's square may pass fp32's range either way), NS_NORM_PARTS of them a matrix; with a momentum buffer,
 // that is updated on the way.
 template <typename T>
-__global__ void __launch_bounds__(256) ns_norm_k(NsTable t, float mu) {
+__global__ void __launch_bounds__(256) ns_norm_k(NsTable t, float mu, unsigned* shared) {
   __shared__ double red[4];
-  const NsMatrix& q = matrix_of(t, blockIdx.x);
-  const int part = blockIdx.x - q.block0;
+  const int at = matrix_of(t, blockIdx.x), part = blockIdx.x - t.first[at];
+  const NsMatrix& q = t.m[at];
+  if (blockIdx.x == 0)  // the counters of shared tiles; who counts last leaves 0 again
+    for (int i = threadIdx.x; i < NS_SHARED_UNITS; i += 256) shared[i] = 0;
   double s = 0.0;
   const int64_t per = (q.rows + NS_NORM_PARTS - 1) / NS_NORM_PARTS;
   const int64_t r1 = min(q.rows, (part + 1) * per);
@@ -102,7 +111,8 @@ template <typename T>
 __global__ void __launch_bounds__(256) ns_start_k(NsTable t, float mu, float eps, float scale) {
   __shared__ float tile[64][65];
   __shared__ double red[4];
-  const NsMatrix& q = matrix_of(t, blockIdx.x);
+  const int at = matrix_of(t, blockIdx.x), id = blockIdx.x - t.first[at];
+  const NsMatrix& q = t.m[at];
   const int th = threadIdx.x, lane = th & 63;
   static_assert(NS_NORM_PARTS == 256, "one part a thread");
   double s = q.norm_parts[th];
@@ -114,10 +124,10 @@ __global__ void __launch_bounds__(256) ns_start_k(NsTable t, float mu, float eps
   // which lets X grow by less than 2^growth, times 2^(small - k growth) as long as that is above 1.
   const int below = norm > 0.0 && norm < (double)eps ? min((int)floor(log2((double)eps / norm)), 200) : 0;
   const double by = ldexp((double)scale, below) / (norm < (double)eps ? (double)eps : norm);  // (a norm that is no number stays one)
-  if (blockIdx.x == q.block0 && th == 0) *q.small = below;
+  if (id == 0 && th == 0) *q.small = below;
   // sides as they lie in memory, filled up
   const int R = q.tall ? q.m : q.n, C = q.tall ? q.n : q.m;
-  const int tiles_c = C / 64, id = blockIdx.x - q.block0;
+  const int tiles_c = C / 64;
   const int64_t r0 = (int64_t)(id / tiles_c) * 64, c0 = (int64_t)(id % tiles_c) * 64;
   for (int i = th >> 6; i < 64; i += 4) {
     const int64_t r = r0 + i, c = c0 + lane;
@@ -143,7 +153,7 @@ __global__ void __launch_bounds__(256) ns_start_k(NsTable t, float mu, float eps
     }
     _Float16* p = along.block((int)(r0 / 32) + rb, (int)(c0 / 16) + kb) + lane * 8;
     *reinterpret_cast<half8*>(p) = hi;
-    *reinterpret_cast<half8*>(p + 512) = lo;
+    *reinterpret_cast<half8*>(p + along.low()) = lo;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       _Float16 h, l;
@@ -152,7 +162,7 @@ __global__ void __launch_bounds__(256) ns_start_k(NsTable t, float mu, float eps
     }
     p = across.block((int)(c0 / 32) + rb, (int)(r0 / 16) + kb) + lane * 8;
     *reinterpret_cast<half8*>(p) = hi;
-    *reinterpret_cast<half8*>(p + 512) = lo;
+    *reinterpret_cast<half8*>(p + across.low()) = lo;
   }
 }
 
@@ -168,6 +178,7 @@ struct NsStep {
   float out_scale;      // of the factor that is written
   float ca, cb, cc;     // NS_POLY: coefficients, b's with A's scale taken out
   float decay;          // NS_LAST: 1 - lr wd
+  unsigned char* shared;  // where workgroups that share a tile meet: a counter for each tile, and their sums
   int grown, growth;    // powers of two that X may have grown by before this step, and in it
 };
 
@@ -189,15 +200,13 @@ __device__ __forceinline__ void put_block(const Factor& rows_j, const Factor& ro
       _Float16 h, l;
       split(v[4 * g + e], h, l);
       hi[e] = h; lo[e] = l;
-      if (other) {
-        typedef _Float16 half2 __attribute__((ext_vector_type(2)));
-        const half2 both = {h, l};
-        turned[acc_row(4 * g + e, lane) * TURN_PITCH + (lane & 31)] = __builtin_bit_cast(uint32_t, both);
-      }
+      typedef _Float16 half2 __attribute__((ext_vector_type(2)));
+      const half2 both = {h, l};
+      turned[acc_row(4 * g + e, lane) * TURN_PITCH + (lane & 31)] = __builtin_bit_cast(uint32_t, both);
     }
     _Float16* p = rows_j.block(j0 / 32, i0 / 16 + (g >> 1)) + ((lane & 31) + 32 * (g & 1)) * 8 + 4 * (lane >> 5);
     *reinterpret_cast<half4*>(p) = hi;
-    if (LOW_J) *reinterpret_cast<half4*>(p + 512) = lo;
+    if (LOW_J) *reinterpret_cast<half4*>(p + rows_j.low()) = lo;
   }
   if (!other) return;
   __builtin_amdgcn_wave_barrier();  // (a wavefront's own LDS accesses stay in order)
@@ -214,7 +223,7 @@ __device__ __forceinline__ void put_block(const Factor& rows_j, const Factor& ro
     }
     _Float16* p = rows_i.block(i0 / 32, j0 / 16 + b) + lane * 8;
     *reinterpret_cast<hift_u32x4*>(p) = hift_u32x4{hi[0], hi[1], hi[2], hi[3]};
-    if (LOW_I) *reinterpret_cast<hift_u32x4*>(p + 512) = hift_u32x4{lo[0], lo[1], lo[2], lo[3]};
+    if (LOW_I) *reinterpret_cast<hift_u32x4*>(p + rows_i.low()) = hift_u32x4{lo[0], lo[1], lo[2], lo[3]};
   }
   __builtin_amdgcn_wave_barrier();
 }
@@ -224,27 +233,30 @@ __device__ __forceinline__ const _Float16* at_block(const Factor& rows_j, int i0
   return rows_j.block(j0 / 32, i0 / 16 + (g >> 1)) + ((lane & 31) + 32 * (g & 1)) * 8 + 4 * (lane >> 5);
 }
 
-// Tiles of 256 x 256 by 2 x 4 wavefronts, of 128 x 128 by 2 x 2.  Both operands travel into LDS with direct-to-LDS loads, as they lie, into a
-// ring of stages of 16 or 32 k; a stage's fragments are read into registers under the products of the stage before.
+// Tiles of 256 x 256 by 2 x 4 wavefronts, of 128 x 128 and 64 x 64 by 2 x 2.  Both operands travel into LDS with direct-to-LDS loads, as they
+// lie, into a ring of stages of 16 to 64 k; a stage's fragments are read into registers under the products of the stage before.
 // PP, QP: numbers of P and Q that take part: 2 and 2 (three products), 1 and 2 (two), 1 and 1 (one).
-template <int SIDE, int PP, int QP>
+// DEEP: the ring of a launch that gives a compute unit one workgroup at most.  That one waits for memory by itself: a stage of 16 KB takes
+// the time of its requests' latency over the stages in flight, so the ring takes most of the LDS.
+template <int SIDE, int PP, int QP, bool DEEP>
 struct NsTile {
   static constexpr int WI = 2, WJ = SIDE == 256 ? 4 : 2, NW = WI * WJ;
   static constexpr int BI = SIDE / 32 / WI, BJ = SIDE / 32 / WJ;   // blocks of 32 x 32 a wavefront
-  static constexpr int KS = PP + QP == 2 ? 2 : 1;                  // blocks along k of a stage
+  static constexpr int KS = SIDE == 64 ? 4 : PP + QP == 2 ? 2 : 1; // blocks along k of a stage
   static constexpr int PN = SIDE / 32 * KS * PP, PIECES = PN + SIDE / 32 * KS * QP;  // KB of P in a stage, and of both
   static constexpr int LOADS = PIECES / NW;                        // load instructions a wavefront and stage, 1 KB each
-  static constexpr int STAGE = PIECES * 1024, RING = SIDE == 256 ? 4 : 3, LDS = RING * STAGE;
+  static constexpr int STAGE = PIECES * 1024, RING = SIDE == 256 || (SIDE == 64 && DEEP) ? 4 : SIDE == 64 ? 2 : DEEP ? 8 : 3, LDS = RING * STAGE;
   static_assert(PIECES % NW == 0 && LDS <= 160 * 1024 && NW * 32 * TURN_PITCH * 4 <= LDS, "blocks turn in the ring");
 };
 
-template <int SIDE, int MODE, int PP, int QP, typename OUT>
-__global__ void __launch_bounds__((64 * NsTile<SIDE, PP, QP>::NW), 2) ns_product_k(NsTable t, NsStep st) {
-  typedef NsTile<SIDE, PP, QP> T;
+template <int SIDE, int MODE, int PP, int QP, bool DEEP, typename OUT>
+__global__ void __launch_bounds__((64 * NsTile<SIDE, PP, QP, DEEP>::NW), (DEEP && SIDE < 256 ? 1 : 2)) ns_product_k(NsTable t, NsStep st) {
+  typedef NsTile<SIDE, PP, QP, DEEP> T;
   constexpr int BI = T::BI, BJ = T::BJ, RING = T::RING, KS = T::KS;
   constexpr bool FEW = PP + QP < 4;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-  const NsMatrix& q = matrix_of(t, blockIdx.x);
+  const int at = matrix_of(t, blockIdx.x), block0 = t.first[at];
+  const NsMatrix& q = t.m[at];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // Workgroups are dealt round-robin to the 8 XCDs (every matrix starts at a multiple of 8): each XCD gets a contiguous run of tiles, so
@@ -252,10 +264,12 @@ __global__ void __launch_bounds__((64 * NsTile<SIDE, PP, QP>::NW), 2) ns_product
   constexpr bool SYM = MODE == NS_GRAM || MODE == NS_POLY;
   const bool turn = MODE == NS_LAST && q.tall;  // dst's columns along the lanes
   const int side_i = (turn ? q.m : q.n) / SIDE, side_j = (SYM || turn ? q.n : q.m) / SIDE;
-  const int tiles = SYM ? side_i * (side_i + 1) / 2 : side_i * side_j;
-  int id = blockIdx.x - q.block0;
-  id = (id & 7) * ((tiles + 7) >> 3) + (id >> 3);
-  if (id >= tiles) return;
+  const int units = (SYM ? side_i * (side_i + 1) / 2 : side_i * side_j) * q.parts;
+  int id = blockIdx.x - block0;
+  id = (id & 7) * ((units + 7) >> 3) + (id >> 3);
+  if (id >= units) return;
+  const int unit = block0 + id, part = id % q.parts;
+  id /= q.parts;
   Factor P, Q;
   int ti, tj;
   if (SYM) {
@@ -274,7 +288,7 @@ __global__ void __launch_bounds__((64 * NsTile<SIDE, PP, QP>::NW), 2) ns_product
     tj = in_band / rows;
   }
   const int small = *q.small, up = max(0, small - st.grown);  // X is stored times 2^up
-  const int stages = P.kb / KS;
+  const int all = P.kb / KS, first = all * part / q.parts, stages = all * (part + 1) / q.parts;  // this workgroup's: [first, stages)
 
   const uint64_t pa = reinterpret_cast<uint64_t>(P.block(ti * (SIDE / 32), 0)), qa = reinterpret_cast<uint64_t>(Q.block(tj * (SIDE / 32), 0));
   const uint32_t lds0 = (uint32_t)reinterpret_cast<uintptr_t>(smem), voff = lane * 16;
@@ -288,7 +302,7 @@ __global__ void __launch_bounds__((64 * NsTile<SIDE, PP, QP>::NW), 2) ns_product
       const int in = is_q ? load - T::PN : load, planes = is_q ? QP : PP, rb = in / (KS * planes), rest = in % (KS * planes);
       const uint64_t base = is_q ? qa : pa;
       const hift_u32x4 rsrc = {(uint32_t)base, (uint32_t)(base >> 32) & 0xFFFFu, 0xFFFFFFF0u, 0x00020000u};
-      const uint32_t soff = ((uint32_t)rb * P.kb + s * KS + rest / planes) * 2048u + (rest % planes) * 1024u;
+      const uint32_t soff = (((uint32_t)rb * 2 + rest % planes) * P.kb + s * KS + rest / planes) * 1024u;
       load_to_lds_b128(rsrc, at + (uint32_t)load * 1024, voff, soff);
     }
   };
@@ -321,11 +335,11 @@ __global__ void __launch_bounds__((64 * NsTile<SIDE, PP, QP>::NW), 2) ns_product
   };
 #pragma unroll
   for (int s = 0; s < RING; ++s)
-    if (s < stages) request(s);
-  if (RING <= stages) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((RING - 1) * T::LOADS) : "memory");
+    if (first + s < stages) request(first + s);
+  if (first + RING <= stages) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((RING - 1) * T::LOADS) : "memory");
   else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
-  read(0, 0);
+  read(0, first);
   // Past the wait the stage after s has landed (all but the younger stages' requests), and past the barrier s's buffer, whose fragments every
   // wavefront has, is free for the stage a whole ring further on.  Near the end fewer requests are in flight: there the wait is for all.
   auto stage = [&](int s, int c, bool tail) __attribute__((always_inline)) {
@@ -337,15 +351,60 @@ __global__ void __launch_bounds__((64 * NsTile<SIDE, PP, QP>::NW), 2) ns_product
     multiply(c);
     __builtin_amdgcn_sched_barrier(0);
   };
-  int s = 0;
+  int s = first;
   for (; s + 1 + RING < stages; s += 2) {
     stage(s, 0, false);
     stage(s + 1, 1, false);
   }
-  // (the number of stages is even)
   for (; s < stages; s += 2) {
     stage(s, 0, true);
-    stage(s + 1, 1, true);
+    if (s + 1 < stages) stage(s + 1, 1, true);
+  }
+
+  if (SIDE < 256 && q.parts > 1) {
+    // Every one of them leaves its sums in memory and counts itself in; the one that finds all others counted adds them up in their order
+    // (its own too: the result must not depend on who came last) and goes on.  Nobody waits.  They run on different XCDs, so the sums go past the
+    // L2s both ways (device scope).
+    constexpr int SC1 = 16, BYTES = SIDE * SIDE * 4;
+    int* is_last = reinterpret_cast<int*>(smem);
+    unsigned* count = reinterpret_cast<unsigned*>(st.shared) + (unit - part);
+    const __amdgpu_buffer_rsrc_t sums = __builtin_amdgcn_make_buffer_rsrc(st.shared + NS_SHARED_UNITS * 4 + (int64_t)(unit - part) * BYTES, 0, q.parts * BYTES, 0x00020000);
+    const int mine = threadIdx.x * 16;
+    typedef float f32x4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int x = 0; x < BI; ++x)
+#pragma unroll
+      for (int y = 0; y < BJ; ++y)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const f32x4 v = {acc[x][y][4 * g], acc[x][y][4 * g + 1], acc[x][y][4 * g + 2], acc[x][y][4 * g + 3]};
+          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(hift_u32x4, v), sums, mine + part * BYTES, ((x * BJ + y) * 4 + g) * T::NW * 1024, SC1);
+        }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this lane's sums have reached memory
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      const unsigned before = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      *is_last = before == (unsigned)q.parts - 1;
+      if (*is_last) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    if (!*is_last) return;
+    for (int u = 0; u < q.parts; ++u) {  // a part's sums are all requested before the first is added
+      f32x4 v[BI][BJ][4];
+#pragma unroll
+      for (int x = 0; x < BI; ++x)
+#pragma unroll
+        for (int y = 0; y < BJ; ++y)
+#pragma unroll
+          for (int g = 0; g < 4; ++g)
+            v[x][y][g] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(sums, mine + u * BYTES, ((x * BJ + y) * 4 + g) * T::NW * 1024, SC1));
+#pragma unroll
+      for (int x = 0; x < BI; ++x)
+#pragma unroll
+        for (int y = 0; y < BJ; ++y)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) acc[x][y][e] = u == 0 ? v[x][y][e >> 2][e & 3] : acc[x][y][e] + v[x][y][e >> 2][e & 3];
+    }
   }
 
   __syncthreads();  // the ring is free: nothing is on its way there either
@@ -363,7 +422,7 @@ __global__ void __launch_bounds__((64 * NsTile<SIDE, PP, QP>::NW), 2) ns_product
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
           const _Float16* f = at_block(a, i, j, g, lane);
-          const half4 hi = *reinterpret_cast<const half4*>(f), lo = *reinterpret_cast<const half4*>(f + 512);
+          const half4 hi = *reinterpret_cast<const half4*>(f), lo = *reinterpret_cast<const half4*>(f + a.low());
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int row = i + acc_row(4 * g + e, lane);
@@ -426,21 +485,18 @@ template <class F>
 uint32_t spread(NsTable& t, F blocks) {
   int64_t at = 0;
   for (int i = 0; i < t.count; ++i) {
-    t.m[i].block0 = (int)at;
+    t.first[i] = (int)at;
     at += blocks(t.m[i]);
   }
+  for (int i = t.count; i < NS_TABLE; ++i) t.first[i] = INT_MAX;
   return (uint32_t)at;
 }
 
-template <int SIDE, int MODE, int PP, int QP, typename OUT = float>
-hipError_t product(NsTable& t, const NsStep& p, hipStream_t st) {
-  typedef NsTile<SIDE, PP, QP> T;
-  const uint32_t blocks = spread(t, [](const NsMatrix& q) {
-    const int64_t n = q.n / SIDE, tiles = MODE == NS_GRAM || MODE == NS_POLY ? n * (n + 1) / 2 : n * (q.m / SIDE);
-    return (tiles + 7) / 8 * 8;
-  });
+template <int SIDE, int MODE, int PP, int QP, bool DEEP, typename OUT>
+hipError_t launch_product(uint32_t blocks, const NsTable& t, const NsStep& p, hipStream_t st) {
+  typedef NsTile<SIDE, PP, QP, DEEP> T;
   static bool attr_done = false;  // one flag per instantiation
-  const auto kern = ns_product_k<SIDE, MODE, PP, QP, OUT>;
+  const auto kern = ns_product_k<SIDE, MODE, PP, QP, DEEP, OUT>;
   if (!attr_done) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS);
     if (e != hipSuccess) return e;
@@ -449,23 +505,61 @@ hipError_t product(NsTable& t, const NsStep& p, hipStream_t st) {
   kern<<<blocks, 64 * T::NW, T::LDS, st>>>(t, p);
   return hipGetLastError();
 }
-
-// The products of one step.  FEW: one product each for A, A A and the last B X, two for the others.
-template <int SIDE, bool FEW>
-hipError_t step_of(NsTable& t, const NsStep& gram, const NsStep& poly, const NsStep& apply, bool last, int dt_dst, hipStream_t st) {
-  constexpr int ONE = FEW ? 1 : 2;
-  hipError_t e = product<SIDE, NS_GRAM, ONE, ONE>(t, gram, st);
-  if (e == hipSuccess) e = product<SIDE, NS_POLY, ONE, ONE>(t, poly, st);
-  if (e != hipSuccess) return e;
-  if (!last) return product<SIDE, NS_APPLY, ONE, 2>(t, apply, st);
-  if (dt_dst == DT_BF16) return product<SIDE, NS_LAST, ONE, ONE, bf16>(t, apply, st);
-  return product<SIDE, NS_LAST, ONE, ONE>(t, apply, st);
+// Workgroups of a product with tiles of SIDE, when each has `most` stages at most
+template <int SIDE, int MODE, int PP, int QP>
+int64_t units_of(NsMatrix& q, int64_t most) {
+  const int64_t n = q.n / SIDE, tiles = MODE == NS_GRAM || MODE == NS_POLY ? n * (n + 1) / 2 : n * (q.m / SIDE);
+  const int64_t stages = (MODE == NS_GRAM ? q.m : q.n) / (16 * NsTile<SIDE, PP, QP, true>::KS);
+  q.parts = (int)((stages + most - 1) / most);
+  return (tiles * q.parts + 7) / 8 * 8;
+}
+template <int SIDE, int MODE, int PP, int QP, typename OUT>
+hipError_t product_of(NsTable& t, const NsStep& p, hipStream_t st) {
+  int64_t most = 1 << 20;
+  if (SIDE < 256) {
+    // the shortest k ranges whose workgroups fit side by side
+    for (most = NS_SHARED_STAGES; most < 1 << 20; most *= 2) {
+      int64_t all = 0;
+      for (int i = 0; i < t.count; ++i) all += units_of<SIDE, MODE, PP, QP>(t.m[i], most);
+      if (all <= NS_SHARED_UNITS) break;
+    }
+  }
+  const uint32_t blocks = spread(t, [&](NsMatrix& q) { return units_of<SIDE, MODE, PP, QP>(q, most); });
+  if (SIDE < 256 && blocks <= 256) return launch_product<SIDE, MODE, PP, QP, true, OUT>(blocks, t, p, st);
+  return launch_product<SIDE, MODE, PP, QP, false, OUT>(blocks, t, p, st);
+}
+// Tiles as large as the sides' filling allows and a launch still has enough of.
+template <int MODE, int PP, int QP, typename OUT = float>
+hipError_t product(NsTable& t, int side, const NsStep& p, hipStream_t st) {
+  const auto tiles = [&](int64_t by) {
+    int64_t all = 0;
+    for (int i = 0; i < t.count; ++i) {
+      const int64_t n = t.m[i].n / by;
+      all += MODE == NS_GRAM || MODE == NS_POLY ? n * (n + 1) / 2 : n * (t.m[i].m / by);
+    }
+    return all;
+  };
+  if (side >= 256 && tiles(256) >= NS_TILES_256) return product_of<256, MODE, PP, QP, OUT>(t, p, st);
+  if (side >= 128 && tiles(128) >= NS_TILES_128) return product_of<128, MODE, PP, QP, OUT>(t, p, st);
+  return product_of<64, MODE, PP, QP, OUT>(t, p, st);
 }
 
-hipError_t steps_of(NsTable& t, int side, int dt_src, int dt_dst, const NsRun& run, bool few, hipStream_t st) {
+// The products of one step.  FEW: one product each for A, A A and the last B X, two for the others.
+template <bool FEW>
+hipError_t step_of(NsTable& t, int side, const NsStep& gram, const NsStep& poly, const NsStep& apply, bool last, int dt_dst, hipStream_t st) {
+  constexpr int ONE = FEW ? 1 : 2;
+  hipError_t e = product<NS_GRAM, ONE, ONE>(t, side, gram, st);
+  if (e == hipSuccess) e = product<NS_POLY, ONE, ONE>(t, side, poly, st);
+  if (e != hipSuccess) return e;
+  if (!last) return product<NS_APPLY, ONE, 2>(t, side, apply, st);
+  if (dt_dst == DT_BF16) return product<NS_LAST, ONE, ONE, bf16>(t, side, apply, st);
+  return product<NS_LAST, ONE, ONE>(t, side, apply, st);
+}
+
+hipError_t steps_of(NsTable& t, int side, int dt_src, int dt_dst, const NsRun& run, bool few, unsigned char* shared, hipStream_t st) {
   const uint32_t parts = spread(t, [](const NsMatrix&) { return NS_NORM_PARTS; });
-  if (dt_src == DT_BF16) ns_norm_k<bf16><<<parts, 256, 0, st>>>(t, run.mu);
-  else ns_norm_k<float><<<parts, 256, 0, st>>>(t, run.mu);
+  if (dt_src == DT_BF16) ns_norm_k<bf16><<<parts, 256, 0, st>>>(t, run.mu, reinterpret_cast<unsigned*>(shared));
+  else ns_norm_k<float><<<parts, 256, 0, st>>>(t, run.mu, reinterpret_cast<unsigned*>(shared));
   double r = 1.001;  // the norm is at least the largest singular value, but for rounding
   NsScales s;
   if (!ns_scales(run.co, r, &s)) return hipErrorInvalidValue;
@@ -475,6 +569,7 @@ hipError_t steps_of(NsTable& t, int side, int dt_src, int dt_dst, const NsRun& r
   else ns_start_k<float><<<squares, 256, 0, st>>>(t, run.mu, run.eps, s.x);
   for (int k = 0; k < run.steps; ++k) {
     NsStep gram{}, poly{}, apply{};
+    gram.shared = poly.shared = apply.shared = shared;
     gram.grown = apply.grown = k * growth;
     gram.growth = apply.growth = growth;
     gram.unscale = 1.f / (s.x * s.x);
@@ -489,8 +584,7 @@ hipError_t steps_of(NsTable& t, int side, int dt_src, int dt_dst, const NsRun& r
     if (!ns_scales(run.co, r, &s)) return hipErrorInvalidValue;
     apply.out_scale = s.x;
     const bool last = k + 1 == run.steps;
-    const auto step = side == 256 ? (few ? step_of<256, true> : step_of<256, false>) : (few ? step_of<128, true> : step_of<128, false>);
-    const hipError_t e = step(t, gram, poly, apply, last, dt_dst, st);
+    const hipError_t e = (few ? step_of<true> : step_of<false>)(t, side, gram, poly, apply, last, dt_dst, st);
     if (e != hipSuccess) return e;
     if (!last)
       for (int i = 0; i < t.count; ++i) std::swap(t.m[i].xt, t.m[i].xt2);
@@ -519,7 +613,7 @@ hipError_t newton_schulz(const NsItem* items, int count, int dt_src, int dt_dst,
   hipError_t err = hipSuccess;
   ns_launches(count, run.few, [&](int i, int64_t* r, int64_t* c) { *r = items[i].rows; *c = items[i].cols; }, [&](const int* which, int n, int side, bool large) {
     NsTable t{};
-    unsigned char* ws = reinterpret_cast<unsigned char*>(workspace);
+    unsigned char* ws = reinterpret_cast<unsigned char*>(workspace) + NS_SHARED_BYTES;
     for (int i = 0; i < n; ++i) {
       const NsItem& it = items[which[i]];
       NsMatrix& q = t.m[t.count++];
@@ -547,7 +641,7 @@ hipError_t newton_schulz(const NsItem* items, int count, int dt_src, int dt_dst,
       q.small = reinterpret_cast<int*>(ws);
       ws += 16;
     }
-    if (err == hipSuccess) err = steps_of(t, side, dt_src, dt_dst, run, large, st);
+    if (err == hipSuccess) err = steps_of(t, side, dt_src, dt_dst, run, large, reinterpret_cast<unsigned char*>(workspace), st);
   });
   return err;
 }

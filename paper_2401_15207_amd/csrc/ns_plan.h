@@ -54,8 +54,16 @@ constexpr int64_t NS_SIDE_MAX = 65536;
 // Matrices share launches until together they have this many entries: a few large ones fill the last round of a launch's tiles over the
 // 256 compute units, more would only need more work space.
 constexpr int64_t NS_TOGETHER = int64_t(1) << 28;
-// Tiles of a matrix's products; both of its sides are filled up with zeros to a multiple.  256 x 256 where at least 64 of them cover it.
+// Both sides of a matrix are filled up with zeros to a multiple of this, the largest tile its products can have: 256 where at least 64
+// such tiles cover it, else 128; 64 in launches that would have fewer than NS_FEW_TILES of 128 in the symmetric products.
+constexpr int64_t NS_FEW_TILES = 160;
 inline int ns_side(int64_t rows, int64_t cols) { return std::min(rows, cols) >= 1280 && rows * cols >= int64_t(64) * 256 * 256 ? 256 : 128; }
+// From how many tiles on a launch takes them that large.
+constexpr int64_t NS_TILES_256 = 192, NS_TILES_128 = 128;
+// Workgroups that share tiles' k ranges, in launches that have fewer workgroups than this otherwise; no range is shorter than so many
+// stages.  Their sums: 64 KB (128 x 128) each, and a counter.
+constexpr int64_t NS_SHARED_UNITS = 304, NS_SHARED_STAGES = 8;
+constexpr size_t NS_SHARED_BYTES = NS_SHARED_UNITS * (4 + 128 * 128 * 4);
 
 // Whose products are fewer for a bf16 result: smaller ones are bound by latency, and further off with them.
 inline bool ns_large(int64_t rows, int64_t cols) { return std::min(rows, cols) >= 512; }
@@ -78,11 +86,11 @@ inline void ns_launches(int count, bool few, S shape, F launch) {
     const int side = kind == 0 ? 256 : 128;
     const bool large = few && kind < 2;
     int which[NS_TABLE], n = 0;
-    int64_t entries = 0, longest[NS_TABLE];
+    int64_t entries = 0, tiles = 0, longest[NS_TABLE];
     const auto flush = [&]() {
-      if (n > 0) launch((const int*)which, n, side, large);
+      if (n > 0) launch((const int*)which, n, side == 128 && !large && tiles < NS_FEW_TILES ? 64 : side, large);
       n = 0;
-      entries = 0;
+      entries = tiles = 0;
     };
     for (int i = 0; i < count; ++i) {
       int64_t r, c;
@@ -97,6 +105,8 @@ inline void ns_launches(int count, bool few, S shape, F launch) {
       which[at] = i;
       longest[at] = std::max(r, c);
       entries += r * c;
+      const int64_t t = ns_up(std::min(r, c), side) / side;
+      tiles += t * (t + 1) / 2;
     }
     flush();
   }
@@ -112,7 +122,7 @@ inline size_t ns_workspace_bytes(int count, S shape) {
         shape(which[i], &r, &c);
         sum += ns_bytes(r, c);
       }
-      most = std::max(most, sum);
+      most = std::max(most, NS_SHARED_BYTES + sum);
     });
   return most;
 }

@@ -30,6 +30,7 @@ extern "C" size_t bytes(int count, const long long* s) {
   return ns_workspace_bytes(count, [&](int i, int64_t* r, int64_t* c) { *r = s[2 * i]; *c = s[2 * i + 1]; });
 }
 extern "C" size_t one(long long r, long long c) { return ns_bytes(r, c); }
+extern "C" size_t shared() { return NS_SHARED_BYTES; }
 """
 
 
@@ -40,7 +41,7 @@ def plan(tmp_path_factory):
     src.write_text(CODE)
     subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-shared", "-fPIC", "-I", CSRC, str(src), "-o", str(so)], check=True)
     lib = ctypes.CDLL(str(so))
-    lib.bytes.restype = lib.one.restype = ctypes.c_size_t
+    lib.bytes.restype = lib.one.restype = lib.shared.restype = ctypes.c_size_t
     lib.one.argtypes = [ctypes.c_longlong] * 2
     return lib
 
@@ -90,12 +91,14 @@ def test_work_space_and_launches(plan):
         return got
 
     small = [(8, 8)] * 40
-    assert launches(small) == [(128, list(range(0, 16))), (128, list(range(16, 32))), (128, list(range(32, 40)))]
-    assert call(plan.bytes, small) == 16 * plan.one(8, 8)
+    assert launches(small) == [(64, list(range(0, 16))), (64, list(range(16, 32))), (64, list(range(32, 40)))]
+    assert call(plan.bytes, small) == plan.shared() + 16 * plan.one(8, 8)
     # tiles of either size apart, the longest first, nothing for a side of 0, and no more than fits together
     mixed = [(64, 64), (4096, 4096), (0, 7), (4096, 11008), (100, 300)]
-    assert launches(mixed) == [(256, [3, 1]), (128, [4, 0])] and launches([(64, 64), (600, 900)]) == [(128, [1, 0])]
-    assert launches([(64, 64), (600, 900), (2048, 2048)], 1) == [(256, [2]), (128, [1]), (128, [0])]   # (products to a step differ)
-    assert call(plan.bytes, mixed) == plan.one(4096, 4096) + plan.one(4096, 11008)
+    assert launches(mixed) == [(256, [3, 1]), (64, [4, 0])] and launches([(64, 64), (600, 900)]) == [(64, [1, 0])]
+    assert launches([(64, 64), (600, 900), (2048, 2048)], 1) == [(256, [2]), (128, [1]), (64, [0])]   # (products to a step differ)
+    assert call(plan.bytes, mixed) == plan.shared() + plan.one(4096, 4096) + plan.one(4096, 11008)
     large = [(16384, 16384), (16384, 16384), (64, 64)]
-    assert launches(large) == [(256, [0]), (256, [1]), (128, [2])] and call(plan.bytes, large) == plan.one(16384, 16384)
+    assert launches(large) == [(256, [0]), (256, [1]), (64, [2])]
+    assert launches([(1024, 1024)] * 6) == [(128, [0, 1, 2, 3, 4, 5])]
+    assert call(plan.bytes, large) == plan.shared() + plan.one(16384, 16384)
