@@ -15,7 +15,8 @@ namespace hift {
 namespace {
 
 constexpr float LOG2E = 1.44269504088896340736f;
-constexpr double LN2 = 0.69314718055994530942;
+constexpr float LN2_HI = 0.69314718246459960938f, LN2_LO = -1.904654299957767e-9f;  // ln 2 = LN2_HI + LN2_LO
+constexpr float LOWEST = -3.402823466e38f;
 constexpr int CANDIDATES = 1024;  // entries that may be at or above a row's threshold before it goes the slow way
 
 struct LogprobArgs {
@@ -39,32 +40,73 @@ __device__ __forceinline__ float unordered(uint32_t o) { return __uint_as_float(
 __device__ __forceinline__ uint64_t top_key(float x, int id) { return (uint64_t)ordered(x) << 32 | (0xFFFFFFFFu - (uint32_t)id); }
 __device__ __forceinline__ int key_id(uint64_t k) { return (int)(0xFFFFFFFFu - (uint32_t)k); }
 
-// A row seen by a workgroup of NT threads: pieces of 16 bytes from its first aligned element on, thread t taking t, t + NT, ..., and the
-// elements before and after them (fewer than a piece at either end), one each for the first threads.
-template <typename T, int NT>
-struct RowOf {
+// A row seen by a workgroup of NT threads: pieces of 16 bytes from its first aligned element on, thread t taking t, t + NT, ..., U at a time,
+// and the elements before and after them (fewer than a piece at either end), one each for the first threads.
+template <typename T>
+struct Piece {
   static constexpr int E = 16 / (int)sizeof(T);
-  const T* x;
-  int V, head, pieces, tail;
-  __device__ RowOf(const T* row, int V_) : x(row), V(V_) {
-    head = min(V, (int)((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / (int)sizeof(T));
-    pieces = (V - head) / E;
-    tail = V - head - pieces * E;
-  }
-  // the one element outside the pieces that is thread t's, or -1
-  __device__ int loose(int t) const { return t < head ? t : t < head + tail ? V - tail + (t - head) : -1; }
-  // f(value, id) for every element of thread t
-  template <class F>
-  __device__ __forceinline__ void each(int t, F f) const {
-    for (int i = t; i < pieces; i += NT) {
-      const Vec<T, E> v = *reinterpret_cast<const Vec<T, E>*>(x + head + (int64_t)i * E);
-#pragma unroll
-      for (int e = 0; e < E; ++e) f(to_f32(v.v[e]), head + i * E + e);
-    }
-    const int l = loose(t);
-    if (l >= 0) f(to_f32(x[l]), l);
+  hift_u32x4 w;
+  __device__ __forceinline__ float at(int e) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[e]);
+    return __uint_as_float(e & 1 ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16);
   }
 };
+template <typename T, int NT>
+struct RowOf {
+  static constexpr int E = Piece<T>::E, U = 4;
+  const T* x;
+  int V, t, head, pieces, loose_id;
+  float loose;
+  __device__ __forceinline__ RowOf(const T* row, int V_) : x(row), V(V_), t(threadIdx.x) {
+    head = min(V, (int)((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / (int)sizeof(T));
+    pieces = (V - head) / E;
+    const int tail = V - head - pieces * E;
+    loose_id = t < head ? t : t < head + tail ? V - tail + (t - head) : -1;
+    loose = loose_id >= 0 ? to_f32(x[loose_id]) : -INFINITY;
+  }
+  // pieces i, i + NT, ..; those past the end as -inf
+  __device__ __forceinline__ void load(Piece<T> (&p)[U], int i) const {
+    constexpr uint32_t MASKED = sizeof(T) == 4 ? 0xFF800000u : 0xFF80FF80u;
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      p[k].w = hift_u32x4{MASKED, MASKED, MASKED, MASKED};
+      if (i + k * NT < pieces) p[k].w = *reinterpret_cast<const hift_u32x4*>(x + head + (int64_t)(i + k * NT) * E);
+    }
+  }
+  // f(value, id) for every element of the thread
+  template <class F>
+  __device__ __forceinline__ void each(F f) const {
+    for (int i = t; i < pieces; i += NT) {
+      const Piece<T> p{*reinterpret_cast<const hift_u32x4*>(x + head + (int64_t)i * E)};
+#pragma unroll
+      for (int e = 0; e < E; ++e) f(p.at(e), head + i * E + e);
+    }
+    if (loose_id >= 0) f(loose, loose_id);
+  }
+};
+
+// Within a row of 16 lanes by DPP, across rows by lane swaps: all 64 lanes receive the result.  `eighth` receives what the 2^STEPS lanes
+// around each have by themselves.
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), CTRL, 0xF, 0xF, false));
+}
+template <int STEPS, class Op>
+__device__ __forceinline__ float wave_all(float v, Op op, float* group = nullptr) {
+  if (STEPS == 0 && group) *group = v;
+  v = op(v, dpp<0xB1>(v));   // the other lane of two
+  if (STEPS == 1 && group) *group = v;
+  v = op(v, dpp<0x4E>(v));   // the other two of four
+  if (STEPS == 2 && group) *group = v;
+  v = op(v, dpp<0x141>(v));  // the other four of eight (mirrored)
+  if (STEPS == 3 && group) *group = v;
+  v = op(v, dpp<0x140>(v));  // the other eight of sixteen (mirrored)
+  if (STEPS == 4 && group) *group = v;
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = op(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return op(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
 
 template <int NW>
 __device__ __forceinline__ uint64_t block_max64(uint64_t v, uint64_t* red) {
@@ -82,89 +124,182 @@ __device__ __forceinline__ uint64_t block_max64(uint64_t v, uint64_t* red) {
   return v;
 }
 
-// One workgroup a row.
-// The alternatives: the k-th largest of the maxima of 64 disjoint parts of the row is at most its k-th largest entry, and few entries are
-// at or above it (the parts interleave); those are collected and each counts how many of them precede it.  Rows where they are more than
-// the list holds, or that hold NaN or +inf, take the largest key below the one before, k times.
-template <typename T, int NT>
-__global__ void __launch_bounds__(NT) logprob_k(LogprobArgs a) {
-  constexpr int NW = NT / 64;
-  __shared__ float red[NW], parts[64];
-  __shared__ uint64_t red64[NW], cand[CANDIDATES];
-  __shared__ float tau_s;
-  __shared__ int count;
-  const int64_t r = blockIdx.x;
-  const int t = threadIdx.x;
-  const T* x = reinterpret_cast<const T*>(a.logits) + r * a.ld;
-  const RowOf<T, NT> row(x, a.V);
-
-  float mine = -INFINITY;
-  row.each(t, [&](float v, int) { mine = fmaxf(mine, v); });
-  const float mx = block_max<NW>(mine, red);
-  const float c = a.scale * LOG2E;
-  const float m2 = mx == -INFINITY ? 0.f : mx * c;
+// Sums of a part of a row against a reference: s = sum 2^d, u = sum 2^d d with d = c x - m2.  A masked entry has d = -inf and adds 0.
+struct Sums {
   float s = 0.f, u = 0.f;
-  row.each(t, [&](float v, int) {
-    const float d = fmaf(v, c, -m2), e = __builtin_amdgcn_exp2f(d);
+  __device__ __forceinline__ void add(float x, float c, float m2) {
+    const float d = fmaf(x, c, -m2), e = __builtin_amdgcn_exp2f(d);
     s += e;
-    u = fmaf(e, fmaxf(d, -1024.f), u);  // (0 times the -inf of a masked entry)
-  });
-  s = block_sum<NW>(s, red);
-  u = block_sum<NW>(u, red);
-  // m2 is the rounded maximum in powers of two; the sum that goes with the rounded maximum itself:
-  const float m = mx == -INFINITY ? 0.f : mx * a.scale;
-  const float ln_s = s > 0.f ? (float)(log((double)s) + ((double)m2 * LN2 - (double)m)) : s == 0.f ? -INFINITY : s;
-  if (t == 0) {
-    if (a.logp) {
-      const int y = a.targets[r];
-      a.logp[r] = y < 0 || y >= a.V ? 0.f : s == 0.f ? -INFINITY : fmaf(to_f32(x[y]), a.scale, -m) - ln_s;
+    u = fmaf(e, fmaxf(d, -1024.f), u);
+  }
+  // the same against a reference larger by `by`
+  __device__ __forceinline__ void shift(float by) {
+    const float f = __builtin_amdgcn_exp2f(-by);
+    u = f * fmaf(-by, s, u);
+    s *= f;
+  }
+};
+
+// One workgroup a row.  Every wavefront forms its sums against its own largest entry; the first one joins them.
+// The alternatives: the k-th largest of the maxima of 64 disjoint parts of the row is at most its k-th largest entry, and few entries are
+// at or above it (the parts interleave: 20 of 64 maxima exceed it where about 24 entries do); those are collected and each counts how
+// many of them precede it.  Rows where they are more than the list holds, or that hold NaN or +inf, take the largest key below the one
+// before, k times.
+template <typename T, int NT>
+__global__ void __launch_bounds__(NT, 8) logprob_k(LogprobArgs a) {
+  constexpr int NW = NT / 64, STEPS = NT == 64 ? 0 : NT == 256 ? 2 : NT == 512 ? 3 : 4;
+  __shared__ float wave_m[NW], wave_s[NW], wave_u[NW];
+  __shared__ uint32_t parts[64];
+  __shared__ uint64_t red64[NW], cand[CANDIDATES];
+  __shared__ float tau_s, m_s, ln_s_s, s_s;
+  __shared__ int count, look_count, looks[NT];
+  const int64_t r = blockIdx.x;
+  const int t = threadIdx.x, lane = t & 63;
+  const T* x = reinterpret_cast<const T*>(a.logits) + r * a.ld;
+  typedef RowOf<T, NT> Row;
+  const Row row(x, a.V);
+  const float c = a.scale * LOG2E;
+  const auto max2 = [](float p, float q) { return fmaxf(p, q); };
+  const auto sum2 = [](float p, float q) { return p + q; };
+
+  // One pass: the next pieces are on their way while the sums take the present ones; where those hold a new largest entry the sums are
+  // shifted first.  Which pieces held it, and the largest of all others, spare nearly every thread the look for its alternatives.
+  float mine = row.loose, second = -INFINITY, group;
+  int best = -1;
+  float m2 = mine == -INFINITY ? 0.f : mine * c;
+  Sums q;
+  if (row.loose_id >= 0) q.add(row.loose, c, m2);
+  Piece<T> now[Row::U], next[Row::U];
+  if (t < row.pieces) row.load(now, t);
+  for (int i = t; i < row.pieces; i += Row::U * NT) {
+    if (i + Row::U * NT < row.pieces) row.load(next, i + Row::U * NT);
+    float most = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < Row::U; ++k)
+#pragma unroll
+      for (int e = 0; e < Row::E; ++e) most = fmaxf(most, now[k].at(e));
+    // (the compiler would keep all elements as floats from the one look to the other)
+#pragma unroll
+    for (int k = 0; k < Row::U; ++k) asm volatile("" : "+v"(now[k].w));
+    if (most > mine) {
+      q.shift(mine == -INFINITY ? 0.f : fmaf(most, c, -m2));
+      second = mine;
+      mine = most;
+      m2 = most * c;
+      best = i;
+    } else {
+      second = fmaxf(second, most);
     }
-    if (a.entropy) a.entropy[r] = s == 0.f ? 0.f : (float)(log((double)s) - LN2 * (double)u / (double)s);
-    if (a.stats) {
-      a.stats[2 * r] = m;
-      a.stats[2 * r + 1] = ln_s;
+#pragma unroll
+    for (int k = 0; k < Row::U; ++k)
+#pragma unroll
+      for (int e = 0; e < Row::E; ++e) q.add(now[k].at(e), c, m2);
+#pragma unroll
+    for (int k = 0; k < Row::U; ++k) now[k] = next[k];
+  }
+  const float wm = wave_all<STEPS>(mine, max2, &group);
+  if (mine != -INFINITY) q.shift(fmaf(wm, c, -m2));
+  q.s = wave_all<0>(q.s, sum2);
+  q.u = wave_all<0>(q.u, sum2);
+  const int k = a.top;
+  if (lane == 0) {
+    wave_m[t >> 6] = wm;
+    wave_s[t >> 6] = q.s;
+    wave_u[t >> 6] = q.u;
+  }
+  // 26 bits of the order suffice for a threshold; the rest makes the 64 of them different
+  if (t % (NT / 64) == 0) parts[t / (NT / 64)] = (ordered(group) & ~63u) | (63 - t / (NT / 64));
+  if (t == 0) count = look_count = 0;
+  __syncthreads();
+  if (t < 64) {
+    float mx = wave_m[0];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) mx = fmaxf(mx, wave_m[w]);
+    const float m2 = mx == -INFINITY ? 0.f : mx * c;
+    Sums all;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      Sums p;
+      p.s = wave_s[w];
+      p.u = wave_u[w];
+      if (wave_m[w] != -INFINITY) p.shift(fmaf(-wave_m[w], c, m2));
+      all.s += p.s;
+      all.u += p.u;
+    }
+    const float s = all.s < INFINITY ? all.s : NAN;
+    // m2 is the rounded maximum in powers of two; ln S is given for the rounded maximum itself
+    const float m = mx == -INFINITY ? 0.f : mx * a.scale;
+    const float ln = __builtin_amdgcn_logf(s) * LN2_HI;
+    const float ln_s = s > 0.f ? ln + fmaf(m2, LN2_LO, fmaf(m2, LN2_HI, -m)) : s == 0.f ? -INFINITY : s;
+    if (t == 0) {
+      if (a.logp) {
+        const int y = a.targets[r];
+        a.logp[r] = y < 0 || y >= a.V ? 0.f : s == 0.f ? -INFINITY : fmaf(to_f32(x[y]), a.scale, -m) - ln_s;
+      }
+      if (a.entropy) a.entropy[r] = s == 0.f ? 0.f : ln - LN2_HI * (all.u / s);
+      if (a.stats) {
+        a.stats[2 * r] = m;
+        a.stats[2 * r + 1] = ln_s;
+      }
+      m_s = m;
+      ln_s_s = ln_s;
+      s_s = s;
     }
   }
-  const int k = a.top;
+  if (k > 0 && (NW > 1 ? t >= 64 && t < 128 : true)) {  // (meanwhile)
+    const uint32_t p = parts[lane];
+    int before = 0;
+#pragma unroll
+    for (int j = 0; j < 64; ++j) before += parts[j] > p;
+    if (before == k - 1) tau_s = (p & ~63u) <= ordered(-INFINITY) ? LOWEST : unordered(p & ~63u);  // (masked entries are never at or above it)
+  }
   if (k == 0) return;
+  __syncthreads();
+  const float s = s_s, m = m_s, ln_s = ln_s_s, tau = tau_s;
   float* top_logp = a.top_logp + r * k;
   int32_t* top_ids = a.top_ids + r * k;
   auto put = [&](int at, float v, int id) {
     top_ids[at] = id;
     top_logp[at] = s == 0.f ? -INFINITY : fmaf(v, a.scale, -m) - ln_s;
   };
-
-  // threshold
-  float part = mine;
-#pragma unroll
-  for (int o = 1; o < NT / 64; o <<= 1) part = fmaxf(part, __shfl_xor(part, o, 64));
-  if (t % (NT / 64) == 0) parts[t / (NT / 64)] = part;
-  if (t == 0) count = 0;
-  __syncthreads();
-  if (t < 64) {
-    const float p = parts[t];
-    int before = 0;
-    for (int j = 0; j < 64; ++j) before += parts[j] > p || (parts[j] == p && j < t);
-    if (before == k - 1) tau_s = p;
+  const bool plain = s < INFINITY;  // neither NaN nor +inf in the row
+  const auto collect = [&](float v, int id) {
+    if (v >= tau) {
+      const int at = atomicAdd(&count, 1);
+      if (at < CANDIDATES) cand[at] = top_key(v, id);
+    }
+  };
+  if (plain && mine >= tau) {
+    if (second >= tau || best < 0) row.each(collect);
+    else looks[atomicAdd(&look_count, 1)] = best;
   }
   __syncthreads();
-  const float tau = tau_s;
-  const bool plain = s < INFINITY;  // neither NaN nor +inf in the row
-  if (plain && mine >= tau)
-    row.each(t, [&](float v, int id) {
-      if (v >= tau && v > -INFINITY) {
-        const int at = atomicAdd(&count, 1);
-        if (at < CANDIDATES) cand[at] = top_key(v, id);
-      }
-    });
+  // the few threads' pieces, a lane an element
+  constexpr int G = Row::U * Row::E;
+  for (int j = t / G; j < look_count; j += NT / G) {
+    const int i = looks[j] + t % G / Row::E * NT;
+    const int id = row.head + i * Row::E + t % Row::E;
+    if (i < row.pieces) collect(to_f32(x[id]), id);
+  }
   __syncthreads();
   const int n = count;
   if (plain && n <= CANDIDATES) {
-    for (int i = t; i < n; i += NT) {
-      const uint64_t key = cand[i];
+    if (n <= 64) {
+      if (t >= 64) return;
+      const uint64_t key = t < n ? cand[t] : 0;
       int before = 0;
-      for (int j = 0; j < n; ++j) before += cand[j] > key;
-      if (before < k) put(before, unordered(key >> 32), key_id(key));
+      for (int j = 0; j < n; ++j) {
+        const uint64_t other = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(key >> 32), j) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)key, j);
+        before += other > key;
+      }
+      if (t < n && before < k) put(before, unordered(key >> 32), key_id(key));
+    } else {
+      for (int i = t; i < n; i += NT) {
+        const uint64_t key = cand[i];
+        int before = 0;
+        for (int j = 0; j < n; ++j) before += cand[j] > key;
+        if (before < k) put(before, unordered(key >> 32), key_id(key));
+      }
     }
     if (n < k && t < 64) {  // fewer entries than asked for are above -inf: the first masked ones follow
       int at = n;
@@ -181,7 +316,7 @@ __global__ void __launch_bounds__(NT) logprob_k(LogprobArgs a) {
   uint64_t last = ~0ull;
   for (int i = 0; i < k; ++i) {
     uint64_t best = 0;
-    row.each(t, [&](float v, int id) {
+    row.each([&](float v, int id) {
       const uint64_t key = top_key(v, id);
       if (key < last && key > best) best = key;
     });
@@ -245,7 +380,14 @@ __global__ void __launch_bounds__(BWD_THREADS) logprob_bwd_k(LogprobBwdArgs a) {
 
 template <typename T>
 hipError_t launch_logprob(int64_t rows, const LogprobArgs& a, hipStream_t st) {
-  logprob_k<T, 512><<<(uint32_t)rows, 512, 0, st>>>(a);
+  const int pieces = a.V / (16 / (int)sizeof(T));
+  const uint32_t grid = (uint32_t)rows;
+#define ROW(NT) logprob_k<T, NT><<<grid, NT, 0, st>>>(a)
+  if (pieces <= 256) ROW(64);
+  else if (pieces <= 2048) ROW(256);
+  else if (rows > 256) ROW(512);
+  else ROW(1024);  // a row a compute unit at most
+#undef ROW
   return hipGetLastError();
 }
 
