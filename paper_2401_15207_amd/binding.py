@@ -329,55 +329,69 @@ def kernel_cross_entropy(dtype, rows, V, logits, labels, row_loss, loss_out, str
     _check(lib.hift_kernel_cross_entropy(dtype, rows, V, _ptr(logits), _ptr(labels), _ptr(row_loss), _ptr(loss_out), st))
 
 
+_DTYPE_CODES = {torch.float32: 0, torch.bfloat16: 1}
+
+
 def _dtype_code(t) -> int:
-    codes = {torch.float32: 0, torch.bfloat16: 1}
-    if t.dtype not in codes:
+    code = _DTYPE_CODES.get(t.dtype)
+    if code is None:
         raise ValueError(f"float32 or bfloat16 expected, not {t.dtype}")
-    return codes[t.dtype]
+    return code
 
 
 def _rows_of(name, t, dtype=None, shape=None, contiguous=False):
     """t as a device matrix whose rows are contiguous; returns the distance between them."""
-    if not t.is_cuda or t.dim() != 2 or (dtype is not None and t.dtype != dtype) or (shape is not None and tuple(t.shape) != tuple(shape)):
+    size = t.shape
+    if not t.is_cuda or len(size) != 2 or (dtype is not None and t.dtype is not dtype) or (shape is not None and size != shape):
         raise ValueError(f"{name}: a device matrix{'' if shape is None else ' ' + str(tuple(shape))}{'' if dtype is None else f' of {dtype}'} "
-                         f"expected, not {tuple(t.shape)} of {t.dtype} on {t.device}")
-    ld = t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 1)
-    if (t.shape[1] > 1 and t.stride(1) != 1) or ld < t.shape[1] or (contiguous and not t.is_contiguous()):
+                         f"expected, not {tuple(size)} of {t.dtype} on {t.device}")
+    ld, step = t.stride()
+    rows, cols = size
+    if rows <= 1:
+        ld = cols
+    if (cols > 1 and step != 1) or ld < cols or (contiguous and not t.is_contiguous()):
         raise ValueError(f"{name}: rows have to be contiguous{' and to follow each other' if contiguous else ''}")
-    return ld
+    return max(ld, 1)
 
 
-def _row_values(name, t, rows, dtype=None, cols=1):
+def _stream_of(t, stream):
+    """The stream given, or torch's current one on the tensor's device (current_stream() makes an object first: 2.7 us)."""
+    if stream is not None:
+        return stream.cuda_stream
+    return torch._C._cuda_getCurrentRawStream(t.device.index) if t.is_cuda else 0
+
+
+def _row_values(name, t, count, dtype=torch.float32):
     if t is None:
         return None
-    if not t.is_cuda or not t.is_contiguous() or t.numel() != rows * cols or t.dtype != (dtype or torch.float32):
-        raise ValueError(f"{name}: {rows * cols} contiguous values of {dtype or torch.float32} on the device expected")
+    if t.dtype is not dtype or t.numel() != count or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name}: {count} contiguous values of {dtype} on the device expected")
     return t.data_ptr()
 
 
 def kernel_token_logprob(logits, vocab, targets, scale, logp, entropy, stats, top_logp=None, top_ids=None, stream=None):
     """logits: [rows, >= vocab] (rows contiguous, any distance apart); the outputs (fp32; top_ids int32) may be None where they are not wanted,
     targets (int32) where logp is; the number of alternatives is top_ids' second size."""
-    st = (stream or torch.cuda.current_stream()).cuda_stream
-    ld, rows = _rows_of("logits", logits), logits.shape[0]
-    if vocab > logits.shape[1]:
-        raise ValueError(f"vocab {vocab}, but rows hold {logits.shape[1]}")
+    st = _stream_of(logits, stream)
+    ld, (rows, width) = _rows_of("logits", logits), logits.shape
+    if vocab > width:
+        raise ValueError(f"vocab {vocab}, but rows hold {width}")
     top = 0 if top_ids is None else top_ids.shape[1]
-    _check(lib.hift_kernel_token_logprob(_dtype_code(logits), rows, vocab, ld, _ptr(logits), _row_values("targets", targets, rows, torch.int32), scale, top,
-                                         _row_values("logp", logp, rows), _row_values("entropy", entropy, rows), _row_values("stats", stats, rows, cols=2),
-                                         _row_values("top_logp", top_logp, rows, cols=top) if top else None,
-                                         _row_values("top_ids", top_ids, rows, torch.int32, top) if top else None, st))
+    _check(lib.hift_kernel_token_logprob(_dtype_code(logits), rows, vocab, ld, logits.data_ptr(), _row_values("targets", targets, rows, torch.int32), scale,
+                                         top, _row_values("logp", logp, rows), _row_values("entropy", entropy, rows), _row_values("stats", stats, 2 * rows),
+                                         _row_values("top_logp", top_logp, rows * top) if top else None,
+                                         _row_values("top_ids", top_ids, rows * top, torch.int32) if top else None, st))
 
 
 def kernel_token_logprob_bwd(logits, vocab, targets, scale, stats, entropy, d_logp, d_entropy, dlogits, stream=None):
     """dlogits: like logits, or logits itself; entropy, d_logp, d_entropy may be None (see hift.h)."""
-    st = (stream or torch.cuda.current_stream()).cuda_stream
-    ld, ldd, rows = _rows_of("logits", logits), _rows_of("dlogits", dlogits, logits.dtype), logits.shape[0]
-    if vocab > logits.shape[1] or vocab > dlogits.shape[1] or dlogits.shape[0] != rows:
-        raise ValueError(f"vocab {vocab}, but logits are {tuple(logits.shape)} and dlogits {tuple(dlogits.shape)}")
-    _check(lib.hift_kernel_token_logprob_bwd(_dtype_code(logits), rows, vocab, ld, _ptr(logits), _row_values("targets", targets, rows, torch.int32), scale,
-                                             _row_values("stats", stats, rows, cols=2), _row_values("entropy", entropy, rows),
-                                             _row_values("d_logp", d_logp, rows), _row_values("d_entropy", d_entropy, rows), ldd, _ptr(dlogits), st))
+    st = _stream_of(logits, stream)
+    ld, ldd, (rows, width), out = _rows_of("logits", logits), _rows_of("dlogits", dlogits, logits.dtype), logits.shape, dlogits.shape
+    if vocab > width or vocab > out[1] or out[0] != rows:
+        raise ValueError(f"vocab {vocab}, but logits are {tuple(logits.shape)} and dlogits {tuple(out)}")
+    _check(lib.hift_kernel_token_logprob_bwd(_dtype_code(logits), rows, vocab, ld, logits.data_ptr(), _row_values("targets", targets, rows, torch.int32), scale,
+                                             _row_values("stats", stats, 2 * rows), _row_values("entropy", entropy, rows),
+                                             _row_values("d_logp", d_logp, rows), _row_values("d_entropy", d_entropy, rows), ldd, dlogits.data_ptr(), st))
 
 
 def _workspace(query, n, arr, workspace, stream):

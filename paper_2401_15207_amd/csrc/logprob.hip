@@ -146,7 +146,7 @@ struct Sums {
 // many of them precede it.  Rows where they are more than the list holds, or that hold NaN or +inf, take the largest key below the one
 // before, k times.
 template <typename T, int NT>
-__global__ void __launch_bounds__(NT, 8) logprob_k(LogprobArgs a) {
+__global__ void __launch_bounds__(NT, NT == 1024 ? 4 : 8) logprob_k(LogprobArgs a) {
   constexpr int NW = NT / 64, STEPS = NT == 64 ? 0 : NT == 256 ? 2 : NT == 512 ? 3 : 4;
   __shared__ float wave_m[NW], wave_s[NW], wave_u[NW];
   __shared__ uint32_t parts[64];

@@ -106,6 +106,16 @@ __global__ void __launch_bounds__(256) ns_norm_k(NsTable t, float mu, unsigned* 
   if (threadIdx.x == 0) q.norm_parts[part] = (red[0] + red[1]) + (red[2] + red[3]);
 }
 
+// What U is multiplied with to become X, times X's scale; returns `small`: a norm below eps leaves X that many powers of two below 1.  Its
+// factors are stored a power of two larger then: X times 2^small, and after k steps, each of which lets X grow by less than 2^growth, times
+// 2^(small - k growth) as long as that is above 1.
+__device__ __forceinline__ int start_scale(double sum_of_squares, float eps, float scale, double* by) {
+  const double norm = sqrt(sum_of_squares);
+  const int small = norm > 0.0 && norm < (double)eps ? min((int)floor(log2((double)eps / norm)), 200) : 0;
+  *by = ldexp((double)scale, small) / (norm < (double)eps ? (double)eps : norm);  // (a norm that is no number stays one)
+  return small;
+}
+
 // ---- U -> X and X^T in fragment order --------------------------------------------------------
 template <typename T>
 __global__ void __launch_bounds__(256) ns_start_k(NsTable t, float mu, float eps, float scale) {
@@ -119,12 +129,9 @@ __global__ void __launch_bounds__(256) ns_start_k(NsTable t, float mu, float eps
   for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
   if (lane == 0) red[th >> 6] = s;
   __syncthreads();
-  const double norm = sqrt((red[0] + red[1]) + (red[2] + red[3]));
-  // A norm below eps leaves X that small.  Its factors are stored a power of two larger then: X times 2^small, and after k steps, each of
-  // which lets X grow by less than 2^growth, times 2^(small - k growth) as long as that is above 1.
-  const int below = norm > 0.0 && norm < (double)eps ? min((int)floor(log2((double)eps / norm)), 200) : 0;
-  const double by = ldexp((double)scale, below) / (norm < (double)eps ? (double)eps : norm);  // (a norm that is no number stays one)
-  if (id == 0 && th == 0) *q.small = below;
+  double by;
+  const int small = start_scale((red[0] + red[1]) + (red[2] + red[3]), eps, scale, &by);
+  if (id == 0 && th == 0) *q.small = small;
   // sides as they lie in memory, filled up
   const int R = q.tall ? q.m : q.n, C = q.tall ? q.n : q.m;
   const int tiles_c = C / 64;
@@ -248,6 +255,20 @@ struct NsTile {
   static constexpr int STAGE = PIECES * 1024, RING = SIDE == 256 || (SIDE == 64 && DEEP) ? 4 : SIDE == 64 ? 2 : DEEP ? 8 : 3, LDS = RING * STAGE;
   static_assert(PIECES % NW == 0 && LDS <= 160 * 1024 && NW * 32 * TURN_PITCH * 4 <= LDS, "blocks turn in the ring");
 };
+
+// entry (row, c) of the result o: into dst, or into the update of the weights
+template <typename OUT>
+__device__ __forceinline__ void put_result(const NsMatrix& q, int64_t row, int64_t c, float o, float decay) {
+  if (row >= q.rows || c >= q.cols) return;
+  if (q.master) {
+    float* w = q.master + row * q.cols + c;
+    const float nw = fmaf(-q.factor, o, decay * *w);
+    *w = nw;
+    if (q.copy) q.copy[row * q.cols + c] = from_f32<bf16>(nw);
+  } else {
+    reinterpret_cast<OUT*>(q.dst)[row * q.ld_dst + c] = from_f32<OUT>(o);
+  }
+}
 
 template <int SIDE, int MODE, int PP, int QP, bool DEEP, typename OUT>
 __global__ void __launch_bounds__((64 * NsTile<SIDE, PP, QP, DEEP>::NW), (DEEP && SIDE < 256 ? 1 : 2)) ns_product_k(NsTable t, NsStep st) {
@@ -461,23 +482,235 @@ __global__ void __launch_bounds__((64 * NsTile<SIDE, PP, QP, DEEP>::NW), (DEEP &
       } else if (MODE == NS_APPLY) {
         put_block<true, !FEW>(Factor{q.xt2, q.n / 16}, Factor{q.x, q.m / 16}, true, i, j, v, turned, lane);
       } else {
-        const int64_t c = j + (lane & 31);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int64_t row = i + acc_row(e, lane);
-          if (row >= q.rows || c >= q.cols) continue;
-          const float o = ldexpf(v[e] * st.unscale, -up);
-          if (q.master) {
-            float* w = q.master + row * q.cols + c;
-            const float nw = fmaf(-q.factor, o, st.decay * *w);
-            *w = nw;
-            if (q.copy) q.copy[row * q.cols + c] = from_f32<bf16>(nw);
-          } else {
-            reinterpret_cast<OUT*>(q.dst)[row * q.ld_dst + c] = from_f32<OUT>(o);
-          }
+        for (int e = 0; e < 16; ++e) put_result<OUT>(q, i + acc_row(e, lane), j + (lane & 31), ldexpf(v[e] * st.unscale, -up), st.decay);
+      }
+    }
+}
+
+// ---- matrices that fit a compute unit's LDS ---------------------------------------------------
+// All steps in one launch, a workgroup a matrix: X, X^T and A (in whose place B goes) stay in LDS, in the same order as in memory, sides filled
+// up to multiples of 32.  What bounds the launches above for such matrices is their number and each one's way to memory and back: six
+// matrices of 64 x 64 to 256 x 64 take 84 us in 17 launches.
+struct NsSteps {
+  int steps, growth;
+  float mu, eps, decay;
+  float ca, cb, cc;
+  float x[NS_STEPS_MAX + 1], a[NS_STEPS_MAX], b[NS_STEPS_MAX];  // scales
+};
+constexpr int SMALL_WAVES = 8, SMALL_TILES = NS_SMALL_TILES;
+
+__device__ __forceinline__ _Float16* entry(const Factor& f, int row, int k) {
+  return f.block(row >> 5, k >> 4) + ((row & 31) + 32 * ((k >> 3) & 1)) * 8 + (k & 7);
+}
+// one 32 x 32 tile of P Q^T, k blocks [k0, k1), an even number of them: two at a time, the next two's fragments on their way, and three
+// sums apart, as a product waits for the one before it in its sum
+__device__ __forceinline__ void small_product(f32x16& acc, const Factor& P, int rb, const Factor& Q, int cb, int k0, int k1, int lane) {
+  half8 f[2][2][4];
+  auto read = [&](int to, int k) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const _Float16 *p = P.block(rb, k + j) + lane * 8, *q = Q.block(cb, k + j) + lane * 8;
+      f[to][j][0] = *reinterpret_cast<const half8*>(p);
+      f[to][j][1] = *reinterpret_cast<const half8*>(p + P.low());
+      f[to][j][2] = *reinterpret_cast<const half8*>(q);
+      f[to][j][3] = *reinterpret_cast<const half8*>(q + Q.low());
+    }
+  };
+  f32x16 low[2] = {};
+  acc = f32x16{};
+  auto multiply = [&](int c) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      low[0] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[c][j][1], f[c][j][2], low[0], 0, 0, 0);
+      low[1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[c][j][0], f[c][j][3], low[1], 0, 0, 0);
+      acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[c][j][0], f[c][j][2], acc, 0, 0, 0);
+    }
+  };
+  if (k0 < k1) read(0, k0);
+  for (int k = k0; k < k1; k += 4) {
+    if (k + 2 < k1) read(1, k + 2);
+    multiply(0);
+    if (k + 4 < k1) read(0, k + 4);
+    if (k + 2 < k1) multiply(1);
+  }
+  acc += low[0] + low[1];
+}
+// block (rows j, k i) from accumulators, as put_block leaves it
+__device__ __forceinline__ void small_put(const Factor& f, int ib, int jb, const f32x16& v, int lane) {
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    half4 hi, lo;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      _Float16 h, l;
+      split(v[4 * g + e], h, l);
+      hi[e] = h; lo[e] = l;
+    }
+    _Float16* p = f.block(jb, ib * 2 + (g >> 1)) + ((lane & 31) + 32 * (g & 1)) * 8 + 4 * (lane >> 5);
+    *reinterpret_cast<half4*>(p) = hi;
+    *reinterpret_cast<half4*>(p + f.low()) = lo;
+  }
+}
+
+// What bounds it: waits one after the other, 7 us a step at 64 x 256 (one workgroup, six barriers) and 25 for the way in and out.
+template <typename T, typename OUT>
+__global__ void __launch_bounds__(64 * SMALL_WAVES) ns_small_k(NsTable t, NsSteps a) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  __shared__ double red[SMALL_WAVES];
+  const NsMatrix& q = t.m[blockIdx.x];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = q.n, m = q.m, nb = n / 32, mb = m / 32;
+  _Float16* const at = reinterpret_cast<_Float16*>(smem);
+  const Factor X{at, m / 16}, XT{at + n * m * 2, n / 16}, AB{at + n * m * 4, n / 16};
+  const int rows = (int)q.rows, cols = (int)q.cols, R = q.tall ? m : n, C = q.tall ? n : m;
+
+  // Eight neighbours of a row a thread and round, lanes down the rows (across them, all lanes of the writes below meet in one LDS bank).
+  const int pieces = R * C / 8;
+  const T* src = reinterpret_cast<const T*>(q.src);
+  double sum = 0.0;
+#pragma unroll 1
+  for (int p = threadIdx.x; p < pieces; p += 64 * SMALL_WAVES) {
+    const int r = p % R, c = p / R * 8;
+    if (r >= rows) continue;
+    float u[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) u[e] = c + e < cols ? to_f32(src[r * q.ld_src + c + e]) : 0.f;
+    if (q.momentum) {
+      float* mp = q.momentum + r * cols + c;
+      float b[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) b[e] = c + e < cols ? mp[e] : 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        b[e] = fmaf(a.mu, b[e], u[e]);
+        if (c + e < cols) mp[e] = b[e];
+        u[e] = fmaf(a.mu, b[e], u[e]);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum += (double)u[e] * u[e];
+  }
+  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+  if (lane == 0) red[wave] = sum;
+  __syncthreads();
+  sum = red[0];
+  for (int w = 1; w < SMALL_WAVES; ++w) sum += red[w];
+  double by;
+  const int small = start_scale(sum, a.eps, a.x[0], &by);
+  // as a factor of rows r and k c, and as one of rows c and k r
+  const Factor along = q.tall ? XT : X, turned = q.tall ? X : XT;
+#pragma unroll 1
+  for (int p = threadIdx.x; p < pieces; p += 64 * SMALL_WAVES) {
+    const int r = p % R, c = p / R * 8;
+    float u[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) u[e] = r < rows && c + e < cols ? to_f32(src[r * q.ld_src + c + e]) : 0.f;
+    if (q.momentum)  // (what this very thread has written)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) u[e] = r < rows && c + e < cols ? fmaf(a.mu, q.momentum[r * cols + c + e], u[e]) : 0.f;
+    half8 hi, lo;
+    _Float16* at_r = entry(turned, c, r);  // (rows of a block are 8 numbers apart)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      _Float16 h, l;
+      split((float)((double)u[e] * by), h, l);
+      hi[e] = h; lo[e] = l;
+      at_r[e * 8] = h;
+      at_r[turned.low() + e * 8] = l;
+    }
+    _Float16* at_c = entry(along, r, c);
+    *reinterpret_cast<half8*>(at_c) = hi;
+    *reinterpret_cast<half8*>(at_c + along.low()) = lo;
+  }
+  __syncthreads();
+
+  const int tiles = nb * nb;  // of A and B: one a wavefront, and two wavefronts each for A's sums
+  const int middle = mb / 2 * 2, tile_a = wave >> 1, half = wave & 1;
+  float* partial = reinterpret_cast<float*>(smem) + n * m * 2;  // [tiles][16][64], where A goes afterwards
+#pragma unroll 1
+  for (int k = 0; k < a.steps; ++k) {
+    const int up = max(0, small - k * a.growth), next_up = max(0, small - (k + 1) * a.growth);
+    f32x16 acc[SMALL_TILES];
+    // A = X X^T
+    if (tile_a < tiles) {
+      small_product(acc[0], X, tile_a / nb, X, tile_a % nb, half ? middle : 0, half ? X.kb : middle, lane);
+      if (half)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) partial[(tile_a * 16 + e) * 64 + lane] = acc[0][e];
+    }
+    __syncthreads();
+    if (tile_a < tiles && !half)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[0][e] += partial[(tile_a * 16 + e) * 64 + lane];
+    __syncthreads();
+    if (tile_a < tiles && !half) {
+      const float to_a = a.a[k] / (a.x[k] * a.x[k]);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[0][e] = ldexpf(acc[0][e] * to_a, -2 * up);
+      small_put(AB, tile_a / nb, tile_a % nb, acc[0], lane);
+    }
+    __syncthreads();
+    // B = a I + b A + c A A, in A's place
+    const int ib = wave / nb, jb = wave % nb;
+    if (wave < tiles) {
+      const float cb = a.cb / a.a[k], cc = a.cc / (a.a[k] * a.a[k]);
+      small_product(acc[0], AB, ib, AB, jb, 0, AB.kb, lane);
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const _Float16* p = at_block(AB, ib * 32, jb * 32, g, lane);
+        const half4 hi = *reinterpret_cast<const half4*>(p), lo = *reinterpret_cast<const half4*>(p + AB.low());
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const bool diagonal = ib == jb && acc_row(4 * g + e, lane) == (lane & 31);
+          acc[0][4 * g + e] = (fmaf(cc, acc[0][4 * g + e], cb * ((float)hi[e] + (float)lo[e])) + (diagonal ? a.ca : 0.f)) * a.b[k];
         }
       }
     }
+    __syncthreads();
+    if (wave < tiles) small_put(AB, ib, jb, acc[0], lane);
+    __syncthreads();
+    // X <- B X; the last one with dst's columns along the lanes
+    const bool last = k + 1 == a.steps, turn = last && q.tall;
+    const int all = nb * mb, tiles_across = turn ? nb : mb;
+    const Factor P = turn ? XT : AB, Q = turn ? AB : XT;
+#pragma unroll
+    for (int o = 0; o < SMALL_TILES; ++o) {
+      const int tile = wave + o * SMALL_WAVES;
+      if (tile < all) small_product(acc[o], P, tile / tiles_across, Q, tile % tiles_across, 0, AB.kb, lane);
+    }
+    const float unscale = (last ? 1.f : a.x[k + 1]) / (a.b[k] * a.x[k]);
+    const int power = last ? -up : next_up - up;
+    __syncthreads();  // every wavefront has read X^T
+    float* result = reinterpret_cast<float*>(smem);  // the last X, as it lies in dst: where X and X^T were
+#pragma unroll
+    for (int o = 0; o < SMALL_TILES; ++o) {
+      const int tile = wave + o * SMALL_WAVES;
+      if (tile >= all) break;
+      const int i = tile / tiles_across, j = tile % tiles_across;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[o][e] = ldexpf(acc[o][e] * unscale, power);
+      if (last) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) result[(i * 32 + acc_row(e, lane)) * C + j * 32 + (lane & 31)] = acc[o][e];
+        continue;
+      }
+      small_put(XT, i, j, acc[o], lane);
+      _Float16* p = entry(X, i * 32 + acc_row(0, lane), j * 32 + (lane & 31));
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        _Float16 h, l;
+        split(acc[o][e], h, l);
+        p[acc_row(e, 0) * 8] = h;
+        p[X.low() + acc_row(e, 0) * 8] = l;
+      }
+    }
+    __syncthreads();
+  }
+  const float* result = reinterpret_cast<const float*>(smem);
+#pragma unroll 4
+  for (int r = wave; r < rows; r += SMALL_WAVES)
+    for (int c = lane; c < cols; c += 64) put_result<OUT>(q, r, c, result[r * C + c], a.decay);
 }
 
 // Gives every matrix of the table its workgroups; blocks(q): how many.
@@ -592,6 +825,30 @@ hipError_t steps_of(NsTable& t, int side, int dt_src, int dt_dst, const NsRun& r
   return hipGetLastError();
 }
 
+hipError_t all_steps_of(const NsTable& t, int dt_src, int dt_dst, const NsRun& run, size_t lds, hipStream_t st) {
+  NsSteps a{};
+  a.steps = run.steps;
+  a.growth = ns_growth(run.co);
+  a.mu = run.mu; a.eps = run.eps; a.decay = run.decay;
+  a.ca = (float)run.co[0]; a.cb = (float)run.co[1]; a.cc = (float)run.co[2];
+  double r = 1.001;
+  for (int k = 0; k <= run.steps; ++k) {
+    NsScales s;
+    if (!ns_scales(run.co, r, &s)) return hipErrorInvalidValue;
+    a.x[k] = s.x;
+    if (k < run.steps) { a.a[k] = s.a; a.b[k] = s.b; }
+    r = std::max(s.r_next, 1.0);
+  }
+  const auto go = [&](auto kern) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, NS_SMALL_LDS);
+    if (e != hipSuccess) return e;
+    kern<<<t.count, 64 * SMALL_WAVES, lds, st>>>(t, a);
+    return hipGetLastError();
+  };
+  if (dt_src == DT_BF16) return dt_dst == DT_BF16 ? go(ns_small_k<bf16, bf16>) : go(ns_small_k<bf16, float>);
+  return dt_dst == DT_BF16 ? go(ns_small_k<float, bf16>) : go(ns_small_k<float, float>);
+}
+
 }  // namespace
 
 bool ns_coefficients_hold(const double (&co)[3], int steps) {
@@ -614,6 +871,8 @@ hipError_t newton_schulz(const NsItem* items, int count, int dt_src, int dt_dst,
   ns_launches(count, run.few, [&](int i, int64_t* r, int64_t* c) { *r = items[i].rows; *c = items[i].cols; }, [&](const int* which, int n, int side, bool large) {
     NsTable t{};
     unsigned char* ws = reinterpret_cast<unsigned char*>(workspace) + NS_SHARED_BYTES;
+    const int fill = side == NS_SMALL ? 32 : side;
+    size_t lds = 0;
     for (int i = 0; i < n; ++i) {
       const NsItem& it = items[which[i]];
       NsMatrix& q = t.m[t.count++];
@@ -621,8 +880,12 @@ hipError_t newton_schulz(const NsItem* items, int count, int dt_src, int dt_dst,
       q.src = it.src; q.momentum = it.momentum; q.dst = it.dst; q.master = it.master; q.copy = (bf16*)it.copy;
       q.factor = (float)(run.lr * 0.2 * sqrt((double)std::max(it.rows, it.cols)));
       q.tall = it.rows > it.cols;
-      q.n = (int)ns_up(std::min(it.rows, it.cols), side);
-      q.m = (int)ns_up(std::max(it.rows, it.cols), side);
+      q.n = (int)ns_up(std::min(it.rows, it.cols), fill);
+      q.m = (int)ns_up(std::max(it.rows, it.cols), fill);
+      if (side == NS_SMALL) {
+        lds = std::max(lds, ns_small_lds(it.rows, it.cols));
+        continue;
+      }
       auto take = [&](int64_t entries) {
         _Float16* p = reinterpret_cast<_Float16*>(ws);
         ws += entries * 4;
@@ -641,7 +904,9 @@ hipError_t newton_schulz(const NsItem* items, int count, int dt_src, int dt_dst,
       q.small = reinterpret_cast<int*>(ws);
       ws += 16;
     }
-    if (err == hipSuccess) err = steps_of(t, side, dt_src, dt_dst, run, large, reinterpret_cast<unsigned char*>(workspace), st);
+    if (err != hipSuccess) return;
+    if (side == NS_SMALL) err = all_steps_of(t, dt_src, dt_dst, run, lds, st);
+    else err = steps_of(t, side, dt_src, dt_dst, run, large, reinterpret_cast<unsigned char*>(workspace), st);
   });
   return err;
 }

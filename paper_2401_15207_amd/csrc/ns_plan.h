@@ -69,6 +69,20 @@ constexpr size_t NS_SHARED_BYTES = NS_SHARED_UNITS * (4 + 128 * 128 * 4);
 inline bool ns_large(int64_t rows, int64_t cols) { return std::min(rows, cols) >= 512; }
 
 inline int64_t ns_up(int64_t x, int side) { return (x + side - 1) / side * side; }
+// Matrices whose factors X, X^T and A (two fp16 numbers to an entry) fit a compute unit's LDS with sides filled up to multiples of 32, and
+// whose tiles of 32 x 32 two a wavefront at most: all steps in one launch, if a list holds no other.  (Among others they ride along: their
+// few tiles take no launches of their own.)
+constexpr int NS_SMALL = 0, NS_SMALL_TILES = 2;
+constexpr size_t NS_SMALL_LDS = 159 * 1024;
+inline size_t ns_small_lds(int64_t rows, int64_t cols) {
+  const int64_t n = ns_up(std::min(rows, cols), 32), m = ns_up(std::max(rows, cols), 32);
+  return (size_t)(2 * n * m + n * n) * 4;
+}
+inline bool ns_small(int64_t rows, int64_t cols) {
+  const int64_t n = ns_up(std::min(rows, cols), 32) / 32, m = ns_up(std::max(rows, cols), 32) / 32;
+  return ns_small_lds(rows, cols) <= NS_SMALL_LDS && n * m <= 8 * NS_SMALL_TILES && n <= 2;
+}
+
 // Work space of one matrix: X, X^T before and after a step, A and B, two fp16 numbers to an entry, two diagonals, the sums
 // of its norm, and how far that is below eps.
 constexpr int NS_NORM_PARTS = 256;
@@ -82,6 +96,25 @@ inline size_t ns_bytes(int64_t rows, int64_t cols) {
 // few: large ones apart, as they take fewer products.
 template <class S, class F>
 inline void ns_launches(int count, bool few, S shape, F launch) {
+  bool all_small = true;
+  for (int i = 0; i < count && all_small; ++i) {
+    int64_t r, c;
+    shape(i, &r, &c);
+    all_small = r == 0 || c == 0 || ns_small(r, c);
+  }
+  if (all_small) {
+    int which[NS_TABLE], n = 0;
+    for (int i = 0; i < count; ++i) {
+      int64_t r, c;
+      shape(i, &r, &c);
+      if (r > 0 && c > 0) which[n++] = i;
+      if (n == NS_TABLE || (i + 1 == count && n > 0)) {
+        launch((const int*)which, n, NS_SMALL, false);
+        n = 0;
+      }
+    }
+    return;
+  }
   for (int kind = 0; kind < (few ? 3 : 2); ++kind) {
     const int side = kind == 0 ? 256 : 128;
     const bool large = few && kind < 2;
@@ -115,8 +148,9 @@ template <class S>
 inline size_t ns_workspace_bytes(int count, S shape) {
   size_t most = 0;
   for (bool few : {false, true})
-    ns_launches(count, few, shape, [&](const int* which, int n, int, bool) {
+    ns_launches(count, few, shape, [&](const int* which, int n, int side, bool) {
       size_t sum = 0;
+      if (side == NS_SMALL) return;
       for (int i = 0; i < n; ++i) {
         int64_t r, c;
         shape(which[i], &r, &c);

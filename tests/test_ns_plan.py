@@ -90,9 +90,15 @@ def test_work_space_and_launches(plan):
             at += 2 + out[at + 1]
         return got
 
+    # what fits LDS: a workgroup a matrix and no work space, but along with others where there are any
     small = [(8, 8)] * 40
+    assert launches(small) == [(0, list(range(0, 16))), (0, list(range(16, 32))), (0, list(range(32, 40)))] and call(plan.bytes, small) == 0
+    assert launches([(256, 64), (0, 9), (64, 256), (64, 64), (17, 500)]) == [(0, [0, 2, 3, 4])]
+    for too_large in ((64, 300), (96, 100), (128, 128), (17, 800)):
+        assert launches([(8, 8), too_large]) == [(64, [1, 0])]
+    small[0] = (64, 300)
     assert launches(small) == [(64, list(range(0, 16))), (64, list(range(16, 32))), (64, list(range(32, 40)))]
-    assert call(plan.bytes, small) == plan.shared() + 16 * plan.one(8, 8)
+    assert call(plan.bytes, small) == plan.shared() + 15 * plan.one(8, 8) + plan.one(64, 300)
     # tiles of either size apart, the longest first, nothing for a side of 0, and no more than fits together
     mixed = [(64, 64), (4096, 4096), (0, 7), (4096, 11008), (100, 300)]
     assert launches(mixed) == [(256, [3, 1]), (64, [4, 0])] and launches([(64, 64), (600, 900)]) == [(64, [1, 0])]
