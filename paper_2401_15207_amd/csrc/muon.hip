@@ -75,6 +75,18 @@ __device__ __forceinline__ void split(float v, _Float16& hi, _Float16& lo) {
   lo = (_Float16)(v - (float)hi);
 }
 
+// One entry's square, its momentum updated on the way
+template <typename T>
+__device__ __forceinline__ double norm_entry(const NsMatrix& q, int64_t at, int64_t at_momentum, float mu) {
+  float u = to_f32(reinterpret_cast<const T*>(q.src)[at]);
+  if (q.momentum) {
+    const float m = fmaf(mu, q.momentum[at_momentum], u);
+    q.momentum[at_momentum] = m;
+    u = fmaf(mu, m, u);
+  }
+  return (double)u * u;
+}
+
 // ---- norm ----------------------------------------------------------------------------------
 // Sums of squares in 64 bits (an entry's square may pass fp32's range either way), NS_NORM_PARTS of them a matrix; with a momentum buffer,
 // that is updated on the way.
@@ -86,20 +98,44 @@ __global__ void __launch_bounds__(256) ns_norm_k(NsTable t, float mu, unsigned* 
   if (blockIdx.x == 0)  // the counters of shared tiles; who counts last leaves 0 again
     for (int i = threadIdx.x; i < NS_SHARED_UNITS; i += 256) shared[i] = 0;
   double s = 0.0;
-  const int64_t per = (q.rows + NS_NORM_PARTS - 1) / NS_NORM_PARTS;
-  const int64_t r1 = min(q.rows, (part + 1) * per);
-  for (int64_t r = part * per; r < r1; ++r)
-    for (int64_t c = threadIdx.x; c < q.cols; c += 256) {
-      float u = to_f32(reinterpret_cast<const T*>(q.src)[r * q.ld_src + c]);
-      if (q.momentum) {
-        const float g = u;
-        float* mp = q.momentum + r * q.cols + c;
-        const float m = fmaf(mu, *mp, g);
-        *mp = m;
-        u = fmaf(mu, m, g);
-      }
-      s += (double)u * u;
+  constexpr int E = 16 / (int)sizeof(T), U = 4;
+  const int64_t all = q.rows * q.cols;
+  if (q.ld_src == q.cols && ((reinterpret_cast<uintptr_t>(q.src) | reinterpret_cast<uintptr_t>(q.momentum)) & 15) == 0) {
+    // one run of pieces of 16 bytes, U of them a thread on their way at a time (202 M entries with momentum: 0.77 -> 0.53 ms against rows of entries)
+    const int64_t pieces = all / E, per = (pieces + NS_NORM_PARTS - 1) / NS_NORM_PARTS, end = min(pieces, (part + 1) * per);
+    const T* src = reinterpret_cast<const T*>(q.src);
+    for (int64_t i = part * per + threadIdx.x; i < end; i += U * 256) {
+      Vec<T, E> g[U];
+      Vec<float, E> m[U];
+#pragma unroll
+      for (int k = 0; k < U; ++k)
+        if (i + k * 256 < end) {
+          g[k] = *reinterpret_cast<const Vec<T, E>*>(src + (i + k * 256) * E);
+          if (q.momentum) m[k] = *reinterpret_cast<const Vec<float, E>*>(q.momentum + (i + k * 256) * E);
+        }
+#pragma unroll
+      for (int k = 0; k < U; ++k)
+        if (i + k * 256 < end) {
+          float u[E];
+#pragma unroll
+          for (int e = 0; e < E; ++e) {
+            u[e] = to_f32(g[k].v[e]);
+            if (q.momentum) {
+              m[k].v[e] = fmaf(mu, m[k].v[e], u[e]);
+              u[e] = fmaf(mu, m[k].v[e], u[e]);
+            }
+            s += (double)u[e] * u[e];
+          }
+          if (q.momentum) *reinterpret_cast<Vec<float, E>*>(q.momentum + (i + k * 256) * E) = m[k];
+        }
     }
+    const int64_t left = pieces * E + threadIdx.x;
+    if (part == NS_NORM_PARTS - 1 && left < all) s += norm_entry<T>(q, left, left, mu);
+  } else {
+    const int64_t per = (q.rows + NS_NORM_PARTS - 1) / NS_NORM_PARTS, r1 = min(q.rows, (part + 1) * per);
+    for (int64_t r = part * per; r < r1; ++r)
+      for (int64_t c = threadIdx.x; c < q.cols; c += 256) s += norm_entry<T>(q, r * q.ld_src + c, r * q.cols + c, mu);
+  }
   for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
   __syncthreads();
@@ -256,14 +292,13 @@ struct NsTile {
   static_assert(PIECES % NW == 0 && LDS <= 160 * 1024 && NW * 32 * TURN_PITCH * 4 <= LDS, "blocks turn in the ring");
 };
 
-// entry (row, c) of the result o: into dst, or into the update of the weights
+// entry (row, c) of the result o: into dst, or into the update of the weights (w: what that one is)
 template <typename OUT>
-__device__ __forceinline__ void put_result(const NsMatrix& q, int64_t row, int64_t c, float o, float decay) {
+__device__ __forceinline__ void put_result(const NsMatrix& q, int64_t row, int64_t c, float o, float decay, float w) {
   if (row >= q.rows || c >= q.cols) return;
   if (q.master) {
-    float* w = q.master + row * q.cols + c;
-    const float nw = fmaf(-q.factor, o, decay * *w);
-    *w = nw;
+    const float nw = fmaf(-q.factor, o, decay * w);
+    q.master[row * q.cols + c] = nw;
     if (q.copy) q.copy[row * q.cols + c] = from_f32<bf16>(nw);
   } else {
     reinterpret_cast<OUT*>(q.dst)[row * q.ld_dst + c] = from_f32<OUT>(o);
@@ -430,62 +465,83 @@ __global__ void __launch_bounds__((64 * NsTile<SIDE, PP, QP, DEEP>::NW), (DEEP &
 
   __syncthreads();  // the ring is free: nothing is on its way there either
   uint32_t* turned = reinterpret_cast<uint32_t*>(smem) + wave * 32 * TURN_PITCH;
+  // What a block of the epilogue reads is requested before the block before it is written: the wait for a load would take in the stores
+  // before it.
+  struct Ahead { half4 hi[4], lo[4]; float rest[4][4], rest_j; f32x16 w; };
+  const Factor f = MODE == NS_POLY ? Factor{q.a, q.n / 16} : turn ? Factor{q.x, q.m / 16} : Factor{q.xt, q.n / 16};
+  const auto block_i = [&](int b) __attribute__((always_inline)) { return ti * SIDE + (wi * BI + b / BJ) * 32; };
+  const auto block_j = [&](int b) __attribute__((always_inline)) { return tj * SIDE + (wj * BJ + b % BJ) * 32; };
+  const auto ahead = [&](Ahead& n, int b) __attribute__((always_inline)) {
+    const int i = block_i(b), j = block_j(b);
+    const float* rest = MODE == NS_POLY ? q.a_rest : q.b_rest;
+    if (MODE == NS_POLY || (!SYM && FEW)) {
 #pragma unroll
-  for (int x = 0; x < BI; ++x)
+      for (int g = 0; g < 4; ++g) {
+        const _Float16* p = at_block(f, i, j, g, lane);
+        n.hi[g] = *reinterpret_cast<const half4*>(p);
+        if (MODE == NS_POLY) n.lo[g] = *reinterpret_cast<const half4*>(p + f.low());
+        if (FEW && !turn)
 #pragma unroll
-    for (int y = 0; y < BJ; ++y) {
-      f32x16 v = acc[x][y];
-      const int i = ti * SIDE + (wi * BI + x) * 32, j = tj * SIDE + (wj * BJ + y) * 32;
-      if (MODE == NS_POLY) {
-        // A at the same place: rows j, k i of a symmetric factor
-        const Factor a{q.a, q.n / 16};
-        const float rest_j = FEW ? q.a_rest[j + (lane & 31)] : 0.f;
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const _Float16* f = at_block(a, i, j, g, lane);
-          const half4 hi = *reinterpret_cast<const half4*>(f), lo = *reinterpret_cast<const half4*>(f + a.low());
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int row = i + acc_row(4 * g + e, lane);
-            float aa = v[4 * g + e];
-            if (FEW) aa = fmaf((float)hi[e], q.a_rest[row] + rest_j, aa);  // what the diagonal's low numbers add to A A
-            v[4 * g + e] = (fmaf(st.cc, aa, st.cb * ((float)hi[e] + (float)lo[e])) + (row == j + (lane & 31) ? st.ca : 0.f)) * st.out_scale;
-          }
-        }
-      } else {
-        if (!SYM && FEW) {
-          // What the diagonal of B's low numbers adds to B X: X at the same place, in the factor whose rows are j
-          const Factor f = turn ? Factor{q.x, q.m / 16} : Factor{q.xt, q.n / 16};
-          const float rest_j = turn ? q.b_rest[j + (lane & 31)] : 0.f;
-#pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            const half4 hi = *reinterpret_cast<const half4*>(at_block(f, i, j, g, lane));
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[4 * g + e] = fmaf((float)hi[e], turn ? rest_j : q.b_rest[i + acc_row(4 * g + e, lane)], v[4 * g + e]);
-          }
-        }
-        if (MODE != NS_LAST) {
-#pragma unroll
-          for (int e = 0; e < 16; ++e) v[e] = ldexpf(v[e] * st.unscale * st.out_scale, MODE == NS_GRAM ? -2 * up : max(0, small - st.grown - st.growth) - up);
-        }
+          for (int e = 0; e < 4; ++e) n.rest[g][e] = rest[i + acc_row(4 * g + e, lane)];
       }
-      if (SYM) {
-        const Factor out{MODE == NS_GRAM ? q.a : q.b, q.n / 16};
-        constexpr bool LOW = !FEW || MODE == NS_GRAM;
-        put_block<LOW, LOW>(out, out, ti != tj, i, j, v, turned, lane);
-        if (FEW && i == j) {
-          float* rest = MODE == NS_GRAM ? q.a_rest : q.b_rest;
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (acc_row(e, lane) == (lane & 31)) rest[i + (lane & 31)] = v[e] - (float)(_Float16)v[e];
-        }
-      } else if (MODE == NS_APPLY) {
-        put_block<true, !FEW>(Factor{q.xt2, q.n / 16}, Factor{q.x, q.m / 16}, true, i, j, v, turned, lane);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) put_result<OUT>(q, i + acc_row(e, lane), j + (lane & 31), ldexpf(v[e] * st.unscale, -up), st.decay);
-      }
+      if (FEW && (turn || MODE == NS_POLY)) n.rest_j = rest[j + (lane & 31)];
     }
+    if (MODE == NS_LAST && q.master)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int64_t row = i + acc_row(e, lane), c = j + (lane & 31);
+        n.w[e] = row < q.rows && c < q.cols ? q.master[row * q.cols + c] : 0.f;
+      }
+  };
+  Ahead next;
+  ahead(next, 0);
+#pragma unroll
+  for (int b = 0; b < BI * BJ; ++b) {
+    f32x16 v = acc[b / BJ][b % BJ];
+    const int i = block_i(b), j = block_j(b);
+    const Ahead now = next;
+    if (b + 1 < BI * BJ) ahead(next, b + 1);
+    if (MODE == NS_POLY) {
+      // A at the same place: rows j, k i of a symmetric factor
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float hi = (float)now.hi[g][e];
+          float aa = v[4 * g + e];
+          if (FEW) aa = fmaf(hi, now.rest[g][e] + now.rest_j, aa);  // what the diagonal's low numbers add to A A
+          const bool diagonal = i + acc_row(4 * g + e, lane) == j + (lane & 31);
+          v[4 * g + e] = (fmaf(st.cc, aa, st.cb * (hi + (float)now.lo[g][e])) + (diagonal ? st.ca : 0.f)) * st.out_scale;
+        }
+    } else if (!SYM && FEW) {
+      // what the diagonal of B's low numbers adds to B X: X at the same place, in the factor whose rows are j
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[4 * g + e] = fmaf((float)now.hi[g][e], turn ? now.rest_j : now.rest[g][e], v[4 * g + e]);
+    }
+    if (MODE == NS_GRAM || MODE == NS_APPLY) {
+      const int power = MODE == NS_GRAM ? -2 * up : max(0, small - st.grown - st.growth) - up;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) v[e] = ldexpf(v[e] * st.unscale * st.out_scale, power);
+    }
+    if (SYM) {
+      const Factor out{MODE == NS_GRAM ? q.a : q.b, q.n / 16};
+      constexpr bool LOW = !FEW || MODE == NS_GRAM;
+      put_block<LOW, LOW>(out, out, ti != tj, i, j, v, turned, lane);
+      if (FEW && i == j) {
+        float* rest = MODE == NS_GRAM ? q.a_rest : q.b_rest;
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (acc_row(e, lane) == (lane & 31)) rest[i + (lane & 31)] = v[e] - (float)(_Float16)v[e];
+      }
+    } else if (MODE == NS_APPLY) {
+      put_block<true, !FEW>(Factor{q.xt2, q.n / 16}, Factor{q.x, q.m / 16}, true, i, j, v, turned, lane);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) put_result<OUT>(q, i + acc_row(e, lane), j + (lane & 31), ldexpf(v[e] * st.unscale, -up), st.decay, now.w[e]);
+    }
+  }
 }
 
 // ---- matrices that fit a compute unit's LDS ---------------------------------------------------
@@ -710,7 +766,7 @@ __global__ void __launch_bounds__(64 * SMALL_WAVES) ns_small_k(NsTable t, NsStep
   const float* result = reinterpret_cast<const float*>(smem);
 #pragma unroll 4
   for (int r = wave; r < rows; r += SMALL_WAVES)
-    for (int c = lane; c < cols; c += 64) put_result<OUT>(q, r, c, result[r * C + c], a.decay);
+    for (int c = lane; c < cols; c += 64) put_result<OUT>(q, r, c, result[r * C + c], a.decay, q.master ? q.master[r * cols + c] : 0.f);
 }
 
 // Gives every matrix of the table its workgroups; blocks(q): how many.
@@ -749,7 +805,7 @@ int64_t units_of(NsMatrix& q, int64_t most) {
 template <int SIDE, int MODE, int PP, int QP, typename OUT>
 hipError_t product_of(NsTable& t, const NsStep& p, hipStream_t st) {
   int64_t most = 1 << 20;
-  if (SIDE < 256) {
+  if constexpr (SIDE < 256) {
     // the shortest k ranges whose workgroups fit side by side
     for (most = NS_SHARED_STAGES; most < 1 << 20; most *= 2) {
       int64_t all = 0;
@@ -758,7 +814,8 @@ hipError_t product_of(NsTable& t, const NsStep& p, hipStream_t st) {
     }
   }
   const uint32_t blocks = spread(t, [&](NsMatrix& q) { return units_of<SIDE, MODE, PP, QP>(q, most); });
-  if (SIDE < 256 && blocks <= 256) return launch_product<SIDE, MODE, PP, QP, true, OUT>(blocks, t, p, st);
+  if constexpr (SIDE < 256)
+    if (blocks <= 256) return launch_product<SIDE, MODE, PP, QP, true, OUT>(blocks, t, p, st);
   return launch_product<SIDE, MODE, PP, QP, false, OUT>(blocks, t, p, st);
 }
 // Tiles as large as the sides' filling allows and a launch still has enough of.
