@@ -115,8 +115,12 @@ typedef struct {
   double eps;          /* AdamW (1e-8 usual) and AdaGrad (1e-10 usual) */
   double weight_decay; /* applied to tensors with two or more dimensions only; AdamW: decoupled,
                           AdaGrad / SGD: added to the gradient */
-  double momentum;     /* SGD; 0 = plain SGD, which keeps no state and moves no bytes */
+  double momentum;     /* SGD; 0 = plain SGD, which keeps no state and moves no bytes; HIFT_MUON (0.95 usual) */
 } hift_opt;
+/* HIFT_MUON (Jordan et al. 2024): the hidden layers' matrices -- q, k, v, gate and up each by itself -- take the update of hift_kernel_muon
+ * (lr, momentum in [0, 1), weight_decay; state array 0 is the momentum, array 1 stays 0), everything else AdamW's with the same lr, beta1,
+ * beta2, eps and weight_decay.  bf16 models: the orthogonalised step is within 2^-9 of itself; fp32 models keep fp32's exactness.  The work
+ * space of one layer (3.2 GB at the 7B shape) is part of the device arena. */
 /* HIFT_ADAFACTOR (section "Memory Efficiency Analysis" lists it among the optimizers): Shazeer and Stern
  * 2018, Algorithm 4 without momentum, with the caller's lr as the step size (no relative step, no
  * parameter scaling); epsilon_1 = 1e-30, clipping threshold 1, beta2_t = 1 - t^-0.8 with t the group's own
@@ -236,6 +240,24 @@ hift_status hift_group_units(const hift_model* mdl, int32_t group_id, int32_t* u
  * above the maxima, seq above the position table.  Token ids are not range-checked on the
  * host: an id outside [0, vocab) is clamped by the kernels. */
 hift_status hift_step(hift_model* mdl, const hift_batch* batch, int32_t group_id, float* loss_out);
+
+/* A forward pass that scores a batch instead of training on it: hift_kernel_token_logprob of the model's logits (rows: batch * seq positions,
+ * arch 1: batch sequences; V: the vocabulary, arch 1: n_classes), batch->labels being the tokens (classes) whose log probabilities are asked
+ * for, -1 for none.  scale: the reciprocal of the temperature.  logp, entropy: device fp32 [rows], top_logp, top_ids: device [rows, top];
+ * logp and entropy NULL where not wanted.  Queued on the compute stream; the call does not wait.
+ * group_id -1: evaluation, at any time, also of models with adapters and without a schedule.  group_id of a group: the pass also keeps what
+ * hift_step_scored needs, which then takes the step: backward from d_logp and d_entropy (device fp32 [rows]: derivatives of the caller's
+ * objective, which the step descends, by the scores; NULL for zeros), and all else as hift_step, on the same batch (same buffers, still
+ * unchanged) and group.  HIFT_ESTATE if the scores are not there: another pass or step, hift_write_params, hift_checkpoint_load or
+ * hift_set_group_schedule drops them, and so does the step itself.  hift_step's loss is d_logp = -1 / (rows with a target), d_entropy = 0. */
+typedef struct {
+  float scale;
+  int32_t top;
+  float *logp, *entropy, *top_logp;
+  int32_t* top_ids;
+} hift_scores;
+hift_status hift_score(hift_model* mdl, const hift_batch* batch, int32_t group_id, const hift_scores* scores);
+hift_status hift_step_scored(hift_model* mdl, const hift_batch* batch, int32_t group_id, const float* d_logp, const float* d_entropy);
 
 /* Learning rate used by following steps.  The caller applies its schedule when
  * hift_cycle_index changes (Algorithm 1: the rate moves only after all layers were updated). */

@@ -386,10 +386,10 @@ def _merge_heads(x):
 
 
 def loss_and_grad(cfg: dict, flat: np.ndarray, tokens: np.ndarray, labels: np.ndarray,
-                  need_grad: bool = True):
+                  need_grad: bool = True, objective=None):
     """Mean loss of the batch and, if asked, its gradient with respect to every parameter
     (flat, canonical order).  tokens int [B, S]; labels int [B, S] (decoders, -1 = no target)
-    or int [B] (encoder)."""
+    or int [B] (encoder).  objective(logits, labels): another value and its gradient in place of the mean cross-entropy."""
     a, L, d, H = cfg["arch"], cfg["n_layers"], cfg["d_model"], cfg["n_heads"]
     eps = cfg["norm_eps"]
     dt = flat.dtype
@@ -469,12 +469,12 @@ def loss_and_grad(cfg: dict, flat: np.ndarray, tokens: np.ndarray, labels: np.nd
     if a == ARCH_POSTLN_ENCODER:
         xc = x.reshape(B, S, d)[:, 0, :]
         logits = xc @ P["wc"].T + P["bc"]
-        loss, dlogits = cross_entropy_fwd(logits, labels.reshape(-1).astype(np.int64))
+        loss, dlogits = (objective or cross_entropy_fwd)(logits, labels.reshape(-1).astype(np.int64))
     else:
         xf, nf = norm_fwd(x, "gf" if rms else "lnf_g", "lnf_b")
         head = "tok_emb" if cfg.get("tie_embeddings", 0) else "whead"
         logits = xf @ P[head].T
-        loss, dlogits = cross_entropy_fwd(logits, labels.reshape(-1).astype(np.int64))
+        loss, dlogits = (objective or cross_entropy_fwd)(logits, labels.reshape(-1).astype(np.int64))
     if not need_grad:
         return float(loss), None
 
@@ -590,6 +590,70 @@ def sgd_update(theta, g, buf, t, lr, momentum, wd, decay_mask):
             buf[...] = momentum * buf + g
         g = buf
     theta -= lr * g
+
+
+# ----------------------------------------------------------------------------------------
+# scored tokens: log probabilities of given tokens and entropies, and the gradient of a sum of both
+# ----------------------------------------------------------------------------------------
+def token_scores(logits, targets, scale=1.0):
+    """(log probability of each row's target or 0 where it has none, entropy of each row) of softmax(scale logits)."""
+    z = scale * logits
+    z = z - z.max(-1, keepdims=True)
+    logp = z - np.log(np.exp(z).sum(-1, keepdims=True))
+    has = (targets >= 0) & (targets < logits.shape[-1])
+    rows = np.arange(len(targets))
+    return np.where(has, logp[rows, np.where(has, targets, 0)], 0.0), -(np.exp(logp) * logp).sum(-1)
+
+
+def token_scores_bwd(logits, targets, scale, d_logp, d_entropy):
+    """Gradient with respect to the logits of sum d_logp logp + d_entropy entropy."""
+    z = scale * logits
+    z = z - z.max(-1, keepdims=True)
+    logp = z - np.log(np.exp(z).sum(-1, keepdims=True))
+    p = np.exp(logp)
+    has = (targets >= 0) & (targets < logits.shape[-1])
+    g = np.where(has, d_logp, 0.0)[:, None]
+    d = -g * p - d_entropy[:, None] * p * (logp - (p * logp).sum(-1, keepdims=True))
+    rows = np.arange(len(targets))
+    d[rows[has], targets[has]] += g[has, 0]
+    return scale * d
+
+
+# ----------------------------------------------------------------------------------------
+# orthogonalised updates (Muon: Jordan et al. 2024)
+# ----------------------------------------------------------------------------------------
+MUON_STEPS, MUON_COEFFICIENTS, MUON_EPS = 5, (3.4445, -4.7750, 2.0315), 1e-7
+
+
+def orthogonalize(u):
+    """Newton-Schulz steps of degree five on u / max(|u|, eps): X <- a X + b X X^T X + c X X^T X X^T X."""
+    a, b, c = MUON_COEFFICIENTS
+    x = u / max(float(np.linalg.norm(u)), MUON_EPS)
+    for _ in range(MUON_STEPS):
+        if x.shape[0] <= x.shape[1]:
+            s = x @ x.T
+            x = a * x + (b * s + c * (s @ s)) @ x
+        else:
+            s = x.T @ x
+            x = a * x + x @ (b * s + c * (s @ s))
+    return x
+
+
+def muon_parts(name: str, shape, unit: int, cfg: dict):
+    """The matrices that a tensor's update orthogonalises one by one, as row ranges; empty where AdamW updates it: vectors, and what
+    belongs to the embeddings and head units.  q, k, v and gate, up are matrices of their own that are stored as one."""
+    if len(shape) < 2 or unit == 0 or unit == cfg["n_layers"] + 1:
+        return []
+    n = {"wqkv": 3, "wgu": 2}.get(name.split(".")[-1], 1)
+    return [(i * shape[0] // n, (i + 1) * shape[0] // n) for i in range(n)]
+
+
+def muon_update(theta, g, buf, lr, momentum, wd):
+    """One matrix, in place: buf <- momentum buf + g; theta <- (1 - lr wd) theta - lr 0.2 sqrt(max side) orthogonalize(g + momentum buf)."""
+    buf[...] = momentum * buf + g
+    step = orthogonalize(g + momentum * buf)
+    theta -= lr * wd * theta
+    theta -= lr * 0.2 * np.sqrt(max(theta.shape)) * step
 
 
 def adafactor_update(theta, g, state, shape, t, lr, wd, decay, eps1=1e-30, clip=1.0, decay_rate=0.8):
@@ -768,7 +832,7 @@ class HiftOracle:
         return lo, hi
 
     # -- Algorithm 1, steps e-k for one batch --
-    def step(self, tokens, labels, group_id: int) -> float:
+    def step(self, tokens, labels, group_id: int, objective=None) -> float:
         if self.k is None or not (0 <= group_id < self.k):
             raise ValueError("bad group")
         if self.half_weights:
@@ -778,7 +842,7 @@ class HiftOracle:
             at = self._half
         else:
             at = self.theta
-        loss, g = loss_and_grad(self.cfg, at, tokens, labels)
+        loss, g = loss_and_grad(self.cfg, at, tokens, labels, objective=objective)
         self.last_grad = g
         lo, hi = self.group_range(group_id)
         self.group_steps[group_id] += 1
@@ -800,12 +864,36 @@ class HiftOracle:
                     adafactor_update(self.theta[off:off + c], g[off:off + c], self.factored.setdefault(name, {}),
                                      shape, tg, o["lr"], o["weight_decay"], len(shape) >= 2)
                 off += c
+        elif o["kind"] == "muon":
+            off = 0
+            for name, shape, _kind, unit in param_tensors(self.cfg):
+                c = int(np.prod(shape))
+                if lo <= off and off + c <= hi:
+                    sl, parts = slice(off, off + c), muon_parts(name, shape, unit, self.cfg)
+                    for r0, r1 in parts:
+                        muon_update(self.theta[sl].reshape(shape)[r0:r1], g[sl].reshape(shape)[r0:r1], self.state1[sl].reshape(shape)[r0:r1], o["lr"],
+                                    o["momentum"], o["weight_decay"])
+                    if not parts:
+                        adamw_update(self.theta[sl], g[sl], self.state1[sl], self.state2[sl], tg, o["lr"], o["beta1"], o["beta2"], o["eps"],
+                                     o["weight_decay"], self.decay_mask[sl])
+                off += c
         else:
             raise ValueError("unknown optimizer")
         if self.half_weights:
             self._half[lo:hi] = bf16_round(self.theta[lo:hi])
         self.t += 1
         return loss
+
+    def step_scored(self, tokens, targets, group_id: int, coefficients, scale: float = 1.0):
+        """A step on an objective of the scores: coefficients(logp, entropy) gives its derivatives by both, one value a row.  Returns the scores."""
+        seen = {}
+
+        def objective(logits, rows):
+            seen["logp"], seen["entropy"] = token_scores(logits, rows, scale)
+            return 0.0, token_scores_bwd(logits, rows, scale, *coefficients(seen["logp"], seen["entropy"]))
+
+        self.step(tokens, targets, group_id, objective=objective)
+        return seen["logp"], seen["entropy"]
 
     def read_params(self, unit_lo: int = 0, unit_hi: int | None = None) -> np.ndarray:
         unit_hi = self.n if unit_hi is None else unit_hi

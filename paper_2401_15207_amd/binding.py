@@ -52,6 +52,10 @@ class Batch(C.Structure):
     _fields_ = [("tokens", C.c_void_p), ("labels", C.c_void_p), ("batch", C.c_int32), ("seq", C.c_int32)]
 
 
+class Scores(C.Structure):
+    _fields_ = [("scale", C.c_float), ("top", C.c_int32), ("logp", C.c_void_p), ("entropy", C.c_void_p), ("top_logp", C.c_void_p), ("top_ids", C.c_void_p)]
+
+
 class TensorInfo(C.Structure):
     _fields_ = [("name", C.c_char * 32), ("unit", C.c_int32), ("kind", C.c_int32), ("offset", C.c_int64),
                 ("rows", C.c_int64), ("cols", C.c_int64)]
@@ -90,6 +94,8 @@ _SIGS = {
     "hift_schedule_group_at": [_vp, _i64, _P(_i32)],
     "hift_group_units": [_vp, _i32, _P(_i32), _P(_i32)],
     "hift_step": [_vp, _P(Batch), _i32, _P(C.c_float)],
+    "hift_score": [_vp, _P(Batch), _i32, _P(Scores)],
+    "hift_step_scored": [_vp, _P(Batch), _i32, _vp, _vp],
     "hift_set_lr": [_vp, C.c_double],
     "hift_cycle_index": [_vp, _P(_i64), _P(_i64)],
     "hift_lora_param_count": [_P(Config), _P(_i64)],
@@ -590,6 +596,39 @@ class HiftModel:
         labels.record_stream(self.compute_stream)
         _check(lib.hift_step(self.h, C.byref(b), group_id, C.byref(loss) if want_loss else None))
         return loss.value if want_loss else None
+
+    def score(self, tokens, targets, group_id: int = -1, temperature: float = 1.0, top: int = 0):
+        """Log probabilities of targets (as labels in step: [B,S] or [B], -1 for none), entropies and, with top > 0, the most probable ids and their
+        log probabilities of every row, as device tensors (ready on torch's current stream).  group_id: of a step_scored to follow."""
+        assert tokens.dtype == self.torch.int32 and targets.dtype == self.torch.int32
+        assert tokens.is_cuda and targets.is_cuda and tokens.is_contiguous() and targets.is_contiguous()
+        f = dict(device=tokens.device, dtype=self.torch.float32)
+        out = {"logp": self.torch.empty(targets.shape, **f), "entropy": self.torch.empty(targets.shape, **f)}
+        if top:
+            out["top_logp"] = self.torch.empty(*targets.shape, top, **f)
+            out["top_ids"] = self.torch.empty(*targets.shape, top, device=tokens.device, dtype=self.torch.int32)
+        s = Scores(1.0 / temperature, top, *[_ptr(out.get(k)) for k in ("logp", "entropy", "top_logp", "top_ids")])
+        b = Batch(tokens.data_ptr(), targets.data_ptr(), tokens.shape[0], tokens.shape[1])
+        cur = self.torch.cuda.current_stream()
+        self.compute_stream.wait_stream(cur)
+        for t in (tokens, targets, *out.values()):
+            t.record_stream(self.compute_stream)
+        _check(lib.hift_score(self.h, C.byref(b), group_id, C.byref(s)))
+        cur.wait_stream(self.compute_stream)
+        return out
+
+    def step_scored(self, tokens, targets, group_id: int, d_logp=None, d_entropy=None):
+        """The step on what score(tokens, targets, group_id) has just scored; d_logp, d_entropy: derivatives of the objective to descend by the scores
+        (float32, in their shape)."""
+        for name, d in (("d_logp", d_logp), ("d_entropy", d_entropy)):
+            if d is not None and (d.dtype != self.torch.float32 or not d.is_cuda or not d.is_contiguous() or d.shape != targets.shape):
+                raise ValueError(f"{name}: contiguous float32 device values in the targets' shape {tuple(targets.shape)} expected")
+        b = Batch(tokens.data_ptr(), targets.data_ptr(), tokens.shape[0], tokens.shape[1])
+        self.compute_stream.wait_stream(self.torch.cuda.current_stream())
+        for t in (tokens, targets, d_logp, d_entropy):
+            if t is not None:
+                t.record_stream(self.compute_stream)
+        _check(lib.hift_step_scored(self.h, C.byref(b), group_id, _ptr(d_logp), _ptr(d_entropy)))
 
     def lora_param_count(self) -> int:
         n = _i64()

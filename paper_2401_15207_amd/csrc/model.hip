@@ -191,7 +191,7 @@ void make_order(int k, int strategy, uint64_t seed, int32_t* out) {
 }
 
 int n_state_of(const hift_opt& o) {
-  if (o.kind == HIFT_ADAMW) return 2;
+  if (o.kind == HIFT_ADAMW || o.kind == HIFT_MUON) return 2;  // (Muon's matrices use the first, what AdamW updates beside them both)
   if (o.kind == HIFT_ADAGRAD) return 1;
   if (o.kind == HIFT_ADAFACTOR) return 0;  // factored statistics: a few numbers per row and column, kept in HBM
   return o.momentum > 0.0 ? 1 : 0;
@@ -199,14 +199,32 @@ int n_state_of(const hift_opt& o) {
 
 hift_status check_opt(const hift_opt* o) {
   if (!o) return fail(HIFT_EINVAL, "optimizer is null");
-  if (o->kind < 0 || o->kind > 3) return fail(HIFT_EINVAL, "optimizer kind %d unknown", o->kind);
+  if (o->kind < 0 || o->kind > 4) return fail(HIFT_EINVAL, "optimizer kind %d unknown", o->kind);
   if (o->momentum < 0.0) return fail(HIFT_EINVAL, "momentum must be >= 0");
+  if (o->kind == HIFT_MUON && !(o->momentum < 1.0)) return fail(HIFT_EINVAL, "momentum must be in [0, 1)");
   return HIFT_OK;
 }
 
 // The steps of HIFT_MUON: Newton-Schulz of degree five with the coefficients of Jordan et al. 2024.
 NsRun muon_run(const hift_opt& o, bool bf16_model) {
   return NsRun{5, {3.4445, -4.7750, 2.0315}, 1e-7f, o.lr, (float)o.momentum, (float)(1.0 - o.lr * o.weight_decay), bf16_model};
+}
+
+// How many matrices side by side a tensor holds that HIFT_MUON orthogonalises one by one: hidden layers' matrices, q | k | v and gate | up
+// apart; 0: AdamW updates it (vectors, the embeddings and the head unit).
+int muon_parts(const Tensor& t, const hift_config& c) {
+  if (t.kind != HIFT_KIND_MATRIX || t.unit < 1 || t.unit > c.n_layers) return 0;
+  const std::string leaf = t.name.substr(t.name.find('.') + 1);
+  return leaf == "wqkv" ? 3 : leaf == "wgu" ? 2 : 1;
+}
+// The matrices of tensor t, without their arrays
+void muon_items(const Tensor& t, const hift_config& c, std::vector<NsItem>* items) {
+  const int n = muon_parts(t, c);
+  for (int i = 0; i < n; ++i) {
+    NsItem it{};
+    it.rows = t.rows / n; it.cols = t.cols; it.ld_src = t.cols;
+    items->push_back(it);
+  }
 }
 
 inline size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -303,6 +321,8 @@ struct hift_model {
   float* rowsq = nullptr;  // [maxT, d / 64] partial sums of squares of the rows a folded normalisation takes
   float* fac = nullptr;      // Adafactor statistics of every tensor (resident: they are tiny)
   float* af_work = nullptr;  // Adafactor reduction scratch
+  void* ns_work = nullptr;   // HIFT_MUON: work space of one layer's orthogonalisation
+  size_t ns_bytes = 0;
   int64_t n_fac = 0;
   size_t af_work_floats = 0;
   float* grad = nullptr;
@@ -331,6 +351,9 @@ struct hift_model {
   // run on gemm_lds_k whatever the vocabulary.  1936 tokens, width 1280, vocabulary 12466, rows of 12466 values (gemm_f32_k) and
   // of 12472: input gradient 728 and 131 us, weight gradient 542 and 66, product 104 and 79; errors against 64 bits over 44 models the same.
   int64_t logits_ld = 0;
+  // what hift_score leaves for hift_step_scored: the group it was made for (-1: none), the batch's sides, the scale, stats and entropies of the rows
+  int scored_group = -1, scored_batch = 0, scored_seq = 0;
+  float scored_scale = 1.f, *score_stats = nullptr, *score_entropy = nullptr;
   float *st_e = nullptr, *st_f = nullptr, *row_loss = nullptr, *part = nullptr;
   int32_t* tok_stamps = nullptr;  // which embeddings backward a token was last seen in, or null: the table's gradient is cleared instead
   int32_t tok_stamp = 0;
@@ -413,6 +436,10 @@ void carve(hift_model* mm, void* dev, size_t* dev_bytes, size_t* pinned_bytes, s
     b.cat = MEM_WORK;
     M.af_work = (float*)b.take(M.af_work_floats * 4);
   }
+  if (M.ns_bytes > 0) {
+    b.cat = MEM_WORK;
+    M.ns_work = b.take(M.ns_bytes);
+  }
   if (M.lora_r > 0) {
     const size_t nl = (size_t)M.n_lora;
     b.cat = MEM_MASTER;
@@ -461,6 +488,8 @@ void carve(hift_model* mm, void* dev, size_t* dev_bytes, size_t* pinned_bytes, s
   }
   b.cat = MEM_WORK;
   M.row_loss = (float*)b.take((T + 1) * 4);
+  M.score_stats = (float*)b.take(T * 2 * 4);
+  M.score_entropy = (float*)b.take(T * 4);
   // (Adafactor reads the gradient several times, and a tied table's has a part in every row)
   M.tok_stamps = d % 4 == 0 && !c.tie_embeddings && M.opt.kind != HIFT_ADAFACTOR && c.lora_rank == 0 ? (int32_t*)b.take(V * 4) : nullptr;
   M.loss_dev = M.loss_at = (float*)b.take(LOSS_RING * 4);
@@ -527,6 +556,15 @@ hift_status init_model_shape(hift_model* M, const hift_config* cfg, const hift_o
       t.fac_off = M->n_fac;
       M->n_fac += t.fac_count();
       M->af_work_floats = std::max(M->af_work_floats, adafactor_work_floats(t.rows, t.cols));
+    }
+  M->ns_bytes = 0;
+  if (opt->kind == HIFT_MUON && cfg->lora_rank == 0)
+    for (int u = 1; u <= cfg->n_layers; ++u) {
+      std::vector<NsItem> items;
+      for (int i = M->lay.unit_first[u]; i < M->lay.unit_first[u + 1]; ++i) muon_items(M->lay.t[i], *cfg, &items);
+      for (const NsItem& it : items)
+        if (it.rows > NS_SIDE_MAX || it.cols > NS_SIDE_MAX) return fail(HIFT_EINVAL, "HIFT_MUON takes matrices of at most %lld on a side", (long long)NS_SIDE_MAX);
+      M->ns_bytes = std::max(M->ns_bytes, ns_workspace(items.data(), (int)items.size()));
     }
   // Which matrices get copies in fragment order: those whose contraction, at the largest batch,
   // is one the packed-operand kernel takes.
@@ -1090,8 +1128,17 @@ Names layer_names(const hift_model* M, int l) {
   return n;
 }
 
-// keep_from: lowest unit the backward pass will reach; layers below it keep no pre-activations
-hift_status forward(hift_model* M, const hift_batch* bt, int keep_from) {
+hift_status score_rows(hift_model* M, int64_t rows, int V, const int32_t* targets, const hift_scores& s) {
+  RW(RW_CROSS_ENTROPY, 1.0 * rows * V * M->es, token_logprob(M->dt, rows, V, M->logits_ld, M->logits, targets, s.scale, s.top, s.logp, M->score_entropy,
+                                                             M->score_stats, s.top_logp, s.top_ids, M->cs));
+  if (s.entropy) HIP_TRY(hipMemcpyAsync(s.entropy, M->score_entropy, (size_t)rows * 4, hipMemcpyDeviceToDevice, M->cs));
+  return HIFT_OK;
+}
+
+// keep_from: lowest unit the backward pass will reach; layers below it keep no pre-activations.  scores: instead of the loss and its gradient,
+// the log probabilities of the labels, entropies and alternatives; the logits stay.
+hift_status forward(hift_model* M, const hift_batch* bt, int keep_from, const hift_scores* scores = nullptr) {
+  M->scored_group = -1;
   const hift_config& c = M->cfg;
   const int B = bt->batch, S = bt->seq;
   const int64_t T = (int64_t)B * S;
@@ -1172,6 +1219,7 @@ hift_status forward(hift_model* M, const hift_batch* bt, int keep_from) {
       RW(RW_FIRST_ROWS, 2.0 * B * d * es, gather_first(dt, B, S, d, xl, M->xcls, st));
     }
     ST_TRY(linear(M, M->xcls, B, M->T_("wc"), &M->T_("bc"), nullptr, M->logits));
+    if (scores) return score_rows(M, B, c.n_classes, bt->labels, *scores);
     if (cross_entropy_counts_apart(B)) RW(RW_LOSS_MEAN, 4.0 * (B), cross_entropy_count(B, bt->labels, M->row_loss, st));
     RW(RW_CROSS_ENTROPY, 2.0 * (B) * (c.n_classes) * es, cross_entropy_rows(dt, B, c.n_classes, M->logits_ld, M->logits, bt->labels, M->row_loss, st));
     RW(RW_LOSS_MEAN, 4.0 * (B), cross_entropy_mean(B, M->row_loss, M->loss_at, st));
@@ -1181,6 +1229,7 @@ hift_status forward(hift_model* M, const hift_batch* bt, int keep_from) {
       else RW(RW_NORM_FWD, 2.0 * T * d * es, norm_fwd(dt, false, T, d, c.norm_eps, xl, M->W("lnf_g"), M->W("lnf_b"), M->xf, M->st_f, st));
     }
     ST_TRY(linear(M, M->xf, T, M->T_(c.tie_embeddings ? "tok_emb" : "whead"), nullptr, nullptr, M->logits, nullptr, nullptr, M->logits_ld));
+    if (scores) return score_rows(M, T, c.vocab, bt->labels, *scores);
     if (cross_entropy_counts_apart(T)) RW(RW_LOSS_MEAN, 4.0 * (T), cross_entropy_count(T, bt->labels, M->row_loss, st));
     RW(RW_CROSS_ENTROPY, 2.0 * (T) * (c.vocab) * es, cross_entropy_rows(dt, T, c.vocab, M->logits_ld, M->logits, bt->labels, M->row_loss, st));
     RW(RW_LOSS_MEAN, 4.0 * (T), cross_entropy_mean(T, M->row_loss, M->loss_at, st));
@@ -1750,6 +1799,7 @@ hift_status hift_set_group_schedule(hift_model* M, hift_strategy s, int32_t m, u
   hift_status st = sync_all(M);
   if (st != HIFT_OK) return st;
   M->forget_slots();
+  M->scored_group = -1;
   M->m = m;
   M->k = group_count(M->lay.n_units, m);
   M->order.resize(M->k);
@@ -1946,15 +1996,62 @@ hift_status hift_cycle_index(const hift_model* M, int64_t* steps_done, int64_t* 
   return HIFT_OK;
 }
 
-hift_status hift_step(hift_model* M, const hift_batch* bt, int32_t gid, float* loss_out) {
+namespace {
+hift_status check_batch(const hift_model* M, const hift_batch* bt) {
   if (!M || !bt) return fail(HIFT_EINVAL, "null argument");
-  if (M->k == 0) return fail(HIFT_ESTATE, "no schedule set");
-  if (gid < 0 || gid >= M->k) return fail(HIFT_EINVAL, "group %d outside [0,%d)", gid, M->k);
   if (bt->batch < 1 || bt->seq < 1 || bt->batch > M->max_batch || bt->seq > M->max_seq_len)
     return fail(HIFT_EINVAL, "batch %d x seq %d outside the maxima %d x %d", bt->batch, bt->seq, M->max_batch,
                 M->max_seq_len);
   if (!bt->tokens || !bt->labels) return fail(HIFT_EINVAL, "tokens or labels null");
+  return HIFT_OK;
+}
+hift_status check_step(const hift_model* M, const hift_batch* bt, int32_t gid) {
+  if (!M || !bt) return fail(HIFT_EINVAL, "null argument");
+  if (M->k == 0) return fail(HIFT_ESTATE, "no schedule set");
+  if (gid < 0 || gid >= M->k) return fail(HIFT_EINVAL, "group %d outside [0,%d)", gid, M->k);
+  ST_TRY(check_batch(M, bt));
   if (M->lora_r > 0) return fail(HIFT_ESTATE, "a model with adapters trains its adapters: use hift_lora_step");
+  return HIFT_OK;
+}
+// What a step's logits turn into their gradient with: nothing here (the loss's forward pass leaves it), or the scores' derivatives
+struct ScoreGrad { const float *d_logp, *d_entropy; };
+hift_status step_of(hift_model* M, const hift_batch* bt, int32_t gid, const ScoreGrad* scored, float* loss_out);
+}  // namespace
+
+hift_status hift_step(hift_model* M, const hift_batch* bt, int32_t gid, float* loss_out) {
+  ST_TRY(check_step(M, bt, gid));
+  return step_of(M, bt, gid, nullptr, loss_out);
+}
+
+hift_status hift_score(hift_model* M, const hift_batch* bt, int32_t gid, const hift_scores* s) {
+  if (!M || !bt || !s) return fail(HIFT_EINVAL, "null argument");
+  if (gid >= 0) ST_TRY(check_step(M, bt, gid));
+  else ST_TRY(check_batch(M, bt));
+  const int V = M->cfg.arch == HIFT_ARCH_POSTLN_ENCODER ? M->cfg.n_classes : M->cfg.vocab;
+  if (!(s->scale > 0.f) || std::isinf(s->scale)) return fail(HIFT_EINVAL, "scale must be positive and finite");
+  if (s->top < 0 || s->top > LOGPROB_TOP_MAX || s->top > V) return fail(HIFT_EINVAL, "top must be in [0, min(%d, %d)]", LOGPROB_TOP_MAX, V);
+  if (s->top > 0 && (!s->top_logp || !s->top_ids)) return fail(HIFT_EINVAL, "top needs top_logp and top_ids");
+  int ulo = M->lay.n_units, uhi;
+  if (gid >= 0) {
+    int64_t plo, cnt;
+    group_range(M, gid, &ulo, &uhi, &plo, &cnt);
+  }
+  ST_TRY(forward(M, bt, ulo, s));
+  M->scored_group = gid >= 0 ? gid : -1;
+  M->scored_batch = bt->batch; M->scored_seq = bt->seq; M->scored_scale = s->scale;
+  return HIFT_OK;
+}
+
+hift_status hift_step_scored(hift_model* M, const hift_batch* bt, int32_t gid, const float* d_logp, const float* d_entropy) {
+  ST_TRY(check_step(M, bt, gid));
+  if (M->scored_group != gid || M->scored_batch != bt->batch || M->scored_seq != bt->seq)
+    return fail(HIFT_ESTATE, "no scores of this batch and group: call hift_score for group %d first, and nothing that changes the model in between", gid);
+  const ScoreGrad g{d_logp, d_entropy};
+  return step_of(M, bt, gid, &g, nullptr);
+}
+
+namespace {
+hift_status step_of(hift_model* M, const hift_batch* bt, int32_t gid, const ScoreGrad* scored, float* loss_out) {
   int ulo, uhi;
   int64_t plo, cnt;
   group_range(M, gid, &ulo, &uhi, &plo, &cnt);
@@ -1966,7 +2063,17 @@ hift_status hift_step(hift_model* M, const hift_batch* bt, int32_t gid, float* l
     ST_TRY(M->held.advance(gid, M->order, M->t, [&](int g, int spare, bool* done) { return fetch_state(M, g, spare, done); }));
   }
 
-  ST_TRY(forward(M, bt, ulo));
+  if (scored) {
+    const bool enc = M->cfg.arch == HIFT_ARCH_POSTLN_ENCODER;
+    const int64_t rows = enc ? bt->batch : (int64_t)bt->batch * bt->seq;
+    const int V = enc ? M->cfg.n_classes : M->cfg.vocab;
+    M->scored_group = -1;  // the logits' place is taken by their gradient
+    RW(RW_CROSS_ENTROPY, 2.0 * rows * V * M->es, token_logprob_bwd(M->dt, rows, V, M->logits_ld, M->logits, bt->labels, M->scored_scale, M->score_stats,
+                                                                   M->score_entropy, scored->d_logp, scored->d_entropy, M->logits_ld, M->logits,
+                                                                   (int)M->logits_ld, M->cs));
+  } else {
+    ST_TRY(forward(M, bt, ulo));
+  }
   ST_TRY(backward(M, bt, ulo, uhi, plo));
 
   // ---- optimizer on the group (its update number drives AdamW's bias correction) ----
@@ -1995,6 +2102,7 @@ hift_status hift_step(hift_model* M, const hift_batch* bt, int32_t gid, float* l
   std::vector<const Tensor*> repack_after;  // matrices whose fragment-order copies the update does not write itself
   {
     double bytes_per = M->n_state == 2 ? 28.0 : (M->n_state == 1 ? 20.0 : 12.0);
+    if (M->opt.kind == HIFT_MUON) oa.kind = HIFT_ADAMW;   // (of what is not orthogonalised)
     if (M->opt.kind == HIFT_ADAFACTOR) bytes_per = 24.0;  // the gradient is read four times (row, column, clipping, update)
     // Which product of AdamW's moments is fused (see opt_math) follows from the layout alone, so that it is the same wherever state
     // and master live: the old moment's for tensors that lie in whole 16-byte pieces in the model and in the group, in a model whose
@@ -2003,14 +2111,33 @@ hift_status hift_step(hift_model* M, const hift_batch* bt, int32_t gid, float* l
     auto grad_fused = [&](const Tensor& t) {
       return t.count() % 8 != 0 || t.off % 4 != 0 || (t.off - plo) % 4 != 0 || (M->n_state == 2 && M->lay.n_params % 4 != 0);
     };
+    std::vector<std::vector<NsItem>> ortho;  // HIFT_MUON: each layer's matrices
     std::vector<OptItem> items, packed_items;
     std::vector<PackItem> packs;
     double bytes = bytes_per * cnt;
+    int ortho_unit = -1;
     for (int i = M->lay.unit_first[ulo]; i < M->lay.unit_first[uhi]; ++i) {
       const Tensor& t = M->lay.t[i];
       const bool has_copies = M->wpk && (t.pk_fwd >= 0 || t.pk_bwd >= 0);
       void* cc = M->dt == DT_BF16 ? M->W(t) : nullptr;  // null also for a matrix kept only in fragment order
       if (cc) bytes += 2.0 * t.count();
+      if (M->opt.kind == HIFT_MUON && muon_parts(t, M->cfg) > 0) {
+        if (ortho.empty() || ortho.back().empty() || ortho_unit != t.unit) ortho.emplace_back();
+        ortho_unit = t.unit;
+        const size_t first = ortho.back().size();
+        muon_items(t, M->cfg, &ortho.back());
+        for (size_t j = first; j < ortho.back().size(); ++j) {
+          NsItem& it = ortho.back()[j];
+          const int64_t at = (int64_t)(j - first) * it.rows * it.cols;
+          it.src = M->grad + (t.off - plo) + at;
+          it.momentum = state_of(t, 0) + at;
+          it.master = master_of(t) + at;
+          it.copy = cc ? reinterpret_cast<unsigned char*>(cc) + at * 2 : nullptr;
+        }
+        bytes -= 8.0 * t.count();  // one state array, read and written
+        if (has_copies) repack_after.push_back(&t);
+        continue;
+      }
       OptItem item{t.count(), t.kind == HIFT_KIND_MATRIX, M->unit_steps[t.unit], master_of(t), M->grad + (t.off - plo), state_of(t, 0), state_of(t, 1), cc, grad_fused(t)};
       if (M->tok_stamps && t.name == "tok_emb") {
         item.stamps = M->tok_stamps; item.stamp = M->tok_stamp; item.row = (int32_t)t.cols;
@@ -2036,6 +2163,8 @@ hift_status hift_step(hift_model* M, const hift_batch* bt, int32_t gid, float* l
       }
       items.clear();
     }
+    for (const auto& layer : ortho)
+      K_TRY(newton_schulz(layer.data(), (int)layer.size(), DT_F32, DT_F32, muon_run(M->opt, M->dt == DT_BF16), M->ns_work, M->cs));
     // gains first: those of a normalisation that is folded into a weight go into its copy with their new values
     if (!items.empty()) K_TRY(optimizer_update(oa, items.data(), (int)items.size(), M->cs));
     if (!packs.empty()) K_TRY(optimizer_update_packed(oa, packed_items.data(), packs.data(), (int)packs.size(), M->cs));
@@ -2070,6 +2199,7 @@ hift_status hift_step(hift_model* M, const hift_batch* bt, int32_t gid, float* l
   }
   return HIFT_OK;
 }
+}  // namespace
 
 // ---- low-rank adapters -------------------------------------------------------------------------------------
 hift_status hift_lora_param_count(const hift_config* cfg, int64_t* n) {
@@ -2189,6 +2319,7 @@ hift_status write_params_from(hift_model* M, int32_t ulo, int32_t uhi, const flo
   int64_t off, cnt;
   ST_TRY(unit_span(M, ulo, uhi, &off, &cnt));
   if ((int64_t)src_count != cnt) return fail(HIFT_EINVAL, "buffer holds %zu floats, units hold %lld", src_count, (long long)cnt);
+  M->scored_group = -1;
   ST_TRY(sync_all(M));
   if (M->master_host) {
     if (src_on_device) {
@@ -2541,6 +2672,7 @@ hift_status hift_kernel_optimizer(const hift_opt* opt, int64_t count, int32_t de
   if (s != HIFT_OK) return s;
   if (count < 0 || t < 1) return fail(HIFT_EINVAL, "count must be >= 0 and t >= 1");
   if (opt->kind == HIFT_ADAFACTOR) return fail(HIFT_EINVAL, "Adafactor works on whole tensors; it has no element-wise kernel entry");
+  if (opt->kind == HIFT_MUON) return fail(HIFT_EINVAL, "HIFT_MUON works on whole matrices: hift_kernel_muon");
   OptArgs oa{opt->kind, opt->lr, opt->beta1, opt->beta2, opt->eps, opt->weight_decay, opt->momentum};
   const uintptr_t low = reinterpret_cast<uintptr_t>(master) | reinterpret_cast<uintptr_t>(grad) | reinterpret_cast<uintptr_t>(state1) |
                         reinterpret_cast<uintptr_t>(state2) | reinterpret_cast<uintptr_t>(compute_copy);
