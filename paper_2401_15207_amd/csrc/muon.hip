@@ -154,12 +154,25 @@ __device__ __forceinline__ int start_scale(double sum_of_squares, float eps, flo
 
 // ---- U -> X and X^T in fragment order --------------------------------------------------------
 template <typename T>
-__global__ void __launch_bounds__(256) ns_start_k(NsTable t, float mu, float eps, float scale) {
+__global__ void __launch_bounds__(256) ns_start_k(NsTable t, float mu, float eps, float scale, bool few) {
   __shared__ float tile[64][65];
   __shared__ double red[4];
   const int at = matrix_of(t, blockIdx.x), id = blockIdx.x - t.first[at];
   const NsMatrix& q = t.m[at];
   const int th = threadIdx.x, lane = th & 63;
+  // sides as they lie in memory, filled up
+  const int R = q.tall ? q.m : q.n, C = q.tall ? q.n : q.m;
+  const int tiles_c = C / 64;
+  const int64_t r0 = (int64_t)(id / tiles_c) * 64, c0 = (int64_t)(id % tiles_c) * 64;
+  // the tile is on its way while the norm's parts are summed
+  float v[16], m[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const int64_t r = r0 + i * 4 + (th >> 6), c = c0 + lane;
+    const bool in = r < q.rows && c < q.cols;
+    v[i] = in ? to_f32(reinterpret_cast<const T*>(q.src)[r * q.ld_src + c]) : 0.f;
+    m[i] = in && q.momentum ? q.momentum[r * q.cols + c] : 0.f;
+  }
   static_assert(NS_NORM_PARTS == 256, "one part a thread");
   double s = q.norm_parts[th];
   for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
@@ -168,19 +181,10 @@ __global__ void __launch_bounds__(256) ns_start_k(NsTable t, float mu, float eps
   double by;
   const int small = start_scale((red[0] + red[1]) + (red[2] + red[3]), eps, scale, &by);
   if (id == 0 && th == 0) *q.small = small;
-  // sides as they lie in memory, filled up
-  const int R = q.tall ? q.m : q.n, C = q.tall ? q.n : q.m;
-  const int tiles_c = C / 64;
-  const int64_t r0 = (int64_t)(id / tiles_c) * 64, c0 = (int64_t)(id % tiles_c) * 64;
-  for (int i = th >> 6; i < 64; i += 4) {
-    const int64_t r = r0 + i, c = c0 + lane;
-    float v = 0.f;
-    if (r < q.rows && c < q.cols) {
-      v = to_f32(reinterpret_cast<const T*>(q.src)[r * q.ld_src + c]);
-      if (q.momentum) v = fmaf(mu, q.momentum[r * q.cols + c], v);
-      v = (float)((double)v * by);
-    }
-    tile[i][lane] = v;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const float u = q.momentum ? fmaf(mu, m[i], v[i]) : v[i];
+    tile[i * 4 + (th >> 6)][lane] = (float)((double)u * by);
   }
   __syncthreads();
   // as a factor of rows R and k C, and as one of rows C and k R
@@ -196,7 +200,7 @@ __global__ void __launch_bounds__(256) ns_start_k(NsTable t, float mu, float eps
     }
     _Float16* p = along.block((int)(r0 / 32) + rb, (int)(c0 / 16) + kb) + lane * 8;
     *reinterpret_cast<half8*>(p) = hi;
-    *reinterpret_cast<half8*>(p + along.low()) = lo;
+    if (!few || q.tall) *reinterpret_cast<half8*>(p + along.low()) = lo;  // (fewer products never read X's own low numbers)
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       _Float16 h, l;
@@ -205,7 +209,7 @@ __global__ void __launch_bounds__(256) ns_start_k(NsTable t, float mu, float eps
     }
     p = across.block((int)(c0 / 32) + rb, (int)(r0 / 16) + kb) + lane * 8;
     *reinterpret_cast<half8*>(p) = hi;
-    *reinterpret_cast<half8*>(p + across.low()) = lo;
+    if (!few || !q.tall) *reinterpret_cast<half8*>(p + across.low()) = lo;
   }
 }
 
@@ -855,8 +859,8 @@ hipError_t steps_of(NsTable& t, int side, int dt_src, int dt_dst, const NsRun& r
   if (!ns_scales(run.co, r, &s)) return hipErrorInvalidValue;
   const int growth = ns_growth(run.co);
   const uint32_t squares = spread(t, [](const NsMatrix& q) { return (int64_t)(q.n / 64) * (q.m / 64); });
-  if (dt_src == DT_BF16) ns_start_k<bf16><<<squares, 256, 0, st>>>(t, run.mu, run.eps, s.x);
-  else ns_start_k<float><<<squares, 256, 0, st>>>(t, run.mu, run.eps, s.x);
+  if (dt_src == DT_BF16) ns_start_k<bf16><<<squares, 256, 0, st>>>(t, run.mu, run.eps, s.x, few);
+  else ns_start_k<float><<<squares, 256, 0, st>>>(t, run.mu, run.eps, s.x, few);
   for (int k = 0; k < run.steps; ++k) {
     NsStep gram{}, poly{}, apply{};
     gram.shared = poly.shared = apply.shared = shared;
