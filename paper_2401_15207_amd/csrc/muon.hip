@@ -560,21 +560,37 @@ struct NsSteps {
 };
 constexpr int SMALL_WAVES = 8, SMALL_TILES = NS_SMALL_TILES;
 
-__device__ __forceinline__ _Float16* entry(const Factor& f, int row, int k) {
-  return f.block(row >> 5, k >> 4) + ((row & 31) + 32 * ((k >> 3) & 1)) * 8 + (k & 7);
-}
+// A factor in LDS: as in memory, or (SPREAD, X) with the halves of a block 544 bytes and blocks 1168 bytes apart, so that the two-byte
+// writes of a turned tile, whose lanes meet in four banks otherwise, fall into all of them.
+template <bool SPREAD>
+struct LdsFactor {
+  static constexpr int HALF = SPREAD ? 272 : 256, BLOCK = SPREAD ? 584 : 512;  // numbers
+  _Float16* p;
+  int kb;
+  static size_t bytes(int rows, int k) { return (size_t)(rows / 32) * (k / 16) * 2 * BLOCK * 2; }
+  __device__ __forceinline__ int low() const { return kb * BLOCK; }
+  __device__ __forceinline__ _Float16* entry(int row, int k) const {
+    return p + ((row >> 5) * 2 * kb + (k >> 4)) * BLOCK + ((k >> 3) & 1) * HALF + (row & 31) * 8 + (k & 7);
+  }
+  __device__ __forceinline__ const half8& fragment(int rb, int b, int lane) const {
+    return *reinterpret_cast<const half8*>(p + (rb * 2 * kb + b) * BLOCK + (lane >> 5) * HALF + (lane & 31) * 8);
+  }
+  __device__ __forceinline__ const half8& low_fragment(int rb, int b, int lane) const {
+    return *reinterpret_cast<const half8*>(p + low() + (rb * 2 * kb + b) * BLOCK + (lane >> 5) * HALF + (lane & 31) * 8);
+  }
+};
 // one 32 x 32 tile of P Q^T, k blocks [k0, k1), an even number of them: two at a time, the next two's fragments on their way, and three
 // sums apart, as a product waits for the one before it in its sum
-__device__ __forceinline__ void small_product(f32x16& acc, const Factor& P, int rb, const Factor& Q, int cb, int k0, int k1, int lane) {
+template <class F, class G>
+__device__ __forceinline__ void small_product(f32x16& acc, const F& P, int rb, const G& Q, int cb, int k0, int k1, int lane) {
   half8 f[2][2][4];
   auto read = [&](int to, int k) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      const _Float16 *p = P.block(rb, k + j) + lane * 8, *q = Q.block(cb, k + j) + lane * 8;
-      f[to][j][0] = *reinterpret_cast<const half8*>(p);
-      f[to][j][1] = *reinterpret_cast<const half8*>(p + P.low());
-      f[to][j][2] = *reinterpret_cast<const half8*>(q);
-      f[to][j][3] = *reinterpret_cast<const half8*>(q + Q.low());
+      f[to][j][0] = P.fragment(rb, k + j, lane);
+      f[to][j][1] = P.low_fragment(rb, k + j, lane);
+      f[to][j][2] = Q.fragment(cb, k + j, lane);
+      f[to][j][3] = Q.low_fragment(cb, k + j, lane);
     }
   };
   f32x16 low[2] = {};
@@ -597,7 +613,7 @@ __device__ __forceinline__ void small_product(f32x16& acc, const Factor& P, int 
   acc += low[0] + low[1];
 }
 // block (rows j, k i) from accumulators, as put_block leaves it
-__device__ __forceinline__ void small_put(const Factor& f, int ib, int jb, const f32x16& v, int lane) {
+__device__ __forceinline__ void small_put(const LdsFactor<false>& f, int ib, int jb, const f32x16& v, int lane) {
 #pragma unroll
   for (int g = 0; g < 4; ++g) {
     half4 hi, lo;
@@ -607,13 +623,12 @@ __device__ __forceinline__ void small_put(const Factor& f, int ib, int jb, const
       split(v[4 * g + e], h, l);
       hi[e] = h; lo[e] = l;
     }
-    _Float16* p = f.block(jb, ib * 2 + (g >> 1)) + ((lane & 31) + 32 * (g & 1)) * 8 + 4 * (lane >> 5);
+    _Float16* p = f.entry(jb * 32 + (lane & 31), ib * 32 + 8 * g + 4 * (lane >> 5));
     *reinterpret_cast<half4*>(p) = hi;
     *reinterpret_cast<half4*>(p + f.low()) = lo;
   }
 }
 
-// What bounds it: waits one after the other, 7 us a step at 64 x 256 (one workgroup, six barriers) and 25 for the way in and out.
 template <typename T, typename OUT>
 __global__ void __launch_bounds__(64 * SMALL_WAVES) ns_small_k(NsTable t, NsSteps a) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
@@ -622,34 +637,38 @@ __global__ void __launch_bounds__(64 * SMALL_WAVES) ns_small_k(NsTable t, NsStep
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = q.n, m = q.m, nb = n / 32, mb = m / 32;
   _Float16* const at = reinterpret_cast<_Float16*>(smem);
-  const Factor X{at, m / 16}, XT{at + n * m * 2, n / 16}, AB{at + n * m * 4, n / 16};
+  const LdsFactor<false> XT{at, n / 16}, AB{at + n * m * 2, n / 16};
+  const LdsFactor<true> X{at + n * m * 2 + n * n * 2, m / 16};
   const int rows = (int)q.rows, cols = (int)q.cols, R = q.tall ? m : n, C = q.tall ? n : m;
 
-  // Eight neighbours of a row a thread and round, lanes down the rows (across them, all lanes of the writes below meet in one LDS bank).
+  // Eight neighbours of a row a thread and round, lanes down the rows; all loads before the first wait.
+  constexpr int ROUNDS = SMALL_TILES * 32 * 32 / 64 / 8;
   const int pieces = R * C / 8;
   const T* src = reinterpret_cast<const T*>(q.src);
+  float u[ROUNDS][8], b[ROUNDS][8];
+#pragma unroll
+  for (int o = 0; o < ROUNDS; ++o) {
+    const int p = threadIdx.x + o * 64 * SMALL_WAVES, r = p % R, c = p / R * 8, left = p < pieces && r < rows ? cols - c : 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      u[o][e] = e < left ? to_f32(src[r * q.ld_src + c + e]) : 0.f;
+      b[o][e] = e < left && q.momentum ? q.momentum[r * cols + c + e] : 0.f;
+    }
+  }
   double sum = 0.0;
-#pragma unroll 1
-  for (int p = threadIdx.x; p < pieces; p += 64 * SMALL_WAVES) {
-    const int r = p % R, c = p / R * 8;
-    if (r >= rows) continue;
-    float u[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) u[e] = c + e < cols ? to_f32(src[r * q.ld_src + c + e]) : 0.f;
+  for (int o = 0; o < ROUNDS; ++o) {
     if (q.momentum) {
-      float* mp = q.momentum + r * cols + c;
-      float b[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) b[e] = c + e < cols ? mp[e] : 0.f;
+      const int p = threadIdx.x + o * 64 * SMALL_WAVES, r = p % R, c = p / R * 8, left = p < pieces && r < rows ? cols - c : 0;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        b[e] = fmaf(a.mu, b[e], u[e]);
-        if (c + e < cols) mp[e] = b[e];
-        u[e] = fmaf(a.mu, b[e], u[e]);
+        b[o][e] = fmaf(a.mu, b[o][e], u[o][e]);
+        if (e < left) q.momentum[r * cols + c + e] = b[o][e];
+        u[o][e] = fmaf(a.mu, b[o][e], u[o][e]);
       }
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sum += (double)u[e] * u[e];
+    for (int e = 0; e < 8; ++e) sum += (double)u[o][e] * u[o][e];
   }
   for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
   if (lane == 0) red[wave] = sum;
@@ -658,36 +677,30 @@ __global__ void __launch_bounds__(64 * SMALL_WAVES) ns_small_k(NsTable t, NsStep
   for (int w = 1; w < SMALL_WAVES; ++w) sum += red[w];
   double by;
   const int small = start_scale(sum, a.eps, a.x[0], &by);
-  // as a factor of rows r and k c, and as one of rows c and k r
-  const Factor along = q.tall ? XT : X, turned = q.tall ? X : XT;
-#pragma unroll 1
-  for (int p = threadIdx.x; p < pieces; p += 64 * SMALL_WAVES) {
-    const int r = p % R, c = p / R * 8;
-    float u[8];
+  // as a factor of rows r and k c, and as one of rows c and k r (whose neighbouring rows are 8 numbers apart)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) u[e] = r < rows && c + e < cols ? to_f32(src[r * q.ld_src + c + e]) : 0.f;
-    if (q.momentum)  // (what this very thread has written)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) u[e] = r < rows && c + e < cols ? fmaf(a.mu, q.momentum[r * cols + c + e], u[e]) : 0.f;
+  for (int o = 0; o < ROUNDS; ++o) {
+    const int p = threadIdx.x + o * 64 * SMALL_WAVES, r = p % R, c = p / R * 8;
+    if (p >= pieces) break;
+    _Float16 *along = q.tall ? XT.entry(r, c) : X.entry(r, c), *turned = q.tall ? X.entry(c, r) : XT.entry(c, r);
+    const int along_low = q.tall ? XT.low() : X.low(), turned_low = q.tall ? X.low() : XT.low();
     half8 hi, lo;
-    _Float16* at_r = entry(turned, c, r);  // (rows of a block are 8 numbers apart)
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       _Float16 h, l;
-      split((float)((double)u[e] * by), h, l);
+      split((float)((double)u[o][e] * by), h, l);
       hi[e] = h; lo[e] = l;
-      at_r[e * 8] = h;
-      at_r[turned.low() + e * 8] = l;
+      turned[e * 8] = h;
+      turned[turned_low + e * 8] = l;
     }
-    _Float16* at_c = entry(along, r, c);
-    *reinterpret_cast<half8*>(at_c) = hi;
-    *reinterpret_cast<half8*>(at_c + along.low()) = lo;
+    *reinterpret_cast<half8*>(along) = hi;
+    *reinterpret_cast<half8*>(along + along_low) = lo;
   }
   __syncthreads();
 
   const int tiles = nb * nb;  // of A and B: one a wavefront, and two wavefronts each for A's sums
   const int middle = mb / 2 * 2, tile_a = wave >> 1, half = wave & 1;
-  float* partial = reinterpret_cast<float*>(smem) + n * m * 2;  // [tiles][16][64], where A goes afterwards
+  float* partial = reinterpret_cast<float*>(smem) + n * m;  // [tiles][16][64], where A goes afterwards
 #pragma unroll 1
   for (int k = 0; k < a.steps; ++k) {
     const int up = max(0, small - k * a.growth), next_up = max(0, small - (k + 1) * a.growth);
@@ -718,7 +731,7 @@ __global__ void __launch_bounds__(64 * SMALL_WAVES) ns_small_k(NsTable t, NsStep
       small_product(acc[0], AB, ib, AB, jb, 0, AB.kb, lane);
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        const _Float16* p = at_block(AB, ib * 32, jb * 32, g, lane);
+        const _Float16* p = AB.entry(jb * 32 + (lane & 31), ib * 32 + 8 * g + 4 * (lane >> 5));
         const half4 hi = *reinterpret_cast<const half4*>(p), lo = *reinterpret_cast<const half4*>(p + AB.low());
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -733,7 +746,7 @@ __global__ void __launch_bounds__(64 * SMALL_WAVES) ns_small_k(NsTable t, NsStep
     // X <- B X; the last one with dst's columns along the lanes
     const bool last = k + 1 == a.steps, turn = last && q.tall;
     const int all = nb * mb, tiles_across = turn ? nb : mb;
-    const Factor P = turn ? XT : AB, Q = turn ? AB : XT;
+    const LdsFactor<false> P = turn ? XT : AB, Q = turn ? AB : XT;
 #pragma unroll
     for (int o = 0; o < SMALL_TILES; ++o) {
       const int tile = wave + o * SMALL_WAVES;
@@ -742,7 +755,7 @@ __global__ void __launch_bounds__(64 * SMALL_WAVES) ns_small_k(NsTable t, NsStep
     const float unscale = (last ? 1.f : a.x[k + 1]) / (a.b[k] * a.x[k]);
     const int power = last ? -up : next_up - up;
     __syncthreads();  // every wavefront has read X^T
-    float* result = reinterpret_cast<float*>(smem);  // the last X, as it lies in dst: where X and X^T were
+    float* result = reinterpret_cast<float*>(smem);  // the last X, as it lies in dst: where X^T was
 #pragma unroll
     for (int o = 0; o < SMALL_TILES; ++o) {
       const int tile = wave + o * SMALL_WAVES;
@@ -756,7 +769,7 @@ __global__ void __launch_bounds__(64 * SMALL_WAVES) ns_small_k(NsTable t, NsStep
         continue;
       }
       small_put(XT, i, j, acc[o], lane);
-      _Float16* p = entry(X, i * 32 + acc_row(0, lane), j * 32 + (lane & 31));
+      _Float16* p = X.entry(i * 32 + acc_row(0, lane), j * 32 + (lane & 31));
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         _Float16 h, l;
@@ -768,9 +781,18 @@ __global__ void __launch_bounds__(64 * SMALL_WAVES) ns_small_k(NsTable t, NsStep
     __syncthreads();
   }
   const float* result = reinterpret_cast<const float*>(smem);
-#pragma unroll 4
-  for (int r = wave; r < rows; r += SMALL_WAVES)
-    for (int c = lane; c < cols; c += 64) put_result<OUT>(q, r, c, result[r * C + c], a.decay, q.master ? q.master[r * cols + c] : 0.f);
+  for (int c = lane; c < cols; c += 64)
+    for (int r = wave; r < rows; r += 4 * SMALL_WAVES) {
+      float o[4], w[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int rk = min(r + k * SMALL_WAVES, rows - 1);
+        o[k] = result[rk * C + c];
+        w[k] = q.master ? q.master[rk * cols + c] : 0.f;
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) put_result<OUT>(q, r + k * SMALL_WAVES, c, o[k], a.decay, w[k]);
+    }
 }
 
 // Gives every matrix of the table its workgroups; blocks(q): how many.
@@ -945,6 +967,7 @@ hipError_t newton_schulz(const NsItem* items, int count, int dt_src, int dt_dst,
       q.m = (int)ns_up(std::max(it.rows, it.cols), fill);
       if (side == NS_SMALL) {
         lds = std::max(lds, ns_small_lds(it.rows, it.cols));
+        static_assert(LdsFactor<true>::BLOCK * 2 == NS_SPREAD_BLOCK, "as ns_small_lds counts");
         continue;
       }
       auto take = [&](int64_t entries) {

@@ -74,9 +74,10 @@ inline int64_t ns_up(int64_t x, int side) { return (x + side - 1) / side * side;
 // few tiles take no launches of their own.)
 constexpr int NS_SMALL = 0, NS_SMALL_TILES = 2;
 constexpr size_t NS_SMALL_LDS = 159 * 1024;
+constexpr int NS_SPREAD_BLOCK = 1168;  // bytes of a 32 x 16 block of X there
 inline size_t ns_small_lds(int64_t rows, int64_t cols) {
   const int64_t n = ns_up(std::min(rows, cols), 32), m = ns_up(std::max(rows, cols), 32);
-  return (size_t)(2 * n * m + n * n) * 4;
+  return (size_t)(n * m + n * n) * 4 + (size_t)(n / 32) * (m / 16) * 2 * NS_SPREAD_BLOCK;
 }
 inline bool ns_small(int64_t rows, int64_t cols) {
   const int64_t n = ns_up(std::min(rows, cols), 32) / 32, m = ns_up(std::max(rows, cols), 32) / 32;
