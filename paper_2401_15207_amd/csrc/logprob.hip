@@ -140,7 +140,10 @@ struct Sums {
   }
 };
 
-// One workgroup a row.  Every wavefront forms its sums against its own largest entry; the first one joins them.
+// One workgroup a row, one pass over it.  Every wavefront forms its sums against its own largest entry; the first one joins them.
+// Bound: the logits' way from memory once rows are many (4096 x 50272 fp32 139 us, 5.9 TB/s; 2048 x 32000 bf16 with 8 alternatives 31 us, 4.2
+// TB/s: one exponential and two multiply-adds an entry take as long as its two bytes); the chain of loads, reductions and barriers for one
+// (1 x 32000 with 20 alternatives 6 us).  Rows are not split over workgroups: one of 128000 takes 13 us, a launch that joins parts 4 more.
 // The alternatives: the k-th largest of the maxima of 64 disjoint parts of the row is at most its k-th largest entry, and few entries are
 // at or above it (the parts interleave: 20 of 64 maxima exceed it where about 24 entries do); those are collected and each counts how
 // many of them precede it.  Rows where they are more than the list holds, or that hold NaN or +inf, take the largest key below the one
@@ -342,6 +345,7 @@ struct LogprobBwdArgs {
 constexpr int BWD_THREADS = 256;
 
 // `parts` workgroups a row.  An element is read and written by one thread, so the gradient may take the logits' place.
+// Bound: the way from and to memory (2048 x 32000 bf16 52 us, 5.1 TB/s; 1000 x 50265 41 us, 4.8 TB/s).
 template <typename T, int E>
 __global__ void __launch_bounds__(BWD_THREADS) logprob_bwd_k(LogprobBwdArgs a) {
   const int64_t r = blockIdx.x / a.parts;
@@ -380,12 +384,16 @@ __global__ void __launch_bounds__(BWD_THREADS) logprob_bwd_k(LogprobBwdArgs a) {
 
 template <typename T>
 hipError_t launch_logprob(int64_t rows, const LogprobArgs& a, hipStream_t st) {
+  // Threads so that one batch of a thread's loads, four pieces, takes most of a row.  Few rows: the more threads the shorter the chain (1 x
+  // 1000 entries in bf16: 4.4 us with 256, 5.0 with 64; 256 x 10000: 5.4 with 512, 7.2 with 256; 64 x 32000: 6.7 with 1024, 8.9 with 512;
+  // but 64 x 16500: 5.9 with 512, 6.9 with 1024).  Many rows fill the chip by themselves, and joining the wavefronts' parts costs more
+  // (2048 x 1000: 6.8 with 64, 8.2 with 256; 2048 x 8000: 11.1 with 256, 15.5 with 512; 2048 x 32000: 32 with 512, 49 with 1024).
   const int pieces = a.V / (16 / (int)sizeof(T));
   const uint32_t grid = (uint32_t)rows;
 #define ROW(NT) logprob_k<T, NT><<<grid, NT, 0, st>>>(a)
-  if (pieces <= 256) ROW(64);
-  else if (pieces <= 2048) ROW(256);
-  else if (rows > 256) ROW(512);
+  if (pieces <= 48 || (pieces <= 256 && rows > 512)) ROW(64);
+  else if (pieces <= 1024) ROW(256);
+  else if (pieces <= 2200 || rows > 256) ROW(512);
   else ROW(1024);  // a row a compute unit at most
 #undef ROW
   return hipGetLastError();
@@ -394,7 +402,8 @@ hipError_t launch_logprob(int64_t rows, const LogprobArgs& a, hipStream_t st) {
 template <typename T>
 hipError_t launch_logprob_bwd(int64_t rows, LogprobBwdArgs a, hipStream_t st) {
   constexpr int E = 16 / (int)sizeof(T);
-  // pieces of 16 bytes where a row of the gradient lies in them as its row of logits does
+  // pieces of 16 bytes where a row of the gradient lies in them as its row of logits does (2048 x 32000 in bf16: 43 us, element by element
+  // 126; in fp32 95 and 160)
   const uintptr_t off = reinterpret_cast<uintptr_t>(a.logits) - reinterpret_cast<uintptr_t>(a.dlogits);
   const bool alike = (off & 15) == 0 && (rows == 1 || (a.ld - a.ldd) * (int64_t)sizeof(T) % 16 == 0);
   const int per = BWD_THREADS * (alike ? E : 1) * 4;

@@ -551,7 +551,7 @@ __global__ void __launch_bounds__((64 * NsTile<SIDE, PP, QP, DEEP>::NW), (DEEP &
 // ---- matrices that fit a compute unit's LDS ---------------------------------------------------
 // All steps in one launch, a workgroup a matrix: X, X^T and A (in whose place B goes) stay in LDS, in the same order as in memory, sides filled
 // up to multiples of 32.  What bounds the launches above for such matrices is their number and each one's way to memory and back: six
-// matrices of 64 x 64 to 256 x 64 take 84 us in 17 launches.
+// matrices of 64 x 64 to 256 x 64 take 82 us in 17 launches, 55 here.
 struct NsSteps {
   int steps, growth;
   float mu, eps, decay;
@@ -820,43 +820,61 @@ hipError_t launch_product(uint32_t blocks, const NsTable& t, const NsStep& p, hi
   kern<<<blocks, 64 * T::NW, T::LDS, st>>>(t, p);
   return hipGetLastError();
 }
-// Workgroups of a product with tiles of SIDE, when each has `most` stages at most
-template <int SIDE, int MODE, int PP, int QP>
-int64_t units_of(NsMatrix& q, int64_t most) {
-  const int64_t n = q.n / SIDE, tiles = MODE == NS_GRAM || MODE == NS_POLY ? n * (n + 1) / 2 : n * (q.m / SIDE);
-  const int64_t stages = (MODE == NS_GRAM ? q.m : q.n) / (16 * NsTile<SIDE, PP, QP, true>::KS);
-  q.parts = (int)((stages + most - 1) / most);
-  return (tiles * q.parts + 7) / 8 * 8;
+// Tiles of side `by` of matrix q's product, and their k.
+template <int MODE>
+int64_t tiles_of(const NsMatrix& q, int by) {
+  const int64_t n = q.n / by;
+  return MODE == NS_GRAM || MODE == NS_POLY ? n * (n + 1) / 2 : n * (q.m / by);
 }
+template <int MODE>
+int64_t k_of(const NsMatrix& q) { return MODE == NS_GRAM ? q.m : q.n; }
+
 template <int SIDE, int MODE, int PP, int QP, typename OUT>
 hipError_t product_of(NsTable& t, const NsStep& p, hipStream_t st) {
-  int64_t most = 1 << 20;
+  constexpr int K = 16 * NsTile<SIDE, PP, QP, true>::KS;
+  const auto parts_of = [&](const NsMatrix& q, int64_t most) { return (k_of<MODE>(q) / K + most - 1) / most; };
+  int64_t most = 1 << 20;  // stages of a workgroup
   if constexpr (SIDE < 256) {
-    // the shortest k ranges whose workgroups fit side by side
-    for (most = NS_SHARED_STAGES; most < 1 << 20; most *= 2) {
-      int64_t all = 0;
-      for (int i = 0; i < t.count; ++i) all += units_of<SIDE, MODE, PP, QP>(t.m[i], most);
-      if (all <= NS_SHARED_UNITS) break;
+    // k ranges that the launch takes least time with, of those whose workgroups lie side by side; the longest of equal ones
+    double least = 0.0;
+    for (int64_t shared = 1 << 13; shared >= NS_SHARED_STAGES; shared /= 2) {
+      NsTiles runs[NS_TABLE];
+      int64_t units = 0, parts = 1;
+      for (int i = 0; i < t.count; ++i) {
+        const int64_t by = parts_of(t.m[i], shared), tiles = tiles_of<MODE>(t.m[i], SIDE);
+        runs[i] = {tiles * by, (double)((k_of<MODE>(t.m[i]) / K + by - 1) / by)};
+        units += (tiles * by + 7) / 8 * 8;
+        parts = std::max(parts, by);
+      }
+      if (parts > 1 && units > NS_SHARED_UNITS) break;
+      const double span = ns_span(runs, t.count);
+      if (parts == 1 || span < least) {
+        least = span;
+        most = shared;
+      }
     }
   }
-  const uint32_t blocks = spread(t, [&](NsMatrix& q) { return units_of<SIDE, MODE, PP, QP>(q, most); });
+  const uint32_t blocks = spread(t, [&](NsMatrix& q) {
+    q.parts = (int)parts_of(q, most);
+    return (tiles_of<MODE>(q, SIDE) * q.parts + 7) / 8 * 8;
+  });
   if constexpr (SIDE < 256)
     if (blocks <= 256) return launch_product<SIDE, MODE, PP, QP, true, OUT>(blocks, t, p, st);
   return launch_product<SIDE, MODE, PP, QP, false, OUT>(blocks, t, p, st);
 }
-// Tiles as large as the sides' filling allows and a launch still has enough of.
+// Tiles of 256 or 128 by how long the launch takes with them, 64 where there would be few of 128.
 template <int MODE, int PP, int QP, typename OUT = float>
 hipError_t product(NsTable& t, int side, const NsStep& p, hipStream_t st) {
-  const auto tiles = [&](int64_t by) {
-    int64_t all = 0;
-    for (int i = 0; i < t.count; ++i) {
-      const int64_t n = t.m[i].n / by;
-      all += MODE == NS_GRAM || MODE == NS_POLY ? n * (n + 1) / 2 : n * (t.m[i].m / by);
-    }
-    return all;
-  };
-  if (side >= 256 && tiles(256) >= NS_TILES_256) return product_of<256, MODE, PP, QP, OUT>(t, p, st);
-  if (side >= 128 && tiles(128) >= NS_TILES_128) return product_of<128, MODE, PP, QP, OUT>(t, p, st);
+  NsTiles large[NS_TABLE], middle[NS_TABLE];
+  int64_t tiles = 0, k = 0;
+  for (int i = 0; i < t.count; ++i) {
+    large[i] = {tiles_of<MODE>(t.m[i], 256), (double)k_of<MODE>(t.m[i]) + (MODE == NS_POLY ? NS_COST_256_POLY : NS_COST_256)};
+    middle[i] = {tiles_of<MODE>(t.m[i], 128), (double)k_of<MODE>(t.m[i]) * 0.25 * (PP == 1 ? NS_COST_128_ONE : NS_COST_128)};
+    tiles += middle[i].count;
+    k = std::max(k, k_of<MODE>(t.m[i]));
+  }
+  if (side >= 256 && ns_span(large, t.count) < ns_span(middle, t.count)) return product_of<256, MODE, PP, QP, OUT>(t, p, st);
+  if (side >= 128 && tiles >= (k < NS_LONG_K ? NS_TILES_128 : NS_TILES_128 / 2)) return product_of<128, MODE, PP, QP, OUT>(t, p, st);
   return product_of<64, MODE, PP, QP, OUT>(t, p, st);
 }
 

@@ -55,23 +55,72 @@ constexpr int64_t NS_SIDE_MAX = 65536;
 // 256 compute units, more would only need more work space.
 constexpr int64_t NS_TOGETHER = int64_t(1) << 28;
 // Both sides of a matrix are filled up with zeros to a multiple of this, the largest tile its products can have: 256 where at least 64
-// such tiles cover it, else 128; 64 in launches that would have fewer than NS_FEW_TILES of 128 in the symmetric products.
-constexpr int64_t NS_FEW_TILES = 160;
+// such tiles cover it, else 128; 64 in launches that would have fewer than NS_FEW_TILES of 128 in the symmetric products, where filling up
+// costs more than larger tiles give (fp32 results: four matrices of odd sizes up to 1000 take 161 us with 64, 173 with 128; eight of
+// 512 x 2048 495 and 459).
+constexpr int64_t NS_FEW_TILES = 64;
 inline int ns_side(int64_t rows, int64_t cols) { return std::min(rows, cols) >= 1280 && rows * cols >= int64_t(64) * 256 * 256 ? 256 : 128; }
-// From how many tiles on a launch takes them that large.
-constexpr int64_t NS_TILES_256 = 192, NS_TILES_128 = 128;
-// Workgroups that share tiles' k ranges, in launches that have fewer workgroups than this otherwise; no range is shorter than so many
-// stages.  Their sums: 64 KB (128 x 128) each, and a counter.
+// From how many tiles of 128 on a launch takes them rather than tiles of 64, half as many where k is long.  Below, workgroups are too few and
+// each one's chain of stages too long.  Layer 1024 wide, fp32 results: 880 us, 1087 with 64 throughout; two matrices of 512 x 512, bf16
+// results: 127 us, 223 with 128; four of 640 x 640: 158, with half as many tiles enough for any k 185; 1536 x 6000: 607, with half as
+// many never enough 690.
+constexpr int64_t NS_TILES_128 = 128, NS_LONG_K = 1536;
+// Between tiles of 256 and 128 the shorter of the two launches, each tile taken to cost its k times its entries.  Tiles of 128 pass their
+// operands through LDS twice as often: what that costs, with one product, where LDS bounds the loop, and with more.  What a tile of 256
+// costs beside its k is its way in and out, which no second workgroup of the compute unit covers; in NS_POLY, which reads the tile's
+// entries of A and writes B's twice, more.  A layer 4096 wide, fp32 and bf16 results: 36.3 and 19.4 ms, with 128 throughout 39.1 and 23.0;
+// three matrices of 2048 x 5632 and four of 2048 x 2048: 5.6 and 3.4 ms, with 256 for all launches of 192 such tiles or more 6.3 and 3.5.
+constexpr double NS_COST_128_ONE = 1.5, NS_COST_128 = 1.3, NS_COST_256 = 200.0, NS_COST_256_POLY = 800.0;
+// Tiles' k ranges are shared between workgroups where that shortens a launch and leaves it no more workgroups than NS_SHARED_UNITS; no range
+// is shorter than so many stages.  Layer 1024 wide, fp32 results: 880 us, 973 without sharing, 972 with at most 256 workgroups, 912 with
+// 512.  Stages: two matrices of 512 x 512 150 us, with 4 157; one of 256 x 1000 121, with 16 127.  The sums: 64 KB (128 x 128) each, and a
+// counter.
 constexpr int64_t NS_SHARED_UNITS = 304, NS_SHARED_STAGES = 8;
 constexpr size_t NS_SHARED_BYTES = NS_SHARED_UNITS * (4 + 128 * 128 * 4);
 
-// Whose products are fewer for a bf16 result: smaller ones are bound by latency, and further off with them.
+// Whose products are fewer for a bf16 result: smaller ones are bound by latency, and further off with them (two of 512 x 512: 127 us, with
+// all products 150; a layer 1024 wide: 0.58 and 0.88 ms; 4096 wide: 19.4 and 36.3).
 inline bool ns_large(int64_t rows, int64_t cols) { return std::min(rows, cols) >= 512; }
+// Among others they take all products, in those others' launches, while their short sides' squares times the long ones are less than this
+// together: launches of their own cost 100 us and more (1000 x 333, 129 x 257, 77 x 1300, 515 x 515: 161 us together, 294 apart).
+constexpr int64_t NS_APART = int64_t(1) << 31;
+
+// How long the 256 compute units take over tiles, run by run, each tile to the unit that is free first.  Runs of equal ones: how many and how long.
+struct NsTiles {
+  int64_t count;
+  double length;
+};
+inline double ns_span(NsTiles* runs, int n) {
+  std::sort(runs, runs + n, [](const NsTiles& p, const NsTiles& q) { return p.length > q.length; });
+  struct { double free; int64_t units; } at[257];  // units by when they are free, the latest first
+  int levels = 1;
+  at[0] = {0.0, 256};
+  double end = 0.0;
+  for (int i = 0; i < n; ++i) {
+    for (int64_t left = runs[i].count; left > 0;) {
+      const auto first = at[--levels];
+      const int64_t take = std::min(left, first.units);
+      if (take < first.units) at[levels++] = {first.free, first.units - take};
+      left -= take;
+      const double done = first.free + runs[i].length;
+      end = std::max(end, done);
+      int to = levels;
+      while (to > 0 && at[to - 1].free < done) --to;
+      if (to > 0 && at[to - 1].free == done) {
+        at[to - 1].units += take;
+        continue;
+      }
+      for (int l = levels++; l > to; --l) at[l] = at[l - 1];
+      at[to] = {done, take};
+    }
+  }
+  return end;
+}
 
 inline int64_t ns_up(int64_t x, int side) { return (x + side - 1) / side * side; }
 // Matrices whose factors X, X^T and A (two fp16 numbers to an entry) fit a compute unit's LDS with sides filled up to multiples of 32, and
-// whose tiles of 32 x 32 two a wavefront at most: all steps in one launch, if a list holds no other.  (Among others they ride along: their
-// few tiles take no launches of their own.)
+// whose tiles of 32 x 32 two a wavefront at most: all steps in one launch, if a list holds no other (64 x 64: 28 us, 68 in launches for each
+// product; four of those, 256 x 64 and 64 x 256: 55 and 82).  (Among others they ride along: their few tiles take no launches of their own.)
 constexpr int NS_SMALL = 0, NS_SMALL_TILES = 2;
 constexpr size_t NS_SMALL_LDS = 159 * 1024;
 constexpr int NS_SPREAD_BLOCK = 1168;  // bytes of a 32 x 16 block of X there
@@ -97,7 +146,7 @@ inline size_t ns_bytes(int64_t rows, int64_t cols) {
 // few: large ones apart, as they take fewer products.
 template <class S, class F>
 inline void ns_launches(int count, bool few, S shape, F launch) {
-  bool all_small = true;
+  bool all_small = true, apart = true;
   for (int i = 0; i < count && all_small; ++i) {
     int64_t r, c;
     shape(i, &r, &c);
@@ -116,9 +165,22 @@ inline void ns_launches(int count, bool few, S shape, F launch) {
     }
     return;
   }
+  if (few) {
+    int64_t work = 0;
+    bool others = false;
+    for (int i = 0; i < count; ++i) {
+      int64_t r, c;
+      shape(i, &r, &c);
+      if (r == 0 || c == 0 || ns_side(r, c) == 256) continue;
+      if (ns_large(r, c)) work += std::min(r, c) * r * c;
+      else others = true;
+    }
+    apart = !others || work >= NS_APART;
+  }
   for (int kind = 0; kind < (few ? 3 : 2); ++kind) {
     const int side = kind == 0 ? 256 : 128;
     const bool large = few && kind < 2;
+    if (kind == 1 && large && !apart) continue;
     int which[NS_TABLE], n = 0;
     int64_t entries = 0, tiles = 0, longest[NS_TABLE];
     const auto flush = [&]() {
@@ -129,7 +191,7 @@ inline void ns_launches(int count, bool few, S shape, F launch) {
     for (int i = 0; i < count; ++i) {
       int64_t r, c;
       shape(i, &r, &c);
-      if (r == 0 || c == 0 || ns_side(r, c) != side || (few && ns_large(r, c) != large)) continue;
+      if (r == 0 || c == 0 || ns_side(r, c) != side || (few && kind > 0 && (apart && ns_large(r, c)) != large)) continue;
       if (n == NS_TABLE || (n > 0 && entries + r * c > NS_TOGETHER)) flush();
       int at = n++;
       for (; at > 0 && longest[at - 1] < std::max(r, c); --at) {

@@ -31,6 +31,11 @@ extern "C" size_t bytes(int count, const long long* s) {
 }
 extern "C" size_t one(long long r, long long c) { return ns_bytes(r, c); }
 extern "C" size_t shared() { return NS_SHARED_BYTES; }
+extern "C" double span(int n, const long long* count, const double* length) {
+  NsTiles runs[16];
+  for (int i = 0; i < n; ++i) runs[i] = {(int64_t)count[i], length[i]};
+  return ns_span(runs, n);
+}
 """
 
 
@@ -41,6 +46,7 @@ def plan(tmp_path_factory):
     src.write_text(CODE)
     subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-shared", "-fPIC", "-I", CSRC, str(src), "-o", str(so)], check=True)
     lib = ctypes.CDLL(str(so))
+    lib.span.restype = ctypes.c_double
     lib.bytes.restype = lib.one.restype = lib.shared.restype = ctypes.c_size_t
     lib.one.argtypes = [ctypes.c_longlong] * 2
     return lib
@@ -102,9 +108,27 @@ def test_work_space_and_launches(plan):
     # tiles of either size apart, the longest first, nothing for a side of 0, and no more than fits together
     mixed = [(64, 64), (4096, 4096), (0, 7), (4096, 11008), (100, 300)]
     assert launches(mixed) == [(256, [3, 1]), (64, [4, 0])] and launches([(64, 64), (600, 900)]) == [(64, [1, 0])]
-    assert launches([(64, 64), (600, 900), (2048, 2048)], 1) == [(256, [2]), (128, [1]), (64, [0])]   # (products to a step differ)
+    # products to a step differ, where large ones are worth launches of their own
+    assert launches([(64, 64), (600, 900), (2048, 2048)], 1) == [(256, [2]), (64, [1, 0])] and launches([(600, 900)], 1) == [(128, [0])]
+    assert launches([(64, 64), (600, 900), (1024, 2048)], 1) == [(128, [2, 1]), (64, [0])]
+    for few in (0, 1):  # every matrix once
+        some = [(64, 64), (600, 900), (2048, 2048), (512, 512), (511, 4096), (0, 9), (5000, 1300), (1300, 900)]
+        assert sorted(i for _, which in launches(some, few) for i in which) == [0, 1, 2, 3, 4, 6, 7]
     assert call(plan.bytes, mixed) == plan.shared() + plan.one(4096, 4096) + plan.one(4096, 11008)
     large = [(16384, 16384), (16384, 16384), (64, 64)]
     assert launches(large) == [(256, [0]), (256, [1]), (64, [2])]
     assert launches([(1024, 1024)] * 6) == [(128, [0, 1, 2, 3, 4, 5])]
     assert call(plan.bytes, large) == plan.shared() + plan.one(16384, 16384)
+
+
+@pytest.mark.parametrize("runs", [[], [(1, 5.0)], [(256, 3.0)], [(257, 3.0)], [(3088, 7.0)], [(408, 11.0), (544, 4.0)], [(1, 100.0), (1000, 1.0)],
+                                  [(0, 4.0), (70, 2.5)], [(i + 1, 1.0 + 0.37 * i) for i in range(16)], [(200 + 31 * i, 9.0 - 0.5 * i) for i in range(16)]])
+def test_span_is_that_of_a_tile_by_tile_assignment(plan, runs):
+    import heapq
+    free = [0.0] * 256
+    for count, length in sorted(runs, key=lambda r: -r[1]):
+        for _ in range(count):
+            heapq.heapreplace(free, free[0] + length)
+    n = len(runs)
+    got = plan.span(n, (ctypes.c_longlong * max(n, 1))(*[c for c, _ in runs]), (ctypes.c_double * max(n, 1))(*[l for _, l in runs]))
+    assert got == pytest.approx(max(free), rel=1e-12)
