@@ -120,7 +120,7 @@ typedef struct {
 /* HIFT_MUON (Jordan et al. 2024): the hidden layers' matrices -- q, k, v, gate and up each by itself -- take the update of hift_kernel_muon
  * (lr, momentum in [0, 1), weight_decay; state array 0 is the momentum, array 1 stays 0), everything else AdamW's with the same lr, beta1,
  * beta2, eps and weight_decay.  bf16 models: the orthogonalised step is within 2^-9 of itself; fp32 models keep fp32's exactness.  The work
- * space of one layer (3.2 GB at the 7B shape) is part of the device arena. */
+ * space of one layer (3.4 GB at the 7B shape) is part of the device arena. */
 /* HIFT_ADAFACTOR (section "Memory Efficiency Analysis" lists it among the optimizers): Shazeer and Stern
  * 2018, Algorithm 4 without momentum, with the caller's lr as the step size (no relative step, no
  * parameter scaling); epsilon_1 = 1e-30, clipping threshold 1, beta2_t = 1 - t^-0.8 with t the group's own
