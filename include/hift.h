@@ -556,12 +556,13 @@ hift_status hift_kernel_token_logprob_bwd(int32_t dtype, int64_t rows, int32_t V
 
 /* Orthogonalisation of matrices by Newton-Schulz steps: X = src / max(|src|_F, eps); `steps` (1 .. 16) times
  * X <- a X + b (X X^T) X + c (X X^T)^2 X; dst = X.  src, dst: device, rows ld_src / ld_dst >= cols apart, of type src_dtype / dst_dtype (HIFT_F32
- * or HIFT_BF16); dst may be src where the types are the same.  Products carry 22 bits of every factor and fp32 sums.  A src of zeros gives
- * zeros; one that holds NaN or infinities gives NaN.  Matrices of one call share launches, so hand in together what is there together.
+ * or HIFT_BF16); dst may be src where the types are the same.  Products carry 22 bits of every factor and fp32 sums; into a bf16 dst
+ * matrices of 512 and more on the short side may take fewer (within 2^-9 of the whole in the 2-norm).  A src of zeros gives zeros; one that holds NaN or infinities gives NaN.  Matrices of one call share launches, so hand in together what is there together.
  * Either side at most 65536 long; a matrix with a side of 0 is skipped.  HIFT_EINVAL also for a < 1 (small singular values would not grow)
  * and for coefficients under which the singular values, all in [0, 1] at first, could leave fp16's range.
  * workspace: device, 16-byte aligned, hift_kernel_orthogonalize_bytes (which reads rows and cols only), free again once the call's work on
- * the stream is done.  No atomics: the same call gives the same bits. */
+ * the stream is done; NULL where that is 0 bytes (small matrices alone).  No sum depends on timing: the same call gives the same bits;
+ * a matrix among others may differ in its last ones from the same matrix alone. */
 typedef struct {
   int64_t rows, cols;
   const void* src; int64_t ld_src;
