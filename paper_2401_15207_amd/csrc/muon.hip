@@ -53,6 +53,8 @@ struct NsMatrix {
   double* norm_parts;
   int* small;           // how many powers of two X is below 1 at the start (norms below eps; ns_start_k)
   int parts;            // workgroups that share the k range of one of its tiles
+  int tile0, tiles;     // of its product's tiles, those from tile0 on
+  int alone;            // workgroups before it that share nothing, if it is the launch's last round
 };
 // first[i]: the first workgroup of a launch that works on matrix i; from `count` on, beyond all of them.
 struct NsTable {
@@ -287,9 +289,9 @@ __device__ __forceinline__ const _Float16* at_block(const Factor& rows_j, int i0
 // lie, into a ring of stages of 16 to 64 k; a stage's fragments are read into registers under the products of the stage before.
 // PP, QP: numbers of P and Q that take part: 2 and 2 (three products), 1 and 2 (two), 1 and 1 (one).
 // What bounds it, a layer 4096 wide with 11008 in its feed-forward block and a bf16 result (256 x 256): A 765 us, 1150 TFLOP/s by the upper
-// tiles' entries, B 500 (1020; 4 rounds of 3.7), X 2.7 ms (1220 by matrix instructions; 13 rounds of 12.06), the last X with the update 1.9:
+// tiles' entries, B 500 (1020; 4 rounds of 3.7), X 2.6 ms (1280 by matrix instructions; 12 rounds and a shared one), the last X with the update 1.9:
 // where one product is taken LDS gives 125 of its 128 bytes a clock, with more the matrix pipe is at the power limit.  A layer 1024 wide
-// (128 x 128): 37, 22, 66 and 86 us, each one round or two of tiles.
+// (128 x 128): 37, 22, 62 and 65 us (with the update 82), each one round or two of tiles.
 // DEEP: the ring of a launch that gives a compute unit one workgroup at most.  That one waits for memory by itself: a stage of 16 KB takes
 // the time of its requests' latency over the stages in flight, so the ring takes most of the LDS.
 template <int SIDE, int PP, int QP, bool DEEP>
@@ -331,12 +333,12 @@ __global__ void __launch_bounds__((64 * NsTile<SIDE, PP, QP, DEEP>::NW), (DEEP &
   constexpr bool SYM = MODE == NS_GRAM || MODE == NS_POLY;
   const bool turn = MODE == NS_LAST && q.tall;  // dst's columns along the lanes
   const int side_i = (turn ? q.m : q.n) / SIDE, side_j = (SYM || turn ? q.n : q.m) / SIDE;
-  const int units = (SYM ? side_i * (side_i + 1) / 2 : side_i * side_j) * q.parts;
+  const int units = q.tiles * q.parts;
   int id = blockIdx.x - block0;
   id = (id & 7) * ((units + 7) >> 3) + (id >> 3);
   if (id >= units) return;
-  const int unit = block0 + id, part = id % q.parts;
-  id /= q.parts;
+  const int unit = block0 + id - q.alone, part = id % q.parts;
+  id = q.tile0 + id / q.parts;
   Factor P, Q;
   int ti, tj;
   if (SYM) {
@@ -428,7 +430,7 @@ __global__ void __launch_bounds__((64 * NsTile<SIDE, PP, QP, DEEP>::NW), (DEEP &
     if (s + 1 < stages) stage(s + 1, 1, true);
   }
 
-  if (SIDE < 256 && q.parts > 1) {
+  if (q.parts > 1) {
     // Every one of them leaves its sums in memory and counts itself in; the one that finds all others counted adds them up in their order
     // (its own too: the result must not depend on who came last) and goes on.  Nobody waits.  They run on different XCDs, so the sums go past the
     // L2s both ways (device scope).
@@ -456,22 +458,26 @@ __global__ void __launch_bounds__((64 * NsTile<SIDE, PP, QP, DEEP>::NW), (DEEP &
     }
     __syncthreads();
     if (!*is_last) return;
-    for (int u = 0; u < q.parts; ++u) {  // a part's sums are all requested before the first is added
-      f32x4 v[BI][BJ][4];
+    constexpr int ROWS = SIDE == 256 ? 1 : BI;  // of blocks at a time, for their registers
 #pragma unroll
-      for (int x = 0; x < BI; ++x)
+    for (int x0 = 0; x0 < BI; x0 += ROWS)
+      for (int u = 0; u < q.parts; ++u) {  // a part's sums are all requested before the first is added
+        f32x4 v[ROWS][BJ][4];
 #pragma unroll
-        for (int y = 0; y < BJ; ++y)
+        for (int x = 0; x < ROWS; ++x)
 #pragma unroll
-          for (int g = 0; g < 4; ++g)
-            v[x][y][g] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(sums, mine + u * BYTES, ((x * BJ + y) * 4 + g) * T::NW * 1024, SC1));
+          for (int y = 0; y < BJ; ++y)
 #pragma unroll
-      for (int x = 0; x < BI; ++x)
+            for (int g = 0; g < 4; ++g)
+              v[x][y][g] = __builtin_bit_cast(
+                  f32x4, __builtin_amdgcn_raw_buffer_load_b128(sums, mine + u * BYTES, (((x0 + x) * BJ + y) * 4 + g) * T::NW * 1024, SC1));
 #pragma unroll
-        for (int y = 0; y < BJ; ++y)
+        for (int x = 0; x < ROWS; ++x)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) acc[x][y][e] = u == 0 ? v[x][y][e >> 2][e & 3] : acc[x][y][e] + v[x][y][e >> 2][e & 3];
-    }
+          for (int y = 0; y < BJ; ++y)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[x0 + x][y][e] = u == 0 ? v[x][y][e >> 2][e & 3] : acc[x0 + x][y][e] + v[x][y][e >> 2][e & 3];
+      }
   }
 
   __syncthreads();  // the ring is free: nothing is on its way there either
@@ -836,6 +842,21 @@ int64_t tiles_of(const NsMatrix& q, int by) {
 template <int MODE>
 int64_t k_of(const NsMatrix& q) { return MODE == NS_GRAM ? q.m : q.n; }
 
+// Equal tiles of 256 that leave a few for a round of their own: how many, and how many workgroups share the k range of each.  0: none that do.
+template <int MODE>
+int rest_of(const NsTable& t, int* parts) {
+  const NsMatrix& z = t.m[t.count - 1];
+  int64_t all = 0;
+  for (int i = 0; i < t.count; ++i) {
+    if (k_of<MODE>(t.m[i]) != k_of<MODE>(z)) return 0;
+    all += tiles_of<MODE>(t.m[i], 256);
+  }
+  const int rest = (int)(all % 256);
+  if (rest == 0 || rest > 128 || all < 256 || rest >= tiles_of<MODE>(z, 256) || k_of<MODE>(z) < NS_REST_K || t.count == NS_TABLE) return 0;
+  *parts = std::min(NS_REST_PARTS, 256 / rest);
+  return rest;
+}
+
 template <int SIDE, int MODE, int PP, int QP, typename OUT>
 hipError_t product_of(NsTable& t, const NsStep& p, hipStream_t st) {
   constexpr int K = 16 * NsTile<SIDE, PP, QP, true>::KS;
@@ -863,16 +884,34 @@ hipError_t product_of(NsTable& t, const NsStep& p, hipStream_t st) {
   }
   const uint32_t blocks = spread(t, [&](NsMatrix& q) {
     q.parts = (int)parts_of(q, most);
-    return (tiles_of<MODE>(q, SIDE) * q.parts + 7) / 8 * 8;
+    q.tile0 = q.alone = 0;
+    q.tiles = (int)tiles_of<MODE>(q, SIDE);
+    return (int64_t)(q.tiles * q.parts + 7) / 8 * 8;
   });
-  if constexpr (SIDE < 256)
+  if constexpr (SIDE < 256) {
     if (blocks <= 256) return launch_product<SIDE, MODE, PP, QP, true, OUT>(blocks, t, p, st);
+  } else {
+    int parts;
+    if (const int rest = rest_of<MODE>(t, &parts)) {
+      NsTable u = t;
+      u.m[u.count] = t.m[t.count - 1];
+      NsMatrix &q = u.m[u.count - 1], &r = u.m[u.count];
+      ++u.count;
+      q.tiles -= rest;
+      r.tile0 = q.tiles;
+      r.tiles = rest;
+      r.parts = parts;
+      const uint32_t more = spread(u, [](const NsMatrix& x) { return (int64_t)(x.tiles * x.parts + 7) / 8 * 8; });
+      r.alone = u.first[u.count - 1];
+      return launch_product<SIDE, MODE, PP, QP, false, OUT>(more, u, p, st);
+    }
+  }
   return launch_product<SIDE, MODE, PP, QP, false, OUT>(blocks, t, p, st);
 }
 // Tiles of 256 or 128 by how long the launch takes with them, 64 where there would be few of 128.
 template <int MODE, int PP, int QP, typename OUT = float>
 hipError_t product(NsTable& t, int side, const NsStep& p, hipStream_t st) {
-  NsTiles large[NS_TABLE], middle[NS_TABLE];
+  NsTiles large[NS_TABLE + 1], middle[NS_TABLE];
   int64_t tiles = 0, k = 0;
   for (int i = 0; i < t.count; ++i) {
     large[i] = {tiles_of<MODE>(t.m[i], 256), (double)k_of<MODE>(t.m[i]) + (MODE == NS_POLY ? NS_COST_256_POLY : NS_COST_256)};
@@ -880,7 +919,12 @@ hipError_t product(NsTable& t, int side, const NsStep& p, hipStream_t st) {
     tiles += middle[i].count;
     k = std::max(k, k_of<MODE>(t.m[i]));
   }
-  if (side >= 256 && ns_span(large, t.count) < ns_span(middle, t.count)) return product_of<256, MODE, PP, QP, OUT>(t, p, st);
+  int runs = t.count, parts;
+  if (const int rest = rest_of<MODE>(t, &parts)) {
+    large[runs - 1].count -= rest;
+    large[runs++] = {rest * parts, (double)k / parts + NS_COST_256_REST};
+  }
+  if (side >= 256 && ns_span(large, runs) < ns_span(middle, t.count)) return product_of<256, MODE, PP, QP, OUT>(t, p, st);
   if (side >= 128 && tiles >= (k < NS_LONG_K ? NS_TILES_128 : NS_TILES_128 / 2)) return product_of<128, MODE, PP, QP, OUT>(t, p, st);
   return product_of<64, MODE, PP, QP, OUT>(t, p, st);
 }
@@ -978,7 +1022,7 @@ hipError_t newton_schulz(const NsItem* items, int count, int dt_src, int dt_dst,
   hipError_t err = hipSuccess;
   ns_launches(count, run.few, [&](int i, int64_t* r, int64_t* c) { *r = items[i].rows; *c = items[i].cols; }, [&](const int* which, int n, int side, bool large) {
     NsTable t{};
-    unsigned char* ws = reinterpret_cast<unsigned char*>(workspace) + NS_SHARED_BYTES;
+    unsigned char* ws = reinterpret_cast<unsigned char*>(workspace) + ns_shared_bytes(side);
     const int fill = side == NS_SMALL ? 32 : side;
     size_t lds = 0;
     for (int i = 0; i < n; ++i) {

@@ -68,15 +68,23 @@ constexpr int64_t NS_TILES_128 = 128, NS_LONG_K = 1536;
 // Between tiles of 256 and 128 the shorter of the two launches, each tile taken to cost its k times its entries.  Tiles of 128 pass their
 // operands through LDS twice as often: what that costs, with one product, where LDS bounds the loop, and with more.  What a tile of 256
 // costs beside its k is its way in and out, which no second workgroup of the compute unit covers; in NS_POLY, which reads the tile's
-// entries of A and writes B's twice, more.  A layer 4096 wide, fp32 and bf16 results: 36.3 and 19.4 ms, with 128 throughout 39.1 and 23.0;
-// three matrices of 2048 x 5632 and four of 2048 x 2048: 5.6 and 3.4 ms, with 256 for all launches of 192 such tiles or more 6.3 and 3.5.
-constexpr double NS_COST_128_ONE = 1.5, NS_COST_128 = 1.3, NS_COST_256 = 200.0, NS_COST_256_POLY = 800.0;
+// entries of A and writes B's twice, more; and a shared tile's (below) the way of its sums through memory.  A layer 4096 wide, fp32 and bf16
+// results: 36.3 and 19.4 ms, with 128 throughout 39.1 and 23.0; three matrices of 2048 x 5632 and four of 2048 x 2048: 5.6 and 3.4 ms, with 256
+// for all launches of 192 such tiles or more 6.3 and 3.5.
+constexpr double NS_COST_128_ONE = 1.5, NS_COST_128 = 1.3, NS_COST_256 = 200.0, NS_COST_256_POLY = 800.0, NS_COST_256_REST = 1200.0;
 // Tiles' k ranges are shared between workgroups where that shortens a launch and leaves it no more workgroups than NS_SHARED_UNITS; no range
 // is shorter than so many stages.  Layer 1024 wide, fp32 results: 880 us, 973 without sharing, 972 with at most 256 workgroups, 912 with
 // 512.  Stages: two matrices of 512 x 512 150 us, with 4 157; one of 256 x 1000 121, with 16 127.  The sums: 64 KB (128 x 128) each, and a
 // counter.
 constexpr int64_t NS_SHARED_UNITS = 304, NS_SHARED_STAGES = 8;
 constexpr size_t NS_SHARED_BYTES = NS_SHARED_UNITS * (4 + 128 * 128 * 4);
+// So are those of the tiles of 256 that would make a last round for at most half the compute units, by at most so many workgroups a tile and
+// where k is at least so long.  fp32 and bf16 results with and without: a layer 4096 wide, whose X takes 12 rounds and 16 tiles, 36.8 and 19.7
+// ms, 37.3 and 19.9; 4096 x 4200 4.20 and 2.30, 4.29 and 2.35.
+constexpr int NS_REST_PARTS = 4;
+constexpr int64_t NS_REST_K = 2048;
+constexpr size_t NS_REST_BYTES = NS_SHARED_UNITS * 4 + size_t(256) * 256 * 256 * 4;
+inline size_t ns_shared_bytes(int side) { return side >= 256 ? NS_REST_BYTES : NS_SHARED_BYTES; }
 
 // Whose products are fewer for a bf16 result: smaller ones are bound by latency, and further off with them (two of 512 x 512: 127 us, with
 // all products 150; a layer 1024 wide: 0.58 and 0.88 ms; 4096 wide: 19.4 and 36.3).
@@ -219,7 +227,7 @@ inline size_t ns_workspace_bytes(int count, S shape) {
         shape(which[i], &r, &c);
         sum += ns_bytes(r, c);
       }
-      most = std::max(most, NS_SHARED_BYTES + sum);
+      most = std::max(most, ns_shared_bytes(side) + sum);
     });
   return most;
 }

@@ -111,6 +111,22 @@ def test_results_in_bf16(shapes):
             assert torch.equal(b, x)
 
 
+@pytest.mark.parametrize("shapes", [[(2048, 9000)], [(8700, 2000)], [(2304, 2200), (2048, 9100)], [(4096, 4200)]])
+def test_last_rounds_of_large_tiles(shapes):
+    import torch
+    import paper_2401_15207_amd as H
+    u = [conditioned(r, c, 40 + i) for i, (r, c) in enumerate(shapes)]
+    want = [reference(x) for x in u]
+    # random matrices: singular values within a factor that `any` covers; smallest over norm at least 1e-3, so five steps' growth of a rounding at most
+    for dt, tol in ((torch.float32, 15 * 2.0 ** -22 * COEF[0] ** 5), (torch.bfloat16, 2.0 ** -8 + 2.0 ** -9)):
+        outs = [[torch.empty(x.shape, device="cuda", dtype=dt) for x in u] for _ in range(2)]
+        for o in outs:
+            H.kernel_orthogonalize(u, o)
+        for a, b, w in zip(outs[0], outs[1], want):
+            assert rel(a, w) <= tol
+            assert torch.equal(a, b)     # whoever adds a tile's sums
+
+
 def test_update_of_large_matrices():
     import torch
     import paper_2401_15207_amd as H

@@ -30,7 +30,7 @@ extern "C" size_t bytes(int count, const long long* s) {
   return ns_workspace_bytes(count, [&](int i, int64_t* r, int64_t* c) { *r = s[2 * i]; *c = s[2 * i + 1]; });
 }
 extern "C" size_t one(long long r, long long c) { return ns_bytes(r, c); }
-extern "C" size_t shared() { return NS_SHARED_BYTES; }
+extern "C" size_t shared(int side) { return ns_shared_bytes(side); }
 extern "C" double span(int n, const long long* count, const double* length) {
   NsTiles runs[16];
   for (int i = 0; i < n; ++i) runs[i] = {(int64_t)count[i], length[i]};
@@ -104,7 +104,7 @@ def test_work_space_and_launches(plan):
         assert launches([(8, 8), too_large]) == [(64, [1, 0])]
     small[0] = (64, 300)
     assert launches(small) == [(64, list(range(0, 16))), (64, list(range(16, 32))), (64, list(range(32, 40)))]
-    assert call(plan.bytes, small) == plan.shared() + 15 * plan.one(8, 8) + plan.one(64, 300)
+    assert call(plan.bytes, small) == plan.shared(128) + 15 * plan.one(8, 8) + plan.one(64, 300)
     # tiles of either size apart, the longest first, nothing for a side of 0, and no more than fits together
     mixed = [(64, 64), (4096, 4096), (0, 7), (4096, 11008), (100, 300)]
     assert launches(mixed) == [(256, [3, 1]), (64, [4, 0])] and launches([(64, 64), (600, 900)]) == [(64, [1, 0])]
@@ -114,11 +114,11 @@ def test_work_space_and_launches(plan):
     for few in (0, 1):  # every matrix once
         some = [(64, 64), (600, 900), (2048, 2048), (512, 512), (511, 4096), (0, 9), (5000, 1300), (1300, 900)]
         assert sorted(i for _, which in launches(some, few) for i in which) == [0, 1, 2, 3, 4, 6, 7]
-    assert call(plan.bytes, mixed) == plan.shared() + plan.one(4096, 4096) + plan.one(4096, 11008)
+    assert call(plan.bytes, mixed) == plan.shared(256) + plan.one(4096, 4096) + plan.one(4096, 11008)
     large = [(16384, 16384), (16384, 16384), (64, 64)]
     assert launches(large) == [(256, [0]), (256, [1]), (64, [2])]
     assert launches([(1024, 1024)] * 6) == [(128, [0, 1, 2, 3, 4, 5])]
-    assert call(plan.bytes, large) == plan.shared() + plan.one(16384, 16384)
+    assert call(plan.bytes, large) == plan.shared(256) + plan.one(16384, 16384)
 
 
 @pytest.mark.parametrize("runs", [[], [(1, 5.0)], [(256, 3.0)], [(257, 3.0)], [(3088, 7.0)], [(408, 11.0), (544, 4.0)], [(1, 100.0), (1000, 1.0)],
