@@ -539,8 +539,9 @@ hift_status hift_kernel_cross_entropy(int32_t dtype, int64_t rows, int32_t V, vo
  *   stats[r] = (m, ln S): what the gradient needs
  *   top_ids[r], top_logp[r]: the `top` (0 .. 32, at most V) largest logits' ids and log probabilities, in falling order; of equal logits the
  *   lowest id comes first, -0 equals 0, NaN precedes everything.
- * Entries of -inf (masked tokens) have probability 0.  A row of nothing else: logp and top_logp -inf, entropy 0, stats (0, -inf).  A NaN or
- * +inf makes its row's numbers NaN.  targets / logp, entropy, stats: device, fp32 (targets int32), NULL where not wanted; top_logp,
+ * Entries of -inf (masked tokens) have probability 0.  A row of nothing else: logp and top_logp -inf, entropy 0, stats (0, -inf).  Masks may be
+ * finite too, down to the type's lowest value: z is held in fp32, and beyond its range a finite logit's z is the largest number of its sign; a log
+ * probability below the range is -inf.  A NaN or +inf makes its row's numbers NaN.  targets / logp, entropy, stats: device, fp32 (targets int32), NULL where not wanted; top_logp,
  * top_ids: device [rows, top].  Sums in fp32 whatever dtype is. */
 hift_status hift_kernel_token_logprob(int32_t dtype, int64_t rows, int32_t V, int64_t ld, const void* logits, const int32_t* targets,
                                       float scale, int32_t top, float* logp, float* entropy, float* stats, float* top_logp,

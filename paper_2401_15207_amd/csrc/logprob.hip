@@ -19,6 +19,18 @@ constexpr float LN2_HI = 0.69314718246459960938f, LN2_LO = -1.904654299957767e-9
 constexpr float LOWEST = -3.402823466e38f;
 constexpr int CANDIDATES = 1024;  // entries that may be at or above a row's threshold before it goes the slow way
 
+// Near rows, whose largest z is at most NEAR from 0, are summed against references that are rounded products: z's rounding shows in what is summed, by
+// 2^-24 of the largest z.  In the others, far ones, every z is rounded and the largest subtracted from it first, which is exact where it matters.
+constexpr float NEAR = 4096.f;
+__device__ __forceinline__ bool is_near(float m) { return fabsf(m) <= NEAR; }
+// z of a far row.  Beyond fp32's range a finite logit's z is the largest number of its sign.
+__device__ __forceinline__ float far_z(float x, float scale) {
+  const float z = x * scale;
+  return fabsf(x) <= -LOWEST ? fminf(fmaxf(z, LOWEST), -LOWEST) : z;
+}
+// z - m in a row whose largest z is m
+__device__ __forceinline__ float below(float x, float scale, float m, bool near) { return near ? fmaf(x, scale, -m) : far_z(x, scale) - m; }
+
 struct LogprobArgs {
   int V, top;
   int64_t ld;
@@ -124,15 +136,21 @@ __device__ __forceinline__ uint64_t block_max64(uint64_t v, uint64_t* red) {
   return v;
 }
 
-// Sums of a part of a row against a reference: s = sum 2^d, u = sum 2^d d with d = c x - m2.  A masked entry has d = -inf and adds 0.
+// Where a part's largest entry lies in powers of two: what its sums refer to.  Not below -2^24: a large finite mask (-1e10, the type's lowest) has no
+// c x that fp32 could hold to within a few powers of two, or at all, and a near row's largest entry is far above; parts without entries
+// start there too.
+__device__ __forceinline__ float reference_of(float largest, float c) { return fmaxf(largest * c, -16777216.f); }
+
+// Sums of a part of a row against a reference: s = sum 2^d, u = sum 2^d d.  A masked entry has d = -inf and adds 0.
 struct Sums {
   float s = 0.f, u = 0.f;
-  __device__ __forceinline__ void add(float x, float c, float m2) {
-    const float d = fmaf(x, c, -m2), e = __builtin_amdgcn_exp2f(d);
+  __device__ __forceinline__ void add(float d) {
+    const float e = __builtin_amdgcn_exp2f(d);
     s += e;
     u = fmaf(e, fmaxf(d, -1024.f), u);
   }
-  // the same against a reference larger by `by`
+  __device__ __forceinline__ void add(float x, float c, float m2) { add(fmaf(x, c, -m2)); }
+  // the same against a reference larger by `by` (0 or more)
   __device__ __forceinline__ void shift(float by) {
     const float f = __builtin_amdgcn_exp2f(-by);
     u = f * fmaf(-by, s, u);
@@ -140,7 +158,8 @@ struct Sums {
   }
 };
 
-// One workgroup a row, one pass over it.  Every wavefront forms its sums against its own largest entry; the first one joins them.
+// One workgroup a row, one pass over it.  Every wavefront forms its sums against its own largest entry; the first one joins them.  Far rows take
+// another pass, against the row's largest.
 // Bound: the logits' way from memory once rows are many (4096 x 50272 fp32 139 us, 5.9 TB/s; 2048 x 32000 bf16 with 8 alternatives 31 us, 4.2
 // TB/s: one exponential and two multiply-adds an entry take as long as its two bytes); the chain of loads, reductions and barriers for one
 // (1 x 32000 with 20 alternatives 6 us).  Rows are not split over workgroups: one of 128000 takes 13 us, a launch that joins parts 4 more.
@@ -154,7 +173,7 @@ __global__ void __launch_bounds__(NT, NT == 1024 ? 4 : 8) logprob_k(LogprobArgs 
   __shared__ float wave_m[NW], wave_s[NW], wave_u[NW];
   __shared__ uint32_t parts[64];
   __shared__ uint64_t red64[NW], cand[CANDIDATES];
-  __shared__ float tau_s, m_s, ln_s_s, s_s;
+  __shared__ float tau_s, ln_s_s, s_s;
   __shared__ int count, look_count, looks[NT];
   const int64_t r = blockIdx.x;
   const int t = threadIdx.x, lane = t & 63;
@@ -169,7 +188,7 @@ __global__ void __launch_bounds__(NT, NT == 1024 ? 4 : 8) logprob_k(LogprobArgs 
   // shifted first.  Which pieces held it, and the largest of all others, spare nearly every thread the look for its alternatives.
   float mine = row.loose, second = -INFINITY, group;
   int best = -1;
-  float m2 = mine == -INFINITY ? 0.f : mine * c;
+  float m2 = reference_of(mine, c);
   Sums q;
   if (row.loose_id >= 0) q.add(row.loose, c, m2);
   Piece<T> now[Row::U], next[Row::U];
@@ -185,10 +204,11 @@ __global__ void __launch_bounds__(NT, NT == 1024 ? 4 : 8) logprob_k(LogprobArgs 
 #pragma unroll
     for (int k = 0; k < Row::U; ++k) asm volatile("" : "+v"(now[k].w));
     if (most > mine) {
-      q.shift(mine == -INFINITY ? 0.f : fmaf(most, c, -m2));
+      const float to = reference_of(most, c);
+      q.shift(to - m2);
       second = mine;
       mine = most;
-      m2 = most * c;
+      m2 = to;
       best = i;
     } else {
       second = fmaxf(second, most);
@@ -201,7 +221,7 @@ __global__ void __launch_bounds__(NT, NT == 1024 ? 4 : 8) logprob_k(LogprobArgs 
     for (int k = 0; k < Row::U; ++k) now[k] = next[k];
   }
   const float wm = wave_all<STEPS>(mine, max2, &group);
-  if (mine != -INFINITY) q.shift(fmaf(wm, c, -m2));
+  q.shift(reference_of(wm, c) - m2);
   q.s = wave_all<0>(q.s, sum2);
   q.u = wave_all<0>(q.u, sum2);
   const int k = a.top;
@@ -214,37 +234,48 @@ __global__ void __launch_bounds__(NT, NT == 1024 ? 4 : 8) logprob_k(LogprobArgs 
   if (t % (NT / 64) == 0) parts[t / (NT / 64)] = (ordered(group) & ~63u) | (63 - t / (NT / 64));
   if (t == 0) count = look_count = 0;
   __syncthreads();
-  if (t < 64) {
-    float mx = wave_m[0];
+  float mx = wave_m[0];
 #pragma unroll
-    for (int w = 1; w < NW; ++w) mx = fmaxf(mx, wave_m[w]);
-    const float m2 = mx == -INFINITY ? 0.f : mx * c;
+  for (int w = 1; w < NW; ++w) mx = fmaxf(mx, wave_m[w]);
+  const float m = mx == -INFINITY ? 0.f : far_z(mx, a.scale);
+  const bool near = is_near(m);
+  if (!near) {  // (+inf too: it gives NaN here)
+    Sums f;
+    row.each([&](float v, int) { f.add((far_z(v, a.scale) - m) * LOG2E); });
+    f.s = wave_all<0>(f.s, sum2);
+    f.u = wave_all<0>(f.u, sum2);
+    if (lane == 0) {
+      wave_s[t >> 6] = f.s;
+      wave_u[t >> 6] = f.u;
+    }
+    __syncthreads();
+  }
+  if (t < 64) {
+    const float m2 = reference_of(mx, c);
     Sums all;
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
       Sums p;
       p.s = wave_s[w];
       p.u = wave_u[w];
-      if (wave_m[w] != -INFINITY) p.shift(fmaf(-wave_m[w], c, m2));
+      if (near) p.shift(m2 - reference_of(wave_m[w], c));
       all.s += p.s;
       all.u += p.u;
     }
     const float s = all.s < INFINITY ? all.s : NAN;
-    // m2 is the rounded maximum in powers of two; ln S is given for the rounded maximum itself
-    const float m = mx == -INFINITY ? 0.f : mx * a.scale;
+    // a near row's m2 is the rounded maximum in powers of two; ln S is given for the rounded maximum itself
     const float ln = __builtin_amdgcn_logf(s) * LN2_HI;
-    const float ln_s = s > 0.f ? ln + fmaf(m2, LN2_LO, fmaf(m2, LN2_HI, -m)) : s == 0.f ? -INFINITY : s;
+    const float ln_s = s > 0.f ? ln + (near ? fmaf(m2, LN2_LO, fmaf(m2, LN2_HI, -m)) : 0.f) : s == 0.f ? -INFINITY : s;
     if (t == 0) {
       if (a.logp) {
         const int y = a.targets[r];
-        a.logp[r] = y < 0 || y >= a.V ? 0.f : s == 0.f ? -INFINITY : fmaf(to_f32(x[y]), a.scale, -m) - ln_s;
+        a.logp[r] = y < 0 || y >= a.V ? 0.f : s == 0.f ? -INFINITY : below(to_f32(x[y]), a.scale, m, near) - ln_s;
       }
       if (a.entropy) a.entropy[r] = s == 0.f ? 0.f : ln - LN2_HI * (all.u / s);
       if (a.stats) {
         a.stats[2 * r] = m;
         a.stats[2 * r + 1] = ln_s;
       }
-      m_s = m;
       ln_s_s = ln_s;
       s_s = s;
     }
@@ -258,12 +289,12 @@ __global__ void __launch_bounds__(NT, NT == 1024 ? 4 : 8) logprob_k(LogprobArgs 
   }
   if (k == 0) return;
   __syncthreads();
-  const float s = s_s, m = m_s, ln_s = ln_s_s, tau = tau_s;
+  const float s = s_s, ln_s = ln_s_s, tau = tau_s;
   float* top_logp = a.top_logp + r * k;
   int32_t* top_ids = a.top_ids + r * k;
   auto put = [&](int at, float v, int id) {
     top_ids[at] = id;
-    top_logp[at] = s == 0.f ? -INFINITY : fmaf(v, a.scale, -m) - ln_s;
+    top_logp[at] = s == 0.f ? -INFINITY : below(v, a.scale, m, near) - ln_s;
   };
   const bool plain = s < INFINITY;  // neither NaN nor +inf in the row
   const auto collect = [&](float v, int id) {
@@ -359,8 +390,9 @@ __global__ void __launch_bounds__(BWD_THREADS) logprob_bwd_k(LogprobBwdArgs a) {
   const float h = a.d_entropy ? a.d_entropy[r] : 0.f;
   const float gh = a.d_entropy ? fmaf(h, a.entropy[r], g) : g;
   const bool empty = ln_s == -INFINITY;  // nothing but masked entries: no gradient
+  const bool near = is_near(m);          // (as the forward pass formed m and ln S)
   auto one = [&](float v, int j) {
-    const float lp = fmaf(v, a.scale, -m) - ln_s;
+    const float lp = below(v, a.scale, m, near) - ln_s;
     const float p = __builtin_amdgcn_exp2f(lp * LOG2E);
     float d = -p * fmaf(h, fmaxf(lp, -1024.f), gh);  // (0 times the -inf of a masked entry)
     if (j == y) d += g;
