@@ -119,8 +119,8 @@ typedef struct {
 } hift_opt;
 /* HIFT_MUON (Jordan et al. 2024): the hidden layers' matrices -- q, k, v, gate and up each by itself -- take the update of hift_kernel_muon
  * (lr, momentum in [0, 1), weight_decay; state array 0 is the momentum, array 1 stays 0), everything else AdamW's with the same lr, beta1,
- * beta2, eps and weight_decay.  bf16 models: the orthogonalised step is within 2^-9 of itself; fp32 models keep fp32's exactness.  The work
- * space of one layer (3.4 GB at the 7B shape) is part of the device arena. */
+ * beta2, eps and weight_decay.  The step that goes into the fp32 weights is as exact as fp32 products give it, in models of either type.  The
+ * work space of one layer (3.4 GB at the 7B shape) is part of the device arena. */
 /* HIFT_ADAFACTOR (section "Memory Efficiency Analysis" lists it among the optimizers): Shazeer and Stern
  * 2018, Algorithm 4 without momentum, with the caller's lr as the step size (no relative step, no
  * parameter scaling); epsilon_1 = 1e-30, clipping threshold 1, beta2_t = 1 - t^-0.8 with t the group's own
@@ -576,7 +576,8 @@ hift_status hift_kernel_orthogonalize(int32_t src_dtype, int32_t dst_dtype, int3
 /* The update of HIFT_MUON for matrices (fp32, contiguous [rows, cols]; compute_copy bf16 or NULL): with mu = opt->momentum
  *   momentum <- mu momentum + grad;   O = orthogonalised (grad + mu momentum): five steps of (3.4445, -4.7750, 2.0315), eps 1e-7
  *   master <- (1 - lr weight_decay) master - lr 0.2 sqrt(max(rows, cols)) O;   compute_copy <- master rounded
- * (the factor gives the step the size that AdamW's has at the same rate).  Uses kind, lr, momentum and weight_decay of opt.  Work space as
+ * (the factor gives the step the size that AdamW's has at the same rate).  Products carry 22 bits of every factor and fp32 sums; what master
+ * and momentum receive does not depend on which matrices have copies.  Uses kind, lr, momentum and weight_decay of opt.  Work space as
  * for hift_kernel_orthogonalize. */
 typedef struct {
   int64_t rows, cols;

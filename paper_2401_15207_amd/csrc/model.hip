@@ -205,9 +205,10 @@ hift_status check_opt(const hift_opt* o) {
   return HIFT_OK;
 }
 
-// The steps of HIFT_MUON: Newton-Schulz of degree five with the coefficients of Jordan et al. 2024.
-NsRun muon_run(const hift_opt& o, bool bf16_model) {
-  return NsRun{5, {3.4445, -4.7750, 2.0315}, 1e-7f, o.lr, (float)o.momentum, (float)(1.0 - o.lr * o.weight_decay), bf16_model};
+// The steps of HIFT_MUON: Newton-Schulz of degree five with the coefficients of Jordan et al. 2024.  All products: the result goes into fp32 weights,
+// with or without bf16 copies of them.
+NsRun muon_run(const hift_opt& o) {
+  return NsRun{5, {3.4445, -4.7750, 2.0315}, 1e-7f, o.lr, (float)o.momentum, (float)(1.0 - o.lr * o.weight_decay), false};
 }
 
 // How many matrices side by side a tensor holds that HIFT_MUON orthogonalises one by one: hidden layers' matrices, q | k | v and gate | up
@@ -2164,7 +2165,7 @@ hift_status step_of(hift_model* M, const hift_batch* bt, int32_t gid, const Scor
       items.clear();
     }
     for (const auto& layer : ortho)
-      K_TRY(newton_schulz(layer.data(), (int)layer.size(), DT_F32, DT_F32, muon_run(M->opt, M->dt == DT_BF16), M->ns_work, M->cs));
+      K_TRY(newton_schulz(layer.data(), (int)layer.size(), DT_F32, DT_F32, muon_run(M->opt), M->ns_work, M->cs));
     // gains first: those of a normalisation that is folded into a weight go into its copy with their new values
     if (!items.empty()) K_TRY(optimizer_update(oa, items.data(), (int)items.size(), M->cs));
     if (!packs.empty()) K_TRY(optimizer_update_packed(oa, packed_items.data(), packs.data(), (int)packs.size(), M->cs));
@@ -2815,9 +2816,7 @@ hift_status hift_kernel_muon(const hift_opt* opt, int32_t count, const hift_muon
       return fail(HIFT_EINVAL, "matrix %d does not lie on whole elements", i);
   }
   ST_TRY(check_ns_workspace(items, workspace, workspace_bytes));
-  // (weights without bf16 copies are an fp32 model's)
-  const bool few = count > 0 && std::all_of(items.begin(), items.end(), [](const NsItem& it) { return it.copy != nullptr; });
-  HIP_TRY(newton_schulz(items.data(), count, DT_F32, DT_F32, muon_run(*opt, few), workspace, (hipStream_t)stream));
+  HIP_TRY(newton_schulz(items.data(), count, DT_F32, DT_F32, muon_run(*opt), workspace, (hipStream_t)stream));
   return HIFT_OK;
 }
 

@@ -1,0 +1,106 @@
+"""What the bits of an orthogonalised result may depend on: neither the type of the result nor what else is handed in.
+
+Tolerances: a bf16 result is the fp32 one rounded, half of 2^-8 of each entry at most.  fp32 results: `any` of the orthogonalisations' tests,
+5 2^-21 a^5 sqrt(short side) absolutely after five steps."""
+import math
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+COEF = (3.4445, -4.7750, 2.0315)
+
+
+def reference(u, steps=5, coef=COEF):
+    x = u.double()
+    tall = x.shape[0] > x.shape[1]
+    x = x.t().contiguous() if tall else x
+    x = x / x.norm()
+    for _ in range(steps):
+        s = x @ x.t().contiguous()
+        x = coef[0] * x + (coef[1] * s + coef[2] * (s @ s)) @ x
+    return x.t() if tall else x
+
+
+def matrices(kind, r, c):
+    """Matrices whose entries' roundings are alike, so that no sum averages them out, and random ones."""
+    import torch
+    g = torch.Generator(device="cuda")
+    g.manual_seed(r + 3 * c)
+    if kind == "constant":
+        return torch.full((r, c), 0.37, device="cuda")
+    if kind == "diagonal":
+        u = torch.zeros(r, c, device="cuda")
+        u.diagonal().copy_(torch.rand(min(r, c), generator=g, device="cuda"))
+        return u
+    if kind == "blocks":       # 8 x 8 times the same block
+        return torch.randn((r + 7) // 8, (c + 7) // 8, generator=g, device="cuda").repeat(8, 8)[:r, :c].contiguous()
+    if kind == "equal magnitudes":     # orthogonal rows of +-1, each with a size of its own
+        h = torch.ones(1, 1, device="cuda")
+        while h.shape[0] < max(r, c):
+            h = torch.cat([torch.cat([h, h], 1), torch.cat([h, -h], 1)], 0)
+        h = h[:r, :c] if r <= c else h[:c, :r].t()
+        size = 0.5 + torch.rand(min(r, c), generator=g, device="cuda")
+        return (h * (size.unsqueeze(1) if r <= c else size)).contiguous()
+    if kind == "low rank":
+        return torch.randn(r, 9, generator=g, device="cuda") @ torch.randn(9, c, generator=g, device="cuda") + 1e-3 * torch.randn(r, c, generator=g, device="cuda")
+    return torch.randn(r, c, generator=g, device="cuda")
+
+
+def test_the_master_weights_do_not_depend_on_copies():
+    """With copies of all matrices, of none, and of some, and beside a matrix without entries: the same master weights and momentum, exact to fp32."""
+    import torch
+    import paper_2401_15207_amd as H
+    shapes = [(520, 1024), (1500, 3000), (64, 64), (0, 9), (700, 640)]
+    g = torch.Generator(device="cuda")
+    g.manual_seed(2)
+    w, m = ([torch.randn(s, generator=g, device="cuda") * size for s in shapes] for size in (0.02, 1e-4))
+    gr = [matrices("equal magnitudes", *s) * 1e-4 if min(s) > 0 else torch.zeros(s, device="cuda") for s in shapes]
+    opt = dict(kind="muon", lr=1e-2, momentum=0.95, weight_decay=0.01)
+    results = []
+    for listed, with_copy in ((range(5), ()), ((0, 1, 2, 4), range(5)), (range(5), range(5)), (range(5), (0, 1, 2, 4)), (range(5), (1, 3))):
+        w1, m1 = [x.clone() for x in w], [x.clone() for x in m]
+        cc = [torch.empty(s, device="cuda", dtype=torch.bfloat16) if i in with_copy else None for i, s in enumerate(shapes)]
+        H.kernel_muon(opt, *[[x[i] for i in listed] for x in (w1, gr, m1, cc)])
+        results.append(w1 + m1)
+        assert all(torch.equal(cc[i], w1[i].to(torch.bfloat16)) for i in with_copy)
+    for other in results[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(results[0], other))
+    for i, s in enumerate(shapes):
+        if min(s) == 0:
+            continue
+        m64 = 0.95 * m[i].double() + gr[i].double()
+        factor = 1e-2 * 0.2 * math.sqrt(max(s))
+        want = (1.0 - 1e-4) * w[i].double() - factor * reference(gr[i].double() + 0.95 * m64)
+        assert (results[0][i].double() - want).norm().item() <= factor * 5 * 2.0 ** -21 * COEF[0] ** 5 * math.sqrt(min(s)) + 2.0 ** -22 * want.norm().item()
+
+
+def test_lists_that_fit_a_compute_unit_in_a_graph():
+    """The single launch of small lists, captured: replays with other inputs in between give the eager call's bits."""
+    import torch
+    import paper_2401_15207_amd as H
+    g = torch.Generator(device="cuda")
+    g.manual_seed(6)
+    shapes = [(64, 64), (33, 7), (256, 64), (64, 200)]
+    assert H.kernel_orthogonalize_bytes(shapes) == 0
+    u = [torch.randn(s, generator=g, device="cuda") for s in shapes]
+    want, other, got, src = [torch.empty_like(x) for x in u], [torch.empty_like(x) for x in u], [torch.empty_like(x) for x in u], [x.clone() for x in u]
+    H.kernel_orthogonalize(u, want)
+    H.kernel_orthogonalize([-x for x in u], other)   # (the matrix instructions' sums are not rounded alike with the other sign)
+    ws, side, graph = torch.empty(16, device="cuda", dtype=torch.uint8), torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        H.kernel_orthogonalize(src, got, workspace=ws)
+    for _ in range(3):
+        for x in got:
+            x.fill_(3.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        for a in src:
+            a.mul_(-1.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, other))
+        for a in src:
+            a.mul_(-1.0)
