@@ -557,8 +557,9 @@ hift_status hift_kernel_token_logprob_bwd(int32_t dtype, int64_t rows, int32_t V
 
 /* Orthogonalisation of matrices by Newton-Schulz steps: X = src / max(|src|_F, eps); `steps` (1 .. 16) times
  * X <- a X + b (X X^T) X + c (X X^T)^2 X; dst = X.  src, dst: device, rows ld_src / ld_dst >= cols apart, of type src_dtype / dst_dtype (HIFT_F32
- * or HIFT_BF16); dst may be src where the types are the same.  Products carry 22 bits of every factor and fp32 sums; into a bf16 dst
- * matrices of 512 and more on the short side may take fewer (within 2^-9 of the whole in the 2-norm).  A src of zeros gives zeros; one that holds NaN or infinities gives NaN.  Matrices of one call share launches, so hand in together what is there together.
+ * or HIFT_BF16); dst may be src where the types are the same.  Products carry 22 bits of every factor and fp32 sums; a bf16 dst receives
+ * the result rounded.  A src of zeros gives zeros; one that holds NaN or infinities gives NaN.  Matrices of one call share launches, so hand in
+ * together what is there together.
  * Either side at most 65536 long; a matrix with a side of 0 is skipped.  HIFT_EINVAL also for a < 1 (small singular values would not grow)
  * and for coefficients under which the singular values, all in [0, 1] at first, could leave fp16's range.
  * workspace: device, 16-byte aligned, hift_kernel_orthogonalize_bytes (which reads rows and cols only), free again once the call's work on

@@ -245,7 +245,6 @@ struct NsRun {
   float eps;
   double lr;     // the update's
   float mu, decay;
-  bool few;      // fewer products for large matrices: the result goes into bf16 numbers (see muon.hip)
 };
 bool ns_coefficients_hold(const double (&co)[3], int steps);  // the singular values stay in range
 size_t ns_workspace(const NsItem* items, int count);          // bytes; newton_schulz wants them 16-byte aligned

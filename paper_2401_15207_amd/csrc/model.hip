@@ -205,10 +205,9 @@ hift_status check_opt(const hift_opt* o) {
   return HIFT_OK;
 }
 
-// The steps of HIFT_MUON: Newton-Schulz of degree five with the coefficients of Jordan et al. 2024.  All products: the result goes into fp32 weights,
-// with or without bf16 copies of them.
+// The steps of HIFT_MUON: Newton-Schulz of degree five with the coefficients of Jordan et al. 2024. 
 NsRun muon_run(const hift_opt& o) {
-  return NsRun{5, {3.4445, -4.7750, 2.0315}, 1e-7f, o.lr, (float)o.momentum, (float)(1.0 - o.lr * o.weight_decay), false};
+  return NsRun{5, {3.4445, -4.7750, 2.0315}, 1e-7f, o.lr, (float)o.momentum, (float)(1.0 - o.lr * o.weight_decay)};
 }
 
 // How many matrices side by side a tensor holds that HIFT_MUON orthogonalises one by one: hidden layers' matrices, q | k | v and gate | up
@@ -2774,7 +2773,7 @@ hift_status hift_kernel_orthogonalize(int32_t src_dtype, int32_t dst_dtype, int3
   if ((src_dtype != HIFT_F32 && src_dtype != HIFT_BF16) || (dst_dtype != HIFT_F32 && dst_dtype != HIFT_BF16)) return fail(HIFT_EINVAL, "dtype unknown");
   if (steps < 1 || steps > NS_STEPS_MAX) return fail(HIFT_EINVAL, "steps must be in [1, %d]", NS_STEPS_MAX);
   if (!(eps >= 1e-30f) || std::isinf(eps)) return fail(HIFT_EINVAL, "eps must be at least 1e-30");
-  NsRun run{steps, {a, b, c}, eps, 0.0, 0.f, 0.f, dst_dtype == HIFT_BF16};
+  NsRun run{steps, {a, b, c}, eps, 0.0, 0.f, 0.f};
   if (!ns_coefficients_hold(run.co, steps)) return fail(HIFT_EINVAL, "the singular values grow without bound under (%g, %g, %g)", a, b, c);
   std::vector<NsItem> items;
   ST_TRY(ns_items(count, matrices, &items, [&](int i, NsItem& it) { ortho_item(matrices[i], it); }));

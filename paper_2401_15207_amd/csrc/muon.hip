@@ -7,15 +7,12 @@
 // bf16 nor one fp16 number holds enough.  Every factor is kept as the sum of two fp16 numbers, high and low (22 bits; see ns_plan.h for
 // the scales), and a product is three matrix instructions, high high + high low + low high, summed in fp32: results as exact as fp32
 // products give them, at a third of the fp16 rate instead of an eleventh of it.
-// A result that goes into bf16 numbers (rounded to 2^-9 of themselves) need not be that exact.  Roundings of A and B act on X as a factor from
-// the left does, so they stay what they are: those of X alone are multiplied.  So with NsRun::few the matrices of 512 and more on the
-// short side take high high alone for A and for A A, high high + high low for B X and high high again for the last B X.  What
-// the roundings of the two diagonals leave, which no sum averages out, is put back by the epilogues (a_rest, b_rest).  Simulated in 64 bits on random,
-// low-rank (noise 1e-3 of it) and decaying (1e-6) matrices of 512 x 512 .. 2048: 3e-4 to 1.3e-3 off in the 2-norm, half as far as the
-// rounding to bf16 itself; with single numbers throughout 3e-3, and 3e-2 where the rank is low.
+// Results in bf16 take the same products.  Single numbers for A, for A A or for the last B X leave roundings that no sum averages out where the
+// entries of a matrix round alike: simulated in 64 bits, diagonal, block-repeated and equal-magnitude matrices come out 2e-3 to 6e-3 off in the
+// 2-norm after five steps and up to 0.2 after sixteen, which is more than the rounding to bf16.
 // Factors lie in the matrix instruction's register order: blocks of 32 rows x 16 k, 1 KB of high or of low numbers, lane l of a wavefront
 // holding row l % 32 and k 8 (l / 32) .. +7 of it, so that a fragment is one contiguous load; blocks along k follow each other, high and
-// low ones apart (side by side, A of high numbers alone took 39 us instead of 36 in a layer 1024 wide).
+// low ones apart.
 #include <limits.h>
 #include <math.h>
 
@@ -49,7 +46,6 @@ struct NsMatrix {
   int n, m;             // short and long side, filled up
   int tall;             // rows > cols: X is U^T
   _Float16 *x, *xt, *xt2, *a, *b;  // X [n, m], X^T [m, n] now and after the step, A and B [n, n]
-  float *a_rest, *b_rest;  // [n] of A's and B's diagonal what the high numbers leave (fewer products)
   double* norm_parts;
   int* small;           // how many powers of two X is below 1 at the start (norms below eps; ns_start_k)
   int parts;            // workgroups that share the k range of one of its tiles
@@ -156,10 +152,10 @@ __device__ __forceinline__ int start_scale(double sum_of_squares, float eps, flo
 }
 
 // ---- U -> X and X^T in fragment order --------------------------------------------------------
-// Squares of 64 x 64 through LDS, so that both orders leave in whole blocks.  Bound: memory, 1.6 GB read and 1.2 (all products: 1.6) written of a layer 4096
-// wide in 590 us; the square is requested before the norm's parts are summed.
+// Squares of 64 x 64 through LDS, so that both orders leave in whole blocks.  Bound: memory, 1.6 GB read and 1.6 written of a layer 4096
+// wide in 670 us; the square is requested before the norm's parts are summed.
 template <typename T>
-__global__ void __launch_bounds__(256) ns_start_k(NsTable t, float mu, float eps, float scale, bool few) {
+__global__ void __launch_bounds__(256) ns_start_k(NsTable t, float mu, float eps, float scale) {
   __shared__ float tile[64][65];
   __shared__ double red[4];
   const int at = matrix_of(t, blockIdx.x), id = blockIdx.x - t.first[at];
@@ -205,7 +201,7 @@ __global__ void __launch_bounds__(256) ns_start_k(NsTable t, float mu, float eps
     }
     _Float16* p = along.block((int)(r0 / 32) + rb, (int)(c0 / 16) + kb) + lane * 8;
     *reinterpret_cast<half8*>(p) = hi;
-    if (!few || q.tall) *reinterpret_cast<half8*>(p + along.low()) = lo;  // (fewer products never read X's own low numbers)
+    *reinterpret_cast<half8*>(p + along.low()) = lo;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       _Float16 h, l;
@@ -214,7 +210,7 @@ __global__ void __launch_bounds__(256) ns_start_k(NsTable t, float mu, float eps
     }
     p = across.block((int)(c0 / 32) + rb, (int)(r0 / 16) + kb) + lane * 8;
     *reinterpret_cast<half8*>(p) = hi;
-    if (!few || !q.tall) *reinterpret_cast<half8*>(p + across.low()) = lo;
+    *reinterpret_cast<half8*>(p + across.low()) = lo;
   }
 }
 
@@ -240,8 +236,7 @@ __device__ __forceinline__ int acc_row(int i, int lane) { return 8 * (i >> 2) + 
 constexpr int TURN_PITCH = 36;  // words: the turned block's rows are read in 16-byte pieces
 
 // v: entries [i0 ..][j0 ..] of a 32 x 32 block, into a factor of rows j and k i (four consecutive k of a lane at a time) and, if
-// `other`, turned around in LDS into one of rows i and k j.  LOW_J, LOW_I: the low numbers too.
-template <bool LOW_J, bool LOW_I>
+// `other`, turned around in LDS into one of rows i and k j.
 __device__ __forceinline__ void put_block(const Factor& rows_j, const Factor& rows_i, bool other, int i0, int j0, const f32x16& v, uint32_t* turned,
                                           int lane) {
 #pragma unroll
@@ -258,7 +253,7 @@ __device__ __forceinline__ void put_block(const Factor& rows_j, const Factor& ro
     }
     _Float16* p = rows_j.block(j0 / 32, i0 / 16 + (g >> 1)) + ((lane & 31) + 32 * (g & 1)) * 8 + 4 * (lane >> 5);
     *reinterpret_cast<half4*>(p) = hi;
-    if (LOW_J) *reinterpret_cast<half4*>(p + rows_j.low()) = lo;
+    *reinterpret_cast<half4*>(p + rows_j.low()) = lo;
   }
   if (!other) return;
   __builtin_amdgcn_wave_barrier();  // (a wavefront's own LDS accesses stay in order)
@@ -275,7 +270,7 @@ __device__ __forceinline__ void put_block(const Factor& rows_j, const Factor& ro
     }
     _Float16* p = rows_i.block(i0 / 32, j0 / 16 + b) + lane * 8;
     *reinterpret_cast<hift_u32x4*>(p) = hift_u32x4{hi[0], hi[1], hi[2], hi[3]};
-    if (LOW_I) *reinterpret_cast<hift_u32x4*>(p + rows_i.low()) = hift_u32x4{lo[0], lo[1], lo[2], lo[3]};
+    *reinterpret_cast<hift_u32x4*>(p + rows_i.low()) = hift_u32x4{lo[0], lo[1], lo[2], lo[3]};
   }
   __builtin_amdgcn_wave_barrier();
 }
@@ -287,19 +282,18 @@ __device__ __forceinline__ const _Float16* at_block(const Factor& rows_j, int i0
 
 // Tiles of 256 x 256 by 2 x 4 wavefronts, of 128 x 128 and 64 x 64 by 2 x 2.  Both operands travel into LDS with direct-to-LDS loads, as they
 // lie, into a ring of stages of 16 to 64 k; a stage's fragments are read into registers under the products of the stage before.
-// PP, QP: numbers of P and Q that take part: 2 and 2 (three products), 1 and 2 (two), 1 and 1 (one).
-// What bounds it, a layer 4096 wide with 11008 in its feed-forward block and a bf16 result (256 x 256): A 765 us, 1150 TFLOP/s by the upper
-// tiles' entries, B 500 (1020; 4 rounds of 3.7), X 2.6 ms (1280 by matrix instructions; 12 rounds and a shared one), the last X with the update 1.9:
-// where one product is taken LDS gives 125 of its 128 bytes a clock, with more the matrix pipe is at the power limit.  A layer 1024 wide
-// (128 x 128): 37, 22, 62 and 65 us (with the update 82), each one round or two of tiles.
+// What bounds it, a layer 4096 wide with 11008 in its feed-forward block (256 x 256): A 1.97 ms, 1340 TFLOP/s by the matrix instructions of the
+// upper tiles, B 1.25 (1220; 4 rounds of 3.7), X 3.8 (1320; 12 rounds and a shared one), the last X with the update 4.1 (1210): the matrix pipe,
+// of which a large fp16 product reaches 1500.  A layer 1024 wide (128 x 128): 65, 37, 81 and 86 us (with the update 105), each one round or two of
+// tiles.
 // DEEP: the ring of a launch that gives a compute unit one workgroup at most.  That one waits for memory by itself: a stage of 16 KB takes
 // the time of its requests' latency over the stages in flight, so the ring takes most of the LDS.
-template <int SIDE, int PP, int QP, bool DEEP>
+template <int SIDE, bool DEEP>
 struct NsTile {
   static constexpr int WI = 2, WJ = SIDE == 256 ? 4 : 2, NW = WI * WJ;
   static constexpr int BI = SIDE / 32 / WI, BJ = SIDE / 32 / WJ;   // blocks of 32 x 32 a wavefront
-  static constexpr int KS = SIDE == 64 ? 4 : PP + QP == 2 ? 2 : 1; // blocks along k of a stage
-  static constexpr int PN = SIDE / 32 * KS * PP, PIECES = PN + SIDE / 32 * KS * QP;  // KB of P in a stage, and of both
+  static constexpr int KS = SIDE == 64 ? 4 : 1;                    // blocks along k of a stage
+  static constexpr int PN = SIDE / 32 * KS * 2, PIECES = 2 * PN;   // KB of P in a stage, and of both
   static constexpr int LOADS = PIECES / NW;                        // load instructions a wavefront and stage, 1 KB each
   static constexpr int STAGE = PIECES * 1024, RING = SIDE == 256 || (SIDE == 64 && DEEP) ? 4 : SIDE == 64 ? 2 : DEEP ? 8 : 3, LDS = RING * STAGE;
   static_assert(PIECES % NW == 0 && LDS <= 160 * 1024 && NW * 32 * TURN_PITCH * 4 <= LDS, "blocks turn in the ring");
@@ -318,11 +312,10 @@ __device__ __forceinline__ void put_result(const NsMatrix& q, int64_t row, int64
   }
 }
 
-template <int SIDE, int MODE, int PP, int QP, bool DEEP, typename OUT>
-__global__ void __launch_bounds__((64 * NsTile<SIDE, PP, QP, DEEP>::NW), (DEEP && SIDE < 256 ? 1 : 2)) ns_product_k(NsTable t, NsStep st) {
-  typedef NsTile<SIDE, PP, QP, DEEP> T;
+template <int SIDE, int MODE, bool DEEP, typename OUT>
+__global__ void __launch_bounds__((64 * NsTile<SIDE, DEEP>::NW), (DEEP && SIDE < 256 ? 1 : 2)) ns_product_k(NsTable t, NsStep st) {
+  typedef NsTile<SIDE, DEEP> T;
   constexpr int BI = T::BI, BJ = T::BJ, RING = T::RING, KS = T::KS;
-  constexpr bool FEW = PP + QP < 4;
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   const int at = matrix_of(t, blockIdx.x), block0 = t.first[at];
   const NsMatrix& q = t.m[at];
@@ -368,15 +361,15 @@ __global__ void __launch_bounds__((64 * NsTile<SIDE, PP, QP, DEEP>::NW), (DEEP &
     for (int i = 0; i < T::LOADS; ++i) {
       const int load = wave * T::LOADS + i;
       const bool is_q = load >= T::PN;
-      const int in = is_q ? load - T::PN : load, planes = is_q ? QP : PP, rb = in / (KS * planes), rest = in % (KS * planes);
+      const int in = is_q ? load - T::PN : load, rb = in / (KS * 2), rest = in % (KS * 2);
       const uint64_t base = is_q ? qa : pa;
       const hift_u32x4 rsrc = {(uint32_t)base, (uint32_t)(base >> 32) & 0xFFFFu, 0xFFFFFFF0u, 0x00020000u};
-      const uint32_t soff = (((uint32_t)rb * 2 + rest % planes) * P.kb + s * KS + rest / planes) * 1024u;
+      const uint32_t soff = (((uint32_t)rb * 2 + rest % 2) * P.kb + s * KS + rest / 2) * 1024u;
       load_to_lds_b128(rsrc, at + (uint32_t)load * 1024, voff, soff);
     }
   };
   const int wi = wave / T::WJ, wj = wave % T::WJ;
-  half8 p[2][KS][BI][PP], r[2][KS][BJ][QP];  // fragments of two stages: high and low numbers
+  half8 p[2][KS][BI][2], r[2][KS][BJ][2];  // fragments of two stages: high and low numbers
   auto read = [&](int to, int s) __attribute__((always_inline)) {
     const unsigned char* at = smem + slot(s) * T::STAGE + lane * 16;
 #pragma unroll
@@ -384,11 +377,11 @@ __global__ void __launch_bounds__((64 * NsTile<SIDE, PP, QP, DEEP>::NW), (DEEP &
 #pragma unroll
       for (int b = 0; b < BI; ++b)
 #pragma unroll
-        for (int h = 0; h < PP; ++h) p[to][k][b][h] = *reinterpret_cast<const half8*>(at + (((wi * BI + b) * KS + k) * PP + h) * 1024);
+        for (int h = 0; h < 2; ++h) p[to][k][b][h] = *reinterpret_cast<const half8*>(at + (((wi * BI + b) * KS + k) * 2 + h) * 1024);
 #pragma unroll
       for (int b = 0; b < BJ; ++b)
 #pragma unroll
-        for (int h = 0; h < QP; ++h) r[to][k][b][h] = *reinterpret_cast<const half8*>(at + (T::PN + ((wj * BJ + b) * KS + k) * QP + h) * 1024);
+        for (int h = 0; h < 2; ++h) r[to][k][b][h] = *reinterpret_cast<const half8*>(at + (T::PN + ((wj * BJ + b) * KS + k) * 2 + h) * 1024);
     }
   };
   f32x16 acc[BI][BJ] = {};
@@ -396,7 +389,7 @@ __global__ void __launch_bounds__((64 * NsTile<SIDE, PP, QP, DEEP>::NW), (DEEP &
 #pragma unroll
     for (int k = 0; k < KS; ++k)
 #pragma unroll
-      for (int h = PP + QP - 2; h >= 0; --h)  // low high, high low, high high
+      for (int h = 2; h >= 0; --h)  // low high, high low, high high
 #pragma unroll
         for (int x = 0; x < BI; ++x)
 #pragma unroll
@@ -484,25 +477,19 @@ __global__ void __launch_bounds__((64 * NsTile<SIDE, PP, QP, DEEP>::NW), (DEEP &
   uint32_t* turned = reinterpret_cast<uint32_t*>(smem) + wave * 32 * TURN_PITCH;
   // What a block of the epilogue reads is requested before the block before it is written: the wait for a load would take in the stores
   // before it.
-  struct Ahead { half4 hi[4], lo[4]; float rest[4][4], rest_j; f32x16 w; };
-  const Factor f = MODE == NS_POLY ? Factor{q.a, q.n / 16} : turn ? Factor{q.x, q.m / 16} : Factor{q.xt, q.n / 16};
+  struct Ahead { half4 hi[4], lo[4]; f32x16 w; };
+  const Factor f{q.a, q.n / 16};
   const auto block_i = [&](int b) __attribute__((always_inline)) { return ti * SIDE + (wi * BI + b / BJ) * 32; };
   const auto block_j = [&](int b) __attribute__((always_inline)) { return tj * SIDE + (wj * BJ + b % BJ) * 32; };
   const auto ahead = [&](Ahead& n, int b) __attribute__((always_inline)) {
     const int i = block_i(b), j = block_j(b);
-    const float* rest = MODE == NS_POLY ? q.a_rest : q.b_rest;
-    if (MODE == NS_POLY || (!SYM && FEW)) {
+    if (MODE == NS_POLY)
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const _Float16* p = at_block(f, i, j, g, lane);
         n.hi[g] = *reinterpret_cast<const half4*>(p);
-        if (MODE == NS_POLY) n.lo[g] = *reinterpret_cast<const half4*>(p + f.low());
-        if (FEW && !turn)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) n.rest[g][e] = rest[i + acc_row(4 * g + e, lane)];
+        n.lo[g] = *reinterpret_cast<const half4*>(p + f.low());
       }
-      if (FEW && (turn || MODE == NS_POLY)) n.rest_j = rest[j + (lane & 31)];
-    }
     if (MODE == NS_LAST && q.master)
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
@@ -524,18 +511,10 @@ __global__ void __launch_bounds__((64 * NsTile<SIDE, PP, QP, DEEP>::NW), (DEEP &
       for (int g = 0; g < 4; ++g)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float hi = (float)now.hi[g][e];
-          float aa = v[4 * g + e];
-          if (FEW) aa = fmaf(hi, now.rest[g][e] + now.rest_j, aa);  // what the diagonal's low numbers add to A A
+          const float entry = (float)now.hi[g][e] + (float)now.lo[g][e];
           const bool diagonal = i + acc_row(4 * g + e, lane) == j + (lane & 31);
-          v[4 * g + e] = (fmaf(st.cc, aa, st.cb * (hi + (float)now.lo[g][e])) + (diagonal ? st.ca : 0.f)) * st.out_scale;
+          v[4 * g + e] = (fmaf(st.cc, v[4 * g + e], st.cb * entry) + (diagonal ? st.ca : 0.f)) * st.out_scale;
         }
-    } else if (!SYM && FEW) {
-      // what the diagonal of B's low numbers adds to B X: X at the same place, in the factor whose rows are j
-#pragma unroll
-      for (int g = 0; g < 4; ++g)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[4 * g + e] = fmaf((float)now.hi[g][e], turn ? now.rest_j : now.rest[g][e], v[4 * g + e]);
     }
     if (MODE == NS_GRAM || MODE == NS_APPLY) {
       const int power = MODE == NS_GRAM ? -2 * up : max(0, small - st.grown - st.growth) - up;
@@ -544,16 +523,9 @@ __global__ void __launch_bounds__((64 * NsTile<SIDE, PP, QP, DEEP>::NW), (DEEP &
     }
     if (SYM) {
       const Factor out{MODE == NS_GRAM ? q.a : q.b, q.n / 16};
-      constexpr bool LOW = !FEW || MODE == NS_GRAM;
-      put_block<LOW, LOW>(out, out, ti != tj, i, j, v, turned, lane);
-      if (FEW && i == j) {
-        float* rest = MODE == NS_GRAM ? q.a_rest : q.b_rest;
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (acc_row(e, lane) == (lane & 31)) rest[i + (lane & 31)] = v[e] - (float)(_Float16)v[e];
-      }
+      put_block(out, out, ti != tj, i, j, v, turned, lane);
     } else if (MODE == NS_APPLY) {
-      put_block<true, !FEW>(Factor{q.xt2, q.n / 16}, Factor{q.x, q.m / 16}, true, i, j, v, turned, lane);
+      put_block(Factor{q.xt2, q.n / 16}, Factor{q.x, q.m / 16}, true, i, j, v, turned, lane);
     } else {
 #pragma unroll
       for (int e = 0; e < 16; ++e) put_result<OUT>(q, i + acc_row(e, lane), j + (lane & 31), ldexpf(v[e] * st.unscale, -up), st.decay, now.w[e]);
@@ -820,11 +792,11 @@ uint32_t spread(NsTable& t, F blocks) {
   return (uint32_t)at;
 }
 
-template <int SIDE, int MODE, int PP, int QP, bool DEEP, typename OUT>
+template <int SIDE, int MODE, bool DEEP, typename OUT>
 hipError_t launch_product(uint32_t blocks, const NsTable& t, const NsStep& p, hipStream_t st) {
-  typedef NsTile<SIDE, PP, QP, DEEP> T;
+  typedef NsTile<SIDE, DEEP> T;
   static bool attr_done = false;  // one flag per instantiation
-  const auto kern = ns_product_k<SIDE, MODE, PP, QP, DEEP, OUT>;
+  const auto kern = ns_product_k<SIDE, MODE, DEEP, OUT>;
   if (!attr_done) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS);
     if (e != hipSuccess) return e;
@@ -857,9 +829,9 @@ int rest_of(const NsTable& t, int* parts) {
   return rest;
 }
 
-template <int SIDE, int MODE, int PP, int QP, typename OUT>
+template <int SIDE, int MODE, typename OUT>
 hipError_t product_of(NsTable& t, const NsStep& p, hipStream_t st) {
-  constexpr int K = 16 * NsTile<SIDE, PP, QP, true>::KS;
+  constexpr int K = 16 * NsTile<SIDE, true>::KS;
   const auto parts_of = [&](const NsMatrix& q, int64_t most) { return (k_of<MODE>(q) / K + most - 1) / most; };
   int64_t most = 1 << 20;  // stages of a workgroup
   if constexpr (SIDE < 256) {
@@ -889,7 +861,7 @@ hipError_t product_of(NsTable& t, const NsStep& p, hipStream_t st) {
     return (int64_t)(q.tiles * q.parts + 7) / 8 * 8;
   });
   if constexpr (SIDE < 256) {
-    if (blocks <= 256) return launch_product<SIDE, MODE, PP, QP, true, OUT>(blocks, t, p, st);
+    if (blocks <= 256) return launch_product<SIDE, MODE, true, OUT>(blocks, t, p, st);
   } else {
     int parts;
     if (const int rest = rest_of<MODE>(t, &parts)) {
@@ -903,19 +875,19 @@ hipError_t product_of(NsTable& t, const NsStep& p, hipStream_t st) {
       r.parts = parts;
       const uint32_t more = spread(u, [](const NsMatrix& x) { return (int64_t)(x.tiles * x.parts + 7) / 8 * 8; });
       r.alone = u.first[u.count - 1];
-      return launch_product<SIDE, MODE, PP, QP, false, OUT>(more, u, p, st);
+      return launch_product<SIDE, MODE, false, OUT>(more, u, p, st);
     }
   }
-  return launch_product<SIDE, MODE, PP, QP, false, OUT>(blocks, t, p, st);
+  return launch_product<SIDE, MODE, false, OUT>(blocks, t, p, st);
 }
 // Tiles of 256 or 128 by how long the launch takes with them, 64 where there would be few of 128.
-template <int MODE, int PP, int QP, typename OUT = float>
+template <int MODE, typename OUT = float>
 hipError_t product(NsTable& t, int side, const NsStep& p, hipStream_t st) {
   NsTiles large[NS_TABLE + 1], middle[NS_TABLE];
   int64_t tiles = 0, k = 0;
   for (int i = 0; i < t.count; ++i) {
     large[i] = {tiles_of<MODE>(t.m[i], 256), (double)k_of<MODE>(t.m[i]) + (MODE == NS_POLY ? NS_COST_256_POLY : NS_COST_256)};
-    middle[i] = {tiles_of<MODE>(t.m[i], 128), (double)k_of<MODE>(t.m[i]) * 0.25 * (PP == 1 ? NS_COST_128_ONE : NS_COST_128)};
+    middle[i] = {tiles_of<MODE>(t.m[i], 128), (double)k_of<MODE>(t.m[i]) * 0.25 * NS_COST_128};
     tiles += middle[i].count;
     k = std::max(k, k_of<MODE>(t.m[i]));
   }
@@ -924,24 +896,22 @@ hipError_t product(NsTable& t, int side, const NsStep& p, hipStream_t st) {
     large[runs - 1].count -= rest;
     large[runs++] = {rest * parts, (double)k / parts + NS_COST_256_REST};
   }
-  if (side >= 256 && ns_span(large, runs) < ns_span(middle, t.count)) return product_of<256, MODE, PP, QP, OUT>(t, p, st);
-  if (side >= 128 && tiles >= (k < NS_LONG_K ? NS_TILES_128 : NS_TILES_128 / 2)) return product_of<128, MODE, PP, QP, OUT>(t, p, st);
-  return product_of<64, MODE, PP, QP, OUT>(t, p, st);
+  if (side >= 256 && ns_span(large, runs) < ns_span(middle, t.count)) return product_of<256, MODE, OUT>(t, p, st);
+  if (side >= 128 && tiles >= (k < NS_LONG_K ? NS_TILES_128 : NS_TILES_128 / 2)) return product_of<128, MODE, OUT>(t, p, st);
+  return product_of<64, MODE, OUT>(t, p, st);
 }
 
-// The products of one step.  FEW: one product each for A, A A and the last B X, two for the others.
-template <bool FEW>
+// The products of one step.
 hipError_t step_of(NsTable& t, int side, const NsStep& gram, const NsStep& poly, const NsStep& apply, bool last, int dt_dst, hipStream_t st) {
-  constexpr int ONE = FEW ? 1 : 2;
-  hipError_t e = product<NS_GRAM, ONE, ONE>(t, side, gram, st);
-  if (e == hipSuccess) e = product<NS_POLY, ONE, ONE>(t, side, poly, st);
+  hipError_t e = product<NS_GRAM>(t, side, gram, st);
+  if (e == hipSuccess) e = product<NS_POLY>(t, side, poly, st);
   if (e != hipSuccess) return e;
-  if (!last) return product<NS_APPLY, ONE, 2>(t, side, apply, st);
-  if (dt_dst == DT_BF16) return product<NS_LAST, ONE, ONE, bf16>(t, side, apply, st);
-  return product<NS_LAST, ONE, ONE>(t, side, apply, st);
+  if (!last) return product<NS_APPLY>(t, side, apply, st);
+  if (dt_dst == DT_BF16) return product<NS_LAST, bf16>(t, side, apply, st);
+  return product<NS_LAST>(t, side, apply, st);
 }
 
-hipError_t steps_of(NsTable& t, int side, int dt_src, int dt_dst, const NsRun& run, bool few, unsigned char* shared, hipStream_t st) {
+hipError_t steps_of(NsTable& t, int side, int dt_src, int dt_dst, const NsRun& run, unsigned char* shared, hipStream_t st) {
   const uint32_t parts = spread(t, [](const NsMatrix&) { return NS_NORM_PARTS; });
   if (dt_src == DT_BF16) ns_norm_k<bf16><<<parts, 256, 0, st>>>(t, run.mu, reinterpret_cast<unsigned*>(shared));
   else ns_norm_k<float><<<parts, 256, 0, st>>>(t, run.mu, reinterpret_cast<unsigned*>(shared));
@@ -950,8 +920,8 @@ hipError_t steps_of(NsTable& t, int side, int dt_src, int dt_dst, const NsRun& r
   if (!ns_scales(run.co, r, &s)) return hipErrorInvalidValue;
   const int growth = ns_growth(run.co);
   const uint32_t squares = spread(t, [](const NsMatrix& q) { return (int64_t)(q.n / 64) * (q.m / 64); });
-  if (dt_src == DT_BF16) ns_start_k<bf16><<<squares, 256, 0, st>>>(t, run.mu, run.eps, s.x, few);
-  else ns_start_k<float><<<squares, 256, 0, st>>>(t, run.mu, run.eps, s.x, few);
+  if (dt_src == DT_BF16) ns_start_k<bf16><<<squares, 256, 0, st>>>(t, run.mu, run.eps, s.x);
+  else ns_start_k<float><<<squares, 256, 0, st>>>(t, run.mu, run.eps, s.x);
   for (int k = 0; k < run.steps; ++k) {
     NsStep gram{}, poly{}, apply{};
     gram.shared = poly.shared = apply.shared = shared;
@@ -969,7 +939,7 @@ hipError_t steps_of(NsTable& t, int side, int dt_src, int dt_dst, const NsRun& r
     if (!ns_scales(run.co, r, &s)) return hipErrorInvalidValue;
     apply.out_scale = s.x;
     const bool last = k + 1 == run.steps;
-    const hipError_t e = (few ? step_of<true> : step_of<false>)(t, side, gram, poly, apply, last, dt_dst, st);
+    const hipError_t e = step_of(t, side, gram, poly, apply, last, dt_dst, st);
     if (e != hipSuccess) return e;
     if (!last)
       for (int i = 0; i < t.count; ++i) std::swap(t.m[i].xt, t.m[i].xt2);
@@ -1020,7 +990,7 @@ size_t ns_workspace(const NsItem* items, int count) {
 
 hipError_t newton_schulz(const NsItem* items, int count, int dt_src, int dt_dst, const NsRun& run, void* workspace, hipStream_t st) {
   hipError_t err = hipSuccess;
-  ns_launches(count, run.few, [&](int i, int64_t* r, int64_t* c) { *r = items[i].rows; *c = items[i].cols; }, [&](const int* which, int n, int side, bool large) {
+  ns_launches(count, false, [&](int i, int64_t* r, int64_t* c) { *r = items[i].rows; *c = items[i].cols; }, [&](const int* which, int n, int side, bool) {
     NsTable t{};
     unsigned char* ws = reinterpret_cast<unsigned char*>(workspace) + ns_shared_bytes(side);
     const int fill = side == NS_SMALL ? 32 : side;
@@ -1049,9 +1019,6 @@ hipError_t newton_schulz(const NsItem* items, int count, int dt_src, int dt_dst,
       q.xt2 = take((int64_t)q.n * q.m);
       q.a = take((int64_t)q.n * q.n);
       q.b = take((int64_t)q.n * q.n);
-      q.a_rest = reinterpret_cast<float*>(ws);
-      q.b_rest = q.a_rest + q.n;
-      ws += q.n * 8;
       q.norm_parts = reinterpret_cast<double*>(ws);
       ws += NS_NORM_PARTS * 8;
       q.small = reinterpret_cast<int*>(ws);
@@ -1059,7 +1026,7 @@ hipError_t newton_schulz(const NsItem* items, int count, int dt_src, int dt_dst,
     }
     if (err != hipSuccess) return;
     if (side == NS_SMALL) err = all_steps_of(t, dt_src, dt_dst, run, lds, st);
-    else err = steps_of(t, side, dt_src, dt_dst, run, large, reinterpret_cast<unsigned char*>(workspace), st);
+    else err = steps_of(t, side, dt_src, dt_dst, run, reinterpret_cast<unsigned char*>(workspace), st);
   });
   return err;
 }

@@ -56,41 +56,39 @@ constexpr int64_t NS_SIDE_MAX = 65536;
 constexpr int64_t NS_TOGETHER = int64_t(1) << 28;
 // Both sides of a matrix are filled up with zeros to a multiple of this, the largest tile its products can have: 256 where at least 64
 // such tiles cover it, else 128; 64 in launches that would have fewer than NS_FEW_TILES of 128 in the symmetric products, where filling up
-// costs more than larger tiles give (fp32 results: four matrices of odd sizes up to 1000 take 161 us with 64, 173 with 128; eight of
-// 512 x 2048 495 and 459).
+// costs more than larger tiles give (four matrices of odd sizes up to 1000 take 163 us with 64, 174 with 128; eight of 512 x 2048 496 and
+// 463).
 constexpr int64_t NS_FEW_TILES = 64;
 inline int ns_side(int64_t rows, int64_t cols) { return std::min(rows, cols) >= 1280 && rows * cols >= int64_t(64) * 256 * 256 ? 256 : 128; }
 // From how many tiles of 128 on a launch takes them rather than tiles of 64, half as many where k is long.  Below, workgroups are too few and
-// each one's chain of stages too long.  Layer 1024 wide, fp32 results: 880 us, 1087 with 64 throughout; two matrices of 512 x 512, bf16
-// results: 127 us, 223 with 128; four of 640 x 640: 158, with half as many tiles enough for any k 185; 1536 x 6000: 607, with half as
-// many never enough 690.
+// each one's chain of stages too long.  Layer 1024 wide: 877 us, 1091 with 64 throughout; two matrices of 512 x 512: 152 us, 247 with 128; four of
+// 640 x 640: 197 and 293; 1536 x 6000: 876, with half as many never enough 1001; eight of 512 x 2048: 463, with half as many enough for any k
+// 482.
 constexpr int64_t NS_TILES_128 = 128, NS_LONG_K = 1536;
 // Between tiles of 256 and 128 the shorter of the two launches, each tile taken to cost its k times its entries.  Tiles of 128 pass their
-// operands through LDS twice as often: what that costs, with one product, where LDS bounds the loop, and with more.  What a tile of 256
-// costs beside its k is its way in and out, which no second workgroup of the compute unit covers; in NS_POLY, which reads the tile's
-// entries of A and writes B's twice, more; and a shared tile's (below) the way of its sums through memory.  A layer 4096 wide, fp32 and bf16
-// results: 36.3 and 19.4 ms, with 128 throughout 39.1 and 23.0; three matrices of 2048 x 5632 and four of 2048 x 2048: 5.6 and 3.4 ms, with 256
-// for all launches of 192 such tiles or more 6.3 and 3.5.
-constexpr double NS_COST_128_ONE = 1.5, NS_COST_128 = 1.3, NS_COST_256 = 200.0, NS_COST_256_POLY = 800.0, NS_COST_256_REST = 1200.0;
+// operands through LDS twice as often: what that costs.  What a tile of 256 costs beside its k is its way in and out, which no second
+// workgroup of the compute unit covers; in NS_POLY, which reads the tile's entries of A and writes B's twice, more; and a shared tile's
+// (below) the way of its sums through memory.  A layer 4096 wide: 36.3 ms, with 128 throughout 39.1; three matrices of 2048 x 5632 and four of
+// 2048 x 2048: 5.6 ms, with 256 for all launches of 192 such tiles or more 6.3.
+constexpr double NS_COST_128 = 1.3, NS_COST_256 = 200.0, NS_COST_256_POLY = 800.0, NS_COST_256_REST = 1200.0;
 // Tiles' k ranges are shared between workgroups where that shortens a launch and leaves it no more workgroups than NS_SHARED_UNITS; no range
-// is shorter than so many stages.  Layer 1024 wide, fp32 results: 880 us, 973 without sharing, 972 with at most 256 workgroups, 912 with
+// is shorter than so many stages.  Layer 1024 wide: 880 us, 973 without sharing, 972 with at most 256 workgroups, 912 with
 // 512.  Stages: two matrices of 512 x 512 150 us, with 4 157; one of 256 x 1000 121, with 16 127.  The sums: 64 KB (128 x 128) each, and a
 // counter.
 constexpr int64_t NS_SHARED_UNITS = 304, NS_SHARED_STAGES = 8;
 constexpr size_t NS_SHARED_BYTES = NS_SHARED_UNITS * (4 + 128 * 128 * 4);
 // So are those of the tiles of 256 that would make a last round for at most half the compute units, by at most so many workgroups a tile and
-// where k is at least so long.  fp32 and bf16 results with and without: a layer 4096 wide, whose X takes 12 rounds and 16 tiles, 36.8 and 19.7
-// ms, 37.3 and 19.9; 4096 x 4200 4.20 and 2.30, 4.29 and 2.35.
+// where k is at least so long.  With and without: a layer 4096 wide, whose X takes 12 rounds and 16 tiles, 36.8 and 37.3 ms; 4096 x 4200 4.20 and
+// 4.29.
 constexpr int NS_REST_PARTS = 4;
 constexpr int64_t NS_REST_K = 2048;
 constexpr size_t NS_REST_BYTES = NS_SHARED_UNITS * 4 + size_t(256) * 256 * 256 * 4;
 inline size_t ns_shared_bytes(int side) { return side >= 256 ? NS_REST_BYTES : NS_SHARED_BYTES; }
 
-// Whose products are fewer for a bf16 result: smaller ones are bound by latency, and further off with them (two of 512 x 512: 127 us, with
-// all products 150; a layer 1024 wide: 0.58 and 0.88 ms; 4096 wide: 19.4 and 36.3).
+// For lists whose large matrices go apart from the others (see ns_launches): which are large.
 inline bool ns_large(int64_t rows, int64_t cols) { return std::min(rows, cols) >= 512; }
-// Among others they take all products, in those others' launches, while their short sides' squares times the long ones are less than this
-// together: launches of their own cost 100 us and more (1000 x 333, 129 x 257, 77 x 1300, 515 x 515: 161 us together, 294 apart).
+// Beside others they stay in those others' launches while their short sides' squares times the long ones are less than this together: launches of
+// their own cost 100 us and more (1000 x 333, 129 x 257, 77 x 1300, 515 x 515: 161 us together, 294 apart).
 constexpr int64_t NS_APART = int64_t(1) << 31;
 
 // How long the 256 compute units take over tiles, run by run, each tile to the unit that is free first.  Runs of equal ones: how many and how long.
@@ -141,17 +139,17 @@ inline bool ns_small(int64_t rows, int64_t cols) {
   return ns_small_lds(rows, cols) <= NS_SMALL_LDS && n * m <= 8 * NS_SMALL_TILES && n <= 2;
 }
 
-// Work space of one matrix: X, X^T before and after a step, A and B, two fp16 numbers to an entry, two diagonals, the sums
-// of its norm, and how far that is below eps.
+// Work space of one matrix: X, X^T before and after a step, A and B, two fp16 numbers to an entry, the sums of its norm, and how far that is
+// below eps.
 constexpr int NS_NORM_PARTS = 256;
 inline size_t ns_bytes(int64_t rows, int64_t cols) {
   const int side = ns_side(rows, cols);
   const int64_t n = ns_up(std::min(rows, cols), side), m = ns_up(std::max(rows, cols), side);
-  return (size_t)(3 * n * m + 2 * n * n) * 4 + (size_t)n * 8 + NS_NORM_PARTS * 8 + 16;
+  return (size_t)(3 * n * m + 2 * n * n) * 4 + NS_NORM_PARTS * 8 + 16;
 }
 // The launches of a list: launch(indexes, how many, tile side, large) for matrices that share them, those with the most work first (their tiles
 // then do not come last).  shape(i, &rows, &cols); matrices without entries are left out.
-// few: large ones apart, as they take fewer products.
+// few: large ones apart, for operators that treat them otherwise.  (All of this library's treat them alike and pass false.)
 template <class S, class F>
 inline void ns_launches(int count, bool few, S shape, F launch) {
   bool all_small = true, apart = true;
@@ -218,17 +216,16 @@ inline void ns_launches(int count, bool few, S shape, F launch) {
 template <class S>
 inline size_t ns_workspace_bytes(int count, S shape) {
   size_t most = 0;
-  for (bool few : {false, true})
-    ns_launches(count, few, shape, [&](const int* which, int n, int side, bool) {
-      size_t sum = 0;
-      if (side == NS_SMALL) return;
-      for (int i = 0; i < n; ++i) {
-        int64_t r, c;
-        shape(which[i], &r, &c);
-        sum += ns_bytes(r, c);
-      }
-      most = std::max(most, ns_shared_bytes(side) + sum);
-    });
+  ns_launches(count, false, shape, [&](const int* which, int n, int side, bool) {
+    size_t sum = 0;
+    if (side == NS_SMALL) return;
+    for (int i = 0; i < n; ++i) {
+      int64_t r, c;
+      shape(which[i], &r, &c);
+      sum += ns_bytes(r, c);
+    }
+    most = std::max(most, ns_shared_bytes(side) + sum);
+  });
   return most;
 }
 

@@ -1,7 +1,7 @@
 """What the bits of an orthogonalised result may depend on: neither the type of the result nor what else is handed in.
 
-Tolerances: a bf16 result is the fp32 one rounded, half of 2^-8 of each entry at most.  fp32 results: `any` of the orthogonalisations' tests,
-5 2^-21 a^5 sqrt(short side) absolutely after five steps."""
+A bf16 result is the fp32 one rounded to nearest, bit for bit.  Tolerance of fp32 results: `any` of the orthogonalisations' tests, 5 2^-21 a^5
+sqrt(short side) absolutely after five steps."""
 import math
 
 import pytest
@@ -45,6 +45,34 @@ def matrices(kind, r, c):
     if kind == "low rank":
         return torch.randn(r, 9, generator=g, device="cuda") @ torch.randn(9, c, generator=g, device="cuda") + 1e-3 * torch.randn(r, c, generator=g, device="cuda")
     return torch.randn(r, c, generator=g, device="cuda")
+
+
+KINDS = ["constant", "diagonal", "blocks", "equal magnitudes", "low rank", "random"]
+
+
+@pytest.mark.parametrize("shape", [(512, 512), (520, 1024), (2048, 640), (1500, 3000)])
+@pytest.mark.parametrize("kind", KINDS)
+def test_a_bf16_result_is_the_fp32_one_rounded(kind, shape):
+    import torch
+    import paper_2401_15207_amd as H
+    u = matrices(kind, *shape)
+    whole, half = torch.empty(shape, device="cuda"), torch.empty(shape, device="cuda", dtype=torch.bfloat16)
+    H.kernel_orthogonalize([u], [whole])
+    H.kernel_orthogonalize([u], [half])
+    assert (whole.double() - reference(u)).norm().item() <= 5 * 2.0 ** -21 * COEF[0] ** 5 * math.sqrt(min(shape))
+    assert torch.equal(half, whole.to(torch.bfloat16))
+
+
+@pytest.mark.parametrize("steps,coef", [(16, COEF), (1, COEF), (8, (2.0, -1.5, 0.5)), (5, (3.0, -6.0, 3.5))])
+def test_other_steps_and_coefficients_in_bf16(steps, coef):
+    import torch
+    import paper_2401_15207_amd as H
+    for kind in ("diagonal", "equal magnitudes", "random"):
+        u = matrices(kind, 640, 700)
+        whole, half = torch.empty_like(u), torch.empty(u.shape, device="cuda", dtype=torch.bfloat16)
+        H.kernel_orthogonalize([u], [whole], steps=steps, coefficients=coef)
+        H.kernel_orthogonalize([u], [half], steps=steps, coefficients=coef)
+        assert torch.equal(half, whole.to(torch.bfloat16)), kind
 
 
 def test_the_master_weights_do_not_depend_on_copies():
