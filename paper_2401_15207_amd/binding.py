@@ -620,6 +620,8 @@ class HiftModel:
     def step_scored(self, tokens, targets, group_id: int, d_logp=None, d_entropy=None):
         """The step on what score(tokens, targets, group_id) has just scored; d_logp, d_entropy: derivatives of the objective to descend by the scores
         (float32, in their shape)."""
+        assert tokens.dtype == self.torch.int32 and targets.dtype == self.torch.int32
+        assert tokens.is_cuda and targets.is_cuda and tokens.is_contiguous() and targets.is_contiguous()
         for name, d in (("d_logp", d_logp), ("d_entropy", d_entropy)):
             if d is not None and (d.dtype != self.torch.float32 or not d.is_cuda or not d.is_contiguous() or d.shape != targets.shape):
                 raise ValueError(f"{name}: contiguous float32 device values in the targets' shape {tuple(targets.shape)} expected")

@@ -16,25 +16,6 @@ TOL = 1e-5
 SGD = dict(kind="sgd", lr=1.0, momentum=0.0, eps=1e-8, weight_decay=0.0)
 
 
-def test_a_step_on_other_buffers_than_the_scored_ones_is_refused():
-    """The next batch's buffers by mistake: of the same sides, so only where they lie tells them from the scored ones."""
-    import torch
-    import paper_2401_15207_amd as H
-    wl = WORKLOADS["C1"]
-    _orc, gpu, theta0 = make_pair(wl, seed=21, opt=SGD)
-    tok, lab = to_dev(*make_batch(wl, 21, 1))
-    tok2, lab2 = to_dev(*make_batch(wl, 21, 2))
-    d = torch.full(lab.shape, -1e-3, device="cuda")
-    for other in ((tok2, lab), (tok, lab2), (tok2, lab2)):
-        gpu.score(tok, lab, 1)
-        with pytest.raises(H.HiftError):
-            gpu.step_scored(*other, 1, d)
-        assert np.array_equal(gpu.read_params(), theta0)
-        gpu.step_scored(tok, lab, 1, d)          # the scores are still there for the batch that they are of
-        assert not np.array_equal(gpu.read_params(), theta0)
-        gpu.write_params(0, gpu.n_units, theta0)
-
-
 def test_tokens_and_targets_of_other_types():
     import torch
     wl = WORKLOADS["C1"]
@@ -48,78 +29,3 @@ def test_tokens_and_targets_of_other_types():
             gpu.step_scored(*args, 1, d)
     gpu.step_scored(tok, lab, 1, d)
     assert not np.array_equal(gpu.read_params(), theta0)
-
-
-def test_derivatives_may_be_written_again_at_once():
-    """On the caller's stream, right after the call: the step reads what was there before."""
-    import torch
-    wl = dict(SMALL2, d_model=256, d_ffn=512, seq=128, batch=8, max_seq=128, n_layers=4)
-    after = []
-    for again in (False, True):
-        _orc, gpu, theta0 = make_pair(wl, seed=23, opt=SGD)
-        tok, lab = to_dev(*make_batch(wl, 23, 1))
-        dl, dh = torch.full(lab.shape, -1e-3, device="cuda"), torch.full(lab.shape, -1e-4, device="cuda")
-        for gid in range(gpu.k):
-            torch.cuda.synchronize()
-            gpu.score(tok, lab, gid)
-            gpu.step_scored(tok, lab, gid, dl, dh)
-            if again:
-                keep = [x.clone() for x in (dl, dh, tok, lab)]
-                for x in (dl, dh, tok, lab):
-                    x.fill_(7)
-                torch.cuda.synchronize()
-                for x, k in zip((dl, dh, tok, lab), keep):
-                    x.copy_(k)
-        after.append(gpu.read_params())
-        assert not np.array_equal(after[-1], theta0)
-    assert np.array_equal(*after)
-
-
-@pytest.mark.parametrize("wl", [WORKLOADS["C1"], SMALL1, SMALL2], ids=["C1", "enc", "rope"])
-def test_scores_of_a_model_with_adapters(wl):
-    """Those of the weights with the adapters merged into them; without a schedule, and no step follows."""
-    import torch
-    import paper_2401_15207_amd as H
-    orc, gpu, theta0, lora0 = _pair(wl, 4, 6.0, seed=24)
-    tok, lab = make_batch(wl, 24, 1)
-    seen = {}
-
-    def look(logits, rows):
-        seen["x"] = logits
-        seen["logp"], seen["entropy"] = O.token_scores(logits, rows)
-        return 0.0, np.zeros_like(logits)
-
-    cfg = model_config(wl)
-    O.loss_and_grad(cfg, O.lora_merge(cfg, theta0.astype(np.float64), lora0.astype(np.float64), 4, 6.0), tok, lab, objective=look)
-    dtok, dlab = to_dev(tok, lab)
-    out = gpu.score(dtok, dlab, top=2)
-    big = np.abs(seen["x"]).max() + 16
-    assert np.abs(out["logp"].cpu().numpy().reshape(-1) - seen["logp"]).max() <= TOL * big
-    assert np.abs(out["entropy"].cpu().numpy().reshape(-1) - seen["entropy"]).max() <= TOL * big
-    order = np.sort(seen["x"], axis=1)[:, ::-1][:, :2]
-    assert np.abs(np.take_along_axis(seen["x"], out["top_ids"].cpu().numpy().reshape(-1, 2), 1) - order).max() <= TOL * big
-    loss = orc.step(tok, lab)
-    assert abs(gpu.lora_step(dtok, dlab) - loss) <= TOL * abs(loss)       # scoring has left the adapters' step as it was
-    with pytest.raises(H.HiftError):
-        gpu.step_scored(dtok, dlab, 0, torch.zeros(lab.shape, device="cuda"))
-
-
-def test_work_space_that_is_none():
-    import torch
-    import paper_2401_15207_amd as H
-    u = torch.randn(300, 300, device="cuda")
-    out, n = torch.empty_like(u), H.kernel_orthogonalize_bytes([(300, 300)])
-    large = torch.empty(2 * n + 64, dtype=torch.uint8, device="cuda")
-    opt = dict(kind="muon", lr=1e-3, momentum=0.9)
-    for bad in (torch.empty(n, dtype=torch.uint8), large[::2], large[:2 * n].view(n, 2)[:, 0], large[:2 * n].view(2, n).t()):
-        with pytest.raises(ValueError):
-            H.kernel_orthogonalize([u], [out], workspace=bad)
-        with pytest.raises(ValueError):
-            H.kernel_muon(opt, [u.clone()], [u], [out], workspace=bad)
-    for bad in (large[1:], large[:n - 1]):       # not on 16 bytes, too small
-        with pytest.raises(H.HiftError):
-            H.kernel_orthogonalize([u], [out], workspace=bad)
-    H.kernel_orthogonalize([u], [out], workspace=large[16:])
-    want = torch.empty_like(u)
-    H.kernel_orthogonalize([u], [want])
-    assert torch.equal(out, want)
