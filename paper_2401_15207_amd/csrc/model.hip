@@ -351,8 +351,9 @@ struct hift_model {
   // run on gemm_lds_k whatever the vocabulary.  1936 tokens, width 1280, vocabulary 12466, rows of 12466 values (gemm_f32_k) and
   // of 12472: input gradient 728 and 131 us, weight gradient 542 and 66, product 104 and 79; errors against 64 bits over 44 models the same.
   int64_t logits_ld = 0;
-  // what hift_score leaves for hift_step_scored: the group it was made for (-1: none), the batch's sides, the scale, stats and entropies of the rows
-  int scored_group = -1, scored_batch = 0, scored_seq = 0;
+  // what hift_score leaves for hift_step_scored: the group it was made for (-1: none), the batch, the scale, stats and entropies of the rows
+  int scored_group = -1;
+  hift_batch scored_of{};
   float scored_scale = 1.f, *score_stats = nullptr, *score_entropy = nullptr;
   float *st_e = nullptr, *st_f = nullptr, *row_loss = nullptr, *part = nullptr;
   int32_t* tok_stamps = nullptr;  // which embeddings backward a token was last seen in, or null: the table's gradient is cleared instead
@@ -2038,13 +2039,14 @@ hift_status hift_score(hift_model* M, const hift_batch* bt, int32_t gid, const h
   }
   ST_TRY(forward(M, bt, ulo, s));
   M->scored_group = gid >= 0 ? gid : -1;
-  M->scored_batch = bt->batch; M->scored_seq = bt->seq; M->scored_scale = s->scale;
+  M->scored_of = *bt; M->scored_scale = s->scale;
   return HIFT_OK;
 }
 
 hift_status hift_step_scored(hift_model* M, const hift_batch* bt, int32_t gid, const float* d_logp, const float* d_entropy) {
   ST_TRY(check_step(M, bt, gid));
-  if (M->scored_group != gid || M->scored_batch != bt->batch || M->scored_seq != bt->seq)
+  const hift_batch& of = M->scored_of;
+  if (M->scored_group != gid || of.batch != bt->batch || of.seq != bt->seq || of.tokens != bt->tokens || of.labels != bt->labels)
     return fail(HIFT_ESTATE, "no scores of this batch and group: call hift_score for group %d first, and nothing that changes the model in between", gid);
   const ScoreGrad g{d_logp, d_entropy};
   return step_of(M, bt, gid, &g, nullptr);

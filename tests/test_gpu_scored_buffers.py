@@ -16,6 +16,25 @@ TOL = 1e-5
 SGD = dict(kind="sgd", lr=1.0, momentum=0.0, eps=1e-8, weight_decay=0.0)
 
 
+def test_a_step_on_other_buffers_than_the_scored_ones_is_refused():
+    """The next batch's buffers by mistake: of the same sides, so only where they lie tells them from the scored ones."""
+    import torch
+    import paper_2401_15207_amd as H
+    wl = WORKLOADS["C1"]
+    _orc, gpu, theta0 = make_pair(wl, seed=21, opt=SGD)
+    tok, lab = to_dev(*make_batch(wl, 21, 1))
+    tok2, lab2 = to_dev(*make_batch(wl, 21, 2))
+    d = torch.full(lab.shape, -1e-3, device="cuda")
+    for other in ((tok2, lab), (tok, lab2), (tok2, lab2)):
+        gpu.score(tok, lab, 1)
+        with pytest.raises(H.HiftError):
+            gpu.step_scored(*other, 1, d)
+        assert np.array_equal(gpu.read_params(), theta0)
+        gpu.step_scored(tok, lab, 1, d)          # the scores are still there for the batch that they are of
+        assert not np.array_equal(gpu.read_params(), theta0)
+        gpu.write_params(0, gpu.n_units, theta0)
+
+
 def test_tokens_and_targets_of_other_types():
     import torch
     wl = WORKLOADS["C1"]
