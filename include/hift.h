@@ -248,9 +248,10 @@ hift_status hift_step(hift_model* mdl, const hift_batch* batch, int32_t group_id
  * group_id -1: evaluation, at any time, also of models with adapters and without a schedule.  group_id of a group: the pass also keeps what
  * hift_step_scored needs, which then takes the step: backward from d_logp and d_entropy (device fp32 [rows]: derivatives of the caller's
  * objective, which the step descends, by the scores; NULL for zeros), and all else as hift_step, on the same batch (same buffers, still
- * unchanged) and group.  HIFT_ESTATE if the scores are not there: they are of other buffers, other sides or another group, or another pass or
- * step, hift_write_params, hift_checkpoint_load or hift_set_group_schedule has dropped them, or the step itself.  hift_step's loss is
- * d_logp = -1 / (rows with a target), d_entropy = 0. */
+ * unchanged) and group.  Queued on the compute stream; d_logp, d_entropy and the batch are read until that is done.  HIFT_ESTATE if the
+ * scores are not there: they are of other buffers, other sides or another group, or another pass or step, hift_write_params,
+ * hift_checkpoint_load or hift_set_group_schedule has dropped them, or the step itself.  hift_step's loss is d_logp = -1 / (rows with a
+ * target), d_entropy = 0. */
 typedef struct {
   float scale;
   int32_t top;

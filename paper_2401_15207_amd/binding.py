@@ -626,11 +626,13 @@ class HiftModel:
             if d is not None and (d.dtype != self.torch.float32 or not d.is_cuda or not d.is_contiguous() or d.shape != targets.shape):
                 raise ValueError(f"{name}: contiguous float32 device values in the targets' shape {tuple(targets.shape)} expected")
         b = Batch(tokens.data_ptr(), targets.data_ptr(), tokens.shape[0], tokens.shape[1])
-        self.compute_stream.wait_stream(self.torch.cuda.current_stream())
+        cur = self.torch.cuda.current_stream()
+        self.compute_stream.wait_stream(cur)
         for t in (tokens, targets, d_logp, d_entropy):
             if t is not None:
                 t.record_stream(self.compute_stream)
         _check(lib.hift_step_scored(self.h, C.byref(b), group_id, _ptr(d_logp), _ptr(d_entropy)))
+        cur.wait_stream(self.compute_stream)   # the caller may write the derivatives and the batch again
 
     def lora_param_count(self) -> int:
         n = _i64()

@@ -48,3 +48,28 @@ def test_tokens_and_targets_of_other_types():
             gpu.step_scored(*args, 1, d)
     gpu.step_scored(tok, lab, 1, d)
     assert not np.array_equal(gpu.read_params(), theta0)
+
+
+def test_derivatives_may_be_written_again_at_once():
+    """On the caller's stream, right after the call: the step reads what was there before."""
+    import torch
+    wl = dict(SMALL2, d_model=256, d_ffn=512, seq=128, batch=8, max_seq=128, n_layers=4)
+    after = []
+    for again in (False, True):
+        _orc, gpu, theta0 = make_pair(wl, seed=23, opt=SGD)
+        tok, lab = to_dev(*make_batch(wl, 23, 1))
+        dl, dh = torch.full(lab.shape, -1e-3, device="cuda"), torch.full(lab.shape, -1e-4, device="cuda")
+        for gid in range(gpu.k):
+            torch.cuda.synchronize()
+            gpu.score(tok, lab, gid)
+            gpu.step_scored(tok, lab, gid, dl, dh)
+            if again:
+                keep = [x.clone() for x in (dl, dh, tok, lab)]
+                for x in (dl, dh, tok, lab):
+                    x.fill_(7)
+                torch.cuda.synchronize()
+                for x, k in zip((dl, dh, tok, lab), keep):
+                    x.copy_(k)
+        after.append(gpu.read_params())
+        assert not np.array_equal(after[-1], theta0)
+    assert np.array_equal(*after)
