@@ -409,6 +409,8 @@ def _workspace(query, n, arr, workspace, stream):
         if stream is not None:
             stream.wait_stream(torch.cuda.current_stream())   # the memory may still be in use there
             workspace.record_stream(stream)
+    elif not workspace.is_cuda or not workspace.is_contiguous():
+        raise ValueError(f"workspace: contiguous device memory expected, not {tuple(workspace.shape)} {workspace.stride()} on {workspace.device}")
     return workspace, workspace.numel() * workspace.element_size()
 
 

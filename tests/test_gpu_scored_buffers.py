@@ -73,3 +73,24 @@ def test_derivatives_may_be_written_again_at_once():
         after.append(gpu.read_params())
         assert not np.array_equal(after[-1], theta0)
     assert np.array_equal(*after)
+
+
+def test_work_space_that_is_none():
+    import torch
+    import paper_2401_15207_amd as H
+    u = torch.randn(300, 300, device="cuda")
+    out, n = torch.empty_like(u), H.kernel_orthogonalize_bytes([(300, 300)])
+    large = torch.empty(2 * n + 64, dtype=torch.uint8, device="cuda")
+    opt = dict(kind="muon", lr=1e-3, momentum=0.9)
+    for bad in (torch.empty(n, dtype=torch.uint8), large[::2], large[:2 * n].view(n, 2)[:, 0], large[:2 * n].view(2, n).t()):
+        with pytest.raises(ValueError):
+            H.kernel_orthogonalize([u], [out], workspace=bad)
+        with pytest.raises(ValueError):
+            H.kernel_muon(opt, [u.clone()], [u], [out], workspace=bad)
+    for bad in (large[1:], large[:n - 1]):       # not on 16 bytes, too small
+        with pytest.raises(H.HiftError):
+            H.kernel_orthogonalize([u], [out], workspace=bad)
+    H.kernel_orthogonalize([u], [out], workspace=large[16:])
+    want = torch.empty_like(u)
+    H.kernel_orthogonalize([u], [want])
+    assert torch.equal(out, want)
