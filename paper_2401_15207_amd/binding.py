@@ -345,11 +345,11 @@ def _dtype_code(t) -> int:
     return code
 
 
-def _rows_of(name, t, dtype=None, shape=None, contiguous=False):
-    """t as a device matrix whose rows are contiguous; returns the distance between them."""
-    size = t.shape
-    if not t.is_cuda or len(size) != 2 or (dtype is not None and t.dtype is not dtype) or (shape is not None and size != shape):
-        raise ValueError(f"{name}: a device matrix{'' if shape is None else ' ' + str(tuple(shape))}{'' if dtype is None else f' of {dtype}'} "
+def _rows_of(name, t, dtype=None, shape=None, contiguous=False, device=None):
+    """t as a matrix on the device of that number (None: any) whose rows are contiguous; returns the distance between them."""
+    size, at = t.shape, t.get_device()
+    if at < 0 or (device is not None and at != device) or len(size) != 2 or (dtype is not None and t.dtype is not dtype) or (shape is not None and size != shape):
+        raise ValueError(f"{name}: a matrix on {'the device' if device is None else f'cuda:{device}'}{'' if shape is None else ' ' + str(tuple(shape))}{'' if dtype is None else f' of {dtype}'} "
                          f"expected, not {tuple(size)} of {t.dtype} on {t.device}")
     ld, step = t.stride()
     rows, cols = size
@@ -367,11 +367,11 @@ def _stream_of(t, stream):
     return torch._C._cuda_getCurrentRawStream(t.device.index) if t.is_cuda else 0
 
 
-def _row_values(name, t, count, dtype=torch.float32):
+def _row_values(name, t, count, device, dtype=torch.float32):
     if t is None:
         return None
-    if t.dtype is not dtype or t.numel() != count or not t.is_cuda or not t.is_contiguous():
-        raise ValueError(f"{name}: {count} contiguous values of {dtype} on the device expected")
+    if t.dtype is not dtype or t.numel() != count or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{name}: {count} contiguous values of {dtype} on cuda:{device} expected")
     return t.data_ptr()
 
 
@@ -379,38 +379,39 @@ def kernel_token_logprob(logits, vocab, targets, scale, logp, entropy, stats, to
     """logits: [rows, >= vocab] (rows contiguous, any distance apart); the outputs (fp32; top_ids int32) may be None where they are not wanted,
     targets (int32) where logp is; the number of alternatives is top_ids' second size."""
     st = _stream_of(logits, stream)
-    ld, (rows, width) = _rows_of("logits", logits), logits.shape
+    ld, (rows, width), at = _rows_of("logits", logits), logits.shape, logits.get_device()
     if vocab > width:
         raise ValueError(f"vocab {vocab}, but rows hold {width}")
     top = 0 if top_ids is None else top_ids.shape[1]
-    _check(lib.hift_kernel_token_logprob(_dtype_code(logits), rows, vocab, ld, logits.data_ptr(), _row_values("targets", targets, rows, torch.int32), scale,
-                                         top, _row_values("logp", logp, rows), _row_values("entropy", entropy, rows), _row_values("stats", stats, 2 * rows),
-                                         _row_values("top_logp", top_logp, rows * top) if top else None,
-                                         _row_values("top_ids", top_ids, rows * top, torch.int32) if top else None, st))
+    _check(lib.hift_kernel_token_logprob(_dtype_code(logits), rows, vocab, ld, logits.data_ptr(), _row_values("targets", targets, rows, at, torch.int32), scale,
+                                         top, _row_values("logp", logp, rows, at), _row_values("entropy", entropy, rows, at),
+                                         _row_values("stats", stats, 2 * rows, at), _row_values("top_logp", top_logp, rows * top, at) if top else None,
+                                         _row_values("top_ids", top_ids, rows * top, at, torch.int32) if top else None, st))
 
 
 def kernel_token_logprob_bwd(logits, vocab, targets, scale, stats, entropy, d_logp, d_entropy, dlogits, stream=None):
     """dlogits: like logits, or logits itself; entropy, d_logp, d_entropy may be None (see hift.h)."""
     st = _stream_of(logits, stream)
-    ld, ldd, (rows, width), out = _rows_of("logits", logits), _rows_of("dlogits", dlogits, logits.dtype), logits.shape, dlogits.shape
+    at, (rows, width), out = logits.get_device(), logits.shape, dlogits.shape
+    ld, ldd = _rows_of("logits", logits), _rows_of("dlogits", dlogits, logits.dtype, device=at)
     if vocab > width or vocab > out[1] or out[0] != rows:
         raise ValueError(f"vocab {vocab}, but logits are {tuple(logits.shape)} and dlogits {tuple(out)}")
-    _check(lib.hift_kernel_token_logprob_bwd(_dtype_code(logits), rows, vocab, ld, logits.data_ptr(), _row_values("targets", targets, rows, torch.int32), scale,
-                                             _row_values("stats", stats, 2 * rows), _row_values("entropy", entropy, rows),
-                                             _row_values("d_logp", d_logp, rows), _row_values("d_entropy", d_entropy, rows), ldd, dlogits.data_ptr(), st))
+    _check(lib.hift_kernel_token_logprob_bwd(_dtype_code(logits), rows, vocab, ld, logits.data_ptr(), _row_values("targets", targets, rows, at, torch.int32),
+                                             scale, _row_values("stats", stats, 2 * rows, at), _row_values("entropy", entropy, rows, at),
+                                             _row_values("d_logp", d_logp, rows, at), _row_values("d_entropy", d_entropy, rows, at), ldd, dlogits.data_ptr(), st))
 
 
-def _workspace(query, n, arr, workspace, stream):
-    """The caller's work space, or one from torch's allocator that it keeps until the stream is done with it."""
+def _workspace(query, n, arr, workspace, stream, device):
+    """The caller's work space, or one on the device of that number from torch's allocator, which keeps it until the stream is done with it."""
     if workspace is None:
         b = _sz()
         _check(query(n, arr, C.byref(b)))
-        workspace = torch.empty(max(b.value, 16), dtype=torch.uint8, device="cuda")
+        workspace = torch.empty(max(b.value, 16), dtype=torch.uint8, device=torch.device("cuda", device))
         if stream is not None:
-            stream.wait_stream(torch.cuda.current_stream())   # the memory may still be in use there
+            stream.wait_stream(torch.cuda.current_stream(device))   # the memory may still be in use there
             workspace.record_stream(stream)
-    elif not workspace.is_cuda or not workspace.is_contiguous():
-        raise ValueError(f"workspace: contiguous device memory expected, not {tuple(workspace.shape)} {workspace.stride()} on {workspace.device}")
+    elif workspace.get_device() != device or not workspace.is_contiguous():
+        raise ValueError(f"workspace: contiguous memory on cuda:{device} expected, not {tuple(workspace.shape)} {workspace.stride()} on {workspace.device}")
     return workspace, workspace.numel() * workspace.element_size()
 
 
@@ -427,35 +428,35 @@ MUON_COEFFICIENTS = (3.4445, -4.7750, 2.0315)
 
 def kernel_orthogonalize(src, dst, steps=5, coefficients=MUON_COEFFICIENTS, eps=1e-7, workspace=None, stream=None):
     """src, dst: lists of device matrices of the same shapes, all of one type each (float32 or bfloat16); dst may be src."""
-    st = (stream or torch.cuda.current_stream()).cuda_stream
     if len(src) != len(dst):
         raise ValueError(f"{len(src)} matrices, {len(dst)} results")
     if not src:
         return
+    st, at = _stream_of(src[0], stream), src[0].get_device()
     arr = (Matrix * len(src))()
     for i, (s, d) in enumerate(zip(src, dst)):
-        lds, ldd = _rows_of(f"src[{i}]", s, src[0].dtype), _rows_of(f"dst[{i}]", d, dst[0].dtype, s.shape)
+        lds, ldd = _rows_of(f"src[{i}]", s, src[0].dtype, device=at), _rows_of(f"dst[{i}]", d, dst[0].dtype, s.shape, device=at)
         arr[i] = Matrix(s.shape[0], s.shape[1], s.data_ptr(), lds, d.data_ptr(), ldd)
-    ws, n = _workspace(lib.hift_kernel_orthogonalize_bytes, len(src), arr, workspace, stream)
+    ws, n = _workspace(lib.hift_kernel_orthogonalize_bytes, len(src), arr, workspace, stream, at)
     _check(lib.hift_kernel_orthogonalize(_dtype_code(src[0]), _dtype_code(dst[0]), len(src), arr, steps, *coefficients, eps, _ptr(ws), n, st))
 
 
 def kernel_muon(opt: dict, master, grad, momentum, compute_copy=None, workspace=None, stream=None):
     """The update of matrices by HIFT_MUON: lists of contiguous float32 matrices, and of their bfloat16 copies (or None)."""
-    st = (stream or torch.cuda.current_stream()).cuda_stream
     n = len(master)
     if len(grad) != n or len(momentum) != n or (compute_copy is not None and len(compute_copy) != n):
         raise ValueError("as many gradients, momentum buffers and copies as matrices expected")
+    st, at = (_stream_of(master[0], stream), master[0].get_device()) if n else (0, 0)
     arr = (MuonMatrix * max(n, 1))()
     for i in range(n):
         w, cc = master[i], None if compute_copy is None else compute_copy[i]
         for name, t, dt in (("master", w, torch.float32), ("grad", grad[i], torch.float32), ("momentum", momentum[i], torch.float32),
                             ("compute_copy", cc, torch.bfloat16)):
             if t is not None:
-                _rows_of(f"{name}[{i}]", t, dt, w.shape, contiguous=True)
+                _rows_of(f"{name}[{i}]", t, dt, w.shape, contiguous=True, device=at)
         arr[i] = MuonMatrix(w.shape[0], w.shape[1], _ptr(w), _ptr(grad[i]), _ptr(momentum[i]), _ptr(cc))
     o = make_opt(opt)
-    ws, nb = _workspace(lib.hift_kernel_muon_bytes, n, arr, workspace, stream)
+    ws, nb = _workspace(lib.hift_kernel_muon_bytes, n, arr, workspace, stream, at) if n else (None, 0)
     _check(lib.hift_kernel_muon(C.byref(o), n, arr, _ptr(ws), nb, st))
 
 
