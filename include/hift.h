@@ -534,7 +534,7 @@ hift_status hift_kernel_cross_entropy(int32_t dtype, int64_t rows, int32_t V, vo
 
 /* Log probabilities of given tokens, entropy of each row and its most probable alternatives: what a loss on scored tokens (policy
  * gradients, preference losses, distillation of sampled answers) is formed from, and what a fine-tuned model would answer.
- * logits: device [rows, V], rows ld >= V apart (any alignment of whole elements); scale > 0: the reciprocal of the temperature.  With
+ * logits: device [rows, V], V at most 2^30, rows ld >= V apart (any alignment of whole elements); scale > 0: the reciprocal of the temperature.  With
  * z = scale * logits, m a row's largest z and S its sum of exp(z - m):
  *   logp[r] = (z[y] - m) - ln S for the row's target y = targets[r]; 0 for a row without one (a target outside [0, V))
  *   entropy[r] = - sum p ln p in nats

@@ -168,6 +168,7 @@ hipError_t cross_entropy_rows(int dt, int64_t rows, int V, int64_t ld, void* log
 hipError_t cross_entropy_mean(int64_t rows, const float* row_loss, float* loss_out, hipStream_t st);
 constexpr int LOGPROB_TOP_MAX = 32;
 constexpr int64_t LOGPROB_ROWS_MAX = int64_t(1) << 22;
+constexpr int LOGPROB_V_MAX = 1 << 30;  // positions in a row, and a launch's stride beyond them, are counted in 32 bits
 // Log probabilities of given tokens, the rows' entropies, the `top` most probable entries and what the gradient needs (logprob.hip).
 // targets (outside [0, V): none, logp 0), logp, entropy, stats [rows, 2], top_logp / top_ids [rows, top]: each may be null where it is not wanted.
 hipError_t token_logprob(int dt, int64_t rows, int V, int64_t ld, const void* logits, const int32_t* targets, float scale, int top, float* logp,

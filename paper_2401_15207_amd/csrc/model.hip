@@ -2029,6 +2029,7 @@ hift_status hift_score(hift_model* M, const hift_batch* bt, int32_t gid, const h
   if (gid >= 0) ST_TRY(check_step(M, bt, gid));
   else ST_TRY(check_batch(M, bt));
   const int V = M->cfg.arch == HIFT_ARCH_POSTLN_ENCODER ? M->cfg.n_classes : M->cfg.vocab;
+  if (V > LOGPROB_V_MAX) return fail(HIFT_EINVAL, "scores of at most %d entries a row", LOGPROB_V_MAX);
   if (!(s->scale > 0.f) || std::isinf(s->scale)) return fail(HIFT_EINVAL, "scale must be positive and finite");
   if (s->top < 0 || s->top > LOGPROB_TOP_MAX || s->top > V) return fail(HIFT_EINVAL, "top must be in [0, min(%d, %d)]", LOGPROB_TOP_MAX, V);
   if (s->top > 0 && (!s->top_logp || !s->top_ids)) return fail(HIFT_EINVAL, "top needs top_logp and top_ids");
@@ -2726,7 +2727,7 @@ hift_status hift_kernel_cross_entropy(int32_t dtype, int64_t rows, int32_t V, vo
 namespace {
 hift_status check_logits(int32_t dtype, int64_t rows, int32_t V, int64_t ld, const void* logits, float scale) {
   if (dtype != HIFT_F32 && dtype != HIFT_BF16) return fail(HIFT_EINVAL, "dtype unknown");
-  if (rows < 0 || V < 1 || ld < V) return fail(HIFT_EINVAL, "bad shape: %lld rows of %d entries, %lld apart", (long long)rows, V, (long long)ld);
+  if (rows < 0 || V < 1 || V > LOGPROB_V_MAX || ld < V) return fail(HIFT_EINVAL, "bad shape: %lld rows of %d entries, %lld apart", (long long)rows, V, (long long)ld);
   if (rows > LOGPROB_ROWS_MAX) return fail(HIFT_EINVAL, "more than %lld rows in one call", (long long)LOGPROB_ROWS_MAX);
   if (!(scale > 0.f) || std::isinf(scale)) return fail(HIFT_EINVAL, "scale must be positive and finite");
   if (rows > 0 && !logits) return fail(HIFT_EINVAL, "logits are null");
