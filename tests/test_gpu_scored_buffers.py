@@ -75,6 +75,35 @@ def test_derivatives_may_be_written_again_at_once():
     assert np.array_equal(*after)
 
 
+@pytest.mark.parametrize("wl", [WORKLOADS["C1"], SMALL1, SMALL2], ids=["C1", "enc", "rope"])
+def test_scores_of_a_model_with_adapters(wl):
+    """Those of the weights with the adapters merged into them; without a schedule, and no step follows."""
+    import torch
+    import paper_2401_15207_amd as H
+    orc, gpu, theta0, lora0 = _pair(wl, 4, 6.0, seed=24)
+    tok, lab = make_batch(wl, 24, 1)
+    seen = {}
+
+    def look(logits, rows):
+        seen["x"] = logits
+        seen["logp"], seen["entropy"] = O.token_scores(logits, rows)
+        return 0.0, np.zeros_like(logits)
+
+    cfg = model_config(wl)
+    O.loss_and_grad(cfg, O.lora_merge(cfg, theta0.astype(np.float64), lora0.astype(np.float64), 4, 6.0), tok, lab, objective=look)
+    dtok, dlab = to_dev(tok, lab)
+    out = gpu.score(dtok, dlab, top=2)
+    big = np.abs(seen["x"]).max() + 16
+    assert np.abs(out["logp"].cpu().numpy().reshape(-1) - seen["logp"]).max() <= TOL * big
+    assert np.abs(out["entropy"].cpu().numpy().reshape(-1) - seen["entropy"]).max() <= TOL * big
+    order = np.sort(seen["x"], axis=1)[:, ::-1][:, :2]
+    assert np.abs(np.take_along_axis(seen["x"], out["top_ids"].cpu().numpy().reshape(-1, 2), 1) - order).max() <= TOL * big
+    loss = orc.step(tok, lab)
+    assert abs(gpu.lora_step(dtok, dlab) - loss) <= TOL * abs(loss)       # scoring has left the adapters' step as it was
+    with pytest.raises(H.HiftError):
+        gpu.step_scored(dtok, dlab, 0, torch.zeros(lab.shape, device="cuda"))
+
+
 def test_work_space_that_is_none():
     import torch
     import paper_2401_15207_amd as H
