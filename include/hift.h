@@ -552,7 +552,8 @@ hift_status hift_kernel_token_logprob(int32_t dtype, int64_t rows, int32_t V, in
  *   scale (d_logp (1(j = y) - p_j) - d_entropy p_j (ln p_j + entropy))
  * (d_logp counts for rows with a target only; the alternatives have no gradient).  stats, entropy: as the forward call left them (entropy may
  * be NULL where d_entropy is); d_logp, d_entropy: device fp32 [rows], NULL for zeros.  dlogits: device [rows, V] of the logits' type, rows
- * ldd apart; may be the logits themselves (ldd = ld).  Masked entries and rows of nothing else receive 0; columns from V on are not written. */
+ * ldd apart; may be the logits themselves (ldd = ld), and may not overlap them otherwise.  Masked entries other than the row's target, and rows of
+ * nothing else, receive 0; a masked target receives scale d_logp, by the formula with p = 0.  Columns from V on are not written. */
 hift_status hift_kernel_token_logprob_bwd(int32_t dtype, int64_t rows, int32_t V, int64_t ld, const void* logits, const int32_t* targets,
                                           float scale, const float* stats, const float* entropy, const float* d_logp,
                                           const float* d_entropy, int64_t ldd, void* dlogits, void* stream);
