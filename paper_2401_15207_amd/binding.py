@@ -600,11 +600,17 @@ class HiftModel:
         _check(lib.hift_step(self.h, C.byref(b), group_id, C.byref(loss) if want_loss else None))
         return loss.value if want_loss else None
 
+    def _check_scored(self, tokens, targets):
+        assert tokens.dtype == self.torch.int32 and targets.dtype == self.torch.int32
+        assert tokens.is_cuda and targets.is_cuda and tokens.is_contiguous() and targets.is_contiguous()
+        rows = tokens.shape[:1] if self.cfg["arch"] == 1 else tokens.shape      # what is scored: sequences, or their positions
+        if tokens.dim() != 2 or targets.shape != rows:
+            raise ValueError(f"targets: {tuple(rows)} expected for tokens {tuple(tokens.shape)}, not {tuple(targets.shape)}")
+
     def score(self, tokens, targets, group_id: int = -1, temperature: float = 1.0, top: int = 0):
         """Log probabilities of targets (as labels in step: [B,S] or [B], -1 for none), entropies and, with top > 0, the most probable ids and their
         log probabilities of every row, as device tensors (ready on torch's current stream).  group_id: of a step_scored to follow."""
-        assert tokens.dtype == self.torch.int32 and targets.dtype == self.torch.int32
-        assert tokens.is_cuda and targets.is_cuda and tokens.is_contiguous() and targets.is_contiguous()
+        self._check_scored(tokens, targets)
         f = dict(device=tokens.device, dtype=self.torch.float32)
         out = {"logp": self.torch.empty(targets.shape, **f), "entropy": self.torch.empty(targets.shape, **f)}
         if top:
@@ -623,8 +629,7 @@ class HiftModel:
     def step_scored(self, tokens, targets, group_id: int, d_logp=None, d_entropy=None):
         """The step on what score(tokens, targets, group_id) has just scored; d_logp, d_entropy: derivatives of the objective to descend by the scores
         (float32, in their shape)."""
-        assert tokens.dtype == self.torch.int32 and targets.dtype == self.torch.int32
-        assert tokens.is_cuda and targets.is_cuda and tokens.is_contiguous() and targets.is_contiguous()
+        self._check_scored(tokens, targets)
         for name, d in (("d_logp", d_logp), ("d_entropy", d_entropy)):
             if d is not None and (d.dtype != self.torch.float32 or not d.is_cuda or not d.is_contiguous() or d.shape != targets.shape):
                 raise ValueError(f"{name}: contiguous float32 device values in the targets' shape {tuple(targets.shape)} expected")

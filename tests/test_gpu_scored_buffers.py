@@ -50,6 +50,26 @@ def test_tokens_and_targets_of_other_types():
     assert not np.array_equal(gpu.read_params(), theta0)
 
 
+@pytest.mark.parametrize("wl", [WORKLOADS["C1"], SMALL1], ids=["C1", "enc"])
+def test_as_many_targets_as_rows(wl):
+    """The scores are written in the targets' shape: one each position of a decoder, one each sequence of an encoder."""
+    import torch
+    _orc, gpu, theta0 = make_pair(wl, seed=25, opt=SGD)
+    tok, lab = to_dev(*make_batch(wl, 25, 1))
+    d = torch.full(lab.shape, -1e-3, device="cuda")
+    gpu.score(tok, lab, 1)
+    for bad in (lab.reshape(-1)[:1].contiguous(), lab[:1].contiguous(), torch.zeros(tok.shape[0], tok.shape[1] + 1, device="cuda", dtype=torch.int32),
+                torch.zeros(tok.shape if lab.dim() == 1 else tok.shape[:1], device="cuda", dtype=torch.int32), lab.unsqueeze(0)):
+        with pytest.raises(ValueError):
+            gpu.score(tok, bad, 1)
+        with pytest.raises(ValueError):
+            gpu.step_scored(tok, bad, 1, torch.zeros(bad.shape, device="cuda"))
+    with pytest.raises(ValueError):
+        gpu.score(tok.reshape(-1), lab, 1)
+    gpu.step_scored(tok, lab, 1, d)      # what was scored is still there
+    assert not np.array_equal(gpu.read_params(), theta0)
+
+
 def test_derivatives_may_be_written_again_at_once():
     """On the caller's stream, right after the call: the step reads what was there before."""
     import torch
