@@ -97,7 +97,7 @@ struct RowOf {
   }
 };
 
-// Within a row of 16 lanes by DPP, across rows by lane swaps: all 64 lanes receive the result.  `eighth` receives what the 2^STEPS lanes
+// Within a row of 16 lanes by DPP, across rows by lane swaps: all 64 lanes receive the result.  `group` receives what the 2^STEPS lanes
 // around each have by themselves.
 template <int CTRL>
 __device__ __forceinline__ float dpp(float v) {
@@ -159,8 +159,9 @@ struct Sums {
 };
 
 // One workgroup a row, one pass over it.  Every wavefront forms its sums against its own largest entry; the first one joins them.  Far rows take
-// another pass, against the row's largest.
-// Bound: the logits' way from memory once rows are many (4096 x 50272 fp32 139 us, 5.9 TB/s; 2048 x 32000 bf16 with 8 alternatives 31 us, 4.2
+// another pass, against the row's largest (that is all that a mask costs which is not -inf, and only where a row holds nothing else: half of each row at
+// the type's lowest value, 2048 x 32000 bf16, 35 us, without 34).
+// Bound: the logits' way from memory once rows are many (4096 x 50272 fp32 138 us, 6.0 TB/s; 2048 x 32000 bf16 with 8 alternatives 32 us, 4.1
 // TB/s: one exponential and two multiply-adds an entry take as long as its two bytes); the chain of loads, reductions and barriers for one
 // (1 x 32000 with 20 alternatives 6 us).  Rows are not split over workgroups: one of 128000 takes 13 us, a launch that joins parts 4 more.
 // The alternatives: the k-th largest of the maxima of 64 disjoint parts of the row is at most its k-th largest entry, and few entries are
@@ -376,7 +377,7 @@ struct LogprobBwdArgs {
 constexpr int BWD_THREADS = 256;
 
 // `parts` workgroups a row.  An element is read and written by one thread, so the gradient may take the logits' place.
-// Bound: the way from and to memory (2048 x 32000 bf16 52 us, 5.1 TB/s; 1000 x 50265 41 us, 4.8 TB/s).
+// Bound: the way from and to memory (2048 x 32000 bf16 52 us, 5.0 TB/s; 1000 x 50265 42 us, 4.8 TB/s).
 template <typename T, int E>
 __global__ void __launch_bounds__(BWD_THREADS) logprob_bwd_k(LogprobBwdArgs a) {
   const int64_t r = blockIdx.x / a.parts;
@@ -417,9 +418,9 @@ __global__ void __launch_bounds__(BWD_THREADS) logprob_bwd_k(LogprobBwdArgs a) {
 template <typename T>
 hipError_t launch_logprob(int64_t rows, const LogprobArgs& a, hipStream_t st) {
   // Threads so that one batch of a thread's loads, four pieces, takes most of a row.  Few rows: the more threads the shorter the chain (1 x
-  // 1000 entries in bf16: 4.4 us with 256, 5.0 with 64; 256 x 10000: 5.4 with 512, 7.2 with 256; 64 x 32000: 6.7 with 1024, 8.9 with 512;
-  // but 64 x 16500: 5.9 with 512, 6.9 with 1024).  Many rows fill the chip by themselves, and joining the wavefronts' parts costs more
-  // (2048 x 1000: 6.8 with 64, 8.2 with 256; 2048 x 8000: 11.1 with 256, 15.5 with 512; 2048 x 32000: 32 with 512, 49 with 1024).
+  // 1000 entries in bf16: 4.5 us with 256, 5.1 with 64; 256 x 10000: 5.8 with 512, 7.2 with 256; 64 x 32000: 7.3 with 1024, 9.3 with 512;
+  // but 64 x 16300: 5.8 with 512, 7.2 with 1024).  Many rows fill the chip by themselves, and joining the wavefronts' parts costs more
+  // (2048 x 1000: 6.9 with 64, 8.4 with 256; 2048 x 8000: 11.3 with 256, 16.1 with 512; 2048 x 32000: 32 with 512, 37 with 1024).
   const int pieces = a.V / (16 / (int)sizeof(T));
   const uint32_t grid = (uint32_t)rows;
 #define ROW(NT) logprob_k<T, NT><<<grid, NT, 0, st>>>(a)
@@ -434,8 +435,8 @@ hipError_t launch_logprob(int64_t rows, const LogprobArgs& a, hipStream_t st) {
 template <typename T>
 hipError_t launch_logprob_bwd(int64_t rows, LogprobBwdArgs a, hipStream_t st) {
   constexpr int E = 16 / (int)sizeof(T);
-  // pieces of 16 bytes where a row of the gradient lies in them as its row of logits does (2048 x 32000 in bf16: 43 us, element by element
-  // 126; in fp32 95 and 160)
+  // pieces of 16 bytes where a row of the gradient lies in them as its row of logits does (2048 x 32000 in bf16: 44 us, element by element
+  // 127; in fp32 96 and 163)
   const uintptr_t off = reinterpret_cast<uintptr_t>(a.logits) - reinterpret_cast<uintptr_t>(a.dlogits);
   const bool alike = (off & 15) == 0 && (rows == 1 || (a.ld - a.ldd) * (int64_t)sizeof(T) % 16 == 0);
   const int per = BWD_THREADS * (alike ? E : 1) * 4;
