@@ -374,8 +374,8 @@ def work(case):
         seen = case["history"] + 1 if case["nested"] else case["history"] / 2
         masks = {"none": 0, "one": 1, "rows": rows}[case["mask"]] * vocab / 8
         history = 4.0 * rows if case["nested"] else 4.0 * rows * seen
-        # allowed tokens lie scattered, so every line of the logits is read (and of their gradient)
-        return {"bytes": rows * vocab * size * (3.0 if case["backward"] else 2.0) + masks + history + (4.0 * vocab if case["bias"] and not case["backward"] else 0), "flops": 6.0 * rows * vocab}
+        # forward every line of the logits is read, since allowed tokens lie scattered; the gradient needs the logits of seen tokens alone
+        return {"bytes": rows * vocab * size * 2.0 + (rows * min(seen, vocab) * size if case["backward"] else 0) + masks + history + (4.0 * vocab if case["bias"] and not case["backward"] else 0), "flops": 6.0 * rows * vocab}
     tokens, heads, kv, hd = tokens_of(case), case["heads"], case["kv_heads"], case["head_dim"]
     rows = sum(n for _, n in tokens)
     if case["op"] == "append":
