@@ -592,6 +592,94 @@ hift_status hift_kernel_muon_bytes(int32_t count, const hift_muon_matrix* matric
 hift_status hift_kernel_muon(const hift_opt* opt, int32_t count, const hift_muon_matrix* matrices, void* workspace, size_t workspace_bytes,
                              void* stream);
 
+/* ---- answers: what a model writes while it is trained on what it wrote --------------------
+ *
+ * Rotary positions.  Pair i of a head turns by position * rate_i, rate_i = base^(-2 i / rot), i < rot / 2; for contexts longer than those a model was
+ * trained on the rates are scaled, factor = how many times longer:
+ *   HIFT_ROTARY_LINEAR  rate_i / factor
+ *   HIFT_ROTARY_BASE    base factor^(rot / (rot - 2)) instead of base: the slowest pair turns factor times slower, the fastest as before (rot > 2)
+ *   HIFT_ROTARY_PARTS   with turns_i = trained rate_i / (2 pi), the turns within `trained` positions: rate_i (k + (1 - k) / factor),
+ *                       k = (turns_i - slow) / (fast - slow) kept within [0, 1]: pairs of more than `fast` turns stay, those below `slow` are slowed
+ * amplitude: what cos and sin are multiplied with (1 usual).  Fields that a scaling does not name are not read.
+ * hift_kernel_rotary_table: cos_sin device fp32 [count, rot / 2, 2] = amplitude (cos, sin) of positions first .. first + count - 1, angles formed in
+ * 64 bits and rounded once.  rot even, 2 .. 256; base 1 .. 1e18, factor 1 .. 1e9; 0 <= first, first + count <= 2^30. */
+enum { HIFT_ROTARY_PLAIN = 0, HIFT_ROTARY_LINEAR = 1, HIFT_ROTARY_BASE = 2, HIFT_ROTARY_PARTS = 3 };
+typedef struct {
+  int32_t rot, scaling;
+  double base, factor, trained, slow, fast, amplitude;
+} hift_rotary;
+hift_status hift_kernel_rotary_table(const hift_rotary* rotary, int64_t first, int64_t count, float* cos_sin, void* stream);
+
+/* Rotation of rows of heads that lie side by side (q, k, or q | k of a fused projection): with (c, s) of the row's position, x1 and x2 of pair i
+ *   y1 = x1 c - x2 s, y2 = x2 c + x1 s;   backward != 0: the adjoint, with -s for s (x is then the gradient of y, y receives that of x)
+ * layout HIFT_ROTARY_HALVES: pair i is columns (i, i + rot / 2) of its head; HIFT_ROTARY_PAIRS: (2 i, 2 i + 1).  Columns of a head from rot on are copied.
+ * x, y: device, rows ldx / ldy >= heads * head_dim elements apart, of any alignment of whole elements (16-byte pieces are faster); y may be x
+ * (ldy = ldx) and may not overlap it otherwise; nothing behind the heads is written.  cos_sin: device fp32 [table_rows, rot / 2, 2], 8-byte aligned.  positions:
+ * device int32 [rows], or NULL for row % seq (1 <= seq <= table_rows); a position outside the table is read as the nearest in it.  Formed in fp32, rounded
+ * once. */
+enum { HIFT_ROTARY_HALVES = 0, HIFT_ROTARY_PAIRS = 1 };
+hift_status hift_kernel_rotary(int32_t dtype, int32_t layout, int32_t backward, int64_t rows, int32_t heads, int32_t head_dim, int32_t rot, const void* x,
+                               int64_t ldx, void* y, int64_t ldy, const int32_t* positions, int32_t seq, const float* cos_sin, int64_t table_rows, void* stream);
+
+/* A paged cache of one layer's keys and values.  Page n of k (of v) is [kv_heads][page][head_dim], page_stride elements behind page n - 1, n < n_pages.
+ * Token t of sequence s lies in slot t % page of page pages[s * pages_ld + t / page], t < max_pages * page.  lengths[s]: the tokens that the sequence had
+ * before the call's; the caller adds the new ones when all layers are done.  Arrays are device memory; what pages and lengths hold is not
+ * checked on the host: a page number outside [0, n_pages) is a page that is not there (a window's old pages may be given back and set to -1) -- what
+ * would be written there is dropped and what would be read is not seen -- and lengths are kept within [0, max_pages * page].
+ * page: a power of two, 16 .. 65536; head_dim: at most 128, whole 16-byte pieces; k, v 16-byte aligned, page_stride whole 16-byte pieces.
+ * A call's new rows: rows [starts[s], starts[s + 1]) belong to sequence s (starts: device int32 [sequences + 1], rising, within [0, rows]) and are its
+ * tokens lengths[s], lengths[s] + 1, ..; max_new: at least as many as any sequence brings (rows beyond it are left out).  Rows that belong to no sequence are neither
+ * read nor written.  No device array is read on the host, so calls can be captured into a graph and replayed while lengths and pages grow. */
+typedef struct {
+  int32_t dtype, kv_heads, head_dim, page, n_pages, sequences, max_pages;
+  int64_t page_stride, pages_ld;
+  void *k, *v;
+  const int32_t *pages, *lengths;
+} hift_cache;
+/* qkv: rows of a fused projection, q of all heads | k | v of the kv_heads, ld elements apart.  k is rotated by its token's position and written to its
+ * page with v; q is rotated to q_out (rows ldq apart; the q columns of qkv itself with ldq = ld; NULL: q is not wanted).  layout, rot, cos_sin, table_rows
+ * as for hift_kernel_rotary; rot 0: nothing turns.  qkv, q_out: the cache's type, 16-byte aligned, rows whole 16-byte pieces apart. */
+hift_status hift_kernel_cache_append(const hift_cache* cache, int64_t rows, const int32_t* starts, int32_t max_new, int32_t heads, int32_t layout, int32_t rot,
+                                     const float* cos_sin, int64_t table_rows, const void* qkv, int64_t ld, void* q_out, int64_t ldq, void* stream);
+/* out[row] = softmax(scale q k^T) v of every query head over the keys that the row sees: tokens of its sequence up to its own position -- its own and
+ * the other new ones are in the cache already (hift_kernel_cache_append) -- and, with window > 0, the last `window` of them.  heads: a multiple of kv_heads; query
+ * head h reads key head h / (heads / kv_heads).  q, out: device, rows [heads * head_dim], ldq / ldo apart, the cache's type, 16-byte aligned, rows whole
+ * 16-byte pieces apart; out may be q (ldo = ldq).  lse: device fp32 [rows, heads] or NULL: log2 of the sum of the exponentials of the scaled scores.
+ * A row that sees nothing: out 0, lse -inf.  Sums and statistics are fp32; bf16 caches: unnormalised probabilities are rounded to bf16 for the
+ * product with v, as in hift_kernel_attention_fwd.  max_length: at least as many as any sequence has with its new tokens; it sets how the keys are split over
+ * workgroups, and a longer sequence only takes longer.  workspace: device, 16-byte aligned, hift_kernel_attention_paged_bytes, NULL where that is 0; free
+ * again once the call's work on the stream is done; calls that may run at the same time (two streams, two graphs) need one each.
+ * No sum depends on timing: the same call gives the same bits. */
+hift_status hift_kernel_attention_paged_bytes(const hift_cache* cache, int64_t rows, int32_t max_new, int64_t max_length, int32_t heads, int32_t window, size_t* bytes);
+hift_status hift_kernel_attention_paged(const hift_cache* cache, int64_t rows, const int32_t* starts, int32_t max_new, int64_t max_length, int32_t heads,
+                                        int32_t window, float scale, const void* q, int64_t ldq, void* out, int64_t ldo, float* lse, void* workspace,
+                                        size_t workspace_bytes, void* stream);
+
+/* Logits as a sampler wants them.  With n = how often row r has seen token j, x = logits[r, j]:
+ *   out[r, j] = (n > 0 ? (x > 0 ? x / repetition : x repetition) - presence : x) - frequency n + bias[j];   -inf where `allowed` has no bit for j
+ * tokens: device int32 [n_tokens]; row r has seen tokens[begin[r]] .. tokens[end[r] - 1] (device int64 [rows], kept within [0, n_tokens]; ranges may overlap, as
+ * the positions of one text do; ids outside [0, V) count for nothing); NULL: nothing was seen.  bias: device fp32 [V], rows ld_bias apart, or one for all rows
+ * with ld_bias 0; NULL: none.  allowed: device, bit j % 32 of word j / 32, rows ld_allowed words apart, or one for all with ld_allowed 0; NULL: all are.
+ * logits, out: device [rows, V] of one type, rows ld / ldo >= V apart, any alignment of whole elements; out may be logits (ldo = ld), and may not
+ * overlap them otherwise.  Formed in fp32 (a division by repetition as a product with its reciprocal), rounded once.  repetition within [2^-60, 2^60], 1 for none;
+ * presence, frequency finite, 0 for none.  hift_kernel_token_logprob reads the result, whole rows of -inf too.
+ * hift_kernel_adjust_logits_bwd: the gradient of what was formed from out (d_out) with respect to the logits: d_out / repetition or d_out repetition for seen
+ * tokens, d_out for others, 0 where `allowed` has no bit.  logits: as the forward call read them.  d_logits may be d_out (with its rows). */
+typedef struct {
+  const int32_t* tokens;
+  int64_t n_tokens;
+  const int64_t *begin, *end;
+  float repetition, presence, frequency;
+  const float* bias;
+  int64_t ld_bias;
+  const uint32_t* allowed;
+  int64_t ld_allowed;
+} hift_adjust;
+hift_status hift_kernel_adjust_logits(int32_t dtype, int64_t rows, int32_t V, int64_t ld, const void* logits, const hift_adjust* by, int64_t ldo, void* out,
+                                      void* stream);
+hift_status hift_kernel_adjust_logits_bwd(int32_t dtype, int64_t rows, int32_t V, int64_t ld, const void* logits, const hift_adjust* by, int64_t ldd_out,
+                                          const void* d_out, int64_t ldd, void* d_logits, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

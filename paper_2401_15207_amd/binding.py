@@ -70,6 +70,20 @@ class MuonMatrix(C.Structure):
                 ("compute_copy", C.c_void_p)]
 
 
+class Rotary(C.Structure):
+    _fields_ = [("rot", C.c_int32), ("scaling", C.c_int32)] + [(n, C.c_double) for n in ("base", "factor", "trained", "slow", "fast", "amplitude")]
+
+
+class Cache(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "kv_heads", "head_dim", "page", "n_pages", "sequences", "max_pages")] + \
+               [("page_stride", C.c_int64), ("pages_ld", C.c_int64)] + [(n, C.c_void_p) for n in ("k", "v", "pages", "lengths")]
+
+
+class Adjust(C.Structure):
+    _fields_ = [("tokens", C.c_void_p), ("n_tokens", C.c_int64), ("begin", C.c_void_p), ("end", C.c_void_p), ("repetition", C.c_float), ("presence", C.c_float),
+                ("frequency", C.c_float), ("bias", C.c_void_p), ("ld_bias", C.c_int64), ("allowed", C.c_void_p), ("ld_allowed", C.c_int64)]
+
+
 lib.hift_last_error.restype = C.c_char_p
 _vp, _i32, _i64, _u64, _sz = C.c_void_p, C.c_int32, C.c_int64, C.c_uint64, C.c_size_t
 _P = C.POINTER
@@ -137,6 +151,13 @@ _SIGS = {
     "hift_kernel_orthogonalize": [_i32, _i32, _i32, _P(Matrix), _i32, C.c_double, C.c_double, C.c_double, C.c_float, _vp, _sz, _vp],
     "hift_kernel_muon_bytes": [_i32, _P(MuonMatrix), _P(_sz)],
     "hift_kernel_muon": [_P(Opt), _i32, _P(MuonMatrix), _vp, _sz, _vp],
+    "hift_kernel_rotary_table": [_P(Rotary), _i64, _i64, _vp, _vp],
+    "hift_kernel_rotary": [_i32, _i32, _i32, _i64, _i32, _i32, _i32, _vp, _i64, _vp, _i64, _vp, _i32, _vp, _i64, _vp],
+    "hift_kernel_cache_append": [_P(Cache), _i64, _vp, _i32, _i32, _i32, _i32, _vp, _i64, _vp, _i64, _vp, _i64, _vp],
+    "hift_kernel_attention_paged_bytes": [_P(Cache), _i64, _i32, _i64, _i32, _i32, _P(_sz)],
+    "hift_kernel_attention_paged": [_P(Cache), _i64, _vp, _i32, _i64, _i32, _i32, C.c_float, _vp, _i64, _vp, _i64, _vp, _vp, _sz, _vp],
+    "hift_kernel_adjust_logits": [_i32, _i64, _i32, _i64, _vp, _P(Adjust), _i64, _vp, _vp],
+    "hift_kernel_adjust_logits_bwd": [_i32, _i64, _i32, _i64, _vp, _P(Adjust), _i64, _vp, _i64, _vp, _vp],
 }
 for _n, _a in _SIGS.items():
     getattr(lib, _n).argtypes = _a
@@ -401,16 +422,21 @@ def kernel_token_logprob_bwd(logits, vocab, targets, scale, stats, entropy, d_lo
                                              _row_values("d_logp", d_logp, rows, at), _row_values("d_entropy", d_entropy, rows, at), ldd, dlogits.data_ptr(), st))
 
 
+def _new_workspace(nbytes, stream, device):
+    workspace = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=torch.device("cuda", device))
+    if stream is not None:
+        stream.wait_stream(torch.cuda.current_stream(device))   # the memory may still be in use there
+        workspace.record_stream(stream)
+    return workspace, workspace.numel()
+
+
 def _workspace(query, n, arr, workspace, stream, device):
     """The caller's work space, or one on the device of that number from torch's allocator, which keeps it until the stream is done with it."""
     if workspace is None:
         b = _sz()
         _check(query(n, arr, C.byref(b)))
-        workspace = torch.empty(max(b.value, 16), dtype=torch.uint8, device=torch.device("cuda", device))
-        if stream is not None:
-            stream.wait_stream(torch.cuda.current_stream(device))   # the memory may still be in use there
-            workspace.record_stream(stream)
-    elif workspace.get_device() != device or not workspace.is_contiguous():
+        return _new_workspace(b.value, stream, device)
+    if workspace.get_device() != device or not workspace.is_contiguous():
         raise ValueError(f"workspace: contiguous memory on cuda:{device} expected, not {tuple(workspace.shape)} {workspace.stride()} on {workspace.device}")
     return workspace, workspace.numel() * workspace.element_size()
 
@@ -458,6 +484,155 @@ def kernel_muon(opt: dict, master, grad, momentum, compute_copy=None, workspace=
     o = make_opt(opt)
     ws, nb = _workspace(lib.hift_kernel_muon_bytes, n, arr, workspace, stream, at) if n else (None, 0)
     _check(lib.hift_kernel_muon(C.byref(o), n, arr, _ptr(ws), nb, st))
+
+
+ROTARY_SCALING = {"plain": 0, "linear": 1, "base": 2, "parts": 3}
+ROTARY_LAYOUT = {"halves": 0, "pairs": 1}
+
+
+def make_rotary(r: dict) -> Rotary:
+    return Rotary(r["rot"], ROTARY_SCALING[r.get("scaling", "plain")], r.get("base", 10000.0), r.get("factor", 1.0), r.get("trained", 1.0), r.get("slow", 0.0),
+                  r.get("fast", 1.0), r.get("amplitude", 1.0))
+
+
+def _table_of(name, cos_sin, device):
+    """A rotary table [rows, rot / 2, 2]: its rows and rot."""
+    size = cos_sin.shape
+    if cos_sin.dtype is not torch.float32 or cos_sin.get_device() != device or len(size) != 3 or size[2] != 2 or not cos_sin.is_contiguous():
+        raise ValueError(f"{name}: contiguous float32 [rows, rot / 2, 2] on cuda:{device} expected, not {tuple(size)} of {cos_sin.dtype} on {cos_sin.device}")
+    return size[0], 2 * size[1]
+
+
+def kernel_rotary_table(rotary: dict, cos_sin, first=0, stream=None):
+    """The table of a rotary embedding (keys of hift_rotary: rot, scaling "plain" / "linear" / "base" / "parts", base, factor, ..) for positions from `first` on."""
+    st = _stream_of(cos_sin, stream)
+    rows, rot = _table_of("cos_sin", cos_sin, max(cos_sin.get_device(), 0))
+    if rot != rotary["rot"]:
+        raise ValueError(f"cos_sin: rot / 2 = {rotary['rot'] // 2} expected, not {rot // 2}")
+    r = make_rotary(rotary)
+    _check(lib.hift_kernel_rotary_table(C.byref(r), first, rows, cos_sin.data_ptr(), st))
+
+
+def kernel_rotary(x, heads, head_dim, y, cos_sin, positions=None, seq=0, layout="halves", backward=False, stream=None):
+    """y = the rows of x ([rows, >= heads * head_dim]) with their heads rotated by the table's entry for positions (int32) or row % seq; y may be x."""
+    st, at = _stream_of(x, stream), x.get_device()
+    ldx, rows = _rows_of("x", x), x.shape[0]
+    ldy = _rows_of("y", y, x.dtype, device=at)
+    if x.shape[1] < heads * head_dim or y.shape[1] < heads * head_dim or y.shape[0] != rows:
+        raise ValueError(f"{rows} rows of {heads} heads of {head_dim} expected, not x {tuple(x.shape)} and y {tuple(y.shape)}")
+    table, rot = _table_of("cos_sin", cos_sin, at)
+    _check(lib.hift_kernel_rotary(_dtype_code(x), ROTARY_LAYOUT[layout], int(backward), rows, heads, head_dim, rot, x.data_ptr(), ldx, y.data_ptr(), ldy,
+                                  _row_values("positions", positions, rows, at, torch.int32), seq, cos_sin.data_ptr(), table, st))
+
+
+class PagedCache:
+    """One layer's paged cache (hift_cache): k, v [pages there are, kv_heads, page, head_dim] (any distance between pages), pages [sequences, most pages of a
+    sequence] and lengths [sequences], both int32.  Holds the tensors; what lengths and pages say may change between calls."""
+
+    def __init__(self, k, v, pages, lengths):
+        at = k.get_device()
+        if k.dim() != 4 or v.shape != k.shape or v.dtype is not k.dtype or v.stride() != k.stride() or at < 0 or v.get_device() != at:
+            raise ValueError(f"k, v: device tensors [n_pages, kv_heads, page, head_dim] of one type expected, not {tuple(k.shape)} {k.dtype} and {tuple(v.shape)} {v.dtype}")
+        n, kv, page, hd = k.shape
+        if n and not (k[0].is_contiguous() and v[0].is_contiguous()):
+            raise ValueError("k, v: a page has to be contiguous")
+        if pages.dim() != 2 or pages.dtype is not torch.int32 or pages.get_device() != at or (pages.shape[1] > 1 and pages.stride(1) != 1):
+            raise ValueError(f"pages: int32 [sequences, pages] on cuda:{at} expected, not {tuple(pages.shape)} of {pages.dtype} on {pages.device}")
+        _row_values("lengths", lengths, pages.shape[0], at, torch.int32)
+        self.k, self.v, self.pages, self.lengths, self.device, self.dtype, self.head_dim, self.kv_heads = k, v, pages, lengths, at, k.dtype, hd, kv
+        most = pages.shape[1]
+        self.c = Cache(_dtype_code(k), kv, hd, page, n, pages.shape[0], most, max(k.stride(0), kv * page * hd) if n > 1 else kv * page * hd,
+                       max(pages.stride(0), most) if pages.shape[0] > 1 else most, k.data_ptr(), v.data_ptr(), pages.data_ptr(), lengths.data_ptr())
+        if n > 1 and k.stride(0) < kv * page * hd:
+            raise ValueError("k, v: pages overlap")
+        self.ref = C.byref(self.c)
+
+
+def _starts_of(cache, starts):
+    return _row_values("starts", starts, cache.c.sequences + 1, cache.device, torch.int32)
+
+
+def kernel_cache_append(cache, starts, qkv, heads, q_out=None, cos_sin=None, layout="halves", max_new=None, stream=None):
+    """Rows q | k | v: k rotated and v to their pages, q rotated to q_out (qkv itself: in place; None: not wanted).  starts: int32 [sequences + 1]; max_new: most new
+    rows of a sequence (None: all of them)."""
+    st, at = _stream_of(qkv, stream), cache.device
+    rows, width = qkv.shape
+    ld = _rows_of("qkv", qkv, cache.dtype, device=at)
+    need = (heads + 2 * cache.kv_heads) * cache.head_dim
+    if width < need:
+        raise ValueError(f"qkv: rows of {need} expected, not {width}")
+    ldq = 0
+    if q_out is not None:
+        ldq = _rows_of("q_out", q_out, cache.dtype, device=at)
+        if q_out.shape[0] != rows or q_out.shape[1] < heads * cache.head_dim:
+            raise ValueError(f"q_out: [{rows}, {heads * cache.head_dim}] expected, not {tuple(q_out.shape)}")
+    table, rot = (0, 0) if cos_sin is None else _table_of("cos_sin", cos_sin, at)
+    _check(lib.hift_kernel_cache_append(cache.ref, rows, _starts_of(cache, starts), rows if max_new is None else max_new, heads, ROTARY_LAYOUT[layout], rot, _ptr(cos_sin),
+                                        table, qkv.data_ptr(), ld, _ptr(q_out), ldq, st))
+
+
+def kernel_attention_paged_bytes(cache, rows, heads, max_new, max_length, window=0) -> int:
+    b = _sz()
+    _check(lib.hift_kernel_attention_paged_bytes(cache.ref, rows, max_new, max_length, heads, window, C.byref(b)))
+    return b.value
+
+
+def kernel_attention_paged(cache, starts, q, heads, out, max_new, max_length, window=0, scale=None, lse=None, workspace=None, stream=None):
+    """out = attention of the new rows q ([rows, heads * head_dim]) over the cache, which holds their keys and values already.  max_new: most new rows of a sequence;
+    max_length: most tokens of one, new ones included; scale: None for 1 / sqrt(head_dim); lse: float32 [rows, heads] or None."""
+    st, at = _stream_of(q, stream), cache.device
+    rows, hd = q.shape[0], cache.head_dim
+    ldq, ldo = _rows_of("q", q, cache.dtype, device=at), _rows_of("out", out, cache.dtype, device=at)
+    if q.shape[1] < heads * hd or out.shape[1] < heads * hd or out.shape[0] != rows:
+        raise ValueError(f"q, out: [{rows}, {heads * hd}] expected, not {tuple(q.shape)} and {tuple(out.shape)}")
+    if workspace is None:
+        need = kernel_attention_paged_bytes(cache, rows, heads, max_new, max_length, window)
+        ws, n = _new_workspace(need, stream, at) if need else (None, 0)
+    else:
+        ws, n = _workspace(None, 0, None, workspace, stream, at)
+    _check(lib.hift_kernel_attention_paged(cache.ref, rows, _starts_of(cache, starts), max_new, max_length, heads, window, hd ** -0.5 if scale is None else scale,
+                                           q.data_ptr(), ldq, out.data_ptr(), ldo, _row_values("lse", lse, rows * heads, at), _ptr(ws), n, st))
+
+
+def _adjust_of(rows, vocab, at, tokens, begin, end, repetition, presence, frequency, bias, allowed):
+    ld_bias = ld_allowed = 0
+    if bias is not None:
+        ld_bias = _rows_of("bias", bias, torch.float32, device=at)
+        if bias.shape[0] not in (1, rows) or bias.shape[1] < vocab:
+            raise ValueError(f"bias: [1 or {rows}, {vocab}] expected, not {tuple(bias.shape)}")
+        ld_bias = ld_bias if bias.shape[0] > 1 else 0
+    if allowed is not None:
+        ld_allowed = _rows_of("allowed", allowed, torch.int32, device=at)
+        if allowed.shape[0] not in (1, rows) or allowed.shape[1] < (vocab + 31) // 32:
+            raise ValueError(f"allowed: [1 or {rows}, {(vocab + 31) // 32}] words expected, not {tuple(allowed.shape)}")
+        ld_allowed = ld_allowed if allowed.shape[0] > 1 else 0
+    if tokens is not None and (begin is None or end is None):
+        raise ValueError("tokens need begin and end")
+    n = 0 if tokens is None else tokens.numel()
+    return Adjust(_row_values("tokens", tokens, n, at, torch.int32), n, _row_values("begin", begin, rows, at, torch.int64), _row_values("end", end, rows, at, torch.int64),
+                  repetition, presence, frequency, _ptr(bias), ld_bias, _ptr(allowed), ld_allowed)
+
+
+def kernel_adjust_logits(logits, vocab, out, tokens=None, begin=None, end=None, repetition=1.0, presence=0.0, frequency=0.0, bias=None, allowed=None, stream=None):
+    """out = logits with penalties for the tokens that each row has seen (tokens int32; begin, end int64 [rows]), a bias (float32 [1 or rows, vocab]) and a mask of
+    allowed tokens (int32 words [1 or rows, ceil(vocab / 32)], bit j % 32 of word j / 32 for token j); out may be logits."""
+    st, at, (rows, width) = _stream_of(logits, stream), logits.get_device(), logits.shape
+    ld, ldo = _rows_of("logits", logits), _rows_of("out", out, logits.dtype, device=at)
+    if vocab > width or vocab > out.shape[1] or out.shape[0] != rows:
+        raise ValueError(f"vocab {vocab}, but logits are {tuple(logits.shape)} and out {tuple(out.shape)}")
+    by = _adjust_of(rows, vocab, at, tokens, begin, end, repetition, presence, frequency, bias, allowed)
+    _check(lib.hift_kernel_adjust_logits(_dtype_code(logits), rows, vocab, ld, logits.data_ptr(), C.byref(by), ldo, out.data_ptr(), st))
+
+
+def kernel_adjust_logits_bwd(logits, vocab, d_out, d_logits, tokens=None, begin=None, end=None, repetition=1.0, presence=0.0, frequency=0.0, bias=None, allowed=None,
+                             stream=None):
+    """d_logits = the gradient with respect to the logits of kernel_adjust_logits (same arguments) whose result has the gradient d_out; may be d_out."""
+    st, at, (rows, width) = _stream_of(logits, stream), logits.get_device(), logits.shape
+    ld, ldg, ldd = _rows_of("logits", logits), _rows_of("d_out", d_out, logits.dtype, device=at), _rows_of("d_logits", d_logits, logits.dtype, device=at)
+    if min(width, d_out.shape[1], d_logits.shape[1]) < vocab or d_out.shape[0] != rows or d_logits.shape[0] != rows:
+        raise ValueError(f"vocab {vocab}, but logits are {tuple(logits.shape)}, d_out {tuple(d_out.shape)} and d_logits {tuple(d_logits.shape)}")
+    by = _adjust_of(rows, vocab, at, tokens, begin, end, repetition, presence, frequency, bias, allowed)
+    _check(lib.hift_kernel_adjust_logits_bwd(_dtype_code(logits), rows, vocab, ld, logits.data_ptr(), C.byref(by), ldg, d_out.data_ptr(), ldd, d_logits.data_ptr(), st))
 
 
 def _hip_runtime():

@@ -1,0 +1,185 @@
+// Logits as a sampler wants them: penalties for tokens that a row has seen, a bias, and a mask of allowed tokens; and the gradient through them.
+//
+// With n the number of times that row r has seen token j (its history is a range of a list of tokens, ranges may overlap):
+//   z = x                                          if n = 0
+//   z = (x > 0 ? x / repetition : x repetition) - presence   otherwise
+//   out = z - frequency n + bias[j];  -inf where the mask has no bit
+// and backwards d = g, g / repetition or g repetition by the same distinction, 0 where the mask has no bit.  In fp32, rounded once.
+//
+// One pass over the logits, bound by memory.  A workgroup takes a slice of a row and counts the row's history for its slice in LDS, in whole
+// numbers, so the order of the additions does not show; the history is read once a slice and comes from L2.  Backwards a logit is read only where
+// a token was seen.
+#include <math.h>
+
+#include <algorithm>
+
+#include "common.h"
+#include "kernels.h"
+
+namespace hift {
+namespace {
+
+constexpr int BLK = 256;
+constexpr int LOOSE = 8;  // elements before the first aligned piece: at most 7
+
+struct AdjustArgs {
+  int V, slice, slices;
+  int64_t rows, ld, ldo, ldg;
+  const void* x;
+  const void* g;  // backward: the gradient that comes in
+  void* out;
+  const int32_t* tokens;
+  int64_t n_tokens;
+  const int64_t *begin, *end;
+  float repetition, inverse, presence, frequency;
+  const float* bias;
+  int64_t ld_bias;
+  const uint32_t* allowed;
+  int64_t ld_allowed;
+  bool aligned;  // rows of all matrices lie alike within 16 bytes
+};
+
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+
+template <typename T, bool BWD>
+__device__ __forceinline__ float adjusted(float x, float g, int n, float bias, bool allowed, const AdjustArgs& p) {
+  if constexpr (BWD) {
+    if (!allowed) return 0.f;
+    return n > 0 ? (x > 0.f ? g * p.inverse : g * p.repetition) : g;
+  } else {
+    if (!allowed) return -INFINITY;
+    const float z = n > 0 ? (x > 0.f ? x * p.inverse : x * p.repetition) - p.presence : x;
+    return z - p.frequency * (float)n + bias;
+  }
+}
+
+template <typename T, bool BWD>
+__global__ void __launch_bounds__(BLK) adjust_k(AdjustArgs p) {
+  extern __shared__ int4 count_quads[];
+  int* counts = reinterpret_cast<int*>(count_quads);  // [LOOSE + slice], the first aligned piece's at LOOSE
+  __shared__ int any;
+  constexpr int E = 16 / (int)sizeof(T);
+  const int64_t row = blockIdx.x / (unsigned)p.slices;
+  const int part = (int)(blockIdx.x % (unsigned)p.slices);
+  const T* x = (const T*)p.x + row * p.ld;
+  const T* g = BWD ? (const T*)p.g + row * p.ldg : nullptr;
+  T* out = (T*)p.out + row * p.ldo;
+  // slices begin at aligned pieces of the row; the first has the elements before them, too
+  const int head = p.aligned ? min(p.V, (int)((16 - (reinterpret_cast<uintptr_t>(BWD ? g : x) & 15)) & 15) / (int)sizeof(T)) : 0;
+  const int lo = part ? (int)min((int64_t)p.V, (int64_t)head + (int64_t)part * p.slice) : 0;
+  const int hi = part + 1 == p.slices ? p.V : (int)min((int64_t)p.V, (int64_t)head + (int64_t)(part + 1) * p.slice);
+  const int n = hi - lo;
+  if (n <= 0) return;
+  const int from = part ? lo : head, shift = LOOSE - (from - lo);  // counts[shift + j - lo] is element j's
+  const int t = threadIdx.x;
+  bool seen = false;
+  if (p.tokens) {
+    const int64_t b = min(max(p.begin[row], (int64_t)0), p.n_tokens), e = min(max(p.end[row], b), p.n_tokens);
+    if (e > b) {
+      if (t == 0) any = 0;
+      for (int i = t; i < n; i += BLK) counts[shift + i] = 0;
+      __syncthreads();
+      int mine = 0;
+      for (int64_t i = b + t; i < e; i += BLK) {
+        const unsigned at = (unsigned)p.tokens[i] - (unsigned)lo;
+        if (at < (unsigned)n) {
+          atomicAdd(&counts[shift + (int)at], 1);
+          mine = 1;
+        }
+      }
+      if (mine) any = 1;
+      __syncthreads();
+      seen = any != 0;
+    }
+  }
+  const float* bias = p.bias ? p.bias + row * p.ld_bias : nullptr;
+  const uint32_t* allowed = p.allowed ? p.allowed + row * p.ld_allowed : nullptr;
+  auto one = [&](int j) __attribute__((always_inline)) {
+    const int c = seen ? counts[shift + j - lo] : 0;
+    const bool let = !allowed || (allowed[j >> 5] >> (j & 31) & 1);
+    out[j] = from_f32<T>(adjusted<T, BWD>(!BWD || c > 0 ? to_f32(x[j]) : 0.f, BWD ? to_f32(g[j]) : 0.f, c, !BWD && bias ? bias[j] : 0.f, let, p));
+  };
+  if (!p.aligned) {
+    for (int j = lo + t; j < hi; j += BLK) one(j);
+    return;
+  }
+  const int pieces = (hi - from) / E;
+  for (int i = t; i < pieces; i += BLK) {
+    const int j0 = from + i * E;
+    typedef Vec<T, E> P;
+    const P in = *reinterpret_cast<const P*>((BWD ? g : x) + j0);
+    int c[E];
+#pragma unroll
+    for (int e = 0; e < E; e += 4) {
+      const int4 q = seen ? count_quads[(LOOSE + i * E + e) / 4] : make_int4(0, 0, 0, 0);
+      c[e] = q.x; c[e + 1] = q.y; c[e + 2] = q.z; c[e + 3] = q.w;
+    }
+    uint32_t bits = 0xFFFFFFFFu;
+    if (allowed) {
+      const int w = j0 >> 5, w1 = (j0 + E - 1) >> 5;
+      bits = (uint32_t)(((uint64_t)allowed[w1] << 32 | allowed[w]) >> (j0 & 31));
+    }
+    float bv[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) bv[e] = 0.f;
+    if (!BWD && bias) {
+#pragma unroll
+      for (int e = 0; e < E; e += 4) {
+        const f32x4_any q = *reinterpret_cast<const f32x4_any*>(bias + j0 + e);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) bv[e + k] = q[k];
+      }
+    }
+    P o;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      float xv = 0.f, gv = 0.f;
+      if constexpr (BWD) {
+        gv = to_f32(in.v[e]);
+        if (c[e] > 0) xv = to_f32(x[j0 + e]);
+      } else {
+        xv = to_f32(in.v[e]);
+      }
+      o.v[e] = from_f32<T>(adjusted<T, BWD>(xv, gv, c[e], bv[e], bits >> e & 1, p));
+    }
+    *reinterpret_cast<P*>(out + j0) = o;
+  }
+  // what is left before the first piece and after the last
+  if (part == 0 && t < head) one(t);
+  const int tail = from + pieces * E;
+  if (t < hi - tail) one(tail + t);
+}
+
+template <typename T, bool BWD>
+hipError_t run(AdjustArgs p, hipStream_t st) {
+  // Slices: 8192 entries (32 KB of counts, five workgroups a compute unit), fewer where rows are few, down to a piece a thread.
+  constexpr int E = 16 / (int)sizeof(T);
+  p.slice = 8192;
+  while (p.slice > BLK * E && p.rows * ((p.V + p.slice - 1) / p.slice) < 512) p.slice /= 2;
+  p.slices = (int)(((int64_t)p.V + p.slice - 1) / p.slice);
+  if (p.rows * p.slices > 0x7FFFFFFF) return hipErrorInvalidValue;
+  const auto low = [](const void* q) { return (int64_t)(reinterpret_cast<uintptr_t>(q) & 15); };
+  p.aligned = low(p.out) == low(BWD ? p.g : p.x) && (p.ldo - (BWD ? p.ldg : p.ld)) % E == 0;
+  adjust_k<T, BWD><<<(unsigned)(p.rows * p.slices), BLK, (size_t)(p.slice + LOOSE) * 4, st>>>(p);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t adjust_logits(int dt, bool backward, int64_t rows, int V, int64_t ld, const void* x, const AdjustBy& by, int64_t ldg, const void* g, int64_t ldo,
+                         void* out, hipStream_t st) {
+  if (rows == 0) return hipSuccess;
+  AdjustArgs p{};
+  p.V = V; p.rows = rows; p.ld = ld; p.ldo = ldo; p.ldg = ldg; p.x = x; p.g = g; p.out = out;
+  // penalties that change nothing need no history
+  const bool neutral = by.repetition == 1.f && (backward || (by.presence == 0.f && by.frequency == 0.f));
+  p.tokens = neutral ? nullptr : by.tokens;
+  p.n_tokens = by.n_tokens; p.begin = by.begin; p.end = by.end;
+  p.repetition = by.repetition; p.inverse = 1.f / by.repetition; p.presence = by.presence; p.frequency = by.frequency;
+  p.bias = backward ? nullptr : by.bias; p.ld_bias = by.ld_bias;
+  p.allowed = by.allowed; p.ld_allowed = by.ld_allowed;
+  if (dt == DT_BF16) return backward ? run<bf16, true>(p, st) : run<bf16, false>(p, st);
+  return backward ? run<float, true>(p, st) : run<float, false>(p, st);
+}
+
+}  // namespace hift

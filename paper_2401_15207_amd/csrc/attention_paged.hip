@@ -1,0 +1,600 @@
+// Attention of new tokens over a paged cache, forward only: bf16 and fp32, grouped heads, a sliding window, from one token a sequence to chunks.
+//
+//   s_j = scale q . k_j over the keys j that a row sees (at most its own position, more than position - window, on pages that there are)
+//   out = sum_j exp(s_j) v_j / sum_j exp(s_j),  lse = log2 sum_j exp(s_j)
+//
+// The new rows of a sequence and the query heads that share a key head make one list of rows, m = token * group + head: it is their tile that
+// meets a tile of keys, so keys and values are read once for all heads of a group.  One pass over the keys with a running maximum and sum
+// per row (log2 domain), as in attention.hip, whose conventions for the matrix instruction's operands and for LDS tiles these kernels share.
+//   few_k    at most 32 rows: all four wavefronts of a workgroup hold the same rows and take turns at the blocks of 32 keys, each through LDS tiles
+//            of its own without any barrier, and their results are joined at the end.  Bound by reading the cache.
+//   many_k   128 rows a workgroup, 32 a wavefront, which share tiles of 64 keys.  Bound by the matrix instructions.
+//   join_k   where the keys of a row were split over workgroups: the parts, weighted by their maxima.
+#include <math.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "common.h"
+#include "kernels.h"
+#include "paged_cache.h"
+
+namespace hift {
+namespace {
+
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+typedef short v4i16 __attribute__((ext_vector_type(4)));
+typedef short v8i16 __attribute__((ext_vector_type(8)));
+
+constexpr int FEW = 32;    // rows of few_k
+constexpr int KB = 32;     // keys of a block
+constexpr int GROUP = 16;  // keys that surely lie on one page
+
+struct Args {
+  CacheView c;
+  int heads, group;     // query heads; those that share a key head
+  int64_t rows, ldq, ldo;
+  int max_new, window;  // window 0: none
+  float scale_log2e;
+  const void* q;
+  void* out;
+  float* lse;           // [rows, heads] or null
+  int few_upto;         // sequences of at most so many rows are few_k's, the others many_k's
+  int row_blocks;       // many_k: blocks of 128 rows of the longest sequence
+  int split, chunk;     // this kernel's workgroups along the keys, and the keys of each
+  float* part;          // [..][HD] sums and, behind all of them, (maximum, sum of exponentials) pairs
+  float2* part_ml;
+};
+
+// ---- tiles of a type and width ----
+// A row of a tile is HD elements without padding; its 16-byte piece c lies at piece position c ^ swizzle(row), which spreads what one LDS
+// instruction reads over the banks.  HD: 64 or 128; narrower heads are zeros behind their width.
+template <typename T, int HD>
+struct Tile {
+  static constexpr int ROWB = HD * (int)sizeof(T), PPR = ROWB / 16, RPI = 64 / PPR, NB = HD / 32;
+  static constexpr int IPG = GROUP / RPI;  // load instructions of 16 keys
+  static constexpr int BLOCKB = KB * ROWB;
+  static constexpr bool F32 = sizeof(T) == 4;
+  static constexpr int NQ = F32 ? HD / 8 : HD / 16;  // fragments of a row
+  typedef typename std::conditional<F32, f32x4, bf16x8>::type Frag;  // 16 bytes of a row
+
+  __device__ static __forceinline__ int swizzle(int r) {
+    if constexpr (F32) return ((r >> 2) & 1) << 3 | ((r >> 3) & 1) << 2 | (r & 3);
+    return PPR == 16 ? (r & 3) << 2 | ((r >> 2) & 3) : (r >> 1) & 7;
+  }
+  // which row of a 32-key block the score fragments' lane r reads: for bf16 with bits 2 and 3 exchanged, so that scores are operands as they lie
+  __device__ static __forceinline__ int key_row(int r) { return F32 ? r : (r & ~12) | ((r & 4) << 1) | ((r & 8) >> 1); }
+  // the key of score element e in a lane of half fh
+  __device__ static __forceinline__ int key_of(int e, int fh) { return F32 ? 8 * (e >> 2) + 4 * fh + (e & 3) : 16 * (e >> 3) + 8 * fh + (e & 7); }
+
+  // Requests 16 keys from token `key0` on (all on one page) of one of the cache's arrays into LDS; keys from `end` on, and those of a page that is
+  // not there, arrive as zeros.  vo: offsets of the lane's pieces within 16 keys (see offsets).
+  __device__ static __forceinline__ void request(const CacheView& c, const void* array, int page, int kv_head, int key0, int end, const uint32_t (&vo)[IPG],
+                                                 uint32_t lds) {
+    const int slot = key0 & (c.page - 1);
+    const int64_t at = (int64_t)max(page, 0) * c.page_stride + ((int64_t)kv_head * c.page + slot) * c.head_dim;
+    const uint64_t a = reinterpret_cast<uint64_t>(array) + (uint64_t)at * sizeof(T);
+    const int n = page < 0 ? 0 : min(max(end - key0, 0), GROUP);
+    const hift_u32x4 rs = {(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)a), (uint32_t)__builtin_amdgcn_readfirstlane((int)((uint32_t)(a >> 32) & 0xFFFFu)),
+                           (uint32_t)__builtin_amdgcn_readfirstlane(n * c.head_dim * (int)sizeof(T)), 0x00020000u};
+#pragma unroll
+    for (int i = 0; i < IPG; ++i) load_to_lds_b128(rs, lds + i * 1024, vo[i], 0);
+  }
+  __device__ static __forceinline__ void offsets(uint32_t (&vo)[IPG], int lane, int head_dim) {
+#pragma unroll
+    for (int i = 0; i < IPG; ++i) {
+      const int r = i * RPI + lane / PPR, c = (lane % PPR) ^ swizzle(r);
+      vo[i] = c * 16 < head_dim * (int)sizeof(T) ? (uint32_t)(r * head_dim * (int)sizeof(T) + c * 16) : 0x80000000u;
+    }
+  }
+  // A row of queries as fragments; piece i of the lane: bytes 32 i + 16 fh
+  __device__ static __forceinline__ void load_row(Frag (&f)[NQ], const T* row, bool ok, int head_dim, int fh) {
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+      hift_u32x4 t = {0u, 0u, 0u, 0u};
+      if (ok && (2 * i + fh) * 16 < head_dim * (int)sizeof(T)) t = *reinterpret_cast<const hift_u32x4*>(reinterpret_cast<const unsigned char*>(row) + (2 * i + fh) * 16);
+      f[i] = __builtin_bit_cast(Frag, t);
+    }
+  }
+  struct Address {
+    int k[NQ];                  // piece of the lane's key row
+    int v[F32 ? 2 : NB][2];     // bf16: transposing reads by column block and half; fp32: see value_of
+  };
+  __device__ static __forceinline__ void addresses(Address& a, int lane) {
+    const int fr = lane & 31, fh = lane >> 5, r = key_row(fr);
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) a.k[i] = r * ROWB + (((2 * i + fh) ^ swizzle(r)) * 16);
+    if constexpr (!F32) {
+      const int sl = lane & 15;
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int hh = 0; hh < 2; ++hh) {
+          const int row = 8 * fh + (sl >> 2) + 4 * hh, col = nb * 32 + 16 * ((lane >> 4) & 1) + 4 * (sl & 3);
+          a.v[nb][hh] = row * ROWB + (((col >> 3) ^ swizzle(row)) * 16) + (col & 7) * 2;
+        }
+    }
+  }
+  // scores of the lane's query row against the block's keys
+  __device__ static __forceinline__ f32x16 scores(const unsigned char* k, const Address& a, const Frag (&q)[NQ]) {
+    f32x16 s;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s[e] = 0.f;
+    Frag f[NQ];
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) f[i] = *reinterpret_cast<const Frag*>(k + a.k[i]);
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+      if constexpr (F32) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s = __builtin_amdgcn_mfma_f32_32x32x2f32(f[i][j], q[i][j], s, 0, 0, 0);
+      } else {
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i], q[i], s, 0, 0, 0);
+      }
+    }
+    return s;
+  }
+  // out += p (of the block's keys) times its values.  Lane: query row lane % 32; element e of out[nb]: column 32 nb + 8 (e / 4) + 4 (lane / 32) + e % 4
+  __device__ static __forceinline__ void values(f32x16 (&out)[NB], const unsigned char* v, const Address& a, const f32x16& p, int lane) {
+    if constexpr (F32) {
+      const int fr = lane & 31, fh = lane >> 5;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int key = key_of(e, 0) + 4 * fh;
+        float f[NB];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) f[nb] = *reinterpret_cast<const float*>(v + key * ROWB + (((nb * 8 + (fr >> 2)) ^ swizzle(key)) * 16) + (fr & 3) * 4);
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) out[nb] = __builtin_amdgcn_mfma_f32_32x32x2f32(f[nb], p[e], out[nb], 0, 0, 0);
+      }
+    } else {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        bf16x8 pf, vf[NB];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) pf[e] = static_cast<__bf16>(p[8 * t + e]);
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          const v4i16 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((v4i16 __attribute__((address_space(3)))*)(v + t * 16 * ROWB + a.v[nb][0]));
+          const v4i16 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((v4i16 __attribute__((address_space(3)))*)(v + t * 16 * ROWB + a.v[nb][1]));
+          const v8i16 both = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+          vf[nb] = __builtin_bit_cast(bf16x8, both);
+        }
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) out[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[nb], pf, out[nb], 0, 0, 0);
+      }
+    }
+  }
+};
+
+// ---- a row's running softmax (log2 domain) ----
+template <int NB>
+struct Running {
+  float m = -INFINITY, l = 0.f;  // reference of the exponentials, equal in a row's two lanes; sum of the lane's exponentials
+  f32x16 o[NB];
+  __device__ __forceinline__ Running() {
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[nb][e] = 0.f;
+  }
+  // Turns raw scores into exponentials.  The reference is raised, and the sums rescaled, only where a score exceeds it by more than 2^8: what is
+  // left stays below 2^8, which costs bf16, a relative format, nothing.
+  template <int N>
+  __device__ __forceinline__ void take(f32x16 (&s)[N], float scale_log2e) {
+    float top = s[0][0];
+#pragma unroll
+    for (int b = 0; b < N; ++b)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) top = fmaxf(top, s[b][e]);
+    top = fmaxf(top, __shfl_xor(top, 32, 64)) * scale_log2e;
+    if (__builtin_amdgcn_ballot_w64(top > m + 8.0f) != 0) {
+      const float now = fmaxf(m, top);
+      const float by = now == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - now);
+      l *= by;
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[nb][e] *= by;
+      m = now;
+    }
+    const float ref = m == -INFINITY ? 0.f : m;  // a row that has seen nothing yet: exp2(-inf - 0) = 0
+#pragma unroll
+    for (int b = 0; b < N; ++b)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        s[b][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][e], scale_log2e, -ref));
+        l += s[b][e];
+      }
+  }
+};
+
+// The keys that a block of rows reads, and this workgroup's part of them
+struct Span {
+  int from, to;  // keys [from, to); `from` a multiple of 32
+  bool direct;   // all the keys there are: the result goes to the output, not to a part
+  bool none;     // no keys for this part
+};
+__device__ __forceinline__ int parts_of(int from, int to, int split, int chunk) { return min(split, max(1, (to - from + chunk - 1) / chunk)); }
+// rows: tokens [t0, t1] of the sequence
+__device__ __forceinline__ void keys_of(const CacheSeq& of, int t0, int t1, int window, int& from, int& to) {
+  to = min(of.total, of.cached + t1 + 1);
+  from = window > 0 ? max(0, of.cached + t0 - window + 1) & ~(KB - 1) : 0;
+  from = min(from, to & ~(KB - 1));
+}
+__device__ __forceinline__ Span span_of(const CacheSeq& of, int t0, int t1, int window, int part, int split, int chunk) {
+  int from, to;
+  keys_of(of, t0, t1, window, from, to);
+  const int n = parts_of(from, to, split, chunk);
+  Span s;
+  s.direct = n == 1;
+  s.none = part >= n;
+  s.from = from + part * chunk;
+  s.to = part + 1 == n ? to : s.from + chunk;
+  return s;
+}
+
+// Where a row of the list m = token * group + head goes
+struct RowAt {
+  int64_t row;
+  int head, pos;
+  bool ok;
+};
+__device__ __forceinline__ RowAt row_at(const Args& p, const CacheSeq& of, int kv_head, int m) {
+  RowAt r;
+  const int token = m / p.group;
+  r.ok = token < of.fresh;
+  r.row = of.row0 + (r.ok ? token : 0);
+  r.head = kv_head * p.group + (m - token * p.group);
+  r.pos = of.cached + token;
+  return r;
+}
+
+__device__ __forceinline__ bool sees(int key, int pos, int total, int window) { return key <= pos && key < total && (window == 0 || key > pos - window); }
+
+template <typename T>
+__device__ __forceinline__ void store_out(const Args& p, const RowAt& r, int c, float v) {
+  if (c < p.c.head_dim) ((T*)p.out)[r.row * p.ldo + (int64_t)r.head * p.c.head_dim + c] = from_f32<T>(v);
+}
+
+// ---- few rows ----
+template <typename T, int HD>
+__global__ void __launch_bounds__(256) few_k(Args p) {
+  typedef Tile<T, HD> L;
+  constexpr int NB = L::NB, IPB = 2 * L::IPG;  // loads of a block of keys
+  extern __shared__ unsigned char lds[];       // [wave][K | V] blocks; at the end [wave][row][HD] sums
+  __shared__ float2 ml[4][FEW];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), fr = lane & 31, fh = lane >> 5;
+  const int pair = (int)(blockIdx.x / (unsigned)p.split), part = (int)(blockIdx.x % (unsigned)p.split);
+  const int s = pair / p.c.kv_heads, kv_head = pair % p.c.kv_heads;
+  const CacheSeq of = cache_seq(p.c, s, p.rows, p.max_new);
+  const int n_rows = of.fresh * p.group;
+  if (n_rows == 0 || n_rows > FEW) return;
+  const Span sp = span_of(of, 0, of.fresh - 1, p.window, part, p.split, p.chunk);
+  if (sp.none) return;
+
+  const RowAt at = row_at(p, of, kv_head, fr);
+  typename L::Frag q[L::NQ];
+  L::load_row(q, (const T*)p.q + at.row * p.ldq + (int64_t)at.head * p.c.head_dim, at.ok, p.c.head_dim, fh);
+  uint32_t vo[L::IPG];
+  L::offsets(vo, lane, p.c.head_dim);
+  typename L::Address ad;
+  L::addresses(ad, lane);
+  unsigned char* Kb = lds + wave * (2 * L::BLOCKB);
+  unsigned char* Vb = Kb + L::BLOCKB;
+  const uint32_t lk = (uint32_t)reinterpret_cast<uintptr_t>(Kb), lv = (uint32_t)reinterpret_cast<uintptr_t>(Vb);
+
+  const int blocks = (sp.to - sp.from + KB - 1) / KB;
+  auto page = [&](int key) { return __builtin_amdgcn_readfirstlane(key < sp.to ? cache_page(p.c, s, key) : -1); };
+  auto request = [&](const void* array, int key0, int pa, int pb, uint32_t dst) __attribute__((always_inline)) {
+    L::request(p.c, array, pa, kv_head, key0, sp.to, vo, dst);
+    L::request(p.c, array, pb, kv_head, key0 + GROUP, sp.to, vo, dst + GROUP * L::ROWB);
+  };
+  Running<NB> run;
+  int b = wave, key0 = sp.from + wave * KB;
+  int pa = -1, pb = -1;
+  if (b < blocks) {
+    pa = page(key0);
+    pb = page(key0 + GROUP);
+    request(p.c.k, key0, pa, pb, lk);
+    request(p.c.v, key0, pa, pb, lv);
+  }
+  for (; b < blocks; b += 4, key0 += 4 * KB) {
+    const bool more = b + 4 < blocks;
+    const int next = key0 + 4 * KB, na = more ? page(next) : -1, nb_ = more ? page(next + GROUP) : -1;
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(IPB) : "memory");  // the keys are there, their values on the way
+    f32x16 sc[1];
+    sc[0] = L::scores(Kb, ad, q);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (more) request(p.c.k, next, na, nb_, lk);
+    const bool plain = pa >= 0 && pb >= 0 && key0 + KB <= sp.to && key0 + KB - 1 <= of.cached && (p.window == 0 || key0 > of.cached + of.fresh - 1 - p.window);
+    if (!plain) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int j = L::key_of(e, fh), key = key0 + j;
+        const bool ok = key < sp.to && sees(key, at.pos, of.total, p.window) && (j < GROUP ? pa : pb) >= 0;
+        sc[0][e] = ok ? sc[0][e] : -INFINITY;
+      }
+    }
+    run.take(sc, p.scale_log2e);
+    if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(IPB) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    L::values(run.o, Vb, ad, sc[0], lane);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (more) request(p.c.v, next, na, nb_, lv);
+    pa = na; pb = nb_;
+  }
+  run.l += __shfl_xor(run.l, 32, 64);
+
+  // the wavefronts' results, joined
+  if (fh == 0) ml[wave][fr] = make_float2(run.m, run.l);
+  float* sums = reinterpret_cast<float*>(lds);  // [wave][FEW][HD]
+  __syncthreads();
+  if (fr < n_rows) {
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<f32x4*>(sums + (wave * FEW + fr) * HD + nb * 32 + 8 * g + 4 * fh) =
+            f32x4{run.o[nb][4 * g], run.o[nb][4 * g + 1], run.o[nb][4 * g + 2], run.o[nb][4 * g + 3]};
+  }
+  __syncthreads();
+  for (int i = tid; i < n_rows * HD; i += 256) {
+    const int m = i / HD, c = i % HD;
+    float top = ml[0][m].x;
+#pragma unroll
+    for (int w = 1; w < 4; ++w) top = fmaxf(top, ml[w][m].x);
+    const float ref = top == -INFINITY ? 0.f : top;
+    float l = 0.f, o = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float by = __builtin_amdgcn_exp2f(ml[w][m].x - ref);
+      l = fmaf(by, ml[w][m].y, l);
+      o = fmaf(by, sums[(w * FEW + m) * HD + c], o);
+    }
+    if (sp.direct) {
+      const RowAt r = row_at(p, of, kv_head, m);
+      store_out<T>(p, r, c, l > 0.f || l != l ? o / l : 0.f);
+      if (c == 0 && p.lse) p.lse[r.row * p.heads + r.head] = top + __builtin_amdgcn_logf(l);
+    } else {
+      const int64_t to = ((int64_t)pair * p.split + part) * FEW + m;
+      p.part[to * HD + c] = o;
+      if (c == 0) p.part_ml[to] = make_float2(top, l);
+    }
+  }
+}
+
+// ---- many rows ----
+template <typename T, int HD>
+__global__ void __launch_bounds__(256) many_k(Args p) {
+  typedef Tile<T, HD> L;
+  constexpr int NB = L::NB, KT = 2 * KB, TILEB = KT * L::ROWB, QB = 128;
+  extern __shared__ unsigned char lds[];  // [buffer][K | V] tiles of 64 keys
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), fr = lane & 31, fh = lane >> 5;
+  int i = (int)blockIdx.x;
+  const int part = i % p.split;
+  i /= p.split;
+  const int block = p.row_blocks - 1 - i % p.row_blocks, pair = i / p.row_blocks;  // the rows with the most keys first
+  const int s = pair / p.c.kv_heads, kv_head = pair % p.c.kv_heads;
+  const CacheSeq of = cache_seq(p.c, s, p.rows, p.max_new);
+  const int n_rows = of.fresh * p.group;
+  if (n_rows <= p.few_upto || block * QB >= n_rows) return;
+  const int m0 = block * QB, m_last = min(n_rows, m0 + QB) - 1;
+  const Span sp = span_of(of, m0 / p.group, m_last / p.group, p.window, part, p.split, p.chunk);
+  if (sp.none) return;
+
+  const int w0 = m0 + wave * 32;  // this wavefront's rows; their first and last positions
+  const int pos_lo = of.cached + min(w0, m_last) / p.group, pos_hi = of.cached + min(w0 + 31, m_last) / p.group;
+  const RowAt at = row_at(p, of, kv_head, w0 + fr);
+  typename L::Frag q[L::NQ];
+  L::load_row(q, (const T*)p.q + at.row * p.ldq + (int64_t)at.head * p.c.head_dim, at.ok, p.c.head_dim, fh);
+  uint32_t vo[L::IPG];
+  L::offsets(vo, lane, p.c.head_dim);
+  typename L::Address ad;
+  L::addresses(ad, lane);
+  const uint32_t lds0 = (uint32_t)reinterpret_cast<uintptr_t>(lds);
+  const int tiles = (sp.to - sp.from + KT - 1) / KT;
+  // every wavefront brings 16 keys of a tile
+  auto page = [&](int key) { return __builtin_amdgcn_readfirstlane(key < sp.to ? cache_page(p.c, s, key) : -1); };
+  __shared__ int pages_there[2][4];
+  auto request = [&](int tile, int pg) __attribute__((always_inline)) {
+    const int key0 = sp.from + tile * KT + wave * GROUP;
+    const uint32_t dst = lds0 + (tile & 1) * (2 * TILEB) + wave * (GROUP * L::ROWB);
+    L::request(p.c, p.c.k, pg, kv_head, key0, sp.to, vo, dst);
+    L::request(p.c, p.c.v, pg, kv_head, key0, sp.to, vo, dst + TILEB);
+    if (lane == 0) pages_there[tile & 1][wave] = pg >= 0;
+  };
+  Running<NB> run;
+  int pg = page(sp.from + wave * GROUP);
+  if (tiles > 0) request(0, pg);
+  for (int t = 0; t < tiles; ++t) {
+    const int key0 = sp.from + t * KT;
+    pg = t + 1 < tiles ? page(key0 + KT + wave * GROUP) : -1;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();  // the tile is complete; nobody reads the other buffer any more
+    if (t + 1 < tiles) request(t + 1, pg);
+    if (key0 > pos_hi || (p.window > 0 && key0 + KT - 1 <= pos_lo - p.window) || w0 > m_last) continue;  // nothing for this wavefront
+    const unsigned char* Kb = lds + (t & 1) * (2 * TILEB);
+    const int* there = pages_there[t & 1];
+    f32x16 sc[2];
+    sc[0] = L::scores(Kb, ad, q);
+    sc[1] = L::scores(Kb + L::BLOCKB, ad, q);
+    const bool plain = (there[0] & there[1] & there[2] & there[3]) && key0 + KT <= sp.to && key0 + KT - 1 <= pos_lo && (p.window == 0 || key0 > pos_hi - p.window);
+    if (!plain) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int j = b * KB + L::key_of(e, fh), key = key0 + j;
+          const bool ok = key < sp.to && sees(key, at.pos, of.total, p.window) && there[j / GROUP];
+          sc[b][e] = ok ? sc[b][e] : -INFINITY;
+        }
+    }
+    run.take(sc, p.scale_log2e);
+    L::values(run.o, Kb + TILEB, ad, sc[0], lane);
+    L::values(run.o, Kb + TILEB + L::BLOCKB, ad, sc[1], lane);
+  }
+  run.l += __shfl_xor(run.l, 32, 64);
+  if (!at.ok) return;
+  if (sp.direct) {
+    const float inv = run.l > 0.f || run.l != run.l ? 1.0f / run.l : 0.f;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const int c = nb * 32 + 8 * g + 4 * fh;
+        if (c < p.c.head_dim) {
+          Vec<T, 4> o;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o.v[e] = from_f32<T>(run.o[nb][4 * g + e] * inv);
+          *reinterpret_cast<Vec<T, 4>*>((T*)p.out + at.row * p.ldo + (int64_t)at.head * p.c.head_dim + c) = o;
+        }
+      }
+    if (fh == 0 && p.lse) p.lse[at.row * p.heads + at.head] = run.m + __builtin_amdgcn_logf(run.l);
+  } else {
+    const int64_t to = (at.row * p.heads + at.head) * p.split + part;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<f32x4*>(p.part + to * HD + nb * 32 + 8 * g + 4 * fh) =
+            f32x4{run.o[nb][4 * g], run.o[nb][4 * g + 1], run.o[nb][4 * g + 2], run.o[nb][4 * g + 3]};
+    if (fh == 0) p.part_ml[to] = make_float2(run.m, run.l);
+  }
+}
+
+// ---- parts of rows whose keys were split ----
+// One wavefront a row and head.  few, many: the two kernels' arguments (split 1: it did not split).
+template <typename T, int HD>
+__global__ void __launch_bounds__(256) join_k(Args few, Args many) {
+  const int lane = threadIdx.x & 63;
+  const int64_t i = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int head = (int)(i % few.heads);
+  const int64_t of_tokens = i / few.heads;
+  if (of_tokens >= (int64_t)few.c.sequences * few.max_new) return;
+  const int s = (int)(of_tokens / few.max_new), token = (int)(of_tokens % few.max_new);
+  const CacheSeq of = cache_seq(few.c, s, few.rows, few.max_new);
+  if (token >= of.fresh) return;
+  const bool is_few = of.fresh * few.group <= few.few_upto;
+  const Args& p = is_few ? few : many;
+  const int kv_head = head / p.group, m = token * p.group + head % p.group;
+  int t0 = 0, t1 = of.fresh - 1, from, to;
+  if (!is_few) {
+    const int block = m / 128;
+    t0 = block * 128 / p.group;
+    t1 = min(of.fresh * p.group, block * 128 + 128) - 1;
+    t1 /= p.group;
+  }
+  keys_of(of, t0, t1, p.window, from, to);
+  const int n = parts_of(from, to, p.split, p.chunk);
+  if (n == 1) return;
+  const int64_t row = of.row0 + token;
+  const int64_t first = is_few ? ((int64_t)s * p.c.kv_heads + kv_head) * p.split * FEW + m : (row * p.heads + head) * p.split;
+  const int64_t step = is_few ? FEW : 1;
+  float top = -INFINITY;
+  for (int k = 0; k < n; ++k) top = fmaxf(top, p.part_ml[first + k * step].x);
+  const float ref = top == -INFINITY ? 0.f : top;
+  float l = 0.f, o[HD / 64];
+#pragma unroll
+  for (int c = 0; c < HD / 64; ++c) o[c] = 0.f;
+  for (int k = 0; k < n; ++k) {
+    const int64_t at = first + k * step;
+    const float by = __builtin_amdgcn_exp2f(p.part_ml[at].x - ref);
+    l = fmaf(by, p.part_ml[at].y, l);
+#pragma unroll
+    for (int c = 0; c < HD / 64; ++c) o[c] = fmaf(by, p.part[at * HD + c * 64 + lane], o[c]);
+  }
+  RowAt r;
+  r.row = row; r.head = head;
+#pragma unroll
+  for (int c = 0; c < HD / 64; ++c) store_out<T>(p, r, c * 64 + lane, l > 0.f || l != l ? o[c] / l : 0.f);
+  if (lane == 0 && p.lse) p.lse[row * p.heads + head] = top + __builtin_amdgcn_logf(l);
+}
+
+// ---- host ----
+struct Plan {
+  int few_split, few_chunk, many_split, many_chunk, row_blocks;
+  bool few, many;
+  int64_t few_parts, many_parts;  // rows of partial sums
+};
+int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+Plan plan_of(const CacheView& c, int64_t rows, int heads, int max_new, int64_t max_length, int window) {
+  Plan p{};
+  const int group = heads / c.kv_heads;
+  const int64_t most = (int64_t)max_new * group;  // rows of the longest sequence
+  p.many = most > FEW;
+  p.few = !p.many || rows < (int64_t)c.sequences * max_new;  // else no sequence is short where the longest is not, as a rule; many_k takes any
+  p.row_blocks = (int)std::max<int64_t>(1, up(most, 128));
+  int64_t span = std::max<int64_t>(1, std::min<int64_t>(max_length, (int64_t)c.max_pages << c.page_shift));
+  if (window > 0) span = std::min<int64_t>(span, (int64_t)window + max_new + KB);
+  auto split = [&](int64_t items, int64_t want, int64_t least, int& n, int& chunk) {
+    const int64_t k = std::max<int64_t>(1, std::min<int64_t>({up(want, std::max<int64_t>(items, 1)), up(span, least), 64}));
+    chunk = (int)(up(up(span, k), 128) * 128);
+    n = (int)up(span, chunk);
+  };
+  split((int64_t)c.sequences * c.kv_heads, 4096, 256, p.few_split, p.few_chunk);
+  split((int64_t)c.kv_heads * (up(rows * group, 128) + c.sequences - 1), 512, 512, p.many_split, p.many_chunk);
+  if (!p.few) p.few_split = 1;
+  if (!p.many) p.many_split = 1;
+  p.few_parts = p.few_split > 1 ? (int64_t)c.sequences * c.kv_heads * p.few_split * FEW : 0;
+  p.many_parts = p.many_split > 1 ? rows * heads * p.many_split : 0;
+  return p;
+}
+
+template <typename T, int HD>
+hipError_t launch(const Plan& pl, Args a, float* workspace, hipStream_t st) {
+  typedef Tile<T, HD> L;
+  a.few_upto = pl.few ? FEW : 0;
+  Args few = a, many = a;
+  const int64_t n = pl.few_parts + pl.many_parts;
+  few.split = pl.few_split; few.chunk = pl.few_chunk; few.part = workspace; few.part_ml = (float2*)(workspace + n * HD);
+  many.split = pl.many_split; many.chunk = pl.many_chunk; many.part = workspace + pl.few_parts * HD; many.part_ml = few.part_ml + pl.few_parts;
+  many.row_blocks = pl.row_blocks;
+  const int64_t pairs = (int64_t)a.c.sequences * a.c.kv_heads;
+  const int64_t few_grid = pairs * pl.few_split, many_grid = pairs * pl.row_blocks * pl.many_split, join_grid = up((int64_t)a.c.sequences * a.max_new * a.heads, 4);
+  if (few_grid > 0x7FFFFFFF || many_grid > 0x7FFFFFFF || join_grid > 0x7FFFFFFF) return hipErrorInvalidValue;
+  constexpr int FEW_LDS = 4 * 2 * L::BLOCKB, MANY_LDS = 2 * 2 * 2 * L::BLOCKB;
+  static_assert(4 * FEW * HD * 4 <= FEW_LDS, "the wavefronts' sums fit where their tiles were");
+  static bool attr_done = false;  // one flag per instantiation
+  if (!attr_done) {
+    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(many_k<T, HD>), hipFuncAttributeMaxDynamicSharedMemorySize, MANY_LDS);
+    if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(few_k<T, HD>), hipFuncAttributeMaxDynamicSharedMemorySize, FEW_LDS);
+    if (e != hipSuccess) return e;
+    attr_done = true;
+  }
+  if (pl.many) {
+    many_k<T, HD><<<(unsigned)many_grid, 256, MANY_LDS, st>>>(many);
+  }
+  if (pl.few) {
+    few_k<T, HD><<<(unsigned)few_grid, 256, FEW_LDS, st>>>(few);
+  }
+  if (n > 0) join_k<T, HD><<<(unsigned)join_grid, 256, 0, st>>>(few, many);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t attention_paged_bytes(const CacheView& c, int64_t rows, int heads, int max_new, int64_t max_length, int window) {
+  if (rows == 0 || c.sequences == 0 || max_new == 0) return 0;
+  const Plan p = plan_of(c, rows, heads, max_new, max_length, window);
+  return (size_t)(p.few_parts + p.many_parts) * ((c.head_dim <= 64 ? 64 : 128) * 4 + 8);
+}
+
+hipError_t attention_paged(int dt, const CacheView& c, int heads, int64_t rows, int max_new, int64_t max_length, int window, float scale, const void* q, int64_t ldq,
+                           void* out, int64_t ldo, float* lse, void* workspace, hipStream_t st) {
+  if (rows == 0 || c.sequences == 0 || max_new == 0) return hipSuccess;
+  const Plan pl = plan_of(c, rows, heads, max_new, max_length, window);
+  Args a{};
+  a.c = c; a.heads = heads; a.group = heads / c.kv_heads;
+  a.rows = rows; a.ldq = ldq; a.ldo = ldo; a.max_new = max_new; a.window = window;
+  a.scale_log2e = scale * 1.4426950408889634f;
+  a.q = q; a.out = out; a.lse = lse;
+  float* ws = (float*)workspace;
+  if (dt == DT_BF16) return c.head_dim <= 64 ? launch<bf16, 64>(pl, a, ws, st) : launch<bf16, 128>(pl, a, ws, st);
+  return c.head_dim <= 64 ? launch<float, 64>(pl, a, ws, st) : launch<float, 128>(pl, a, ws, st);
+}
+
+}  // namespace hift

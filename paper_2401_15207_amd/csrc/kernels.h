@@ -251,4 +251,41 @@ bool ns_coefficients_hold(const double (&co)[3], int steps);  // the singular va
 size_t ns_workspace(const NsItem* items, int count);          // bytes; newton_schulz wants them 16-byte aligned
 hipError_t newton_schulz(const NsItem* items, int count, int dt_src, int dt_dst, const NsRun& run, void* workspace, hipStream_t st);
 
+// ---- answers ----
+// Rotary positions (rotary.hip).  Table: [count, rot / 2] pairs amplitude (cos, sin) of positions first ..; turns: whole turns a position by pair.
+constexpr int ROTARY_ROT_MAX = 256;
+hipError_t rotary_table(int rot, const double* turns, double amplitude, int64_t first, int64_t count, float* cos_sin, hipStream_t st);
+// Rows of `heads` heads side by side; the first rot columns of each turn by the table's entry for positions[row] (null: row % seq), the others
+// are copied.  pairs: (2 i, 2 i + 1), else (i, i + rot / 2).  y may be x.
+hipError_t rotary(int dt, bool pairs, bool backward, int64_t rows, int heads, int hd, int rot, const void* x, int64_t ldx, void* y, int64_t ldy,
+                  const int32_t* positions, int seq, const float* cos_sin, int table_rows, hipStream_t st);
+// A paged cache: page n of k and v is [kv_heads][page][head_dim], page_stride elements from the one before; pages: the sequences' page numbers;
+// sequence s has lengths[s] tokens and brings the rows [starts[s], starts[s + 1]).
+struct CacheView {
+  void *k, *v;
+  int64_t page_stride;
+  int n_pages, page, page_shift, kv_heads, head_dim, sequences, max_pages;
+  const int32_t* pages;
+  int64_t pages_ld;
+  const int32_t *lengths, *starts;
+};
+// rows q | k | v of a fused projection: q rotated to `q` (null: not wanted), k rotated and v to their pages; rot 0: no rotation
+hipError_t cache_append(int dt, const CacheView& c, int heads, bool pairs, int rot, const float* cos_sin, int table_rows, int64_t rows, int max_new,
+                        const void* qkv, int64_t ld, void* q, int64_t ldq, hipStream_t st);
+// attention of the new rows over the cache (attention_paged.hip)
+size_t attention_paged_bytes(const CacheView& c, int64_t rows, int heads, int max_new, int64_t max_length, int window);
+hipError_t attention_paged(int dt, const CacheView& c, int heads, int64_t rows, int max_new, int64_t max_length, int window, float scale, const void* q, int64_t ldq,
+                           void* out, int64_t ldo, float* lse, void* workspace, hipStream_t st);
+// logits with penalties for seen tokens, bias and mask, or the gradient g through them (adjust.hip)
+struct AdjustBy {
+  const int32_t* tokens;
+  int64_t n_tokens;
+  const int64_t *begin, *end;
+  float repetition, presence, frequency;
+  const float* bias; int64_t ld_bias;
+  const uint32_t* allowed; int64_t ld_allowed;
+};
+hipError_t adjust_logits(int dt, bool backward, int64_t rows, int V, int64_t ld, const void* x, const AdjustBy& by, int64_t ldg, const void* g, int64_t ldo,
+                         void* out, hipStream_t st);
+
 }  // namespace hift

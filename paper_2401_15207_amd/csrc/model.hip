@@ -2822,4 +2822,181 @@ hift_status hift_kernel_muon(const hift_opt* opt, int32_t count, const hift_muon
   return HIFT_OK;
 }
 
+// ---- answers ----
+namespace {
+int64_t size_of(int32_t dtype) { return dtype == HIFT_BF16 ? 2 : 4; }
+bool pieces16(const void* p, int64_t ld, int64_t es) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld * es % 16 == 0; }
+
+hift_status check_table(int32_t layout, int32_t rot, int32_t head_dim, const float* cos_sin, int64_t table_rows) {
+  if (layout != HIFT_ROTARY_HALVES && layout != HIFT_ROTARY_PAIRS) return fail(HIFT_EINVAL, "layout unknown");
+  if (rot < 2 || rot % 2 || rot > head_dim || rot > ROTARY_ROT_MAX) return fail(HIFT_EINVAL, "rot must be even, in [2, min(head_dim, %d)]", ROTARY_ROT_MAX);
+  if (!cos_sin || reinterpret_cast<uintptr_t>(cos_sin) % 8) return fail(HIFT_EINVAL, "cos_sin null or not 8-byte aligned");
+  if (table_rows < 1 || table_rows > INT32_MAX) return fail(HIFT_EINVAL, "table_rows must be in [1, 2^31)");
+  return HIFT_OK;
+}
+
+// The cache and the new rows of a call; starts may be null where only sizes matter.
+hift_status cache_view(const hift_cache* c, int64_t rows, const int32_t* starts, int32_t max_new, int32_t heads, CacheView* out) {
+  if (!c) return fail(HIFT_EINVAL, "cache is null");
+  if (c->dtype != HIFT_F32 && c->dtype != HIFT_BF16) return fail(HIFT_EINVAL, "dtype unknown");
+  const int64_t es = size_of(c->dtype);
+  if (c->head_dim < 1 || c->head_dim > 128 || c->head_dim * es % 16) return fail(HIFT_EINVAL, "head_dim must be whole 16-byte pieces and at most 128");
+  if (c->page < 16 || c->page > 65536 || (c->page & (c->page - 1))) return fail(HIFT_EINVAL, "page must be a power of two in [16, 65536]");
+  if (c->kv_heads < 1 || heads < 1 || heads % c->kv_heads || heads > 65536) return fail(HIFT_EINVAL, "heads must be a multiple of kv_heads, at most 65536");
+  if (c->n_pages < 0 || c->sequences < 0 || c->max_pages < 0) return fail(HIFT_EINVAL, "negative size");
+  if ((int64_t)c->max_pages * c->page > int64_t(1) << 30) return fail(HIFT_EINVAL, "sequences of at most 2^30 tokens");
+  if (c->page_stride < (int64_t)c->kv_heads * c->page * c->head_dim || c->page_stride * es % 16)
+    return fail(HIFT_EINVAL, "page_stride is shorter than a page or not whole 16-byte pieces");
+  if (c->n_pages > 0 && (!c->k || !c->v || !pieces16(c->k, 0, es) || !pieces16(c->v, 0, es))) return fail(HIFT_EINVAL, "k or v null or not 16-byte aligned");
+  if (c->sequences > 0 && c->max_pages > 0 && (!c->pages || (c->sequences > 1 && c->pages_ld < c->max_pages)))
+    return fail(HIFT_EINVAL, "pages null, or its rows shorter than max_pages");
+  if (rows < 0 || rows > int64_t(1) << 30 || max_new < 0) return fail(HIFT_EINVAL, "bad shape: %lld new rows, at most %d a sequence", (long long)rows, max_new);
+  if ((int64_t)c->sequences * std::min<int64_t>(max_new, rows) * heads > INT32_MAX)
+    return fail(HIFT_EINVAL, "%d sequences of up to %d new rows and %d heads are too many for one call", c->sequences, max_new, heads);
+  if (c->sequences > 0 && rows > 0 && !c->lengths) return fail(HIFT_EINVAL, "lengths are null");
+  CacheView v{};
+  v.k = c->k; v.v = c->v; v.page_stride = c->page_stride; v.n_pages = c->n_pages; v.page = c->page;
+  v.page_shift = __builtin_ctz((unsigned)c->page);
+  v.kv_heads = c->kv_heads; v.head_dim = c->head_dim; v.sequences = c->sequences; v.max_pages = c->max_pages;
+  v.pages = c->pages; v.pages_ld = c->pages_ld; v.lengths = c->lengths; v.starts = starts;
+  *out = v;
+  return HIFT_OK;
+}
+
+hift_status check_adjust(int32_t dtype, int64_t rows, int32_t V, int64_t ld, const void* logits, const hift_adjust* by, AdjustBy* out) {
+  ST_TRY(check_logits(dtype, rows, V, ld, logits, 1.f));
+  if (!by) return fail(HIFT_EINVAL, "by is null");
+  if (rows * ((V + 8191) / 8192) > INT32_MAX) return fail(HIFT_EINVAL, "%lld rows of %d entries are too many for one call", (long long)rows, V);
+  if (!(by->repetition >= 0x1p-60f && by->repetition <= 0x1p60f)) return fail(HIFT_EINVAL, "repetition must be in [2^-60, 2^60]");
+  if (!std::isfinite(by->presence) || !std::isfinite(by->frequency)) return fail(HIFT_EINVAL, "presence and frequency must be finite");
+  if (by->n_tokens < 0 || (by->tokens && (!by->begin || !by->end))) return fail(HIFT_EINVAL, "tokens need begin and end, and a count");
+  if (by->bias && by->ld_bias != 0 && by->ld_bias < V) return fail(HIFT_EINVAL, "rows of the bias overlap");
+  if (by->allowed && by->ld_allowed != 0 && by->ld_allowed < (V + 31) / 32) return fail(HIFT_EINVAL, "rows of the mask overlap");
+  if ((reinterpret_cast<uintptr_t>(by->tokens) | reinterpret_cast<uintptr_t>(by->bias) | reinterpret_cast<uintptr_t>(by->allowed)) % 4 ||
+      (reinterpret_cast<uintptr_t>(by->begin) | reinterpret_cast<uintptr_t>(by->end)) % 8)
+    return fail(HIFT_EINVAL, "tokens, begin, end, bias or allowed do not lie on whole elements");
+  *out = AdjustBy{by->tokens, by->n_tokens, by->begin, by->end, by->repetition, by->presence, by->frequency, by->bias, by->ld_bias, by->allowed, by->ld_allowed};
+  return HIFT_OK;
+}
+}  // namespace
+
+hift_status hift_kernel_rotary_table(const hift_rotary* r, int64_t first, int64_t count, float* cos_sin, void* stream) {
+  if (!r) return fail(HIFT_EINVAL, "rotary is null");
+  if (r->rot < 2 || r->rot % 2 || r->rot > ROTARY_ROT_MAX) return fail(HIFT_EINVAL, "rot must be even, in [2, %d]", ROTARY_ROT_MAX);
+  if (r->scaling < HIFT_ROTARY_PLAIN || r->scaling > HIFT_ROTARY_PARTS) return fail(HIFT_EINVAL, "scaling unknown");
+  const auto positive = [](double v) { return v > 0.0 && std::isfinite(v); };
+  if (!(r->base >= 1.0 && r->base <= 1e18) || !positive(r->amplitude)) return fail(HIFT_EINVAL, "base must be in [1, 1e18] and amplitude positive");
+  if (r->scaling != HIFT_ROTARY_PLAIN && !(r->factor >= 1.0 && r->factor <= 1e9)) return fail(HIFT_EINVAL, "factor must be in [1, 1e9]");
+  if (r->scaling == HIFT_ROTARY_BASE && r->rot < 4) return fail(HIFT_EINVAL, "a scaled base needs rot > 2");
+  if (r->scaling == HIFT_ROTARY_PARTS && (!positive(r->trained) || !std::isfinite(r->slow) || !std::isfinite(r->fast) || !(r->fast > r->slow)))
+    return fail(HIFT_EINVAL, "trained must be positive and fast above slow");
+  if (first < 0 || count < 0 || first > int64_t(1) << 30 || count > (int64_t(1) << 30) - first) return fail(HIFT_EINVAL, "positions outside [0, 2^30)");
+  if (count > 0 && (!cos_sin || reinterpret_cast<uintptr_t>(cos_sin) % 8)) return fail(HIFT_EINVAL, "cos_sin null or not 8-byte aligned");
+  const double two_pi = 6.283185307179586476925;
+  const double base = r->scaling == HIFT_ROTARY_BASE ? r->base * std::pow(r->factor, r->rot / (r->rot - 2.0)) : r->base;
+  double turns[ROTARY_ROT_MAX / 2];
+  for (int i = 0; i < r->rot / 2; ++i) {
+    double rate = std::pow(base, -2.0 * i / r->rot);
+    if (r->scaling == HIFT_ROTARY_LINEAR) rate /= r->factor;
+    if (r->scaling == HIFT_ROTARY_PARTS) {
+      const double keep = std::min(1.0, std::max(0.0, (r->trained * rate / two_pi - r->slow) / (r->fast - r->slow)));
+      rate *= keep + (1.0 - keep) / r->factor;
+    }
+    turns[i] = rate / two_pi;
+  }
+  HIP_TRY(rotary_table(r->rot, turns, r->amplitude, first, count, cos_sin, (hipStream_t)stream));
+  return HIFT_OK;
+}
+
+hift_status hift_kernel_rotary(int32_t dtype, int32_t layout, int32_t backward, int64_t rows, int32_t heads, int32_t head_dim, int32_t rot, const void* x,
+                               int64_t ldx, void* y, int64_t ldy, const int32_t* positions, int32_t seq, const float* cos_sin, int64_t table_rows, void* stream) {
+  if (dtype != HIFT_F32 && dtype != HIFT_BF16) return fail(HIFT_EINVAL, "dtype unknown");
+  const int64_t width = (int64_t)heads * head_dim;
+  if (rows < 0 || rows > INT32_MAX || heads < 0 || head_dim < 2 || width > int64_t(1) << 24)
+    return fail(HIFT_EINVAL, "bad shape: %lld rows of %d heads of %d", (long long)rows, heads, head_dim);
+  if (ldx < width || ldy < width) return fail(HIFT_EINVAL, "a leading dimension is shorter than the rows it strides over");
+  ST_TRY(check_table(layout, rot, head_dim, cos_sin, table_rows));
+  if (!positions && (seq < 1 || seq > table_rows)) return fail(HIFT_EINVAL, "without positions, seq must be in [1, table_rows]");
+  if (rows > 0 && heads > 0 && (!x || !y)) return fail(HIFT_EINVAL, "x or y null");
+  if ((reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(y)) % (uintptr_t)size_of(dtype) || reinterpret_cast<uintptr_t>(positions) % 4)
+    return fail(HIFT_EINVAL, "x, y or positions do not lie on whole elements");
+  if (x == y && ldx != ldy) return fail(HIFT_EINVAL, "in place the rows lie where they were (ldy = ldx)");
+  HIP_TRY(rotary(dtype == HIFT_BF16 ? DT_BF16 : DT_F32, layout == HIFT_ROTARY_PAIRS, backward != 0, rows, heads, head_dim, rot, x, ldx, y, ldy, positions, seq, cos_sin,
+                 (int)table_rows, (hipStream_t)stream));
+  return HIFT_OK;
+}
+
+hift_status hift_kernel_cache_append(const hift_cache* cache, int64_t rows, const int32_t* starts, int32_t max_new, int32_t heads, int32_t layout, int32_t rot,
+                                     const float* cos_sin, int64_t table_rows, const void* qkv, int64_t ld, void* q_out, int64_t ldq, void* stream) {
+  CacheView c;
+  ST_TRY(cache_view(cache, rows, starts, max_new, heads, &c));
+  if (rot != 0) ST_TRY(check_table(layout, rot, c.head_dim, cos_sin, table_rows));
+  const int64_t es = size_of(cache->dtype), width = (int64_t)(heads + 2 * (int64_t)c.kv_heads) * c.head_dim;
+  if (ld < width || (q_out && ldq < (int64_t)heads * c.head_dim)) return fail(HIFT_EINVAL, "a leading dimension is shorter than the rows it strides over");
+  if (rows == 0 || c.sequences == 0 || max_new == 0) return HIFT_OK;
+  if (!starts || !qkv) return fail(HIFT_EINVAL, "starts or qkv null");
+  if (!pieces16(qkv, ld, es) || (q_out && !pieces16(q_out, ldq, es))) return fail(HIFT_EINVAL, "qkv and q_out must be 16-byte aligned, their rows whole 16-byte pieces apart");
+  if (q_out == qkv && ldq != ld) return fail(HIFT_EINVAL, "in place the rows lie where they were (ldq = ld)");
+  HIP_TRY(cache_append(cache->dtype == HIFT_BF16 ? DT_BF16 : DT_F32, c, heads, layout == HIFT_ROTARY_PAIRS, rot, cos_sin, (int)table_rows, rows,
+                       (int)std::min<int64_t>(max_new, rows), qkv, ld, q_out, ldq, (hipStream_t)stream));
+  return HIFT_OK;
+}
+
+hift_status hift_kernel_attention_paged_bytes(const hift_cache* cache, int64_t rows, int32_t max_new, int64_t max_length, int32_t heads, int32_t window, size_t* bytes) {
+  if (!bytes) return fail(HIFT_EINVAL, "bytes is null");
+  CacheView c;
+  ST_TRY(cache_view(cache, rows, nullptr, max_new, heads, &c));
+  if (max_length < 0 || window < 0) return fail(HIFT_EINVAL, "negative max_length or window");
+  *bytes = attention_paged_bytes(c, rows, heads, (int)std::min<int64_t>(max_new, rows), max_length, window);
+  return HIFT_OK;
+}
+
+hift_status hift_kernel_attention_paged(const hift_cache* cache, int64_t rows, const int32_t* starts, int32_t max_new, int64_t max_length, int32_t heads,
+                                        int32_t window, float scale, const void* q, int64_t ldq, void* out, int64_t ldo, float* lse, void* workspace,
+                                        size_t workspace_bytes, void* stream) {
+  size_t need = 0;
+  ST_TRY(hift_kernel_attention_paged_bytes(cache, rows, max_new, max_length, heads, window, &need));
+  CacheView c;
+  ST_TRY(cache_view(cache, rows, starts, max_new, heads, &c));
+  if (!(scale > 0.f) || std::isinf(scale)) return fail(HIFT_EINVAL, "scale must be positive and finite");
+  const int64_t es = size_of(cache->dtype), width = (int64_t)heads * c.head_dim;
+  if (ldq < width || ldo < width) return fail(HIFT_EINVAL, "a leading dimension is shorter than the rows it strides over");
+  if (rows == 0 || c.sequences == 0 || max_new == 0) return HIFT_OK;
+  if (!starts || !q || !out) return fail(HIFT_EINVAL, "starts, q or out null");
+  if (!pieces16(q, ldq, es) || !pieces16(out, ldo, es)) return fail(HIFT_EINVAL, "q and out must be 16-byte aligned, their rows whole 16-byte pieces apart");
+  if (q == out && ldq != ldo) return fail(HIFT_EINVAL, "in place the rows lie where they were (ldo = ldq)");
+  if (reinterpret_cast<uintptr_t>(lse) % 4) return fail(HIFT_EINVAL, "lse does not lie on whole elements");
+  if (need > 0 && (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 15)))
+    return fail(HIFT_EINVAL, "workspace of %zu bytes, 16-byte aligned, expected", need);
+  HIP_TRY(attention_paged(cache->dtype == HIFT_BF16 ? DT_BF16 : DT_F32, c, heads, rows, (int)std::min<int64_t>(max_new, rows), max_length, window, scale, q, ldq, out, ldo,
+                          lse, workspace, (hipStream_t)stream));
+  return HIFT_OK;
+}
+
+hift_status hift_kernel_adjust_logits(int32_t dtype, int64_t rows, int32_t V, int64_t ld, const void* logits, const hift_adjust* by, int64_t ldo, void* out,
+                                      void* stream) {
+  AdjustBy a;
+  ST_TRY(check_adjust(dtype, rows, V, ld, logits, by, &a));
+  if (ldo < V) return fail(HIFT_EINVAL, "rows of out are %lld apart and %d long", (long long)ldo, V);
+  if (rows > 0 && !out) return fail(HIFT_EINVAL, "out is null");
+  if (reinterpret_cast<uintptr_t>(out) % (uintptr_t)size_of(dtype)) return fail(HIFT_EINVAL, "out does not lie on whole elements");
+  if (out == logits && ldo != ld) return fail(HIFT_EINVAL, "in place the rows lie where they were (ldo = ld)");
+  HIP_TRY(adjust_logits(dtype == HIFT_BF16 ? DT_BF16 : DT_F32, false, rows, V, ld, logits, a, 0, nullptr, ldo, out, (hipStream_t)stream));
+  return HIFT_OK;
+}
+
+hift_status hift_kernel_adjust_logits_bwd(int32_t dtype, int64_t rows, int32_t V, int64_t ld, const void* logits, const hift_adjust* by, int64_t ldd_out,
+                                          const void* d_out, int64_t ldd, void* d_logits, void* stream) {
+  AdjustBy a;
+  ST_TRY(check_adjust(dtype, rows, V, ld, logits, by, &a));
+  if (ldd_out < V || ldd < V) return fail(HIFT_EINVAL, "rows of the gradients are %lld and %lld apart and %d long", (long long)ldd_out, (long long)ldd, V);
+  if (rows > 0 && (!d_out || !d_logits)) return fail(HIFT_EINVAL, "d_out or d_logits null");
+  if ((reinterpret_cast<uintptr_t>(d_out) | reinterpret_cast<uintptr_t>(d_logits)) % (uintptr_t)size_of(dtype))
+    return fail(HIFT_EINVAL, "the gradients do not lie on whole elements");
+  if (rows > 0 && d_logits == logits) return fail(HIFT_EINVAL, "the gradient may not take the logits' place");
+  if (d_logits == d_out && ldd != ldd_out) return fail(HIFT_EINVAL, "in place the rows lie where they were (ldd = ldd_out)");
+  HIP_TRY(adjust_logits(dtype == HIFT_BF16 ? DT_BF16 : DT_F32, true, rows, V, ld, logits, a, ldd_out, d_out, ldd, d_logits, (hipStream_t)stream));
+  return HIFT_OK;
+}
+
 }  // extern "C"
