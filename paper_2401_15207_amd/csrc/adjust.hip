@@ -21,6 +21,7 @@ namespace {
 
 constexpr int BLK = 256;
 constexpr int LOOSE = 8;  // elements before the first aligned piece: at most 7
+constexpr int U = 4;      // pieces of 16 bytes of a thread, at most
 
 struct AdjustArgs {
   int V, slice, slices;
@@ -56,7 +57,7 @@ __device__ __forceinline__ float adjusted(float x, float g, int n, float bias, b
 template <typename T, bool BWD>
 __global__ void __launch_bounds__(BLK) adjust_k(AdjustArgs p) {
   extern __shared__ int4 count_quads[];
-  int* counts = reinterpret_cast<int*>(count_quads);  // [LOOSE + slice], the first aligned piece's at LOOSE
+  int* counts = reinterpret_cast<int*>(count_quads);  // [LOOSE + slice] in whole quads, the first aligned piece's at LOOSE
   __shared__ int any;
   constexpr int E = 16 / (int)sizeof(T);
   const int64_t row = blockIdx.x / (unsigned)p.slices;
@@ -71,13 +72,19 @@ __global__ void __launch_bounds__(BLK) adjust_k(AdjustArgs p) {
   const int n = hi - lo;
   if (n <= 0) return;
   const int from = part ? lo : head, shift = LOOSE - (from - lo);  // counts[shift + j - lo] is element j's
-  const int t = threadIdx.x;
+  const int t = threadIdx.x, pieces = p.aligned ? (hi - from) / E : 0;
+  // what the pass streams is on its way while the history is counted
+  typedef Vec<T, E> P;
+  P in[U];
+#pragma unroll
+  for (int k = 0; k < U; ++k)
+    if (t + k * BLK < pieces) in[k] = *reinterpret_cast<const P*>((BWD ? g : x) + from + (t + k * BLK) * E);
   bool seen = false;
   if (p.tokens) {
     const int64_t b = min(max(p.begin[row], (int64_t)0), p.n_tokens), e = min(max(p.end[row], b), p.n_tokens);
     if (e > b) {
       if (t == 0) any = 0;
-      for (int i = t; i < n; i += BLK) counts[shift + i] = 0;
+      for (int i = t; i < (shift + n + 3) / 4; i += BLK) count_quads[i] = make_int4(0, 0, 0, 0);
       __syncthreads();
       int mine = 0;
       for (int64_t i = b + t; i < e; i += BLK) {
@@ -103,11 +110,11 @@ __global__ void __launch_bounds__(BLK) adjust_k(AdjustArgs p) {
     for (int j = lo + t; j < hi; j += BLK) one(j);
     return;
   }
-  const int pieces = (hi - from) / E;
-  for (int i = t; i < pieces; i += BLK) {
+#pragma unroll
+  for (int k = 0; k < U; ++k) {
+    const int i = t + k * BLK;
+    if (i >= pieces) break;
     const int j0 = from + i * E;
-    typedef Vec<T, E> P;
-    const P in = *reinterpret_cast<const P*>((BWD ? g : x) + j0);
     int c[E];
 #pragma unroll
     for (int e = 0; e < E; e += 4) {
@@ -127,7 +134,7 @@ __global__ void __launch_bounds__(BLK) adjust_k(AdjustArgs p) {
       for (int e = 0; e < E; e += 4) {
         const f32x4_any q = *reinterpret_cast<const f32x4_any*>(bias + j0 + e);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) bv[e + k] = q[k];
+        for (int z = 0; z < 4; ++z) bv[e + z] = q[z];
       }
     }
     P o;
@@ -135,10 +142,10 @@ __global__ void __launch_bounds__(BLK) adjust_k(AdjustArgs p) {
     for (int e = 0; e < E; ++e) {
       float xv = 0.f, gv = 0.f;
       if constexpr (BWD) {
-        gv = to_f32(in.v[e]);
+        gv = to_f32(in[k].v[e]);
         if (c[e] > 0) xv = to_f32(x[j0 + e]);
       } else {
-        xv = to_f32(in.v[e]);
+        xv = to_f32(in[k].v[e]);
       }
       o.v[e] = from_f32<T>(adjusted<T, BWD>(xv, gv, c[e], bv[e], bits >> e & 1, p));
     }
@@ -152,15 +159,15 @@ __global__ void __launch_bounds__(BLK) adjust_k(AdjustArgs p) {
 
 template <typename T, bool BWD>
 hipError_t run(AdjustArgs p, hipStream_t st) {
-  // Slices: 8192 entries (32 KB of counts, five workgroups a compute unit), fewer where rows are few, down to a piece a thread.
+  // Slices: U pieces a thread, fewer where rows are few, down to one.
   constexpr int E = 16 / (int)sizeof(T);
-  p.slice = 8192;
+  p.slice = U * BLK * E;
   while (p.slice > BLK * E && p.rows * ((p.V + p.slice - 1) / p.slice) < 512) p.slice /= 2;
   p.slices = (int)(((int64_t)p.V + p.slice - 1) / p.slice);
   if (p.rows * p.slices > 0x7FFFFFFF) return hipErrorInvalidValue;
   const auto low = [](const void* q) { return (int64_t)(reinterpret_cast<uintptr_t>(q) & 15); };
   p.aligned = low(p.out) == low(BWD ? p.g : p.x) && (p.ldo - (BWD ? p.ldg : p.ld)) % E == 0;
-  adjust_k<T, BWD><<<(unsigned)(p.rows * p.slices), BLK, (size_t)(p.slice + LOOSE) * 4, st>>>(p);
+  adjust_k<T, BWD><<<(unsigned)(p.rows * p.slices), BLK, (size_t)(LOOSE + p.slice + 4) * 4, st>>>(p);
   return hipGetLastError();
 }
 

@@ -6,8 +6,8 @@
 // The new rows of a sequence and the query heads that share a key head make one list of rows, m = token * group + head: it is their tile that
 // meets a tile of keys, so keys and values are read once for all heads of a group.  One pass over the keys with a running maximum and sum
 // per row (log2 domain), as in attention.hip, whose conventions for the matrix instruction's operands and for LDS tiles these kernels share.
-//   few_k    at most 32 rows: all four wavefronts of a workgroup hold the same rows and take turns at the blocks of 32 keys, each through LDS tiles
-//            of its own without any barrier, and their results are joined at the end.  Bound by reading the cache.
+//   few_k    32 rows a workgroup: all four wavefronts hold the same rows and take turns at the blocks of 32 keys, each through LDS tiles of its own
+//            without any barrier, and their results are joined at the end.  Bound by reading the cache.
 //   many_k   128 rows a workgroup, 32 a wavefront, which share tiles of 64 keys.  Bound by the matrix instructions.
 //   join_k   where the keys of a row were split over workgroups: the parts, weighted by their maxima.
 #include <math.h>
@@ -43,7 +43,7 @@ struct Args {
   void* out;
   float* lse;           // [rows, heads] or null
   int few_upto;         // sequences of at most so many rows are few_k's, the others many_k's
-  int row_blocks;       // many_k: blocks of 128 rows of the longest sequence
+  int row_blocks;       // this kernel's blocks of rows of the longest sequence
   int split, chunk;     // this kernel's workgroups along the keys, and the keys of each
   float* part;          // [..][HD] sums and, behind all of them, (maximum, sum of exponentials) pairs
   float2* part_ml;
@@ -72,16 +72,22 @@ struct Tile {
 
   // Requests 16 keys from token `key0` on (all on one page) of one of the cache's arrays into LDS; keys from `end` on, and those of a page that is
   // not there, arrive as zeros.  vo: offsets of the lane's pieces within 16 keys (see offsets).
-  __device__ static __forceinline__ void request(const CacheView& c, const void* array, int page, int kv_head, int key0, int end, const uint32_t (&vo)[IPG],
-                                                 uint32_t lds) {
-    const int slot = key0 & (c.page - 1);
-    const int64_t at = (int64_t)max(page, 0) * c.page_stride + ((int64_t)kv_head * c.page + slot) * c.head_dim;
-    const uint64_t a = reinterpret_cast<uint64_t>(array) + (uint64_t)at * sizeof(T);
+  int64_t page_bytes;
+  int head_at, slots, row_bytes;  // the head's first key within a page; slots of a page less one; bytes of a key
+  __device__ __forceinline__ Tile(const CacheView& c, int kv_head)
+      : page_bytes(c.page_stride * (int64_t)sizeof(T)), head_at(kv_head * c.page), slots(c.page - 1), row_bytes(c.head_dim * (int)sizeof(T)) {}
+  __device__ __forceinline__ void request(const void* array, int key0, int page, int end, const uint32_t (&vo)[IPG], uint32_t lds) const {
+    const uint64_t a = reinterpret_cast<uint64_t>(array) + (uint64_t)((int64_t)max(page, 0) * page_bytes + (int64_t)(head_at + (key0 & slots)) * row_bytes);
     const int n = page < 0 ? 0 : min(max(end - key0, 0), GROUP);
     const hift_u32x4 rs = {(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)a), (uint32_t)__builtin_amdgcn_readfirstlane((int)((uint32_t)(a >> 32) & 0xFFFFu)),
-                           (uint32_t)__builtin_amdgcn_readfirstlane(n * c.head_dim * (int)sizeof(T)), 0x00020000u};
+                           (uint32_t)__builtin_amdgcn_readfirstlane(n * row_bytes), 0x00020000u};
 #pragma unroll
     for (int i = 0; i < IPG; ++i) load_to_lds_b128(rs, lds + i * 1024, vo[i], 0);
+  }
+  // 32 keys, on one page or two
+  __device__ __forceinline__ void request(const void* array, int key0, int pa, int pb, int end, const uint32_t (&vo)[IPG], uint32_t lds) const {
+    request(array, key0, pa, end, vo, lds);
+    request(array, key0 + GROUP, pb, end, vo, lds + GROUP * ROWB);
   }
   __device__ static __forceinline__ void offsets(uint32_t (&vo)[IPG], int lane, int head_dim) {
 #pragma unroll
@@ -253,7 +259,17 @@ __device__ __forceinline__ RowAt row_at(const Args& p, const CacheSeq& of, int k
   return r;
 }
 
-__device__ __forceinline__ bool sees(int key, int pos, int total, int window) { return key <= pos && key < total && (window == 0 || key > pos - window); }
+// Scores of keys that the lane's row does not see become -inf.  a, b: whether the pages of the block's halves are there.
+template <class L>
+__device__ __forceinline__ void mask_scores(f32x16& s, int key0, int fh, int end, int pos, int total, int window, bool a, bool b) {
+  const int last = min(min(pos, total - 1), end - 1) - key0, first = window > 0 ? pos - window + 1 - key0 : -1;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    const int j = L::key_of(e, 0) + (L::key_of(0, 1) - L::key_of(0, 0)) * fh;
+    const bool ok = (j <= last) & (j >= first) & (L::key_of(e, 0) < GROUP ? a : b);
+    s[e] = ok ? s[e] : -INFINITY;
+  }
+}
 
 template <typename T>
 __device__ __forceinline__ void store_out(const Args& p, const RowAt& r, int c, float v) {
@@ -261,6 +277,8 @@ __device__ __forceinline__ void store_out(const Args& p, const RowAt& r, int c, 
 }
 
 // ---- few rows ----
+constexpr int PAGED = 64 * GROUP;  // keys whose page numbers a wavefront holds, a lane each 16
+
 template <typename T, int HD>
 __global__ void __launch_bounds__(256) few_k(Args p) {
   typedef Tile<T, HD> L;
@@ -268,15 +286,22 @@ __global__ void __launch_bounds__(256) few_k(Args p) {
   extern __shared__ unsigned char lds[];       // [wave][K | V] blocks; at the end [wave][row][HD] sums
   __shared__ float2 ml[4][FEW];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), fr = lane & 31, fh = lane >> 5;
-  const int pair = (int)(blockIdx.x / (unsigned)p.split), part = (int)(blockIdx.x % (unsigned)p.split);
+  int i = (int)blockIdx.x;
+  const int part = i % p.split;
+  i /= p.split;
+  const int block = p.row_blocks - 1 - i % p.row_blocks, pair = i / p.row_blocks;  // the rows with the most keys first
   const int s = pair / p.c.kv_heads, kv_head = pair % p.c.kv_heads;
   const CacheSeq of = cache_seq(p.c, s, p.rows, p.max_new);
-  const int n_rows = of.fresh * p.group;
-  if (n_rows == 0 || n_rows > FEW) return;
-  const Span sp = span_of(of, 0, of.fresh - 1, p.window, part, p.split, p.chunk);
+  const int all_rows = of.fresh * p.group, m0 = block * FEW, n_rows = min(all_rows - m0, FEW);
+  if (n_rows <= 0 || all_rows > p.few_upto) return;
+  const int t0 = m0 / p.group, t1 = (m0 + n_rows - 1) / p.group;  // first and last token
+  const Span sp = span_of(of, t0, t1, p.window, part, p.split, p.chunk);
   if (sp.none) return;
 
-  const RowAt at = row_at(p, of, kv_head, fr);
+  // page numbers of the keys from `from` on
+  auto pages_from = [&](int from) { return from + lane * GROUP < sp.to ? cache_page_any(p.c, s, from + lane * GROUP) : -1; };
+  int paged = sp.from, pages = pages_from(paged), pages_next = -1;
+  const RowAt at = row_at(p, of, kv_head, m0 + fr);
   typename L::Frag q[L::NQ];
   L::load_row(q, (const T*)p.q + at.row * p.ldq + (int64_t)at.head * p.c.head_dim, at.ok, p.c.head_dim, fh);
   uint32_t vo[L::IPG];
@@ -286,46 +311,45 @@ __global__ void __launch_bounds__(256) few_k(Args p) {
   unsigned char* Kb = lds + wave * (2 * L::BLOCKB);
   unsigned char* Vb = Kb + L::BLOCKB;
   const uint32_t lk = (uint32_t)reinterpret_cast<uintptr_t>(Kb), lv = (uint32_t)reinterpret_cast<uintptr_t>(Vb);
+  const L head(p.c, kv_head);
 
   const int blocks = (sp.to - sp.from + KB - 1) / KB;
-  auto page = [&](int key) { return __builtin_amdgcn_readfirstlane(key < sp.to ? cache_page(p.c, s, key) : -1); };
-  auto request = [&](const void* array, int key0, int pa, int pb, uint32_t dst) __attribute__((always_inline)) {
-    L::request(p.c, array, pa, kv_head, key0, sp.to, vo, dst);
-    L::request(p.c, array, pb, kv_head, key0 + GROUP, sp.to, vo, dst + GROUP * L::ROWB);
-  };
-  Running<NB> run;
-  int b = wave, key0 = sp.from + wave * KB;
-  int pa = -1, pb = -1;
+  int b = wave, key0 = sp.from + wave * KB, pa = -1, pb = -1;
   if (b < blocks) {
-    pa = page(key0);
-    pb = page(key0 + GROUP);
-    request(p.c.k, key0, pa, pb, lk);
-    request(p.c.v, key0, pa, pb, lv);
+    const int g = (key0 - paged) / GROUP;
+    pa = __builtin_amdgcn_readlane(pages, g);
+    pb = __builtin_amdgcn_readlane(pages, g + 1);
+    head.request(p.c.k, key0, pa, pb, sp.to, vo, lk);
+    head.request(p.c.v, key0, pa, pb, sp.to, vo, lv);
   }
+  Running<NB> run;
+  // the compiler waits for the rows here, once, and not in the loop, where it would wait for everything on its way
+#pragma unroll
+  for (int k = 0; k < L::NQ; ++k) asm volatile("" : "+v"(q[k]));
+  const int pos_lo = of.cached + t0, pos_hi = of.cached + t1;
   for (; b < blocks; b += 4, key0 += 4 * KB) {
     const bool more = b + 4 < blocks;
-    const int next = key0 + 4 * KB, na = more ? page(next) : -1, nb_ = more ? page(next + GROUP) : -1;
+    const int next = key0 + 4 * KB;
+    if (next >= paged + PAGED) {  // blocks are 4 KB keys apart, and PAGED is a multiple of that
+      paged += PAGED;
+      pages = pages_from(paged);
+    }
+    const int g = (next - paged) / GROUP;
+    const int na = more ? __builtin_amdgcn_readlane(pages, g) : -1, nb = more ? __builtin_amdgcn_readlane(pages, g + 1) : -1;
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(IPB) : "memory");  // the keys are there, their values on the way
     f32x16 sc[1];
     sc[0] = L::scores(Kb, ad, q);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    if (more) request(p.c.k, next, na, nb_, lk);
-    const bool plain = pa >= 0 && pb >= 0 && key0 + KB <= sp.to && key0 + KB - 1 <= of.cached && (p.window == 0 || key0 > of.cached + of.fresh - 1 - p.window);
-    if (!plain) {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int j = L::key_of(e, fh), key = key0 + j;
-        const bool ok = key < sp.to && sees(key, at.pos, of.total, p.window) && (j < GROUP ? pa : pb) >= 0;
-        sc[0][e] = ok ? sc[0][e] : -INFINITY;
-      }
-    }
+    if (more) head.request(p.c.k, next, na, nb, sp.to, vo, lk);
+    const bool plain = (pa | pb) >= 0 && key0 + KB <= sp.to && key0 + KB - 1 <= pos_lo && (p.window == 0 || key0 > pos_hi - p.window);
+    if (!plain) mask_scores<L>(sc[0], key0, fh, sp.to, at.pos, of.total, p.window, pa >= 0, pb >= 0);
     run.take(sc, p.scale_log2e);
     if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(IPB) : "memory");
     else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     L::values(run.o, Vb, ad, sc[0], lane);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    if (more) request(p.c.v, next, na, nb_, lv);
-    pa = na; pb = nb_;
+    if (more) head.request(p.c.v, next, na, nb, sp.to, vo, lv);
+    pa = na; pb = nb;
   }
   run.l += __shfl_xor(run.l, 32, 64);
 
@@ -356,11 +380,11 @@ __global__ void __launch_bounds__(256) few_k(Args p) {
       o = fmaf(by, sums[(w * FEW + m) * HD + c], o);
     }
     if (sp.direct) {
-      const RowAt r = row_at(p, of, kv_head, m);
+      const RowAt r = row_at(p, of, kv_head, m0 + m);
       store_out<T>(p, r, c, l > 0.f || l != l ? o / l : 0.f);
       if (c == 0 && p.lse) p.lse[r.row * p.heads + r.head] = top + __builtin_amdgcn_logf(l);
     } else {
-      const int64_t to = ((int64_t)pair * p.split + part) * FEW + m;
+      const int64_t to = (((int64_t)pair * p.row_blocks + block) * p.split + part) * FEW + m;
       p.part[to * HD + c] = o;
       if (c == 0) p.part_ml[to] = make_float2(top, l);
     }
@@ -400,11 +424,12 @@ __global__ void __launch_bounds__(256) many_k(Args p) {
   // every wavefront brings 16 keys of a tile
   auto page = [&](int key) { return __builtin_amdgcn_readfirstlane(key < sp.to ? cache_page(p.c, s, key) : -1); };
   __shared__ int pages_there[2][4];
+  const L head(p.c, kv_head);
   auto request = [&](int tile, int pg) __attribute__((always_inline)) {
     const int key0 = sp.from + tile * KT + wave * GROUP;
     const uint32_t dst = lds0 + (tile & 1) * (2 * TILEB) + wave * (GROUP * L::ROWB);
-    L::request(p.c, p.c.k, pg, kv_head, key0, sp.to, vo, dst);
-    L::request(p.c, p.c.v, pg, kv_head, key0, sp.to, vo, dst + TILEB);
+    head.request(p.c.k, key0, pg, sp.to, vo, dst);
+    head.request(p.c.v, key0, pg, sp.to, vo, dst + TILEB);
     if (lane == 0) pages_there[tile & 1][wave] = pg >= 0;
   };
   Running<NB> run;
@@ -425,13 +450,7 @@ __global__ void __launch_bounds__(256) many_k(Args p) {
     const bool plain = (there[0] & there[1] & there[2] & there[3]) && key0 + KT <= sp.to && key0 + KT - 1 <= pos_lo && (p.window == 0 || key0 > pos_hi - p.window);
     if (!plain) {
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int j = b * KB + L::key_of(e, fh), key = key0 + j;
-          const bool ok = key < sp.to && sees(key, at.pos, of.total, p.window) && there[j / GROUP];
-          sc[b][e] = ok ? sc[b][e] : -INFINITY;
-        }
+      for (int b = 0; b < 2; ++b) mask_scores<L>(sc[b], key0 + b * KB, fh, sp.to, at.pos, of.total, p.window, there[2 * b] != 0, there[2 * b + 1] != 0);
     }
     run.take(sc, p.scale_log2e);
     L::values(run.o, Kb + TILEB, ad, sc[0], lane);
@@ -467,32 +486,29 @@ __global__ void __launch_bounds__(256) many_k(Args p) {
 }
 
 // ---- parts of rows whose keys were split ----
-// One wavefront a row and head.  few, many: the two kernels' arguments (split 1: it did not split).
+// One wavefront a row and head.  few, many: the two kernels' arguments (split 1: it did not split); tokens: the first ones of a sequence that may
+// have been split.
 template <typename T, int HD>
-__global__ void __launch_bounds__(256) join_k(Args few, Args many) {
+__global__ void __launch_bounds__(256) join_k(Args few, Args many, int tokens) {
   const int lane = threadIdx.x & 63;
   const int64_t i = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int head = (int)(i % few.heads);
   const int64_t of_tokens = i / few.heads;
-  if (of_tokens >= (int64_t)few.c.sequences * few.max_new) return;
-  const int s = (int)(of_tokens / few.max_new), token = (int)(of_tokens % few.max_new);
+  if (of_tokens >= (int64_t)few.c.sequences * tokens) return;
+  const int s = (int)(of_tokens / tokens), token = (int)(of_tokens % tokens);
   const CacheSeq of = cache_seq(few.c, s, few.rows, few.max_new);
   if (token >= of.fresh) return;
   const bool is_few = of.fresh * few.group <= few.few_upto;
   const Args& p = is_few ? few : many;
   const int kv_head = head / p.group, m = token * p.group + head % p.group;
-  int t0 = 0, t1 = of.fresh - 1, from, to;
-  if (!is_few) {
-    const int block = m / 128;
-    t0 = block * 128 / p.group;
-    t1 = min(of.fresh * p.group, block * 128 + 128) - 1;
-    t1 /= p.group;
-  }
-  keys_of(of, t0, t1, p.window, from, to);
+  const int side = is_few ? FEW : 128, block = m / side;
+  int from, to;
+  keys_of(of, block * side / p.group, (min(of.fresh * p.group, block * side + side) - 1) / p.group, p.window, from, to);
   const int n = parts_of(from, to, p.split, p.chunk);
   if (n == 1) return;
   const int64_t row = of.row0 + token;
-  const int64_t first = is_few ? ((int64_t)s * p.c.kv_heads + kv_head) * p.split * FEW + m : (row * p.heads + head) * p.split;
+  const int64_t first =
+      is_few ? ((((int64_t)s * p.c.kv_heads + kv_head) * p.row_blocks + block) * p.split) * FEW + m % FEW : (row * p.heads + head) * p.split;
   const int64_t step = is_few ? FEW : 1;
   float top = -INFINITY;
   for (int k = 0; k < n; ++k) top = fmaxf(top, p.part_ml[first + k * step].x);
@@ -516,7 +532,7 @@ __global__ void __launch_bounds__(256) join_k(Args few, Args many) {
 
 // ---- host ----
 struct Plan {
-  int few_split, few_chunk, many_split, many_chunk, row_blocks;
+  int few_split, few_chunk, few_blocks, few_upto, many_split, many_chunk, many_blocks, tokens;
   bool few, many;
   int64_t few_parts, many_parts;  // rows of partial sums
 };
@@ -524,10 +540,13 @@ int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 Plan plan_of(const CacheView& c, int64_t rows, int heads, int max_new, int64_t max_length, int window) {
   Plan p{};
   const int group = heads / c.kv_heads;
-  const int64_t most = (int64_t)max_new * group;  // rows of the longest sequence
-  p.many = most > FEW;
+  const int64_t most = (int64_t)max_new * group, pairs = (int64_t)c.sequences * c.kv_heads;  // rows of the longest sequence
+  // many_k shares a tile of keys among four times the rows; few_k gives four times the workgroups, and takes all where they do not fill the chip
+  p.many = most > FEW && pairs * up(most, FEW) > 1024;
   p.few = !p.many || rows < (int64_t)c.sequences * max_new;  // else no sequence is short where the longest is not, as a rule; many_k takes any
-  p.row_blocks = (int)std::max<int64_t>(1, up(most, 128));
+  p.few_upto = !p.many ? INT32_MAX : p.few ? FEW : 0;
+  p.few_blocks = (int)(p.many ? 1 : std::max<int64_t>(1, up(most, FEW)));
+  p.many_blocks = (int)std::max<int64_t>(1, up(most, 128));
   int64_t span = std::max<int64_t>(1, std::min<int64_t>(max_length, (int64_t)c.max_pages << c.page_shift));
   if (window > 0) span = std::min<int64_t>(span, (int64_t)window + max_new + KB);
   auto split = [&](int64_t items, int64_t want, int64_t least, int& n, int& chunk) {
@@ -535,26 +554,29 @@ Plan plan_of(const CacheView& c, int64_t rows, int heads, int max_new, int64_t m
     chunk = (int)(up(up(span, k), 128) * 128);
     n = (int)up(span, chunk);
   };
-  split((int64_t)c.sequences * c.kv_heads, 4096, 256, p.few_split, p.few_chunk);
+  split(pairs * p.few_blocks, 4096, 256, p.few_split, p.few_chunk);
   split((int64_t)c.kv_heads * (up(rows * group, 128) + c.sequences - 1), 512, 512, p.many_split, p.many_chunk);
   if (!p.few) p.few_split = 1;
   if (!p.many) p.many_split = 1;
-  p.few_parts = p.few_split > 1 ? (int64_t)c.sequences * c.kv_heads * p.few_split * FEW : 0;
+  p.few_parts = p.few_split > 1 ? pairs * p.few_blocks * p.few_split * FEW : 0;
   p.many_parts = p.many_split > 1 ? rows * heads * p.many_split : 0;
+  p.tokens = p.many && p.many_split == 1 ? std::min(max_new, FEW) : max_new;
   return p;
 }
 
 template <typename T, int HD>
 hipError_t launch(const Plan& pl, Args a, float* workspace, hipStream_t st) {
   typedef Tile<T, HD> L;
-  a.few_upto = pl.few ? FEW : 0;
+  a.few_upto = pl.few_upto;
   Args few = a, many = a;
   const int64_t n = pl.few_parts + pl.many_parts;
   few.split = pl.few_split; few.chunk = pl.few_chunk; few.part = workspace; few.part_ml = (float2*)(workspace + n * HD);
   many.split = pl.many_split; many.chunk = pl.many_chunk; many.part = workspace + pl.few_parts * HD; many.part_ml = few.part_ml + pl.few_parts;
-  many.row_blocks = pl.row_blocks;
+  few.row_blocks = pl.few_blocks;
+  many.row_blocks = pl.many_blocks;
   const int64_t pairs = (int64_t)a.c.sequences * a.c.kv_heads;
-  const int64_t few_grid = pairs * pl.few_split, many_grid = pairs * pl.row_blocks * pl.many_split, join_grid = up((int64_t)a.c.sequences * a.max_new * a.heads, 4);
+  const int64_t few_grid = pairs * pl.few_blocks * pl.few_split, many_grid = pairs * pl.many_blocks * pl.many_split,
+                join_grid = up((int64_t)a.c.sequences * pl.tokens * a.heads, 4);
   if (few_grid > 0x7FFFFFFF || many_grid > 0x7FFFFFFF || join_grid > 0x7FFFFFFF) return hipErrorInvalidValue;
   constexpr int FEW_LDS = 4 * 2 * L::BLOCKB, MANY_LDS = 2 * 2 * 2 * L::BLOCKB;
   static_assert(4 * FEW * HD * 4 <= FEW_LDS, "the wavefronts' sums fit where their tiles were");
@@ -571,7 +593,7 @@ hipError_t launch(const Plan& pl, Args a, float* workspace, hipStream_t st) {
   if (pl.few) {
     few_k<T, HD><<<(unsigned)few_grid, 256, FEW_LDS, st>>>(few);
   }
-  if (n > 0) join_k<T, HD><<<(unsigned)join_grid, 256, 0, st>>>(few, many);
+  if (n > 0) join_k<T, HD><<<(unsigned)join_grid, 256, 0, st>>>(few, many, pl.tokens);
   return hipGetLastError();
 }
 

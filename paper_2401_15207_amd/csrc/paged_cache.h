@@ -35,5 +35,12 @@ __device__ __forceinline__ int cache_page(const CacheView& c, int s, int pos) {
   const int page = reinterpret_cast<Constant>(reinterpret_cast<uintptr_t>(c.pages))[(int64_t)s * c.pages_ld + i];
   return (unsigned)page < (unsigned)c.n_pages ? page : -1;
 }
+// The same for a token of the lane's own.
+__device__ __forceinline__ int cache_page_any(const CacheView& c, int s, int pos) {
+  const int i = pos >> c.page_shift;
+  if (i >= c.max_pages) return -1;
+  const int page = c.pages[(int64_t)s * c.pages_ld + i];
+  return (unsigned)page < (unsigned)c.n_pages ? page : -1;
+}
 
 }  // namespace hift

@@ -47,15 +47,21 @@ __device__ __forceinline__ void turn_of(double f, double& c, double& s) {
   if (k >= 2) s = -s;
 }
 
-// One thread a pair and position.  Angles are held in turns and in 64 bits: at position 2^20 their error is below 2^-32 of a turn.
+// A workgroup takes TABLE_EACH entries in a row.  Angles are held in turns and in 64 bits: at position 2^20 their error is below 2^-32 of a turn.
+constexpr int TABLE_EACH = 4 * BLK;
 __global__ void __launch_bounds__(BLK) rotary_table_k(TableArgs p) {
-  const int64_t i = (int64_t)blockIdx.x * BLK + threadIdx.x;
-  if (i >= p.count * p.half) return;
-  const int64_t row = i / p.half;
-  const double a = (double)(p.first + row) * p.turns[(int)(i - row * p.half)];
-  double c, s;
-  turn_of(a - rint(a), c, s);
-  p.cs[i] = make_float2((float)(c * p.amplitude), (float)(s * p.amplitude));
+  const int64_t first = (int64_t)blockIdx.x * TABLE_EACH, row0 = first / p.half, left = p.count * p.half - first;
+  const int in = (int)(first - row0 * p.half);
+#pragma unroll
+  for (int k = 0; k < TABLE_EACH; k += BLK) {
+    const int i = k + (int)threadIdx.x;
+    if (i >= left) return;
+    const unsigned at = (unsigned)(in + i), row = at / (unsigned)p.half, pair = at - row * (unsigned)p.half;
+    const double a = (double)(p.first + row0 + row) * p.turns[pair];
+    double c, s;
+    turn_of(a - rint(a), c, s);
+    p.cs[first + i] = make_float2((float)(c * p.amplitude), (float)(s * p.amplitude));
+  }
 }
 
 // ---- rotation ----
@@ -264,7 +270,7 @@ hipError_t rotary_table(int rot, const double* turns, double amplitude, int64_t 
   TableArgs p{};
   p.half = rot / 2; p.first = first; p.count = count; p.amplitude = amplitude; p.cs = (float2*)cos_sin;
   std::copy(turns, turns + rot / 2, p.turns);
-  const int64_t blocks = (count * p.half + BLK - 1) / BLK;
+  const int64_t blocks = (count * p.half + TABLE_EACH - 1) / TABLE_EACH;
   if (blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
   rotary_table_k<<<(unsigned)blocks, BLK, 0, st>>>(p);
   return hipGetLastError();
