@@ -19,9 +19,9 @@
 namespace hift {
 namespace {
 
-constexpr int BLK = 256;
+constexpr int BLK = 512;
 constexpr int LOOSE = 8;  // elements before the first aligned piece: at most 7
-constexpr int U = 4;      // pieces of 16 bytes of a thread, at most
+constexpr int U = 2;      // pieces of 16 bytes of a thread, at most
 
 struct AdjustArgs {
   int V, slice, slices;
@@ -42,11 +42,14 @@ struct AdjustArgs {
 
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 
-template <typename T, bool BWD>
-__device__ __forceinline__ float adjusted(float x, float g, int n, float bias, bool allowed, const AdjustArgs& p) {
+constexpr int POSITIVE = INT32_MIN;  // backward: the bit of a count that says that the logit is above 0
+
+// x: the logit, or backward the gradient; n: the count
+template <bool BWD>
+__device__ __forceinline__ float adjusted(float x, int n, float bias, bool allowed, const AdjustArgs& p) {
   if constexpr (BWD) {
     if (!allowed) return 0.f;
-    return n > 0 ? (x > 0.f ? g * p.inverse : g * p.repetition) : g;
+    return n == 0 ? x : n < 0 ? x * p.inverse : x * p.repetition;
   } else {
     if (!allowed) return -INFINITY;
     const float z = n > 0 ? (x > 0.f ? x * p.inverse : x * p.repetition) - p.presence : x;
@@ -90,8 +93,10 @@ __global__ void __launch_bounds__(BLK) adjust_k(AdjustArgs p) {
       for (int64_t i = b + t; i < e; i += BLK) {
         const unsigned at = (unsigned)p.tokens[i] - (unsigned)lo;
         if (at < (unsigned)n) {
-          atomicAdd(&counts[shift + (int)at], 1);
+          const int had = atomicAdd(&counts[shift + (int)at], 1);
           mine = 1;
+          // backward, the first to meet the token looks its logit up, all of them at the same time: the sign is all that counts
+          if (BWD && had == 0 && to_f32(x[lo + (int)at]) > 0.f) atomicOr(&counts[shift + (int)at], POSITIVE);
         }
       }
       if (mine) any = 1;
@@ -104,7 +109,7 @@ __global__ void __launch_bounds__(BLK) adjust_k(AdjustArgs p) {
   auto one = [&](int j) __attribute__((always_inline)) {
     const int c = seen ? counts[shift + j - lo] : 0;
     const bool let = !allowed || (allowed[j >> 5] >> (j & 31) & 1);
-    out[j] = from_f32<T>(adjusted<T, BWD>(!BWD || c > 0 ? to_f32(x[j]) : 0.f, BWD ? to_f32(g[j]) : 0.f, c, !BWD && bias ? bias[j] : 0.f, let, p));
+    out[j] = from_f32<T>(adjusted<BWD>(to_f32((BWD ? g : x)[j]), c, !BWD && bias ? bias[j] : 0.f, let, p));
   };
   if (!p.aligned) {
     for (int j = lo + t; j < hi; j += BLK) one(j);
@@ -139,16 +144,7 @@ __global__ void __launch_bounds__(BLK) adjust_k(AdjustArgs p) {
     }
     P o;
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      float xv = 0.f, gv = 0.f;
-      if constexpr (BWD) {
-        gv = to_f32(in[k].v[e]);
-        if (c[e] > 0) xv = to_f32(x[j0 + e]);
-      } else {
-        xv = to_f32(in[k].v[e]);
-      }
-      o.v[e] = from_f32<T>(adjusted<T, BWD>(xv, gv, c[e], bv[e], bits >> e & 1, p));
-    }
+    for (int e = 0; e < E; ++e) o.v[e] = from_f32<T>(adjusted<BWD>(to_f32(in[k].v[e]), c[e], bv[e], bits >> e & 1, p));
     *reinterpret_cast<P*>(out + j0) = o;
   }
   // what is left before the first piece and after the last

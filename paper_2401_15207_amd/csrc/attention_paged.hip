@@ -7,9 +7,10 @@
 // meets a tile of keys, so keys and values are read once for all heads of a group.  One pass over the keys with a running maximum and sum
 // per row (log2 domain), as in attention.hip, whose conventions for the matrix instruction's operands and for LDS tiles these kernels share.
 //   few_k    32 rows a workgroup: all four wavefronts hold the same rows and take turns at the blocks of 32 keys, each through LDS tiles of its own
-//            without any barrier, and their results are joined at the end.  Bound by reading the cache.
+//            without any barrier, and their results are joined at the end.  Bound by reading the cache.  Lengths are known on the device only, and
+//            differ: the keys of all sequences and heads, one after the other, are cut into equal runs, a workgroup each, wherever that falls.
 //   many_k   128 rows a workgroup, 32 a wavefront, which share tiles of 64 keys.  Bound by the matrix instructions.
-//   join_k   where the keys of a row were split over workgroups: the parts, weighted by their maxima.
+//   join_k   rows whose keys fell to several workgroups: the parts, weighted by their maxima.
 #include <math.h>
 
 #include <algorithm>
@@ -21,6 +22,8 @@
 
 namespace hift {
 namespace {
+
+#define UNIFORM(x) __builtin_amdgcn_readfirstlane(x)
 
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
@@ -43,10 +46,11 @@ struct Args {
   void* out;
   float* lse;           // [rows, heads] or null
   int few_upto;         // sequences of at most so many rows are few_k's, the others many_k's
-  int row_blocks;       // this kernel's blocks of rows of the longest sequence
-  int split, chunk;     // this kernel's workgroups along the keys, and the keys of each
-  float* part;          // [..][HD] sums and, behind all of them, (maximum, sum of exponentials) pairs
-  float2* part_ml;
+  int few_blocks, many_blocks;  // blocks of rows of the longest sequence
+  int runs;             // few_k's workgroups; 0: one a block of rows and key head, and nothing to join
+  int64_t* plan;        // [0]: steps of a run; [1 + e]: steps before entry e
+  float2* part_ml;      // [run][2][FEW] (maximum, sum of exponentials) of a run's first and last rows where those are shared with other runs
+  float* part;          // [run][2][FEW][HD] their sums
 };
 
 // ---- tiles of a type and width ----
@@ -79,8 +83,8 @@ struct Tile {
   __device__ __forceinline__ void request(const void* array, int key0, int page, int end, const uint32_t (&vo)[IPG], uint32_t lds) const {
     const uint64_t a = reinterpret_cast<uint64_t>(array) + (uint64_t)((int64_t)max(page, 0) * page_bytes + (int64_t)(head_at + (key0 & slots)) * row_bytes);
     const int n = page < 0 ? 0 : min(max(end - key0, 0), GROUP);
-    const hift_u32x4 rs = {(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)a), (uint32_t)__builtin_amdgcn_readfirstlane((int)((uint32_t)(a >> 32) & 0xFFFFu)),
-                           (uint32_t)__builtin_amdgcn_readfirstlane(n * row_bytes), 0x00020000u};
+    const hift_u32x4 rs = {(uint32_t)UNIFORM((int)(uint32_t)a), (uint32_t)UNIFORM((int)((uint32_t)(a >> 32) & 0xFFFFu)),
+                           (uint32_t)UNIFORM(n * row_bytes), 0x00020000u};
 #pragma unroll
     for (int i = 0; i < IPG; ++i) load_to_lds_b128(rs, lds + i * 1024, vo[i], 0);
   }
@@ -218,29 +222,11 @@ struct Running {
   }
 };
 
-// The keys that a block of rows reads, and this workgroup's part of them
-struct Span {
-  int from, to;  // keys [from, to); `from` a multiple of 32
-  bool direct;   // all the keys there are: the result goes to the output, not to a part
-  bool none;     // no keys for this part
-};
-__device__ __forceinline__ int parts_of(int from, int to, int split, int chunk) { return min(split, max(1, (to - from + chunk - 1) / chunk)); }
-// rows: tokens [t0, t1] of the sequence
+// The keys [from, to) that tokens [t0, t1] of a sequence read; `from` is a multiple of 32.
 __device__ __forceinline__ void keys_of(const CacheSeq& of, int t0, int t1, int window, int& from, int& to) {
   to = min(of.total, of.cached + t1 + 1);
   from = window > 0 ? max(0, of.cached + t0 - window + 1) & ~(KB - 1) : 0;
   from = min(from, to & ~(KB - 1));
-}
-__device__ __forceinline__ Span span_of(const CacheSeq& of, int t0, int t1, int window, int part, int split, int chunk) {
-  int from, to;
-  keys_of(of, t0, t1, window, from, to);
-  const int n = parts_of(from, to, split, chunk);
-  Span s;
-  s.direct = n == 1;
-  s.none = part >= n;
-  s.from = from + part * chunk;
-  s.to = part + 1 == n ? to : s.from + chunk;
-  return s;
 }
 
 // Where a row of the list m = token * group + head goes
@@ -278,30 +264,35 @@ __device__ __forceinline__ void store_out(const Args& p, const RowAt& r, int c, 
 
 // ---- few rows ----
 constexpr int PAGED = 64 * GROUP;  // keys whose page numbers a wavefront holds, a lane each 16
+constexpr int STEP = 4 * KB;       // keys that a workgroup takes at a time
 
+// An entry: a block of 32 rows of a sequence, entry s * few_blocks + block; its key heads take `steps` steps each.
+struct Entry {
+  CacheSeq of;
+  int m0, n_rows, t0, t1, from, to, steps;
+  __device__ __forceinline__ Entry(const Args& p, int s, int block) : of(cache_seq(p.c, s, p.rows, p.max_new)), m0(block * FEW) {
+    const int all = of.fresh * p.group;
+    n_rows = all <= p.few_upto ? min(all - m0, FEW) : 0;
+    steps = 0;
+    if (n_rows <= 0) return;
+    t0 = m0 / p.group;
+    t1 = (m0 + n_rows - 1) / p.group;
+    keys_of(of, t0, t1, p.window, from, to);
+    steps = max(1, (to - from + STEP - 1) / STEP);
+  }
+};
+
+// Steps [step0, step1) of an entry's key head.  shared: -1 where these are all its steps, otherwise the place [..][FEW] its results go to.
 template <typename T, int HD>
-__global__ void __launch_bounds__(256) few_k(Args p) {
+__device__ __forceinline__ void few_rows(const Args& p, const Entry& en, int s, int kv_head, int step0, int step1, int64_t shared, unsigned char* lds, float2 (*ml)[FEW]) {
   typedef Tile<T, HD> L;
   constexpr int NB = L::NB, IPB = 2 * L::IPG;  // loads of a block of keys
-  extern __shared__ unsigned char lds[];       // [wave][K | V] blocks; at the end [wave][row][HD] sums
-  __shared__ float2 ml[4][FEW];
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), fr = lane & 31, fh = lane >> 5;
-  int i = (int)blockIdx.x;
-  const int part = i % p.split;
-  i /= p.split;
-  const int block = p.row_blocks - 1 - i % p.row_blocks, pair = i / p.row_blocks;  // the rows with the most keys first
-  const int s = pair / p.c.kv_heads, kv_head = pair % p.c.kv_heads;
-  const CacheSeq of = cache_seq(p.c, s, p.rows, p.max_new);
-  const int all_rows = of.fresh * p.group, m0 = block * FEW, n_rows = min(all_rows - m0, FEW);
-  if (n_rows <= 0 || all_rows > p.few_upto) return;
-  const int t0 = m0 / p.group, t1 = (m0 + n_rows - 1) / p.group;  // first and last token
-  const Span sp = span_of(of, t0, t1, p.window, part, p.split, p.chunk);
-  if (sp.none) return;
-
-  // page numbers of the keys from `from` on
-  auto pages_from = [&](int from) { return from + lane * GROUP < sp.to ? cache_page_any(p.c, s, from + lane * GROUP) : -1; };
-  int paged = sp.from, pages = pages_from(paged), pages_next = -1;
-  const RowAt at = row_at(p, of, kv_head, m0 + fr);
+  const int tid = threadIdx.x, lane = tid & 63, wave = UNIFORM(tid >> 6), fr = lane & 31, fh = lane >> 5;
+  const int from = UNIFORM(en.from + step0 * STEP), to = UNIFORM(min(en.to, en.from + step1 * STEP)), n_rows = UNIFORM(en.n_rows);
+  // page numbers of the keys from `k0` on
+  auto pages_from = [&](int k0) { return k0 + lane * GROUP < to ? cache_page_any(p.c, s, k0 + lane * GROUP) : -1; };
+  int paged = from, pages = pages_from(paged);
+  const RowAt at = row_at(p, en.of, kv_head, en.m0 + fr);
   typename L::Frag q[L::NQ];
   L::load_row(q, (const T*)p.q + at.row * p.ldq + (int64_t)at.head * p.c.head_dim, at.ok, p.c.head_dim, fh);
   uint32_t vo[L::IPG];
@@ -313,24 +304,23 @@ __global__ void __launch_bounds__(256) few_k(Args p) {
   const uint32_t lk = (uint32_t)reinterpret_cast<uintptr_t>(Kb), lv = (uint32_t)reinterpret_cast<uintptr_t>(Vb);
   const L head(p.c, kv_head);
 
-  const int blocks = (sp.to - sp.from + KB - 1) / KB;
-  int b = wave, key0 = sp.from + wave * KB, pa = -1, pb = -1;
-  if (b < blocks) {
-    const int g = (key0 - paged) / GROUP;
+  int key0 = from + wave * KB, pa = -1, pb = -1;
+  if (key0 < to) {
+    const int g = wave * (KB / GROUP);
     pa = __builtin_amdgcn_readlane(pages, g);
     pb = __builtin_amdgcn_readlane(pages, g + 1);
-    head.request(p.c.k, key0, pa, pb, sp.to, vo, lk);
-    head.request(p.c.v, key0, pa, pb, sp.to, vo, lv);
+    head.request(p.c.k, key0, pa, pb, to, vo, lk);
+    head.request(p.c.v, key0, pa, pb, to, vo, lv);
   }
   Running<NB> run;
   // the compiler waits for the rows here, once, and not in the loop, where it would wait for everything on its way
 #pragma unroll
   for (int k = 0; k < L::NQ; ++k) asm volatile("" : "+v"(q[k]));
-  const int pos_lo = of.cached + t0, pos_hi = of.cached + t1;
-  for (; b < blocks; b += 4, key0 += 4 * KB) {
-    const bool more = b + 4 < blocks;
-    const int next = key0 + 4 * KB;
-    if (next >= paged + PAGED) {  // blocks are 4 KB keys apart, and PAGED is a multiple of that
+  const int pos_lo = UNIFORM(en.of.cached + en.t0), pos_hi = UNIFORM(en.of.cached + en.t1);
+  for (; key0 < to; key0 += STEP) {
+    const int next = key0 + STEP;
+    const bool more = next < to;
+    if (next >= paged + PAGED) {  // PAGED is a multiple of STEP
       paged += PAGED;
       pages = pages_from(paged);
     }
@@ -340,15 +330,15 @@ __global__ void __launch_bounds__(256) few_k(Args p) {
     f32x16 sc[1];
     sc[0] = L::scores(Kb, ad, q);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    if (more) head.request(p.c.k, next, na, nb, sp.to, vo, lk);
-    const bool plain = (pa | pb) >= 0 && key0 + KB <= sp.to && key0 + KB - 1 <= pos_lo && (p.window == 0 || key0 > pos_hi - p.window);
-    if (!plain) mask_scores<L>(sc[0], key0, fh, sp.to, at.pos, of.total, p.window, pa >= 0, pb >= 0);
+    if (more) head.request(p.c.k, next, na, nb, to, vo, lk);
+    const bool plain = (pa | pb) >= 0 && key0 + KB <= to && key0 + KB - 1 <= pos_lo && (p.window == 0 || key0 > pos_hi - p.window);
+    if (!plain) mask_scores<L>(sc[0], key0, fh, to, at.pos, en.of.total, p.window, pa >= 0, pb >= 0);
     run.take(sc, p.scale_log2e);
     if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(IPB) : "memory");
     else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     L::values(run.o, Vb, ad, sc[0], lane);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    if (more) head.request(p.c.v, next, na, nb, sp.to, vo, lv);
+    if (more) head.request(p.c.v, next, na, nb, to, vo, lv);
     pa = na; pb = nb;
   }
   run.l += __shfl_xor(run.l, 32, 64);
@@ -379,15 +369,78 @@ __global__ void __launch_bounds__(256) few_k(Args p) {
       l = fmaf(by, ml[w][m].y, l);
       o = fmaf(by, sums[(w * FEW + m) * HD + c], o);
     }
-    if (sp.direct) {
-      const RowAt r = row_at(p, of, kv_head, m0 + m);
+    if (shared < 0) {
+      const RowAt r = row_at(p, en.of, kv_head, en.m0 + m);
       store_out<T>(p, r, c, l > 0.f || l != l ? o / l : 0.f);
       if (c == 0 && p.lse) p.lse[r.row * p.heads + r.head] = top + __builtin_amdgcn_logf(l);
     } else {
-      const int64_t to = (((int64_t)pair * p.row_blocks + block) * p.split + part) * FEW + m;
-      p.part[to * HD + c] = o;
-      if (c == 0) p.part_ml[to] = make_float2(top, l);
+      p.part[(shared + m) * HD + c] = o;
+      if (c == 0) p.part_ml[shared + m] = make_float2(top, l);
     }
+  }
+}
+
+template <typename T, int HD>
+__global__ void __launch_bounds__(256) few_k(Args p) {
+  typedef Tile<T, HD> L;
+  extern __shared__ unsigned char lds[];  // [wave][K | V] blocks; at the end of a block of rows [wave][row][HD] sums
+  __shared__ float2 ml[4][FEW];
+  const int kv_heads = p.c.kv_heads;
+  if (p.runs == 0) {
+    const int pair = (int)(blockIdx.x / (unsigned)p.few_blocks), block = p.few_blocks - 1 - (int)(blockIdx.x % (unsigned)p.few_blocks);
+    const int s = pair / kv_heads;
+    const Entry en(p, s, block);
+    if (en.steps > 0) few_rows<T, HD>(p, en, s, pair % kv_heads, 0, en.steps, -1, lds, ml);
+    return;
+  }
+  // steps of all entries, and where this run begins
+  __shared__ int64_t sums[256];
+  __shared__ int64_t found_before;
+  __shared__ int found;
+  const int tid = threadIdx.x, entries = p.c.sequences * p.few_blocks, each = (entries + 255) / 256;
+  const int e0 = min(tid * each, entries), e1 = min(e0 + each, entries);
+  int64_t mine = 0;
+  for (int e = e0; e < e1; ++e) mine += (int64_t)Entry(p, e / p.few_blocks, e % p.few_blocks).steps * kv_heads;
+  sums[tid] = mine;
+  if (tid == 0) found = -1;
+  __syncthreads();
+  int64_t before = 0, all = 0;
+  const int used = each ? (entries + each - 1) / each : 0;
+  for (int k = 0; k < used; ++k) {
+    const int64_t v = sums[k];
+    before += k < tid ? v : 0;
+    all += v;
+  }
+  const int64_t run = max((all + p.runs - 1) / p.runs, (int64_t)1), at0 = (int64_t)blockIdx.x * run, at1 = min(at0 + run, all);
+  if (blockIdx.x == 0 && tid == 0) p.plan[0] = run;
+  if (blockIdx.x == 0 || (before <= at0 && at0 < before + mine)) {
+    int64_t b = before;
+    for (int e = e0; e < e1; ++e) {
+      const int64_t n = (int64_t)Entry(p, e / p.few_blocks, e % p.few_blocks).steps * kv_heads;
+      if (blockIdx.x == 0) p.plan[1 + e] = b;
+      if (b <= at0 && at0 < b + n) {
+        found = e;
+        found_before = b;
+      }
+      b += n;
+    }
+  }
+  __syncthreads();
+  int e = UNIFORM(found);
+  if (e < 0) return;
+  int64_t at = at0, first = found_before;
+  for (; at < at1 && e < entries; ++e) {
+    const int s = e / p.few_blocks;
+    const Entry en(p, s, e % p.few_blocks);
+    while (at < at1 && at < first + (int64_t)en.steps * kv_heads) {
+      const int in = UNIFORM((int)(at - first)), kv_head = UNIFORM(in / en.steps), step0 = in - kv_head * UNIFORM(en.steps);
+      const int n = UNIFORM((int)min((int64_t)(en.steps - step0), at1 - at));
+      const bool whole = n == en.steps;
+      few_rows<T, HD>(p, en, s, kv_head, step0, step0 + n, whole ? -1 : ((int64_t)blockIdx.x * 2 + (step0 == 0)) * FEW, lds, ml);
+      __syncthreads();  // the next block's keys go where the sums were
+      at += n;
+    }
+    first += (int64_t)en.steps * kv_heads;
   }
 }
 
@@ -397,18 +450,15 @@ __global__ void __launch_bounds__(256) many_k(Args p) {
   typedef Tile<T, HD> L;
   constexpr int NB = L::NB, KT = 2 * KB, TILEB = KT * L::ROWB, QB = 128;
   extern __shared__ unsigned char lds[];  // [buffer][K | V] tiles of 64 keys
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), fr = lane & 31, fh = lane >> 5;
-  int i = (int)blockIdx.x;
-  const int part = i % p.split;
-  i /= p.split;
-  const int block = p.row_blocks - 1 - i % p.row_blocks, pair = i / p.row_blocks;  // the rows with the most keys first
+  const int tid = threadIdx.x, lane = tid & 63, wave = UNIFORM(tid >> 6), fr = lane & 31, fh = lane >> 5;
+  const int block = p.many_blocks - 1 - (int)(blockIdx.x % (unsigned)p.many_blocks), pair = (int)(blockIdx.x / (unsigned)p.many_blocks);  // most keys first
   const int s = pair / p.c.kv_heads, kv_head = pair % p.c.kv_heads;
   const CacheSeq of = cache_seq(p.c, s, p.rows, p.max_new);
   const int n_rows = of.fresh * p.group;
   if (n_rows <= p.few_upto || block * QB >= n_rows) return;
   const int m0 = block * QB, m_last = min(n_rows, m0 + QB) - 1;
-  const Span sp = span_of(of, m0 / p.group, m_last / p.group, p.window, part, p.split, p.chunk);
-  if (sp.none) return;
+  int from, to;
+  keys_of(of, m0 / p.group, m_last / p.group, p.window, from, to);
 
   const int w0 = m0 + wave * 32;  // this wavefront's rows; their first and last positions
   const int pos_lo = of.cached + min(w0, m_last) / p.group, pos_hi = of.cached + min(w0 + 31, m_last) / p.group;
@@ -420,23 +470,23 @@ __global__ void __launch_bounds__(256) many_k(Args p) {
   typename L::Address ad;
   L::addresses(ad, lane);
   const uint32_t lds0 = (uint32_t)reinterpret_cast<uintptr_t>(lds);
-  const int tiles = (sp.to - sp.from + KT - 1) / KT;
+  const int tiles = (to - from + KT - 1) / KT;
   // every wavefront brings 16 keys of a tile
-  auto page = [&](int key) { return __builtin_amdgcn_readfirstlane(key < sp.to ? cache_page(p.c, s, key) : -1); };
+  auto page = [&](int key) { return UNIFORM(key < to ? cache_page(p.c, s, key) : -1); };
   __shared__ int pages_there[2][4];
   const L head(p.c, kv_head);
   auto request = [&](int tile, int pg) __attribute__((always_inline)) {
-    const int key0 = sp.from + tile * KT + wave * GROUP;
+    const int key0 = from + tile * KT + wave * GROUP;
     const uint32_t dst = lds0 + (tile & 1) * (2 * TILEB) + wave * (GROUP * L::ROWB);
-    head.request(p.c.k, key0, pg, sp.to, vo, dst);
-    head.request(p.c.v, key0, pg, sp.to, vo, dst + TILEB);
+    head.request(p.c.k, key0, pg, to, vo, dst);
+    head.request(p.c.v, key0, pg, to, vo, dst + TILEB);
     if (lane == 0) pages_there[tile & 1][wave] = pg >= 0;
   };
   Running<NB> run;
-  int pg = page(sp.from + wave * GROUP);
+  int pg = page(from + wave * GROUP);
   if (tiles > 0) request(0, pg);
   for (int t = 0; t < tiles; ++t) {
-    const int key0 = sp.from + t * KT;
+    const int key0 = from + t * KT;
     pg = t + 1 < tiles ? page(key0 + KT + wave * GROUP) : -1;
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();  // the tile is complete; nobody reads the other buffer any more
@@ -447,10 +497,10 @@ __global__ void __launch_bounds__(256) many_k(Args p) {
     f32x16 sc[2];
     sc[0] = L::scores(Kb, ad, q);
     sc[1] = L::scores(Kb + L::BLOCKB, ad, q);
-    const bool plain = (there[0] & there[1] & there[2] & there[3]) && key0 + KT <= sp.to && key0 + KT - 1 <= pos_lo && (p.window == 0 || key0 > pos_hi - p.window);
+    const bool plain = (there[0] & there[1] & there[2] & there[3]) && key0 + KT <= to && key0 + KT - 1 <= pos_lo && (p.window == 0 || key0 > pos_hi - p.window);
     if (!plain) {
 #pragma unroll
-      for (int b = 0; b < 2; ++b) mask_scores<L>(sc[b], key0 + b * KB, fh, sp.to, at.pos, of.total, p.window, there[2 * b] != 0, there[2 * b + 1] != 0);
+      for (int b = 0; b < 2; ++b) mask_scores<L>(sc[b], key0 + b * KB, fh, to, at.pos, of.total, p.window, there[2 * b] != 0, there[2 * b + 1] != 0);
     }
     run.take(sc, p.scale_log2e);
     L::values(run.o, Kb + TILEB, ad, sc[0], lane);
@@ -458,86 +508,66 @@ __global__ void __launch_bounds__(256) many_k(Args p) {
   }
   run.l += __shfl_xor(run.l, 32, 64);
   if (!at.ok) return;
-  if (sp.direct) {
-    const float inv = run.l > 0.f || run.l != run.l ? 1.0f / run.l : 0.f;
+  const float inv = run.l > 0.f || run.l != run.l ? 1.0f / run.l : 0.f;
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
+  for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int c = nb * 32 + 8 * g + 4 * fh;
-        if (c < p.c.head_dim) {
-          Vec<T, 4> o;
+    for (int g = 0; g < 4; ++g) {
+      const int c = nb * 32 + 8 * g + 4 * fh;
+      if (c < p.c.head_dim) {
+        Vec<T, 4> o;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) o.v[e] = from_f32<T>(run.o[nb][4 * g + e] * inv);
-          *reinterpret_cast<Vec<T, 4>*>((T*)p.out + at.row * p.ldo + (int64_t)at.head * p.c.head_dim + c) = o;
-        }
+        for (int e = 0; e < 4; ++e) o.v[e] = from_f32<T>(run.o[nb][4 * g + e] * inv);
+        *reinterpret_cast<Vec<T, 4>*>((T*)p.out + at.row * p.ldo + (int64_t)at.head * p.c.head_dim + c) = o;
       }
-    if (fh == 0 && p.lse) p.lse[at.row * p.heads + at.head] = run.m + __builtin_amdgcn_logf(run.l);
-  } else {
-    const int64_t to = (at.row * p.heads + at.head) * p.split + part;
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-      for (int g = 0; g < 4; ++g)
-        *reinterpret_cast<f32x4*>(p.part + to * HD + nb * 32 + 8 * g + 4 * fh) =
-            f32x4{run.o[nb][4 * g], run.o[nb][4 * g + 1], run.o[nb][4 * g + 2], run.o[nb][4 * g + 3]};
-    if (fh == 0) p.part_ml[to] = make_float2(run.m, run.l);
-  }
+    }
+  if (fh == 0 && p.lse) p.lse[at.row * p.heads + at.head] = run.m + __builtin_amdgcn_logf(run.l);
 }
 
-// ---- parts of rows whose keys were split ----
-// One wavefront a row and head.  few, many: the two kernels' arguments (split 1: it did not split); tokens: the first ones of a sequence that may
-// have been split.
+// ---- rows whose keys fell to several runs ----
+// One wavefront a row and head of the first `tokens` tokens of a sequence.
 template <typename T, int HD>
-__global__ void __launch_bounds__(256) join_k(Args few, Args many, int tokens) {
+__global__ void __launch_bounds__(256) join_k(Args p, int tokens) {
   const int lane = threadIdx.x & 63;
-  const int64_t i = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int head = (int)(i % few.heads);
-  const int64_t of_tokens = i / few.heads;
-  if (of_tokens >= (int64_t)few.c.sequences * tokens) return;
-  const int s = (int)(of_tokens / tokens), token = (int)(of_tokens % tokens);
-  const CacheSeq of = cache_seq(few.c, s, few.rows, few.max_new);
-  if (token >= of.fresh) return;
-  const bool is_few = of.fresh * few.group <= few.few_upto;
-  const Args& p = is_few ? few : many;
-  const int kv_head = head / p.group, m = token * p.group + head % p.group;
-  const int side = is_few ? FEW : 128, block = m / side;
-  int from, to;
-  keys_of(of, block * side / p.group, (min(of.fresh * p.group, block * side + side) - 1) / p.group, p.window, from, to);
-  const int n = parts_of(from, to, p.split, p.chunk);
-  if (n == 1) return;
-  const int64_t row = of.row0 + token;
-  const int64_t first =
-      is_few ? ((((int64_t)s * p.c.kv_heads + kv_head) * p.row_blocks + block) * p.split) * FEW + m % FEW : (row * p.heads + head) * p.split;
-  const int64_t step = is_few ? FEW : 1;
+  const int64_t i = (int64_t)blockIdx.x * 4 + UNIFORM(threadIdx.x >> 6);
+  const int head = (int)(i % p.heads);
+  const int64_t st = i / p.heads;
+  if (st >= (int64_t)p.c.sequences * tokens) return;
+  const int s = (int)(st / tokens), token = (int)(st % tokens), kv_head = head / p.group, m = token * p.group + head % p.group, block = m / FEW;
+  const Entry en(p, s, block);
+  if (en.steps == 0 || token >= en.of.fresh) return;
+  const int64_t run = p.plan[0], first = p.plan[1 + (int64_t)s * p.few_blocks + block] + (int64_t)kv_head * en.steps;
+  const int64_t r0 = first / run, r1 = (first + en.steps - 1) / run;
+  if (r0 == r1) return;
+  auto place = [&](int64_t r) { return (r * 2 + (r == r0)) * FEW + m % FEW; };
   float top = -INFINITY;
-  for (int k = 0; k < n; ++k) top = fmaxf(top, p.part_ml[first + k * step].x);
+  for (int64_t r = r0; r <= r1; ++r) top = fmaxf(top, p.part_ml[place(r)].x);
   const float ref = top == -INFINITY ? 0.f : top;
   float l = 0.f, o[HD / 64];
 #pragma unroll
   for (int c = 0; c < HD / 64; ++c) o[c] = 0.f;
-  for (int k = 0; k < n; ++k) {
-    const int64_t at = first + k * step;
+  for (int64_t r = r0; r <= r1; ++r) {
+    const int64_t at = place(r);
     const float by = __builtin_amdgcn_exp2f(p.part_ml[at].x - ref);
     l = fmaf(by, p.part_ml[at].y, l);
 #pragma unroll
     for (int c = 0; c < HD / 64; ++c) o[c] = fmaf(by, p.part[at * HD + c * 64 + lane], o[c]);
   }
   RowAt r;
-  r.row = row; r.head = head;
+  r.row = en.of.row0 + token; r.head = head;
 #pragma unroll
   for (int c = 0; c < HD / 64; ++c) store_out<T>(p, r, c * 64 + lane, l > 0.f || l != l ? o[c] / l : 0.f);
-  if (lane == 0 && p.lse) p.lse[row * p.heads + head] = top + __builtin_amdgcn_logf(l);
+  if (lane == 0 && p.lse) p.lse[r.row * p.heads + head] = top + __builtin_amdgcn_logf(l);
 }
 
 // ---- host ----
 struct Plan {
-  int few_split, few_chunk, few_blocks, few_upto, many_split, many_chunk, many_blocks, tokens;
   bool few, many;
-  int64_t few_parts, many_parts;  // rows of partial sums
+  int few_blocks, few_upto, many_blocks, runs, tokens;
+  int64_t entries;
 };
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
-Plan plan_of(const CacheView& c, int64_t rows, int heads, int max_new, int64_t max_length, int window) {
+Plan plan_of(int dt, const CacheView& c, int64_t rows, int heads, int max_new, int64_t max_length, int window) {
   Plan p{};
   const int group = heads / c.kv_heads;
   const int64_t most = (int64_t)max_new * group, pairs = (int64_t)c.sequences * c.kv_heads;  // rows of the longest sequence
@@ -547,37 +577,27 @@ Plan plan_of(const CacheView& c, int64_t rows, int heads, int max_new, int64_t m
   p.few_upto = !p.many ? INT32_MAX : p.few ? FEW : 0;
   p.few_blocks = (int)(p.many ? 1 : std::max<int64_t>(1, up(most, FEW)));
   p.many_blocks = (int)std::max<int64_t>(1, up(most, 128));
+  p.entries = (int64_t)c.sequences * p.few_blocks;
+  p.tokens = p.many ? std::min(max_new, FEW) : max_new;
   int64_t span = std::max<int64_t>(1, std::min<int64_t>(max_length, (int64_t)c.max_pages << c.page_shift));
-  if (window > 0) span = std::min<int64_t>(span, (int64_t)window + max_new + KB);
-  auto split = [&](int64_t items, int64_t want, int64_t least, int& n, int& chunk) {
-    const int64_t k = std::max<int64_t>(1, std::min<int64_t>({up(want, std::max<int64_t>(items, 1)), up(span, least), 64}));
-    chunk = (int)(up(up(span, k), 128) * 128);
-    n = (int)up(span, chunk);
-  };
-  split(pairs * p.few_blocks, 4096, 256, p.few_split, p.few_chunk);
-  split((int64_t)c.kv_heads * (up(rows * group, 128) + c.sequences - 1), 512, 512, p.many_split, p.many_chunk);
-  if (!p.few) p.few_split = 1;
-  if (!p.many) p.many_split = 1;
-  p.few_parts = p.few_split > 1 ? pairs * p.few_blocks * p.few_split * FEW : 0;
-  p.many_parts = p.many_split > 1 ? rows * heads * p.many_split : 0;
-  p.tokens = p.many && p.many_split == 1 ? std::min(max_new, FEW) : max_new;
+  if (window > 0) span = std::min<int64_t>(span, (int64_t)window + FEW + KB);
+  // as many runs as workgroups are on the chip at a time: LDS holds four blocks of rows of 128 bytes, two of 256, one of 512
+  const int row_bytes = (c.head_dim <= 64 ? 64 : 128) * (dt == DT_BF16 ? 2 : 4), resident = 256 * 512 / row_bytes;
+  if (p.few && span > 4 * STEP) p.runs = (int)std::min<int64_t>(resident, pairs * p.few_blocks * up(span, STEP));
   return p;
 }
+size_t plan_bytes(const Plan& p) { return p.runs ? (size_t)((1 + p.entries) * 8 + 15) / 16 * 16 : 0; }
 
 template <typename T, int HD>
-hipError_t launch(const Plan& pl, Args a, float* workspace, hipStream_t st) {
+hipError_t launch(const Plan& pl, Args a, void* workspace, hipStream_t st) {
   typedef Tile<T, HD> L;
-  a.few_upto = pl.few_upto;
-  Args few = a, many = a;
-  const int64_t n = pl.few_parts + pl.many_parts;
-  few.split = pl.few_split; few.chunk = pl.few_chunk; few.part = workspace; few.part_ml = (float2*)(workspace + n * HD);
-  many.split = pl.many_split; many.chunk = pl.many_chunk; many.part = workspace + pl.few_parts * HD; many.part_ml = few.part_ml + pl.few_parts;
-  few.row_blocks = pl.few_blocks;
-  many.row_blocks = pl.many_blocks;
+  a.few_upto = pl.few_upto; a.few_blocks = pl.few_blocks; a.many_blocks = pl.many_blocks; a.runs = pl.runs;
+  a.plan = (int64_t*)workspace;
+  a.part_ml = (float2*)((unsigned char*)workspace + plan_bytes(pl));
+  a.part = (float*)(a.part_ml + (int64_t)pl.runs * 2 * FEW);
   const int64_t pairs = (int64_t)a.c.sequences * a.c.kv_heads;
-  const int64_t few_grid = pairs * pl.few_blocks * pl.few_split, many_grid = pairs * pl.many_blocks * pl.many_split,
-                join_grid = up((int64_t)a.c.sequences * pl.tokens * a.heads, 4);
-  if (few_grid > 0x7FFFFFFF || many_grid > 0x7FFFFFFF || join_grid > 0x7FFFFFFF) return hipErrorInvalidValue;
+  const int64_t few_grid = pl.runs ? pl.runs : pairs * pl.few_blocks, many_grid = pairs * pl.many_blocks, join_grid = up((int64_t)a.c.sequences * pl.tokens * a.heads, 4);
+  if (few_grid > 0x7FFFFFFF || many_grid > 0x7FFFFFFF || join_grid > 0x7FFFFFFF || pl.entries > 0x7FFFFFFF) return hipErrorInvalidValue;
   constexpr int FEW_LDS = 4 * 2 * L::BLOCKB, MANY_LDS = 2 * 2 * 2 * L::BLOCKB;
   static_assert(4 * FEW * HD * 4 <= FEW_LDS, "the wavefronts' sums fit where their tiles were");
   static bool attr_done = false;  // one flag per instantiation
@@ -587,36 +607,31 @@ hipError_t launch(const Plan& pl, Args a, float* workspace, hipStream_t st) {
     if (e != hipSuccess) return e;
     attr_done = true;
   }
-  if (pl.many) {
-    many_k<T, HD><<<(unsigned)many_grid, 256, MANY_LDS, st>>>(many);
-  }
-  if (pl.few) {
-    few_k<T, HD><<<(unsigned)few_grid, 256, FEW_LDS, st>>>(few);
-  }
-  if (n > 0) join_k<T, HD><<<(unsigned)join_grid, 256, 0, st>>>(few, many, pl.tokens);
+  if (pl.many) many_k<T, HD><<<(unsigned)many_grid, 256, MANY_LDS, st>>>(a);
+  if (pl.few) few_k<T, HD><<<(unsigned)few_grid, 256, FEW_LDS, st>>>(a);
+  if (pl.runs) join_k<T, HD><<<(unsigned)join_grid, 256, 0, st>>>(a, pl.tokens);
   return hipGetLastError();
 }
 
 }  // namespace
 
-size_t attention_paged_bytes(const CacheView& c, int64_t rows, int heads, int max_new, int64_t max_length, int window) {
+size_t attention_paged_bytes(int dt, const CacheView& c, int64_t rows, int heads, int max_new, int64_t max_length, int window) {
   if (rows == 0 || c.sequences == 0 || max_new == 0) return 0;
-  const Plan p = plan_of(c, rows, heads, max_new, max_length, window);
-  return (size_t)(p.few_parts + p.many_parts) * ((c.head_dim <= 64 ? 64 : 128) * 4 + 8);
+  const Plan p = plan_of(dt, c, rows, heads, max_new, max_length, window);
+  return plan_bytes(p) + (size_t)p.runs * 2 * FEW * (8 + (c.head_dim <= 64 ? 64 : 128) * 4);
 }
 
 hipError_t attention_paged(int dt, const CacheView& c, int heads, int64_t rows, int max_new, int64_t max_length, int window, float scale, const void* q, int64_t ldq,
                            void* out, int64_t ldo, float* lse, void* workspace, hipStream_t st) {
   if (rows == 0 || c.sequences == 0 || max_new == 0) return hipSuccess;
-  const Plan pl = plan_of(c, rows, heads, max_new, max_length, window);
+  const Plan pl = plan_of(dt, c, rows, heads, max_new, max_length, window);
   Args a{};
   a.c = c; a.heads = heads; a.group = heads / c.kv_heads;
   a.rows = rows; a.ldq = ldq; a.ldo = ldo; a.max_new = max_new; a.window = window;
   a.scale_log2e = scale * 1.4426950408889634f;
   a.q = q; a.out = out; a.lse = lse;
-  float* ws = (float*)workspace;
-  if (dt == DT_BF16) return c.head_dim <= 64 ? launch<bf16, 64>(pl, a, ws, st) : launch<bf16, 128>(pl, a, ws, st);
-  return c.head_dim <= 64 ? launch<float, 64>(pl, a, ws, st) : launch<float, 128>(pl, a, ws, st);
+  if (dt == DT_BF16) return c.head_dim <= 64 ? launch<bf16, 64>(pl, a, workspace, st) : launch<bf16, 128>(pl, a, workspace, st);
+  return c.head_dim <= 64 ? launch<float, 64>(pl, a, workspace, st) : launch<float, 128>(pl, a, workspace, st);
 }
 
 }  // namespace hift

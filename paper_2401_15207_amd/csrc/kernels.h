@@ -273,7 +273,7 @@ struct CacheView {
 hipError_t cache_append(int dt, const CacheView& c, int heads, bool pairs, int rot, const float* cos_sin, int table_rows, int64_t rows, int max_new,
                         const void* qkv, int64_t ld, void* q, int64_t ldq, hipStream_t st);
 // attention of the new rows over the cache (attention_paged.hip)
-size_t attention_paged_bytes(const CacheView& c, int64_t rows, int heads, int max_new, int64_t max_length, int window);
+size_t attention_paged_bytes(int dt, const CacheView& c, int64_t rows, int heads, int max_new, int64_t max_length, int window);
 hipError_t attention_paged(int dt, const CacheView& c, int heads, int64_t rows, int max_new, int64_t max_length, int window, float scale, const void* q, int64_t ldq,
                            void* out, int64_t ldo, float* lse, void* workspace, hipStream_t st);
 // logits with penalties for seen tokens, bias and mask, or the gradient g through them (adjust.hip)

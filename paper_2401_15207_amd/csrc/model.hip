@@ -2947,7 +2947,7 @@ hift_status hift_kernel_attention_paged_bytes(const hift_cache* cache, int64_t r
   CacheView c;
   ST_TRY(cache_view(cache, rows, nullptr, max_new, heads, &c));
   if (max_length < 0 || window < 0) return fail(HIFT_EINVAL, "negative max_length or window");
-  *bytes = attention_paged_bytes(c, rows, heads, (int)std::min<int64_t>(max_new, rows), max_length, window);
+  *bytes = attention_paged_bytes(cache->dtype == HIFT_BF16 ? DT_BF16 : DT_F32, c, rows, heads, (int)std::min<int64_t>(max_new, rows), max_length, window);
   return HIFT_OK;
 }
 

@@ -25,6 +25,7 @@ struct TableArgs {
   double amplitude;
   float2* cs;
   double turns[ROTARY_ROT_MAX / 2];  // whole turns a position, by pair
+  double step_cos[ROTARY_ROT_MAX / 2], step_sin[ROTARY_ROT_MAX / 2];  // and their cosine and sine
 };
 
 // cos and sin of 2 pi f, |f| <= 1/2: the multiple of a quarter nearest to f aside, what is left is an angle of at most pi / 4, of which the
@@ -47,20 +48,27 @@ __device__ __forceinline__ void turn_of(double f, double& c, double& s) {
   if (k >= 2) s = -s;
 }
 
-// A workgroup takes TABLE_EACH entries in a row.  Angles are held in turns and in 64 bits: at position 2^20 their error is below 2^-32 of a turn.
-constexpr int TABLE_EACH = 4 * BLK;
+// A thread takes a pair at TABLE_ROWS positions, the first from its angle (in turns and 64 bits: at position 2^20 the error is below 2^-32 of a turn) and
+// each next one by the rotation of one position, which takes a fifth of the operations and adds less than 2^-50 a step.
+constexpr int TABLE_ROWS = 8;
 __global__ void __launch_bounds__(BLK) rotary_table_k(TableArgs p) {
-  const int64_t first = (int64_t)blockIdx.x * TABLE_EACH, row0 = first / p.half, left = p.count * p.half - first;
-  const int in = (int)(first - row0 * p.half);
+  const int64_t first = (int64_t)blockIdx.x * BLK, group0 = first / p.half;
+  const unsigned at = (unsigned)(first - group0 * p.half) + threadIdx.x, group = at / (unsigned)p.half, pair = at - group * (unsigned)p.half;
+  const int64_t row = (group0 + group) * TABLE_ROWS;
+  if (row >= p.count) return;
+  const double a = (double)(p.first + row) * p.turns[pair], dc = p.step_cos[pair], ds = p.step_sin[pair];
+  double c, s;
+  turn_of(a - rint(a), c, s);
+  c *= p.amplitude;
+  s *= p.amplitude;
+  float2* out = p.cs + row * p.half + pair;
+  const int n = (int)min(p.count - row, (int64_t)TABLE_ROWS);
 #pragma unroll
-  for (int k = 0; k < TABLE_EACH; k += BLK) {
-    const int i = k + (int)threadIdx.x;
-    if (i >= left) return;
-    const unsigned at = (unsigned)(in + i), row = at / (unsigned)p.half, pair = at - row * (unsigned)p.half;
-    const double a = (double)(p.first + row0 + row) * p.turns[pair];
-    double c, s;
-    turn_of(a - rint(a), c, s);
-    p.cs[first + i] = make_float2((float)(c * p.amplitude), (float)(s * p.amplitude));
+  for (int k = 0; k < TABLE_ROWS; ++k) {
+    if (k < n) out[(int64_t)k * p.half] = make_float2((float)c, (float)s);
+    const double next = fma(c, dc, -s * ds);
+    s = fma(s, dc, c * ds);
+    c = next;
   }
 }
 
@@ -270,7 +278,11 @@ hipError_t rotary_table(int rot, const double* turns, double amplitude, int64_t 
   TableArgs p{};
   p.half = rot / 2; p.first = first; p.count = count; p.amplitude = amplitude; p.cs = (float2*)cos_sin;
   std::copy(turns, turns + rot / 2, p.turns);
-  const int64_t blocks = (count * p.half + TABLE_EACH - 1) / TABLE_EACH;
+  for (int i = 0; i < p.half; ++i) {
+    p.step_cos[i] = cos(6.283185307179586476925 * turns[i]);
+    p.step_sin[i] = sin(6.283185307179586476925 * turns[i]);
+  }
+  const int64_t blocks = ((count + TABLE_ROWS - 1) / TABLE_ROWS * p.half + BLK - 1) / BLK;
   if (blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
   rotary_table_k<<<(unsigned)blocks, BLK, 0, st>>>(p);
   return hipGetLastError();
