@@ -9,7 +9,8 @@
 //   few_k    32 rows a workgroup: all four wavefronts hold the same rows and take turns at the blocks of 32 keys, each through LDS tiles of its own
 //            without any barrier, and their results are joined at the end.  Bound by reading the cache.  Lengths are known on the device only, and
 //            differ: the keys of all sequences and heads, one after the other, are cut into equal runs, a workgroup each, wherever that falls.
-//   many_k   128 rows a workgroup, 32 a wavefront, which share tiles of 64 keys.  Bound by the matrix instructions.
+//   wide_k   (bf16) 256 rows a workgroup, 32 a wavefront, which share tiles of 64 keys; many_k (fp32) 128 rows.  Bound by the matrix
+//            instructions.
 //   join_k   rows whose keys fell to several workgroups: the parts, weighted by their maxima.
 #include <math.h>
 
@@ -45,7 +46,7 @@ struct Args {
   const void* q;
   void* out;
   float* lse;           // [rows, heads] or null
-  int few_upto;         // sequences of at most so many rows are few_k's, the others many_k's
+  int few_upto;         // sequences of at most so many rows are few_k's, the others wide_k's or many_k's
   int few_blocks, many_blocks;  // blocks of rows of the longest sequence
   int runs;             // few_k's workgroups; 0: one a block of rows and key head, and nothing to join
   int64_t* plan;        // [0]: steps of a run; [1 + e]: steps before entry e
@@ -147,6 +148,13 @@ struct Tile {
     }
     return s;
   }
+  // bf16: values of keys 16 t ..+15 of a block, columns 32 nb ..+31, as the matrix instruction takes them
+  __device__ static __forceinline__ bf16x8 value_frag(const unsigned char* v, const Address& a, int t, int nb) {
+    const v4i16 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((v4i16 __attribute__((address_space(3)))*)(v + t * 16 * ROWB + a.v[nb][0]));
+    const v4i16 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((v4i16 __attribute__((address_space(3)))*)(v + t * 16 * ROWB + a.v[nb][1]));
+    const v8i16 both = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    return __builtin_bit_cast(bf16x8, both);
+  }
   // out += p (of the block's keys) times its values.  Lane: query row lane % 32; element e of out[nb]: column 32 nb + 8 (e / 4) + 4 (lane / 32) + e % 4
   __device__ static __forceinline__ void values(f32x16 (&out)[NB], const unsigned char* v, const Address& a, const f32x16& p, int lane) {
     if constexpr (F32) {
@@ -167,12 +175,7 @@ struct Tile {
 #pragma unroll
         for (int e = 0; e < 8; ++e) pf[e] = static_cast<__bf16>(p[8 * t + e]);
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb) {
-          const v4i16 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((v4i16 __attribute__((address_space(3)))*)(v + t * 16 * ROWB + a.v[nb][0]));
-          const v4i16 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((v4i16 __attribute__((address_space(3)))*)(v + t * 16 * ROWB + a.v[nb][1]));
-          const v8i16 both = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-          vf[nb] = __builtin_bit_cast(bf16x8, both);
-        }
+        for (int nb = 0; nb < NB; ++nb) vf[nb] = value_frag(v, a, t, nb);
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) out[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[nb], pf, out[nb], 0, 0, 0);
       }
@@ -444,7 +447,7 @@ __global__ void __launch_bounds__(256) few_k(Args p) {
   }
 }
 
-// ---- many rows ----
+// ---- many rows, fp32 ----
 template <typename T, int HD>
 __global__ void __launch_bounds__(256) many_k(Args p) {
   typedef Tile<T, HD> L;
@@ -524,6 +527,163 @@ __global__ void __launch_bounds__(256) many_k(Args p) {
   if (fh == 0 && p.lse) p.lse[at.row * p.heads + at.head] = run.m + __builtin_amdgcn_logf(run.l);
 }
 
+// ---- many rows, bf16 ----
+// 256 rows a workgroup, 32 a wavefront, two wavefronts a SIMD.  Within a wavefront the products of one block of 32 keys run beside the exponentials of
+// the one before:
+//   scores of block i (8 MFMAs)                     beside the second half of the exponentials of block i - 1
+//   P V of block i - 1, its first 16 keys (4 MFMAs) beside the row maxima of block i
+//   its other 16 keys (4 MFMAs)                     beside the first half of the exponentials of block i
+template <int HD>
+__global__ void __launch_bounds__(512) wide_k(Args p) {
+  typedef Tile<bf16, HD> L;
+  constexpr int NB = L::NB, NQ = L::NQ, KT = 2 * KB, TILEB = KT * L::ROWB, QB = 256;
+  extern __shared__ unsigned char lds[];  // [2] tiles of K | [3] of V
+  __shared__ int pages_there[4][4];       // by tile and 16 keys
+  const int tid = threadIdx.x, lane = tid & 63, wave = UNIFORM(tid >> 6), fr = lane & 31, fh = lane >> 5;
+  const int block = p.many_blocks - 1 - (int)(blockIdx.x % (unsigned)p.many_blocks), pair = (int)(blockIdx.x / (unsigned)p.many_blocks);  // most keys first
+  const int s = pair / p.c.kv_heads, kv_head = pair % p.c.kv_heads;
+  const CacheSeq of = cache_seq(p.c, s, p.rows, p.max_new);
+  const int n_rows = of.fresh * p.group;
+  if (n_rows <= p.few_upto || block * QB >= n_rows) return;
+  const int m0 = block * QB, m_last = min(n_rows, m0 + QB) - 1;
+  int from, to;
+  keys_of(of, m0 / p.group, m_last / p.group, p.window, from, to);
+  const int w0 = m0 + wave * 32, w_last = min(w0 + 31, m_last);  // this wavefront's rows
+  const int pos_lo = of.cached + w0 / p.group, pos_hi = of.cached + w_last / p.group;
+  const RowAt at = row_at(p, of, kv_head, w0 + fr);
+  typename L::Frag q[NQ];
+  L::load_row(q, (const bf16*)p.q + at.row * p.ldq + (int64_t)at.head * p.c.head_dim, at.ok, p.c.head_dim, fh);
+  uint32_t vo[L::IPG];
+  L::offsets(vo, lane, p.c.head_dim);
+  typename L::Address ad;
+  L::addresses(ad, lane);
+  const uint32_t lds0 = (uint32_t)reinterpret_cast<uintptr_t>(lds);
+  const L head(p.c, kv_head);
+  const int tiles = (to - from + KT - 1) / KT;
+  // tiles that this wavefront's rows see
+  const int mine = w0 > m_last ? 0 : min(tiles, (min(to, pos_hi + 1) - from + KT - 1) / KT);
+
+  // whether all pages are there
+  bool lane_whole = true;
+  for (int key = from + lane * GROUP; key < to; key += 64 * GROUP) lane_whole &= cache_page_any(p.c, s, key) >= 0;
+  const bool whole = __builtin_amdgcn_ballot_w64(!lane_whole) == 0;
+  // every wavefront brings 16 keys of a tile, or their values
+  const int part = (wave & 3) * GROUP;
+  auto page = [&](int t) { const int key = from + t * KT + part; return UNIFORM(t < tiles && key < to ? cache_page(p.c, s, key) : -1); };
+  int page_next = page(0);
+  uint32_t v_last = 0, v_now = 0, v_next = 2 * TILEB;  // LDS offsets of the values of the tile before, of this one and of the next
+  auto request = [&](int t) __attribute__((always_inline)) {
+    head.request(wave < 4 ? p.c.k : p.c.v, from + t * KT + part, page_next, to, vo, lds0 + (wave < 4 ? (t & 1) * TILEB : v_next) + part * L::ROWB);
+    if (lane == 0 && wave < 4) pages_there[t & 3][wave] = page_next >= 0;
+    page_next = page(t + 1);
+  };
+  // Tile t is there; the next one sets out.
+  auto advance = [&](int t) __attribute__((always_inline)) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    v_last = v_now;
+    v_now = v_next;
+    v_next = v_next == 4 * TILEB ? 2 * TILEB : v_next + TILEB;
+    if (t + 1 < tiles) request(t + 1);
+  };
+
+  float m = -INFINITY, ref = 0.f, l = 0.f;
+  f32x16 o[NB];
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[nb][e] = 0.f;
+  bf16x8 pr[2];  // probabilities by half of the block
+
+  auto exponentials = [&](const f32x16& S, int h) __attribute__((always_inline)) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(S[8 * h + e], p.scale_log2e, -ref));
+      l += x;
+      pr[h][e] = static_cast<__bf16>(x);
+    }
+  };
+  auto times_values = [&](const unsigned char* V, int h) __attribute__((always_inline)) {
+    bf16x8 f[NB];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) f[nb] = L::value_frag(V, ad, h, nb);
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) o[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[nb], pr[h], o[nb], 0, 0, 0);
+  };
+  auto row_max = [&](const f32x16& S) __attribute__((always_inline)) {
+    float top = S[0];
+#pragma unroll
+    for (int e = 1; e < 16; ++e) top = fmaxf(top, S[e]);
+    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+    return fmaxf(__uint_as_float(both[0]), __uint_as_float(both[1])) * p.scale_log2e;
+  };
+  auto mask = [&](f32x16& S, int t, int b) __attribute__((always_inline)) {
+    const int key0 = from + t * KT + b * KB;
+    if (whole && key0 + KB <= to && key0 + KB - 1 <= pos_lo && (p.window == 0 || key0 > pos_hi - p.window)) return;
+    mask_scores<L>(S, key0, fh, to, at.pos, of.total, p.window, pages_there[t & 3][2 * b] != 0, pages_there[t & 3][2 * b + 1] != 0);
+  };
+  // The reference is raised, and what was summed against it rescaled, where a score exceeds it by more than 2^8 (see Running).
+  auto raise = [&](float top) __attribute__((always_inline)) {
+    const float now = fmaxf(m, top), by = now == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - now);
+    l *= by;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[nb][e] *= by;
+    m = now;
+    ref = now == -INFINITY ? 0.f : now;
+  };
+
+  // scores of block b of tile t into `now` while the block before, its scores in `last` and its values at V, is finished
+  auto step = [&](int t, int b, const f32x16& last, f32x16& now, const unsigned char* V) __attribute__((always_inline)) {
+    now = L::scores(lds + (t & 1) * TILEB + b * L::BLOCKB, ad, q);
+    exponentials(last, 1);
+    mask(now, t, b);
+    times_values(V, 0);
+    const float top = row_max(now);
+    times_values(V, 1);
+    if (__builtin_amdgcn_ballot_w64(top > m + 8.0f) != 0) raise(top);
+    exponentials(now, 0);
+  };
+  if (tiles > 0) request(0);
+  int t = 0;
+  if (mine > 0) {
+    f32x16 S0, S1;
+    advance(0);
+    S0 = L::scores(lds, ad, q);
+    mask(S0, 0, 0);
+    raise(row_max(S0));
+    exponentials(S0, 0);
+    step(0, 1, S0, S1, lds + v_now);
+    for (t = 1; t < mine; ++t) {
+      advance(t);
+      step(t, 0, S1, S0, lds + v_last + L::BLOCKB);
+      step(t, 1, S0, S1, lds + v_now);
+    }
+    exponentials(S1, 1);
+    times_values(lds + v_now + L::BLOCKB, 0);
+    times_values(lds + v_now + L::BLOCKB, 1);
+  }
+  for (; t < tiles; ++t) advance(t);  // the others' tiles
+
+  l += __shfl_xor(l, 32, 64);
+  if (!at.ok) return;
+  const float inv = l > 0.f || l != l ? 1.0f / l : 0.f;
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int c = nb * 32 + 8 * g + 4 * fh;
+      if (c < p.c.head_dim) {
+        Vec<bf16, 4> v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v.v[e] = from_f32<bf16>(o[nb][4 * g + e] * inv);
+        *reinterpret_cast<Vec<bf16, 4>*>((bf16*)p.out + at.row * p.ldo + (int64_t)at.head * p.c.head_dim + c) = v;
+      }
+    }
+  if (fh == 0 && p.lse) p.lse[at.row * p.heads + at.head] = m + __builtin_amdgcn_logf(l);
+}
+
 // ---- rows whose keys fell to several runs ----
 // One wavefront a row and head of the first `tokens` tokens of a sequence.
 template <typename T, int HD>
@@ -571,12 +731,12 @@ Plan plan_of(int dt, const CacheView& c, int64_t rows, int heads, int max_new, i
   Plan p{};
   const int group = heads / c.kv_heads;
   const int64_t most = (int64_t)max_new * group, pairs = (int64_t)c.sequences * c.kv_heads;  // rows of the longest sequence
-  // many_k shares a tile of keys among four times the rows; few_k gives four times the workgroups, and takes all where they do not fill the chip
+  // the kernels for many rows share a tile of keys among more of them; few_k gives more workgroups, and takes all where they do not fill the chip
   p.many = most > FEW && pairs * up(most, FEW) > 1024;
-  p.few = !p.many || rows < (int64_t)c.sequences * max_new;  // else no sequence is short where the longest is not, as a rule; many_k takes any
+  p.few = !p.many || rows < (int64_t)c.sequences * max_new;  // else no sequence is short where the longest is not, as a rule; wide_k and many_k take any
   p.few_upto = !p.many ? INT32_MAX : p.few ? FEW : 0;
   p.few_blocks = (int)(p.many ? 1 : std::max<int64_t>(1, up(most, FEW)));
-  p.many_blocks = (int)std::max<int64_t>(1, up(most, 128));
+  p.many_blocks = (int)std::max<int64_t>(1, up(most, dt == DT_BF16 ? 256 : 128));
   p.entries = (int64_t)c.sequences * p.few_blocks;
   p.tokens = p.many ? std::min(max_new, FEW) : max_new;
   int64_t span = std::max<int64_t>(1, std::min<int64_t>(max_length, (int64_t)c.max_pages << c.page_shift));
@@ -589,6 +749,12 @@ Plan plan_of(int dt, const CacheView& c, int64_t rows, int heads, int max_new, i
 size_t plan_bytes(const Plan& p) { return p.runs ? (size_t)((1 + p.entries) * 8 + 15) / 16 * 16 : 0; }
 
 template <typename T, int HD>
+auto many_kernel() {
+  if constexpr (sizeof(T) == 2) return wide_k<HD>;
+  else return many_k<T, HD>;
+}
+
+template <typename T, int HD>
 hipError_t launch(const Plan& pl, Args a, void* workspace, hipStream_t st) {
   typedef Tile<T, HD> L;
   a.few_upto = pl.few_upto; a.few_blocks = pl.few_blocks; a.many_blocks = pl.many_blocks; a.runs = pl.runs;
@@ -598,16 +764,17 @@ hipError_t launch(const Plan& pl, Args a, void* workspace, hipStream_t st) {
   const int64_t pairs = (int64_t)a.c.sequences * a.c.kv_heads;
   const int64_t few_grid = pl.runs ? pl.runs : pairs * pl.few_blocks, many_grid = pairs * pl.many_blocks, join_grid = up((int64_t)a.c.sequences * pl.tokens * a.heads, 4);
   if (few_grid > 0x7FFFFFFF || many_grid > 0x7FFFFFFF || join_grid > 0x7FFFFFFF || pl.entries > 0x7FFFFFFF) return hipErrorInvalidValue;
-  constexpr int FEW_LDS = 4 * 2 * L::BLOCKB, MANY_LDS = 2 * 2 * 2 * L::BLOCKB;
+  constexpr int FEW_LDS = 4 * 2 * L::BLOCKB, MANY_LDS = (sizeof(T) == 2 ? 5 : 4) * 2 * L::BLOCKB;
   static_assert(4 * FEW * HD * 4 <= FEW_LDS, "the wavefronts' sums fit where their tiles were");
+  const auto many = many_kernel<T, HD>();
   static bool attr_done = false;  // one flag per instantiation
   if (!attr_done) {
-    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(many_k<T, HD>), hipFuncAttributeMaxDynamicSharedMemorySize, MANY_LDS);
+    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(many), hipFuncAttributeMaxDynamicSharedMemorySize, MANY_LDS);
     if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(few_k<T, HD>), hipFuncAttributeMaxDynamicSharedMemorySize, FEW_LDS);
     if (e != hipSuccess) return e;
     attr_done = true;
   }
-  if (pl.many) many_k<T, HD><<<(unsigned)many_grid, 256, MANY_LDS, st>>>(a);
+  if (pl.many) many<<<(unsigned)many_grid, sizeof(T) == 2 ? 512 : 256, MANY_LDS, st>>>(a);
   if (pl.few) few_k<T, HD><<<(unsigned)few_grid, 256, FEW_LDS, st>>>(a);
   if (pl.runs) join_k<T, HD><<<(unsigned)join_grid, 256, 0, st>>>(a, pl.tokens);
   return hipGetLastError();
