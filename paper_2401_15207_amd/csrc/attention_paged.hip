@@ -9,7 +9,7 @@
 //   few_k    32 rows a workgroup: all four wavefronts hold the same rows and take turns at the blocks of 32 keys, each through LDS tiles of its own
 //            without any barrier, and their results are joined at the end.  Bound by reading the cache.  Lengths are known on the device only, and
 //            differ: the keys of all sequences and heads, one after the other, are cut into equal runs, a workgroup each, wherever that falls.
-//   wide_k   (bf16) 256 rows a workgroup, 32 a wavefront, which share tiles of 64 keys; many_k (fp32) 128 rows.  Bound by the matrix
+//   wide_k (bf16), many_k (fp32)   128 rows a workgroup, 32 a wavefront, which share tiles of 64 keys.  Bound by the matrix
 //            instructions.
 //   join_k   rows whose keys fell to several workgroups: the parts, weighted by their maxima.
 #include <math.h>
@@ -528,20 +528,44 @@ __global__ void __launch_bounds__(256) many_k(Args p) {
 }
 
 // ---- many rows, bf16 ----
-// 256 rows a workgroup, 32 a wavefront, two wavefronts a SIMD.  Within a wavefront the products of one block of 32 keys run beside the exponentials of
+// 128 rows a workgroup, 32 a wavefront, two workgroups a compute unit.  Within a wavefront the products of one block of 32 keys run beside the exponentials of
 // the one before:
-//   scores of block i (8 MFMAs)                     beside the second half of the exponentials of block i - 1
-//   P V of block i - 1, its first 16 keys (4 MFMAs) beside the row maxima of block i
-//   its other 16 keys (4 MFMAs)                     beside the first half of the exponentials of block i
+//   scores of block i (8 MFMAs)     beside the exponentials of block i - 1
+//   P V of block i - 1 (8 MFMAs)    beside the row maxima of block i
+
+// The sequence that has `rank` longer ones before it; with more than 256 of them, which fill the chip in any order, the rank-th.
+__device__ __forceinline__ int longest(const Args& p, int rank, int* lengths) {
+  const int n = p.c.sequences, tid = threadIdx.x;
+  if (n == 1 || n > 256) return rank;
+  int mine = 0;
+  if (tid < n) {
+    const CacheSeq of = cache_seq(p.c, tid, p.rows, p.max_new);
+    lengths[tid] = mine = of.fresh ? of.total : -1;
+  }
+  __syncthreads();
+  int before = 0;
+  if (tid < n)
+    for (int k = 0; k < n; ++k) before += (lengths[k] > mine) | ((lengths[k] == mine) & (k < tid));
+  __syncthreads();
+  if (tid < n && before == rank) lengths[0] = tid;
+  __syncthreads();
+  const int s = UNIFORM(lengths[0]);
+  __syncthreads();
+  return s;
+}
+
 template <int HD>
-__global__ void __launch_bounds__(512) wide_k(Args p) {
+__global__ void __launch_bounds__(256, 2) wide_k(Args p) {
   typedef Tile<bf16, HD> L;
-  constexpr int NB = L::NB, NQ = L::NQ, KT = 2 * KB, TILEB = KT * L::ROWB, QB = 256;
+  constexpr int NB = L::NB, NQ = L::NQ, KT = 2 * KB, TILEB = KT * L::ROWB, QB = 128;
   extern __shared__ unsigned char lds[];  // [2] tiles of K | [3] of V
-  __shared__ int pages_there[4][4];       // by tile and 16 keys
   const int tid = threadIdx.x, lane = tid & 63, wave = UNIFORM(tid >> 6), fr = lane & 31, fh = lane >> 5;
-  const int block = p.many_blocks - 1 - (int)(blockIdx.x % (unsigned)p.many_blocks), pair = (int)(blockIdx.x / (unsigned)p.many_blocks);  // most keys first
-  const int s = pair / p.c.kv_heads, kv_head = pair % p.c.kv_heads;
+  // Workgroups start in the order of their index: those with the most keys first.  Neighbours take different heads, so that the workgroups of a head, which read
+  // the same keys, are on one of the eight dies where the heads are a multiple of them.
+  int i = (int)blockIdx.x;
+  const int kv_head = i % p.c.kv_heads;
+  i /= p.c.kv_heads;
+  const int block = p.many_blocks - 1 - i % p.many_blocks, s = longest(p, i / p.many_blocks, reinterpret_cast<int*>(lds));
   const CacheSeq of = cache_seq(p.c, s, p.rows, p.max_new);
   const int n_rows = of.fresh * p.group;
   if (n_rows <= p.few_upto || block * QB >= n_rows) return;
@@ -567,24 +591,23 @@ __global__ void __launch_bounds__(512) wide_k(Args p) {
   bool lane_whole = true;
   for (int key = from + lane * GROUP; key < to; key += 64 * GROUP) lane_whole &= cache_page_any(p.c, s, key) >= 0;
   const bool whole = __builtin_amdgcn_ballot_w64(!lane_whole) == 0;
-  // every wavefront brings 16 keys of a tile, or their values
-  const int part = (wave & 3) * GROUP;
+  // every wavefront brings 16 keys of a tile and their values
+  const int part = wave * GROUP;
   auto page = [&](int t) { const int key = from + t * KT + part; return UNIFORM(t < tiles && key < to ? cache_page(p.c, s, key) : -1); };
   int page_next = page(0);
   uint32_t v_last = 0, v_now = 0, v_next = 2 * TILEB;  // LDS offsets of the values of the tile before, of this one and of the next
   auto request = [&](int t) __attribute__((always_inline)) {
-    head.request(wave < 4 ? p.c.k : p.c.v, from + t * KT + part, page_next, to, vo, lds0 + (wave < 4 ? (t & 1) * TILEB : v_next) + part * L::ROWB);
-    if (lane == 0 && wave < 4) pages_there[t & 3][wave] = page_next >= 0;
+    head.request(p.c.k, from + t * KT + part, page_next, to, vo, lds0 + (t & 1) * TILEB + part * L::ROWB);
+    head.request(p.c.v, from + t * KT + part, page_next, to, vo, lds0 + v_next + part * L::ROWB);
     page_next = page(t + 1);
   };
-  // Tile t is there; the next one sets out.
-  auto advance = [&](int t) __attribute__((always_inline)) {
+  // Tile t is there, and where the next one goes nobody reads any more.
+  auto advance = [&]() __attribute__((always_inline)) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
     v_last = v_now;
     v_now = v_next;
     v_next = v_next == 4 * TILEB ? 2 * TILEB : v_next + TILEB;
-    if (t + 1 < tiles) request(t + 1);
   };
 
   float m = -INFINITY, ref = 0.f, l = 0.f;
@@ -603,10 +626,15 @@ __global__ void __launch_bounds__(512) wide_k(Args p) {
       pr[h][e] = static_cast<__bf16>(x);
     }
   };
-  auto times_values = [&](const unsigned char* V, int h) __attribute__((always_inline)) {
-    bf16x8 f[NB];
+  auto read_keys = [&](bf16x8 (&f)[NQ], const unsigned char* K) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) f[i] = *reinterpret_cast<const bf16x8*>(K + ad.k[i]);
+  };
+  auto read_values = [&](bf16x8 (&f)[NB], const unsigned char* V, int h) __attribute__((always_inline)) {
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) f[nb] = L::value_frag(V, ad, h, nb);
+  };
+  auto times_values = [&](const bf16x8 (&f)[NB], int h) __attribute__((always_inline)) {
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) o[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[nb], pr[h], o[nb], 0, 0, 0);
   };
@@ -620,7 +648,8 @@ __global__ void __launch_bounds__(512) wide_k(Args p) {
   auto mask = [&](f32x16& S, int t, int b) __attribute__((always_inline)) {
     const int key0 = from + t * KT + b * KB;
     if (whole && key0 + KB <= to && key0 + KB - 1 <= pos_lo && (p.window == 0 || key0 > pos_hi - p.window)) return;
-    mask_scores<L>(S, key0, fh, to, at.pos, of.total, p.window, pages_there[t & 3][2 * b] != 0, pages_there[t & 3][2 * b + 1] != 0);
+    const bool there0 = whole || cache_page(p.c, s, key0) >= 0, there1 = whole || cache_page(p.c, s, key0 + GROUP) >= 0;
+    mask_scores<L>(S, key0, fh, to, at.pos, of.total, p.window, there0, there1);
   };
   // The reference is raised, and what was summed against it rescaled, where a score exceeds it by more than 2^8 (see Running).
   auto raise = [&](float top) __attribute__((always_inline)) {
@@ -634,37 +663,64 @@ __global__ void __launch_bounds__(512) wide_k(Args p) {
     ref = now == -INFINITY ? 0.f : now;
   };
 
-  // scores of block b of tile t into `now` while the block before, its scores in `last` and its values at V, is finished
-  auto step = [&](int t, int b, const f32x16& last, f32x16& now, const unsigned char* V) __attribute__((always_inline)) {
-    now = L::scores(lds + (t & 1) * TILEB + b * L::BLOCKB, ad, q);
+  // Scores of block b of tile t into `now` while the block before, its scores in `last` and its values at V, is finished.  What is multiplied has been read from
+  // LDS a phase before: keys f by the caller, for the next block of the tile here.
+  auto step = [&](int t, int b, const f32x16& last, f32x16& now, const unsigned char* V, bf16x8 (&f)[NQ]) __attribute__((always_inline)) {
+    bf16x8 v0[NB], v1[NB];
+    read_values(v0, V, 0);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) now[e] = 0.f;
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) now = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i], q[i], now, 0, 0, 0);
+    exponentials(last, 0);
     exponentials(last, 1);
+    __builtin_amdgcn_sched_group_barrier(0x100, 2 * NB, 0);  // two exponentials after each MFMA
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x2, 5 * 8 / NQ, 0);
+      __builtin_amdgcn_sched_group_barrier(0x400, 2 * 8 / NQ, 0);
+    }
+    asm volatile("" : "+v"(pr[0]), "+v"(pr[1]), "+v"(l));  // here and not behind the branches below
+    if (b == 0 && t + 1 < tiles) request(t + 1);
     mask(now, t, b);
-    times_values(V, 0);
+    read_values(v1, V, 1);
+    times_values(v0, 0);
+    if (b == 0) read_keys(f, lds + (t & 1) * TILEB + L::BLOCKB);
+    times_values(v1, 1);
     const float top = row_max(now);
-    times_values(V, 1);
     if (__builtin_amdgcn_ballot_w64(top > m + 8.0f) != 0) raise(top);
-    exponentials(now, 0);
   };
   if (tiles > 0) request(0);
   int t = 0;
   if (mine > 0) {
     f32x16 S0, S1;
-    advance(0);
+    bf16x8 f[NQ];
+    advance();
+    if (tiles > 1) request(1);
     S0 = L::scores(lds, ad, q);
     mask(S0, 0, 0);
     raise(row_max(S0));
-    exponentials(S0, 0);
-    step(0, 1, S0, S1, lds + v_now);
+    read_keys(f, lds + L::BLOCKB);
+    step(0, 1, S0, S1, lds + v_now, f);
     for (t = 1; t < mine; ++t) {
-      advance(t);
-      step(t, 0, S1, S0, lds + v_last + L::BLOCKB);
-      step(t, 1, S0, S1, lds + v_now);
+      advance();
+      read_keys(f, lds + (t & 1) * TILEB);
+      step(t, 0, S1, S0, lds + v_last + L::BLOCKB, f);
+      step(t, 1, S0, S1, lds + v_now, f);
     }
+    exponentials(S1, 0);
     exponentials(S1, 1);
-    times_values(lds + v_now + L::BLOCKB, 0);
-    times_values(lds + v_now + L::BLOCKB, 1);
+    bf16x8 v[NB];
+    read_values(v, lds + v_now + L::BLOCKB, 0);
+    times_values(v, 0);
+    read_values(v, lds + v_now + L::BLOCKB, 1);
+    times_values(v, 1);
   }
-  for (; t < tiles; ++t) advance(t);  // the others' tiles
+  for (; t < tiles; ++t) {  // the others' tiles
+    advance();
+    if (t + 1 < tiles) request(t + 1);
+  }
 
   l += __shfl_xor(l, 32, 64);
   if (!at.ok) return;
@@ -736,7 +792,7 @@ Plan plan_of(int dt, const CacheView& c, int64_t rows, int heads, int max_new, i
   p.few = !p.many || rows < (int64_t)c.sequences * max_new;  // else no sequence is short where the longest is not, as a rule; wide_k and many_k take any
   p.few_upto = !p.many ? INT32_MAX : p.few ? FEW : 0;
   p.few_blocks = (int)(p.many ? 1 : std::max<int64_t>(1, up(most, FEW)));
-  p.many_blocks = (int)std::max<int64_t>(1, up(most, dt == DT_BF16 ? 256 : 128));
+  p.many_blocks = (int)std::max<int64_t>(1, up(most, 128));
   p.entries = (int64_t)c.sequences * p.few_blocks;
   p.tokens = p.many ? std::min(max_new, FEW) : max_new;
   int64_t span = std::max<int64_t>(1, std::min<int64_t>(max_length, (int64_t)c.max_pages << c.page_shift));
@@ -774,7 +830,7 @@ hipError_t launch(const Plan& pl, Args a, void* workspace, hipStream_t st) {
     if (e != hipSuccess) return e;
     attr_done = true;
   }
-  if (pl.many) many<<<(unsigned)many_grid, sizeof(T) == 2 ? 512 : 256, MANY_LDS, st>>>(a);
+  if (pl.many) many<<<(unsigned)many_grid, 256, MANY_LDS, st>>>(a);
   if (pl.few) few_k<T, HD><<<(unsigned)few_grid, 256, FEW_LDS, st>>>(a);
   if (pl.runs) join_k<T, HD><<<(unsigned)join_grid, 256, 0, st>>>(a, pl.tokens);
   return hipGetLastError();
