@@ -9,8 +9,8 @@
 //   few_k    32 rows a workgroup: all four wavefronts hold the same rows and take turns at the blocks of 32 keys, each through LDS tiles of its own
 //            without any barrier, and their results are joined at the end.  Bound by reading the cache.  Lengths are known on the device only, and
 //            differ: the keys of all sequences and heads, one after the other, are cut into equal runs, a workgroup each, wherever that falls.
-//   wide_k (bf16), many_k (fp32)   128 rows a workgroup, 32 a wavefront, which share tiles of 64 keys.  Bound by the matrix
-//            instructions.
+//   mixed_k  128 rows a workgroup, 32 a wavefront, which share tiles of 64 keys; bound by the matrix instructions.  Its first workgroups take the
+//            sequences of few rows.
 //   join_k   rows whose keys fell to several workgroups: the parts, weighted by their maxima.
 #include <math.h>
 
@@ -46,9 +46,10 @@ struct Args {
   const void* q;
   void* out;
   float* lse;           // [rows, heads] or null
-  int few_upto;         // sequences of at most so many rows are few_k's, the others wide_k's or many_k's
+  int few_upto;         // sequences of at most so many rows are few_k's, the others mixed_k's
   int few_blocks, many_blocks;  // blocks of rows of the longest sequence
-  int runs;             // few_k's workgroups; 0: one a block of rows and key head, and nothing to join
+  int runs;             // few_k's workgroups, or 0
+  int few_first;        // mixed_k: workgroups that few rows take
   int64_t* plan;        // [0]: steps of a run; [1 + e]: steps before entry e
   float2* part_ml;      // [run][2][FEW] (maximum, sum of exponentials) of a run's first and last rows where those are shared with other runs
   float* part;          // [run][2][FEW][HD] their sums
@@ -56,14 +57,15 @@ struct Args {
 
 // ---- tiles of a type and width ----
 // A row of a tile is HD elements without padding; its 16-byte piece c lies at piece position c ^ swizzle(row), which spreads what one LDS
-// instruction reads over the banks.  HD: 64 or 128; narrower heads are zeros behind their width.
-template <typename T, int HD>
+// instruction reads over the banks.  HD: 64 or 128; narrower heads are zeros behind their width, and the blocks of 32 columns behind it, from NB_ on, take no
+// part in the products.
+template <typename T, int HD, int NB_>
 struct Tile {
-  static constexpr int ROWB = HD * (int)sizeof(T), PPR = ROWB / 16, RPI = 64 / PPR, NB = HD / 32;
+  static constexpr int ROWB = HD * (int)sizeof(T), PPR = ROWB / 16, RPI = 64 / PPR, NB = NB_;
   static constexpr int IPG = GROUP / RPI;  // load instructions of 16 keys
   static constexpr int BLOCKB = KB * ROWB;
   static constexpr bool F32 = sizeof(T) == 4;
-  static constexpr int NQ = F32 ? HD / 8 : HD / 16;  // fragments of a row
+  static constexpr int NQ = F32 ? NB * 4 : NB * 2;  // fragments of a row
   typedef typename std::conditional<F32, f32x4, bf16x8>::type Frag;  // 16 bytes of a row
 
   __device__ static __forceinline__ int swizzle(int r) {
@@ -267,7 +269,7 @@ __device__ __forceinline__ void store_out(const Args& p, const RowAt& r, int c, 
 
 // ---- few rows ----
 constexpr int PAGED = 64 * GROUP;  // keys whose page numbers a wavefront holds, a lane each 16
-constexpr int STEP = 4 * KB;       // keys that a workgroup takes at a time
+constexpr int STEP = 4 * KB;       // keys that a workgroup of four wavefronts takes at a time
 
 // An entry: a block of 32 rows of a sequence, entry s * few_blocks + block; its key heads take `steps` steps each.
 struct Entry {
@@ -285,10 +287,10 @@ struct Entry {
   }
 };
 
-// Steps [step0, step1) of an entry's key head.  shared: -1 where these are all its steps, otherwise the place [..][FEW] its results go to.
-template <typename T, int HD>
+// Steps [step0, step1) of an entry's key head, by W wavefronts.  shared: -1 where these are all its steps, otherwise the place [..][FEW] its results go to.
+template <typename T, int HD, int NB_, int W>
 __device__ __forceinline__ void few_rows(const Args& p, const Entry& en, int s, int kv_head, int step0, int step1, int64_t shared, unsigned char* lds, float2 (*ml)[FEW]) {
-  typedef Tile<T, HD> L;
+  typedef Tile<T, HD, NB_> L;
   constexpr int NB = L::NB, IPB = 2 * L::IPG;  // loads of a block of keys
   const int tid = threadIdx.x, lane = tid & 63, wave = UNIFORM(tid >> 6), fr = lane & 31, fh = lane >> 5;
   const int from = UNIFORM(en.from + step0 * STEP), to = UNIFORM(min(en.to, en.from + step1 * STEP)), n_rows = UNIFORM(en.n_rows);
@@ -320,10 +322,10 @@ __device__ __forceinline__ void few_rows(const Args& p, const Entry& en, int s, 
 #pragma unroll
   for (int k = 0; k < L::NQ; ++k) asm volatile("" : "+v"(q[k]));
   const int pos_lo = UNIFORM(en.of.cached + en.t0), pos_hi = UNIFORM(en.of.cached + en.t1);
-  for (; key0 < to; key0 += STEP) {
-    const int next = key0 + STEP;
+  for (; key0 < to; key0 += W * KB) {
+    const int next = key0 + W * KB;
     const bool more = next < to;
-    if (next >= paged + PAGED) {  // PAGED is a multiple of STEP
+    if (next >= paged + PAGED) {  // PAGED is a multiple of W KB
       paged += PAGED;
       pages = pages_from(paged);
     }
@@ -359,15 +361,15 @@ __device__ __forceinline__ void few_rows(const Args& p, const Entry& en, int s, 
             f32x4{run.o[nb][4 * g], run.o[nb][4 * g + 1], run.o[nb][4 * g + 2], run.o[nb][4 * g + 3]};
   }
   __syncthreads();
-  for (int i = tid; i < n_rows * HD; i += 256) {
-    const int m = i / HD, c = i % HD;
+  for (int i = tid; i < n_rows * (NB * 32); i += 64 * W) {
+    const int m = i / (NB * 32), c = i % (NB * 32);
     float top = ml[0][m].x;
 #pragma unroll
-    for (int w = 1; w < 4; ++w) top = fmaxf(top, ml[w][m].x);
+    for (int w = 1; w < W; ++w) top = fmaxf(top, ml[w][m].x);
     const float ref = top == -INFINITY ? 0.f : top;
     float l = 0.f, o = 0.f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < W; ++w) {
       const float by = __builtin_amdgcn_exp2f(ml[w][m].x - ref);
       l = fmaf(by, ml[w][m].y, l);
       o = fmaf(by, sums[(w * FEW + m) * HD + c], o);
@@ -383,19 +385,26 @@ __device__ __forceinline__ void few_rows(const Args& p, const Entry& en, int s, 
   }
 }
 
-template <typename T, int HD>
-__global__ void __launch_bounds__(256) few_k(Args p) {
-  typedef Tile<T, HD> L;
+// One workgroup a block of rows and key head
+template <typename T, int HD, int NB, int W>
+__device__ __forceinline__ void few_whole(const Args& p, int i, unsigned char* lds, float2 (*ml)[FEW]) {
+  const int pair = i / p.few_blocks, block = p.few_blocks - 1 - i % p.few_blocks, s = pair / p.c.kv_heads;
+  const Entry en(p, s, block);
+  if (en.steps > 0) few_rows<T, HD, NB, W>(p, en, s, pair % p.c.kv_heads, 0, en.steps, -1, lds, ml);
+}
+template <typename T, int HD, int NB, int W>
+__global__ void __launch_bounds__(64 * W) few_whole_k(Args p) {
   extern __shared__ unsigned char lds[];  // [wave][K | V] blocks; at the end of a block of rows [wave][row][HD] sums
+  __shared__ float2 ml[W][FEW];
+  few_whole<T, HD, NB, W>(p, (int)blockIdx.x, lds, ml);
+}
+
+// Equal runs of steps
+template <typename T, int HD, int NB>
+__global__ void __launch_bounds__(256) few_k(Args p) {
+  extern __shared__ unsigned char lds[];
   __shared__ float2 ml[4][FEW];
   const int kv_heads = p.c.kv_heads;
-  if (p.runs == 0) {
-    const int pair = (int)(blockIdx.x / (unsigned)p.few_blocks), block = p.few_blocks - 1 - (int)(blockIdx.x % (unsigned)p.few_blocks);
-    const int s = pair / kv_heads;
-    const Entry en(p, s, block);
-    if (en.steps > 0) few_rows<T, HD>(p, en, s, pair % kv_heads, 0, en.steps, -1, lds, ml);
-    return;
-  }
   // steps of all entries, and where this run begins
   __shared__ int64_t sums[256];
   __shared__ int64_t found_before;
@@ -439,7 +448,7 @@ __global__ void __launch_bounds__(256) few_k(Args p) {
       const int in = UNIFORM((int)(at - first)), kv_head = UNIFORM(in / en.steps), step0 = in - kv_head * UNIFORM(en.steps);
       const int n = UNIFORM((int)min((int64_t)(en.steps - step0), at1 - at));
       const bool whole = n == en.steps;
-      few_rows<T, HD>(p, en, s, kv_head, step0, step0 + n, whole ? -1 : ((int64_t)blockIdx.x * 2 + (step0 == 0)) * FEW, lds, ml);
+      few_rows<T, HD, NB, 4>(p, en, s, kv_head, step0, step0 + n, whole ? -1 : ((int64_t)blockIdx.x * 2 + (step0 == 0)) * FEW, lds, ml);
       __syncthreads();  // the next block's keys go where the sums were
       at += n;
     }
@@ -448,13 +457,13 @@ __global__ void __launch_bounds__(256) few_k(Args p) {
 }
 
 // ---- many rows, fp32 ----
-template <typename T, int HD>
-__global__ void __launch_bounds__(256) many_k(Args p) {
-  typedef Tile<T, HD> L;
+template <int HD, int NB_>
+__device__ __forceinline__ void many_rows_f32(const Args& p, const int index, unsigned char* lds /* [buffer][K | V] tiles of 64 keys */) {
+  typedef float T;
+  typedef Tile<T, HD, NB_> L;
   constexpr int NB = L::NB, KT = 2 * KB, TILEB = KT * L::ROWB, QB = 128;
-  extern __shared__ unsigned char lds[];  // [buffer][K | V] tiles of 64 keys
   const int tid = threadIdx.x, lane = tid & 63, wave = UNIFORM(tid >> 6), fr = lane & 31, fh = lane >> 5;
-  const int block = p.many_blocks - 1 - (int)(blockIdx.x % (unsigned)p.many_blocks), pair = (int)(blockIdx.x / (unsigned)p.many_blocks);  // most keys first
+  const int block = p.many_blocks - 1 - index % p.many_blocks, pair = index / p.many_blocks;  // most keys first
   const int s = pair / p.c.kv_heads, kv_head = pair % p.c.kv_heads;
   const CacheSeq of = cache_seq(p.c, s, p.rows, p.max_new);
   const int n_rows = of.fresh * p.group;
@@ -554,15 +563,14 @@ __device__ __forceinline__ int longest(const Args& p, int rank, int* lengths) {
   return s;
 }
 
-template <int HD>
-__global__ void __launch_bounds__(256, 2) wide_k(Args p) {
-  typedef Tile<bf16, HD> L;
+template <int HD, int NB_>
+__device__ __forceinline__ void many_rows_bf16(const Args& p, const int index, unsigned char* lds /* [2] tiles of K | [3] of V */) {
+  typedef Tile<bf16, HD, NB_> L;
   constexpr int NB = L::NB, NQ = L::NQ, KT = 2 * KB, TILEB = KT * L::ROWB, QB = 128;
-  extern __shared__ unsigned char lds[];  // [2] tiles of K | [3] of V
   const int tid = threadIdx.x, lane = tid & 63, wave = UNIFORM(tid >> 6), fr = lane & 31, fh = lane >> 5;
   // Workgroups start in the order of their index: those with the most keys first.  Neighbours take different heads, so that the workgroups of a head, which read
   // the same keys, are on one of the eight dies where the heads are a multiple of them.
-  int i = (int)blockIdx.x;
+  int i = index;
   const int kv_head = i % p.c.kv_heads;
   i /= p.c.kv_heads;
   const int block = p.many_blocks - 1 - i % p.many_blocks, s = longest(p, i / p.many_blocks, reinterpret_cast<int*>(lds));
@@ -684,10 +692,12 @@ __global__ void __launch_bounds__(256, 2) wide_k(Args p) {
     asm volatile("" : "+v"(pr[0]), "+v"(pr[1]), "+v"(l));  // here and not behind the branches below
     if (b == 0 && t + 1 < tiles) request(t + 1);
     mask(now, t, b);
+    __builtin_amdgcn_s_setprio(1);  // before the exponentials of the other wavefront of the SIMD
     read_values(v1, V, 1);
     times_values(v0, 0);
     if (b == 0) read_keys(f, lds + (t & 1) * TILEB + L::BLOCKB);
     times_values(v1, 1);
+    __builtin_amdgcn_s_setprio(0);
     const float top = row_max(now);
     if (__builtin_amdgcn_ballot_w64(top > m + 8.0f) != 0) raise(top);
   };
@@ -740,6 +750,15 @@ __global__ void __launch_bounds__(256, 2) wide_k(Args p) {
   if (fh == 0 && p.lse) p.lse[at.row * p.heads + at.head] = m + __builtin_amdgcn_logf(l);
 }
 
+// Sequences of many rows, and those of few, if there may be any: the first few_first workgroups, one a key head.
+template <typename T, int HD, int NB>
+__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) mixed_k(Args p) {
+  extern __shared__ unsigned char lds[];
+  if ((int)blockIdx.x < p.few_first) few_whole<T, HD, NB, 4>(p, (int)blockIdx.x, lds, reinterpret_cast<float2(*)[FEW]>(lds + 4 * 2 * KB * HD * sizeof(T)));
+  else if constexpr (sizeof(T) == 2) many_rows_bf16<HD, NB>(p, (int)blockIdx.x - p.few_first, lds);
+  else many_rows_f32<HD, NB>(p, (int)blockIdx.x - p.few_first, lds);
+}
+
 // ---- rows whose keys fell to several runs ----
 // One wavefront a row and head of the first `tokens` tokens of a sequence.
 template <typename T, int HD>
@@ -778,8 +797,8 @@ __global__ void __launch_bounds__(256) join_k(Args p, int tokens) {
 
 // ---- host ----
 struct Plan {
-  bool few, many;
-  int few_blocks, few_upto, many_blocks, runs, tokens;
+  bool many;
+  int few_blocks, few_upto, few_first, many_blocks, runs, waves;
   int64_t entries;
 };
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -787,53 +806,78 @@ Plan plan_of(int dt, const CacheView& c, int64_t rows, int heads, int max_new, i
   Plan p{};
   const int group = heads / c.kv_heads;
   const int64_t most = (int64_t)max_new * group, pairs = (int64_t)c.sequences * c.kv_heads;  // rows of the longest sequence
-  // the kernels for many rows share a tile of keys among more of them; few_k gives more workgroups, and takes all where they do not fill the chip
+  // the kernel for many rows shares a tile of keys among more of them; few_k gives more workgroups, and takes all where they do not fill the chip
   p.many = most > FEW && pairs * up(most, FEW) > 1024;
-  p.few = !p.many || rows < (int64_t)c.sequences * max_new;  // else no sequence is short where the longest is not, as a rule; wide_k and many_k take any
-  p.few_upto = !p.many ? INT32_MAX : p.few ? FEW : 0;
+  const bool few = !p.many || rows < (int64_t)c.sequences * max_new;  // else no sequence is short where the longest is not, as a rule; the others take any
+  p.few_upto = !p.many ? INT32_MAX : few ? FEW : 0;
+  p.few_first = p.many && few ? (int)pairs : 0;
   p.few_blocks = (int)(p.many ? 1 : std::max<int64_t>(1, up(most, FEW)));
   p.many_blocks = (int)std::max<int64_t>(1, up(most, 128));
   p.entries = (int64_t)c.sequences * p.few_blocks;
-  p.tokens = p.many ? std::min(max_new, FEW) : max_new;
+  if (p.many) return p;
   int64_t span = std::max<int64_t>(1, std::min<int64_t>(max_length, (int64_t)c.max_pages << c.page_shift));
   if (window > 0) span = std::min<int64_t>(span, (int64_t)window + FEW + KB);
   // as many runs as workgroups are on the chip at a time: LDS holds four blocks of rows of 128 bytes, two of 256, one of 512
   const int row_bytes = (c.head_dim <= 64 ? 64 : 128) * (dt == DT_BF16 ? 2 : 4), resident = 256 * 512 / row_bytes;
-  if (p.few && span > 4 * STEP) p.runs = (int)std::min<int64_t>(resident, pairs * p.few_blocks * up(span, STEP));
+  const int64_t items = pairs * p.few_blocks;
+  p.waves = items <= 256 && row_bytes <= 256 && span > STEP ? 8 : 4;
+  if (span > p.waves * STEP) {
+    p.waves = 4;
+    p.runs = (int)std::min<int64_t>(resident, items * up(span, STEP));
+  }
   return p;
 }
 size_t plan_bytes(const Plan& p) { return p.runs ? (size_t)((1 + p.entries) * 8 + 15) / 16 * 16 : 0; }
 
-template <typename T, int HD>
-auto many_kernel() {
-  if constexpr (sizeof(T) == 2) return wide_k<HD>;
-  else return many_k<T, HD>;
+// LDS beyond 64 KB has to be asked for, once an instantiation
+template <auto KERNEL, int LDS>
+hipError_t allow_lds() {
+  static bool done = false;
+  if (LDS <= 65536 || done) return hipSuccess;
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(KERNEL), hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
+  done = e == hipSuccess;
+  return e;
 }
 
-template <typename T, int HD>
-hipError_t launch(const Plan& pl, Args a, void* workspace, hipStream_t st) {
-  typedef Tile<T, HD> L;
-  a.few_upto = pl.few_upto; a.few_blocks = pl.few_blocks; a.many_blocks = pl.many_blocks; a.runs = pl.runs;
+template <typename T, int HD, int NB>
+hipError_t launch(const Plan& pl, Args a, int max_new, void* workspace, hipStream_t st) {
+  a.few_upto = pl.few_upto; a.few_blocks = pl.few_blocks; a.many_blocks = pl.many_blocks; a.runs = pl.runs; a.few_first = pl.few_first;
   a.plan = (int64_t*)workspace;
   a.part_ml = (float2*)((unsigned char*)workspace + plan_bytes(pl));
   a.part = (float*)(a.part_ml + (int64_t)pl.runs * 2 * FEW);
-  const int64_t pairs = (int64_t)a.c.sequences * a.c.kv_heads;
-  const int64_t few_grid = pl.runs ? pl.runs : pairs * pl.few_blocks, many_grid = pairs * pl.many_blocks, join_grid = up((int64_t)a.c.sequences * pl.tokens * a.heads, 4);
-  if (few_grid > 0x7FFFFFFF || many_grid > 0x7FFFFFFF || join_grid > 0x7FFFFFFF || pl.entries > 0x7FFFFFFF) return hipErrorInvalidValue;
-  constexpr int FEW_LDS = 4 * 2 * L::BLOCKB, MANY_LDS = (sizeof(T) == 2 ? 5 : 4) * 2 * L::BLOCKB;
+  const int64_t pairs = (int64_t)a.c.sequences * a.c.kv_heads, rows = (int64_t)a.c.sequences * max_new * a.heads;
+  const int64_t grid = pl.many ? pl.few_first + pairs * pl.many_blocks : pl.runs ? pl.runs : pairs * pl.few_blocks;
+  if (grid > 0x7FFFFFFF || up(rows, 4) > 0x7FFFFFFF || pl.entries > 0x7FFFFFFF) return hipErrorInvalidValue;
+  constexpr int BLOCKB = KB * HD * (int)sizeof(T), FEW_LDS = 4 * 2 * BLOCKB, MANY_LDS = (sizeof(T) == 2 ? 5 : 4) * 2 * BLOCKB;
+  constexpr int MIXED_LDS = std::max(MANY_LDS, FEW_LDS + 4 * FEW * 8);
   static_assert(4 * FEW * HD * 4 <= FEW_LDS, "the wavefronts' sums fit where their tiles were");
-  const auto many = many_kernel<T, HD>();
-  static bool attr_done = false;  // one flag per instantiation
-  if (!attr_done) {
-    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(many), hipFuncAttributeMaxDynamicSharedMemorySize, MANY_LDS);
-    if (e == hipSuccess) e = hipFuncSetAttribute(reinterpret_cast<const void*>(few_k<T, HD>), hipFuncAttributeMaxDynamicSharedMemorySize, FEW_LDS);
-    if (e != hipSuccess) return e;
-    attr_done = true;
+  const dim3 g((unsigned)grid);
+  if (pl.many) {
+    if (hipError_t e = allow_lds<mixed_k<T, HD, NB>, MIXED_LDS>()) return e;
+    mixed_k<T, HD, NB><<<g, 256, MIXED_LDS, st>>>(a);
+  } else if (pl.runs) {
+    if (hipError_t e = allow_lds<few_k<T, HD, NB>, FEW_LDS>()) return e;
+    few_k<T, HD, NB><<<g, 256, FEW_LDS, st>>>(a);
+    join_k<T, HD><<<(unsigned)up(rows, 4), 256, 0, st>>>(a, max_new);
+  } else if (pl.waves == 8) {
+    if constexpr (2 * FEW_LDS <= 131072) {
+      if (hipError_t e = allow_lds<few_whole_k<T, HD, NB, 8>, 2 * FEW_LDS>()) return e;
+      few_whole_k<T, HD, NB, 8><<<g, 512, 2 * FEW_LDS, st>>>(a);
+    }
+  } else {
+    if (hipError_t e = allow_lds<few_whole_k<T, HD, NB, 4>, FEW_LDS>()) return e;
+    few_whole_k<T, HD, NB, 4><<<g, 256, FEW_LDS, st>>>(a);
   }
-  if (pl.many) many<<<(unsigned)many_grid, 256, MANY_LDS, st>>>(a);
-  if (pl.few) few_k<T, HD><<<(unsigned)few_grid, 256, FEW_LDS, st>>>(a);
-  if (pl.runs) join_k<T, HD><<<(unsigned)join_grid, 256, 0, st>>>(a, pl.tokens);
   return hipGetLastError();
+}
+template <typename T>
+hipError_t launch_width(const Plan& pl, const Args& a, int max_new, void* workspace, hipStream_t st) {
+  switch ((a.c.head_dim + 31) / 32) {
+    case 1: return launch<T, 64, 1>(pl, a, max_new, workspace, st);
+    case 2: return launch<T, 64, 2>(pl, a, max_new, workspace, st);
+    case 3: return launch<T, 128, 3>(pl, a, max_new, workspace, st);
+    default: return launch<T, 128, 4>(pl, a, max_new, workspace, st);
+  }
 }
 
 }  // namespace
@@ -853,8 +897,7 @@ hipError_t attention_paged(int dt, const CacheView& c, int heads, int64_t rows, 
   a.rows = rows; a.ldq = ldq; a.ldo = ldo; a.max_new = max_new; a.window = window;
   a.scale_log2e = scale * 1.4426950408889634f;
   a.q = q; a.out = out; a.lse = lse;
-  if (dt == DT_BF16) return c.head_dim <= 64 ? launch<bf16, 64>(pl, a, workspace, st) : launch<bf16, 128>(pl, a, workspace, st);
-  return c.head_dim <= 64 ? launch<float, 64>(pl, a, workspace, st) : launch<float, 128>(pl, a, workspace, st);
+  return dt == DT_BF16 ? launch_width<bf16>(pl, a, max_new, workspace, st) : launch_width<float>(pl, a, max_new, workspace, st);
 }
 
 }  // namespace hift
