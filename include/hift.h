@@ -655,6 +655,32 @@ hift_status hift_kernel_attention_paged(const hift_cache* cache, int64_t rows, c
                                         int32_t window, float scale, const void* q, int64_t ldq, void* out, int64_t ldo, float* lse, void* workspace,
                                         size_t workspace_bytes, void* stream);
 
+/* The model writes on: new tokens of several sequences go through it with its present weights, over a paged cache of all its layers -- a prompt, a chunk of
+ * one, or a token a sequence -- and leave their keys and values there (decoders only; bf16 models round q and k before and after their rotation).
+ *   cache         layer 0's: the model's type, heads and head width (which has to suit hift_cache); layer l's k and v lie l * layer_stride elements further
+ *   tokens        device int32 [rows]; starts, max_new, max_length as for hift_kernel_attention_paged; rows at most max_batch * max_seq of the model's creation,
+ *                 max_length at most its max_seq
+ *   pick          device int32 [n_pick]: the rows whose logits are wanted (kept within [0, rows)), or NULL for all (n_pick = rows)
+ *   logits        device [n_pick, vocab] of the model's type, rows ld apart
+ * Queued on the compute stream; the call does not wait.  workspace: device, 16-byte aligned, hift_extend_bytes.  What the pass computes replaces the
+ * activations of the last one: scores that hift_score has left are dropped (HIFT_ESTATE from hift_step_scored), nothing else changes.  Models with adapters
+ * answer with them.  What hift_step trains afterwards leaves the cache as it is: it holds keys and values of the weights before. */
+typedef struct {
+  const hift_cache* cache;
+  int64_t layer_stride;
+  const int32_t* tokens;
+  int64_t rows;
+  const int32_t* starts;
+  int32_t max_new;
+  int64_t max_length;
+  const int32_t* pick;
+  int64_t n_pick;
+  void* logits;
+  int64_t ld;
+} hift_extension;
+hift_status hift_extend_bytes(const hift_model* mdl, const hift_extension* extension, size_t* bytes);
+hift_status hift_extend(hift_model* mdl, const hift_extension* extension, void* workspace, size_t workspace_bytes);
+
 /* Logits as a sampler wants them.  With n = how often row r has seen token j, x = logits[r, j]:
  *   out[r, j] = (n > 0 ? (x > 0 ? x / repetition : x repetition) - presence : x) - frequency n + bias[j];   -inf where `allowed` has no bit for j
  * tokens: device int32 [n_tokens]; row r has seen tokens[begin[r]] .. tokens[end[r] - 1] (device int64 [rows], kept within [0, n_tokens]; ranges may overlap, as

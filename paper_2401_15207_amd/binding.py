@@ -84,6 +84,11 @@ class Adjust(C.Structure):
                 ("frequency", C.c_float), ("bias", C.c_void_p), ("ld_bias", C.c_int64), ("allowed", C.c_void_p), ("ld_allowed", C.c_int64)]
 
 
+class Extension(C.Structure):
+    _fields_ = [("cache", C.c_void_p), ("layer_stride", C.c_int64), ("tokens", C.c_void_p), ("rows", C.c_int64), ("starts", C.c_void_p), ("max_new", C.c_int32),
+                ("max_length", C.c_int64), ("pick", C.c_void_p), ("n_pick", C.c_int64), ("logits", C.c_void_p), ("ld", C.c_int64)]
+
+
 lib.hift_last_error.restype = C.c_char_p
 _vp, _i32, _i64, _u64, _sz = C.c_void_p, C.c_int32, C.c_int64, C.c_uint64, C.c_size_t
 _P = C.POINTER
@@ -156,6 +161,8 @@ _SIGS = {
     "hift_kernel_cache_append": [_P(Cache), _i64, _vp, _i32, _i32, _i32, _i32, _vp, _i64, _vp, _i64, _vp, _i64, _vp],
     "hift_kernel_attention_paged_bytes": [_P(Cache), _i64, _i32, _i64, _i32, _i32, _P(_sz)],
     "hift_kernel_attention_paged": [_P(Cache), _i64, _vp, _i32, _i64, _i32, _i32, C.c_float, _vp, _i64, _vp, _i64, _vp, _vp, _sz, _vp],
+    "hift_extend_bytes": [_vp, _P(Extension), _P(_sz)],
+    "hift_extend": [_vp, _P(Extension), _vp, _sz],
     "hift_kernel_adjust_logits": [_i32, _i64, _i32, _i64, _vp, _P(Adjust), _i64, _vp, _vp],
     "hift_kernel_adjust_logits_bwd": [_i32, _i64, _i32, _i64, _vp, _P(Adjust), _i64, _vp, _i64, _vp, _vp],
 }
@@ -526,11 +533,15 @@ def kernel_rotary(x, heads, head_dim, y, cos_sin, positions=None, seq=0, layout=
 
 
 class PagedCache:
-    """One layer's paged cache (hift_cache): k, v [pages there are, kv_heads, page, head_dim] (any distance between pages), pages [sequences, most pages of a
-    sequence] and lengths [sequences], both int32.  Holds the tensors; what lengths and pages say may change between calls."""
+    """A paged cache (hift_cache): k, v [pages there are, kv_heads, page, head_dim] (any distance between pages), pages [sequences, most pages of a sequence] and
+    lengths [sequences], both int32.  For models, k and v have a first dimension more, the layers, and the kernels take layer 0.  Holds the tensors; what lengths
+    and pages say may change between calls."""
 
     def __init__(self, k, v, pages, lengths):
-        at = k.get_device()
+        at, self.layers, self.layer_stride = k.get_device(), 1, 0
+        if k.dim() == 5 and v.shape == k.shape and v.stride() == k.stride() and len(k):
+            self.layers, self.layer_stride, self.all = k.shape[0], k.stride(0), (k, v)
+            k, v = k[0], v[0]
         if k.dim() != 4 or v.shape != k.shape or v.dtype is not k.dtype or v.stride() != k.stride() or at < 0 or v.get_device() != at:
             raise ValueError(f"k, v: device tensors [n_pages, kv_heads, page, head_dim] of one type expected, not {tuple(k.shape)} {k.dtype} and {tuple(v.shape)} {v.dtype}")
         n, kv, page, hd = k.shape
@@ -816,6 +827,30 @@ class HiftModel:
                 t.record_stream(self.compute_stream)
         _check(lib.hift_step_scored(self.h, C.byref(b), group_id, _ptr(d_logp), _ptr(d_entropy)))
         cur.wait_stream(self.compute_stream)   # the caller may write the derivatives and the batch again
+
+    def extend(self, tokens, starts, cache, max_new: int, max_length: int, pick=None):
+        """New tokens (int32 [rows]) of the cache's sequences (rows starts[s] .. starts[s + 1] - 1 are sequence s's, int32) through the model: their keys and values go
+        into the cache, their logits come back, [rows, vocab] or, of the rows in pick (int32), [len(pick), vocab], ready on torch's current stream.  max_new: most new
+        tokens of a sequence; max_length: most tokens of one with them.  The caller adds the new tokens to cache.lengths."""
+        torch, at = self.torch, self.device.index or 0
+        rows = tokens.numel()
+        if cache.device != at or cache.layers != self.cfg["n_layers"]:
+            raise ValueError(f"cache: {self.cfg['n_layers']} layers on cuda:{at} expected, not {cache.layers} on cuda:{cache.device}")
+        n = rows if pick is None else pick.numel()
+        logits = torch.empty(n, self.cfg["vocab"], device=self.device, dtype=torch.bfloat16 if self.cfg["dtype"] else torch.float32)
+        e = Extension(C.addressof(cache.c), cache.layer_stride, _row_values("tokens", tokens, rows, at, torch.int32), rows, _starts_of(cache, starts), max_new, max_length,
+                      _row_values("pick", pick, n, at, torch.int32), n, logits.data_ptr(), self.cfg["vocab"])
+        b = _sz()
+        _check(lib.hift_extend_bytes(self.h, C.byref(e), C.byref(b)))
+        ws = torch.empty(max(b.value, 16), dtype=torch.uint8, device=self.device)
+        cur = torch.cuda.current_stream(self.device)
+        self.compute_stream.wait_stream(cur)
+        for t in (tokens, starts, pick, logits, ws, cache.k, cache.v, cache.pages, cache.lengths):
+            if t is not None:
+                t.record_stream(self.compute_stream)
+        _check(lib.hift_extend(self.h, C.byref(e), _ptr(ws), b.value))
+        cur.wait_stream(self.compute_stream)
+        return logits
 
     def lora_param_count(self) -> int:
         n = _i64()

@@ -53,12 +53,13 @@ inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 template <typename T, int V>
 __global__ void __launch_bounds__(BLK) embed_fwd_k(const int32_t* __restrict__ tokens, int64_t T_, int S,
                                                     int d, int vocab, const T* __restrict__ tok_emb,
-                                                    const T* __restrict__ pos_emb, T* __restrict__ x) {
+                                                    const T* __restrict__ pos_emb, T* __restrict__ x,
+                                                    const int32_t* __restrict__ positions) {
   const int64_t t = blockIdx.x;
   int id = tokens[t];
   id = id < 0 ? 0 : (id >= vocab ? vocab - 1 : id);
   const T* er = tok_emb + (int64_t)id * d;
-  const T* pr = pos_emb ? pos_emb + (int64_t)(t % S) * d : nullptr;
+  const T* pr = pos_emb ? pos_emb + (positions ? (int64_t)min(max(positions[t], 0), S - 1) : t % S) * d : nullptr;
   T* xr = x + t * d;
   for (int j = threadIdx.x * V; j < d; j += BLK * V) {
     float a[V];
@@ -70,6 +71,16 @@ __global__ void __launch_bounds__(BLK) embed_fwd_k(const int32_t* __restrict__ t
       for (int e = 0; e < V; ++e) a[e] += b[e];
     }
     stv<T, V>(xr + j, a);
+  }
+}
+
+template <typename T, int V>
+__global__ void __launch_bounds__(BLK) gather_rows_k(const int32_t* __restrict__ pick, int64_t rows, int d, const T* __restrict__ x, T* __restrict__ y) {
+  const int64_t from = min(max((int64_t)pick[blockIdx.x], (int64_t)0), rows - 1), to = blockIdx.x;
+  for (int j = threadIdx.x * V; j < d; j += BLK * V) {
+    float a[V];
+    ldv<T, V>(x + from * d + j, a);
+    stv<T, V>(y + to * d + j, a);
   }
 }
 
@@ -1178,11 +1189,11 @@ __global__ void __launch_bounds__(BLK) af_vec_k(int64_t n, float b2, float lr, f
 static inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 hipError_t embed_fwd(int dt, const int32_t* tokens, int64_t T_, int S, int d, int V_, const void* tok_emb,
-                     const void* pos_emb, void* x, hipStream_t st) {
+                     const void* pos_emb, void* x, hipStream_t st, const int32_t* positions) {
   if (T_ == 0) return hipSuccess;
 #define OK(v) (d % (v) == 0 && aligned16(tok_emb) && aligned16(pos_emb) && aligned16(x))
   DISPATCH_TV(dt, OK, (embed_fwd_k<T, V><<<dim3((unsigned)T_), BLK, 0, st>>>(
-                          tokens, T_, S, d, V_, (const T*)tok_emb, (const T*)pos_emb, (T*)x)));
+                          tokens, T_, S, d, V_, (const T*)tok_emb, (const T*)pos_emb, (T*)x, positions)));
 #undef OK
   LAUNCH_CHECK();
 }
@@ -1223,6 +1234,14 @@ hipError_t scatter_first(int dt, int B, int S, int d, const void* dy, void* dx, 
   hipError_t e = fill_zero(dx, (size_t)B * S * d * dt_size(dt), st);
   if (e != hipSuccess) return e;
   return first_rows(dt, B, S, d, dy, dx, true, st);
+}
+
+hipError_t gather_rows(int dt, int64_t n, const int32_t* pick, int64_t rows, int d, const void* x, void* y, hipStream_t st) {
+  if (n == 0) return hipSuccess;
+#define OK(v) (d % (v) == 0 && aligned16(x) && aligned16(y))
+  DISPATCH_TV(dt, OK, (gather_rows_k<T, V><<<dim3((unsigned)n), BLK, 0, st>>>(pick, rows, d, (const T*)x, (T*)y)));
+#undef OK
+  LAUNCH_CHECK();
 }
 
 hipError_t norm_fwd(int dt, bool rms, int64_t rows, int d, float eps, const void* x, const void* g, const void* b,

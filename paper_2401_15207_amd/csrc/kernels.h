@@ -105,8 +105,9 @@ hipError_t gemm_packed(const Gemm& g, const void* Bp, hipStream_t st);
 size_t packed_ws_needed(const Gemm& g);
 
 // ---- row-wise and elementwise kernels ------------------------------------------------------
+// positions (or null: row t has t % S): of the rows, kept within [0, S)
 hipError_t embed_fwd(int dt, const int32_t* tokens, int64_t T, int S, int d, int V,
-                     const void* tok_emb, const void* pos_emb, void* x, hipStream_t st);
+                     const void* tok_emb, const void* pos_emb, void* x, hipStream_t st, const int32_t* positions = nullptr);
 // bf16 rows [rows, d] (d a multiple of 8): out[row][0] = sum of squares, out[row][1 .. n) = 0 (see Gemm::rowsq)
 hipError_t row_sumsq(int64_t rows, int d, const void* x, int n, float* out, hipStream_t st);
 hipError_t norm_fwd(int dt, bool rms, int64_t rows, int d, float eps, const void* x, const void* g,
@@ -272,6 +273,10 @@ struct CacheView {
 // rows q | k | v of a fused projection: q rotated to `q` (null: not wanted), k rotated and v to their pages; rot 0: no rotation
 hipError_t cache_append(int dt, const CacheView& c, int heads, bool pairs, int rot, const float* cos_sin, int table_rows, int64_t rows, int max_new,
                         const void* qkv, int64_t ld, void* q, int64_t ldq, hipStream_t st);
+// position of every new row of a cache's sequences; 0 for rows of none
+hipError_t cache_positions(const CacheView& c, int64_t rows, int max_new, int32_t* positions, hipStream_t st);
+// rows pick[0 .. n) (kept within [0, rows)) of x [rows, d] -> y [n, d]
+hipError_t gather_rows(int dt, int64_t n, const int32_t* pick, int64_t rows, int d, const void* x, void* y, hipStream_t st);
 // attention of the new rows over the cache (attention_paged.hip)
 size_t attention_paged_bytes(int dt, const CacheView& c, int64_t rows, int heads, int max_new, int64_t max_length, int window);
 hipError_t attention_paged(int dt, const CacheView& c, int heads, int64_t rows, int max_new, int64_t max_length, int window, float scale, const void* q, int64_t ldq,

@@ -716,6 +716,7 @@ struct LinEpi {
   bool keep_pre = true;
   bool fused = false;
   float* norm_stats = nullptr;  // weights with a folded normalisation: where (0, 1 / rms) per row goes, or null
+  bool rotate = true;           // false: the rotation is left out (its block order is undone all the same)
   bool gelu = false;            // plain block order: bias and GELU in the epilogue (act [rows, out]; keep_pre as above)
 };
 
@@ -757,7 +758,7 @@ hift_status linear(hift_model* M, const void* x, int64_t rows, const Tensor& w, 
         if (!epi->keep_pre) g.C = nullptr;
       } else {
         g.epi = EPI_ROPE;
-        g.cos_sin = M->cos_sin; g.S = epi->S; g.rot_cols = 2 * (int64_t)M->cfg.d_model;
+        g.cos_sin = M->cos_sin; g.S = epi->S; g.rot_cols = epi->rotate ? 2 * (int64_t)M->cfg.d_model : 0;
       }
       epi->fused = true;
       if (w.pk_gain >= 0) {
@@ -1136,9 +1137,34 @@ hift_status score_rows(hift_model* M, int64_t rows, int V, const int32_t* target
   return HIFT_OK;
 }
 
+// New tokens over a paged cache instead of a batch: the cache's first layer, and what hift_extension says
+struct Extend {
+  CacheView cache;
+  int64_t layer_bytes;
+  const hift_extension* of;
+  int32_t* positions;  // work space: of the rows
+  void* attention;     // and the attention's
+};
+CacheView layer_cache(const Extend& ex, int l) {
+  CacheView c = ex.cache;
+  c.k = (unsigned char*)c.k + l * ex.layer_bytes;
+  c.v = (unsigned char*)c.v + l * ex.layer_bytes;
+  return c;
+}
+hift_status attention_extend(hift_model* M, LayerAct& a, int l, const Extend& ex) {
+  const hift_extension& e = *ex.of;
+  const int H = M->cfg.n_heads, d = M->cfg.d_model, hd = d / H, max_new = (int)std::min<int64_t>(e.max_new, e.rows);
+  const CacheView c = layer_cache(ex, l);
+  const int rot = M->cfg.arch == HIFT_ARCH_RMS_ROPE_DECODER ? hd : 0;
+  RW(RW_ROPE, 6.0 * e.rows * d * M->es, cache_append(M->dt, c, H, false, rot, M->cos_sin, M->cfg.max_seq, e.rows, max_new, a.qkv, 3 * (int64_t)d, a.qkv, 3 * (int64_t)d, M->cs));
+  Scope sc(M, CAT_ATTN, 4.0 * e.rows * (double)e.max_length * d);
+  K_TRY(attention_paged(M->dt, c, H, e.rows, max_new, e.max_length, 0, 1.0f / sqrtf((float)hd), a.qkv, 3 * (int64_t)d, a.ctx, d, nullptr, ex.attention, M->cs));
+  return HIFT_OK;
+}
+
 // keep_from: lowest unit the backward pass will reach; layers below it keep no pre-activations.  scores: instead of the loss and its gradient,
-// the log probabilities of the labels, entropies and alternatives; the logits stay.
-hift_status forward(hift_model* M, const hift_batch* bt, int keep_from, const hift_scores* scores = nullptr) {
+// the log probabilities of the labels, entropies and alternatives; the logits stay.  ex: new tokens over a cache (bt: their tokens, one sequence of all rows).
+hift_status forward(hift_model* M, const hift_batch* bt, int keep_from, const hift_scores* scores = nullptr, const Extend* ex = nullptr) {
   M->scored_group = -1;
   const hift_config& c = M->cfg;
   const int B = bt->batch, S = bt->seq;
@@ -1151,7 +1177,7 @@ hift_status forward(hift_model* M, const hift_batch* bt, int keep_from, const hi
   {
     const void* pos = rms ? nullptr : M->W("pos_emb");
     void* dst = enc ? M->e0 : M->xs[0];
-    RW(RW_EMBED_FWD, (double)T * d * es * (pos ? 3 : 2), embed_fwd(dt, bt->tokens, T, S, d, c.vocab, M->W("tok_emb"), pos, dst, st));
+    RW(RW_EMBED_FWD, (double)T * d * es * (pos ? 3 : 2), embed_fwd(dt, bt->tokens, T, ex ? c.max_seq : S, d, c.vocab, M->W("tok_emb"), pos, dst, st, ex ? ex->positions : nullptr));
     if (enc) RW(RW_NORM_FWD, 2.0 * T * d * es, norm_fwd(dt, false, T, d, c.norm_eps, M->e0, M->W("lne_g"), M->W("lne_b"), M->xs[0], M->st_e, st));
   }
   bool have_sq = false;  // M->rowsq holds the sums of squares of the rows the next normalisation takes
@@ -1171,15 +1197,17 @@ hift_status forward(hift_model* M, const hift_batch* bt, int keep_from, const hi
     LinEpi rot;
     rot.S = S;
     rot.norm_stats = a.st1;
+    rot.rotate = !ex;
     ST_TRY(linear(M, h1, T, *n.wqkv, n.bqkv, nullptr, a.qkv, &rot));
     if (M->lora_r > 0) {
       if (rot.fused) return fail(HIFT_ESTATE, "adapters need the projections before their rotation");
       ST_TRY(lora_fwd(M, l, h1, T, a.qkv));
     }
-    if (rms && !rot.fused) {
+    if (ex) ST_TRY(attention_extend(M, a, l, *ex));
+    else if (rms && !rot.fused) {
       RW(RW_ROPE, 4.0 * T * d * es, rope(dt, a.qkv, T, S, H, hd, M->cos_sin, +1, st));
     }
-    ST_TRY(attention_fwd(M, a, B, S, l + 1 >= keep_from));
+    if (!ex) ST_TRY(attention_fwd(M, a, B, S, l + 1 >= keep_from));
     if (enc) {
       ST_TRY(linear(M, a.ctx, T, *n.wo, n.bo, x, a.na));  // s1 = x + attn
       RW(RW_NORM_FWD, 2.0 * T * d * es, norm_fwd(dt, false, T, d, c.norm_eps, a.na, M->W(*n.n1g), M->W(*n.n1b), a.xmid, a.st1, st));
@@ -1215,6 +1243,17 @@ hift_status forward(hift_model* M, const hift_batch* bt, int keep_from, const hi
     }
   }
   void* xl = M->xs[c.n_layers];
+  if (ex) {
+    const hift_extension& e = *ex->of;
+    if (e.pick) {
+      RW(RW_FIRST_ROWS, 2.0 * e.n_pick * d * es, gather_rows(dt, e.n_pick, e.pick, T, d, xl, M->xs[0], st));
+      xl = M->xs[0];
+    }
+    RW(RW_NORM_FWD, 2.0 * e.n_pick * d * es, norm_fwd(dt, rms, e.n_pick, d, c.norm_eps, xl, M->W(rms ? "gf" : "lnf_g"), rms ? nullptr : M->W("lnf_b"), M->xf, M->st_f, st));
+    ST_TRY(linear(M, M->xf, e.n_pick, M->T_(c.tie_embeddings ? "tok_emb" : "whead"), nullptr, nullptr, M->logits, nullptr, nullptr, M->logits_ld));
+    HIP_TRY(hipMemcpy2DAsync(e.logits, (size_t)e.ld * M->es, M->logits, (size_t)M->logits_ld * M->es, (size_t)c.vocab * M->es, (size_t)e.n_pick, hipMemcpyDeviceToDevice, st));
+    return HIFT_OK;
+  }
   if (enc) {
     {
       RW(RW_FIRST_ROWS, 2.0 * B * d * es, gather_first(dt, B, S, d, xl, M->xcls, st));
@@ -2997,6 +3036,52 @@ hift_status hift_kernel_adjust_logits_bwd(int32_t dtype, int64_t rows, int32_t V
   if (d_logits == d_out && ldd != ldd_out) return fail(HIFT_EINVAL, "in place the rows lie where they were (ldd = ldd_out)");
   HIP_TRY(adjust_logits(dtype == HIFT_BF16 ? DT_BF16 : DT_F32, true, rows, V, ld, logits, a, ldd_out, d_out, ldd, d_logits, (hipStream_t)stream));
   return HIFT_OK;
+}
+
+namespace {
+// The checks of an extension, its view of the cache and the parts of its work space
+hift_status check_extension(const hift_model* M, const hift_extension* e, Extend* out, size_t* bytes) {
+  if (!M || !e) return fail(HIFT_EINVAL, "null argument");
+  const hift_config& c = M->cfg;
+  if (c.arch == HIFT_ARCH_POSTLN_ENCODER) return fail(HIFT_EINVAL, "only decoders write answers");
+  CacheView v{};
+  ST_TRY(cache_view(e->cache, e->rows, e->starts, e->max_new, c.n_heads, &v));
+  if (e->cache->dtype != c.dtype || v.kv_heads != c.n_heads || v.head_dim != c.d_model / c.n_heads) return fail(HIFT_EINVAL, "the cache's type and heads are not the model's");
+  if (e->rows > M->maxT) return fail(HIFT_EINVAL, "%lld new rows, but the model holds %lld", (long long)e->rows, (long long)M->maxT);
+  if (e->max_length < 0 || e->max_length > c.max_seq) return fail(HIFT_EINVAL, "max_length outside the %d positions of the model", c.max_seq);
+  if (e->n_pick < 0 || e->n_pick > M->maxT || (!e->pick && e->n_pick != e->rows)) return fail(HIFT_EINVAL, "n_pick is not the number of rows whose logits are wanted");
+  if (e->ld < c.vocab) return fail(HIFT_EINVAL, "rows of the logits are %lld apart and %d long", (long long)e->ld, c.vocab);
+  const int64_t es = M->es;
+  if (c.n_layers > 1 && (e->layer_stride < 1 || e->layer_stride * es % 16)) return fail(HIFT_EINVAL, "layer_stride must be whole 16-byte pieces");
+  if (e->rows > 0 && (!e->tokens || !e->starts)) return fail(HIFT_EINVAL, "tokens or starts null");
+  if (e->n_pick > 0 && e->rows > 0 && !e->logits) return fail(HIFT_EINVAL, "logits are null");
+  if (reinterpret_cast<uintptr_t>(e->logits) % (uintptr_t)es || (reinterpret_cast<uintptr_t>(e->tokens) | reinterpret_cast<uintptr_t>(e->pick) | reinterpret_cast<uintptr_t>(e->starts)) % 4)
+    return fail(HIFT_EINVAL, "tokens, starts, pick or logits do not lie on whole elements");
+  const size_t head = ((size_t)e->rows * 4 + 255) / 256 * 256;
+  if (out) {
+    out->cache = v; out->layer_bytes = e->layer_stride * es; out->of = e;
+  }
+  if (bytes) *bytes = e->rows == 0 ? 0 : head + attention_paged_bytes(M->dt, v, e->rows, c.n_heads, (int)std::min<int64_t>(e->max_new, e->rows), e->max_length, 0);
+  return HIFT_OK;
+}
+}  // namespace
+
+hift_status hift_extend_bytes(const hift_model* M, const hift_extension* e, size_t* bytes) {
+  if (!bytes) return fail(HIFT_EINVAL, "bytes is null");
+  return check_extension(M, e, nullptr, bytes);
+}
+
+hift_status hift_extend(hift_model* M, const hift_extension* e, void* workspace, size_t workspace_bytes) {
+  Extend ex{};
+  size_t need = 0;
+  ST_TRY(check_extension(M, e, &ex, &need));
+  if (e->rows == 0 || ex.cache.sequences == 0) return HIFT_OK;
+  if (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 15)) return fail(HIFT_EINVAL, "workspace of %zu bytes, 16-byte aligned, expected", need);
+  ex.positions = (int32_t*)workspace;
+  ex.attention = (unsigned char*)workspace + ((size_t)e->rows * 4 + 255) / 256 * 256;
+  if (M->cfg.arch == HIFT_ARCH_PRELN_DECODER) HIP_TRY(cache_positions(ex.cache, e->rows, (int)std::min<int64_t>(e->max_new, e->rows), ex.positions, M->cs));
+  const hift_batch bt{e->tokens, nullptr, 1, (int32_t)e->rows};
+  return forward(M, &bt, M->lay.n_units, nullptr, &ex);
 }
 
 }  // extern "C"

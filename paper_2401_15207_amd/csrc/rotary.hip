@@ -261,6 +261,21 @@ __global__ void __launch_bounds__(BLK) append_k(AppendArgs p) {
   }
 }
 
+// One thread a row: the sequence that the row belongs to is looked for among the starts.
+__global__ void __launch_bounds__(BLK) cache_positions_k(CacheView c, int64_t rows, int max_new, int32_t* positions) {
+  const int64_t row = (int64_t)blockIdx.x * BLK + threadIdx.x;
+  if (row >= rows) return;
+  int lo = 0, hi = c.sequences;  // the last sequence that starts at the row or before
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (c.starts[mid] <= row) lo = mid;
+    else hi = mid;
+  }
+  const CacheSeq of = cache_seq(c, lo, rows, max_new);
+  const int64_t token = row - of.row0;
+  positions[row] = token >= 0 && token < of.fresh ? of.cached + (int)token : 0;
+}
+
 template <typename T, int V>
 hipError_t append_v(AppendArgs p, bool pairs, hipStream_t st) {
   p.units = p.half / V + (p.c.head_dim - 2 * p.half) / V;
@@ -306,6 +321,12 @@ hipError_t rotary(int dt, bool pairs, bool backward, int64_t rows, int heads, in
   if (v == 4) return rotate_v<float, 4>(p, pairs, st);
   if (v == 2) return rotate_v<float, 2>(p, pairs, st);
   return rotate_v<float, 1>(p, pairs, st);
+}
+
+hipError_t cache_positions(const CacheView& c, int64_t rows, int max_new, int32_t* positions, hipStream_t st) {
+  if (rows == 0) return hipSuccess;
+  cache_positions_k<<<(unsigned)((rows + BLK - 1) / BLK), BLK, 0, st>>>(c, rows, max_new, positions);
+  return hipGetLastError();
 }
 
 hipError_t cache_append(int dt, const CacheView& c, int heads, bool pairs, int rot, const float* cos_sin, int table_rows, int64_t rows, int max_new,
