@@ -493,6 +493,9 @@ def kernel_muon(opt: dict, master, grad, momentum, compute_copy=None, workspace=
     _check(lib.hift_kernel_muon(C.byref(o), n, arr, _ptr(ws), nb, st))
 
 
+_raw_stream = torch._C._cuda_getCurrentRawStream
+
+
 ROTARY_SCALING = {"plain": 0, "linear": 1, "base": 2, "parts": 3}
 ROTARY_LAYOUT = {"halves": 0, "pairs": 1}
 
@@ -505,15 +508,15 @@ def make_rotary(r: dict) -> Rotary:
 def _table_of(name, cos_sin, device):
     """A rotary table [rows, rot / 2, 2]: its rows and rot."""
     size = cos_sin.shape
-    if cos_sin.dtype is not torch.float32 or cos_sin.get_device() != device or len(size) != 3 or size[2] != 2 or not cos_sin.is_contiguous():
+    if len(size) != 3 or size[2] != 2 or cos_sin.dtype is not torch.float32 or cos_sin.get_device() != device or not cos_sin.is_contiguous():
         raise ValueError(f"{name}: contiguous float32 [rows, rot / 2, 2] on cuda:{device} expected, not {tuple(size)} of {cos_sin.dtype} on {cos_sin.device}")
     return size[0], 2 * size[1]
 
 
 def kernel_rotary_table(rotary: dict, cos_sin, first=0, stream=None):
     """The table of a rotary embedding (keys of hift_rotary: rot, scaling "plain" / "linear" / "base" / "parts", base, factor, ..) for positions from `first` on."""
-    st = _stream_of(cos_sin, stream)
     rows, rot = _table_of("cos_sin", cos_sin, max(cos_sin.get_device(), 0))
+    st = _stream_of(cos_sin, stream)
     if rot != rotary["rot"]:
         raise ValueError(f"cos_sin: rot / 2 = {rotary['rot'] // 2} expected, not {rot // 2}")
     r = make_rotary(rotary)
@@ -522,10 +525,11 @@ def kernel_rotary_table(rotary: dict, cos_sin, first=0, stream=None):
 
 def kernel_rotary(x, heads, head_dim, y, cos_sin, positions=None, seq=0, layout="halves", backward=False, stream=None):
     """y = the rows of x ([rows, >= heads * head_dim]) with their heads rotated by the table's entry for positions (int32) or row % seq; y may be x."""
-    st, at = _stream_of(x, stream), x.get_device()
-    ldx, rows = _rows_of("x", x), x.shape[0]
-    ldy = _rows_of("y", y, x.dtype, device=at)
-    if x.shape[1] < heads * head_dim or y.shape[1] < heads * head_dim or y.shape[0] != rows:
+    at, (rows, wx), (ry, wy) = x.get_device(), x.shape, y.shape
+    ldx = _rows_of("x", x)
+    ldy = ldx if y is x else _rows_of("y", y, x.dtype, device=at)
+    st = _raw_stream(at) if stream is None else stream.cuda_stream
+    if wx < heads * head_dim or wy < heads * head_dim or ry != rows:
         raise ValueError(f"{rows} rows of {heads} heads of {head_dim} expected, not x {tuple(x.shape)} and y {tuple(y.shape)}")
     table, rot = _table_of("cos_sin", cos_sin, at)
     _check(lib.hift_kernel_rotary(_dtype_code(x), ROTARY_LAYOUT[layout], int(backward), rows, heads, head_dim, rot, x.data_ptr(), ldx, y.data_ptr(), ldy,
@@ -566,16 +570,16 @@ def _starts_of(cache, starts):
 def kernel_cache_append(cache, starts, qkv, heads, q_out=None, cos_sin=None, layout="halves", max_new=None, stream=None):
     """Rows q | k | v: k rotated and v to their pages, q rotated to q_out (qkv itself: in place; None: not wanted).  starts: int32 [sequences + 1]; max_new: most new
     rows of a sequence (None: all of them)."""
-    st, at = _stream_of(qkv, stream), cache.device
-    rows, width = qkv.shape
+    at, (rows, width) = cache.device, qkv.shape
     ld = _rows_of("qkv", qkv, cache.dtype, device=at)
+    st = _raw_stream(at) if stream is None else stream.cuda_stream
     need = (heads + 2 * cache.kv_heads) * cache.head_dim
     if width < need:
         raise ValueError(f"qkv: rows of {need} expected, not {width}")
-    ldq = 0
-    if q_out is not None:
-        ldq = _rows_of("q_out", q_out, cache.dtype, device=at)
-        if q_out.shape[0] != rows or q_out.shape[1] < heads * cache.head_dim:
+    ldq = ld
+    if q_out is not None and q_out is not qkv:
+        ldq, (rq, wq) = _rows_of("q_out", q_out, cache.dtype, device=at), q_out.shape
+        if rq != rows or wq < heads * cache.head_dim:
             raise ValueError(f"q_out: [{rows}, {heads * cache.head_dim}] expected, not {tuple(q_out.shape)}")
     table, rot = (0, 0) if cos_sin is None else _table_of("cos_sin", cos_sin, at)
     _check(lib.hift_kernel_cache_append(cache.ref, rows, _starts_of(cache, starts), rows if max_new is None else max_new, heads, ROTARY_LAYOUT[layout], rot, _ptr(cos_sin),
@@ -591,10 +595,10 @@ def kernel_attention_paged_bytes(cache, rows, heads, max_new, max_length, window
 def kernel_attention_paged(cache, starts, q, heads, out, max_new, max_length, window=0, scale=None, lse=None, workspace=None, stream=None):
     """out = attention of the new rows q ([rows, heads * head_dim]) over the cache, which holds their keys and values already.  max_new: most new rows of a sequence;
     max_length: most tokens of one, new ones included; scale: None for 1 / sqrt(head_dim); lse: float32 [rows, heads] or None."""
-    st, at = _stream_of(q, stream), cache.device
-    rows, hd = q.shape[0], cache.head_dim
+    at, hd, (rows, wq), (ro, wo) = cache.device, cache.head_dim, q.shape, out.shape
     ldq, ldo = _rows_of("q", q, cache.dtype, device=at), _rows_of("out", out, cache.dtype, device=at)
-    if q.shape[1] < heads * hd or out.shape[1] < heads * hd or out.shape[0] != rows:
+    st = _raw_stream(at) if stream is None else stream.cuda_stream
+    if wq < heads * hd or wo < heads * hd or ro != rows:
         raise ValueError(f"q, out: [{rows}, {heads * hd}] expected, not {tuple(q.shape)} and {tuple(out.shape)}")
     if workspace is None:
         need = kernel_attention_paged_bytes(cache, rows, heads, max_new, max_length, window)
@@ -627,9 +631,11 @@ def _adjust_of(rows, vocab, at, tokens, begin, end, repetition, presence, freque
 def kernel_adjust_logits(logits, vocab, out, tokens=None, begin=None, end=None, repetition=1.0, presence=0.0, frequency=0.0, bias=None, allowed=None, stream=None):
     """out = logits with penalties for the tokens that each row has seen (tokens int32; begin, end int64 [rows]), a bias (float32 [1 or rows, vocab]) and a mask of
     allowed tokens (int32 words [1 or rows, ceil(vocab / 32)], bit j % 32 of word j / 32 for token j); out may be logits."""
-    st, at, (rows, width) = _stream_of(logits, stream), logits.get_device(), logits.shape
-    ld, ldo = _rows_of("logits", logits), _rows_of("out", out, logits.dtype, device=at)
-    if vocab > width or vocab > out.shape[1] or out.shape[0] != rows:
+    at, (rows, width), (ro, wo) = logits.get_device(), logits.shape, out.shape
+    ld = _rows_of("logits", logits)
+    ldo = ld if out is logits else _rows_of("out", out, logits.dtype, device=at)
+    st = _raw_stream(at) if stream is None else stream.cuda_stream
+    if vocab > width or vocab > wo or ro != rows:
         raise ValueError(f"vocab {vocab}, but logits are {tuple(logits.shape)} and out {tuple(out.shape)}")
     by = _adjust_of(rows, vocab, at, tokens, begin, end, repetition, presence, frequency, bias, allowed)
     _check(lib.hift_kernel_adjust_logits(_dtype_code(logits), rows, vocab, ld, logits.data_ptr(), C.byref(by), ldo, out.data_ptr(), st))
@@ -638,10 +644,11 @@ def kernel_adjust_logits(logits, vocab, out, tokens=None, begin=None, end=None, 
 def kernel_adjust_logits_bwd(logits, vocab, d_out, d_logits, tokens=None, begin=None, end=None, repetition=1.0, presence=0.0, frequency=0.0, bias=None, allowed=None,
                              stream=None):
     """d_logits = the gradient with respect to the logits of kernel_adjust_logits (same arguments) whose result has the gradient d_out; may be d_out."""
-    st, at, (rows, width) = _stream_of(logits, stream), logits.get_device(), logits.shape
+    at, (rows, width) = logits.get_device(), logits.shape
     ld, ldg, ldd = _rows_of("logits", logits), _rows_of("d_out", d_out, logits.dtype, device=at), _rows_of("d_logits", d_logits, logits.dtype, device=at)
     if min(width, d_out.shape[1], d_logits.shape[1]) < vocab or d_out.shape[0] != rows or d_logits.shape[0] != rows:
         raise ValueError(f"vocab {vocab}, but logits are {tuple(logits.shape)}, d_out {tuple(d_out.shape)} and d_logits {tuple(d_logits.shape)}")
+    st = _raw_stream(at) if stream is None else stream.cuda_stream
     by = _adjust_of(rows, vocab, at, tokens, begin, end, repetition, presence, frequency, bias, allowed)
     _check(lib.hift_kernel_adjust_logits_bwd(_dtype_code(logits), rows, vocab, ld, logits.data_ptr(), C.byref(by), ldg, d_out.data_ptr(), ldd, d_logits.data_ptr(), st))
 

@@ -7,8 +7,8 @@
 // and backwards d = g, g / repetition or g repetition by the same distinction, 0 where the mask has no bit.  In fp32, rounded once.
 //
 // One pass over the logits, bound by memory.  A workgroup takes a slice of a row and counts the row's history for its slice in LDS, in whole
-// numbers, so the order of the additions does not show; the history is read once a slice and comes from L2.  Backwards a logit is read only where
-// a token was seen.
+// numbers, so the order of the additions does not show; the history is read once a slice and comes from L2.  Backwards two bits a token do, whether it was
+// seen and whether its logit is above 0, and logits are read only where a token was seen.
 #include <math.h>
 
 #include <algorithm>
@@ -21,7 +21,9 @@ namespace {
 
 constexpr int BLK = 512;
 constexpr int LOOSE = 8;  // elements before the first aligned piece: at most 7
-constexpr int U = 2;      // pieces of 16 bytes of a thread, at most
+// Pieces of 16 bytes of a thread, at most: forward LDS holds a count for each entry (four workgroups fill a compute unit), backward two bits.
+template <bool BWD>
+constexpr int U = BWD ? 4 : 2;
 
 struct AdjustArgs {
   int V, slice, slices;
@@ -42,9 +44,7 @@ struct AdjustArgs {
 
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 
-constexpr int POSITIVE = INT32_MIN;  // backward: the bit of a count that says that the logit is above 0
-
-// x: the logit, or backward the gradient; n: the count
+// x: the logit, or backward the gradient; n: the count, backward 1 for a seen token and -1 for one whose logit is above 0
 template <bool BWD>
 __device__ __forceinline__ float adjusted(float x, int n, float bias, bool allowed, const AdjustArgs& p) {
   if constexpr (BWD) {
@@ -59,8 +59,10 @@ __device__ __forceinline__ float adjusted(float x, int n, float bias, bool allow
 
 template <typename T, bool BWD>
 __global__ void __launch_bounds__(BLK) adjust_k(AdjustArgs p) {
+  // forward counts [LOOSE + slice], in whole quads; backward bits [2][(LOOSE + slice) / 32]: seen, and above 0.  The first aligned piece is at LOOSE.
   extern __shared__ int4 count_quads[];
-  int* counts = reinterpret_cast<int*>(count_quads);  // [LOOSE + slice] in whole quads, the first aligned piece's at LOOSE
+  int* counts = reinterpret_cast<int*>(count_quads);
+  const int words = (LOOSE + p.slice) / 32 + 1;
   __shared__ int any;
   constexpr int E = 16 / (int)sizeof(T);
   const int64_t row = blockIdx.x / (unsigned)p.slices;
@@ -78,25 +80,45 @@ __global__ void __launch_bounds__(BLK) adjust_k(AdjustArgs p) {
   const int t = threadIdx.x, pieces = p.aligned ? (hi - from) / E : 0;
   // what the pass streams is on its way while the history is counted
   typedef Vec<T, E> P;
-  P in[U];
+  P in[U<BWD>];
+  uint64_t let[U<BWD>];
+  f32x4_any add[U<BWD>][E / 4];
+  const float* bias = p.bias ? p.bias + row * p.ld_bias : nullptr;
+  const uint32_t* allowed = p.allowed ? p.allowed + row * p.ld_allowed : nullptr;
 #pragma unroll
-  for (int k = 0; k < U; ++k)
-    if (t + k * BLK < pieces) in[k] = *reinterpret_cast<const P*>((BWD ? g : x) + from + (t + k * BLK) * E);
+  for (int k = 0; k < U<BWD>; ++k)
+    if (t + k * BLK < pieces) {
+      const int j0 = from + (t + k * BLK) * E;
+      in[k] = *reinterpret_cast<const P*>((BWD ? g : x) + j0);
+      if (allowed) let[k] = (uint64_t)allowed[(j0 + E - 1) >> 5] << 32 | allowed[j0 >> 5];
+      if (!BWD && bias) {
+#pragma unroll
+        for (int e = 0; e < E / 4; ++e) add[k][e] = *reinterpret_cast<const f32x4_any*>(bias + j0 + 4 * e);
+      }
+    }
   bool seen = false;
   if (p.tokens) {
     const int64_t b = min(max(p.begin[row], (int64_t)0), p.n_tokens), e = min(max(p.end[row], b), p.n_tokens);
     if (e > b) {
       if (t == 0) any = 0;
-      for (int i = t; i < (shift + n + 3) / 4; i += BLK) count_quads[i] = make_int4(0, 0, 0, 0);
+      if (BWD)
+        for (int i = t; i < 2 * words; i += BLK) counts[i] = 0;
+      else
+        for (int i = t; i < (shift + n + 3) / 4; i += BLK) count_quads[i] = make_int4(0, 0, 0, 0);
       __syncthreads();
       int mine = 0;
       for (int64_t i = b + t; i < e; i += BLK) {
         const unsigned at = (unsigned)p.tokens[i] - (unsigned)lo;
         if (at < (unsigned)n) {
-          const int had = atomicAdd(&counts[shift + (int)at], 1);
+          const int j = shift + (int)at;
           mine = 1;
-          // backward, the first to meet the token looks its logit up, all of them at the same time: the sign is all that counts
-          if (BWD && had == 0 && to_f32(x[lo + (int)at]) > 0.f) atomicOr(&counts[shift + (int)at], POSITIVE);
+          if constexpr (BWD) {
+            // the first to meet the token looks its logit up, all of them at the same time
+            const int had = atomicOr(&counts[j >> 5], 1 << (j & 31));
+            if (!(had >> (j & 31) & 1) && to_f32(x[lo + (int)at]) > 0.f) atomicOr(&counts[words + (j >> 5)], 1 << (j & 31));
+          } else {
+            atomicAdd(&counts[j], 1);
+          }
         }
       }
       if (mine) any = 1;
@@ -104,10 +126,13 @@ __global__ void __launch_bounds__(BLK) adjust_k(AdjustArgs p) {
       seen = any != 0;
     }
   }
-  const float* bias = p.bias ? p.bias + row * p.ld_bias : nullptr;
-  const uint32_t* allowed = p.allowed ? p.allowed + row * p.ld_allowed : nullptr;
   auto one = [&](int j) __attribute__((always_inline)) {
-    const int c = seen ? counts[shift + j - lo] : 0;
+    int c = 0;
+    if (seen) {
+      const int i = shift + j - lo;
+      if constexpr (BWD) c = counts[i >> 5] >> (i & 31) & 1 ? (counts[words + (i >> 5)] >> (i & 31) & 1 ? -1 : 1) : 0;
+      else c = counts[i];
+    }
     const bool let = !allowed || (allowed[j >> 5] >> (j & 31) & 1);
     out[j] = from_f32<T>(adjusted<BWD>(to_f32((BWD ? g : x)[j]), c, !BWD && bias ? bias[j] : 0.f, let, p));
   };
@@ -116,35 +141,26 @@ __global__ void __launch_bounds__(BLK) adjust_k(AdjustArgs p) {
     return;
   }
 #pragma unroll
-  for (int k = 0; k < U; ++k) {
+  for (int k = 0; k < U<BWD>; ++k) {
     const int i = t + k * BLK;
     if (i >= pieces) break;
     const int j0 = from + i * E;
     int c[E];
+    if constexpr (BWD) {
+      const int b = LOOSE + i * E, w = seen ? counts[b >> 5] >> (b & 31) : 0, above = seen ? counts[words + (b >> 5)] >> (b & 31) : 0;  // a piece lies in one word
 #pragma unroll
-    for (int e = 0; e < E; e += 4) {
-      const int4 q = seen ? count_quads[(LOOSE + i * E + e) / 4] : make_int4(0, 0, 0, 0);
-      c[e] = q.x; c[e + 1] = q.y; c[e + 2] = q.z; c[e + 3] = q.w;
-    }
-    uint32_t bits = 0xFFFFFFFFu;
-    if (allowed) {
-      const int w = j0 >> 5, w1 = (j0 + E - 1) >> 5;
-      bits = (uint32_t)(((uint64_t)allowed[w1] << 32 | allowed[w]) >> (j0 & 31));
-    }
-    float bv[E];
-#pragma unroll
-    for (int e = 0; e < E; ++e) bv[e] = 0.f;
-    if (!BWD && bias) {
+      for (int e = 0; e < E; ++e) c[e] = w >> e & 1 ? (above >> e & 1 ? -1 : 1) : 0;
+    } else {
 #pragma unroll
       for (int e = 0; e < E; e += 4) {
-        const f32x4_any q = *reinterpret_cast<const f32x4_any*>(bias + j0 + e);
-#pragma unroll
-        for (int z = 0; z < 4; ++z) bv[e + z] = q[z];
+        const int4 q = seen ? count_quads[(LOOSE + i * E + e) / 4] : make_int4(0, 0, 0, 0);
+        c[e] = q.x; c[e + 1] = q.y; c[e + 2] = q.z; c[e + 3] = q.w;
       }
     }
+    const uint32_t bits = allowed ? (uint32_t)(let[k] >> (j0 & 31)) : 0xFFFFFFFFu;
     P o;
 #pragma unroll
-    for (int e = 0; e < E; ++e) o.v[e] = from_f32<T>(adjusted<BWD>(to_f32(in[k].v[e]), c[e], bv[e], bits >> e & 1, p));
+    for (int e = 0; e < E; ++e) o.v[e] = from_f32<T>(adjusted<BWD>(to_f32(in[k].v[e]), c[e], !BWD && bias ? add[k][e / 4][e % 4] : 0.f, bits >> e & 1, p));
     *reinterpret_cast<P*>(out + j0) = o;
   }
   // what is left before the first piece and after the last
@@ -155,15 +171,16 @@ __global__ void __launch_bounds__(BLK) adjust_k(AdjustArgs p) {
 
 template <typename T, bool BWD>
 hipError_t run(AdjustArgs p, hipStream_t st) {
-  // Slices: U pieces a thread, fewer where rows are few, down to one.
+  // Slices: U pieces a thread, fewer where rows are few, down to one
   constexpr int E = 16 / (int)sizeof(T);
-  p.slice = U * BLK * E;
+  p.slice = U<BWD> * BLK * E;
   while (p.slice > BLK * E && p.rows * ((p.V + p.slice - 1) / p.slice) < 512) p.slice /= 2;
   p.slices = (int)(((int64_t)p.V + p.slice - 1) / p.slice);
   if (p.rows * p.slices > 0x7FFFFFFF) return hipErrorInvalidValue;
   const auto low = [](const void* q) { return (int64_t)(reinterpret_cast<uintptr_t>(q) & 15); };
   p.aligned = low(p.out) == low(BWD ? p.g : p.x) && (p.ldo - (BWD ? p.ldg : p.ld)) % E == 0;
-  adjust_k<T, BWD><<<(unsigned)(p.rows * p.slices), BLK, (size_t)(LOOSE + p.slice + 4) * 4, st>>>(p);
+  const size_t lds = BWD ? ((LOOSE + p.slice) / 32 + 1) * 8 : (size_t)(LOOSE + p.slice + 4) * 4;
+  adjust_k<T, BWD><<<(unsigned)(p.rows * p.slices), BLK, lds, st>>>(p);
   return hipGetLastError();
 }
 

@@ -50,7 +50,7 @@ struct Args {
   int few_blocks, many_blocks;  // blocks of rows of the longest sequence
   int runs;             // few_k's workgroups, or 0
   int few_first;        // mixed_k: workgroups that few rows take
-  int64_t* plan;        // [0]: steps of a run; [1 + e]: steps before entry e
+  int64_t* plan;        // [0]: steps in all; [1 + e]: steps before entry e
   float2* part_ml;      // [run][2][FEW] (maximum, sum of exponentials) of a run's first and last rows where those are shared with other runs
   float* part;          // [run][2][FEW][HD] their sums
 };
@@ -399,7 +399,9 @@ __global__ void __launch_bounds__(64 * W) few_whole_k(Args p) {
   few_whole<T, HD, NB, W>(p, (int)blockIdx.x, lds, ml);
 }
 
-// Equal runs of steps
+// Equal runs of steps: run w is [w all / runs, (w + 1) all / runs), rounded down, with no more runs than steps, so that none is empty.
+__device__ __forceinline__ int64_t run_start(int w, int64_t all, int runs) { return w * all / runs; }
+__device__ __forceinline__ int run_of(int64_t step, int64_t all, int runs) { return (int)(((step + 1) * runs - 1) / all); }
 template <typename T, int HD, int NB>
 __global__ void __launch_bounds__(256) few_k(Args p) {
   extern __shared__ unsigned char lds[];
@@ -411,8 +413,8 @@ __global__ void __launch_bounds__(256) few_k(Args p) {
   __shared__ int found;
   const int tid = threadIdx.x, entries = p.c.sequences * p.few_blocks, each = (entries + 255) / 256;
   const int e0 = min(tid * each, entries), e1 = min(e0 + each, entries);
-  int64_t mine = 0;
-  for (int e = e0; e < e1; ++e) mine += (int64_t)Entry(p, e / p.few_blocks, e % p.few_blocks).steps * kv_heads;
+  int64_t mine = 0, last = 0;
+  for (int e = e0; e < e1; ++e) mine += last = (int64_t)Entry(p, e / p.few_blocks, e % p.few_blocks).steps * kv_heads;
   sums[tid] = mine;
   if (tid == 0) found = -1;
   __syncthreads();
@@ -423,12 +425,14 @@ __global__ void __launch_bounds__(256) few_k(Args p) {
     before += k < tid ? v : 0;
     all += v;
   }
-  const int64_t run = max((all + p.runs - 1) / p.runs, (int64_t)1), at0 = (int64_t)blockIdx.x * run, at1 = min(at0 + run, all);
-  if (blockIdx.x == 0 && tid == 0) p.plan[0] = run;
+  const int runs = (int)min((int64_t)p.runs, all);
+  if (blockIdx.x == 0 && tid == 0) p.plan[0] = all;
+  if ((int)blockIdx.x >= runs) return;
+  const int64_t at0 = run_start((int)blockIdx.x, all, runs), at1 = run_start((int)blockIdx.x + 1, all, runs);
   if (blockIdx.x == 0 || (before <= at0 && at0 < before + mine)) {
     int64_t b = before;
     for (int e = e0; e < e1; ++e) {
-      const int64_t n = (int64_t)Entry(p, e / p.few_blocks, e % p.few_blocks).steps * kv_heads;
+      const int64_t n = each == 1 ? last : (int64_t)Entry(p, e / p.few_blocks, e % p.few_blocks).steps * kv_heads;
       if (blockIdx.x == 0) p.plan[1 + e] = b;
       if (b <= at0 && at0 < b + n) {
         found = e;
@@ -769,24 +773,43 @@ __global__ void __launch_bounds__(256) join_k(Args p, int tokens) {
   const int64_t st = i / p.heads;
   if (st >= (int64_t)p.c.sequences * tokens) return;
   const int s = (int)(st / tokens), token = (int)(st % tokens), kv_head = head / p.group, m = token * p.group + head % p.group, block = m / FEW;
+  const int64_t all = p.plan[0], before = p.plan[1 + (int64_t)s * p.few_blocks + block];
   const Entry en(p, s, block);
   if (en.steps == 0 || token >= en.of.fresh) return;
-  const int64_t run = p.plan[0], first = p.plan[1 + (int64_t)s * p.few_blocks + block] + (int64_t)kv_head * en.steps;
-  const int64_t r0 = first / run, r1 = (first + en.steps - 1) / run;
+  const int64_t first = before + (int64_t)kv_head * en.steps;
+  const int runs = (int)min((int64_t)p.runs, all), r0 = run_of(first, all, runs), r1 = run_of(first + en.steps - 1, all, runs);
   if (r0 == r1) return;
-  auto place = [&](int64_t r) { return (r * 2 + (r == r0)) * FEW + m % FEW; };
-  float top = -INFINITY;
-  for (int64_t r = r0; r <= r1; ++r) top = fmaxf(top, p.part_ml[place(r)].x);
-  const float ref = top == -INFINITY ? 0.f : top;
-  float l = 0.f, o[HD / 64];
+  // four parts at a time, all their loads on the way together
+  constexpr int P = 4;
+  float top = -INFINITY, l = 0.f, o[HD / 64];
 #pragma unroll
   for (int c = 0; c < HD / 64; ++c) o[c] = 0.f;
-  for (int64_t r = r0; r <= r1; ++r) {
-    const int64_t at = place(r);
-    const float by = __builtin_amdgcn_exp2f(p.part_ml[at].x - ref);
-    l = fmaf(by, p.part_ml[at].y, l);
+  for (int r = r0; r <= r1; r += P) {
+    float2 ml[P];
+    float v[P][HD / 64];
 #pragma unroll
-    for (int c = 0; c < HD / 64; ++c) o[c] = fmaf(by, p.part[at * HD + c * 64 + lane], o[c]);
+    for (int k = 0; k < P; ++k) {
+      const int64_t at = ((int64_t)min(r + k, r1) * 2 + (min(r + k, r1) == r0)) * FEW + m % FEW;
+      ml[k] = p.part_ml[at];
+#pragma unroll
+      for (int c = 0; c < HD / 64; ++c) v[k][c] = p.part[at * HD + c * 64 + lane];
+    }
+    float now = top;
+#pragma unroll
+    for (int k = 0; k < P; ++k) now = fmaxf(now, ml[k].x);
+    const float ref = now == -INFINITY ? 0.f : now, by = __builtin_amdgcn_exp2f(top - ref);
+    l *= by;
+#pragma unroll
+    for (int c = 0; c < HD / 64; ++c) o[c] *= by;
+#pragma unroll
+    for (int k = 0; k < P; ++k) {
+      const float w = r + k <= r1 ? __builtin_amdgcn_exp2f(ml[k].x - ref) : 0.f;
+      l = fmaf(w, ml[k].y, l);
+#pragma unroll
+      for (int c = 0; c < HD / 64; ++c)
+        if (r + k <= r1) o[c] = fmaf(w, v[k][c], o[c]);
+    }
+    top = now;
   }
   RowAt r;
   r.row = en.of.row0 + token; r.head = head;
