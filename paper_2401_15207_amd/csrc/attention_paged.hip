@@ -50,9 +50,10 @@ struct Args {
   int few_blocks, many_blocks;  // blocks of rows of the longest sequence
   int runs;             // few_k's workgroups, or 0
   int few_first;        // mixed_k: workgroups that few rows take
+  int split, chunk;     // mixed_k: workgroups along the keys of a block of many rows, and keys of each
   int64_t* plan;        // [0]: steps in all; [1 + e]: steps before entry e
-  float2* part_ml;      // [run][2][FEW] (maximum, sum of exponentials) of a run's first and last rows where those are shared with other runs
-  float* part;          // [run][2][FEW][HD] their sums
+  float2* part_ml;      // (maximum, sum of exponentials) of shared rows: few_k [run][2][FEW], a run's first and last block of rows; mixed_k [rows][heads][split]
+  float* part;          // [..][HD] their sums
 };
 
 // ---- tiles of a type and width ----
@@ -460,6 +461,46 @@ __global__ void __launch_bounds__(256) few_k(Args p) {
   }
 }
 
+// ---- many rows ----
+// Part `part` of the keys [from, to) of a block of rows; how many parts have keys
+__device__ __forceinline__ int part_of(const Args& p, int part, int& from, int& to) {
+  const int n = min(p.split, max(1, (to - from + p.chunk - 1) / p.chunk));
+  const int last = to;
+  from += part * p.chunk;
+  if (part + 1 < n) to = from + p.chunk;
+  else to = part + 1 == n ? last : from;
+  return n;
+}
+// A row's result: to the output, or as a part.  o: see Tile::values
+template <typename T, int HD, int NB>
+__device__ __forceinline__ void finish_row(const Args& p, const RowAt& at, const f32x16 (&o)[NB], float m, float l, int part, int parts, int fh) {
+  if (!at.ok) return;
+  if (parts > 1) {
+    const int64_t to = (at.row * p.heads + at.head) * p.split + part;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<f32x4*>(p.part + to * HD + nb * 32 + 8 * g + 4 * fh) = f32x4{o[nb][4 * g], o[nb][4 * g + 1], o[nb][4 * g + 2], o[nb][4 * g + 3]};
+    if (fh == 0) p.part_ml[to] = make_float2(m, l);
+    return;
+  }
+  const float inv = l > 0.f || l != l ? 1.0f / l : 0.f;
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int c = nb * 32 + 8 * g + 4 * fh;
+      if (c < p.c.head_dim) {
+        Vec<T, 4> v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v.v[e] = from_f32<T>(o[nb][4 * g + e] * inv);
+        *reinterpret_cast<Vec<T, 4>*>((T*)p.out + at.row * p.ldo + (int64_t)at.head * p.c.head_dim + c) = v;
+      }
+    }
+  if (fh == 0 && p.lse) p.lse[at.row * p.heads + at.head] = m + __builtin_amdgcn_logf(l);
+}
+
 // ---- many rows, fp32 ----
 template <int HD, int NB_>
 __device__ __forceinline__ void many_rows_f32(const Args& p, const int index, unsigned char* lds /* [buffer][K | V] tiles of 64 keys */) {
@@ -467,7 +508,8 @@ __device__ __forceinline__ void many_rows_f32(const Args& p, const int index, un
   typedef Tile<T, HD, NB_> L;
   constexpr int NB = L::NB, KT = 2 * KB, TILEB = KT * L::ROWB, QB = 128;
   const int tid = threadIdx.x, lane = tid & 63, wave = UNIFORM(tid >> 6), fr = lane & 31, fh = lane >> 5;
-  const int block = p.many_blocks - 1 - index % p.many_blocks, pair = index / p.many_blocks;  // most keys first
+  int i = index / p.split;
+  const int part = index - i * p.split, block = p.many_blocks - 1 - i % p.many_blocks, pair = i / p.many_blocks;  // most keys first
   const int s = pair / p.c.kv_heads, kv_head = pair % p.c.kv_heads;
   const CacheSeq of = cache_seq(p.c, s, p.rows, p.max_new);
   const int n_rows = of.fresh * p.group;
@@ -475,6 +517,8 @@ __device__ __forceinline__ void many_rows_f32(const Args& p, const int index, un
   const int m0 = block * QB, m_last = min(n_rows, m0 + QB) - 1;
   int from, to;
   keys_of(of, m0 / p.group, m_last / p.group, p.window, from, to);
+  const int parts = part_of(p, part, from, to);
+  if (part >= parts) return;
 
   const int w0 = m0 + wave * 32;  // this wavefront's rows; their first and last positions
   const int pos_lo = of.cached + min(w0, m_last) / p.group, pos_hi = of.cached + min(w0 + 31, m_last) / p.group;
@@ -523,21 +567,7 @@ __device__ __forceinline__ void many_rows_f32(const Args& p, const int index, un
     L::values(run.o, Kb + TILEB + L::BLOCKB, ad, sc[1], lane);
   }
   run.l += __shfl_xor(run.l, 32, 64);
-  if (!at.ok) return;
-  const float inv = run.l > 0.f || run.l != run.l ? 1.0f / run.l : 0.f;
-#pragma unroll
-  for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const int c = nb * 32 + 8 * g + 4 * fh;
-      if (c < p.c.head_dim) {
-        Vec<T, 4> o;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o.v[e] = from_f32<T>(run.o[nb][4 * g + e] * inv);
-        *reinterpret_cast<Vec<T, 4>*>((T*)p.out + at.row * p.ldo + (int64_t)at.head * p.c.head_dim + c) = o;
-      }
-    }
-  if (fh == 0 && p.lse) p.lse[at.row * p.heads + at.head] = run.m + __builtin_amdgcn_logf(run.l);
+  finish_row<T, HD, NB>(p, at, run.o, run.m, run.l, part, parts, fh);
 }
 
 // ---- many rows, bf16 ----
@@ -574,8 +604,8 @@ __device__ __forceinline__ void many_rows_bf16(const Args& p, const int index, u
   const int tid = threadIdx.x, lane = tid & 63, wave = UNIFORM(tid >> 6), fr = lane & 31, fh = lane >> 5;
   // Workgroups start in the order of their index: those with the most keys first.  Neighbours take different heads, so that the workgroups of a head, which read
   // the same keys, are on one of the eight dies where the heads are a multiple of them.
-  int i = index;
-  const int kv_head = i % p.c.kv_heads;
+  int i = index / p.split;
+  const int part = index - i * p.split, kv_head = i % p.c.kv_heads;
   i /= p.c.kv_heads;
   const int block = p.many_blocks - 1 - i % p.many_blocks, s = longest(p, i / p.many_blocks, reinterpret_cast<int*>(lds));
   const CacheSeq of = cache_seq(p.c, s, p.rows, p.max_new);
@@ -584,6 +614,8 @@ __device__ __forceinline__ void many_rows_bf16(const Args& p, const int index, u
   const int m0 = block * QB, m_last = min(n_rows, m0 + QB) - 1;
   int from, to;
   keys_of(of, m0 / p.group, m_last / p.group, p.window, from, to);
+  const int parts = part_of(p, part, from, to);
+  if (part >= parts) return;
   const int w0 = m0 + wave * 32, w_last = min(w0 + 31, m_last);  // this wavefront's rows
   const int pos_lo = of.cached + w0 / p.group, pos_hi = of.cached + w_last / p.group;
   const RowAt at = row_at(p, of, kv_head, w0 + fr);
@@ -597,20 +629,20 @@ __device__ __forceinline__ void many_rows_bf16(const Args& p, const int index, u
   const L head(p.c, kv_head);
   const int tiles = (to - from + KT - 1) / KT;
   // tiles that this wavefront's rows see
-  const int mine = w0 > m_last ? 0 : min(tiles, (min(to, pos_hi + 1) - from + KT - 1) / KT);
+  const int mine = w0 > m_last ? 0 : max(0, min(tiles, (min(to, pos_hi + 1) - from + KT - 1) / KT));
 
   // whether all pages are there
   bool lane_whole = true;
   for (int key = from + lane * GROUP; key < to; key += 64 * GROUP) lane_whole &= cache_page_any(p.c, s, key) >= 0;
   const bool whole = __builtin_amdgcn_ballot_w64(!lane_whole) == 0;
   // every wavefront brings 16 keys of a tile and their values
-  const int part = wave * GROUP;
-  auto page = [&](int t) { const int key = from + t * KT + part; return UNIFORM(t < tiles && key < to ? cache_page(p.c, s, key) : -1); };
+  const int own = wave * GROUP;
+  auto page = [&](int t) { const int key = from + t * KT + own; return UNIFORM(t < tiles && key < to ? cache_page(p.c, s, key) : -1); };
   int page_next = page(0);
   uint32_t v_last = 0, v_now = 0, v_next = 2 * TILEB;  // LDS offsets of the values of the tile before, of this one and of the next
   auto request = [&](int t) __attribute__((always_inline)) {
-    head.request(p.c.k, from + t * KT + part, page_next, to, vo, lds0 + (t & 1) * TILEB + part * L::ROWB);
-    head.request(p.c.v, from + t * KT + part, page_next, to, vo, lds0 + v_next + part * L::ROWB);
+    head.request(p.c.k, from + t * KT + own, page_next, to, vo, lds0 + (t & 1) * TILEB + own * L::ROWB);
+    head.request(p.c.v, from + t * KT + own, page_next, to, vo, lds0 + v_next + own * L::ROWB);
     page_next = page(t + 1);
   };
   // Tile t is there, and where the next one goes nobody reads any more.
@@ -737,21 +769,7 @@ __device__ __forceinline__ void many_rows_bf16(const Args& p, const int index, u
   }
 
   l += __shfl_xor(l, 32, 64);
-  if (!at.ok) return;
-  const float inv = l > 0.f || l != l ? 1.0f / l : 0.f;
-#pragma unroll
-  for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      const int c = nb * 32 + 8 * g + 4 * fh;
-      if (c < p.c.head_dim) {
-        Vec<bf16, 4> v;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v.v[e] = from_f32<bf16>(o[nb][4 * g + e] * inv);
-        *reinterpret_cast<Vec<bf16, 4>*>((bf16*)p.out + at.row * p.ldo + (int64_t)at.head * p.c.head_dim + c) = v;
-      }
-    }
-  if (fh == 0 && p.lse) p.lse[at.row * p.heads + at.head] = m + __builtin_amdgcn_logf(l);
+  finish_row<bf16, HD, NB>(p, at, o, m, l, part, parts, fh);
 }
 
 // Sequences of many rows, and those of few, if there may be any: the first few_first workgroups, one a key head.
@@ -763,90 +781,147 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) mixed_k(Args p) {
   else many_rows_f32<HD, NB>(p, (int)blockIdx.x - p.few_first, lds);
 }
 
-// ---- rows whose keys fell to several runs ----
-// One wavefront a row and head of the first `tokens` tokens of a sequence.
-template <typename T, int HD>
+// ---- rows whose keys fell to several workgroups ----
+// W wavefronts, one or four, for each row and head of the first `tokens` tokens of a sequence; they take turns at the parts, four at a time, all their
+// loads on the way together.
+template <typename T, int HD, bool RUNS, int W>
 __global__ void __launch_bounds__(256) join_k(Args p, int tokens) {
-  const int lane = threadIdx.x & 63;
-  const int64_t i = (int64_t)blockIdx.x * 4 + UNIFORM(threadIdx.x >> 6);
-  const int head = (int)(i % p.heads);
-  const int64_t st = i / p.heads;
-  if (st >= (int64_t)p.c.sequences * tokens) return;
-  const int s = (int)(st / tokens), token = (int)(st % tokens), kv_head = head / p.group, m = token * p.group + head % p.group, block = m / FEW;
-  const int64_t all = p.plan[0], before = p.plan[1 + (int64_t)s * p.few_blocks + block];
-  const Entry en(p, s, block);
-  if (en.steps == 0 || token >= en.of.fresh) return;
-  const int64_t first = before + (int64_t)kv_head * en.steps;
-  const int runs = (int)min((int64_t)p.runs, all), r0 = run_of(first, all, runs), r1 = run_of(first + en.steps - 1, all, runs);
-  if (r0 == r1) return;
-  // four parts at a time, all their loads on the way together
-  constexpr int P = 4;
-  float top = -INFINITY, l = 0.f, o[HD / 64];
+  constexpr int P = 4, C = HD / 64;
+  __shared__ float sums[W == 1 ? 1 : W][HD];
+  __shared__ float2 ml[4];
+  const int lane = threadIdx.x & 63, wave = W == 1 ? 0 : UNIFORM(threadIdx.x >> 6);
+  const int item = W == 1 ? (int)blockIdx.x * 4 + UNIFORM(threadIdx.x >> 6) : (int)blockIdx.x;
+  const int head = (int)((unsigned)item % (unsigned)p.heads), st = (int)((unsigned)item / (unsigned)p.heads);
+  const int s = st / tokens, token = st % tokens, kv_head = head / p.group, m = token * p.group + head % p.group;
+  if (s >= p.c.sequences) return;
+  int n;          // parts
+  int64_t first;  // the first one's place; the others follow, every `apart`-th
+  int64_t apart;
+  int64_t row;
+  if constexpr (RUNS) {
+    const int block = m / FEW;
+    const int64_t all = p.plan[0], before = p.plan[1 + (int64_t)s * p.few_blocks + block];
+    const Entry en(p, s, block);
+    if (en.steps == 0 || token >= en.of.fresh) return;
+    const int64_t step = before + (int64_t)kv_head * en.steps;
+    const int runs = (int)min((int64_t)p.runs, all), r0 = run_of(step, all, runs);
+    n = run_of(step + en.steps - 1, all, runs) - r0 + 1;
+    first = ((int64_t)r0 * 2) * FEW + m % FEW;  // the first part is a run's last block of rows, the others are their run's first
+    apart = 2 * FEW;
+    row = en.of.row0 + token;
+  } else {
+    const CacheSeq of = cache_seq(p.c, s, p.rows, p.max_new);
+    const int rows = of.fresh * p.group, block = m / 128;
+    if (token >= of.fresh || rows <= p.few_upto) return;
+    int from, to;
+    keys_of(of, block * 128 / p.group, (min(rows, block * 128 + 128) - 1) / p.group, p.window, from, to);
+    n = part_of(p, 0, from, to);
+    row = of.row0 + token;
+    first = (row * p.heads + head) * p.split;
+    apart = 1;
+  }
+  if (n == 1) return;
+  float top = -INFINITY, l = 0.f, o[C];
 #pragma unroll
-  for (int c = 0; c < HD / 64; ++c) o[c] = 0.f;
-  for (int r = r0; r <= r1; r += P) {
-    float2 ml[P];
-    float v[P][HD / 64];
+  for (int c = 0; c < C; ++c) o[c] = 0.f;
+  for (int r = wave * P; r < n; r += W * P) {
+    float2 z[P];
+    float v[P][C];
 #pragma unroll
     for (int k = 0; k < P; ++k) {
-      const int64_t at = ((int64_t)min(r + k, r1) * 2 + (min(r + k, r1) == r0)) * FEW + m % FEW;
-      ml[k] = p.part_ml[at];
+      const int i = min(r + k, n - 1);
+      const int64_t at = first + i * apart + (RUNS && i == 0 ? FEW : 0);
+      z[k] = p.part_ml[at];
 #pragma unroll
-      for (int c = 0; c < HD / 64; ++c) v[k][c] = p.part[at * HD + c * 64 + lane];
+      for (int c = 0; c < C; ++c) v[k][c] = p.part[at * HD + c * 64 + lane];
     }
     float now = top;
 #pragma unroll
-    for (int k = 0; k < P; ++k) now = fmaxf(now, ml[k].x);
+    for (int k = 0; k < P; ++k) now = fmaxf(now, z[k].x);
     const float ref = now == -INFINITY ? 0.f : now, by = __builtin_amdgcn_exp2f(top - ref);
     l *= by;
 #pragma unroll
-    for (int c = 0; c < HD / 64; ++c) o[c] *= by;
+    for (int c = 0; c < C; ++c) o[c] *= by;
 #pragma unroll
-    for (int k = 0; k < P; ++k) {
-      const float w = r + k <= r1 ? __builtin_amdgcn_exp2f(ml[k].x - ref) : 0.f;
-      l = fmaf(w, ml[k].y, l);
+    for (int k = 0; k < P; ++k)
+      if (r + k < n) {
+        const float w = __builtin_amdgcn_exp2f(z[k].x - ref);
+        l = fmaf(w, z[k].y, l);
 #pragma unroll
-      for (int c = 0; c < HD / 64; ++c)
-        if (r + k <= r1) o[c] = fmaf(w, v[k][c], o[c]);
-    }
+        for (int c = 0; c < C; ++c) o[c] = fmaf(w, v[k][c], o[c]);
+      }
     top = now;
   }
   RowAt r;
-  r.row = en.of.row0 + token; r.head = head;
+  r.row = row; r.head = head;
+  if constexpr (W == 1) {
 #pragma unroll
-  for (int c = 0; c < HD / 64; ++c) store_out<T>(p, r, c * 64 + lane, l > 0.f || l != l ? o[c] / l : 0.f);
-  if (lane == 0 && p.lse) p.lse[r.row * p.heads + head] = top + __builtin_amdgcn_logf(l);
+    for (int c = 0; c < C; ++c) store_out<T>(p, r, c * 64 + lane, l > 0.f || l != l ? o[c] / l : 0.f);
+    if (lane == 0 && p.lse) p.lse[row * p.heads + head] = top + __builtin_amdgcn_logf(l);
+    return;
+  }
+#pragma unroll
+  for (int c = 0; c < C; ++c) sums[wave][c * 64 + lane] = o[c];
+  if (lane == 0) ml[wave] = make_float2(top, l);
+  __syncthreads();
+  if (threadIdx.x >= HD) return;
+  float all_top = ml[0].x, all_l = 0.f, all_o = 0.f;
+#pragma unroll
+  for (int w = 1; w < W; ++w) all_top = fmaxf(all_top, ml[w].x);
+  const float ref = all_top == -INFINITY ? 0.f : all_top;
+#pragma unroll
+  for (int w = 0; w < W; ++w) {
+    const float by = __builtin_amdgcn_exp2f(ml[w].x - ref);
+    all_l = fmaf(by, ml[w].y, all_l);
+    all_o = fmaf(by, sums[w][threadIdx.x], all_o);
+  }
+  store_out<T>(p, r, threadIdx.x, all_l > 0.f || all_l != all_l ? all_o / all_l : 0.f);
+  if (threadIdx.x == 0 && p.lse) p.lse[row * p.heads + head] = all_top + __builtin_amdgcn_logf(all_l);
 }
 
 // ---- host ----
 struct Plan {
   bool many;
-  int few_blocks, few_upto, few_first, many_blocks, runs, waves;
-  int64_t entries;
+  int few_blocks, few_upto, few_first, many_blocks, split, chunk, runs, waves;
+  int64_t entries, parts;  // rows of partial sums
 };
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 Plan plan_of(int dt, const CacheView& c, int64_t rows, int heads, int max_new, int64_t max_length, int window) {
   Plan p{};
   const int group = heads / c.kv_heads;
   const int64_t most = (int64_t)max_new * group, pairs = (int64_t)c.sequences * c.kv_heads;  // rows of the longest sequence
-  // the kernel for many rows shares a tile of keys among more of them; few_k gives more workgroups, and takes all where they do not fill the chip
-  p.many = most > FEW && pairs * up(most, FEW) > 1024;
+  int64_t span = std::max<int64_t>(1, std::min<int64_t>(max_length, (int64_t)c.max_pages << c.page_shift));
+  // as many workgroups as are on the chip at a time: LDS holds four blocks of rows of 128 bytes, two of 256, one of 512
+  const int row_bytes = (c.head_dim <= 64 ? 64 : 128) * (dt == DT_BF16 ? 2 : 4), resident = 256 * 512 / row_bytes;
+  // mixed_k shares a tile of keys among more rows; few_k gives more workgroups, and takes all where there are few rows.  bf16, us, few_k / mixed_k: 16 sequences,
+  // 16 new over 2000, 32 / 8 heads (256 blocks of 32 rows) 73 / 41; 1, 256 over 8192, 32 / 8 (256) 180 / 63; 1, 128 over 500, 8 / 8 (32) 16 / 23.  fp32, where an
+  // instruction takes eight times as long and the chain of a workgroup shows: 2, 300 over 300, 16 / 4 (304) 64 / 98; 1, 1024, 32 / 32 (1024) 201 / 157.
+  p.many = most > FEW && pairs * up(most, FEW) > (dt == DT_BF16 ? 128 : 512);
   const bool few = !p.many || rows < (int64_t)c.sequences * max_new;  // else no sequence is short where the longest is not, as a rule; the others take any
   p.few_upto = !p.many ? INT32_MAX : few ? FEW : 0;
   p.few_first = p.many && few ? (int)pairs : 0;
   p.few_blocks = (int)(p.many ? 1 : std::max<int64_t>(1, up(most, FEW)));
   p.many_blocks = (int)std::max<int64_t>(1, up(most, 128));
   p.entries = (int64_t)c.sequences * p.few_blocks;
-  if (p.many) return p;
-  int64_t span = std::max<int64_t>(1, std::min<int64_t>(max_length, (int64_t)c.max_pages << c.page_shift));
+  p.split = 1; p.chunk = INT32_MAX / 2;
+  if (p.many) {
+    if (window > 0) span = std::min<int64_t>(span, (int64_t)window + 128 / group + KB);
+    // the keys are split where a compute unit would not have a workgroup (2, 512 over 4096, 32 / 32 heads: 114 -> 78 us), and not beyond: the parts cost more
+    const int64_t n = std::min<int64_t>({up(256, pairs * p.many_blocks), up(span, 512), 64});
+    if (n > 1) {
+      p.chunk = (int)(up(up(span, n), 64) * 64);
+      p.split = (int)up(span, p.chunk);
+      p.parts = rows * heads * p.split;
+    }
+    return p;
+  }
   if (window > 0) span = std::min<int64_t>(span, (int64_t)window + FEW + KB);
-  // as many runs as workgroups are on the chip at a time: LDS holds four blocks of rows of 128 bytes, two of 256, one of 512
-  const int row_bytes = (c.head_dim <= 64 ? 64 : 128) * (dt == DT_BF16 ? 2 : 4), resident = 256 * 512 / row_bytes;
   const int64_t items = pairs * p.few_blocks;
   p.waves = items <= 256 && row_bytes <= 256 && span > STEP ? 8 : 4;
-  if (span > p.waves * STEP) {
+  if (span > (items >= resident ? 8 : p.waves) * STEP) {
     p.waves = 4;
     p.runs = (int)std::min<int64_t>(resident, items * up(span, STEP));
+    p.parts = (int64_t)p.runs * 2 * FEW;
   }
   return p;
 }
@@ -864,13 +939,13 @@ hipError_t allow_lds() {
 
 template <typename T, int HD, int NB>
 hipError_t launch(const Plan& pl, Args a, int max_new, void* workspace, hipStream_t st) {
-  a.few_upto = pl.few_upto; a.few_blocks = pl.few_blocks; a.many_blocks = pl.many_blocks; a.runs = pl.runs; a.few_first = pl.few_first;
+  a.few_upto = pl.few_upto; a.few_blocks = pl.few_blocks; a.many_blocks = pl.many_blocks; a.runs = pl.runs; a.few_first = pl.few_first; a.split = pl.split; a.chunk = pl.chunk;
   a.plan = (int64_t*)workspace;
   a.part_ml = (float2*)((unsigned char*)workspace + plan_bytes(pl));
-  a.part = (float*)(a.part_ml + (int64_t)pl.runs * 2 * FEW);
+  a.part = (float*)(a.part_ml + up(pl.parts, 2) * 2);
   const int64_t pairs = (int64_t)a.c.sequences * a.c.kv_heads, rows = (int64_t)a.c.sequences * max_new * a.heads;
-  const int64_t grid = pl.many ? pl.few_first + pairs * pl.many_blocks : pl.runs ? pl.runs : pairs * pl.few_blocks;
-  if (grid > 0x7FFFFFFF || up(rows, 4) > 0x7FFFFFFF || pl.entries > 0x7FFFFFFF) return hipErrorInvalidValue;
+  const int64_t grid = pl.many ? pl.few_first + pairs * pl.many_blocks * pl.split : pl.runs ? pl.runs : pairs * pl.few_blocks;
+  if (grid > 0x7FFFFFFF || rows > 0x7FFFFFFF || pl.entries > 0x7FFFFFFF) return hipErrorInvalidValue;
   constexpr int BLOCKB = KB * HD * (int)sizeof(T), FEW_LDS = 4 * 2 * BLOCKB, MANY_LDS = (sizeof(T) == 2 ? 5 : 4) * 2 * BLOCKB;
   constexpr int MIXED_LDS = std::max(MANY_LDS, FEW_LDS + 4 * FEW * 8);
   static_assert(4 * FEW * HD * 4 <= FEW_LDS, "the wavefronts' sums fit where their tiles were");
@@ -878,10 +953,13 @@ hipError_t launch(const Plan& pl, Args a, int max_new, void* workspace, hipStrea
   if (pl.many) {
     if (hipError_t e = allow_lds<mixed_k<T, HD, NB>, MIXED_LDS>()) return e;
     mixed_k<T, HD, NB><<<g, 256, MIXED_LDS, st>>>(a);
+    if (pl.split > 4) join_k<T, HD, false, 4><<<(unsigned)rows, 256, 0, st>>>(a, max_new);
+    else if (pl.split > 1) join_k<T, HD, false, 1><<<(unsigned)up(rows, 4), 256, 0, st>>>(a, max_new);
   } else if (pl.runs) {
     if (hipError_t e = allow_lds<few_k<T, HD, NB>, FEW_LDS>()) return e;
     few_k<T, HD, NB><<<g, 256, FEW_LDS, st>>>(a);
-    join_k<T, HD><<<(unsigned)up(rows, 4), 256, 0, st>>>(a, max_new);
+    if (pl.runs > 4 * pairs * pl.few_blocks) join_k<T, HD, true, 4><<<(unsigned)rows, 256, 0, st>>>(a, max_new);  // more than four parts a row
+    else join_k<T, HD, true, 1><<<(unsigned)up(rows, 4), 256, 0, st>>>(a, max_new);
   } else if (pl.waves == 8) {
     if constexpr (2 * FEW_LDS <= 131072) {
       if (hipError_t e = allow_lds<few_whole_k<T, HD, NB, 8>, 2 * FEW_LDS>()) return e;
@@ -908,7 +986,7 @@ hipError_t launch_width(const Plan& pl, const Args& a, int max_new, void* worksp
 size_t attention_paged_bytes(int dt, const CacheView& c, int64_t rows, int heads, int max_new, int64_t max_length, int window) {
   if (rows == 0 || c.sequences == 0 || max_new == 0) return 0;
   const Plan p = plan_of(dt, c, rows, heads, max_new, max_length, window);
-  return plan_bytes(p) + (size_t)p.runs * 2 * FEW * (8 + (c.head_dim <= 64 ? 64 : 128) * 4);
+  return p.parts ? plan_bytes(p) + (size_t)up(p.parts, 2) * 16 + (size_t)p.parts * (c.head_dim <= 64 ? 64 : 128) * 4 : 0;
 }
 
 hipError_t attention_paged(int dt, const CacheView& c, int heads, int64_t rows, int max_new, int64_t max_length, int window, float scale, const void* q, int64_t ldq,
