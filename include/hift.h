@@ -645,7 +645,8 @@ hift_status hift_kernel_cache_append(const hift_cache* cache, int64_t rows, cons
  * the other new ones are in the cache already (hift_kernel_cache_append) -- and, with window > 0, the last `window` of them.  heads: a multiple of kv_heads; query
  * head h reads key head h / (heads / kv_heads).  q, out: device, rows [heads * head_dim], ldq / ldo apart, the cache's type, 16-byte aligned, rows whole
  * 16-byte pieces apart; out may be q (ldo = ldq).  lse: device fp32 [rows, heads] or NULL: log2 of the sum of the exponentials of the scaled scores.
- * A row that sees nothing: out 0, lse -inf.  Sums and statistics are fp32; bf16 caches: unnormalised probabilities are rounded to bf16 for the
+ * A row that sees nothing: out 0, lse -inf.  What is in slots that hold no token, or on pages that are not there, does not matter; a value v of a token that is
+ * not finite makes numbers of its block of rows NaN, also of rows before the token.  Sums and statistics are fp32; bf16 caches: unnormalised probabilities are rounded to bf16 for the
  * product with v, as in hift_kernel_attention_fwd.  max_length: at least as many as any sequence has with its new tokens; it sets how the keys are split over
  * workgroups, and a longer sequence only takes longer.  workspace: device, 16-byte aligned, hift_kernel_attention_paged_bytes, NULL where that is 0; free
  * again once the call's work on the stream is done; calls that may run at the same time (two streams, two graphs) need one each.

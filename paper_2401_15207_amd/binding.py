@@ -493,9 +493,6 @@ def kernel_muon(opt: dict, master, grad, momentum, compute_copy=None, workspace=
     _check(lib.hift_kernel_muon(C.byref(o), n, arr, _ptr(ws), nb, st))
 
 
-_raw_stream = torch._C._cuda_getCurrentRawStream
-
-
 ROTARY_SCALING = {"plain": 0, "linear": 1, "base": 2, "parts": 3}
 ROTARY_LAYOUT = {"halves": 0, "pairs": 1}
 
@@ -528,7 +525,7 @@ def kernel_rotary(x, heads, head_dim, y, cos_sin, positions=None, seq=0, layout=
     at, (rows, wx), (ry, wy) = x.get_device(), x.shape, y.shape
     ldx = _rows_of("x", x)
     ldy = ldx if y is x else _rows_of("y", y, x.dtype, device=at)
-    st = _raw_stream(at) if stream is None else stream.cuda_stream
+    st = torch._C._cuda_getCurrentRawStream(at) if stream is None else stream.cuda_stream
     if wx < heads * head_dim or wy < heads * head_dim or ry != rows:
         raise ValueError(f"{rows} rows of {heads} heads of {head_dim} expected, not x {tuple(x.shape)} and y {tuple(y.shape)}")
     table, rot = _table_of("cos_sin", cos_sin, at)
@@ -539,7 +536,7 @@ def kernel_rotary(x, heads, head_dim, y, cos_sin, positions=None, seq=0, layout=
 class PagedCache:
     """A paged cache (hift_cache): k, v [pages there are, kv_heads, page, head_dim] (any distance between pages), pages [sequences, most pages of a sequence] and
     lengths [sequences], both int32.  For models, k and v have a first dimension more, the layers, and the kernels take layer 0.  Holds the tensors; what lengths
-    and pages say may change between calls."""
+    and pages say may change between calls, and other tensors may take their place."""
 
     def __init__(self, k, v, pages, lengths):
         at, self.layers, self.layer_stride = k.get_device(), 1, 0
@@ -551,19 +548,41 @@ class PagedCache:
         n, kv, page, hd = k.shape
         if n and not (k[0].is_contiguous() and v[0].is_contiguous()):
             raise ValueError("k, v: a page has to be contiguous")
-        if pages.dim() != 2 or pages.dtype is not torch.int32 or pages.get_device() != at or (pages.shape[1] > 1 and pages.stride(1) != 1):
-            raise ValueError(f"pages: int32 [sequences, pages] on cuda:{at} expected, not {tuple(pages.shape)} of {pages.dtype} on {pages.device}")
-        _row_values("lengths", lengths, pages.shape[0], at, torch.int32)
-        self.k, self.v, self.pages, self.lengths, self.device, self.dtype, self.head_dim, self.kv_heads = k, v, pages, lengths, at, k.dtype, hd, kv
-        most = pages.shape[1]
-        self.c = Cache(_dtype_code(k), kv, hd, page, n, pages.shape[0], most, max(k.stride(0), kv * page * hd) if n > 1 else kv * page * hd,
-                       max(pages.stride(0), most) if pages.shape[0] > 1 else most, k.data_ptr(), v.data_ptr(), pages.data_ptr(), lengths.data_ptr())
         if n > 1 and k.stride(0) < kv * page * hd:
             raise ValueError("k, v: pages overlap")
+        self.k, self.v, self.device, self.dtype, self.head_dim, self.kv_heads = k, v, at, k.dtype, hd, kv
+        self.c = Cache(_dtype_code(k), kv, hd, page, n, 0, 0, k.stride(0) if n > 1 else kv * page * hd, 0, k.data_ptr(), v.data_ptr(), None, None)
         self.ref = C.byref(self.c)
+        self.pages, self.lengths = pages, lengths
+
+    @property
+    def pages(self):
+        return self._pages
+
+    @pages.setter
+    def pages(self, pages):
+        if pages.dim() != 2 or pages.dtype is not torch.int32 or pages.get_device() != self.device or (pages.shape[1] > 1 and pages.stride(1) != 1):
+            raise ValueError(f"pages: int32 [sequences, pages] on cuda:{self.device} expected, not {tuple(pages.shape)} of {pages.dtype} on {pages.device}")
+        rows, most = pages.shape
+        if rows > 1 and pages.stride(0) < most:
+            raise ValueError("pages: rows overlap")
+        c = self.c
+        c.sequences, c.max_pages, c.pages_ld, c.pages = rows, most, pages.stride(0) if rows > 1 else most, pages.data_ptr()
+        self._pages = pages
+
+    @property
+    def lengths(self):
+        return self._lengths
+
+    @lengths.setter
+    def lengths(self, lengths):
+        self.c.lengths = _row_values("lengths", lengths, self.c.sequences, self.device, torch.int32)
+        self._lengths = lengths
 
 
 def _starts_of(cache, starts):
+    if cache._lengths.numel() != cache.c.sequences:
+        raise ValueError(f"lengths: {cache.c.sequences} expected, as many as pages has rows, not {cache._lengths.numel()}")
     return _row_values("starts", starts, cache.c.sequences + 1, cache.device, torch.int32)
 
 
@@ -572,7 +591,7 @@ def kernel_cache_append(cache, starts, qkv, heads, q_out=None, cos_sin=None, lay
     rows of a sequence (None: all of them)."""
     at, (rows, width) = cache.device, qkv.shape
     ld = _rows_of("qkv", qkv, cache.dtype, device=at)
-    st = _raw_stream(at) if stream is None else stream.cuda_stream
+    st = torch._C._cuda_getCurrentRawStream(at) if stream is None else stream.cuda_stream
     need = (heads + 2 * cache.kv_heads) * cache.head_dim
     if width < need:
         raise ValueError(f"qkv: rows of {need} expected, not {width}")
@@ -597,7 +616,7 @@ def kernel_attention_paged(cache, starts, q, heads, out, max_new, max_length, wi
     max_length: most tokens of one, new ones included; scale: None for 1 / sqrt(head_dim); lse: float32 [rows, heads] or None."""
     at, hd, (rows, wq), (ro, wo) = cache.device, cache.head_dim, q.shape, out.shape
     ldq, ldo = _rows_of("q", q, cache.dtype, device=at), _rows_of("out", out, cache.dtype, device=at)
-    st = _raw_stream(at) if stream is None else stream.cuda_stream
+    st = torch._C._cuda_getCurrentRawStream(at) if stream is None else stream.cuda_stream
     if wq < heads * hd or wo < heads * hd or ro != rows:
         raise ValueError(f"q, out: [{rows}, {heads * hd}] expected, not {tuple(q.shape)} and {tuple(out.shape)}")
     if workspace is None:
@@ -634,7 +653,7 @@ def kernel_adjust_logits(logits, vocab, out, tokens=None, begin=None, end=None, 
     at, (rows, width), (ro, wo) = logits.get_device(), logits.shape, out.shape
     ld = _rows_of("logits", logits)
     ldo = ld if out is logits else _rows_of("out", out, logits.dtype, device=at)
-    st = _raw_stream(at) if stream is None else stream.cuda_stream
+    st = torch._C._cuda_getCurrentRawStream(at) if stream is None else stream.cuda_stream
     if vocab > width or vocab > wo or ro != rows:
         raise ValueError(f"vocab {vocab}, but logits are {tuple(logits.shape)} and out {tuple(out.shape)}")
     by = _adjust_of(rows, vocab, at, tokens, begin, end, repetition, presence, frequency, bias, allowed)
@@ -648,7 +667,7 @@ def kernel_adjust_logits_bwd(logits, vocab, d_out, d_logits, tokens=None, begin=
     ld, ldg, ldd = _rows_of("logits", logits), _rows_of("d_out", d_out, logits.dtype, device=at), _rows_of("d_logits", d_logits, logits.dtype, device=at)
     if min(width, d_out.shape[1], d_logits.shape[1]) < vocab or d_out.shape[0] != rows or d_logits.shape[0] != rows:
         raise ValueError(f"vocab {vocab}, but logits are {tuple(logits.shape)}, d_out {tuple(d_out.shape)} and d_logits {tuple(d_logits.shape)}")
-    st = _raw_stream(at) if stream is None else stream.cuda_stream
+    st = torch._C._cuda_getCurrentRawStream(at) if stream is None else stream.cuda_stream
     by = _adjust_of(rows, vocab, at, tokens, begin, end, repetition, presence, frequency, bias, allowed)
     _check(lib.hift_kernel_adjust_logits_bwd(_dtype_code(logits), rows, vocab, ld, logits.data_ptr(), C.byref(by), ldg, d_out.data_ptr(), ldd, d_logits.data_ptr(), st))
 

@@ -2905,7 +2905,7 @@ hift_status cache_view(const hift_cache* c, int64_t rows, const int32_t* starts,
 hift_status check_adjust(int32_t dtype, int64_t rows, int32_t V, int64_t ld, const void* logits, const hift_adjust* by, AdjustBy* out) {
   ST_TRY(check_logits(dtype, rows, V, ld, logits, 1.f));
   if (!by) return fail(HIFT_EINVAL, "by is null");
-  if (rows * ((V + 8191) / 8192) > INT32_MAX) return fail(HIFT_EINVAL, "%lld rows of %d entries are too many for one call", (long long)rows, V);
+  if (rows * ((V + 4095) / 4096) > INT32_MAX) return fail(HIFT_EINVAL, "%lld rows of %d entries are too many for one call", (long long)rows, V);
   if (!(by->repetition >= 0x1p-60f && by->repetition <= 0x1p60f)) return fail(HIFT_EINVAL, "repetition must be in [2^-60, 2^60]");
   if (!std::isfinite(by->presence) || !std::isfinite(by->frequency)) return fail(HIFT_EINVAL, "presence and frequency must be finite");
   if (by->n_tokens < 0 || (by->tokens && (!by->begin || !by->end))) return fail(HIFT_EINVAL, "tokens need begin and end, and a count");

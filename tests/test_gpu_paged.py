@@ -94,8 +94,13 @@ MANY = [([(0, 128)], 2, 2, 128, 16), ([(0, 33)], 1, 1, 64, 16), ([(77, 200)], 4,
         ([(1, 64)], 8, 1, 80, 64), ([(1000, 300)], 2, 1, 128, 128), ([(5, 40), (6, 40)], 3, 1, 16, 16)]
 
 
+# enough blocks of 32 rows for the kernel of many rows (over 128 of them in bf16, over 512 in fp32), keys split over workgroups or not, short sequences among long ones
+MIXED = [([(0, 200), (30, 1), (700, 130), (5, 0)], 16, 16, 64, 16), ([(2000, 150), (3, 140)], 16, 16, 128, 32), ([(1500, 300)], 64, 16, 96, 64),
+         ([(900, 300), (5, 2)], 64, 32, 32, 64), ([(10, 40)] * 9 + [(2100, 1)], 64, 32, 16, 16), ([(0, 257)] * 3, 24, 8, 80, 128)]
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
-@pytest.mark.parametrize("case", FEW + MANY)
+@pytest.mark.parametrize("case", FEW + MANY + MIXED)
 @pytest.mark.parametrize("window", [0, 1, 50])
 def test_attention(dtype, case, window):
     m = Made(*case, dtype, seed=len(case[0]) + case[3], more_rows=2)
@@ -124,9 +129,19 @@ def test_a_chunk_over_a_long_cache_in_parts(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
-@pytest.mark.parametrize("tokens", [[(100, 1), (60, 2)], [(100, 60), (20, 1)]])
-def test_pages_that_are_not_there(dtype, tokens):
-    m = Made(tokens, 4, 2, 64, 16, dtype)
+def test_bounds_that_are_too_low_or_too_high(dtype):
+    """max_length sets how the work is cut up and nothing else: eight wavefronts or four, runs, parts."""
+    for tokens, heads, kv in [([(3000, 1)], 8, 8), ([(3000, 150), (0, 33)], 32, 32)]:
+        m = Made(tokens, heads, kv, 64, 16, dtype)
+        for bound in (0, 300, 900, 1200, 4000, 2 ** 40):
+            out, lse = m.attend(max_length=bound)
+            m.check(out, lse)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("tokens,heads", [([(100, 1), (60, 2)], 4), ([(100, 60), (20, 1)], 4), ([(100, 60), (1000, 60)], 256)])
+def test_pages_that_are_not_there(dtype, tokens, heads):
+    m = Made(tokens, heads, max(2, heads // 2), 64, 16, dtype)
     gone = [(0, 0), (0, 3), (1, 1)]
     m.pages[0, 0], m.pages[0, 3], m.pages[1, 1] = -1, m.k.shape[0], 2 ** 31 - 1
     out, lse = m.attend()
@@ -134,7 +149,7 @@ def test_pages_that_are_not_there(dtype, tokens):
     # nothing left at all: zeros, and -inf
     m.pages.fill_(-5)
     out, lse = m.attend()
-    m.check(out, lse, gone=[(s, i) for s in range(2) for i in range(12)])
+    m.check(out, lse, gone=[(s, i) for s in range(2) for i in range(80)])
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
