@@ -2865,6 +2865,8 @@ hift_status hift_kernel_muon(const hift_opt* opt, int32_t count, const hift_muon
 namespace {
 int64_t size_of(int32_t dtype) { return dtype == HIFT_BF16 ? 2 : 4; }
 bool pieces16(const void* p, int64_t ld, int64_t es) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld * es % 16 == 0; }
+// Whether the rows of two matrices that begin at one place do not lie on each other; a single row has no distance to the next.
+bool rows_differ(const void* a, int64_t lda, const void* b, int64_t ldb, int64_t rows) { return a == b && lda != ldb && rows > 1; }
 
 hift_status check_table(int32_t layout, int32_t rot, int32_t head_dim, const float* cos_sin, int64_t table_rows) {
   if (layout != HIFT_ROTARY_HALVES && layout != HIFT_ROTARY_PAIRS) return fail(HIFT_EINVAL, "layout unknown");
@@ -2959,7 +2961,7 @@ hift_status hift_kernel_rotary(int32_t dtype, int32_t layout, int32_t backward, 
   if (rows > 0 && heads > 0 && (!x || !y)) return fail(HIFT_EINVAL, "x or y null");
   if ((reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(y)) % (uintptr_t)size_of(dtype) || reinterpret_cast<uintptr_t>(positions) % 4)
     return fail(HIFT_EINVAL, "x, y or positions do not lie on whole elements");
-  if (x == y && ldx != ldy) return fail(HIFT_EINVAL, "in place the rows lie where they were (ldy = ldx)");
+  if (rows_differ(x, ldx, y, ldy, rows)) return fail(HIFT_EINVAL, "in place the rows lie where they were (ldy = ldx)");
   HIP_TRY(rotary(dtype == HIFT_BF16 ? DT_BF16 : DT_F32, layout == HIFT_ROTARY_PAIRS, backward != 0, rows, heads, head_dim, rot, x, ldx, y, ldy, positions, seq, cos_sin,
                  (int)table_rows, (hipStream_t)stream));
   return HIFT_OK;
@@ -2974,8 +2976,8 @@ hift_status hift_kernel_cache_append(const hift_cache* cache, int64_t rows, cons
   if (ld < width || (q_out && ldq < (int64_t)heads * c.head_dim)) return fail(HIFT_EINVAL, "a leading dimension is shorter than the rows it strides over");
   if (rows == 0 || c.sequences == 0 || max_new == 0) return HIFT_OK;
   if (!starts || !qkv) return fail(HIFT_EINVAL, "starts or qkv null");
-  if (!pieces16(qkv, ld, es) || (q_out && !pieces16(q_out, ldq, es))) return fail(HIFT_EINVAL, "qkv and q_out must be 16-byte aligned, their rows whole 16-byte pieces apart");
-  if (q_out == qkv && ldq != ld) return fail(HIFT_EINVAL, "in place the rows lie where they were (ldq = ld)");
+  if (!pieces16(qkv, rows > 1 ? ld : 0, es) || (q_out && !pieces16(q_out, rows > 1 ? ldq : 0, es))) return fail(HIFT_EINVAL, "qkv and q_out must be 16-byte aligned, their rows whole 16-byte pieces apart");
+  if (rows_differ(q_out, ldq, qkv, ld, rows)) return fail(HIFT_EINVAL, "in place the rows lie where they were (ldq = ld)");
   HIP_TRY(cache_append(cache->dtype == HIFT_BF16 ? DT_BF16 : DT_F32, c, heads, layout == HIFT_ROTARY_PAIRS, rot, cos_sin, (int)table_rows, rows,
                        (int)std::min<int64_t>(max_new, rows), qkv, ld, q_out, ldq, (hipStream_t)stream));
   return HIFT_OK;
@@ -3002,8 +3004,8 @@ hift_status hift_kernel_attention_paged(const hift_cache* cache, int64_t rows, c
   if (ldq < width || ldo < width) return fail(HIFT_EINVAL, "a leading dimension is shorter than the rows it strides over");
   if (rows == 0 || c.sequences == 0 || max_new == 0) return HIFT_OK;
   if (!starts || !q || !out) return fail(HIFT_EINVAL, "starts, q or out null");
-  if (!pieces16(q, ldq, es) || !pieces16(out, ldo, es)) return fail(HIFT_EINVAL, "q and out must be 16-byte aligned, their rows whole 16-byte pieces apart");
-  if (q == out && ldq != ldo) return fail(HIFT_EINVAL, "in place the rows lie where they were (ldo = ldq)");
+  if (!pieces16(q, rows > 1 ? ldq : 0, es) || !pieces16(out, rows > 1 ? ldo : 0, es)) return fail(HIFT_EINVAL, "q and out must be 16-byte aligned, their rows whole 16-byte pieces apart");
+  if (rows_differ(q, ldq, out, ldo, rows)) return fail(HIFT_EINVAL, "in place the rows lie where they were (ldo = ldq)");
   if (reinterpret_cast<uintptr_t>(lse) % 4) return fail(HIFT_EINVAL, "lse does not lie on whole elements");
   if (need > 0 && (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 15)))
     return fail(HIFT_EINVAL, "workspace of %zu bytes, 16-byte aligned, expected", need);
@@ -3019,7 +3021,7 @@ hift_status hift_kernel_adjust_logits(int32_t dtype, int64_t rows, int32_t V, in
   if (ldo < V) return fail(HIFT_EINVAL, "rows of out are %lld apart and %d long", (long long)ldo, V);
   if (rows > 0 && !out) return fail(HIFT_EINVAL, "out is null");
   if (reinterpret_cast<uintptr_t>(out) % (uintptr_t)size_of(dtype)) return fail(HIFT_EINVAL, "out does not lie on whole elements");
-  if (out == logits && ldo != ld) return fail(HIFT_EINVAL, "in place the rows lie where they were (ldo = ld)");
+  if (rows_differ(out, ldo, logits, ld, rows)) return fail(HIFT_EINVAL, "in place the rows lie where they were (ldo = ld)");
   HIP_TRY(adjust_logits(dtype == HIFT_BF16 ? DT_BF16 : DT_F32, false, rows, V, ld, logits, a, 0, nullptr, ldo, out, (hipStream_t)stream));
   return HIFT_OK;
 }
@@ -3033,7 +3035,7 @@ hift_status hift_kernel_adjust_logits_bwd(int32_t dtype, int64_t rows, int32_t V
   if ((reinterpret_cast<uintptr_t>(d_out) | reinterpret_cast<uintptr_t>(d_logits)) % (uintptr_t)size_of(dtype))
     return fail(HIFT_EINVAL, "the gradients do not lie on whole elements");
   if (rows > 0 && d_logits == logits) return fail(HIFT_EINVAL, "the gradient may not take the logits' place");
-  if (d_logits == d_out && ldd != ldd_out) return fail(HIFT_EINVAL, "in place the rows lie where they were (ldd = ldd_out)");
+  if (rows_differ(d_logits, ldd, d_out, ldd_out, rows)) return fail(HIFT_EINVAL, "in place the rows lie where they were (ldd = ldd_out)");
   HIP_TRY(adjust_logits(dtype == HIFT_BF16 ? DT_BF16 : DT_F32, true, rows, V, ld, logits, a, ldd_out, d_out, ldd, d_logits, (hipStream_t)stream));
   return HIFT_OK;
 }

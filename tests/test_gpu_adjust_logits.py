@@ -220,3 +220,16 @@ def test_replayed_from_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, want)
+
+
+def test_one_row_in_place_by_views_of_other_widths():
+    """A single row has no distance to the next."""
+    x = torch.randn(1, 300, generator=torch.Generator().manual_seed(3)).cuda()
+    tokens, begin, end = torch.tensor([5, 7, 7], device="cuda", dtype=torch.int32), torch.zeros(1, device="cuda", dtype=torch.int64), torch.full((1,), 3, device="cuda", dtype=torch.int64)
+    by = dict(tokens=tokens, begin=begin, end=end, repetition=2.0)
+    want, grad, d = torch.empty(1, 290, device="cuda"), torch.empty(1, 290, device="cuda"), torch.randn(1, 300, generator=torch.Generator().manual_seed(4)).cuda()
+    H.kernel_adjust_logits(x, 290, want, frequency=0.5, **by)
+    H.kernel_adjust_logits_bwd(x, 290, d, grad, **by)
+    H.kernel_adjust_logits_bwd(x, 290, d, d[:, :290], **by)
+    H.kernel_adjust_logits(x, 290, x[:, :290], frequency=0.5, **by)
+    assert torch.equal(x[:, :290], want) and torch.equal(d[:, :290], grad)

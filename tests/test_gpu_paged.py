@@ -365,3 +365,60 @@ def test_replayed_from_a_graph_while_answers_grow():
         torch.cuda.synchronize()
         assert torch.equal(out, want) and torch.equal(q, q2)
     assert m.lengths.tolist() == [35, 105, 5]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_one_row_in_place_by_views_of_other_widths(dtype):
+    """A single row has no distance to the next: its views of different widths are in place all the same, and its width need not be whole pieces."""
+    m = Made([(40, 1)], 4, 2, 64, 16, dtype)
+    qkv = torch.randn(1, 8 * 64 + 3, generator=torch.Generator().manual_seed(5)).to("cuda", m.dtype)
+    cs, q, at = table(64, 64), torch.empty(1, 256, device="cuda", dtype=m.dtype), torch.tensor([40], device="cuda", dtype=torch.int32)
+    H.kernel_cache_append(m.cache, m.starts, qkv, 4, q, cs)
+    want, turned_q = torch.empty_like(q), qkv.clone()
+    H.kernel_rotary(turned_q, 4, 64, turned_q[:, :256], cs, positions=at)
+    assert torch.equal(turned_q[:, :256], q) and torch.equal(turned_q[:, 256:], qkv[:, 256:])
+    H.kernel_cache_append(m.cache, m.starts, qkv, 4, qkv[:, :256], cs)
+    assert torch.equal(qkv[:, :256], q)
+    H.kernel_attention_paged(m.cache, m.starts, q, 4, want, 1, 41)
+    H.kernel_attention_paged(m.cache, m.starts, qkv, 4, qkv[:, :256], 1, 41)
+    assert torch.equal(qkv[:, :256], want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("new", [1, 300])
+def test_pages_beyond_32_bits(dtype, new):
+    """Pages 2^30 + 64 elements apart: the last one's bytes, and with five its elements too, lie beyond 2^32."""
+    heads, kv, hd, page, cached = 32, 16, 64, 512, 700
+    pool = torch.empty(2, 4 * (2 ** 30 + 64) + kv * page * hd, device="cuda", dtype=DT[dtype])
+    k, v = (x.as_strided((5, kv, page, hd), (2 ** 30 + 64, page * hd, hd, 1), x.storage_offset()) for x in pool)
+    g = torch.Generator(device="cuda").manual_seed(6)
+    for x in (k, v):
+        for n in range(5):
+            x[n].normal_(generator=g)
+    order = torch.tensor([[4, 1, 3]], device="cuda", dtype=torch.int32)
+    near = [torch.stack([x[n] for n in (4, 1, 3)]) for x in (k, v)]
+    q = torch.randn(new, (heads + 2 * kv) * hd, device="cuda", generator=g).to(DT[dtype])
+    starts, lengths = torch.tensor([0, new], device="cuda", dtype=torch.int32), torch.tensor([cached], device="cuda", dtype=torch.int32)
+    outs = []
+    for kk, vv, pages in ((k, v, order), (*near, torch.tensor([[0, 1, 2]], device="cuda", dtype=torch.int32))):
+        cache, out = H.PagedCache(kk, vv, pages, lengths), torch.empty(new, heads * hd, device="cuda", dtype=DT[dtype])
+        H.kernel_cache_append(cache, starts, q, heads)
+        H.kernel_attention_paged(cache, starts, q[:, :heads * hd], heads, out, new, cached + new)
+        outs.append(out)
+    assert not outs[0].isnan().any() and torch.equal(outs[0], outs[1])
+    for x, y in zip((k, v), near):
+        assert all(torch.equal(x[n], y[i]) for i, n in enumerate((4, 1, 3)))
+
+
+def test_two_calls_at_once():
+    """Two streams with a cache each, keys of both split over workgroups: each has a workspace of its own, and the results are those of the calls alone."""
+    made = [Made([(3000, 1), (100, 2)], 8, 2, 128, 16, "bf16", seed=8), Made([(2500, 150)], 16, 16, 64, 32, "bf16", seed=9)]
+    want = [m.attend()[0] for m in made]
+    streams, outs = [torch.cuda.Stream() for _ in made], [[torch.empty_like(w) for _ in range(8)] for w in want]
+    torch.cuda.synchronize()
+    for i in range(8):
+        for m, st, out in zip(made, streams, outs):
+            H.kernel_attention_paged(m.cache, m.starts, m.q, m.heads, out[i], m.max_new, m.max_length, stream=st)
+    torch.cuda.synchronize()
+    for w, out in zip(want, outs):
+        assert all(torch.equal(o, w) for o in out)
