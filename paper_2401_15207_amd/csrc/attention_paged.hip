@@ -84,18 +84,21 @@ struct Tile {
   int head_at, slots, row_bytes;  // the head's first key within a page; slots of a page less one; bytes of a key
   __device__ __forceinline__ Tile(const CacheView& c, int kv_head)
       : page_bytes(c.page_stride * (int64_t)sizeof(T)), head_at(kv_head * c.page), slots(c.page - 1), row_bytes(c.head_dim * (int)sizeof(T)) {}
+  // PAST: keys that no other workgroup reads leave the caches first.
+  template <bool PAST = false>
   __device__ __forceinline__ void request(const void* array, int key0, int page, int end, const uint32_t (&vo)[IPG], uint32_t lds) const {
     const uint64_t a = reinterpret_cast<uint64_t>(array) + (uint64_t)((int64_t)max(page, 0) * page_bytes + (int64_t)(head_at + (key0 & slots)) * row_bytes);
     const int n = page < 0 ? 0 : min(max(end - key0, 0), GROUP);
     const hift_u32x4 rs = {(uint32_t)UNIFORM((int)(uint32_t)a), (uint32_t)UNIFORM((int)((uint32_t)(a >> 32) & 0xFFFFu)),
                            (uint32_t)UNIFORM(n * row_bytes), 0x00020000u};
 #pragma unroll
-    for (int i = 0; i < IPG; ++i) load_to_lds_b128(rs, lds + i * 1024, vo[i], 0);
+    for (int i = 0; i < IPG; ++i) load_to_lds_b128<PAST>(rs, lds + i * 1024, vo[i], 0);
   }
   // 32 keys, on one page or two
+  template <bool PAST>
   __device__ __forceinline__ void request(const void* array, int key0, int pa, int pb, int end, const uint32_t (&vo)[IPG], uint32_t lds) const {
-    request(array, key0, pa, end, vo, lds);
-    request(array, key0 + GROUP, pb, end, vo, lds + GROUP * ROWB);
+    request<PAST>(array, key0, pa, end, vo, lds);
+    request<PAST>(array, key0 + GROUP, pb, end, vo, lds + GROUP * ROWB);
   }
   __device__ static __forceinline__ void offsets(uint32_t (&vo)[IPG], int lane, int head_dim) {
 #pragma unroll
@@ -289,7 +292,7 @@ struct Entry {
 };
 
 // Steps [step0, step1) of an entry's key head, by W wavefronts.  shared: -1 where these are all its steps, otherwise the place [..][FEW] its results go to.
-template <typename T, int HD, int NB_, int W>
+template <typename T, int HD, int NB_, int W, bool PAST>
 __device__ __forceinline__ void few_rows(const Args& p, const Entry& en, int s, int kv_head, int step0, int step1, int64_t shared, unsigned char* lds, float2 (*ml)[FEW]) {
   typedef Tile<T, HD, NB_> L;
   constexpr int NB = L::NB, IPB = 2 * L::IPG;  // loads of a block of keys
@@ -315,8 +318,8 @@ __device__ __forceinline__ void few_rows(const Args& p, const Entry& en, int s, 
     const int g = wave * (KB / GROUP);
     pa = __builtin_amdgcn_readlane(pages, g);
     pb = __builtin_amdgcn_readlane(pages, g + 1);
-    head.request(p.c.k, key0, pa, pb, to, vo, lk);
-    head.request(p.c.v, key0, pa, pb, to, vo, lv);
+    head.template request<PAST>(p.c.k, key0, pa, pb, to, vo, lk);
+    head.template request<PAST>(p.c.v, key0, pa, pb, to, vo, lv);
   }
   Running<NB> run;
   // the compiler waits for the rows here, once, and not in the loop, where it would wait for everything on its way
@@ -336,7 +339,7 @@ __device__ __forceinline__ void few_rows(const Args& p, const Entry& en, int s, 
     f32x16 sc[1];
     sc[0] = L::scores(Kb, ad, q);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    if (more) head.request(p.c.k, next, na, nb, to, vo, lk);
+    if (more) head.template request<PAST>(p.c.k, next, na, nb, to, vo, lk);
     const bool plain = (pa | pb) >= 0 && key0 + KB <= to && key0 + KB - 1 <= pos_lo && (p.window == 0 || key0 > pos_hi - p.window);
     if (!plain) mask_scores<L>(sc[0], key0, fh, to, at.pos, en.of.total, p.window, pa >= 0, pb >= 0);
     run.take(sc, p.scale_log2e);
@@ -344,7 +347,7 @@ __device__ __forceinline__ void few_rows(const Args& p, const Entry& en, int s, 
     else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     L::values(run.o, Vb, ad, sc[0], lane);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    if (more) head.request(p.c.v, next, na, nb, to, vo, lv);
+    if (more) head.template request<PAST>(p.c.v, next, na, nb, to, vo, lv);
     pa = na; pb = nb;
   }
   run.l += __shfl_xor(run.l, 32, 64);
@@ -387,23 +390,23 @@ __device__ __forceinline__ void few_rows(const Args& p, const Entry& en, int s, 
 }
 
 // One workgroup a block of rows and key head
-template <typename T, int HD, int NB, int W>
+template <typename T, int HD, int NB, int W, bool PAST>
 __device__ __forceinline__ void few_whole(const Args& p, int i, unsigned char* lds, float2 (*ml)[FEW]) {
   const int pair = i / p.few_blocks, block = p.few_blocks - 1 - i % p.few_blocks, s = pair / p.c.kv_heads;
   const Entry en(p, s, block);
-  if (en.steps > 0) few_rows<T, HD, NB, W>(p, en, s, pair % p.c.kv_heads, 0, en.steps, -1, lds, ml);
+  if (en.steps > 0) few_rows<T, HD, NB, W, PAST>(p, en, s, pair % p.c.kv_heads, 0, en.steps, -1, lds, ml);
 }
-template <typename T, int HD, int NB, int W>
+template <typename T, int HD, int NB, int W, bool PAST>
 __global__ void __launch_bounds__(64 * W) few_whole_k(Args p) {
   extern __shared__ unsigned char lds[];  // [wave][K | V] blocks; at the end of a block of rows [wave][row][HD] sums
   __shared__ float2 ml[W][FEW];
-  few_whole<T, HD, NB, W>(p, (int)blockIdx.x, lds, ml);
+  few_whole<T, HD, NB, W, PAST>(p, (int)blockIdx.x, lds, ml);
 }
 
 // Equal runs of steps: run w is [w all / runs, (w + 1) all / runs), rounded down, with no more runs than steps, so that none is empty.
 __device__ __forceinline__ int64_t run_start(int w, int64_t all, int runs) { return w * all / runs; }
 __device__ __forceinline__ int run_of(int64_t step, int64_t all, int runs) { return (int)(((step + 1) * runs - 1) / all); }
-template <typename T, int HD, int NB>
+template <typename T, int HD, int NB, bool PAST>
 __global__ void __launch_bounds__(256) few_k(Args p) {
   extern __shared__ unsigned char lds[];
   __shared__ float2 ml[4][FEW];
@@ -453,7 +456,7 @@ __global__ void __launch_bounds__(256) few_k(Args p) {
       const int in = UNIFORM((int)(at - first)), kv_head = UNIFORM(in / en.steps), step0 = in - kv_head * UNIFORM(en.steps);
       const int n = UNIFORM((int)min((int64_t)(en.steps - step0), at1 - at));
       const bool whole = n == en.steps;
-      few_rows<T, HD, NB, 4>(p, en, s, kv_head, step0, step0 + n, whole ? -1 : ((int64_t)blockIdx.x * 2 + (step0 == 0)) * FEW, lds, ml);
+      few_rows<T, HD, NB, 4, PAST>(p, en, s, kv_head, step0, step0 + n, whole ? -1 : ((int64_t)blockIdx.x * 2 + (step0 == 0)) * FEW, lds, ml);
       __syncthreads();  // the next block's keys go where the sums were
       at += n;
     }
@@ -776,7 +779,7 @@ __device__ __forceinline__ void many_rows_bf16(const Args& p, const int index, u
 template <typename T, int HD, int NB>
 __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) mixed_k(Args p) {
   extern __shared__ unsigned char lds[];
-  if ((int)blockIdx.x < p.few_first) few_whole<T, HD, NB, 4>(p, (int)blockIdx.x, lds, reinterpret_cast<float2(*)[FEW]>(lds + 4 * 2 * KB * HD * sizeof(T)));
+  if ((int)blockIdx.x < p.few_first) few_whole<T, HD, NB, 4, false>(p, (int)blockIdx.x, lds, reinterpret_cast<float2(*)[FEW]>(lds + 4 * 2 * KB * HD * sizeof(T)));
   else if constexpr (sizeof(T) == 2) many_rows_bf16<HD, NB>(p, (int)blockIdx.x - p.few_first, lds);
   else many_rows_f32<HD, NB>(p, (int)blockIdx.x - p.few_first, lds);
 }
@@ -881,7 +884,7 @@ __global__ void __launch_bounds__(256) join_k(Args p, int tokens) {
 
 // ---- host ----
 struct Plan {
-  bool many;
+  bool many, past;
   int few_blocks, few_upto, few_first, many_blocks, split, chunk, runs, waves;
   int64_t entries, parts;  // rows of partial sums
 };
@@ -917,6 +920,10 @@ Plan plan_of(int dt, const CacheView& c, int64_t rows, int heads, int max_new, i
     return p;
   }
   if (window > 0) span = std::min<int64_t>(span, (int64_t)window + FEW + KB);
+  // Keys that one workgroup alone reads, of more than the eight L2s hold, go past them.  One token a sequence, us, with / without, each call on another cache of the
+  // size as a model's layers are: 8 over 4000, 32 / 8 heads 35.8 / 39.6; 8 over 1000, 32 / 32 23.8 / 26.7; 64 over 2000, 32 / 8 97 / 108; smaller ones that a call
+  // before has left in the L2s: 8 over 500, 32 / 8 9.2 / 8.5; several blocks of rows on the same keys: 1, 128 over 8000, 2 / 2 34.9 / 33.0.
+  p.past = p.few_blocks == 1 && (int64_t)c.sequences * span * c.kv_heads * 2 * c.head_dim * (dt == DT_BF16 ? 2 : 4) >= int64_t(1) << 25;
   const int64_t items = pairs * p.few_blocks;
   p.waves = items <= 256 && row_bytes <= 256 && span > STEP ? 8 : 4;
   if (span > (items >= resident ? 8 : p.waves) * STEP) {
@@ -938,6 +945,21 @@ hipError_t allow_lds() {
   return e;
 }
 
+template <typename T, int HD, int NB, bool PAST>
+hipError_t whole(int waves, dim3 g, const Args& a, hipStream_t st) {
+  constexpr int FOUR = 4 * 2 * KB * HD * (int)sizeof(T);
+  if constexpr (2 * FOUR <= 131072) {
+    if (waves == 8) {
+      if (hipError_t e = allow_lds<few_whole_k<T, HD, NB, 8, PAST>, 2 * FOUR>()) return e;
+      few_whole_k<T, HD, NB, 8, PAST><<<g, 512, 2 * FOUR, st>>>(a);
+      return hipSuccess;
+    }
+  }
+  if (hipError_t e = allow_lds<few_whole_k<T, HD, NB, 4, PAST>, FOUR>()) return e;
+  few_whole_k<T, HD, NB, 4, PAST><<<g, 256, FOUR, st>>>(a);
+  return hipSuccess;
+}
+
 template <typename T, int HD, int NB>
 hipError_t launch(const Plan& pl, Args a, int max_new, void* workspace, hipStream_t st) {
   a.few_upto = pl.few_upto; a.few_blocks = pl.few_blocks; a.many_blocks = pl.many_blocks; a.runs = pl.runs; a.few_first = pl.few_first; a.split = pl.split; a.chunk = pl.chunk;
@@ -957,18 +979,19 @@ hipError_t launch(const Plan& pl, Args a, int max_new, void* workspace, hipStrea
     if (pl.split > 4) join_k<T, HD, false, 4><<<(unsigned)rows, 256, 0, st>>>(a, max_new);
     else if (pl.split > 1) join_k<T, HD, false, 1><<<(unsigned)up(rows, 4), 256, 0, st>>>(a, max_new);
   } else if (pl.runs) {
-    if (hipError_t e = allow_lds<few_k<T, HD, NB>, FEW_LDS>()) return e;
-    few_k<T, HD, NB><<<g, 256, FEW_LDS, st>>>(a);
+    if (pl.past) {
+      if (hipError_t e = allow_lds<few_k<T, HD, NB, true>, FEW_LDS>()) return e;
+      few_k<T, HD, NB, true><<<g, 256, FEW_LDS, st>>>(a);
+    } else {
+      if (hipError_t e = allow_lds<few_k<T, HD, NB, false>, FEW_LDS>()) return e;
+      few_k<T, HD, NB, false><<<g, 256, FEW_LDS, st>>>(a);
+    }
     if (pl.runs > 4 * pairs * pl.few_blocks) join_k<T, HD, true, 4><<<(unsigned)rows, 256, 0, st>>>(a, max_new);  // more than four parts a row
     else join_k<T, HD, true, 1><<<(unsigned)up(rows, 4), 256, 0, st>>>(a, max_new);
-  } else if (pl.waves == 8) {
-    if constexpr (2 * FEW_LDS <= 131072) {
-      if (hipError_t e = allow_lds<few_whole_k<T, HD, NB, 8>, 2 * FEW_LDS>()) return e;
-      few_whole_k<T, HD, NB, 8><<<g, 512, 2 * FEW_LDS, st>>>(a);
-    }
+  } else if (pl.past) {
+    if (hipError_t e = whole<T, HD, NB, true>(pl.waves, g, a, st)) return e;
   } else {
-    if (hipError_t e = allow_lds<few_whole_k<T, HD, NB, 4>, FEW_LDS>()) return e;
-    few_whole_k<T, HD, NB, 4><<<g, 256, FEW_LDS, st>>>(a);
+    if (hipError_t e = whole<T, HD, NB, false>(pl.waves, g, a, st)) return e;
   }
   return hipGetLastError();
 }

@@ -64,11 +64,19 @@ typedef __attribute__((ext_vector_type(4))) uint32_t hift_u32x4;
 // lands 16 l bytes further.  Inline assembly, with hand-placed s_waitcnt where the data is read:
 // the compiler cannot see which LDS reads depend on which load and would otherwise wait for all
 // of them before every read.
+// PAST: what is read once and leaves the caches first.
+template <bool PAST = false>
 __device__ __forceinline__ void load_to_lds_b128(hift_u32x4 rsrc, uint32_t lds_addr, uint32_t voff, uint32_t soff) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
-               :
-               : "s"(lds_addr), "v"(voff), "s"(rsrc), "s"(soff)
-               : "memory");
+  if constexpr (PAST)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen nt lds"
+                 :
+                 : "s"(lds_addr), "v"(voff), "s"(rsrc), "s"(soff)
+                 : "memory");
+  else
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+                 :
+                 : "s"(lds_addr), "v"(voff), "s"(rsrc), "s"(soff)
+                 : "memory");
 }
 
 // x Phi(x) and its derivative Phi(x) + x phi(x)

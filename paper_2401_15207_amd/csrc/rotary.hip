@@ -78,6 +78,12 @@ template <typename T, int V>
 struct alignas(sizeof(T) * V) Elems {
   T v[V];
 };
+// The same of a row that nobody reads again: it leaves the caches first.
+template <typename T, int V>
+__device__ __forceinline__ Elems<T, V> last_read(const T* p) {
+  typedef T Wide __attribute__((ext_vector_type(V)));
+  return __builtin_bit_cast(Elems<T, V>, __builtin_nontemporal_load(reinterpret_cast<const Wide*>(p)));
+}
 
 // Written out, so that every variant gives the same bits.
 __device__ __forceinline__ float first_of(float x1, float x2, float2 t) { return fmaf(-x2, t.y, x1 * t.x); }
@@ -240,9 +246,9 @@ __global__ void __launch_bounds__(BLK) append_k(AppendArgs p) {
     const Unit<T, V> unit(u, p.half, PAIRS, p.cs + (int64_t)min(pos, p.table_rows - 1) * p.half, 1.f);
     const int from = p.q ? 0 : p.heads, to = page < 0 ? p.heads : p.heads + kv;
     for (int h = from + lane_head; h < to; h += per) {
-      E a = *reinterpret_cast<const E*>(x + (int64_t)h * hd + unit.a), b;
+      E a = last_read<T, V>(x + (int64_t)h * hd + unit.a), b;
       if (unit.turns) {
-        b = *reinterpret_cast<const E*>(x + (int64_t)h * hd + unit.b);
+        b = last_read<T, V>(x + (int64_t)h * hd + unit.b);
         unit.template turn<PAIRS>(a, b);
       }
       T* y = h < p.heads ? (T*)p.q + row * p.ldq + (int64_t)h * hd : (T*)p.c.k + slot + (h - p.heads) * head_at;
@@ -257,7 +263,7 @@ __global__ void __launch_bounds__(BLK) append_k(AppendArgs p) {
   const int pieces = hd / VV;
   for (int i = threadIdx.x; i < kv * pieces; i += BLK) {
     const int h = i / pieces, c = (i % pieces) * VV;
-    *reinterpret_cast<EV*>((T*)p.c.v + slot + h * head_at + c) = *reinterpret_cast<const EV*>(v + (int64_t)h * hd + c);
+    *reinterpret_cast<EV*>((T*)p.c.v + slot + h * head_at + c) = last_read<T, VV>(v + (int64_t)h * hd + c);
   }
 }
 
