@@ -9,8 +9,12 @@
 //   few_k    32 rows a workgroup: all four wavefronts hold the same rows and take turns at the blocks of 32 keys, each through LDS tiles of its own
 //            without any barrier, and their results are joined at the end.  Bound by reading the cache.  Lengths are known on the device only, and
 //            differ: the keys of all sequences and heads, one after the other, are cut into equal runs, a workgroup each, wherever that falls.
-//   mixed_k  128 rows a workgroup, 32 a wavefront, which share tiles of 64 keys; bound by the matrix instructions.  Its first workgroups take the
-//            sequences of few rows.
+//            A token each of 64 sequences of up to 8000, 32 / 8 heads of 128 bf16 (1.04 GB): 189 us with its join, 5.5 TB/s (a workgroup a sequence and head 253).
+//   few_whole_k  the same, one workgroup a block of rows and key head, where runs would be too short.  One token over 500, 32 / 32 heads: 8.4 us, the chain
+//            of its loads, products and joins.
+//   mixed_k  128 rows a workgroup, 32 a wavefront, which share tiles of 64 keys; bound by the matrix instructions and the LDS reads that feed them (bf16: 16 KB for
+//            16 instructions of 32 cycles, four wavefronts: 128 bytes a cycle, all that LDS gives).  Its first workgroups take the sequences of few rows.
+//            Chunks of 700 to 1024 of 4 sequences over up to 4096, 32 / 32 heads bf16: 187 us, 815 TFLOP/s (a large product on the card 1250); fp32, 1024 over none 158 us.
 //   join_k   rows whose keys fell to several workgroups: the parts, weighted by their maxima.
 #include <math.h>
 
@@ -574,7 +578,8 @@ __device__ __forceinline__ void many_rows_f32(const Args& p, const int index, un
 }
 
 // ---- many rows, bf16 ----
-// 128 rows a workgroup, 32 a wavefront, two workgroups a compute unit.  Within a wavefront the products of one block of 32 keys run beside the exponentials of
+// 128 rows a workgroup, 32 a wavefront, two workgroups a compute unit (chunks: 187 us; 256 rows in eight wavefronts the same; 64 rows a wavefront would halve the
+// LDS reads, but need more registers than there are: 663).  Within a wavefront the products of one block of 32 keys run beside the exponentials of
 // the one before:
 //   scores of block i (8 MFMAs)     beside the exponentials of block i - 1
 //   P V of block i - 1 (8 MFMAs)    beside the row maxima of block i
@@ -925,6 +930,9 @@ Plan plan_of(int dt, const CacheView& c, int64_t rows, int heads, int max_new, i
   // before has left in the L2s: 8 over 500, 32 / 8 9.2 / 8.5; several blocks of rows on the same keys: 1, 128 over 8000, 2 / 2 34.9 / 33.0.
   p.past = p.few_blocks == 1 && (int64_t)c.sequences * span * c.kv_heads * 2 * c.head_dim * (dt == DT_BF16 ? 2 : 4) >= int64_t(1) << 25;
   const int64_t items = pairs * p.few_blocks;
+  // Eight wavefronts a block of rows where there are no more blocks than compute units (one token, 32 / 32 heads, us, eight / four: 1 over 500 8.1 / 9.9, 1 over 1000
+  // 11.2 / 15.1, 8 over 1000 24.0 / 24.2, 32 over 500 47.2 / 42.2).  Runs cost a search for their begin and a second launch, which pays where the longest sequence is
+  // long (whole / runs: 1 over 800 9.8 / 11.1, 1 over 1000 11.2 / 11.2, 8 of one length 1000 24.0 / 33.5) -- sequences of one length apart, at 32 x 1500 140 / 152.
   p.waves = items <= 256 && row_bytes <= 256 && span > STEP ? 8 : 4;
   if (span > (items >= resident ? 8 : p.waves) * STEP) {
     p.waves = 4;
@@ -976,8 +984,7 @@ hipError_t launch(const Plan& pl, Args a, int max_new, void* workspace, hipStrea
   if (pl.many) {
     if (hipError_t e = allow_lds<mixed_k<T, HD, NB>, MIXED_LDS>()) return e;
     mixed_k<T, HD, NB><<<g, 256, MIXED_LDS, st>>>(a);
-    if (pl.split > 4) join_k<T, HD, false, 4><<<(unsigned)rows, 256, 0, st>>>(a, max_new);
-    else if (pl.split > 1) join_k<T, HD, false, 1><<<(unsigned)up(rows, 4), 256, 0, st>>>(a, max_new);
+    if (pl.split > 1) join_k<T, HD, false, 1><<<(unsigned)up(rows, 4), 256, 0, st>>>(a, max_new);
   } else if (pl.runs) {
     if (pl.past) {
       if (hipError_t e = allow_lds<few_k<T, HD, NB, true>, FEW_LDS>()) return e;
@@ -986,7 +993,10 @@ hipError_t launch(const Plan& pl, Args a, int max_new, void* workspace, hipStrea
       if (hipError_t e = allow_lds<few_k<T, HD, NB, false>, FEW_LDS>()) return e;
       few_k<T, HD, NB, false><<<g, 256, FEW_LDS, st>>>(a);
     }
-    if (pl.runs > 4 * pairs * pl.few_blocks) join_k<T, HD, true, 4><<<(unsigned)rows, 256, 0, st>>>(a, max_new);  // more than four parts a row
+    // Four wavefronts a row where it has more than four parts and one each would not fill the chip's 1024 SIMDs (us, four / one: 1, 1 over 16000, 8 / 1 heads 17.2 /
+    // 32.6; 1, 8 over 8000, 32 / 8 32.5 / 41.1; 1, 128 over 4000, 8 / 8 (1024 rows) 46.9 / 48.6; 4, 16 over 4000, 32 / 4 (2048) 40.5 / 38.1; of 4096 and more rows, in 5
+    // to 8 parts: 1, 256 over 8192, 32 / 8 64.9 / 55.8).
+    if (pl.runs > 4 * pairs * pl.few_blocks && rows <= 1024) join_k<T, HD, true, 4><<<(unsigned)rows, 256, 0, st>>>(a, max_new);
     else join_k<T, HD, true, 1><<<(unsigned)up(rows, 4), 256, 0, st>>>(a, max_new);
   } else if (pl.past) {
     if (hipError_t e = whole<T, HD, NB, true>(pl.waves, g, a, st)) return e;
