@@ -581,7 +581,7 @@ __device__ __forceinline__ void many_rows_f32(const Args& p, const int index, un
 // 128 rows a workgroup, 32 a wavefront, two workgroups a compute unit (chunks: 187 us; 256 rows in eight wavefronts the same; 64 rows a wavefront would halve the
 // LDS reads, but need more registers than there are: 663).  Within a wavefront the products of one block of 32 keys run beside the exponentials of
 // the one before:
-//   scores of block i (8 MFMAs)     beside the exponentials of block i - 1
+//   scores of block i (8 MFMAs)     in turn with the exponentials of block i - 1 (products first, then exponentials: 4096 over none, 16 / 2 heads 109 us, in turn 99)
 //   P V of block i - 1 (8 MFMAs)    beside the row maxima of block i
 
 // The sequence that has `rank` longer ones before it; with more than 256 of them, which fill the chip in any order, the rank-th.
@@ -670,13 +670,15 @@ __device__ __forceinline__ void many_rows_bf16(const Args& p, const int index, u
     for (int e = 0; e < 16; ++e) o[nb][e] = 0.f;
   bf16x8 pr[2];  // probabilities by half of the block
 
-  auto exponentials = [&](const f32x16& S, int h) __attribute__((always_inline)) {
+  // of elements [first, last) of a block
+  auto exponentials = [&](const f32x16& S, int first, int last) __attribute__((always_inline)) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(S[8 * h + e], p.scale_log2e, -ref));
-      l += x;
-      pr[h][e] = static_cast<__bf16>(x);
-    }
+    for (int e = 0; e < 16; ++e)
+      if (e >= first && e < last) {
+        const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(S[e], p.scale_log2e, -ref));
+        l += x;
+        pr[e >> 3][e & 7] = static_cast<__bf16>(x);
+      }
   };
   auto read_keys = [&](bf16x8 (&f)[NQ], const unsigned char* K) __attribute__((always_inline)) {
 #pragma unroll
@@ -722,26 +724,20 @@ __device__ __forceinline__ void many_rows_bf16(const Args& p, const int index, u
     read_values(v0, V, 0);
 #pragma unroll
     for (int e = 0; e < 16; ++e) now[e] = 0.f;
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int i = 0; i < NQ; ++i) now = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i], q[i], now, 0, 0, 0);
-    exponentials(last, 0);
-    exponentials(last, 1);
-    __builtin_amdgcn_sched_group_barrier(0x100, 2 * NB, 0);  // two exponentials after each MFMA
-#pragma unroll
-    for (int i = 0; i < NQ; ++i) {
-      __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x2, 5 * 8 / NQ, 0);
-      __builtin_amdgcn_sched_group_barrier(0x400, 2 * 8 / NQ, 0);
+    for (int i = 0; i < NQ; ++i) {  // each product takes as long as the exponentials behind it: left to itself, the compiler puts all products first
+      now = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i], q[i], now, 0, 0, 0);
+      exponentials(last, i * 16 / NQ, (i + 1) * 16 / NQ);
+      __builtin_amdgcn_sched_barrier(0);
     }
     asm volatile("" : "+v"(pr[0]), "+v"(pr[1]), "+v"(l));  // here and not behind the branches below
     if (b == 0 && t + 1 < tiles) request(t + 1);
     mask(now, t, b);
-    __builtin_amdgcn_s_setprio(1);  // before the exponentials of the other wavefront of the SIMD
     read_values(v1, V, 1);
     times_values(v0, 0);
     if (b == 0) read_keys(f, lds + (t & 1) * TILEB + L::BLOCKB);
     times_values(v1, 1);
-    __builtin_amdgcn_s_setprio(0);
     const float top = row_max(now);
     if (__builtin_amdgcn_ballot_w64(top > m + 8.0f) != 0) raise(top);
   };
@@ -763,8 +759,7 @@ __device__ __forceinline__ void many_rows_bf16(const Args& p, const int index, u
       step(t, 0, S1, S0, lds + v_last + L::BLOCKB, f);
       step(t, 1, S0, S1, lds + v_now, f);
     }
-    exponentials(S1, 0);
-    exponentials(S1, 1);
+    exponentials(S1, 0, 16);
     bf16x8 v[NB];
     read_values(v, lds + v_now + L::BLOCKB, 0);
     times_values(v, 0);
@@ -902,7 +897,7 @@ Plan plan_of(int dt, const CacheView& c, int64_t rows, int heads, int max_new, i
   // as many workgroups as are on the chip at a time: LDS holds four blocks of rows of 128 bytes, two of 256, one of 512
   const int row_bytes = (c.head_dim <= 64 ? 64 : 128) * (dt == DT_BF16 ? 2 : 4), resident = 256 * 512 / row_bytes;
   // mixed_k shares a tile of keys among more rows; few_k gives more workgroups, and takes all where there are few rows.  bf16, us, few_k / mixed_k: 16 sequences,
-  // 16 new over 2000, 32 / 8 heads (256 blocks of 32 rows) 73 / 41; 1, 256 over 8192, 32 / 8 (256) 180 / 63; 1, 128 over 500, 8 / 8 (32) 16 / 23.  fp32, where an
+  // 16 new over 2000, 32 / 8 heads (256 blocks of 32 rows) 73 / 33; 1, 256 over 8192, 32 / 8 (256) 180 / 57; 1, 128 over 500, 8 / 8 (32) 16 / 23.  fp32, where an
   // instruction takes eight times as long and the chain of a workgroup shows: 2, 300 over 300, 16 / 4 (304) 64 / 98; 1, 1024, 32 / 32 (1024) 201 / 157.
   p.many = most > FEW && pairs * up(most, FEW) > (dt == DT_BF16 ? 128 : 512);
   const bool few = !p.many || rows < (int64_t)c.sequences * max_new;  // else no sequence is short where the longest is not, as a rule; the others take any
@@ -915,7 +910,7 @@ Plan plan_of(int dt, const CacheView& c, int64_t rows, int heads, int max_new, i
   if (p.many) {
     if (window > 0) span = std::min<int64_t>(span, (int64_t)window + 128 / group + KB);
     // The keys are split where the chip would not be full, but not into parts of less than about 1024, whose joining costs more (bf16, us, whole / split: 1, 512 over
-    // 4096, 32 / 32 heads 114 / 62; 2, 1024 over 8192, 8 / 1 129 / 99; 1, 1024 over none, 32 / 32 in two 34 / 46).
+    // 4096, 32 / 32 heads 99 / 61; 2, 1024 over 8192, 8 / 1 190 / 97; 8, 64 over 2048, 32 / 32 52 / 57; 1, 1024 over none, 32 / 32 in parts of 512 30 / 45).
     const int64_t n = std::min<int64_t>({up(dt == DT_BF16 ? 512 : 256, pairs * p.many_blocks), up(span, 1024), 64});
     if (n > 1) {
       p.chunk = (int)(up(up(span, n), 64) * 64);
