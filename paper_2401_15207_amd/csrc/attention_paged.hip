@@ -909,9 +909,11 @@ Plan plan_of(int dt, const CacheView& c, int64_t rows, int heads, int max_new, i
   p.split = 1; p.chunk = INT32_MAX / 2;
   if (p.many) {
     if (window > 0) span = std::min<int64_t>(span, (int64_t)window + 128 / group + KB);
-    // The keys are split where the chip would not be full, but not into parts of less than about 1024, whose joining costs more (bf16, us, whole / split: 1, 512 over
-    // 4096, 32 / 32 heads 99 / 61; 2, 1024 over 8192, 8 / 1 190 / 97; 8, 64 over 2048, 32 / 32 52 / 57; 1, 1024 over none, 32 / 32 in parts of 512 30 / 45).
-    const int64_t n = std::min<int64_t>({up(dt == DT_BF16 ? 512 : 256, pairs * p.many_blocks), up(span, 1024), 64});
+    // The keys are split where a compute unit would not have a workgroup, until it has two (fp32: one), but not into parts of less than about 1024, whose joining costs
+    // more (bf16, us, whole / split: 1, 512 over 4096, 32 / 32 heads (128 workgroups) 99 / 61; 2, 1024 over 8192, 8 / 1 (128) 190 / 97; 8, 64 over 2048, 32 / 32 (256)
+    // 52 / 57; 1, 1024 over 4096, 32 / 32 (256) 113 / 116; 1, 1024 over none, 32 / 32 in parts of 512 30 / 45).
+    const int64_t blocks = pairs * p.many_blocks;
+    const int64_t n = blocks >= 256 ? 1 : std::min<int64_t>({up(dt == DT_BF16 ? 512 : 256, blocks), up(span, 1024), 64});
     if (n > 1) {
       p.chunk = (int)(up(up(span, n), 64) * 64);
       p.split = (int)up(span, p.chunk);
