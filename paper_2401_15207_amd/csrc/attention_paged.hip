@@ -14,7 +14,7 @@
 //            of its loads, products and joins.
 //   mixed_k  128 rows a workgroup, 32 a wavefront, which share tiles of 64 keys; bound by the matrix instructions and the LDS reads that feed them (bf16: 16 KB for
 //            16 instructions of 32 cycles, four wavefronts: 128 bytes a cycle, all that LDS gives).  Its first workgroups take the sequences of few rows.
-//            Chunks of 700 to 1024 of 4 sequences over up to 4096, 32 / 32 heads bf16: 187 us, 815 TFLOP/s (a large product on the card 1250); fp32, 1024 over none 158 us.
+//            Chunks of 700 to 1024 of 4 sequences over up to 4096, 32 / 32 heads bf16: 187 us, 815 TFLOP/s (a large product on the card 1250); fp32, 1024 over none 152 us.
 //   join_k   rows whose keys fell to several workgroups: the parts, weighted by their maxima.
 #include <math.h>
 
@@ -516,8 +516,9 @@ __device__ __forceinline__ void many_rows_f32(const Args& p, const int index, un
   constexpr int NB = L::NB, KT = 2 * KB, TILEB = KT * L::ROWB, QB = 128;
   const int tid = threadIdx.x, lane = tid & 63, wave = UNIFORM(tid >> 6), fr = lane & 31, fh = lane >> 5;
   int i = index / p.split;
-  const int part = index - i * p.split, block = p.many_blocks - 1 - i % p.many_blocks, pair = i / p.many_blocks;  // most keys first
-  const int s = pair / p.c.kv_heads, kv_head = pair % p.c.kv_heads;
+  const int part = index - i * p.split, kv_head = i % p.c.kv_heads;  // in the order of many_rows_bf16
+  i /= p.c.kv_heads;
+  const int block = p.many_blocks - 1 - i % p.many_blocks, s = i / p.many_blocks;
   const CacheSeq of = cache_seq(p.c, s, p.rows, p.max_new);
   const int n_rows = of.fresh * p.group;
   if (n_rows <= p.few_upto || block * QB >= n_rows) return;
@@ -898,7 +899,7 @@ Plan plan_of(int dt, const CacheView& c, int64_t rows, int heads, int max_new, i
   const int row_bytes = (c.head_dim <= 64 ? 64 : 128) * (dt == DT_BF16 ? 2 : 4), resident = 256 * 512 / row_bytes;
   // mixed_k shares a tile of keys among more rows; few_k gives more workgroups, and takes all where there are few rows.  bf16, us, few_k / mixed_k: 16 sequences,
   // 16 new over 2000, 32 / 8 heads (256 blocks of 32 rows) 73 / 33; 1, 256 over 8192, 32 / 8 (256) 180 / 57; 1, 128 over 500, 8 / 8 (32) 16 / 23.  fp32, where an
-  // instruction takes eight times as long and the chain of a workgroup shows: 2, 300 over 300, 16 / 4 (304) 64 / 98; 1, 1024, 32 / 32 (1024) 201 / 157.
+  // instruction takes eight times as long and the chain of a workgroup shows: 2, 300 over 300, 16 / 4 (304) 64 / 98; 1, 1024, 32 / 32 (1024) 201 / 152.
   p.many = most > FEW && pairs * up(most, FEW) > (dt == DT_BF16 ? 128 : 512);
   const bool few = !p.many || rows < (int64_t)c.sequences * max_new;  // else no sequence is short where the longest is not, as a rule; the others take any
   p.few_upto = !p.many ? INT32_MAX : few ? FEW : 0;
@@ -909,11 +910,12 @@ Plan plan_of(int dt, const CacheView& c, int64_t rows, int heads, int max_new, i
   p.split = 1; p.chunk = INT32_MAX / 2;
   if (p.many) {
     if (window > 0) span = std::min<int64_t>(span, (int64_t)window + 128 / group + KB);
-    // The keys are split where a compute unit would not have a workgroup, until it has two (fp32: one), but not into parts of less than about 1024, whose joining costs
+    // The keys are split where a compute unit would not have a workgroup, until it has two, but not into parts of less than about 1024 (fp32: 512), whose joining costs
     // more (bf16, us, whole / split: 1, 512 over 4096, 32 / 32 heads (128 workgroups) 99 / 61; 2, 1024 over 8192, 8 / 1 (128) 190 / 97; 8, 64 over 2048, 32 / 32 (256)
-    // 52 / 57; 1, 1024 over 4096, 32 / 32 (256) 113 / 116; 1, 1024 over none, 32 / 32 in parts of 512 30 / 45).
+    // 52 / 57; 1, 1024 over 4096, 32 / 32 (256) 113 / 116; 1, 1024 over none, 32 / 32 in parts of 512 30 / 45;
+    // fp32: 1, 2048 over none, 12 / 12 (192) 264 / 224; 1, 1024 over none, 32 / 32 (256) 152 / 178).
     const int64_t blocks = pairs * p.many_blocks;
-    const int64_t n = blocks >= 256 ? 1 : std::min<int64_t>({up(dt == DT_BF16 ? 512 : 256, blocks), up(span, 1024), 64});
+    const int64_t n = blocks >= 256 ? 1 : std::min<int64_t>({up(512, blocks), up(span, dt == DT_BF16 ? 1024 : 512), 64});
     if (n > 1) {
       p.chunk = (int)(up(up(span, n), 64) * 64);
       p.split = (int)up(span, p.chunk);
