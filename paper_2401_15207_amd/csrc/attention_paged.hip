@@ -900,7 +900,9 @@ Plan plan_of(int dt, const CacheView& c, int64_t rows, int heads, int max_new, i
   // mixed_k shares a tile of keys among more rows; few_k gives more workgroups, and takes all where there are few rows.  bf16, us, few_k / mixed_k: 16 sequences,
   // 16 new over 2000, 32 / 8 heads (256 blocks of 32 rows) 73 / 33; 1, 256 over 8192, 32 / 8 (256) 180 / 57; 1, 128 over 500, 8 / 8 (32) 16 / 23.  fp32, where an
   // instruction takes eight times as long and the chain of a workgroup shows: 2, 300 over 300, 16 / 4 (304) 64 / 98; 1, 1024, 32 / 32 (1024) 201 / 152.
-  p.many = most > FEW && pairs * up(most, FEW) > (dt == DT_BF16 ? 128 : 512);
+  // fp32 workgroups of 128 rows want more than half of them, as their products take longest: 36 sequences, 30 new over 1882, 32 / 16 of 64 (60 rows) 241 / 415; 16, 64
+  // over 700, 32 / 32 (64) 177 / 257; 45, 38 over 119, 64 / 32 of 32 (76) 80 / 59; 16, 96 over 700, 32 / 32 (96) 274 / 280.
+  p.many = most > (dt == DT_BF16 ? 1 : 2) * FEW && pairs * up(most, FEW) > (dt == DT_BF16 ? 128 : 512);
   const bool few = !p.many || rows < (int64_t)c.sequences * max_new;  // else no sequence is short where the longest is not, as a rule; the others take any
   p.few_upto = !p.many ? INT32_MAX : few ? FEW : 0;
   p.few_first = p.many && few ? (int)pairs : 0;
@@ -932,8 +934,11 @@ Plan plan_of(int dt, const CacheView& c, int64_t rows, int heads, int max_new, i
   // Eight wavefronts a block of rows where there are no more blocks than compute units (one token, 32 / 32 heads, us, eight / four: 1 over 500 8.1 / 9.9, 1 over 1000
   // 11.2 / 15.1, 8 over 1000 24.0 / 24.2, 32 over 500 47.2 / 42.2).  Runs cost a search for their begin and a second launch, which pays where the longest sequence is
   // long (whole / runs: 1 over 800 9.8 / 11.1, 1 over 1000 11.2 / 11.2, 8 of one length 1000 24.0 / 33.5) -- sequences of one length apart, at 32 x 1500 140 / 152.
-  p.waves = items <= 256 && row_bytes <= 256 && span > STEP ? 8 : 4;
-  if (span > (items >= resident ? 8 : p.waves) * STEP) {
+  // fp32 steps take longer, so a chip that is not full has runs from two on (1 over 400, 8 / 8 25.4 / 16.2; 8 over 300, 8 / 8 22.2 / 18.7; 4 over 477, 4 / 4 25.7 /
+  // 16.5; in one step each 2 x 4 over 228, 4 / 4 of 80 13.8 / 15.0).  Where keys are fewer than the wavefronts' blocks, the others would only take LDS from other
+  // workgroups (128 over 20, 32 / 32 bf16, four wavefronts / one 42.5 / 16.5; over 60, fp32, four / two 160 / 94).
+  p.waves = items <= 256 && row_bytes <= 256 && span > STEP ? 8 : span <= KB ? 1 : span <= 2 * KB ? 2 : 4;
+  if (span > (items >= resident ? 8 : dt == DT_F32 && 2 * items <= resident ? 2 : std::max(p.waves, 4)) * STEP) {
     p.waves = 4;
     p.runs = (int)std::min<int64_t>(resident, items * up(span, STEP));
     p.parts = (int64_t)p.runs * 2 * FEW;
@@ -954,17 +959,20 @@ hipError_t allow_lds() {
 
 template <typename T, int HD, int NB, bool PAST>
 hipError_t whole(int waves, dim3 g, const Args& a, hipStream_t st) {
-  constexpr int FOUR = 4 * 2 * KB * HD * (int)sizeof(T);
-  if constexpr (2 * FOUR <= 131072) {
-    if (waves == 8) {
-      if (hipError_t e = allow_lds<few_whole_k<T, HD, NB, 8, PAST>, 2 * FOUR>()) return e;
-      few_whole_k<T, HD, NB, 8, PAST><<<g, 512, 2 * FOUR, st>>>(a);
-      return hipSuccess;
+  const auto run = [&](auto w) -> hipError_t {
+    constexpr int W = decltype(w)::value, LDS = W * 2 * KB * HD * (int)sizeof(T);
+    if constexpr (LDS <= 131072) {
+      if (hipError_t e = allow_lds<few_whole_k<T, HD, NB, W, PAST>, LDS>()) return e;
+      few_whole_k<T, HD, NB, W, PAST><<<g, 64 * W, LDS, st>>>(a);
     }
+    return hipSuccess;
+  };
+  switch (waves) {
+    case 1: return run(std::integral_constant<int, 1>());
+    case 2: return run(std::integral_constant<int, 2>());
+    case 8: return run(std::integral_constant<int, 8>());
+    default: return run(std::integral_constant<int, 4>());
   }
-  if (hipError_t e = allow_lds<few_whole_k<T, HD, NB, 4, PAST>, FOUR>()) return e;
-  few_whole_k<T, HD, NB, 4, PAST><<<g, 256, FOUR, st>>>(a);
-  return hipSuccess;
 }
 
 template <typename T, int HD, int NB>
