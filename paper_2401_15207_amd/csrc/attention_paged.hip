@@ -897,31 +897,38 @@ Plan plan_of(int dt, const CacheView& c, int64_t rows, int heads, int max_new, i
   int64_t span = std::max<int64_t>(1, std::min<int64_t>(max_length, (int64_t)c.max_pages << c.page_shift));
   // as many workgroups as are on the chip at a time: LDS holds four blocks of rows of 128 bytes, two of 256, one of 512
   const int row_bytes = (c.head_dim <= 64 ? 64 : 128) * (dt == DT_BF16 ? 2 : 4), resident = 256 * 512 / row_bytes;
-  // mixed_k shares a tile of keys among more rows; few_k gives more workgroups, and takes all where there are few rows.  bf16, us, few_k / mixed_k: 16 sequences,
-  // 16 new over 2000, 32 / 8 heads (256 blocks of 32 rows) 73 / 33; 1, 256 over 8192, 32 / 8 (256) 180 / 57; 1, 128 over 500, 8 / 8 (32) 16 / 23.  fp32, where an
-  // instruction takes eight times as long and the chain of a workgroup shows: 2, 300 over 300, 16 / 4 (304) 64 / 98; 1, 1024, 32 / 32 (1024) 201 / 152.
-  // fp32 workgroups of 128 rows want more than half of them, as their products take longest: 36 sequences, 30 new over 1882, 32 / 16 of 64 (60 rows) 241 / 415; 16, 64
-  // over 700, 32 / 32 (64) 177 / 257; 45, 38 over 119, 64 / 32 of 32 (76) 80 / 59; 16, 96 over 700, 32 / 32 (96) 274 / 280.
-  p.many = most > (dt == DT_BF16 ? 1 : 2) * FEW && pairs * up(most, FEW) > (dt == DT_BF16 ? 128 : 512);
-  const bool few = !p.many || rows < (int64_t)c.sequences * max_new;  // else no sequence is short where the longest is not, as a rule; the others take any
-  p.few_upto = !p.many ? INT32_MAX : few ? FEW : 0;
-  p.few_first = p.many && few ? (int)pairs : 0;
+  // mixed_k shares a tile of keys among more rows, and its parts of the keys need no search for where they begin; few_k has four wavefronts on the same rows, none idle.
+  // bf16, us, few_k / mixed_k: 16 sequences, 16 new over 2000, 32 / 8 heads (64 rows) 73 / 33; 1, 256 over 8192, 32 / 8 180 / 57; 1, 128 over 4000, 8 / 8 47 / 21; 1, 40
+  // over 200, 16 / 16 of 64 9.3 / 8.8; of at most 32 rows, where three of four wavefronts of mixed_k idle: 4, 4 over 4000, 32 / 8 (32 key heads in all) 31 / 22; 1, 20
+  // over 2000, 8 / 8 14.4 / 13.2; 16, 20 over 1000, 8 / 8 (128) 21 / 26; 1, 1 over 16000, 8 / 1 (8 rows) 17 / 21.
+  // fp32, where products take eight times as long, and idle wavefronts show: 36, 30 over 1882, 32 / 16 of 64 (60 rows) 241 / 415; 16, 64 over 700, 32 / 32 (64) 177 / 257;
+  // 45, 38 over 119, 64 / 32 of 32 (76) 80 / 59; 2, 300 over 300, 16 / 4 (1200 rows, 8 key heads) 64 / 98; 1, 1024, 32 / 32 201 / 152.
+  if (dt == DT_BF16) p.many = most > FEW || (most > FEW / 4 && pairs <= 64);
+  else p.many = most > 2 * FEW && pairs * up(most, FEW) > 512;
+  p.few_upto = p.many ? 0 : INT32_MAX;
   p.few_blocks = (int)(p.many ? 1 : std::max<int64_t>(1, up(most, FEW)));
   p.many_blocks = (int)std::max<int64_t>(1, up(most, 128));
   p.entries = (int64_t)c.sequences * p.few_blocks;
   p.split = 1; p.chunk = INT32_MAX / 2;
   if (p.many) {
     if (window > 0) span = std::min<int64_t>(span, (int64_t)window + 128 / group + KB);
-    // The keys are split where a compute unit would not have a workgroup, until it has two, but not into parts of less than about 1024 (fp32: 512), whose joining costs
-    // more (bf16, us, whole / split: 1, 512 over 4096, 32 / 32 heads (128 workgroups) 99 / 61; 2, 1024 over 8192, 8 / 1 (128) 190 / 97; 8, 64 over 2048, 32 / 32 (256)
-    // 52 / 57; 1, 1024 over 4096, 32 / 32 (256) 113 / 116; 1, 1024 over none, 32 / 32 in parts of 512 30 / 45;
-    // fp32: 1, 2048 over none, 12 / 12 (192) 264 / 224; 1, 1024 over none, 32 / 32 (256) 152 / 178).
+    // The keys are split where a compute unit would not have a workgroup, until it has two, but into parts that cost more than their joining (bf16, us, whole / split:
+    // 1, 512 over 4096, 32 / 32 heads (128 workgroups) 99 / 61; 2, 1024 over 8192, 8 / 1 (128) 190 / 97; 8, 64 over 2048, 32 / 32 (256) 52 / 57; 1, 1024 over none, 32 / 32
+    // (256) in parts of 512 30 / 45; fp32: 1, 2048 over none, 12 / 12 (192) 264 / 224; 1, 1024 over none, 32 / 32 (256) 152 / 178): 1024 keys (fp32: 512), 256 where
+    // workgroups are few (parts of 512 / 256 / 128: 1, 128 over 1000, 8 / 8 18.2 / 16.1 / 15.9; 1, 128 over 4000, 8 / 8
+    // 23.5 / 20.9 / 25.5; 1024 / 256: 1, 300 over 3000, 16 / 16 29.6 / 32.4).
     const int64_t blocks = pairs * p.many_blocks;
-    const int64_t n = blocks >= 256 ? 1 : std::min<int64_t>({up(512, blocks), up(span, dt == DT_BF16 ? 1024 : 512), 64});
+    const int64_t n = blocks >= 256 ? 1 : std::min<int64_t>({up(512, blocks), up(span, dt != DT_BF16 ? 512 : blocks > 64 ? 1024 : blocks > 32 ? 512 : 256), 64});
     if (n > 1) {
       p.chunk = (int)(up(up(span, n), 64) * 64);
       p.split = (int)up(span, p.chunk);
       p.parts = rows * heads * p.split;
+    }
+    // Without parts, sequences of few rows among the others are few_rows' where there may be any (else none is short where the longest is not, as a rule); parts of
+    // their keys are spread over the chip with the others' (11 sequences of up to 36 new, 4 / 4 heads bf16, over up to 6713: 72 us with whole keys, 47 so).
+    if (p.split == 1 && rows < (int64_t)c.sequences * max_new) {
+      p.few_upto = FEW;
+      p.few_first = (int)pairs;
     }
     return p;
   }

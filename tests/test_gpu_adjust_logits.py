@@ -233,3 +233,27 @@ def test_one_row_in_place_by_views_of_other_widths():
     H.kernel_adjust_logits_bwd(x, 290, d, d[:, :290], **by)
     H.kernel_adjust_logits(x, 290, x[:, :290], frequency=0.5, **by)
     assert torch.equal(x[:, :290], want) and torch.equal(d[:, :290], grad)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("v,ld", [(50000, 50000), (50001, 50004)])
+def test_large_matrices_as_their_halves(dtype, v, ld):
+    """A call that goes past the caches gives the bits of two that do not."""
+    rows, g = 400 if dtype == "bf16" else 200, torch.Generator(device="cuda").manual_seed(9)
+    x, d = (torch.randn(rows, ld, device="cuda", generator=g).to(DT[dtype]) for _ in range(2))
+    tokens = torch.randint(0, v, (rows * 64,), device="cuda", generator=g, dtype=torch.int32)
+    begin = torch.arange(rows, device="cuda") * 64
+    end, bias = begin + 64, torch.randn(1, v, device="cuda", generator=g)
+    allowed = torch.randint(-2 ** 31, 2 ** 31 - 1, (rows, (v + 31) // 32), device="cuda", generator=g).to(torch.int32)
+    half = rows // 2
+    assert rows * v * 2 * x.element_size() >= 2 ** 26 > half * v * 2 * x.element_size()
+    out, grad, outs, grads = (torch.full_like(x, -7.0) for _ in range(4))
+    for to, dto, parts in ((out, grad, [slice(0, rows)]), (outs, grads, [slice(0, half), slice(half, rows)])):
+        for r in parts:
+            by = dict(tokens=tokens, begin=begin[r], end=end[r], repetition=1.5, allowed=allowed[r])
+            H.kernel_adjust_logits(x[r], v, to[r], presence=0.5, frequency=0.25, bias=bias, **by)
+            H.kernel_adjust_logits_bwd(x[r], v, d[r], dto[r], **by)
+    assert torch.equal(out, outs) and torch.equal(grad, grads)
+    seen = torch.zeros(rows, v, dtype=torch.bool, device="cuda").scatter_(1, tokens.view(rows, 64).long(), True)
+    let = (allowed[:, torch.arange(v, device="cuda") // 32] >> (torch.arange(v, device="cuda") % 32)[None, :].to(torch.int32)) & 1 != 0
+    assert torch.equal(torch.isinf(out[:, :v]), ~let) and torch.equal(grad[:, :v][let & ~seen], d[:, :v][let & ~seen])

@@ -422,3 +422,28 @@ def test_two_calls_at_once():
     torch.cuda.synchronize()
     for w, out in zip(want, outs):
         assert all(torch.equal(o, w) for o in out)
+
+
+# keys split over workgroups, with sequences of few rows and of none among the others; keys of one and of two blocks; rows on either side of the choice of kernel
+RAGGED = [([(3000, 1), (100, 40), (2500, 0), (0, 3), (700, 17)], 4, 2, 64, 16), ([(2000, 9), (40, 1)], 4, 4, 128, 32), ([(1500, 33)], 2, 2, 80, 16), ([(900, 4), (1, 4)], 32, 8, 128, 16),
+          ([(31, 1), (5, 1), (0, 1)], 4, 4, 96, 16), ([(60, 2), (33, 1)], 8, 2, 128, 32), ([(300, 65)], 1, 1, 128, 16), ([(400, 1), (150, 1)], 2, 2, 128, 16)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("case", RAGGED)
+@pytest.mark.parametrize("window", [0, 33, 700])
+def test_sequences_of_few_rows_among_split_keys(dtype, case, window):
+    m = Made(*case, dtype, seed=11, more_rows=1)
+    out, lse = m.attend(window)
+    m.check(out, lse, window)
+    again, lse2 = m.attend(window)
+    assert torch.equal(again, out) and torch.equal(lse2, lse)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("tokens", [[(2100, 1), (700, 1), (0, 1)], [(520, 1)] * 3 + [(580, 1)], [(130 + 5 * i, 1) for i in range(17)]])
+def test_caches_larger_than_the_l2(dtype, tokens):
+    """Keys that go past the caches: in runs, and a workgroup a head with eight and with four wavefronts."""
+    m = Made(tokens, 32, 32, 128, 16, dtype, seed=12)
+    out, lse = m.attend()
+    m.check(out, lse)
