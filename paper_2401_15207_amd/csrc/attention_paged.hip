@@ -14,7 +14,7 @@
 //            of its loads, products and joins.
 //   mixed_k  128 rows a workgroup, 32 a wavefront, which share tiles of 64 keys; bound by the matrix instructions and the LDS reads that feed them (bf16: 16 KB for
 //            16 instructions of 32 cycles, four wavefronts: 128 bytes a cycle, all that LDS gives).  Its first workgroups take the sequences of few rows.
-//            Chunks of 700 to 1024 of 4 sequences over up to 4096, 32 / 32 heads bf16: 187 us, 815 TFLOP/s (a large product on the card 1250); fp32, 1024 over none 152 us.
+//            Chunks of 700 to 1024 of 4 sequences over up to 4096, 32 / 32 heads bf16: 188 to 198 us by the card, 770 to 815 TFLOP/s (a large product 1250); fp32, 1024 over none 152 us.
 //   join_k   rows whose keys fell to several workgroups: the parts, weighted by their maxima.
 #include <math.h>
 
@@ -579,7 +579,7 @@ __device__ __forceinline__ void many_rows_f32(const Args& p, const int index, un
 }
 
 // ---- many rows, bf16 ----
-// 128 rows a workgroup, 32 a wavefront, two workgroups a compute unit (chunks: 187 us; 256 rows in eight wavefronts the same; 64 rows a wavefront would halve the
+// 128 rows a workgroup, 32 a wavefront, two workgroups a compute unit (chunks: 188 us; 256 rows in eight wavefronts the same; 64 rows a wavefront would halve the
 // LDS reads, but need more registers than there are: 663).  Within a wavefront the products of one block of 32 keys run beside the exponentials of
 // the one before:
 //   scores of block i (8 MFMAs)     in turn with the exponentials of block i - 1 (products first, then exponentials: 4096 over none, 16 / 2 heads 109 us, in turn 99)
