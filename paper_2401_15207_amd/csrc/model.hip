@@ -1251,7 +1251,7 @@ hift_status forward(hift_model* M, const hift_batch* bt, int keep_from, const hi
     }
     RW(RW_NORM_FWD, 2.0 * e.n_pick * d * es, norm_fwd(dt, rms, e.n_pick, d, c.norm_eps, xl, M->W(rms ? "gf" : "lnf_g"), rms ? nullptr : M->W("lnf_b"), M->xf, M->st_f, st));
     ST_TRY(linear(M, M->xf, e.n_pick, M->T_(c.tie_embeddings ? "tok_emb" : "whead"), nullptr, nullptr, M->logits, nullptr, nullptr, M->logits_ld));
-    HIP_TRY(hipMemcpy2DAsync(e.logits, (size_t)e.ld * M->es, M->logits, (size_t)M->logits_ld * M->es, (size_t)c.vocab * M->es, (size_t)e.n_pick, hipMemcpyDeviceToDevice, st));
+    RW(RW_FIRST_ROWS, 2.0 * e.n_pick * c.vocab * es, wanted_logits(dt, ex->cache, T, (int)std::min<int64_t>(e.max_new, T), e.n_pick, e.pick, c.vocab, M->logits, M->logits_ld, e.logits, e.ld, st));
     return HIFT_OK;
   }
   if (enc) {
@@ -3077,7 +3077,7 @@ hift_status hift_extend(hift_model* M, const hift_extension* e, void* workspace,
   Extend ex{};
   size_t need = 0;
   ST_TRY(check_extension(M, e, &ex, &need));
-  if (e->rows == 0 || ex.cache.sequences == 0) return HIFT_OK;
+  if (e->rows == 0) return HIFT_OK;
   if (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 15)) return fail(HIFT_EINVAL, "workspace of %zu bytes, 16-byte aligned, expected", need);
   ex.positions = (int32_t*)workspace;
   ex.attention = (unsigned char*)workspace + ((size_t)e->rows * 4 + 255) / 256 * 256;

@@ -272,10 +272,9 @@ __global__ void __launch_bounds__(BLK) append_k(AppendArgs p) {
   }
 }
 
-// One thread a row: the sequence that the row belongs to is looked for among the starts.
-__global__ void __launch_bounds__(BLK) cache_positions_k(CacheView c, int64_t rows, int max_new, int32_t* positions) {
-  const int64_t row = (int64_t)blockIdx.x * BLK + threadIdx.x;
-  if (row >= rows) return;
+// Position of a new row, -1 for one that belongs to no sequence or lies beyond max_new: the sequence is looked for among the starts.
+__device__ __forceinline__ int position_of(const CacheView& c, int64_t row, int64_t rows, int max_new) {
+  if (c.sequences == 0) return -1;
   int lo = 0, hi = c.sequences;  // the last sequence that starts at the row or before
   while (hi - lo > 1) {
     const int mid = (lo + hi) / 2;
@@ -284,7 +283,34 @@ __global__ void __launch_bounds__(BLK) cache_positions_k(CacheView c, int64_t ro
   }
   const CacheSeq of = cache_seq(c, lo, rows, max_new);
   const int64_t token = row - of.row0;
-  positions[row] = token >= 0 && token < of.fresh ? of.cached + (int)token : 0;
+  return token >= 0 && token < of.fresh ? of.cached + (int)token : -1;
+}
+
+// One thread a row
+__global__ void __launch_bounds__(BLK) cache_positions_k(CacheView c, int64_t rows, int max_new, int32_t* positions) {
+  const int64_t row = (int64_t)blockIdx.x * BLK + threadIdx.x;
+  if (row < rows) positions[row] = max(position_of(c, row, rows, max_new), 0);
+}
+
+// One workgroup a wanted row: its logits, or zeros where the row belongs to no sequence (nothing has computed its attention).
+template <typename T, int V>
+__global__ void __launch_bounds__(BLK) wanted_logits_k(CacheView c, int64_t rows, int max_new, const int32_t* __restrict__ pick, int vocab, const T* __restrict__ x, int64_t ldx,
+                                                       T* __restrict__ y, int64_t ldy) {
+  const int64_t i = blockIdx.x, row = pick ? min(max((int64_t)pick[i], (int64_t)0), rows - 1) : i;
+  const bool none = position_of(c, row, rows, max_new) < 0;
+  typedef Elems<T, V> E;
+  for (int j = threadIdx.x * V; j < vocab; j += BLK * V) {
+    E e = *reinterpret_cast<const E*>(x + i * ldx + j);
+    if (none) {
+#pragma unroll
+      for (int k = 0; k < V; ++k) e.v[k] = from_f32<T>(0.f);
+    }
+    *reinterpret_cast<E*>(y + i * ldy + j) = e;
+  }
+}
+template <typename T, int V>
+void wanted_v(const CacheView& c, int64_t rows, int max_new, int64_t n, const int32_t* pick, int vocab, const void* x, int64_t ldx, void* y, int64_t ldy, hipStream_t st) {
+  wanted_logits_k<T, V><<<(unsigned)n, BLK, 0, st>>>(c, rows, max_new, pick, vocab, (const T*)x, ldx, (T*)y, ldy);
 }
 
 template <typename T, int V>
@@ -337,6 +363,23 @@ hipError_t rotary(int dt, bool pairs, bool backward, int64_t rows, int heads, in
 hipError_t cache_positions(const CacheView& c, int64_t rows, int max_new, int32_t* positions, hipStream_t st) {
   if (rows == 0) return hipSuccess;
   cache_positions_k<<<(unsigned)((rows + BLK - 1) / BLK), BLK, 0, st>>>(c, rows, max_new, positions);
+  return hipGetLastError();
+}
+
+hipError_t wanted_logits(int dt, const CacheView& c, int64_t rows, int max_new, int64_t n, const int32_t* pick, int vocab, const void* x, int64_t ldx, void* y, int64_t ldy,
+                         hipStream_t st) {
+  if (n == 0) return hipSuccess;
+  const int v = vector_of(dt == DT_BF16 ? 2 : 4, any_bits({vocab, ldx, ldy}), reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(y));
+  if (dt == DT_BF16) {
+    if (v == 8) wanted_v<bf16, 8>(c, rows, max_new, n, pick, vocab, x, ldx, y, ldy, st);
+    else if (v == 4) wanted_v<bf16, 4>(c, rows, max_new, n, pick, vocab, x, ldx, y, ldy, st);
+    else if (v == 2) wanted_v<bf16, 2>(c, rows, max_new, n, pick, vocab, x, ldx, y, ldy, st);
+    else wanted_v<bf16, 1>(c, rows, max_new, n, pick, vocab, x, ldx, y, ldy, st);
+  } else {
+    if (v == 4) wanted_v<float, 4>(c, rows, max_new, n, pick, vocab, x, ldx, y, ldy, st);
+    else if (v == 2) wanted_v<float, 2>(c, rows, max_new, n, pick, vocab, x, ldx, y, ldy, st);
+    else wanted_v<float, 1>(c, rows, max_new, n, pick, vocab, x, ldx, y, ldy, st);
+  }
   return hipGetLastError();
 }
 
