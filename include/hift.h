@@ -657,7 +657,8 @@ hift_status hift_kernel_attention_paged(const hift_cache* cache, int64_t rows, c
                                         size_t workspace_bytes, void* stream);
 
 /* The model writes on: new tokens of several sequences go through it with its present weights, over a paged cache of all its layers -- a prompt, a chunk of
- * one, or a token a sequence -- and leave their keys and values there (decoders only; bf16 models round q and k before and after their rotation).
+ * one, or a token a sequence -- and leave their keys and values there (decoders only; a bf16 model's
+ * q and k are rounded as in its own passes over so many rows: once where the projection's kernel rotates them, otherwise before and after their rotation).
  *   cache         layer 0's: the model's type, heads and head width (which has to suit hift_cache); layer l's k and v lie l * layer_stride elements further
  *   tokens        device int32 [rows]; starts, max_new, max_length as for hift_kernel_attention_paged; rows at most max_batch * max_seq of the model's creation,
  *                 max_length at most its max_seq

@@ -275,6 +275,8 @@ hipError_t cache_append(int dt, const CacheView& c, int heads, bool pairs, int r
                         const void* qkv, int64_t ld, void* q, int64_t ldq, hipStream_t st);
 // position of every new row of a cache's sequences; 0 for rows of none
 hipError_t cache_positions(const CacheView& c, int64_t rows, int max_new, int32_t* positions, hipStream_t st);
+// out [rows, rot / 2]: the table's entries of those positions
+hipError_t cache_angles(const CacheView& c, int64_t rows, int max_new, int rot, const float* cos_sin, int table_rows, float* out, hipStream_t st);
 // logits x [n, vocab] of the rows pick[0 .. n) (null: row i) -> y, zeros for rows that belong to no sequence
 hipError_t wanted_logits(int dt, const CacheView& c, int64_t rows, int max_new, int64_t n, const int32_t* pick, int vocab, const void* x, int64_t ldx, void* y, int64_t ldy,
                          hipStream_t st);

@@ -707,16 +707,16 @@ struct Scope {
 
 
 // What a linear layer's epilogue may take over when the weight's packed copy is ordered for it:
-// the rotary embedding of q and k (S = sequence length), or the gated activation (act [rows, out/2];
+// the rotary embedding of q and k (cos_sin, S: rows of its table, row t takes t % S), or the gated activation (act [rows, out/2];
 // keep_pre = false: the pre-activations are not needed later and y is not written).  fused reports
 // whether it did; if not, y holds the plain product and the caller runs the separate kernel.
 struct LinEpi {
+  const float* cos_sin = nullptr;
   int S = 0;
   void* act = nullptr;
   bool keep_pre = true;
   bool fused = false;
   float* norm_stats = nullptr;  // weights with a folded normalisation: where (0, 1 / rms) per row goes, or null
-  bool rotate = true;           // false: the rotation is left out (its block order is undone all the same)
   bool gelu = false;            // plain block order: bias and GELU in the epilogue (act [rows, out]; keep_pre as above)
 };
 
@@ -758,7 +758,7 @@ hift_status linear(hift_model* M, const void* x, int64_t rows, const Tensor& w, 
         if (!epi->keep_pre) g.C = nullptr;
       } else {
         g.epi = EPI_ROPE;
-        g.cos_sin = M->cos_sin; g.S = epi->S; g.rot_cols = epi->rotate ? 2 * (int64_t)M->cfg.d_model : 0;
+        g.cos_sin = epi->cos_sin; g.S = epi->S; g.rot_cols = 2 * (int64_t)M->cfg.d_model;
       }
       epi->fused = true;
       if (w.pk_gain >= 0) {
@@ -1142,7 +1142,8 @@ struct Extend {
   CacheView cache;
   int64_t layer_bytes;
   const hift_extension* of;
-  int32_t* positions;  // work space: of the rows
+  int32_t* positions;  // work space: of the rows, for models that add a position's embedding
+  float* angles;       // of the rows, for projections whose kernel rotates (else null)
   void* attention;     // and the attention's
 };
 CacheView layer_cache(const Extend& ex, int l) {
@@ -1151,12 +1152,15 @@ CacheView layer_cache(const Extend& ex, int l) {
   c.v = (unsigned char*)c.v + l * ex.layer_bytes;
   return c;
 }
-hift_status attention_extend(hift_model* M, LayerAct& a, int l, const Extend& ex) {
+// rotated: the projection has turned q and k, before their one rounding, as in a batch's pass.  Otherwise they are turned on their way into the cache, and rounded
+// before and after, as the rope kernel of a batch's pass does.
+hift_status attention_extend(hift_model* M, LayerAct& a, int l, const Extend& ex, bool rotated) {
   const hift_extension& e = *ex.of;
   const int H = M->cfg.n_heads, d = M->cfg.d_model, hd = d / H, max_new = (int)std::min<int64_t>(e.max_new, e.rows);
   const CacheView c = layer_cache(ex, l);
-  const int rot = M->cfg.arch == HIFT_ARCH_RMS_ROPE_DECODER ? hd : 0;
-  RW(RW_ROPE, 6.0 * e.rows * d * M->es, cache_append(M->dt, c, H, false, rot, M->cos_sin, M->cfg.max_seq, e.rows, max_new, a.qkv, 3 * (int64_t)d, a.qkv, 3 * (int64_t)d, M->cs));
+  const int rot = M->cfg.arch == HIFT_ARCH_RMS_ROPE_DECODER && !rotated ? hd : 0;
+  RW(RW_ROPE, (rot ? 6.0 : 4.0) * e.rows * d * M->es, cache_append(M->dt, c, H, false, rot, M->cos_sin, M->cfg.max_seq, e.rows, max_new, a.qkv, 3 * (int64_t)d,
+                                                                   rot ? a.qkv : nullptr, 3 * (int64_t)d, M->cs));
   Scope sc(M, CAT_ATTN, 4.0 * e.rows * (double)e.max_length * d);
   K_TRY(attention_paged(M->dt, c, H, e.rows, max_new, e.max_length, 0, 1.0f / sqrtf((float)hd), a.qkv, 3 * (int64_t)d, a.ctx, d, nullptr, ex.attention, M->cs));
   return HIFT_OK;
@@ -1195,15 +1199,15 @@ hift_status forward(hift_model* M, const hift_batch* bt, int keep_from, const hi
       h1 = a.na;
     }
     LinEpi rot;
+    rot.cos_sin = ex ? ex->angles : M->cos_sin;
     rot.S = S;
     rot.norm_stats = a.st1;
-    rot.rotate = !ex;
     ST_TRY(linear(M, h1, T, *n.wqkv, n.bqkv, nullptr, a.qkv, &rot));
     if (M->lora_r > 0) {
       if (rot.fused) return fail(HIFT_ESTATE, "adapters need the projections before their rotation");
       ST_TRY(lora_fwd(M, l, h1, T, a.qkv));
     }
-    if (ex) ST_TRY(attention_extend(M, a, l, *ex));
+    if (ex) ST_TRY(attention_extend(M, a, l, *ex, rot.fused));
     else if (rms && !rot.fused) {
       RW(RW_ROPE, 4.0 * T * d * es, rope(dt, a.qkv, T, S, H, hd, M->cos_sin, +1, st));
     }
@@ -3041,6 +3045,13 @@ hift_status hift_kernel_adjust_logits_bwd(int32_t dtype, int64_t rows, int32_t V
 }
 
 namespace {
+// Whether a kernel of the projections may rotate; bytes of an extension's work space before the attention's: a row's angles then, or its position
+bool projection_rotates(const hift_model* M) { return layer_names(M, 0).wqkv->pk_order == PK_ORDER_PAIR64; }
+size_t extension_head(const hift_model* M, int64_t rows) {
+  const size_t a_row = projection_rotates(M) ? (size_t)M->cfg.d_model / M->cfg.n_heads * sizeof(float) : sizeof(int32_t);
+  return ((size_t)rows * a_row + 255) / 256 * 256;
+}
+
 // The checks of an extension, its view of the cache and the parts of its work space
 hift_status check_extension(const hift_model* M, const hift_extension* e, Extend* out, size_t* bytes) {
   if (!M || !e) return fail(HIFT_EINVAL, "null argument");
@@ -3059,7 +3070,7 @@ hift_status check_extension(const hift_model* M, const hift_extension* e, Extend
   if (e->n_pick > 0 && e->rows > 0 && !e->logits) return fail(HIFT_EINVAL, "logits are null");
   if (reinterpret_cast<uintptr_t>(e->logits) % (uintptr_t)es || (reinterpret_cast<uintptr_t>(e->tokens) | reinterpret_cast<uintptr_t>(e->pick) | reinterpret_cast<uintptr_t>(e->starts)) % 4)
     return fail(HIFT_EINVAL, "tokens, starts, pick or logits do not lie on whole elements");
-  const size_t head = ((size_t)e->rows * 4 + 255) / 256 * 256;
+  const size_t head = extension_head(M, e->rows);
   if (out) {
     out->cache = v; out->layer_bytes = e->layer_stride * es; out->of = e;
   }
@@ -3079,9 +3090,15 @@ hift_status hift_extend(hift_model* M, const hift_extension* e, void* workspace,
   ST_TRY(check_extension(M, e, &ex, &need));
   if (e->rows == 0) return HIFT_OK;
   if (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 15)) return fail(HIFT_EINVAL, "workspace of %zu bytes, 16-byte aligned, expected", need);
-  ex.positions = (int32_t*)workspace;
-  ex.attention = (unsigned char*)workspace + ((size_t)e->rows * 4 + 255) / 256 * 256;
-  if (M->cfg.arch == HIFT_ARCH_PRELN_DECODER) HIP_TRY(cache_positions(ex.cache, e->rows, (int)std::min<int64_t>(e->max_new, e->rows), ex.positions, M->cs));
+  const int max_new = (int)std::min<int64_t>(e->max_new, e->rows);
+  ex.attention = (unsigned char*)workspace + extension_head(M, e->rows);
+  if (M->cfg.arch == HIFT_ARCH_PRELN_DECODER) {
+    ex.positions = (int32_t*)workspace;
+    HIP_TRY(cache_positions(ex.cache, e->rows, max_new, ex.positions, M->cs));
+  } else if (projection_rotates(M)) {
+    ex.angles = (float*)workspace;
+    HIP_TRY(cache_angles(ex.cache, e->rows, max_new, M->cfg.d_model / M->cfg.n_heads, M->cos_sin, M->cfg.max_seq, ex.angles, M->cs));
+  }
   const hift_batch bt{e->tokens, nullptr, 1, (int32_t)e->rows};
   return forward(M, &bt, M->lay.n_units, nullptr, &ex);
 }

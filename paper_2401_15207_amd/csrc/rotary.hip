@@ -292,6 +292,14 @@ __global__ void __launch_bounds__(BLK) cache_positions_k(CacheView c, int64_t ro
   if (row < rows) positions[row] = max(position_of(c, row, rows, max_new), 0);
 }
 
+// The table's entries of the rows' positions, one after the other: a thread one pair
+__global__ void __launch_bounds__(BLK) cache_angles_k(CacheView c, int64_t rows, int max_new, int half, const float2* __restrict__ cs, int table_rows, float2* __restrict__ out) {
+  const int64_t i = (int64_t)blockIdx.x * BLK + threadIdx.x, row = i / half;
+  if (row >= rows) return;
+  const int at = min(max(position_of(c, row, rows, max_new), 0), table_rows - 1);
+  out[i] = cs[(int64_t)at * half + (i - row * half)];
+}
+
 // One workgroup a wanted row: its logits, or zeros where the row belongs to no sequence (nothing has computed its attention).
 template <typename T, int V>
 __global__ void __launch_bounds__(BLK) wanted_logits_k(CacheView c, int64_t rows, int max_new, const int32_t* __restrict__ pick, int vocab, const T* __restrict__ x, int64_t ldx,
@@ -363,6 +371,14 @@ hipError_t rotary(int dt, bool pairs, bool backward, int64_t rows, int heads, in
 hipError_t cache_positions(const CacheView& c, int64_t rows, int max_new, int32_t* positions, hipStream_t st) {
   if (rows == 0) return hipSuccess;
   cache_positions_k<<<(unsigned)((rows + BLK - 1) / BLK), BLK, 0, st>>>(c, rows, max_new, positions);
+  return hipGetLastError();
+}
+
+hipError_t cache_angles(const CacheView& c, int64_t rows, int max_new, int rot, const float* cos_sin, int table_rows, float* out, hipStream_t st) {
+  if (rows == 0) return hipSuccess;
+  const int64_t blocks = (rows * (rot / 2) + BLK - 1) / BLK;
+  if (blocks > 0x7FFFFFFF) return hipErrorInvalidValue;
+  cache_angles_k<<<(unsigned)blocks, BLK, 0, st>>>(c, rows, max_new, rot / 2, (const float2*)cos_sin, table_rows, (float2*)out);
   return hipGetLastError();
 }
 
