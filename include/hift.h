@@ -662,7 +662,8 @@ hift_status hift_kernel_attention_paged(const hift_cache* cache, int64_t rows, c
  *   cache         layer 0's: the model's type, heads and head width (which has to suit hift_cache); layer l's k and v lie l * layer_stride elements further
  *   tokens        device int32 [rows]; starts, max_new, max_length as for hift_kernel_attention_paged; rows at most max_batch * max_seq of the model's creation,
  *                 max_length at most its max_seq
- *   pick          device int32 [n_pick]: the rows whose logits are wanted (kept within [0, rows)), or NULL for all (n_pick = rows)
+ *   pick          device int32 [n_pick]: the rows whose logits are wanted (kept within [0, rows)), or NULL for all (n_pick = rows); n_pick = 0: none are, as
+ *                 for the chunks of a prompt but its last
  *   logits        device [n_pick, vocab] of the model's type, rows ld apart; zeros for rows that belong to no sequence or lie beyond max_new
  * Queued on the compute stream; the call does not wait.  workspace: device, 16-byte aligned, hift_extend_bytes.  What the pass computes replaces the
  * activations of the last one: scores that hift_score has left are dropped (HIFT_ESTATE from hift_step_scored), nothing else changes.  Models with adapters

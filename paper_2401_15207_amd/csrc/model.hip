@@ -1249,6 +1249,7 @@ hift_status forward(hift_model* M, const hift_batch* bt, int keep_from, const hi
   void* xl = M->xs[c.n_layers];
   if (ex) {
     const hift_extension& e = *ex->of;
+    if (e.n_pick == 0) return HIFT_OK;
     if (e.pick) {
       RW(RW_FIRST_ROWS, 2.0 * e.n_pick * d * es, gather_rows(dt, e.n_pick, e.pick, T, d, xl, M->xs[0], st));
       xl = M->xs[0];
@@ -3062,7 +3063,7 @@ hift_status check_extension(const hift_model* M, const hift_extension* e, Extend
   if (e->cache->dtype != c.dtype || v.kv_heads != c.n_heads || v.head_dim != c.d_model / c.n_heads) return fail(HIFT_EINVAL, "the cache's type and heads are not the model's");
   if (e->rows > M->maxT) return fail(HIFT_EINVAL, "%lld new rows, but the model holds %lld", (long long)e->rows, (long long)M->maxT);
   if (e->max_length < 0 || e->max_length > c.max_seq) return fail(HIFT_EINVAL, "max_length outside the %d positions of the model", c.max_seq);
-  if (e->n_pick < 0 || e->n_pick > M->maxT || (!e->pick && e->n_pick != e->rows)) return fail(HIFT_EINVAL, "n_pick is not the number of rows whose logits are wanted");
+  if (e->n_pick < 0 || e->n_pick > M->maxT || (!e->pick && e->n_pick != 0 && e->n_pick != e->rows)) return fail(HIFT_EINVAL, "n_pick is not the number of rows whose logits are wanted");
   if (e->ld < c.vocab) return fail(HIFT_EINVAL, "rows of the logits are %lld apart and %d long", (long long)e->ld, c.vocab);
   const int64_t es = M->es;
   if (c.n_layers > 1 && (e->layer_stride < 1 || e->layer_stride * es % 16)) return fail(HIFT_EINVAL, "layer_stride must be whole 16-byte pieces");

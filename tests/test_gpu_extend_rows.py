@@ -1,4 +1,4 @@
-"""What hift_extend says of rows that belong to no sequence, and how often it rounds."""
+"""What hift_extend says of rows that belong to no sequence, of chunks without logits, and of how often it rounds."""
 import numpy as np
 import pytest
 import torch
@@ -52,6 +52,21 @@ def test_rows_without_any_sequence(name):
     whole = cache_for(gpu, 2, 32)
     none = H.PagedCache(*whole.all, torch.empty(0, 2, dtype=torch.int32, device="cuda"), torch.empty(0, dtype=torch.int32, device="cuda"))
     assert (gpu.extend(ints(5, 6, 7), ints(0), none, 3, 9) == 0).all()
+
+
+@pytest.mark.parametrize("name", ["C1", "rope"])
+def test_a_chunk_without_logits(name):
+    """All chunks of a prompt but the last: nobody wants their logits."""
+    wl = dict(C1=WORKLOADS["C1"], rope=SMALL2)[name]
+    orc, gpu, _ = make_pair(wl, seed=6, jitter=0.02)
+    tok, _ = make_batch(wl, 6, 1)
+    want = oracle_logits(orc, orc.theta, tok)
+    cache = cache_for(gpu, 1, 32)
+    a, b = (torch.from_numpy(tok[0, i:j].astype(np.int32)).cuda() for i, j in ((0, 9), (9, 14)))
+    assert gpu.extend(a, ints(0, 9), cache, 9, 9, pick=ints()).shape == (0, wl["vocab"])
+    cache.lengths += 9
+    got = gpu.extend(b, ints(0, 5), cache, 5, 14).cpu().numpy()
+    assert np.abs(got - want[0, 9:14]).max() <= 1e-5 * (np.abs(want).max() + 1)
 
 
 def test_keys_are_rounded_once():
