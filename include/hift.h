@@ -649,7 +649,9 @@ hift_status hift_kernel_cache_append(const hift_cache* cache, int64_t rows, cons
  * not finite makes numbers of its block of rows NaN, also of rows before the token.  Sums and statistics are fp32; bf16 caches: unnormalised probabilities are rounded to bf16 for the
  * product with v, as in hift_kernel_attention_fwd.  max_length: at least as many as any sequence has with its new tokens; it sets how the keys are split over
  * workgroups, and a longer sequence only takes longer.  workspace: device, 16-byte aligned, hift_kernel_attention_paged_bytes, NULL where that is 0; free
- * again once the call's work on the stream is done; calls that may run at the same time (two streams, two graphs) need one each.
+ * again once the call's work on the stream is done; calls that may run at the same time (two streams, two graphs) need one each.  A buffer for some max_length and
+ * window also suffices where max_length or max_pages is smaller, and with any window where it was asked for without one (any smaller one otherwise); other
+ * numbers of rows, sequences or heads and another max_new may need more or less, fewer of them more than many too: ask for each shape that a program calls.
  * No sum depends on timing: the same call gives the same bits. */
 hift_status hift_kernel_attention_paged_bytes(const hift_cache* cache, int64_t rows, int32_t max_new, int64_t max_length, int32_t heads, int32_t window, size_t* bytes);
 hift_status hift_kernel_attention_paged(const hift_cache* cache, int64_t rows, const int32_t* starts, int32_t max_new, int64_t max_length, int32_t heads,

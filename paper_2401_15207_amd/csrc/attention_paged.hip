@@ -922,7 +922,7 @@ Plan plan_of(int dt, const CacheView& c, int64_t rows, int heads, int max_new, i
     if (n > 1) {
       p.chunk = (int)(up(up(span, n), 64) * 64);
       p.split = (int)up(span, p.chunk);
-      p.parts = rows * heads * p.split;
+      p.parts = rows * heads * n;  // of which `split` <= n are used: n does not fall where keys get more, whole tiles may leave fewer parts
     }
     // Without parts, sequences of few rows among the others are few_rows' where there may be any (else none is short where the longest is not, as a rule); parts of
     // their keys are spread over the chip with the others' (11 sequences of up to 36 new, 4 / 4 heads bf16, over up to 6713: 72 us with whole keys, 47 so).
