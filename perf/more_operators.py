@@ -162,7 +162,7 @@ def prepare_cache(case, g):
         import paper_2401_15207_amd as H
         s["cache"] = H.PagedCache(s["k"], s["v"], s["pages"], s["lengths"])
         if case["op"] == "attend":
-            n = H.kernel_attention_paged_bytes(s["cache"], rows, case["heads"], s["max_new"], s["max_length"])
+            n = H.kernel_attention_paged_bytes(s["cache"], rows, case["heads"], s["max_new"], s["max_length"], window=case["window"])
             s["workspace"] = torch.empty(max(n, 16), dtype=torch.uint8, device="cuda")
     return s
 
