@@ -23,6 +23,7 @@
 
 #include "common.h"
 #include "kernels.h"
+#include "lds_allowed.h"
 #include "paged_cache.h"
 
 namespace hift {
@@ -954,14 +955,10 @@ Plan plan_of(int dt, const CacheView& c, int64_t rows, int heads, int max_new, i
 }
 size_t plan_bytes(const Plan& p) { return p.runs ? (size_t)((1 + p.entries) * 8 + 15) / 16 * 16 : 0; }
 
-// LDS beyond 64 KB has to be asked for, once an instantiation
 template <auto KERNEL, int LDS>
 hipError_t allow_lds() {
-  static bool done = false;
-  if (LDS <= 65536 || done) return hipSuccess;
-  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(KERNEL), hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
-  done = e == hipSuccess;
-  return e;
+  static LdsAllowed allowed;  // one an instantiation
+  return allowed(reinterpret_cast<const void*>(KERNEL), LDS);
 }
 
 template <typename T, int HD, int NB, bool PAST>

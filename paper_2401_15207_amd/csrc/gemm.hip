@@ -14,6 +14,7 @@
 
 #include "common.h"
 #include "kernels.h"
+#include "lds_allowed.h"
 #include "packed_layout.h"
 
 namespace hift {
@@ -970,12 +971,8 @@ namespace {
 // Launch of a packed-operand kernel with its dynamic LDS size enabled once per kernel.
 template <auto Kern>
 hipError_t launch_pk(dim3 grid, int threads, int lds, hipStream_t st, const GemmP& p, const u32x4* bp) {
-  static bool attr_done = false;
-  if (!attr_done) {
-    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(Kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-    if (e != hipSuccess) return e;
-    attr_done = true;
-  }
+  static LdsAllowed allowed;  // one a kernel
+  if (hipError_t e = allowed(reinterpret_cast<const void*>(Kern), lds)) return e;
   Kern<<<grid, threads, lds, st>>>(p, bp, p.K / 16);
   return hipGetLastError();
 }
@@ -1089,13 +1086,8 @@ hipError_t gemm(const Gemm& g, hipStream_t st) {
       p.tiles_n = (int)(g.N / 256);
       const bool past = g.out_f32 && !g.bias && !g.R && g.M * g.N * 4 >= PAST_CACHES_BYTES;
       const auto kern = past ? gemm_tt_k<float, true> : g.out_f32 ? gemm_tt_k<float, false> : gemm_tt_k<bf16, false>;
-      static bool attr[3] = {false, false, false};
-      bool& done = attr[past ? 2 : g.out_f32];
-      if (!done) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, LDS_TT);
-        if (e != hipSuccess) return e;
-        done = true;
-      }
+      static LdsAllowed allowed[3];
+      if (hipError_t e = allowed[past ? 2 : g.out_f32](reinterpret_cast<const void*>(kern), LDS_TT)) return e;
       kern<<<dim3((unsigned)(p.tiles_m * p.tiles_n)), 256, LDS_TT, st>>>(p);
       return hipGetLastError();
     }

@@ -14,6 +14,7 @@
 
 #include "common.h"
 #include "kernels.h"
+#include "lds_allowed.h"
 
 namespace hift {
 namespace {
@@ -253,14 +254,8 @@ hipError_t launch(F32P& p, int nz, hipStream_t st) {
   constexpr int LDS = BUFS * 2 * BT * (KC + 4) * (int)sizeof(float);
   static_assert(LDS <= 160 * 1024, "LDS of a gfx950 compute unit");
   auto kern = gemm_f32_k<BT, KC, BUFS, AK, BKM, WIDE, T, OutT, EPI>;
-  if (LDS > 64 * 1024) {
-    static bool attr_done = false;  // one flag per instantiation
-    if (!attr_done) {
-      hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
-      if (e != hipSuccess) return e;
-      attr_done = true;
-    }
-  }
+  static LdsAllowed allowed;  // one an instantiation
+  if (hipError_t e = allowed(reinterpret_cast<const void*>(kern), LDS)) return e;
   p.tiles_m = (int)((p.M + BT - 1) / BT);
   const int tiles_n = (int)((p.N + BT - 1) / BT);
   kern<<<dim3((unsigned)(p.tiles_m * tiles_n), (unsigned)nz), 256, LDS, st>>>(p);

@@ -21,6 +21,7 @@
 
 #include "common.h"
 #include "kernels.h"
+#include "lds_allowed.h"
 #include "lds_tiles.h"
 
 namespace hift {
@@ -388,13 +389,9 @@ hipError_t launch(LdsP& p, int nz, hipStream_t st) {
   constexpr int BM = TILE.bm, BN = TILE.bn, RING = TILE.ring;
   constexpr int LDS = Tile<BM, BN, RING>::LDS;
   static_assert(LDS <= 160 * 1024, "LDS of a gfx950 compute unit");
-  static bool attr_done = false;  // one flag per instantiation
   auto kern = gemm_lds_k<BM, BN, RING, AK, BKM, OutT, EPI>;
-  if (!attr_done) {
-    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, LDS);
-    if (e != hipSuccess) return e;
-    attr_done = true;
-  }
+  static LdsAllowed allowed;  // one an instantiation
+  if (hipError_t e = allowed(reinterpret_cast<const void*>(kern), LDS)) return e;
   p.tiles_m = (int)((p.M + BM - 1) / BM);
   p.tiles_n = (int)((p.N + BN - 1) / BN);
   kern<<<dim3((unsigned)(p.tiles_m * p.tiles_n), (unsigned)nz), 64 * Tile<BM, BN, RING>::NW, LDS, st>>>(p);

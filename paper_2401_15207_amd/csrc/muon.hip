@@ -18,6 +18,7 @@
 
 #include "common.h"
 #include "kernels.h"
+#include "lds_allowed.h"
 #include "ns_plan.h"
 
 namespace hift {
@@ -795,13 +796,9 @@ uint32_t spread(NsTable& t, F blocks) {
 template <int SIDE, int MODE, bool DEEP, typename OUT>
 hipError_t launch_product(uint32_t blocks, const NsTable& t, const NsStep& p, hipStream_t st) {
   typedef NsTile<SIDE, DEEP> T;
-  static bool attr_done = false;  // one flag per instantiation
   const auto kern = ns_product_k<SIDE, MODE, DEEP, OUT>;
-  if (!attr_done) {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, T::LDS);
-    if (e != hipSuccess) return e;
-    attr_done = true;
-  }
+  static LdsAllowed allowed;  // one an instantiation
+  if (hipError_t e = allowed(reinterpret_cast<const void*>(kern), T::LDS)) return e;
   kern<<<blocks, 64 * T::NW, T::LDS, st>>>(t, p);
   return hipGetLastError();
 }
