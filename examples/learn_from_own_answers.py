@@ -1,9 +1,10 @@
-"""A decoder that writes answers and learns from them: policy gradient on its own samples, one group of layers a step.
+"""A decoder that writes answers and learns from them: policy gradient from its own samples, one group of layers a step.
 
 Every step the model continues prompts token by token over a paged cache (HiftModel.extend): the logits of each next token pass through the penalties for repeated
 tokens and a mask of allowed ones (kernel_adjust_logits), the most probable alternatives and their log probabilities come from kernel_token_logprob, and one of
-them is drawn.  The answers are then scored in one pass over the whole texts and the HiFT step is taken on the derivatives that their reward gives.  Needs an
-MI355X; prompts and weights are synthetic.
+them is drawn.  The answers are then scored in one pass over the whole texts, at the temperature they were drawn at, and the HiFT step is taken on the derivatives
+that their reward gives.  The gradient is that of the model's own distribution at this temperature: that answers were drawn with a penalty for repeated tokens, from
+allowed ones alone and among the most probable, it leaves out.  Needs an MI355X; prompts and weights are synthetic.
 
     python examples/learn_from_own_answers.py [--workload C1] [--batch 16] [--sweeps 10] [--dtype fp32]
 """
@@ -13,10 +14,10 @@ import sys
 
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 
-TOP, PAGE = 16, 16
+TOP, PAGE, TEMPERATURE = 16, 16, 0.9
 
 
-def answers(H, model, prompts, answer, allowed, temperature=0.9, repetition=1.1):
+def answers(H, model, prompts, answer, allowed, temperature=TEMPERATURE, repetition=1.1):
     """Continues prompts [batch, length] (int32) by `answer` tokens each: the texts [batch, length + answer]."""
     import torch
     batch, length = prompts.shape
@@ -73,7 +74,7 @@ def run(workload="C1", batch=16, sweeps=10, prompt=8, answer=16, dtype="fp32", l
         reward = reward_of(texts, prompt, vocab)
         targets = torch.full_like(texts, -1)
         targets[:, prompt - 1:-1] = texts[:, prompt:]
-        model.score(texts, targets, group)
+        model.score(texts, targets, group, temperature=TEMPERATURE)
         d_logp = torch.zeros(batch, total, device="cuda")
         d_logp[:, prompt - 1:-1] = -(reward - reward.mean()) / reward.numel()
         model.step_scored(texts, targets, group, d_logp, None)
