@@ -599,7 +599,8 @@ hift_status hift_kernel_muon(const hift_opt* opt, int32_t count, const hift_muon
  *   HIFT_ROTARY_LINEAR  rate_i / factor
  *   HIFT_ROTARY_BASE    base factor^(rot / (rot - 2)) instead of base: the slowest pair turns factor times slower, the fastest as before (rot > 2)
  *   HIFT_ROTARY_PARTS   with turns_i = trained rate_i / (2 pi), the turns within `trained` positions: rate_i (k + (1 - k) / factor),
- *                       k = (turns_i - slow) / (fast - slow) kept within [0, 1]: pairs of more than `fast` turns stay, those below `slow` are slowed
+ *                       k = (turns_i - slow) / (fast - slow) kept within [0, 1]: pairs of more than `fast` turns stay, those below `slow` are slowed.  Between the two the
+ *                       share runs with the number of turns; a model trained with a share that runs with the pair's index i between them had other angles there
  * amplitude: what cos and sin are multiplied with (1 usual).  Fields that a scaling does not name are not read.
  * hift_kernel_rotary_table: cos_sin device fp32 [count, rot / 2, 2] = amplitude (cos, sin) of positions first .. first + count - 1, angles formed in
  * 64 bits and rounded once.  rot even, 2 .. 256; base 1 .. 1e18, factor 1 .. 1e9; 0 <= first, first + count <= 2^30. */

@@ -12,10 +12,16 @@
 //            A token each of 64 sequences of up to 8000, 32 / 8 heads of 128 bf16 (1.04 GB): 189 us with its join, 5.5 TB/s (a workgroup a sequence and head 253).
 //   few_whole_k  the same, one workgroup a block of rows and key head, where runs would be too short.  One token over 500, 32 / 32 heads: 8.4 us, the chain
 //            of its loads, products and joins.
-//   mixed_k  128 rows a workgroup, 32 a wavefront, which share tiles of 64 keys; bound by the matrix instructions and the LDS reads that feed them (bf16: 16 KB for
-//            16 instructions of 32 cycles, four wavefronts: 128 bytes a cycle, all that LDS gives).  Its first workgroups take the sequences of few rows.
-//            Chunks of 700 to 1024 of 4 sequences over up to 4096, 32 / 32 heads bf16: 188 to 198 us by the card, 770 to 815 TFLOP/s (a large product 1250); fp32, 1024 over none 152 us.
+//   mixed_k  128 rows a workgroup, 32 a wavefront, which share tiles of 64 keys.  Its first workgroups take the sequences of few rows.
+//            Chunks of 700 to 1024 of 4 sequences over up to 4096, 32 / 32 heads bf16: 188 to 198 us by the card, 770 to 815 TFLOP/s (a large product 1250).  No single unit
+//            bounds them: the matrix pipes are busy 41 % of the time; LDS reads (16 KB a wavefront for 16 instructions of 32 cycles) weigh most and the phases overlap in part
+//            (an earlier state of 231 us: without loads 198, without exponentials 205, without LDS reads 157).  With at most 256 workgroups (1024 over none 30 us, products 7) a
+//            SIMD has one wavefront, which waits out each tile: 1.9 us, products 0.43.  fp32, 1024 over none 152 us of 56: one workgroup a compute unit (131 KB of LDS), the
+//            longest with twice the mean work, products and exponentials one after the other.
 //   join_k   rows whose keys fell to several workgroups: the parts, weighted by their maxima.
+//
+// bf16: exponentials are rounded to bf16 for the product with v, which is what the matrix instruction takes, as in attention.hip; their sum, the maxima and all products' sums are
+// fp32.  Results are off by 0.0021 of their size instead of 0.0016 (one rounding of the result alone); keeping what that rounding leaves would take the product twice.
 #include <math.h>
 
 #include <algorithm>
@@ -581,7 +587,7 @@ __device__ __forceinline__ void many_rows_f32(const Args& p, const int index, un
 
 // ---- many rows, bf16 ----
 // 128 rows a workgroup, 32 a wavefront, two workgroups a compute unit (chunks: 188 us; 256 rows in eight wavefronts the same; 64 rows a wavefront would halve the
-// LDS reads, but need more registers than there are: 663).  Within a wavefront the products of one block of 32 keys run beside the exponentials of
+// LDS reads, but spilled as compiled: 663).  Within a wavefront the products of one block of 32 keys run beside the exponentials of
 // the one before:
 //   scores of block i (8 MFMAs)     in turn with the exponentials of block i - 1 (products first, then exponentials: 4096 over none, 16 / 2 heads 109 us, in turn 99)
 //   P V of block i - 1 (8 MFMAs)    beside the row maxima of block i

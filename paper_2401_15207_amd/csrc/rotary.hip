@@ -1,5 +1,5 @@
 // Rotary positions: the table of angles, the rotation of rows of heads by it, forward and backward, and the rotation of a batch's new
-// queries and keys on their way into a paged cache.
+// queries and keys on their way into a paged cache.  And what else a model's new rows need by their place in such a cache: positions, angles, the wanted logits.
 //
 // Pair i of a head (of the first `rot` columns: (i, i + rot / 2) or (2 i, 2 i + 1)) turns by position * rate_i.  Rotated by (cos, sin) of the table:
 //   y1 = x1 cos - x2 sin, y2 = x2 cos + x1 sin;   the adjoint has -sin for sin.
