@@ -105,8 +105,10 @@ def test_keys_are_rounded_once():
     assert far.max() <= 1.0, f"off by up to {far.max():.2f} of one rounding"
 
 
-def test_packed_weights_against_the_oracle():
-    orc, gpu, _ = make_pair(PACKED, seed=7, jitter=0.02, dtype=1)
+@pytest.mark.parametrize("how", [dict(), dict(master_on_host=1, state_on_host=1), dict(unfused=1)])
+def test_packed_weights_against_the_oracle(how):
+    """With packed copies alone; with row-major ones beside them, which few rows take and the rotation is the cache's; and with the rotation apart."""
+    orc, gpu, _ = make_pair(PACKED, seed=7, jitter=0.02, dtype=1, **how)
     tok, _ = make_batch(PACKED, 7, 1)
     tok = tok[:3]
     want = oracle_logits(orc, O.bf16_round(orc.theta), tok)
